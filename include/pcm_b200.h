@@ -365,6 +365,57 @@ int grpo_adamw_step_lora(const grpo_model_cfg* cfg, const grpo_adamw_cfg* opt, i
                          grpo_grads* m, grpo_grads* v, float* grad_norm, void* scratch, size_t scratch_bytes,
                          pcm_stream stream);
 
+/* ---- the ends of a wider vocabulary -----------------------------------------------------------------
+ * The actor update above scores 256 action bins with the loss inside its head GEMM.  A policy on a language backbone
+ * embeds instruction tokens and scores its action tokens over the backbone's whole vocabulary; these calls are the two
+ * ends of such a policy.  They need no context.  Conventions of this section:
+ *   - tok is device int32, contiguous.  A token below 0 marks a padded row: its values are 0 (top_id -1), it has no
+ *     gradient and what it would read is not read.  A token >= vocab is treated the same and sets bit 5 (value 32) of
+ *     device_status.
+ *   - device_status (device [1], may be NULL) is only ever OR-ed into: clear it before the first call, read it when
+ *     the stream has got there.  Bit 0: a bounded wait in a tensor-core kernel expired.
+ *   - Row strides ld* are in elements; a row is contiguous.  Rows may start anywhere their type allows unless a call
+ *     says otherwise; 16-byte accesses are used where rows are aligned for them.
+ *   - No call allocates or synchronises; all can be captured in a CUDA graph.  A workspace is scratch of one call:
+ *     calls that may run at the same time need one each.  n = 0 rows is a valid call.
+ *   - Results do not depend on launch order: there are no floating-point atomics. */
+#define PCM_MAX_TOP 16
+#define PCM_MAX_EMBED_DIM 65536
+
+/* out[i] = round(scale * table[tok[i]]) for i < n: table [vocab][d], out [n][d], both of `dtype` (a grpo_dtype).
+ * The product is formed in fp32 and rounded once; scale = 1 copies bits. */
+int grpo_embed(int32_t dtype, const void* table, int64_t ld_table, int32_t vocab, int32_t d, const int32_t* tok, int32_t n,
+               float scale, void* out, int64_t ld_out, uint32_t* device_status, pcm_stream stream);
+
+/* Its gradient: grad[v] = scale * sum over {i : tok[i] = v} of dout[i] in fp32 for every v < vocab (0 for tokens that
+ * do not occur); with GRPO_ACCUMULATE in flags it is added to grad.  dout [n][d] of `dtype`, grad [vocab][d] fp32,
+ * contiguous.  Tokens are sorted first; the rows of a token are summed in ascending i within tiles of 16 or 64 sorted
+ * rows, the tiles in order.  d <= PCM_MAX_EMBED_DIM.  workspace: device, 256-byte aligned,
+ * >= grpo_embed_workspace_bytes() (0 when the sizes are not supported). */
+size_t grpo_embed_workspace_bytes(int32_t n, int32_t vocab, int32_t d);
+int grpo_embed_bwd(int32_t dtype, const void* dout, int64_t ld_dout, const int32_t* tok, int32_t n, int32_t vocab, int32_t d,
+                   float scale, uint32_t flags, float* grad, uint32_t* device_status, void* workspace, size_t workspace_bytes,
+                   pcm_stream stream);
+
+/* Log-probabilities of given tokens from logits [n_rows][vocab] of `dtype`, z = logits / temperature:
+ *     lse = log sum_v exp z_v,  logp = z_tok - lse,  entropy = -sum_v p_v log p_v  (p = softmax(z), in nats)
+ * and the `top` (0 .. PCM_MAX_TOP, <= vocab) largest logits of each row, largest first, equal ones by ascending index:
+ * top_id [n_rows][top] and their log-probabilities top_logp [n_rows][top].  All sums in fp32.
+ * Logits of -inf (a masked vocabulary) have p = 0; a row of nothing but -inf has lse = logp = top_logp = -inf and
+ * entropy 0.  With a NaN or +inf in a row, its lse, logp, entropy and top_logp are NaN; top_id orders a NaN above +inf.
+ * tok may be NULL when logp is (every row counts then); logp, entropy, lse may each be NULL. */
+int grpo_token_logp(int32_t dtype, const void* logits, int64_t ld, int32_t n_rows, int32_t vocab, const int32_t* tok,
+                    float temperature, int32_t top, float* logp, float* entropy, float* lse, int32_t* top_id, float* top_logp,
+                    uint32_t* device_status, pcm_stream stream);
+
+/* Gradient of a loss with d loss / d logp = dlogp [n_rows] and d loss / d entropy = dentropy [n_rows] (may be NULL):
+ *     dlogits_v = (1 / temperature) (dlogp (1[v = tok] - p_v) - dentropy p_v (log p_v + entropy))
+ * lse and entropy (needed with dentropy) are those of the forward call.  dlogits is of `dtype`, with its own row
+ * stride; it may be the logits themselves (same pointer, same stride).  A row whose lse is -inf gets zeros. */
+int grpo_token_logp_bwd(int32_t dtype, const void* logits, int64_t ld, int32_t n_rows, int32_t vocab, const int32_t* tok,
+                        float temperature, const float* lse, const float* entropy, const float* dlogp, const float* dentropy,
+                        void* dlogits, int64_t ld_dlogits, uint32_t* device_status, pcm_stream stream);
+
 /* ---- diagnostic entry points (per-kernel tests and measurements; not part of Algorithm 1) -------
  * grpo_gemm: C[m][n] = sum_k A(m,k) B(n,k) (+ R[m][n]) with the GEMM kernels the actor update uses.
  * a_kmajor != 0: A is stored [M][K] with row stride lda, else [K][M]; likewise B ([N][K] / [K][N]).

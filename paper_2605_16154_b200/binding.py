@@ -144,6 +144,13 @@ _lib.grpo_adamw_step_lora.argtypes = [C.POINTER(grpo_model_cfg), C.POINTER(grpo_
                                       C.POINTER(grpo_grads), C.POINTER(grpo_grads), C.POINTER(grpo_grads), C.c_void_p,
                                       C.c_void_p, C.c_size_t, C.c_void_p]
 _lib.grpo_adamw_step_lora.restype = C.c_int
+_I, _L, _F = C.c_int32, C.c_int64, C.c_float
+_lib.grpo_embed.argtypes = [_I, _P, _L, _I, _I, _P, _I, _F, _P, _L, _P, _P]
+_lib.grpo_embed_workspace_bytes.argtypes = [_I, _I, _I]
+_lib.grpo_embed_workspace_bytes.restype = C.c_size_t
+_lib.grpo_embed_bwd.argtypes = [_I, _P, _L, _P, _I, _I, _I, _F, C.c_uint32, _P, _P, _P, C.c_size_t, _P]
+_lib.grpo_token_logp.argtypes = [_I, _P, _L, _I, _I, _P, _F, _I, _P, _P, _P, _P, _P, _P, _P]
+_lib.grpo_token_logp_bwd.argtypes = [_I, _P, _L, _I, _I, _P, _F, _P, _P, _P, _P, _P, _L, _P, _P]
 _lib.pcm_launch_count.restype = C.c_int64
 _lib.pcm_first_use_on_device.argtypes = [C.POINTER(C.c_uint64), C.c_int32]
 _lib.pcm_first_use_on_device.restype = C.c_int32
@@ -151,7 +158,8 @@ _lib.pcm_profile_enable.argtypes = [C.c_int32]
 _lib.pcm_profile_read.argtypes = [C.POINTER(pcm_profile)]
 for _name in ("pcm_create", "pcm_destroy", "pcm_poll_status", "pcm_state_export", "pcm_state_import",
               "pcm_score_phases", "pcm_update_keep_probs", "pcm_sample_chunks", "grpo_pack_chunks",
-              "grpo_actor_fwd_bwd", "grpo_gemm", "grpo_attention", "pcm_profile_enable", "pcm_profile_read"):
+              "grpo_actor_fwd_bwd", "grpo_gemm", "grpo_attention", "pcm_profile_enable", "pcm_profile_read",
+              "grpo_embed", "grpo_embed_bwd", "grpo_token_logp", "grpo_token_logp_bwd"):
     getattr(_lib, _name).restype = C.c_int
 
 EXPORTED = ("pcm_create", "pcm_destroy", "pcm_poll_status", "pcm_state_export", "pcm_state_import",
@@ -160,7 +168,8 @@ EXPORTED = ("pcm_create", "pcm_destroy", "pcm_poll_status", "pcm_state_export", 
             "pcm_profile_enable", "pcm_profile_read", "pcm_score_phases_static",
             "grpo_adamw_scratch_bytes", "grpo_adamw_step", "grpo_adamw_step_lora", "pcm_label_phases", "pcm_score_phases_f32",
             "grpo_attention_wait_status", "pcm_first_use_on_device", "grpo_lora_workspace_bytes",
-            "grpo_actor_fwd_bwd_lora")
+            "grpo_actor_fwd_bwd_lora", "grpo_embed", "grpo_embed_workspace_bytes", "grpo_embed_bwd", "grpo_token_logp",
+            "grpo_token_logp_bwd")
 
 
 def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
@@ -433,6 +442,157 @@ def grpo_actor_fwd_bwd(model: Model, packed: Packed, eps_low: float = 0.2, eps_h
                                           C.byref(stats) if stats is not None else None, ws_ptr, ws_bytes, _stream())
     _check("grpo_actor_fwd_bwd", rc)
     return loss, logp, grads, stats
+
+
+# ------------------------------------------------------------------------------------------------
+# The ends of a wider vocabulary.  These wrappers launch on the current stream of the tensors' own device and refuse
+# (PcmError) what the C calls would misread: mixed devices, other types, rows that are not contiguous.
+_DTYPES = {torch.float32: GRPO_F32, torch.bfloat16: GRPO_BF16}
+PCM_MAX_TOP = 16
+STATUS_BAD_TOKEN = 32
+
+
+def _require(call: str, ok: bool, code: int = -1) -> None:
+    if not ok:
+        raise PcmError(call, code)
+
+
+def _matrix(call: str, t: torch.Tensor, device=None):
+    """(dtype code, address, row stride) of a device matrix with contiguous rows."""
+    _require(call, isinstance(t, torch.Tensor) and t.is_cuda and t.dim() == 2 and t.dtype in _DTYPES and
+             (device is None or t.device == device))
+    n, c = t.shape
+    ld = t.stride(0)
+    if n <= 1 or c == 0:                                       # the stride of a single row says nothing
+        ld = max(c, ld if n == 1 else 0)
+    _require(call, c <= 1 or t.stride(1) == 1 or n == 0)
+    _require(call, ld >= c)                                    # rows that overlap (an expanded view)
+    return _DTYPES[t.dtype], t.data_ptr(), ld
+
+
+def _vector(call: str, t: Optional[torch.Tensor], device, dtype, n: int) -> Optional[int]:
+    if t is None:
+        return None
+    _require(call, isinstance(t, torch.Tensor) and t.device == device and t.dtype == dtype and t.numel() == n and
+             t.is_contiguous())
+    return t.data_ptr()
+
+
+class _on:
+    """Makes a tensor's device current for one call; yields that device's current stream."""
+
+    def __init__(self, device):
+        self.device = device
+
+    def __enter__(self):
+        self.before = torch.cuda.current_device()
+        if self.before != self.device.index:
+            torch.cuda.set_device(self.device)
+        return torch.cuda.current_stream(self.device).cuda_stream
+
+    def __exit__(self, *exc):
+        if self.before != self.device.index:
+            torch.cuda.set_device(self.before)
+
+
+def _workspace(call: str, workspace: Optional[torch.Tensor], need: int, device):
+    """256-byte aligned scratch: the caller's, or a new allocation of at least `need` bytes."""
+    if workspace is None:
+        workspace = torch.empty(need + 256, dtype=torch.uint8, device=device)
+    _require(call, workspace.device == device and workspace.dtype == torch.uint8 and workspace.is_contiguous(), -3)
+    off = (-workspace.data_ptr()) % 256
+    return workspace, workspace.data_ptr() + off, max(0, workspace.numel() - off)
+
+
+def grpo_embed(table: torch.Tensor, tok: torch.Tensor, scale: float = 1.0, out: Optional[torch.Tensor] = None,
+               status: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Rows scale * table[tok] as [n, d] in the table's type; zero rows for tokens outside the vocabulary."""
+    call = "grpo_embed"
+    dt, tp, ld = _matrix(call, table)
+    dev = table.device
+    n, (vocab, d) = tok.numel(), table.shape
+    tk = _vector(call, tok, dev, torch.int32, n)
+    if out is None:
+        out = torch.empty((n, d), dtype=table.dtype, device=dev)
+    odt, op, ldo = _matrix(call, out, dev)
+    _require(call, odt == dt and out.shape == (n, d))
+    with _on(dev) as stream:
+        _check(call, _lib.grpo_embed(dt, tp, ld, vocab, d, tk, n, scale, op, ldo,
+                                     _vector(call, status, dev, torch.int32, 1), stream))
+    return out
+
+
+def grpo_embed_workspace_bytes(n: int, vocab: int, d: int) -> int:
+    return int(_lib.grpo_embed_workspace_bytes(n, vocab, d))
+
+
+def grpo_embed_bwd(dout: torch.Tensor, tok: torch.Tensor, vocab: int, scale: float = 1.0,
+                   grad: Optional[torch.Tensor] = None, accumulate: bool = False,
+                   workspace: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """fp32 gradient [vocab, d] of grpo_embed's table; with `accumulate` it is added to the given `grad`."""
+    call = "grpo_embed_bwd"
+    dt, dp, ld = _matrix(call, dout)
+    dev = dout.device
+    n, d = dout.shape
+    tk = _vector(call, tok, dev, torch.int32, n)
+    _require(call, grad is not None or not accumulate)
+    need = grpo_embed_workspace_bytes(n, vocab, d)
+    _require("grpo_embed_workspace_bytes", need > 0, -2)
+    if grad is None:
+        grad = torch.empty((vocab, d), dtype=torch.float32, device=dev)
+    gp = _vector(call, grad, dev, torch.float32, vocab * d)
+    ws, wp, wn = _workspace(call, workspace, need, dev)
+    with _on(dev) as stream:
+        _check(call, _lib.grpo_embed_bwd(dt, dp, ld, tk, n, vocab, d, scale, GRPO_ACCUMULATE if accumulate else 0, gp,
+                                         _vector(call, status, dev, torch.int32, 1), wp, wn, stream))
+    return grad
+
+
+def grpo_token_logp(logits: torch.Tensor, tok: Optional[torch.Tensor], temperature: float = 1.0, top: int = 0,
+                    out: Optional[Dict[str, torch.Tensor]] = None, status: Optional[torch.Tensor] = None):
+    """(logp, entropy, lse, top_id, top_logp) of logits [n, vocab] for the tokens tok [n]; the last two are None with
+    top = 0, logp is None without tokens.  `out` may hold tensors to write instead (same names)."""
+    call = "grpo_token_logp"
+    dt, zp, ld = _matrix(call, logits)
+    dev = logits.device
+    n, vocab = logits.shape
+    out = out or {}
+
+    def take(name, shape, dtype):
+        t = out.get(name)
+        return torch.empty(shape, dtype=dtype, device=dev) if t is None else t
+    f32, i32 = torch.float32, torch.int32
+    logp = take("logp", n, f32) if tok is not None else None
+    entropy, lse = take("entropy", n, f32), take("lse", n, f32)
+    top_id, top_logp = (take("top_id", (n, top), i32), take("top_logp", (n, top), f32)) if top > 0 else (None, None)
+    with _on(dev) as stream:
+        _check(call, _lib.grpo_token_logp(dt, zp, ld, n, vocab, _vector(call, tok, dev, i32, n), temperature, top,
+                                          _vector(call, logp, dev, f32, n), _vector(call, entropy, dev, f32, n),
+                                          _vector(call, lse, dev, f32, n), _vector(call, top_id, dev, i32, n * top),
+                                          _vector(call, top_logp, dev, f32, n * top),
+                                          _vector(call, status, dev, i32, 1), stream))
+    return logp, entropy, lse, top_id, top_logp
+
+
+def grpo_token_logp_bwd(logits: torch.Tensor, tok: torch.Tensor, lse: torch.Tensor, entropy: Optional[torch.Tensor],
+                        dlogp: torch.Tensor, dentropy: Optional[torch.Tensor] = None, temperature: float = 1.0,
+                        dlogits: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """d loss / d logits in the logits' type; `dlogits` may be the logits themselves."""
+    call = "grpo_token_logp_bwd"
+    dt, zp, ld = _matrix(call, logits)
+    dev = logits.device
+    n, vocab = logits.shape
+    if dlogits is None:
+        dlogits = torch.empty((n, vocab), dtype=logits.dtype, device=dev)
+    ddt, dp, ldd = _matrix(call, dlogits, dev)
+    _require(call, ddt == dt and dlogits.shape == logits.shape and tok is not None and lse is not None and dlogp is not None)
+    f32 = torch.float32
+    with _on(dev) as stream:
+        _check(call, _lib.grpo_token_logp_bwd(dt, zp, ld, n, vocab, _vector(call, tok, dev, torch.int32, n), temperature,
+                                              _vector(call, lse, dev, f32, n), _vector(call, entropy, dev, f32, n),
+                                              _vector(call, dlogp, dev, f32, n), _vector(call, dentropy, dev, f32, n), dp,
+                                              ldd, _vector(call, status, dev, torch.int32, 1), stream))
+    return dlogits
 
 
 # ------------------------------------------------------------------------------------------------

@@ -17,6 +17,7 @@ constexpr unsigned STATUS_BAD_PHASE = 2u;     // phase label >= n_phases
 constexpr unsigned STATUS_TOO_LONG = 4u;      // trajectory longer than max_len
 constexpr unsigned STATUS_BAD_OFFSETS = 8u;   // traj_off / kept_idx inconsistent with host sizes
 constexpr unsigned STATUS_BAD_ACTION = 16u;   // continuous action not finite or beyond the fixed-point range
+constexpr unsigned STATUS_BAD_TOKEN = 32u;     // token id >= vocab
 
 #define PCM_CUDA_TRY(expr)                         \
   do {                                             \

@@ -416,6 +416,30 @@ int grpo_token_logp_bwd(int32_t dtype, const void* logits, int64_t ld, int32_t n
                         float temperature, const float* lse, const float* entropy, const float* dlogp, const float* dentropy,
                         void* dlogits, int64_t ld_dlogits, uint32_t* device_status, pcm_stream stream);
 
+/* The same log-probabilities straight from the last hidden states x [n_rows][d] and the head's weight w_h [vocab][d]
+ * (both bf16): z = x w_h^T / temperature is never stored, its fp32 accumulator tiles are reduced where they are.
+ * x and w_h 16-byte aligned, d and both row strides multiples of 8 (PCM_ERR_SHAPE otherwise).  For top alternatives, and
+ * for fp32 policies, form the logits with grpo_gemm and use grpo_token_logp.  logp, entropy, lse may each be NULL.
+ * workspace: device, 256-byte aligned, >= grpo_head_logp_workspace_bytes() (0 when the sizes are not supported): 16
+ * bytes for each row and 128 tokens. */
+size_t grpo_head_logp_workspace_bytes(int32_t n_rows, int32_t d, int32_t vocab);
+int grpo_head_logp(const void* x, int64_t ld_x, int32_t n_rows, int32_t d, const void* w_h, int64_t ld_w, int32_t vocab,
+                   const int32_t* tok, float temperature, float* logp, float* entropy, float* lse, uint32_t* device_status,
+                   void* workspace, size_t workspace_bytes, pcm_stream stream);
+
+/* Its gradients, with dlogits as in grpo_token_logp_bwd (formed in fp32 from a second x w_h^T):
+ *     dx = dlogits w_h  (bf16 [n_rows][d], row stride ld_dx, from dlogits rounded to bf16)
+ *     dw = dlogits^T x  (fp32 [vocab][d], contiguous, 16-byte aligned; GRPO_ACCUMULATE in flags adds to it), from dlogits
+ *                       as a sum of two bf16 values
+ * Either may be NULL.  x may hold anything, NaN too, in rows without a token.  The rows are processed chunk_rows (>= 1) at
+ * a time, which sizes the workspace (2 d + 4 vocab bytes a row and a constant); the results differ between chunk sizes
+ * by fp32 rounding only.  For a tied embedding pass its fp32 gradient as dw with GRPO_ACCUMULATE. */
+size_t grpo_head_logp_bwd_workspace_bytes(int32_t n_rows, int32_t d, int32_t vocab, int32_t chunk_rows);
+int grpo_head_logp_bwd(const void* x, int64_t ld_x, int32_t n_rows, int32_t d, const void* w_h, int64_t ld_w, int32_t vocab,
+                       const int32_t* tok, float temperature, const float* lse, const float* entropy, const float* dlogp,
+                       const float* dentropy, int32_t chunk_rows, uint32_t flags, void* dx, int64_t ld_dx, float* dw,
+                       uint32_t* device_status, void* workspace, size_t workspace_bytes, pcm_stream stream);
+
 /* ---- diagnostic entry points (per-kernel tests and measurements; not part of Algorithm 1) -------
  * grpo_gemm: C[m][n] = sum_k A(m,k) B(n,k) (+ R[m][n]) with the GEMM kernels the actor update uses.
  * a_kmajor != 0: A is stored [M][K] with row stride lda, else [K][M]; likewise B ([N][K] / [K][N]).

@@ -151,6 +151,13 @@ _lib.grpo_embed_workspace_bytes.restype = C.c_size_t
 _lib.grpo_embed_bwd.argtypes = [_I, _P, _L, _P, _I, _I, _I, _F, C.c_uint32, _P, _P, _P, C.c_size_t, _P]
 _lib.grpo_token_logp.argtypes = [_I, _P, _L, _I, _I, _P, _F, _I, _P, _P, _P, _P, _P, _P, _P]
 _lib.grpo_token_logp_bwd.argtypes = [_I, _P, _L, _I, _I, _P, _F, _P, _P, _P, _P, _P, _L, _P, _P]
+_lib.grpo_head_logp_workspace_bytes.argtypes = [_I, _I, _I]
+_lib.grpo_head_logp_workspace_bytes.restype = C.c_size_t
+_lib.grpo_head_logp.argtypes = [_P, _L, _I, _I, _P, _L, _I, _P, _F, _P, _P, _P, _P, _P, C.c_size_t, _P]
+_lib.grpo_head_logp_bwd_workspace_bytes.argtypes = [_I, _I, _I, _I]
+_lib.grpo_head_logp_bwd_workspace_bytes.restype = C.c_size_t
+_lib.grpo_head_logp_bwd.argtypes = [_P, _L, _I, _I, _P, _L, _I, _P, _F, _P, _P, _P, _P, _I, C.c_uint32, _P, _L, _P, _P, _P,
+                                    C.c_size_t, _P]
 _lib.pcm_launch_count.restype = C.c_int64
 _lib.pcm_first_use_on_device.argtypes = [C.POINTER(C.c_uint64), C.c_int32]
 _lib.pcm_first_use_on_device.restype = C.c_int32
@@ -159,7 +166,8 @@ _lib.pcm_profile_read.argtypes = [C.POINTER(pcm_profile)]
 for _name in ("pcm_create", "pcm_destroy", "pcm_poll_status", "pcm_state_export", "pcm_state_import",
               "pcm_score_phases", "pcm_update_keep_probs", "pcm_sample_chunks", "grpo_pack_chunks",
               "grpo_actor_fwd_bwd", "grpo_gemm", "grpo_attention", "pcm_profile_enable", "pcm_profile_read",
-              "grpo_embed", "grpo_embed_bwd", "grpo_token_logp", "grpo_token_logp_bwd"):
+              "grpo_embed", "grpo_embed_bwd", "grpo_token_logp", "grpo_token_logp_bwd", "grpo_head_logp",
+              "grpo_head_logp_bwd"):
     getattr(_lib, _name).restype = C.c_int
 
 EXPORTED = ("pcm_create", "pcm_destroy", "pcm_poll_status", "pcm_state_export", "pcm_state_import",
@@ -169,7 +177,8 @@ EXPORTED = ("pcm_create", "pcm_destroy", "pcm_poll_status", "pcm_state_export", 
             "grpo_adamw_scratch_bytes", "grpo_adamw_step", "grpo_adamw_step_lora", "pcm_label_phases", "pcm_score_phases_f32",
             "grpo_attention_wait_status", "pcm_first_use_on_device", "grpo_lora_workspace_bytes",
             "grpo_actor_fwd_bwd_lora", "grpo_embed", "grpo_embed_workspace_bytes", "grpo_embed_bwd", "grpo_token_logp",
-            "grpo_token_logp_bwd")
+            "grpo_token_logp_bwd", "grpo_head_logp_workspace_bytes", "grpo_head_logp", "grpo_head_logp_bwd_workspace_bytes",
+            "grpo_head_logp_bwd")
 
 
 def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
@@ -593,6 +602,77 @@ def grpo_token_logp_bwd(logits: torch.Tensor, tok: torch.Tensor, lse: torch.Tens
                                               _vector(call, dlogp, dev, f32, n), _vector(call, dentropy, dev, f32, n), dp,
                                               ldd, _vector(call, status, dev, torch.int32, 1), stream))
     return dlogits
+
+
+def grpo_head_logp_workspace_bytes(n: int, d: int, vocab: int) -> int:
+    return int(_lib.grpo_head_logp_workspace_bytes(n, d, vocab))
+
+
+def grpo_head_logp(x: torch.Tensor, w_h: torch.Tensor, tok: torch.Tensor, temperature: float = 1.0,
+                   workspace: Optional[torch.Tensor] = None, out: Optional[Dict[str, torch.Tensor]] = None,
+                   status: Optional[torch.Tensor] = None):
+    """(logp, entropy, lse) of the tokens tok [n] under softmax(x w_h^T / temperature): x [n, d], w_h [vocab, d], bf16."""
+    call = "grpo_head_logp"
+    dt, xp, ldx = _matrix(call, x)
+    dev = x.device
+    wdt, wp, ldw = _matrix(call, w_h, dev)
+    (n, d), (vocab, dw_) = x.shape, w_h.shape
+    _require(call, dt == wdt == GRPO_BF16 and d == dw_ and tok is not None)
+    need = grpo_head_logp_workspace_bytes(n, d, vocab)
+    _require("grpo_head_logp_workspace_bytes", need > 0, -2)
+    ws, wsp, wsn = _workspace(call, workspace, need, dev)
+    out = out or {}
+    f32 = torch.float32
+    logp, entropy, lse = (out[k] if k in out else torch.empty(n, dtype=f32, device=dev) for k in ("logp", "entropy", "lse"))
+    with _on(dev) as stream:
+        _check(call, _lib.grpo_head_logp(xp, ldx, n, d, wp, ldw, vocab, _vector(call, tok, dev, torch.int32, n), temperature,
+                                         _vector(call, logp, dev, f32, n), _vector(call, entropy, dev, f32, n),
+                                         _vector(call, lse, dev, f32, n), _vector(call, status, dev, torch.int32, 1), wsp, wsn,
+                                         stream))
+    return logp, entropy, lse
+
+
+HEAD_CHUNK_BYTES = 4 << 30
+
+
+def grpo_head_logp_bwd_workspace_bytes(n: int, d: int, vocab: int, chunk_rows: int) -> int:
+    return int(_lib.grpo_head_logp_bwd_workspace_bytes(n, d, vocab, chunk_rows))
+
+
+def grpo_head_logp_bwd(x: torch.Tensor, w_h: torch.Tensor, tok: torch.Tensor, lse: torch.Tensor, entropy: Optional[torch.Tensor],
+                       dlogp: torch.Tensor, dentropy: Optional[torch.Tensor] = None, temperature: float = 1.0,
+                       dx: Optional[torch.Tensor] = None, dw: Optional[torch.Tensor] = None, accumulate: bool = False,
+                       want_dx: bool = True, want_dw: bool = True, chunk_rows: int = 0,
+                       workspace: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None):
+    """(dx bf16 [n, d], dw fp32 [vocab, d]) of a loss with the given gradients by logp and entropy; with `accumulate` dw is
+    added to.  chunk_rows = 0 takes as many rows at a time as HEAD_CHUNK_BYTES of logit gradients hold."""
+    call = "grpo_head_logp_bwd"
+    dt, xp, ldx = _matrix(call, x)
+    dev = x.device
+    wdt, wp, ldw = _matrix(call, w_h, dev)
+    (n, d), (vocab, dw_) = x.shape, w_h.shape
+    _require(call, dt == wdt == GRPO_BF16 and d == dw_ and tok is not None and lse is not None and dlogp is not None)
+    _require(call, chunk_rows >= 0 and (dw is not None or not accumulate))
+    if chunk_rows == 0:
+        chunk_rows = max(256, HEAD_CHUNK_BYTES // (4 * vocab) // 256 * 256)
+    need = grpo_head_logp_bwd_workspace_bytes(n, d, vocab, chunk_rows)
+    _require("grpo_head_logp_bwd_workspace_bytes", need > 0, -2)
+    ws, wsp, wsn = _workspace(call, workspace, need, dev)
+    if dx is None and want_dx:
+        dx = torch.empty((n, d), dtype=x.dtype, device=dev)
+    if dw is None and want_dw:
+        dw = torch.empty((vocab, d), dtype=torch.float32, device=dev)
+    f32 = torch.float32
+    ddt, dxp, lddx = _matrix(call, dx, dev) if dx is not None else (GRPO_BF16, None, d)
+    _require(call, ddt == GRPO_BF16 and (dx is None or dx.shape == x.shape))
+    with _on(dev) as stream:
+        _check(call, _lib.grpo_head_logp_bwd(xp, ldx, n, d, wp, ldw, vocab, _vector(call, tok, dev, torch.int32, n), temperature,
+                                             _vector(call, lse, dev, f32, n), _vector(call, entropy, dev, f32, n),
+                                             _vector(call, dlogp, dev, f32, n), _vector(call, dentropy, dev, f32, n), chunk_rows,
+                                             GRPO_ACCUMULATE if accumulate else 0, dxp, lddx,
+                                             _vector(call, dw, dev, f32, vocab * d), _vector(call, status, dev, torch.int32, 1),
+                                             wsp, wsn, stream))
+    return dx, dw
 
 
 # ------------------------------------------------------------------------------------------------

@@ -57,6 +57,9 @@ struct TcParams {
   int kb_total;                               // all k-blocks of the contraction (first pair + continuation)
   int ext_ksteps;                             // MMAs of 16 k-columns in a k-block of the continuation (K2 / 16)
   float alpha;                                // scale of the product in the plain store epilogue
+  VocabHeadArgs vh;                           // EPI_VOCAB_STATS, EPI_VOCAB_DZ
+  int chain_kb, accumulate;                   // EPI_CHAIN
+  long long part_stride;
 };
 
 __device__ __forceinline__ void store_bf16x32(__nv_bfloat16* dst, const float (&v)[32]) {
@@ -327,6 +330,87 @@ __device__ __forceinline__ void epi_tile(const TcParams& p, uint32_t tmem_acc, i
             staged_store_bf16(stage, lane_, v, dz, p.ldc, row - lane_, p.M, n0 + c0);
           }
         }
+      } else if constexpr (EPI == EPI_VOCAB_STATS) {
+        // A thread owns one row of 128 columns: softmax statistics with a running maximum, 32 columns at a time, so
+        // tensor memory is read once.  Parts are stored column-block-major: a warp's 32 rows are 512 contiguous bytes.
+        const int first = n0 + chalf * (BN / 2);
+        static_assert(BN == 256, "a part covers 128 columns");
+        if (first >= p.N) return;
+        const float c = p.vh.inv_t * VOCAB_LOG2E;
+        const int t = row < p.M ? p.vh.tok[row] : -1;
+        VocabStat st{-INFINITY, 0.f, 0.f};
+        float zt = 0.f;
+#pragma unroll 1
+        for (int c0 = 0; c0 < BN / 2; c0 += 32) {
+          const int col = first + c0;
+          if (col >= p.N) break;
+          uint32_t r[32];
+          tmem_ld_32x32(tmem_acc + (uint32_t)(chalf * (BN / 2) + c0), r);
+          tmem_ld_wait();
+          if (p.N - col < 32) {                 // columns behind the vocabulary: zero fill, not logits
+#pragma unroll
+            for (int e = 0; e < 32; ++e)
+              if (e >= p.N - col) r[e] = 0xFF800000u;
+          }
+          float bm = __uint_as_float(r[0]);
+#pragma unroll
+          for (int e = 1; e < 32; ++e) bm = max_nan(bm, __uint_as_float(r[e]));
+          stat_raise(st, bm, c);
+          if (__any_sync(0xffffffffu, (unsigned)(t - col) < 32u)) {
+#pragma unroll
+            for (int e = 0; e < 32; ++e) zt = t - col == e ? __uint_as_float(r[e]) : zt;
+          }
+          if (st.m != -INFINITY) {
+#pragma unroll
+            for (int e = 0; e < 32; ++e) {
+              const float x2 = fmaxf((__uint_as_float(r[e]) - st.m) * c, -1000.f);
+              const float x = ex2(x2);
+              st.s += x;
+              st.w += x * x2;
+            }
+          }
+        }
+        if (row < p.M) p.vh.part[(long long)(first / 128) * p.M + row] = make_float4(st.m, st.s, st.w, zt);
+      } else if constexpr (EPI == EPI_VOCAB_DZ) {
+        // d loss / d z in fp32 from the accumulator, then bf16 twice: the rounded value and what the rounding left, so
+        // that the weight gradient (fp32) does not carry a bf16 rounding of every term.
+        const bool in = row < p.M;
+        const int t = in ? p.vh.tok[row] : -1;
+        const float lse = in ? p.vh.lse[row] : 0.f;
+        const bool live = t >= 0 && t < p.vh.vocab && lse != -INFINITY;
+        const float H = live && p.vh.dent ? p.vh.entropy[row] : 0.f;
+        const float gt = live ? p.vh.dlogp[row] * p.vh.inv_t : 0.f, ht = live && p.vh.dent ? p.vh.dent[row] * p.vh.inv_t : 0.f;
+        __nv_bfloat16* hi = reinterpret_cast<__nv_bfloat16*>(p.C);
+        __nv_bfloat16* lo = reinterpret_cast<__nv_bfloat16*>(p.vh.dz_lo);
+#pragma unroll 1
+        for (int c0 = chalf * (BN / 2); c0 < (chalf + 1) * (BN / 2); c0 += 32) {
+          const int col = n0 + c0;
+          if (col >= p.N) break;
+          uint32_t r[32];
+          tmem_ld_32x32(tmem_acc + (uint32_t)c0, r);
+          tmem_ld_wait();
+#pragma unroll
+          for (int e = 0; e < 32; ++e)
+            r[e] = live ? __float_as_uint(vocab_slope(__uint_as_float(r[e]), p.vh.inv_t, lse, H, gt, ht, t - col == e)) : 0u;
+          stage_put_rows(stage, lane_, r);
+          __syncwarp();
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            float v[8], h[8];
+            stage_get8(stage, lane_, i, v);
+            const int gr = row - lane_ + i * 8 + (lane_ >> 2);
+            const long long at = (long long)gr * p.ldc + col + (lane_ & 3) * 8;
+            const uint4 ph = pack8_bf16(v);
+            unpack8_bf16(ph, h);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) h[e] = v[e] - h[e];
+            if (gr < p.M) {
+              *reinterpret_cast<uint4*>(hi + at) = ph;
+              *reinterpret_cast<uint4*>(lo + at) = pack8_bf16(h);
+            }
+          }
+          __syncwarp();
+        }
       } else if constexpr (EPI == EPI_SWIGLU_FWD) {
         // accumulator columns [0,128) = gate, [128,256) = up, for hidden units hid0 .. hid0+127
         const int hid0 = n0 / 2, F = p.up_row0;
@@ -522,6 +606,59 @@ __device__ __forceinline__ void epi_tile(const TcParams& p, uint32_t tmem_acc, i
       }
 }
 
+// EPI_CHAIN: one accumulator piece into the running sums of this thread's row, and the finished tile out to memory.
+template <int BN>
+__device__ __forceinline__ void chain_add(uint32_t tmem_acc, int chalf, float (&sum)[BN / 2]) {
+#pragma unroll
+  for (int c0 = 0; c0 < BN / 2; c0 += 32) {
+    uint32_t r[32];
+    tmem_ld_32x32(tmem_acc + (uint32_t)(chalf * (BN / 2) + c0), r);
+    tmem_ld_wait();
+#pragma unroll
+    for (int e = 0; e < 32; ++e) sum[c0 + e] += __uint_as_float(r[e]);
+  }
+}
+template <int BN>
+__device__ __forceinline__ void chain_store(const TcParams& p, int row, int n0, int chalf, int split, float* stage,
+                                            const float (&sum)[BN / 2]) {
+  const int lane = threadIdx.x & 31, row_base = row - lane;
+#pragma unroll
+  for (int c0 = 0; c0 < BN / 2; c0 += 32) {
+    const int col = n0 + chalf * (BN / 2) + c0;
+    if (col >= p.N) break;
+    float* srow = stage + lane * EPI_STAGE_STRIDE;
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      *reinterpret_cast<float4*>(srow + 4 * e) = make_float4(sum[c0 + 4 * e], sum[c0 + 4 * e + 1], sum[c0 + 4 * e + 2], sum[c0 + 4 * e + 3]);
+    __syncwarp();
+    if (p.c_dtype == DT_F32) {
+      float* C = reinterpret_cast<float*>(p.C) + (long long)split * p.part_stride;
+      const int cc = col + (lane & 7) * 4;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int gr = row_base + i * 4 + (lane >> 3);
+        float4 v = *reinterpret_cast<const float4*>(stage + (i * 4 + (lane >> 3)) * EPI_STAGE_STRIDE + (lane & 7) * 4);
+        if (gr < p.M && cc < p.N) {
+          float4* q = reinterpret_cast<float4*>(C + (long long)gr * p.ldc + cc);
+          if (p.accumulate) { const float4 w = *q; v.x += w.x; v.y += w.y; v.z += w.z; v.w += w.w; }
+          *q = v;
+        }
+      }
+    } else {
+      __nv_bfloat16* C = reinterpret_cast<__nv_bfloat16*>(p.C);
+      const int cc = col + (lane & 3) * 8;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        float v[8];
+        stage_get8(stage, lane, i, v);
+        const int gr = row_base + i * 8 + (lane >> 2);
+        if (gr < p.M && cc < p.N) *reinterpret_cast<uint4*>(C + (long long)gr * p.ldc + cc) = pack8_bf16(v);
+      }
+    }
+    __syncwarp();
+  }
+}
+
 template <int BN, int EPI>
 __global__ void __launch_bounds__(TC_THREADS, 1)
 gemm_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB,
@@ -619,8 +756,21 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
         const unsigned ab = tcount & 1u, aph = (tcount >> 1) & 1u;
         if (*abort_flag || !mbar_wait_bounded(&acc_empty[ab], aph ^ 1u, TC_WAIT_LIMIT_NS)) { ok = false; break; }
         tc_fence_after();
-        const uint32_t tmem_acc = tmem_base + ab * BN;
+        uint32_t tmem_acc = tmem_base + ab * BN;
+        int piece_end = EPI == EPI_CHAIN ? kb_lo + p.chain_kb : kb_hi;      // EPI_CHAIN: the next accumulator hand-over
+        bool fresh = true;
         for (int kb = kb_lo; kb < kb_hi; ++kb, ++it) {
+          if constexpr (EPI == EPI_CHAIN) {
+            if (kb == piece_end) {
+              umma_commit(&acc_full[tcount & 1u]);
+              ++tcount;
+              if (*abort_flag || !mbar_wait_bounded(&acc_empty[tcount & 1u], ((tcount >> 1) & 1u) ^ 1u, TC_WAIT_LIMIT_NS)) { ok = false; break; }
+              tc_fence_after();
+              tmem_acc = tmem_base + (tcount & 1u) * BN;
+              piece_end += p.chain_kb;
+              fresh = true;
+            }
+          }
           const int st = it % TC_STAGES;
           const unsigned ph = (it / TC_STAGES) & 1u;
           if (*abort_flag || !mbar_wait_bounded(&full[st], ph, TC_WAIT_LIMIT_NS)) { ok = false; break; }
@@ -633,11 +783,12 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
             if (k >= ksteps) break;
             const uint64_t da = make_smem_desc(sa + k * a_step, a_lbo, 1024u);
             const uint64_t db = make_smem_desc(sb + k * b_step, b_lbo, 1024u);
-            umma_bf16(tmem_acc, da, db, idesc, (kb > kb_lo || k > 0) ? 1u : 0u);
+            umma_bf16(tmem_acc, da, db, idesc, (!fresh || k > 0) ? 1u : 0u);
           }
+          fresh = false;
           umma_commit(&empty[st]);            // frees the stage once the MMAs above have read it
         }
-        if (ok) umma_commit(&acc_full[ab]);
+        if (ok) umma_commit(&acc_full[EPI == EPI_CHAIN ? tcount & 1u : ab]);
       }
       if (!ok) { *abort_flag = 1; atomicOr(&g_tc_status, 1u); }
     }
@@ -650,6 +801,31 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
       const int split = tile / tiles_mn, mn = tile - split * tiles_mn;
       const int m0 = (mn / p.tiles_n) * TC_BM, n0 = (mn % p.tiles_n) * BN;
       const int row = m0 + quad * 32 + lane;
+      if constexpr (EPI == EPI_CHAIN) {
+        const int kb_lo = split * p.kb_per_split, kb_hi = min(kb_lo + p.kb_per_split, num_kb_total);
+        float sum[BN / 2];
+#pragma unroll
+        for (int e = 0; e < BN / 2; ++e) sum[e] = 0.f;
+        int ok = 1;
+        for (int kb = kb_lo; kb < kb_hi; kb += p.chain_kb) {
+          const unsigned pb = tcount & 1u, pph = (tcount >> 1) & 1u;
+          if (lane == 0) {
+            ok = (!*abort_flag && mbar_wait_bounded(&acc_full[pb], pph, TC_WAIT_LIMIT_NS * 2ull)) ? 1 : 0;
+            if (!ok) { *abort_flag = 1; atomicOr(&g_tc_status, 1u); }
+          }
+          ok = __shfl_sync(0xffffffffu, ok, 0);
+          if (!ok) break;
+          tc_fence_after();
+          chain_add<BN>(tmem_base + pb * BN + ((uint32_t)(quad * 32) << 16), chalf, sum);
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&acc_empty[pb]);
+          if (kb + p.chain_kb < kb_hi) ++tcount;                   // the loop over tiles counts the last piece
+        }
+        if (!ok) break;
+        chain_store<BN>(p, row, n0, chalf, split, epi_stage + (warp - 2) * EPI_STAGE_FLOATS, sum);
+        continue;
+      }
       const unsigned ab = tcount & 1u, aph = (tcount >> 1) & 1u;
       EpiRegs pre;
       epi_prefetch<BN, EPI>(p, row, n0, chalf, pre);
@@ -843,13 +1019,24 @@ gemm_tc2_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
         const unsigned ab = tcount & 1u, aph = (tcount >> 1) & 1u;
         if (*abort_flag || !mbar_wait_bounded(&acc_empty[ab], aph ^ 1u, TC_WAIT_LIMIT_NS)) { ok = false; break; }
         tc_fence_after();
-        const uint32_t tmem_acc = tmem_base + ab * BN;
+        uint32_t tmem_acc = tmem_base + ab * BN;
+        int piece_lo = kb_lo;                    // EPI_CHAIN: where the current accumulator piece began
         for (int kb = kb_lo; kb < kb_hi; ++kb) {
+          if constexpr (EPI == EPI_CHAIN) {
+            if (kb - piece_lo == p.chain_kb) {   // hand this piece over, go on in the other buffer
+              umma_commit_pair(&acc_full[tcount & 1u], 3);
+              ++tcount;
+              if (*abort_flag || !mbar_wait_bounded(&acc_empty[tcount & 1u], ((tcount >> 1) & 1u) ^ 1u, TC_WAIT_LIMIT_NS)) { ok = false; break; }
+              tc_fence_after();
+              tmem_acc = tmem_base + (tcount & 1u) * BN;
+              piece_lo = kb;
+            }
+          }
           if (!mbar_wait_bounded(&full[st], ph, TC_WAIT_LIMIT_NS)) { ok = false; break; }
           tc_fence_after();
           const uint32_t alo = da_lo + st_off, blo = db_lo + st_off;
-          umma_bf16_pair(tmem_acc, desc(alo, da_hi), desc(blo, db_hi), idesc, kb > kb_lo ? 1u : 0u);
-          if (kb < p.kb_main) {
+          umma_bf16_pair(tmem_acc, desc(alo, da_hi), desc(blo, db_hi), idesc, kb > piece_lo ? 1u : 0u);
+          if (EPI == EPI_CHAIN || kb < p.kb_main) {
 #pragma unroll
             for (int k = 1; k < TC_BK / 16; ++k)
               umma_bf16_pair(tmem_acc, desc(alo + k * a_step16, da_hi), desc(blo + k * b_step16, db_hi), idesc, 1u);
@@ -862,7 +1049,7 @@ gemm_tc2_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
           st_off += T2_STAGE_BYTES >> 4;
           if (++st == T2_STAGES) { st = 0; st_off = 0; ph ^= 1u; }
         }
-        if (ok) umma_commit_pair(&acc_full[ab], 3);
+        if (ok) umma_commit_pair(&acc_full[EPI == EPI_CHAIN ? tcount & 1u : ab], 3);
       }
       if (!ok) { *abort_flag = 1; atomicOr(&g_tc_status, 1u); }
     }
@@ -875,6 +1062,31 @@ gemm_tc2_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
       const int split = tile / tiles_mn, mn = tile - split * tiles_mn;
       const int m0 = (mn / p.tiles_n) * (2 * TC_BM) + (int)rank * TC_BM, n0 = (mn % p.tiles_n) * BN;
       const int row = m0 + quad * 32 + lane;
+      if constexpr (EPI == EPI_CHAIN) {
+        const int kb_lo = split * p.kb_per_split, kb_hi = min(kb_lo + p.kb_per_split, num_kb_total);
+        float sum[BN / 2];
+#pragma unroll
+        for (int e = 0; e < BN / 2; ++e) sum[e] = 0.f;
+        int ok = 1;
+        for (int kb = kb_lo; kb < kb_hi; kb += p.chain_kb) {
+          const unsigned pb = tcount & 1u, pph = (tcount >> 1) & 1u;
+          if (lane == 0) {
+            ok = (!*abort_flag && mbar_wait_bounded(&acc_full[pb], pph, TC_WAIT_LIMIT_NS * 2ull)) ? 1 : 0;
+            if (!ok) { *abort_flag = 1; atomicOr(&g_tc_status, 1u); }
+          }
+          ok = __shfl_sync(0xffffffffu, ok, 0);
+          if (!ok) break;
+          tc_fence_after();
+          chain_add<BN>(tmem_base + pb * BN + ((uint32_t)(quad * 32) << 16), chalf, sum);
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive_cluster(mapa_shared(smem_u32(&acc_empty[pb]), 0));
+          if (kb + p.chain_kb < kb_hi) ++tcount;                   // the loop over tiles counts the last piece
+        }
+        if (!ok) break;
+        chain_store<BN>(p, row, n0, chalf, split, epi_stage + (warp - 2) * EPI_STAGE_FLOATS, sum);
+        continue;
+      }
       const unsigned ab = tcount & 1u, aph = (tcount >> 1) & 1u;
       EpiRegs pre;
       epi_prefetch<BN, EPI>(p, row, n0, chalf, pre);
@@ -972,8 +1184,12 @@ static void fill_params(TcParams& p, const GemmArgs& g) {
   p.up_row0 = g.N / 2;
   p.hl = g.epi.hl;
   p.kb_main = (g.K + TC_BK - 1) / TC_BK;
-  p.kb_total = p.kb_main + (g.K2 > 0 ? 1 : 0);
-  p.ext_ksteps = g.K2 / 16;
+  p.kb_total = p.kb_main + (g.K2 > 0 ? (g.K2 + TC_BK - 1) / TC_BK : 0);     // K2 <= 64 but for EPI_CHAIN
+  p.ext_ksteps = g.epi.kind == EPI_CHAIN ? TC_BK / 16 : g.K2 / 16;
+  p.vh = g.epi.vh;
+  p.chain_kb = g.epi.chain_kb > 0 ? g.epi.chain_kb : p.kb_total;
+  p.accumulate = g.epi.accumulate;
+  p.part_stride = g.epi.part_stride;
   p.alpha = g.alpha;
   p.kb_per_split = 1; p.tiles_m = p.tiles_n = p.splits = 1;
 }
@@ -1009,6 +1225,7 @@ static int launch_tc(const GemmArgs& g, cudaStream_t s) {
     splits = (int)(want < cap ? want : cap);
     if (splits < 1) splits = 1;
   }
+  if (EPI == EPI_CHAIN) splits = g.epi.splits;
   p.kb_per_split = (num_kb + splits - 1) / splits;
   splits = (num_kb + p.kb_per_split - 1) / p.kb_per_split;          // no empty split
   static unsigned long long attr_devices = 0;
@@ -1071,6 +1288,7 @@ static int launch_tc2(const GemmArgs& g, cudaStream_t s) {
       if (score > best) { best = score; splits = actual; }
     }
   }
+  if (EPI == EPI_CHAIN) splits = g.epi.splits;
   p.kb_per_split = (num_kb + splits - 1) / splits;
   splits = (num_kb + p.kb_per_split - 1) / p.kb_per_split;
   p.tiles_m = tiles_m; p.tiles_n = tiles_n; p.splits = splits;
@@ -1097,7 +1315,48 @@ static int launch_tc2(const GemmArgs& g, cudaStream_t s) {
   return PCM_OK;
 }
 
+static bool chain_pair(const GemmArgs& g) { return pair_enabled() && g.N > TC_BM && g.M > TC_BM; }
+static int chain_bn(const GemmArgs& g) { return g.N > 128 ? 256 : 128; }
+
+// Without enough tiles for every SM the contraction is split, but not below 16 k-blocks a split, nor beyond one wave: a
+// part is a tile's fp32 sums, so the parts of one launch never exceed what the SMs hold as accumulators at one time.
+int gemm_chain_splits(const GemmArgs& g) {
+  const bool pair = chain_pair(g);
+  const long long bm = pair ? 2 * TC_BM : TC_BM, bn = pair ? T2_BN : chain_bn(g);
+  const long long tiles = ((g.M + bm - 1) / bm) * ((g.N + bn - 1) / bn);
+  const long long slots = pair ? sm_count() / 2 : sm_count();
+  const int kb = (g.K + TC_BK - 1) / TC_BK + (g.K2 + TC_BK - 1) / TC_BK;
+  long long splits = slots / tiles;
+  if (splits > kb / 16) splits = kb / 16;
+  if (splits < 2) return 1;
+  const int per = (int)((kb + splits - 1) / splits);
+  return (kb + per - 1) / per;
+}
+size_t chain_part_bytes() { return (size_t)sm_count() * TC_BM * T2_BN * 4; }
+
+__global__ void forward_status_kernel(unsigned* status) {
+  if (g_tc_status) atomicOr(status, STATUS_TIMEOUT);
+}
+int gemm_forward_status(unsigned* status, cudaStream_t s) {
+  if (!status) return PCM_OK;
+  forward_status_kernel<<<1, 1, 0, s>>>(status);
+  PCM_LAUNCH_CHECK();
+  return PCM_OK;
+}
+
 bool gemm_epilogue_supported(const GemmArgs& g) {
+  if (g.epi.kind == EPI_VOCAB_STATS || g.epi.kind == EPI_VOCAB_DZ || g.epi.kind == EPI_CHAIN) {
+    // any N (EPI_CHAIN: a multiple of 8), so the general conditions are checked here
+    if (g.ab_dtype != DT_BF16 || g.M < 1 || g.N < 1 || g.K < 1 || (g.lda % 8) || (g.ldb % 8) || !encode_fn()) return false;
+    if (((uintptr_t)g.A | (uintptr_t)g.B | (uintptr_t)g.C) & 15) return false;
+    if (g.epi.kind == EPI_VOCAB_STATS) return g.a_kmajor && g.b_kmajor && g.epi.vh.tok && g.epi.vh.part && !g.K2;
+    if (g.epi.kind == EPI_VOCAB_DZ)
+      return g.a_kmajor && g.b_kmajor && g.C && g.c_dtype == DT_BF16 && g.ldc % 32 == 0 && g.ldc >= g.N && g.epi.vh.dz_lo &&
+             !((uintptr_t)g.epi.vh.dz_lo & 15) && g.epi.vh.tok && g.epi.vh.lse && g.epi.vh.dlogp && !g.K2;
+    return g.C && g.N % 8 == 0 && g.ldc % 8 == 0 && g.epi.splits >= 1 && (g.epi.splits == 1 || (g.c_dtype == DT_F32 && !g.epi.accumulate)) &&
+           (!g.epi.accumulate || g.c_dtype == DT_F32) && !g.R && g.alpha == 1.f &&
+           (!g.K2 || (g.K2 > 0 && g.A2 && g.B2 && !(g.lda2 % 8) && !(g.ldb2 % 8) && !(((uintptr_t)g.A2 | (uintptr_t)g.B2) & 15)));
+  }
   if (!gemm_tcgen05_supported(g) || g.c_dtype != DT_BF16 || g.R) return false;
   const GemmEpilogue& e = g.epi;
   switch (e.kind) {
@@ -1137,6 +1396,16 @@ int gemm_tcgen05(const GemmArgs& g, cudaStream_t s) {
     case EPI_HEAD_LOSS:
       if (!gemm_epilogue_supported(g)) return PCM_ERR_SHAPE;
       return launch_tc<256, EPI_HEAD_LOSS>(g, s);
+    case EPI_VOCAB_STATS:
+      if (!gemm_epilogue_supported(g)) return PCM_ERR_SHAPE;
+      return pair_enabled() && g.M > TC_BM ? launch_tc2<EPI_VOCAB_STATS>(g, s) : launch_tc<256, EPI_VOCAB_STATS>(g, s);
+    case EPI_VOCAB_DZ:
+      if (!gemm_epilogue_supported(g)) return PCM_ERR_SHAPE;
+      return pair_enabled() && g.M > TC_BM ? launch_tc2<EPI_VOCAB_DZ>(g, s) : launch_tc<256, EPI_VOCAB_DZ>(g, s);
+    case EPI_CHAIN:
+      if (!gemm_epilogue_supported(g)) return PCM_ERR_SHAPE;
+      if (chain_pair(g)) return launch_tc2<EPI_CHAIN>(g, s);
+      return chain_bn(g) == 256 ? launch_tc<256, EPI_CHAIN>(g, s) : launch_tc<128, EPI_CHAIN>(g, s);
     default: break;
   }
   if (pair) return launch_tc2<EPI_NONE>(g, s);

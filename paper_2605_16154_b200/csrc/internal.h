@@ -2,6 +2,7 @@
 #pragma once
 #include "common.cuh"
 #include "head_loss.cuh"
+#include "vocab.cuh"
 
 namespace pcm {
 
@@ -13,7 +14,8 @@ enum { DT_F32 = 0, DT_BF16 = 1 };
 //   b_kmajor: B stored [N][K] with row stride ldb;   otherwise B stored [K][N] with row stride ldb.
 // Work fused into the tensor-core GEMM's epilogue (ignored by the SIMT kernel: callers use it only
 // when gemm_tcgen05_supported() holds).
-enum { EPI_NONE = 0, EPI_SWIGLU_FWD = 1, EPI_SWIGLU_BWD = 2, EPI_ROPE = 3, EPI_HEAD_LOSS = 4 };
+enum { EPI_NONE = 0, EPI_SWIGLU_FWD = 1, EPI_SWIGLU_BWD = 2, EPI_ROPE = 3, EPI_HEAD_LOSS = 4, EPI_VOCAB_STATS = 5, EPI_VOCAB_DZ = 6,
+       EPI_CHAIN = 7 };
 struct GemmEpilogue {
   int kind = EPI_NONE;
   // EPI_SWIGLU_FWD: B is [2F][K] (gate rows, then up rows); C receives gate | up as [M][2F] and
@@ -29,6 +31,16 @@ struct GemmEpilogue {
   //                 hl.want_dz, C = d loss / d z [M][256] bf16.  z is never stored.
   const float2* rope_tab = nullptr; int S = 0, dh = 0, d = 0;
   HeadLossArgs hl;
+  // EPI_VOCAB_STATS: the product is the logits z [M][N] of a vocabulary of any width N; the epilogue reduces every 128
+  //                 columns of a row to softmax statistics (vh.part).  z is never stored, C is not used.
+  // EPI_VOCAB_DZ:   the same product again; C [M][ldc] (bf16, ldc a multiple of 32) and vh.dz_lo receive d loss / d z.
+  VocabHeadArgs vh;
+  // EPI_CHAIN:      C = or += A B (fp32 or bf16, N a multiple of 8).  The tensor core's accumulator is not rounded to
+  //                 nearest, so a long contraction drifts; here it is drained every chain_kb k-blocks and the pieces
+  //                 are added in registers, in fp32 and in order.  The continuation A2 / B2 may have any K2.
+  //                 splits > 1: each split of the contraction stores its own fp32 part, part_stride elements apart.
+  int chain_kb = 0, splits = 1, accumulate = 0;
+  long long part_stride = 0;
 };
 
 struct GemmArgs {
@@ -57,6 +69,13 @@ bool gemm_tcgen05_supported(const GemmArgs& g);
 // True when gemm() would run g on the CTA-pair kernel (256 x 256 tiles) rather than on a single-CTA or SIMT kernel.
 bool gemm_runs_on_pairs(const GemmArgs& g);
 bool gemm_tcgen05_pair(const GemmArgs& g);      // the tensor-core path's own choice, given that it takes g
+// Splits of the contraction with which an EPI_CHAIN product of this shape fills the GPU; its fp32 parts take at most
+// chain_part_bytes(), a bound that holds for every shape.
+int gemm_chain_splits(const GemmArgs& g);
+size_t chain_part_bytes();
+// Sets STATUS_TIMEOUT in *status (device; nothing where it is null), in stream order, when a bounded wait of a
+// tensor-core GEMM has run out since the status was last polled.
+int gemm_forward_status(unsigned* status, cudaStream_t s);
 // True when the tensor-core kernel can run g including its fused epilogue.
 bool gemm_epilogue_supported(const GemmArgs& g);
 // Reads and clears the tensor-core kernels' device status word (synchronous copy).

@@ -5,6 +5,7 @@
 
 #include "async_ptx.cuh"
 #include "internal.h"
+#include "vocab.cuh"
 
 namespace pcm {
 
@@ -399,19 +400,6 @@ embed_join_kernel(const EmbedPlan pl, float scale, float* __restrict__ grad, int
 // ------------------------------------------------------------------------------------------------
 // Log-probabilities of given tokens from logits.
 // ------------------------------------------------------------------------------------------------
-constexpr float LOG2E = 1.44269504088896340736f;
-constexpr float LN2 = 0.69314718055994530942f;
-
-__device__ __forceinline__ float max_nan(float a, float b) {
-  float r;
-  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
-  return r;
-}
-__device__ __forceinline__ float ex2(float x) {
-  float r;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
-  return r;
-}
 // Whole numbers in the order of the floats they stand for: -0 and +0 are one value, a NaN of either sign is above all.
 __device__ __forceinline__ unsigned order_of(float z) {
   if (z != z) return 0xFFFFFFFFu;
@@ -422,34 +410,6 @@ __device__ __forceinline__ float float_of_order(unsigned o) {
   if (o == 0xFFFFFFFFu) return __uint_as_float(0x7FFFFFFFu);
   return __uint_as_float((o & 0x80000000u) ? (o ^ 0x80000000u) : ~o);
 }
-
-// Softmax statistics of a part of a row: m the largest logit, s = sum 2^t and w = sum 2^t t with t = (z - m) c,
-// c = log2(e) / temperature.  t is held at -1000 or above, so that a masked logit (-inf, or the type's lowest
-// value) adds 2^t = 0 to both sums instead of 0 * -inf.
-struct VocabStat { float m, s, w; };
-
-__device__ __forceinline__ VocabStat stat_join(const VocabStat& a, const VocabStat& b, float c) {
-  const float m = max_nan(a.m, b.m);
-  // equal maxima (two empty parts with -inf, or twice +inf) shift by nothing
-  const float da = a.m == m ? 0.f : fmaxf((a.m - m) * c, -1000.f), db = b.m == m ? 0.f : fmaxf((b.m - m) * c, -1000.f);
-  const float fa = ex2(da), fb = ex2(db);
-  return VocabStat{m, a.s * fa + b.s * fb, fa * (a.w + a.s * da) + fb * (b.w + b.s * db)};
-}
-
-// Everything of one row that follows from its statistics.  A row whose logits are all -inf carries no distribution:
-// lse = -inf, entropy 0.  A NaN or +inf among them makes both NaN.
-struct RowResult {
-  float m, log_s, inv_t, lse, entropy;
-  __device__ RowResult(const VocabStat& st, float inv_t_) : m(st.m), log_s(0.f), inv_t(inv_t_), lse(st.m), entropy(0.f) {
-    if (m == -INFINITY) return;
-    if (!(m < INFINITY)) { m = lse = entropy = __uint_as_float(0x7FFFFFFFu); return; }
-    log_s = logf(st.s);
-    lse = m * inv_t + log_s;
-    entropy = log_s - (st.w / st.s) * LN2;
-  }
-  // z - m first: large logits do not swallow the logarithm
-  __device__ float logp(float z) const { return m == -INFINITY ? -INFINITY : (z - m) * inv_t - log_s; }
-};
 
 struct LogpParams {
   const void* logits; long long ld;
@@ -471,17 +431,6 @@ __device__ __forceinline__ void part_add(VocabStat& st, const float (&v)[Vec16<T
     const float x = ex2(t);
     st.s += x;
     st.w += x * t;
-  }
-}
-
-// Raises the reference value of the statistics to at least z (NaN propagates).
-__device__ __forceinline__ void stat_raise(VocabStat& st, float z, float c) {
-  const float m = max_nan(st.m, z);
-  if (m != st.m) {
-    const float d = fmaxf((st.m - m) * c, -1000.f), f = ex2(d);
-    st.w = f * (st.w + st.s * d);
-    st.s *= f;
-    st.m = m;
   }
 }
 
@@ -544,7 +493,7 @@ token_logp_kernel(const LogpParams p, int ranks) {
   const int rank = NT == 32 || ranks == 1 ? 0 : (int)cluster_ctarank();
   const long long row = NT == 32 ? (long long)blockIdx.x * ROWS + (threadIdx.x >> 5) : blockIdx.x / ranks;
   if (row >= p.M) return;                     // whole warps (NT = 32) only: the grid is exact otherwise
-  const float c = p.inv_t * LOG2E;
+  const float c = p.inv_t * VOCAB_LOG2E;
   const int t = p.tok ? p.tok[row] : 0;
   const bool bad = p.tok && t >= p.V, skip = p.tok && (t < 0 || bad);
   const int top = p.top;
@@ -805,14 +754,7 @@ token_logp_bwd_kernel(const LogpBwdParams p, int chunks) {
   const float gt = g * p.inv_t, ht = h * p.inv_t, H = p.dent ? p.entropy[row] : 0.f;
   const T* z = reinterpret_cast<const T*>(p.logits) + row * p.ld;
   T* dz = reinterpret_cast<T*>(p.dlogits) + row * p.ld_d;
-  auto slope = [&](float zv, int idx) {
-    const float lp = zv * p.inv_t - lse;
-    const float pr = __expf(lp);
-    // p = 0 stands for masked logits too, whose log p is -inf
-    float r = pr == 0.f ? 0.f : -pr * (gt + ht * (lp + H));
-    if (idx == t) r += gt;
-    return r;
-  };
+  auto slope = [&](float zv, int idx) { return vocab_slope(zv, p.inv_t, lse, H, gt, ht, idx == t); };
   if constexpr (VEC) {
     const int head = min(p.V, (int)(((16u - ((unsigned)(uintptr_t)z & 15u)) & 15u) / sizeof(T)));
     const int nv = (p.V - head) / N, tail = head + nv * N;

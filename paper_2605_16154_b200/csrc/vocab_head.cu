@@ -1,0 +1,237 @@
+// Log-probabilities of given tokens straight from the last hidden states x [M][d] and the head's weight w [V][d], and
+// their gradients.  The logits z = x w^T exist only as accumulator tiles in tensor memory:
+//   forward   the head GEMM's epilogue reduces each row's 128-column blocks to softmax statistics (16 bytes per block and
+//             row instead of 256 or 512 of logits); a small kernel joins them.  Bound by the tensor cores from a few
+//             hundred rows on, by reading w below.
+//   backward  the same product once more, its epilogue writing d loss / d z in bf16 (rounded value and remainder) for a
+//             chunk of rows; then dx = dz w and dw (+)= dz^T x.
+#include <cmath>
+
+#include "internal.h"
+
+namespace pcm {
+
+constexpr int VH_GROUPS = 16;                 // column-block slices of a row joined side by side
+constexpr int VH_CHAIN_KB = 8;                // k-blocks (512 rows) per accumulator piece of dw
+
+// 32 rows per block: thread (lane, slice) runs over every 16th part of row 32 b + lane, then slice 0 joins the slices.
+__global__ void __launch_bounds__(32 * VH_GROUPS)
+vocab_stats_join_kernel(const float4* __restrict__ part, int M, int V, const int* __restrict__ tok, float inv_t,
+                        float* __restrict__ logp, float* __restrict__ entropy, float* __restrict__ lse, unsigned* status) {
+  __shared__ VocabStat sm[VH_GROUPS][32];
+  const int lane = threadIdx.x & 31, slice = threadIdx.x >> 5;
+  const long long row = (long long)blockIdx.x * 32 + lane;
+  const int blocks = (V + 127) / 128;
+  const float c = inv_t * VOCAB_LOG2E;
+  VocabStat st{-INFINITY, 0.f, 0.f};
+  if (row < M) {
+#pragma unroll 4
+    for (int b = slice; b < blocks; b += VH_GROUPS) {
+      const float4 q = __ldg(part + (long long)b * M + row);
+      st = stat_join(st, VocabStat{q.x, q.y, q.z}, c);
+    }
+  }
+  sm[slice][lane] = st;
+  __syncthreads();
+  if (slice != 0 || row >= M) return;
+  for (int k = 1; k < VH_GROUPS; ++k) st = stat_join(st, sm[k][lane], c);
+  const int t = tok[row];
+  const bool live = t >= 0 && t < V;
+  if (t >= V && status) atomicOr(status, STATUS_BAD_TOKEN);
+  const RowResult res(st, inv_t);
+  if (logp) logp[row] = live ? res.logp(part[(long long)(t / 128) * M + row].w) : 0.f;
+  if (entropy) entropy[row] = live ? res.entropy : 0.f;
+  if (lse) lse[row] = live ? res.lse : 0.f;
+}
+
+// The hidden states with zeros in the rows that have no token: their d z is zero, but zero times whatever a padded row
+// holds (NaN, inf) need not be.
+__global__ void __launch_bounds__(256)
+live_rows_kernel(const uint4* __restrict__ x, long long ld8, int M, int d8, const int* __restrict__ tok, int V, uint4* __restrict__ out,
+                 unsigned* status) {
+  const long long total = (long long)M * d8;
+  for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < total; i += (long long)gridDim.x * 256) {
+    const long long row = i / d8;
+    const int c = (int)(i - row * d8), t = tok[row];
+    const bool live = t >= 0 && t < V;
+    if (t >= V && c == 0 && status) atomicOr(status, STATUS_BAD_TOKEN);
+    out[i] = live ? x[row * ld8 + c] : make_uint4(0, 0, 0, 0);
+  }
+}
+
+// Parts of a split contraction added in order, four columns a thread.
+template <bool BF16>
+__global__ void __launch_bounds__(256)
+parts_sum_kernel(const float* __restrict__ part, long long stride, int splits, long long M, int N, void* __restrict__ C, long long ldc,
+                 int accumulate) {
+  const int n4 = N / 4;
+  const long long total = M * n4;
+  for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < total; i += (long long)gridDim.x * 256) {
+    const long long row = i / n4;
+    const int col = (int)(i - row * n4) * 4;
+    float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+    for (int k = 0; k < splits; ++k) {
+      const float4 w = __ldcs(reinterpret_cast<const float4*>(part + (long long)k * stride + row * N + col));
+      a.x += w.x; a.y += w.y; a.z += w.z; a.w += w.w;
+    }
+    if constexpr (BF16) {
+      const __nv_bfloat162 lo = __floats2bfloat162_rn(a.x, a.y), hi = __floats2bfloat162_rn(a.z, a.w);
+      uint2 o;
+      o.x = *reinterpret_cast<const uint32_t*>(&lo); o.y = *reinterpret_cast<const uint32_t*>(&hi);
+      *reinterpret_cast<uint2*>(reinterpret_cast<__nv_bfloat16*>(C) + row * ldc + col) = o;
+    } else {
+      float4* q = reinterpret_cast<float4*>(reinterpret_cast<float*>(C) + row * ldc + col);
+      if (accumulate) { const float4 w = *q; a.x += w.x; a.y += w.y; a.z += w.z; a.w += w.w; }
+      *q = a;
+    }
+  }
+}
+
+// g (EPI_CHAIN, C its final destination) in one launch, or in splits through `parts` and a summing kernel.
+static int chain_gemm(GemmArgs g, float* parts, cudaStream_t s) {
+  const int splits = gemm_chain_splits(g);
+  if (splits == 1) return gemm_tcgen05(g, s);
+  GemmArgs q = g;
+  q.C = parts; q.ldc = g.N; q.c_dtype = DT_F32;
+  q.epi.splits = splits; q.epi.accumulate = 0; q.epi.part_stride = (long long)g.M * g.N;
+  const int rc = gemm_tcgen05(q, s);
+  if (rc != PCM_OK) return rc;
+  const long long total = (long long)g.M * (g.N / 4);
+  const int grid = (int)(ceil_div(total, 256) < 8 * sm_count() ? ceil_div(total, 256) : 8 * sm_count());
+  if (g.c_dtype == DT_BF16)
+    parts_sum_kernel<true><<<grid, 256, 0, s>>>(parts, q.epi.part_stride, splits, g.M, g.N, g.C, g.ldc, 0);
+  else
+    parts_sum_kernel<false><<<grid, 256, 0, s>>>(parts, q.epi.part_stride, splits, g.M, g.N, g.C, g.ldc, g.epi.accumulate);
+  PCM_LAUNCH_CHECK();
+  return PCM_OK;
+}
+
+static size_t round256(size_t v) { return (v + 255) / 256 * 256; }
+
+struct HeadBwdPlan { size_t x, hi, lo, parts, total; long long ldz; int rows; };
+static HeadBwdPlan head_bwd_plan(int M, int d, int V, int chunk_rows) {
+  HeadBwdPlan pl;
+  pl.rows = chunk_rows < M ? chunk_rows : M;
+  pl.ldz = ((long long)V + 31) / 32 * 32;     // whole 32-column slices of the epilogue
+  pl.x = 0;
+  pl.hi = round256((size_t)pl.rows * d * 2);
+  pl.lo = pl.hi + round256((size_t)pl.rows * pl.ldz * 2);
+  pl.parts = pl.lo + round256((size_t)pl.rows * pl.ldz * 2);
+  pl.total = pl.parts + chain_part_bytes();
+  return pl;
+}
+
+static bool head_args_ok(const void* x, int64_t ld_x, const void* w, int64_t ld_w, int32_t d, const int32_t* tok) {
+  return x && w && tok && !(((uintptr_t)x | (uintptr_t)w) & 15) && ld_x >= d && ld_w >= d;
+}
+static bool temperature_ok(float t) { return t > 0.f && std::isfinite(t) && std::isfinite(1.f / t); }
+static bool head_shape_ok(int64_t ld_x, int64_t ld_w, int32_t d) { return d % 8 == 0 && ld_x % 8 == 0 && ld_w % 8 == 0; }
+
+}  // namespace pcm
+
+using namespace pcm;
+
+extern "C" size_t grpo_head_logp_workspace_bytes(int32_t n_rows, int32_t d, int32_t vocab) {
+  if (n_rows < 0 || d < 8 || d % 8 || vocab < 1) return 0;
+  return round256((size_t)((vocab + 127) / 128) * (size_t)n_rows * sizeof(float4)) + 256;
+}
+
+extern "C" int grpo_head_logp(const void* x, int64_t ld_x, int32_t n_rows, int32_t d, const void* w_h, int64_t ld_w, int32_t vocab,
+                              const int32_t* tok, float temperature, float* logp, float* entropy, float* lse,
+                              uint32_t* device_status, void* workspace, size_t workspace_bytes, pcm_stream stream) {
+  if (n_rows < 0 || d < 1 || vocab < 1 || !temperature_ok(temperature)) return PCM_ERR_ARG;
+  if (!head_shape_ok(ld_x, ld_w, d)) return PCM_ERR_SHAPE;
+  if (n_rows == 0) return PCM_OK;
+  if (!head_args_ok(x, ld_x, w_h, ld_w, d, tok)) return PCM_ERR_ARG;
+  if (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < grpo_head_logp_workspace_bytes(n_rows, d, vocab)) return PCM_ERR_WORKSPACE;
+  cudaStream_t s = (cudaStream_t)stream;
+  const float inv_t = 1.f / temperature;
+  float4* part = (float4*)workspace;
+  GemmArgs g{n_rows, vocab, d, x, ld_x, true, w_h, ld_w, true, DT_BF16, nullptr, 0, DT_BF16, nullptr, 0};
+  g.epi.kind = EPI_VOCAB_STATS;
+  g.epi.vh.tok = tok; g.epi.vh.inv_t = inv_t; g.epi.vh.part = part; g.epi.vh.vocab = vocab;
+  prof_begin(PC_GEMM, s);
+  int rc = gemm_tcgen05(g, s);
+  prof_end(s, 2.0 * n_rows * vocab * d, 2.0 * d * ((double)n_rows + vocab));
+  if (rc != PCM_OK) return rc;
+  prof_begin(PC_LOSS, s);
+  vocab_stats_join_kernel<<<ceil_div(n_rows, 32), 32 * VH_GROUPS, 0, s>>>(part, n_rows, vocab, tok, inv_t, logp, entropy, lse, device_status);
+  g_launches.fetch_add(1, std::memory_order_relaxed);
+  prof_end(s, 0.0, 16.0 * n_rows * ((vocab + 127) / 128));
+  PCM_CUDA_TRY(cudaPeekAtLastError());
+  return gemm_forward_status(device_status, s);
+}
+
+extern "C" size_t grpo_head_logp_bwd_workspace_bytes(int32_t n_rows, int32_t d, int32_t vocab, int32_t chunk_rows) {
+  if (n_rows < 0 || d < 8 || d % 8 || vocab < 1 || chunk_rows < 1) return 0;
+  return head_bwd_plan(n_rows, d, vocab, chunk_rows).total + 256;
+}
+
+extern "C" int grpo_head_logp_bwd(const void* x, int64_t ld_x, int32_t n_rows, int32_t d, const void* w_h, int64_t ld_w,
+                                  int32_t vocab, const int32_t* tok, float temperature, const float* lse, const float* entropy,
+                                  const float* dlogp, const float* dentropy, int32_t chunk_rows, uint32_t flags, void* dx,
+                                  int64_t ld_dx, float* dw, uint32_t* device_status, void* workspace, size_t workspace_bytes,
+                                  pcm_stream stream) {
+  if (n_rows < 0 || d < 1 || vocab < 1 || chunk_rows < 1 || !temperature_ok(temperature) || (flags & ~GRPO_ACCUMULATE)) return PCM_ERR_ARG;
+  if (!head_shape_ok(ld_x, ld_w, d) || (dx && ld_dx % 8)) return PCM_ERR_SHAPE;
+  if ((!dx && !dw) || (dx && (((uintptr_t)dx & 15) || ld_dx < d)) || (dw && ((uintptr_t)dw & 15))) return PCM_ERR_ARG;
+  const bool accumulate = flags & GRPO_ACCUMULATE;
+  cudaStream_t s = (cudaStream_t)stream;
+  if (n_rows == 0) {
+    if (dw && !accumulate) PCM_CUDA_TRY(cudaMemsetAsync(dw, 0, (size_t)vocab * d * sizeof(float), s));
+    return PCM_OK;
+  }
+  if (!head_args_ok(x, ld_x, w_h, ld_w, d, tok) || !lse || !dlogp || (dentropy && !entropy)) return PCM_ERR_ARG;
+  if (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < grpo_head_logp_bwd_workspace_bytes(n_rows, d, vocab, chunk_rows))
+    return PCM_ERR_WORKSPACE;
+  const HeadBwdPlan pl = head_bwd_plan(n_rows, d, vocab, chunk_rows);
+  unsigned char* base = (unsigned char*)workspace;
+  uint4* x_live = (uint4*)(base + pl.x);
+  void *hi = base + pl.hi, *lo = base + pl.lo;
+  float* parts = (float*)(base + pl.parts);
+  const float inv_t = 1.f / temperature;
+  for (int r0 = 0; r0 < n_rows; r0 += pl.rows) {
+    const int rows = n_rows - r0 < pl.rows ? n_rows - r0 : pl.rows;
+    const unsigned short* xr = (const unsigned short*)x + (long long)r0 * ld_x;
+    const double flops = 2.0 * rows * vocab * d;
+    prof_begin(PC_ELEM, s);
+    const int d8 = d / 8;
+    const int blocks = ceil_div((long long)rows * d8, 1024);
+    live_rows_kernel<<<blocks, 256, 0, s>>>((const uint4*)xr, ld_x / 8, rows, d8, tok + r0, vocab, x_live, device_status);
+    g_launches.fetch_add(1, std::memory_order_relaxed);
+    prof_end(s, 0.0, 4.0 * rows * d);
+    PCM_CUDA_TRY(cudaPeekAtLastError());
+
+    GemmArgs z{rows, vocab, d, x_live, d, true, w_h, ld_w, true, DT_BF16, hi, pl.ldz, DT_BF16, nullptr, 0};
+    z.epi.kind = EPI_VOCAB_DZ;
+    VocabHeadArgs& v = z.epi.vh;
+    v.tok = tok + r0; v.inv_t = inv_t; v.lse = lse + r0; v.dlogp = dlogp + r0; v.vocab = vocab; v.dz_lo = lo;
+    v.dent = dentropy ? dentropy + r0 : nullptr;
+    v.entropy = dentropy ? entropy + r0 : nullptr;
+    prof_begin(PC_GEMM, s);
+    int rc = gemm_tcgen05(z, s);
+    prof_end(s, flops, 2.0 * d * ((double)rows + vocab) + 4.0 * rows * vocab);
+    if (rc != PCM_OK) return rc;
+    if (dx) {
+      GemmArgs q{rows, d, vocab, hi, pl.ldz, true, w_h, ld_w, false, DT_BF16, (unsigned short*)dx + (long long)r0 * ld_dx, ld_dx, DT_BF16, nullptr, 0};
+      q.epi.kind = EPI_CHAIN;                  // bf16 result: one accumulator piece
+      prof_begin(PC_GEMM, s);
+      rc = chain_gemm(q, parts, s);
+      prof_end(s, flops, 2.0 * rows * vocab + 2.0 * vocab * d + 2.0 * rows * d);
+      if (rc != PCM_OK) return rc;
+    }
+    if (dw) {
+      GemmArgs q{vocab, d, rows, hi, pl.ldz, false, x_live, d, false, DT_BF16, dw, d, DT_F32, nullptr, 0};
+      q.A2 = lo; q.lda2 = pl.ldz; q.B2 = x_live; q.ldb2 = d; q.K2 = rows;
+      q.epi.kind = EPI_CHAIN;
+      q.epi.chain_kb = VH_CHAIN_KB;
+      q.epi.accumulate = accumulate || r0 > 0;
+      prof_begin(PC_GEMM, s);
+      rc = chain_gemm(q, parts, s);
+      prof_end(s, 2.0 * flops, 4.0 * rows * vocab + 4.0 * rows * d + 4.0 * vocab * d);
+      if (rc != PCM_OK) return rc;
+    }
+  }
+  return gemm_forward_status(device_status, s);
+}

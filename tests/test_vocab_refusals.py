@@ -26,7 +26,22 @@ LOGP = dict(dtype=1, logits=P, ld=100, n_rows=5, vocab=100, tok=P, temperature=1
 LOGP_BWD = dict(dtype=1, logits=P, ld=100, n_rows=5, vocab=100, tok=P, temperature=1.0, lse=P, entropy=P, dlogp=P, dentropy=P,
                 dlogits=2 * P, ld_dlogits=100, status=None, stream=None)
 
+HEAD = dict(x=P, ld_x=64, n_rows=5, d=64, w=P, ld_w=64, vocab=100, tok=P, temperature=1.0, logp=P, entropy=P, lse=P, status=None,
+            workspace=P, workspace_bytes=1 << 30, stream=None)
+HEAD_BWD = dict(x=P, ld_x=64, n_rows=5, d=64, w=P, ld_w=64, vocab=100, tok=P, temperature=1.0, lse=P, entropy=P, dlogp=P, dentropy=P,
+                chunk_rows=5, flags=0, dx=P, ld_dx=64, dw=P, status=None, workspace=P, workspace_bytes=1 << 30, stream=None)
+
 CASES = [
+    ("grpo_head_logp", HEAD, [
+        (dict(x=None), ARG), (dict(w=None), ARG), (dict(tok=None), ARG), (dict(x=P + 8), ARG), (dict(w=P + 2), ARG), (dict(n_rows=-1), ARG),
+        (dict(d=0), ARG), (dict(vocab=0), ARG), (dict(ld_x=56), ARG), (dict(ld_w=8), ARG), (dict(temperature=0.0), ARG),
+        (dict(temperature=NAN), ARG), (dict(d=60), SHAPE), (dict(ld_x=68), SHAPE), (dict(ld_w=65), SHAPE), (dict(workspace=None), WORKSPACE),
+        (dict(workspace=P + 128), WORKSPACE), (dict(workspace_bytes=64), WORKSPACE)]),
+    ("grpo_head_logp_bwd", HEAD_BWD, [
+        (dict(x=None), ARG), (dict(w=None), ARG), (dict(tok=None), ARG), (dict(lse=None), ARG), (dict(dlogp=None), ARG),
+        (dict(entropy=None), ARG), (dict(dx=None, dw=None), ARG), (dict(dx=P + 8), ARG), (dict(dw=P + 4), ARG), (dict(ld_dx=56), ARG),
+        (dict(chunk_rows=0), ARG), (dict(flags=6), ARG), (dict(temperature=-2.0), ARG), (dict(d=12), SHAPE), (dict(ld_dx=70), SHAPE),
+        (dict(workspace_bytes=1 << 10), WORKSPACE), (dict(workspace=P + 8), WORKSPACE)]),
     ("grpo_embed", EMBED, [
         (dict(dtype=2), ARG), (dict(dtype=-1), ARG), (dict(table=None), ARG), (dict(tok=None), ARG), (dict(out=None), ARG),
         (dict(n=-1), ARG), (dict(vocab=0), ARG), (dict(d=0), ARG), (dict(ld_table=63), ARG), (dict(ld_out=63), ARG),
@@ -70,6 +85,10 @@ def test_workspace_sizes():
     small, large = B.grpo_embed_workspace_bytes(1, 2, 1), B.grpo_embed_workspace_bytes(119808, 32000, 1024)
     assert 0 < small < large
     # two buffers of (token, position) pairs, and two partial rows for every 64 sorted rows
+    assert B.grpo_head_logp_workspace_bytes(5, 12, 100) == 0 and B.grpo_head_logp_bwd_workspace_bytes(5, 16, 100, 0) == 0
+    assert B.grpo_head_logp_workspace_bytes(1000, 64, 129) >= 2 * 16 * 1000
+    assert B.grpo_head_logp_bwd_workspace_bytes(100, 64, 500, 10) < B.grpo_head_logp_bwd_workspace_bytes(100, 64, 500, 100)
+    assert B.grpo_head_logp_bwd_workspace_bytes(100, 64, 500, 100) == B.grpo_head_logp_bwd_workspace_bytes(100, 64, 500, 1000)
     assert large >= 2 * 8 * 119808 + 2 * 4 * 1024 * 119808 // 64
 
 

@@ -93,305 +93,383 @@ embed_kernel(const T* __restrict__ table, long long ld_table, int vocab, int d, 
 
 // ------------------------------------------------------------------------------------------------
 // Gradient of the embedding: grad[v] (+)= scale * sum over {i : tok[i] = v} of dout[i], in fp32 and in ascending i.
-//   1. embed_sort_kernel: (token, position) pairs into token order by a stable radix sort inside one cluster;
-//   2. embed_sum_kernel: tiles of `rows` sorted pairs, each summed in order; a token that lies inside one tile is
-//      final, one that crosses tiles leaves a partial sum per tile; rows of absent tokens are written as zero;
-//   3. embed_join_kernel: the partial sums of the crossing tokens, in tile order.
+//   1. (token, position) pairs into token order, stably: up to 1024 pairs by a bitonic network in one block, more by a
+//      radix sort of 8-bit digits over up to 256 blocks;
+//   2. embed_sum_kernel: tiles of `rows` sorted pairs, each summed in order; a token that crosses more than one border
+//      between tiles leaves a partial sum per tile;
+//   3. embed_join_kernel: the partial sums of those tokens, in tile order.
 // No floating-point atomics: the same inputs give the same bits.  Bound by HBM: dout once, grad once.
 // ------------------------------------------------------------------------------------------------
-constexpr int ES_THREADS = 1024, ES_WARPS = ES_THREADS / 32, ES_BINS = 256, ES_MAX_RANKS = 8, ES_BATCH = 8;
+constexpr int EJ_WARPS = 16;
+constexpr int ES_THREADS = 1024, ES_WARPS = ES_THREADS / 32, ES_BINS = 256, ES_MAX_BLOCKS = 256;
 
 struct EmbedPlan {
   int n, vocab, d;
   int rows, tiles, dpad;                      // sorted pairs per tile, tiles, floats per partial row
+  int keys, blocks;                           // pairs per block of the radix sort (a multiple of 1024), blocks
   uint2* buf[2];                              // (token, position) pairs
-  uint8_t* present;                           // [vocab] 1 where a token occurs
-  int* n_jobs; int* jobs;                     // tiles in which a crossing token begins
+  unsigned* hist;                             // [blocks][256] digit counts of a block's pairs
+  uint8_t* present;                           // [vocab] 1 where a token occurs: marked by its sums, so once for each tile
+  int* n_jobs; uint2* jobs;                   // (token, last tile) of every token that left parts
+  int* first_tile;                            // [vocab] for those tokens: the tile that they begin in
   float* part;                                // [tiles][2][dpad]: of a token that began before the tile, of one that goes on behind it
-  const uint2* sorted;                        // the buffer that the last pass of the sort fills
+  const uint2* sorted;                        // the buffer that the sort ends in
 };
 
-struct EmbedSortSmem {
-  unsigned count[ES_WARPS][ES_BINS];
-  unsigned total[ES_BINS];
-  unsigned base[ES_BINS];
-  unsigned warp_sum[ES_BINS / 32];
-};
+// Tokens outside the vocabulary take the key behind its last one.
+__device__ __forceinline__ unsigned embed_key(int t, int vocab) { return t >= 0 && t < vocab ? (unsigned)t : (unsigned)vocab; }
 
-__device__ __forceinline__ unsigned ld_shared_cluster(uint32_t addr) {
-  unsigned v;
-  asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(addr) : "memory");
-  return v;
+// The kernels of one gradient run back to back: each is launched while its predecessor drains and waits here for its results.
+__device__ __forceinline__ void wait_for_predecessor() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void let_successor_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+
+// Up to 1024 pairs: a bitonic network over keys (token above, position below: positions differ, so the order is the stable
+// one), in 32 bits when token and position fit.  Exchanges up to 16 apart are shuffles, the others go through shared memory.
+template <typename K, int POS_BITS>
+__global__ void __launch_bounds__(ES_THREADS)
+embed_sort_small_kernel(const int* __restrict__ tok, const EmbedPlan pl, unsigned* status) {
+  __shared__ K sm[2][ES_THREADS];
+  const int i = threadIdx.x;
+  const int t_own = i < pl.n ? tok[i] : 0;
+  for (int v = i; v < (pl.vocab + 15) / 16; v += (int)blockDim.x) reinterpret_cast<uint4*>(pl.present)[v] = make_uint4(0, 0, 0, 0);
+  if (i == 0) *pl.n_jobs = 0;
+  K key = ~(K)0;
+  if (i < pl.n) {
+    if (t_own >= pl.vocab && status) atomicOr(status, STATUS_BAD_TOKEN);
+    key = ((K)embed_key(t_own, pl.vocab) << POS_BITS) | (K)i;
+  }
+  int turn = 0;
+  for (int k = 2; k <= (int)blockDim.x; k <<= 1) {
+    const bool up = (i & k) == 0;
+    for (int j = k >> 1; j; j >>= 1) {
+      K other;
+      if (j < 32) {
+        other = __shfl_xor_sync(0xffffffffu, key, j);
+      } else {                                // two buffers in turn: one barrier an exchange
+        sm[turn][i] = key;
+        __syncthreads();
+        other = sm[turn][i ^ j];
+        turn ^= 1;
+      }
+      const K lo = key < other ? key : other, hi = key < other ? other : key;
+      key = (((i & j) == 0) == up) ? lo : hi;
+    }
+  }
+  let_successor_start();
+  if (i < pl.n) pl.buf[0][i] = make_uint2((unsigned)(key >> POS_BITS), (unsigned)key & ((1u << 10) - 1u));
 }
 
+// Digit counts of one pass for each block's pairs.  The first one also clears what the sums will mark.
 __global__ void __launch_bounds__(ES_THREADS)
-embed_sort_kernel(const int* __restrict__ tok, const EmbedPlan pl, int ranks, int passes, int bits, unsigned* status) {
-  __shared__ EmbedSortSmem sm;
-  const int rank = ranks == 1 ? 0 : (int)cluster_ctarank();
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int lo = (int)((long long)pl.n * rank / ranks), hi = (int)((long long)pl.n * (rank + 1) / ranks);
-  const int wlo = lo + (int)((long long)(hi - lo) * warp / ES_WARPS), whi = lo + (int)((long long)(hi - lo) * (warp + 1) / ES_WARPS);
-  for (long long i = (long long)rank * ES_THREADS + threadIdx.x; i < (pl.vocab + 15) / 16; i += (long long)ranks * ES_THREADS)
-    reinterpret_cast<uint4*>(pl.present)[i] = make_uint4(0, 0, 0, 0);
-  if (rank == 0 && threadIdx.x == 0) *pl.n_jobs = 0;
+embed_count_kernel(const int* __restrict__ tok, const EmbedPlan pl, int pass, int bits, unsigned* status) {
+  __shared__ unsigned count[ES_BINS];
+  const int tid = threadIdx.x;
+  if (tid < ES_BINS) count[tid] = 0;
+  __syncthreads();
   const unsigned mask = (1u << bits) - 1u;
-  for (int pass = 0; pass < passes; ++pass) {
-    const uint2* src = (pass & 1) ? pl.buf[0] : pl.buf[1];
-    uint2* dst = (pass & 1) ? pl.buf[1] : pl.buf[0];
-    const int shift = pass * bits;
-    const bool last = pass == passes - 1;
-    // the pair at sorted-so-far position i; tokens outside the vocabulary take the key behind its last one
-    auto fetch = [&](int i, uint2& kv) {
-      if (pass == 0) {
-        const int t = tok[i];
-        kv = make_uint2(t >= 0 && t < pl.vocab ? (unsigned)t : (unsigned)pl.vocab, (unsigned)i);
-        return t >= pl.vocab;
-      }
-      kv = __ldcg(src + i);
-      return false;
-    };
-    for (int i = threadIdx.x; i < ES_WARPS * ES_BINS; i += ES_THREADS) (&sm.count[0][0])[i] = 0;
-    __syncthreads();
-    bool bad = false;
-    for (int b = wlo; b < whi; b += 32 * ES_BATCH) {
-      uint2 kv[ES_BATCH];
-#pragma unroll
-      for (int u = 0; u < ES_BATCH; ++u) {
-        const int i = b + u * 32 + lane;
-        if (i < whi) bad |= fetch(i, kv[u]);
-      }
-#pragma unroll
-      for (int u = 0; u < ES_BATCH; ++u) {
-        const bool in = b + u * 32 + lane < whi;
-        const unsigned dig = in ? (kv[u].x >> shift) & mask : 0xFFFFFFFFu;
-        const unsigned same = __match_any_sync(0xffffffffu, dig);
-        if (in && lane == __ffs(same) - 1) sm.count[warp][dig] += __popc(same);
-        __syncwarp();
-      }
+  const long long lo = (long long)blockIdx.x * pl.keys, hi = min(lo + pl.keys, (long long)pl.n);
+  if (pass == 0) {
+    const long long first = (long long)blockIdx.x * ES_THREADS + tid, stride = (long long)gridDim.x * ES_THREADS;
+    for (long long v = first; v < (pl.vocab + 15) / 16; v += stride) reinterpret_cast<uint4*>(pl.present)[v] = make_uint4(0, 0, 0, 0);
+    if (first == 0) *pl.n_jobs = 0;
+    let_successor_start();
+    for (long long i = lo + tid; i < hi; i += ES_THREADS) {
+      const int t = tok[i];
+      if (t >= pl.vocab && status) atomicOr(status, STATUS_BAD_TOKEN);
+      atomicAdd(&count[embed_key(t, pl.vocab) & mask], 1u);
     }
-    if (bad && status) atomicOr(status, STATUS_BAD_TOKEN);
+  } else {
+    wait_for_predecessor();
+    let_successor_start();
+    const uint2* src = (pass & 1) ? pl.buf[0] : pl.buf[1];
+    for (long long i = lo + tid; i < hi; i += ES_THREADS) atomicAdd(&count[(__ldcg(src + i).x >> (pass * bits)) & mask], 1u);
+  }
+  __syncthreads();
+  if (tid < ES_BINS) pl.hist[blockIdx.x * ES_BINS + tid] = count[tid];
+}
+
+// Lanes of the warp that hold the same digit as this one, among the lanes with `in`: a ballot for each bit of the digit.
+__device__ __forceinline__ unsigned same_digit(unsigned dig, bool in, int bits) {
+  unsigned same = __ballot_sync(0xffffffffu, in);
+#pragma unroll
+  for (int b = 0; b < 8; ++b) {
+    if (b < bits) {
+      const bool on = (dig >> b) & 1u;
+      const unsigned ones = __ballot_sync(0xffffffffu, on);
+      same &= on ? ones : ~ones;
+    }
+  }
+  return same;
+}
+
+// One pass: every pair to where its digit puts it, 1024 pairs of the block at a time in their order.  (Counting the next
+// pass's digits here, by atomics on the blocks that the pairs land in, took 8 us of 119808 pairs; its own kernel takes 4.)
+__global__ void __launch_bounds__(ES_THREADS)
+embed_scatter_kernel(const int* __restrict__ tok, const EmbedPlan pl, int pass, int bits) {
+  __shared__ unsigned count[ES_WARPS][ES_BINS];
+  __shared__ unsigned sums[2][ES_WARPS * 32 / ES_BINS][ES_BINS];
+  __shared__ unsigned base[ES_BINS], warp_sum[ES_BINS / 32];
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const long long lo = (long long)blockIdx.x * pl.keys, hi = min(lo + pl.keys, (long long)pl.n);
+  const int first_tok = pass == 0 && lo + tid < hi ? tok[lo + tid] : 0;      // an input: it need not wait
+  wait_for_predecessor();
+  const unsigned* hist = pl.hist;
+  const uint2* src = (pass & 1) ? pl.buf[0] : pl.buf[1];
+  uint2* dst = (pass & 1) ? pl.buf[1] : pl.buf[0];
+  const unsigned mask = (1u << bits) - 1u;
+  const int shift = pass * bits;
+  {
+    // per digit: pairs in all blocks and in the blocks before this one; four threads share a digit
+    const int dig = tid & (ES_BINS - 1), q = tid / ES_BINS, quarter = ES_THREADS / ES_BINS;
+    unsigned before = 0, all = 0;
+#pragma unroll 8
+    for (int b = q; b < pl.blocks; b += quarter) {
+      const unsigned k = __ldcg(hist + b * ES_BINS + dig);
+      all += k;
+      before += b < (int)blockIdx.x ? k : 0;
+    }
+    sums[0][q][dig] = all;
+    sums[1][q][dig] = before;
+  }
+  __syncthreads();
+  if (tid < ES_BINS) {
+    unsigned all = 0, before = 0;
+    for (int q = 0; q < ES_THREADS / ES_BINS; ++q) { all += sums[0][q][tid]; before += sums[1][q][tid]; }
+    unsigned incl = all;
+#pragma unroll
+    for (int off = 1; off < 32; off <<= 1) {
+      const unsigned o = __shfl_up_sync(0xffffffffu, incl, off);
+      incl += lane >= off ? o : 0;
+    }
+    if (lane == 31) warp_sum[warp] = incl;
+    base[tid] = incl - all + before;
+  }
+  __syncthreads();
+  if (tid < ES_BINS)
+    for (int w = 0; w < warp; ++w) base[tid] += warp_sum[w];
+  let_successor_start();
+  for (long long i0 = lo; i0 < hi; i0 += ES_THREADS) {
+    const long long i = i0 + tid;
+    const bool in = i < hi;
+    uint2 kv = make_uint2(0u, 0u);
+    if (in) kv = pass == 0 ? make_uint2(embed_key(i0 == lo ? first_tok : tok[i], pl.vocab), (unsigned)i) : __ldcg(src + i);
+    for (int k = tid; k < ES_WARPS * ES_BINS; k += ES_THREADS) (&count[0][0])[k] = 0;
     __syncthreads();
-    // per digit: where each warp's pairs begin among this block's
-    if (threadIdx.x < ES_BINS) {
-      unsigned run = 0;
+    const unsigned dig = (kv.x >> shift) & mask;
+    const unsigned same = same_digit(dig, in, bits);
+    if (in && lane == __ffs(same) - 1) count[warp][dig] = __popc(same);
+    __syncthreads();
+    unsigned total = 0;
+    if (tid < ES_BINS) {                      // per digit: the warps' counts into where each warp's pairs begin
 #pragma unroll 8
       for (int w = 0; w < ES_WARPS; ++w) {
-        const unsigned k = sm.count[w][threadIdx.x];
-        sm.count[w][threadIdx.x] = run;
-        run += k;
+        const unsigned k = count[w][tid];
+        count[w][tid] = total;
+        total += k;
       }
-      sm.total[threadIdx.x] = run;
     }
     __syncthreads();
-    if (ranks > 1) cluster_sync_all();
-    // per digit: pairs of smaller digits in all blocks, then of this digit in the blocks before this one
-    unsigned before = 0, all = 0, incl = 0;
-    if (threadIdx.x < ES_BINS) {
-      const uint32_t mine = smem_u32(&sm.total[threadIdx.x]);
-      for (int r = 0; r < ranks; ++r) {
-        const unsigned k = ranks == 1 ? sm.total[threadIdx.x] : ld_shared_cluster(mapa_shared(mine, (uint32_t)r));
-        all += k;
-        before += r < rank ? k : 0;
-      }
-      incl = all;
-#pragma unroll
-      for (int off = 1; off < 32; off <<= 1) {
-        const unsigned o = __shfl_up_sync(0xffffffffu, incl, off);
-        incl += lane >= off ? o : 0;
-      }
-      if (lane == 31) sm.warp_sum[warp] = incl;
+    if (in) {
+      const unsigned at = base[dig] + count[warp][dig] + __popc(same & ((1u << lane) - 1u));
+      dst[at] = kv;
     }
     __syncthreads();
-    if (threadIdx.x < ES_BINS) {
-      unsigned start = incl - all;
-      for (int w = 0; w < warp; ++w) start += sm.warp_sum[w];
-      sm.base[threadIdx.x] = start + before;
-    }
-    __syncthreads();
-    for (int b = wlo; b < whi; b += 32 * ES_BATCH) {
-      uint2 kv[ES_BATCH];
-#pragma unroll
-      for (int u = 0; u < ES_BATCH; ++u) {
-        const int i = b + u * 32 + lane;
-        if (i < whi) fetch(i, kv[u]);
-      }
-#pragma unroll
-      for (int u = 0; u < ES_BATCH; ++u) {
-        const bool in = b + u * 32 + lane < whi;
-        const unsigned dig = in ? (kv[u].x >> shift) & mask : 0xFFFFFFFFu;
-        const unsigned same = __match_any_sync(0xffffffffu, dig);
-        unsigned at = 0;
-        if (in) at = sm.base[dig] + sm.count[warp][dig] + __popc(same & ((1u << lane) - 1u));
-        __syncwarp();
-        if (in) {
-          if (lane == __ffs(same) - 1) sm.count[warp][dig] += __popc(same);
-          dst[at] = kv[u];
-          if (last && kv[u].x < (unsigned)pl.vocab) pl.present[kv[u].x] = 1;
-        }
-        __syncwarp();
-      }
-    }
-    if (ranks > 1) cluster_sync_all();        // the pairs are in place, the digit totals have been read
-    else __syncthreads();
+    if (tid < ES_BINS) base[tid] += total;
   }
 }
 
+// A warp sums one tile (up to 32 sorted pairs, one per lane) over the columns of its slab: NV pieces of 16 bytes (or of one
+// element) per lane, eight rows in flight.  What a row needs besides its bytes is kept small, because instructions, not
+// bytes, bounded the version in which every thread looked at every pair: which rows open a token and which count comes
+// from two ballots.
 template <typename T, bool VEC>
 __global__ void __launch_bounds__(128)
 embed_sum_kernel(const T* __restrict__ dout, long long ld, const EmbedPlan pl, float scale, float* __restrict__ grad, int accumulate,
-                 int ct_log2, int slabs, int tile_blocks) {
-  constexpr int N = VEC ? Vec16<T>::N : 1;
-  if ((int)blockIdx.x >= tile_blocks) {       // rows of absent tokens, 32 per block
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    for (int k = 0; k < 8; ++k) {
-      const long long v = (long long)(blockIdx.x - tile_blocks) * 32 + k * 4 + warp;
-      if (v >= pl.vocab || pl.present[v]) continue;
-      float* g = grad + v * pl.d;
-      if (VEC) {
-        for (int c = lane * 4; c < pl.d; c += 128) __stcs(reinterpret_cast<float4*>(g + c), make_float4(0.f, 0.f, 0.f, 0.f));
-      } else {
-        for (int c = lane; c < pl.d; c += 32) g[c] = 0.f;
-      }
-    }
-    return;
-  }
-  const int slab = blockIdx.x % slabs;
-  const int tile = ((blockIdx.x / slabs) << (7 - ct_log2)) + (threadIdx.x >> ct_log2);
-  const int col = (slab << (ct_log2)) * N + (threadIdx.x & ((1 << ct_log2) - 1)) * N;
-  if (tile >= pl.tiles || col >= pl.d) return;
+                 int slabs) {
+  constexpr int N = VEC ? Vec16<T>::N : 1, NV = VEC ? 2 : 4, U = 8;
+  wait_for_predecessor();
+  let_successor_start();
+  const int lane = threadIdx.x & 31;
+  const long long item = (long long)blockIdx.x * 4 + (threadIdx.x >> 5);
+  const int tile = (int)(item / slabs), slab = (int)(item - (long long)tile * slabs);
+  if (tile >= pl.tiles) return;
   const uint2* pair = pl.sorted;
   const int lo = tile * pl.rows, hi = min(lo + pl.rows, pl.n);
-  const unsigned before = lo > 0 ? pair[lo - 1].x : 0xFFFFFFFFu, behind = hi < pl.n ? pair[hi].x : 0xFFFFFFFFu;
-  unsigned cur = pair[lo].x;
-  bool first = true;
-  float acc[N];
+  const unsigned none = 0xFFFFFFFFu, vocab = (unsigned)pl.vocab;
+  auto pair_at = [&](long long i, long long end) { return i < end ? pair[i] : make_uint2(none, 0u); };
+  const uint2 own = pair_at(lo + lane, hi);
+  const uint2 beyond = pair_at((long long)hi + lane, min((long long)hi + pl.rows, (long long)pl.n));
+  // A token that crosses one border between tiles belongs to the tile it begins in; one that crosses more leaves a part
+  // in every tile it touches.
+  const unsigned head = __shfl_sync(0xffffffffu, own.x, 0), tail = __shfl_sync(0xffffffffu, own.x, hi - lo - 1);
+  const unsigned behind = __shfl_sync(0xffffffffu, beyond.x, 0);
+  const unsigned before = lo > 0 ? pair[lo - 1].x : none, far_before = lo > pl.rows ? pair[lo - pl.rows - 1].x : none;
+  const unsigned far_behind = (long long)hi + pl.rows < pl.n ? pair[hi + pl.rows].x : none;
+  const bool head_on = before == head;                                         // began before this tile
+  const bool tail_on = behind == tail && !(head_on && head == tail);           // begins here and goes on behind it
+  const bool head_far = head_on && (far_before == head || behind == head);
+  const bool tail_far = tail_on && far_behind == tail;
+  const unsigned skip = head_on && !head_far ? head : none;                    // the tile before sums it
+  int col[NV];
 #pragma unroll
-  for (int e = 0; e < N; ++e) acc[e] = 0.f;
-  auto put = [&](float* dst, float f, bool add) {
+  for (int j = 0; j < NV; ++j) col[j] = (slab * NV + j) * 32 * N + lane * N;
+  unsigned cur = none;
+  float acc[NV][N];
+  auto put = [&](float* dst, const float (&a)[N], float f, bool add) {
+    if constexpr (N >= 4) {
 #pragma unroll
-    for (int e = 0; e < N; e += (N >= 4 ? 4 : 1)) {
-      if constexpr (N >= 4) {
-        float4 o = make_float4(acc[e] * f, acc[e + 1] * f, acc[e + 2] * f, acc[e + 3] * f);
+      for (int e = 0; e < N; e += 4) {
+        float4 o = make_float4(a[e] * f, a[e + 1] * f, a[e + 2] * f, a[e + 3] * f);
         float4* q = reinterpret_cast<float4*>(dst + e);
         if (add) { const float4 w = *q; o.x += w.x; o.y += w.y; o.z += w.z; o.w += w.w; }
         *q = o;
-      } else {
-        dst[e] = add ? dst[e] + acc[e] * f : acc[e] * f;
       }
-    }
-  };
-  auto flush = [&](bool goes_on) {
-    if (cur >= (unsigned)pl.vocab) return;
-    const bool began_before = first && cur == before;
-    if (began_before) {
-      put(pl.part + ((long long)tile * 2) * pl.dpad + col, 1.f, false);
-    } else if (goes_on) {
-      put(pl.part + ((long long)tile * 2 + 1) * pl.dpad + col, 1.f, false);
-      if (col == 0) pl.jobs[atomicAdd(pl.n_jobs, 1)] = tile;
     } else {
-      put(grad + (long long)cur * pl.d + col, scale, accumulate != 0);
+      dst[0] = add ? dst[0] + a[0] * f : a[0] * f;
     }
   };
-  for (int i0 = lo; i0 < hi; i0 += 8) {
-    uint2 kv[8];
-    uint4 raw[8];
-    float one[8];
+  auto flush = [&]() {
+    if (cur == none) return;
+    if (slab == 0 && lane == 0) pl.present[cur] = 1;
+    float* dst = grad + (long long)cur * pl.d;
+    float f = scale;
+    bool add = accumulate != 0;
+    if (head_far && cur == head) {
+      dst = pl.part + ((long long)tile * 2) * pl.dpad;
+      f = 1.f; add = false;
+      if (slab == 0 && lane == 0 && behind != head) pl.jobs[atomicAdd(pl.n_jobs, 1)] = make_uint2(head, (unsigned)tile);    // it ends here
+    } else if (tail_far && cur == tail) {
+      dst = pl.part + ((long long)tile * 2 + 1) * pl.dpad;
+      f = 1.f; add = false;
+      if (slab == 0 && lane == 0) pl.first_tile[tail] = tile;
+    }
 #pragma unroll
-    for (int u = 0; u < 8; ++u) kv[u] = i0 + u < hi ? pair[i0 + u] : make_uint2(0xFFFFFFFFu, 0u);
+    for (int j = 0; j < NV; ++j)
+      if (col[j] < pl.d) put(dst + col[j], acc[j], f, add);
+  };
+  // `kv`: up to 32 pairs, one per lane; rows with a bit in `live` count, those with one in `open` begin a token
+  auto run = [&](const uint2& kv, unsigned live, unsigned open) {
+    const int rows = 32 - __clz(live);
+    for (int i0 = live ? (__ffs(live) - 1) & ~(U - 1) : 32; i0 < rows; i0 += U) {
+      uint4 raw[VEC ? U : 1][NV];
+      float one[VEC ? 1 : U][NV];
 #pragma unroll
-    for (int u = 0; u < 8; ++u)
-      if (kv[u].x < (unsigned)pl.vocab) {
-        const T* q = dout + (long long)kv[u].y * ld + col;
-        if constexpr (VEC) raw[u] = __ldcs(reinterpret_cast<const uint4*>(q));
-        else one[u] = as_f32(*q);
+      for (int u = 0; u < U; ++u) {
+        const unsigned at = __shfl_sync(0xffffffffu, kv.y, i0 + u);
+        if ((live >> (i0 + u)) & 1u) {
+          const T* q = dout + (long long)at * ld;
+#pragma unroll
+          for (int j = 0; j < NV; ++j) {
+            if constexpr (VEC) raw[u][j] = col[j] < pl.d ? __ldcs(reinterpret_cast<const uint4*>(q + col[j])) : make_uint4(0, 0, 0, 0);
+            else one[u][j] = col[j] < pl.d ? as_f32(q[col[j]]) : 0.f;
+          }
+        }
       }
 #pragma unroll
-    for (int u = 0; u < 8; ++u) {
-      if (i0 + u >= hi) break;
-      if (kv[u].x != cur) {
-        flush(false);
-        cur = kv[u].x;
-        first = false;
+      for (int u = 0; u < U; ++u) {
+        if (!((live >> (i0 + u)) & 1u)) continue;
+        if ((open >> (i0 + u)) & 1u) {
+          flush();
+          cur = __shfl_sync(0xffffffffu, kv.x, i0 + u);
 #pragma unroll
-        for (int e = 0; e < N; ++e) acc[e] = 0.f;
-      }
-      if (cur < (unsigned)pl.vocab) {
-        if constexpr (VEC) {
-          float f[N];
-          Vec16<T>::unpack(raw[u], f);
+          for (int j = 0; j < NV; ++j)
 #pragma unroll
-          for (int e = 0; e < N; ++e) acc[e] += f[e];
-        } else {
-          acc[0] += one[u];
+            for (int e = 0; e < N; ++e) acc[j][e] = 0.f;
+        }
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+          if constexpr (VEC) {
+            float f[N];
+            Vec16<T>::unpack(raw[u][j], f);
+#pragma unroll
+            for (int e = 0; e < N; ++e) acc[j][e] += f[e];
+          } else {
+            acc[j][0] += one[u][j];
+          }
         }
       }
     }
-  }
-  flush(cur == behind);
+  };
+  const unsigned prev = __shfl_up_sync(0xffffffffu, own.x, 1);
+  run(own, __ballot_sync(0xffffffffu, own.x < vocab && own.x != skip), __ballot_sync(0xffffffffu, lane == 0 || prev != own.x));
+  if (tail_on && !tail_far) run(beyond, __ballot_sync(0xffffffffu, beyond.x == tail && tail < vocab), 0u);
+  flush();
 }
 
-// One warp per crossing token and 128 columns; a token over more than 16 tiles is shared by the block's eight warps.
-__global__ void __launch_bounds__(256)
-embed_join_kernel(const EmbedPlan pl, float scale, float* __restrict__ grad, int accumulate) {
-  __shared__ float4 sum[8][32];
-  __shared__ int span[8];
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int n_jobs = *pl.n_jobs;
-  if ((int)blockIdx.x * 8 >= n_jobs) return;
-  const uint2* pair = pl.sorted;
-  const int col = (blockIdx.y * 32 + lane) * 4;
-  const int job = blockIdx.x * 8 + warp;
-  // tiles after the first one that the token reaches into
-  int more = 0;
-  if (job < n_jobs) {
-    const int t = pl.jobs[job];
-    const unsigned key = pair[(long long)(t + 1) * pl.rows - 1].x;
-    for (int base = t + 1;; base += 32) {
-      const int u = base + lane;
-      const bool on = u < pl.tiles && pair[(long long)u * pl.rows].x == key;
-      const unsigned m = __ballot_sync(0xffffffffu, on);
-      if (m != 0xffffffffu) { more += __ffs(~m) - 1; break; }
-      more += 32;
-    }
+// Zeros into the rows of the tokens from v0 on, EJ_WARPS of them, that do not occur.
+__device__ void zero_absent_rows(const EmbedPlan& pl, float* __restrict__ grad, long long v0) {
+  const long long v = v0 + (threadIdx.x >> 5);
+  const int lane = threadIdx.x & 31;
+  if (v >= pl.vocab || pl.present[v]) return;
+  float* g = grad + v * pl.d;
+  if (!((uintptr_t)grad & 15) && pl.d % 4 == 0) {
+    for (int c = lane * 4; c < pl.d; c += 128) __stcs(reinterpret_cast<float4*>(g + c), make_float4(0.f, 0.f, 0.f, 0.f));
+  } else {
+    for (int c = lane; c < pl.d; c += 32) g[c] = 0.f;
   }
-  if (lane == 0) span[warp] = more;
-  __syncthreads();
+}
+
+// The first blocks: one warp per token that left parts and 128 columns; a token over more than 16 tiles is shared by the
+// block's warps.  The others write the rows of absent tokens: stores that need HBM and little else, next to sums that wait
+// for one load after the other.
+__global__ void __launch_bounds__(EJ_WARPS * 32)
+embed_join_kernel(const EmbedPlan pl, float scale, float* __restrict__ grad, int accumulate, int groups, int slabs) {
+  __shared__ float4 sum[EJ_WARPS][32];
+  __shared__ unsigned key[EJ_WARPS];
+  __shared__ int first[EJ_WARPS], span[EJ_WARPS];           // tiles: the first one, how many
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  wait_for_predecessor();
+  if ((int)blockIdx.x >= groups * slabs) {
+    zero_absent_rows(pl, grad, (long long)(blockIdx.x - groups * slabs) * EJ_WARPS);
+    return;
+  }
+  const int n_jobs = *pl.n_jobs;
+  const int group = blockIdx.x / slabs, col = ((blockIdx.x - group * slabs) * 32 + lane) * 4;
+  const bool in = col < pl.d;                 // partial rows are padded to a multiple of four
   auto add_tiles = [&](float4& a, int t, int lo, int hi) {      // partial sums of tiles t + lo .. t + hi - 1 (0: the first tile)
-#pragma unroll 4
+#pragma unroll 8
     for (int k = lo; k < hi; ++k) {
       const float* q = pl.part + ((long long)(t + k) * 2 + (k == 0 ? 1 : 0)) * pl.dpad + col;
       const float4 w = *reinterpret_cast<const float4*>(q);
       a.x += w.x; a.y += w.y; a.z += w.z; a.w += w.w;
     }
   };
-  auto finish = [&](const float4& a, int t) {
-    const unsigned key = pair[(long long)(t + 1) * pl.rows - 1].x;
+  auto finish = [&](const float4& a, unsigned key) {
     float* g = grad + (long long)key * pl.d + col;
     const float v[4] = {a.x * scale, a.y * scale, a.z * scale, a.w * scale};
 #pragma unroll
     for (int e = 0; e < 4; ++e)
       if (col + e < pl.d) g[e] = accumulate ? g[e] + v[e] : v[e];
   };
-  const bool in = col < pl.d;                 // partial rows are padded to a multiple of four
-  if (job < n_jobs && span[warp] <= 16 && in) {
-    float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
-    const int t = pl.jobs[job];
-    add_tiles(a, t, 0, span[warp] + 1);
-    finish(a, t);
-  }
-  for (int j = 0; j < 8; ++j) {
-    if (span[j] <= 16) continue;              // the same for the whole block
-    const int t = pl.jobs[blockIdx.x * 8 + j], len = span[j] + 1;
-    float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (in) add_tiles(a, t, len * warp / 8, len * (warp + 1) / 8);
-    sum[warp][lane] = a;
-    __syncthreads();
-    if (warp == 0 && in) {
-      for (int w = 1; w < 8; ++w) {
-        const float4 b = sum[w][lane];
-        a.x += b.x; a.y += b.y; a.z += b.z; a.w += b.w;
+  for (int base = group * EJ_WARPS; base < n_jobs; base += groups * EJ_WARPS) {
+    if (base + warp < n_jobs) {
+      const uint2 job = pl.jobs[base + warp];
+      const int t = pl.first_tile[job.x], len = (int)job.y - t + 1;
+      if (lane == 0) { key[warp] = job.x; first[warp] = t; span[warp] = len; }
+      if (len <= 16 && in) {
+        float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
+        add_tiles(a, t, 0, len);
+        finish(a, job.x);
       }
-      finish(a, t);
+    } else if (lane == 0) {
+      span[warp] = 0;
+    }
+    __syncthreads();
+    for (int j = 0; j < EJ_WARPS; ++j) {
+      const int len = span[j];
+      if (len <= 16) continue;                // the same for the whole block
+      float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (in) add_tiles(a, first[j], (int)((long long)len * warp / EJ_WARPS), (int)((long long)len * (warp + 1) / EJ_WARPS));
+      sum[warp][lane] = a;
+      __syncthreads();
+      if (warp == 0 && in) {
+        for (int w = 1; w < EJ_WARPS; ++w) {
+          const float4 b = sum[w][lane];
+          a.x += b.x; a.y += b.y; a.z += b.z; a.w += b.w;
+        }
+        finish(a, key[j]);
+      }
+      __syncthreads();
     }
     __syncthreads();
   }
@@ -422,17 +500,47 @@ struct LogpParams {
   unsigned* status;
 };
 
-template <typename T>
-__device__ __forceinline__ void part_add(VocabStat& st, const float (&v)[Vec16<T>::N], float c) {
-  constexpr int N = Vec16<T>::N;
-#pragma unroll
-  for (int e = 0; e < N; ++e) {
-    const float t = fmaxf((v[e] - st.m) * c, -1000.f);
-    const float x = ex2(t);
-    st.s += x;
-    st.w += x * t;
-  }
+// Two fp32 lanes of one 64-bit register: half the issue slots of scalar adds and products.
+__device__ __forceinline__ unsigned long long pack2(float a, float b) {
+  unsigned long long r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+  return r;
 }
+__device__ __forceinline__ void unpack2(unsigned long long v, float& a, float& b) {
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v));
+}
+__device__ __forceinline__ unsigned long long add2(unsigned long long a, unsigned long long b) {
+  unsigned long long r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ unsigned long long mul2(unsigned long long a, unsigned long long b) {
+  unsigned long long r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ unsigned long long fma2(unsigned long long a, unsigned long long b, unsigned long long c) {
+  unsigned long long r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+// Largest of a 16-byte vector's elements, NaN if one is.
+template <typename T> __device__ __forceinline__ float vec_max(const uint4& r);
+template <> __device__ __forceinline__ float vec_max<float>(const uint4& r) {
+  return max_nan(max_nan(__uint_as_float(r.x), __uint_as_float(r.y)), max_nan(__uint_as_float(r.z), __uint_as_float(r.w)));
+}
+__device__ __forceinline__ uint32_t max2_bf16(uint32_t a, uint32_t b) {
+  uint32_t r;
+  asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
+template <> __device__ __forceinline__ float vec_max<__nv_bfloat16>(const uint4& r) {
+  const uint32_t w = max2_bf16(max2_bf16(r.x, r.y), max2_bf16(r.z, r.w));
+  return max_nan(__uint_as_float(w << 16), __uint_as_float(w & 0xFFFF0000u));
+}
+template <typename T> __device__ __forceinline__ uint4 vec_of_minus_inf();
+template <> __device__ __forceinline__ uint4 vec_of_minus_inf<float>() { return make_uint4(0xFF800000u, 0xFF800000u, 0xFF800000u, 0xFF800000u); }
+template <> __device__ __forceinline__ uint4 vec_of_minus_inf<__nv_bfloat16>() { return make_uint4(0xFF80FF80u, 0xFF80FF80u, 0xFF80FF80u, 0xFF80FF80u); }
 
 // A row (or a cluster rank's share of it) as 16-byte vectors plus up to N - 1 single elements before and after.
 template <typename T>
@@ -467,10 +575,13 @@ constexpr int LP_MAX_RANKS = 8;
 // NT threads work on one row's share.  NT = 32: a warp per row, several rows per block.  Otherwise one block per share,
 // `ranks` blocks of a cluster per row.
 template <int NT> struct LogpSmem {
-  static constexpr int CAP = NT == 32 ? 128 : 1024;
+  static constexpr int CAP = NT == 32 ? 128 : 256;
+  static constexpr int W = NT / 32;
   unsigned long long cand[CAP];               // candidates of the top list: order_of(z) above, ~index below
+  unsigned long long warp_best[W];
   unsigned group_max[32];
-  VocabStat part[32];
+  VocabStat part[W];
+  int warp_count[W];
   int n_cand;
   unsigned long long best[NT == 32 ? 1 : LP_MAX_RANKS * LP_MAX_TOP];   // rank 0: the shares' own top lists
   VocabStat share[NT == 32 ? 1 : LP_MAX_RANKS];
@@ -480,11 +591,143 @@ template <int NT> __device__ __forceinline__ void row_sync() {
   if constexpr (NT == 32) __syncwarp(); else __syncthreads();
 }
 
+__device__ __forceinline__ unsigned long long top_key(float z, int idx) {
+  return ((unsigned long long)order_of(z) << 32) | (0xFFFFFFFFu - (unsigned)idx);
+}
+
+// The `top` largest elements of a share into sm.cand[0 .. returned), unordered (all of them when the share has fewer).
+//   1. The threads form 32 groups; the top-th largest of the groups' maxima, `limit`, is a value that at least `top`
+//      elements reach.  Few threads have a maximum that reaches it: their elements are read again, a warp at a time, and
+//      those that do go on the list.
+//   2. If they do not fit (many equal values: a constant row, a mask that leaves fewer than `top`), the list takes what
+//      lies above the limit, and then elements equal to it, in ascending order, until it has `top`.
+//   3. If not even those fit, one search of the share for each place.
 template <typename T, int NT>
+__device__ __noinline__ int top_list(LogpSmem<NT>& sm, const RowShare<T>& sh, float own, int tid, int top) {
+  using V16 = Vec16<T>;
+  constexpr int N = V16::N, W = NT / 32, CAP = LogpSmem<NT>::CAP;
+  const int lane = tid & 31, warp = tid >> 5;
+  const unsigned own_max = order_of(own);
+  unsigned limit = 0;
+  {
+    unsigned mine = sm.group_max[lane];
+    for (int k = 0; k < top; ++k) {
+      limit = __reduce_max_sync(0xffffffffu, mine);
+      if (lane == __ffs(__ballot_sync(0xffffffffu, mine == limit)) - 1) mine = 0;
+    }
+  }
+  auto collect = [&](unsigned least) {        // elements of order >= least onto the list; returns how many there are
+    auto offer = [&](float z, int idx) {
+      if (order_of(z) >= least) {
+        const int at = atomicAdd(&sm.n_cand, 1);
+        if (at < CAP) sm.cand[at] = top_key(z, idx);
+      }
+    };
+    for (unsigned owners = __ballot_sync(0xffffffffu, own_max >= least); owners; owners &= owners - 1) {
+      if (*reinterpret_cast<volatile int*>(&sm.n_cand) > CAP) break;       // it has overflowed: the rest would be thrown away
+      const int owner = warp * 32 + __ffs(owners) - 1;
+      for (int v = sh.v_lo + owner + lane * NT; v < sh.v_hi; v += 32 * NT) {
+        float f[N];
+        V16::unpack(__ldg(sh.vec(v)), f);
+#pragma unroll
+        for (int k = 0; k < N; ++k) offer(f[k], sh.head + v * N + k);
+      }
+    }
+    const int e = sh.single(tid);
+    if (e >= 0) offer(as_f32(sh.p[e]), e);
+    row_sync<NT>();
+    return sm.n_cand;
+  };
+  int n = collect(limit);
+  if (n <= CAP) return n;
+  row_sync<NT>();
+  if (tid == 0) sm.n_cand = 0;
+  row_sync<NT>();
+  n = limit == 0xFFFFFFFFu ? 0 : collect(limit + 1);
+  if (n <= CAP) {
+    if (n >= top) return n;
+    const int above = n;
+    int found = 0;
+    // `bits`: which of `count` consecutive elements from `idx` on equal the limit; threads hold them in ascending order
+    auto take = [&](unsigned bits, int idx) {
+      const int own_n = __popc(bits);
+      int incl = own_n;
+#pragma unroll
+      for (int off = 1; off < 32; off <<= 1) {
+        const int o = __shfl_up_sync(0xffffffffu, incl, off);
+        incl += lane >= off ? o : 0;
+      }
+      int before = found + incl - own_n, total = __shfl_sync(0xffffffffu, incl, 31);
+      if constexpr (W > 1) {
+        if (lane == 31) sm.warp_count[warp] = incl;
+        __syncthreads();
+        total = 0;
+        for (int w = 0; w < W; ++w) {
+          before += w < warp ? sm.warp_count[w] : 0;
+          total += sm.warp_count[w];
+        }
+        __syncthreads();
+      }
+      for (; bits && above + before < top; bits &= bits - 1, ++before)
+        sm.cand[above + before] = ((unsigned long long)limit << 32) | (0xFFFFFFFFu - (unsigned)(idx + __ffs(bits) - 1));
+      found += total;
+    };
+    const int first = tid, last = sh.tail + tid;
+    take(sh.has_head && first < sh.head && order_of(as_f32(sh.p[first])) == limit ? 1u : 0u, first);
+    for (int v0 = sh.v_lo; v0 < sh.v_hi && above + found < top; v0 += NT) {
+      const int v = v0 + tid;
+      unsigned bits = 0;
+      if (v < sh.v_hi) {
+        float f[N];
+        V16::unpack(__ldg(sh.vec(v)), f);
+#pragma unroll
+        for (int k = 0; k < N; ++k) bits |= order_of(f[k]) == limit ? 1u << k : 0u;
+      }
+      take(bits, sh.head + v * N);
+    }
+    if (above + found < top) take(sh.has_tail && last < sh.V && order_of(as_f32(sh.p[last])) == limit ? 1u : 0u, last);
+    row_sync<NT>();
+    return min(top, above + found);
+  }
+  unsigned long long below = ~0ull;
+  for (int place = 0; place < top; ++place) {
+    unsigned long long best = 0;
+    auto offer = [&](float z, int idx) {
+      const unsigned long long key = top_key(z, idx);
+      if (key < below && key > best) best = key;
+    };
+    const int e = sh.single(tid);
+    if (e >= 0) offer(as_f32(sh.p[e]), e);
+#pragma unroll 4
+    for (int v = sh.v_lo + tid; v < sh.v_hi; v += NT) {
+      float f[N];
+      V16::unpack(__ldg(sh.vec(v)), f);
+#pragma unroll
+      for (int k = 0; k < N; ++k) offer(f[k], sh.head + v * N + k);
+    }
+#pragma unroll
+    for (int off = 16; off; off >>= 1) {
+      const unsigned long long o = __shfl_xor_sync(0xffffffffu, best, off);
+      best = o > best ? o : best;
+    }
+    if constexpr (W > 1) {
+      __syncthreads();
+      if (lane == 0) sm.warp_best[warp] = best;
+      __syncthreads();
+      for (int w = 0; w < W; ++w) best = sm.warp_best[w] > best ? sm.warp_best[w] : best;
+    }
+    if (tid == 0) sm.cand[place] = best;
+    below = best;
+  }
+  row_sync<NT>();
+  return top;                                 // more than CAP elements lie above the limit, so there are `top`
+}
+
+template <typename T, int NT, bool TOP>
 __global__ void __launch_bounds__(NT == 32 ? 256 : NT)
 token_logp_kernel(const LogpParams p, int ranks) {
   using V16 = Vec16<T>;
-  constexpr int N = V16::N, U = 4;
+  constexpr int N = V16::N, U = 4, W = NT / 32;
   constexpr int ROWS = NT == 32 ? 8 : 1;
   __shared__ LogpSmem<NT> smem_all[ROWS];
   LogpSmem<NT>& sm = smem_all[NT == 32 ? threadIdx.x >> 5 : 0];
@@ -496,7 +739,7 @@ token_logp_kernel(const LogpParams p, int ranks) {
   const float c = p.inv_t * VOCAB_LOG2E;
   const int t = p.tok ? p.tok[row] : 0;
   const bool bad = p.tok && t >= p.V, skip = p.tok && (t < 0 || bad);
-  const int top = p.top;
+  const int top = TOP ? p.top : 0;
   if (skip) {                                 // the same for every thread of the row, every rank of its cluster
     if (rank == 0) {
       if (tid == 0) {
@@ -512,145 +755,101 @@ token_logp_kernel(const LogpParams p, int ranks) {
   const RowShare<T> sh(reinterpret_cast<const T*>(p.logits) + row * p.ld, p.V, rank, ranks);
   if (tid == 0) sm.n_cand = 0;
 
-  // ---- one pass over the share -------------------------------------------------------------------
-  VocabStat st{-INFINITY, 0.f, 0.f};
+  // ---- one pass over the share: U vectors at a time, the next U on their way --------------------------------
+  // Missing vectors read as -inf, which adds nothing (-inf - m, NaN when m is -inf too, is held at -1000).
+  float m = -INFINITY;
+  unsigned long long s2 = pack2(0.f, 0.f), w2 = s2;
+  const unsigned long long c2 = pack2(c, c);
   {
     const int e = sh.single(tid);
     if (e >= 0) {
-      const float z = as_f32(sh.p[e]);
-      st.m = z;
-      const float x = z == -INFINITY ? 0.f : 1.f;
-      st.s = x;
+      m = as_f32(sh.p[e]);
+      s2 = pack2(m == -INFINITY ? 0.f : 1.f, 0.f);
     }
   }
+  uint4 next[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u) next[u] = sh.v_lo + tid + u * NT < sh.v_hi ? __ldg(sh.vec(sh.v_lo + tid + u * NT)) : vec_of_minus_inf<T>();
   for (int v0 = sh.v_lo + tid; v0 < sh.v_hi; v0 += U * NT) {
     uint4 r[U];
 #pragma unroll
-    for (int u = 0; u < U; ++u)
-      if (v0 + u * NT < sh.v_hi) r[u] = __ldg(sh.vec(v0 + u * NT));
-    float bm = -INFINITY;
+    for (int u = 0; u < U; ++u) r[u] = next[u];
 #pragma unroll
-    for (int u = 0; u < U; ++u)
-      if (v0 + u * NT < sh.v_hi) {
-        float f[N];
-        V16::unpack(r[u], f);
-#pragma unroll
-        for (int e = 0; e < N; ++e) bm = max_nan(bm, f[e]);
-      }
-    stat_raise(st, bm, c);
-    if (st.m != -INFINITY) {
-#pragma unroll
-      for (int u = 0; u < U; ++u)
-        if (v0 + u * NT < sh.v_hi) {
-          float f[N];
-          V16::unpack(r[u], f);
-          part_add<T>(st, f, c);
-        }
+    for (int u = 0; u < U; ++u) {
+      const int v = v0 + (U + u) * NT;
+      next[u] = v < sh.v_hi ? __ldg(sh.vec(v)) : vec_of_minus_inf<T>();
     }
-  }
-
-  // ---- join the threads -----------------------------------------------------------------------------
-  const unsigned own_max = order_of(st.m);    // -inf where the thread has no element: never above an element's
-  if (top > 0) {
-    unsigned g = own_max;
+    float bm = vec_max<T>(r[0]);
 #pragma unroll
-    for (int off = 1; off < NT / 32; off <<= 1) g = max(g, __shfl_xor_sync(0xffffffffu, g, off));
-    if (tid % (NT / 32) == 0) sm.group_max[tid / (NT / 32)] = g;
-  }
-#pragma unroll
-  for (int off = 16; off; off >>= 1) {
-    VocabStat o;
-    o.m = __shfl_xor_sync(0xffffffffu, st.m, off);
-    o.s = __shfl_xor_sync(0xffffffffu, st.s, off);
-    o.w = __shfl_xor_sync(0xffffffffu, st.w, off);
-    st = stat_join(st, o, c);
-  }
-  if (lane == 0) sm.part[tid >> 5] = st;
-  row_sync<NT>();
-  if (NT > 32) {
-    st = lane < NT / 32 ? sm.part[lane] : VocabStat{-INFINITY, 0.f, 0.f};
-#pragma unroll
-    for (int off = 16; off; off >>= 1) {
-      VocabStat o;
-      o.m = __shfl_xor_sync(0xffffffffu, st.m, off);
-      o.s = __shfl_xor_sync(0xffffffffu, st.s, off);
-      o.w = __shfl_xor_sync(0xffffffffu, st.w, off);
-      st = stat_join(st, o, c);
+    for (int u = 1; u < U; ++u) bm = max_nan(bm, vec_max<T>(r[u]));
+    bm = max_nan(bm, m);
+    if (bm != m) {
+      const float d = fmaxf((m - bm) * c, -1000.f), f = ex2(d);
+      const unsigned long long f2 = pack2(f, f);
+      w2 = mul2(f2, fma2(s2, pack2(d, d), w2));
+      s2 = mul2(f2, s2);
+      m = bm;
     }
-  }
-
-  // Every thread takes lane 0's result: the lanes join in different orders, and which lane writes a place of the top
-  // list is decided by an atomic counter.
-  st.m = __shfl_sync(0xffffffffu, st.m, 0);
-  st.s = __shfl_sync(0xffffffffu, st.s, 0);
-  st.w = __shfl_sync(0xffffffffu, st.w, 0);
-
-  // ---- top list of the share ---------------------------------------------------------------------
-  // The threads form 32 groups; the top-th largest of the groups' maxima is a value that at least `top` elements
-  // reach.  Only threads whose own maximum reaches it read their elements again (from L2) and put those that do on a
-  // list, whose members find their places by counting.  A list that overflows (many equal values, a mask that leaves
-  // fewer than `top`) falls back to one search of the share for each place.
-  int n = 0;
-  bool overflow = false;
-  if (top > 0) {
-    const unsigned mine = sm.group_max[lane];
-    int place = 0;
+    const unsigned long long neg_m = pack2(-m, -m);
 #pragma unroll
-    for (int j = 0; j < 32; ++j) {
-      const unsigned o = __shfl_sync(0xffffffffu, mine, j);
-      place += (o > mine || (o == mine && j < lane)) ? 1 : 0;
-    }
-    const unsigned limit = __shfl_sync(0xffffffffu, mine, __ffs(__ballot_sync(0xffffffffu, place == top - 1)) - 1);
-    if (own_max >= limit) {
-      auto offer = [&](float z, int idx) {
-        const unsigned o = order_of(z);
-        if (o >= limit) {
-          const int at = atomicAdd(&sm.n_cand, 1);
-          if (at < LogpSmem<NT>::CAP) sm.cand[at] = ((unsigned long long)o << 32) | (0xFFFFFFFFu - (unsigned)idx);
-        }
-      };
-      const int e = sh.single(tid);
-      if (e >= 0) offer(as_f32(sh.p[e]), e);
-      for (int v = sh.v_lo + tid; v < sh.v_hi; v += NT) {
-        float f[N];
-        V16::unpack(__ldg(sh.vec(v)), f);
-#pragma unroll
-        for (int k = 0; k < N; ++k) offer(f[k], sh.head + v * N + k);
-      }
-    }
-    row_sync<NT>();
-    n = sm.n_cand;
-    overflow = n > LogpSmem<NT>::CAP;
-  }
-  auto search = [&](unsigned long long below) {          // largest key of the share under `below`, 0 when there is none
-    unsigned long long best = 0;
-    auto offer = [&](float z, int idx) {
-      const unsigned long long key = ((unsigned long long)order_of(z) << 32) | (0xFFFFFFFFu - (unsigned)idx);
-      if (key < below && key > best) best = key;
-    };
-    const int e = sh.single(tid);
-    if (e >= 0) offer(as_f32(sh.p[e]), e);
-    for (int v = sh.v_lo + tid; v < sh.v_hi; v += NT) {
+    for (int u = 0; u < U; ++u) {
       float f[N];
-      V16::unpack(__ldg(sh.vec(v)), f);
+      V16::unpack(r[u], f);
 #pragma unroll
-      for (int k = 0; k < N; ++k) offer(f[k], sh.head + v * N + k);
+      for (int e = 0; e < N; e += 2) {
+        float t0, t1;
+        unpack2(mul2(add2(pack2(f[e], f[e + 1]), neg_m), c2), t0, t1);
+        t0 = fmaxf(t0, -1000.f);
+        t1 = fmaxf(t1, -1000.f);
+        const unsigned long long x2 = pack2(ex2(t0), ex2(t1));
+        s2 = add2(s2, x2);
+        w2 = fma2(x2, pack2(t0, t1), w2);
+      }
     }
+  }
+
+  // ---- join the threads: lanes against their common maximum, then the warps one after the other --------------
+  if constexpr (TOP) {
+    unsigned g = order_of(m);                 // -inf where the thread has no element: never above an element's
+#pragma unroll
+    for (int off = 1; off < W; off <<= 1) g = max(g, __shfl_xor_sync(0xffffffffu, g, off));
+    if (tid % W == 0) sm.group_max[tid / W] = g;
+  }
+  VocabStat st;
+  {
+    float a, b, wa, wb;
+    unpack2(s2, a, b);
+    unpack2(w2, wa, wb);
+    float s = a + b, w = wa + wb;
+    asm("redux.sync.max.NaN.f32 %0, %1, 0xffffffff;" : "=f"(st.m) : "f"(m));
+    const float d = m == st.m ? 0.f : fmaxf((m - st.m) * c, -1000.f), f = ex2(d);
+    w = f * (w + s * d);
+    s *= f;
 #pragma unroll
     for (int off = 16; off; off >>= 1) {
-      const unsigned long long o = __shfl_xor_sync(0xffffffffu, best, off);
-      best = o > best ? o : best;
+      s += __shfl_xor_sync(0xffffffffu, s, off);
+      w += __shfl_xor_sync(0xffffffffu, w, off);
     }
-    if (NT > 32) {
-      __syncthreads();
-      if (lane == 0) sm.cand[tid >> 5] = best;
-      __syncthreads();
-      best = 0;
-      for (int i = 0; i < NT / 32; ++i) best = sm.cand[i] > best ? sm.cand[i] : best;
-    }
-    return best;
-  };
+    st.s = s;
+    st.w = w;
+  }
+  if constexpr (W > 1) {
+    if (lane == 0) sm.part[tid >> 5] = st;
+    __syncthreads();
+    st = sm.part[0];
+#pragma unroll
+    for (int w = 1; w < W; ++w) st = stat_join(st, sm.part[w], c);
+  } else {
+    __syncwarp();
+  }
 
+  int n = 0;
+  if constexpr (TOP) n = top_list<T, NT>(sm, sh, m, tid, top);
+  auto place_of = [&](unsigned long long key) {
+    int place = 0;
+    for (int j = 0; j < n; ++j) place += sm.cand[j] > key ? 1 : 0;
+    return place;
+  };
   auto write_top = [&](const RowResult& res, int place, unsigned long long key) {
     p.top_id[row * top + place] = (int)(0xFFFFFFFFu - (unsigned)key);
     p.top_logp[row * top + place] = res.logp(float_of_order((unsigned)(key >> 32)));
@@ -663,19 +862,10 @@ token_logp_kernel(const LogpParams p, int ranks) {
   if (NT == 32 || ranks == 1) {
     const RowResult res(st, p.inv_t);
     if (tid == 0) write_row(res);
-    if (top > 0 && !overflow) {
-      for (int i = tid; i < n; i += NT) {
-        const unsigned long long key = sm.cand[i];
-        int place = 0;
-        for (int j = 0; j < n; ++j) place += sm.cand[j] > key ? 1 : 0;
-        if (place < top) write_top(res, place, key);
-      }
-    } else if (top > 0) {
-      unsigned long long below = ~0ull;
-      for (int k = 0; k < top; ++k) {
-        below = search(below);
-        if (tid == 0) write_top(res, k, below);
-      }
+    for (int i = tid; i < n; i += NT) {
+      const unsigned long long key = sm.cand[i];
+      const int place = place_of(key);
+      if (place < top) write_top(res, place, key);
     }
     return;
   }
@@ -683,28 +873,21 @@ token_logp_kernel(const LogpParams p, int ranks) {
     // ---- join the shares of a cluster on rank 0 ----
     cluster_sync_all();                       // rank 0 runs: its shared memory may be written
     const uint32_t share0 = mapa_shared(smem_u32(&sm.share[rank]), 0);
-    const uint32_t best0 = mapa_shared(smem_u32(&sm.best[rank * LP_MAX_TOP]), 0);
-    auto put = [&](int place, unsigned long long key) {
-      asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(best0 + (uint32_t)place * 8u), "l"(key) : "memory");
-    };
     if (tid == 0) {
       asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(share0), "f"(st.m) : "memory");
       asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(share0 + 4u), "f"(st.s) : "memory");
       asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(share0 + 8u), "f"(st.w) : "memory");
     }
-    if (top > 0 && !overflow) {
-      if (tid >= n && tid < top) put(tid, 0);           // a share with fewer elements than places
+    if constexpr (TOP) {
+      const uint32_t best0 = mapa_shared(smem_u32(&sm.best[rank * LP_MAX_TOP]), 0);
+      auto put = [&](int place, unsigned long long key) {
+        asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(best0 + (uint32_t)place * 8u), "l"(key) : "memory");
+      };
+      if (tid >= n && tid < top) put(tid, 0);             // a share with fewer elements than places
       for (int i = tid; i < n; i += NT) {
         const unsigned long long key = sm.cand[i];
-        int place = 0;
-        for (int j = 0; j < n; ++j) place += sm.cand[j] > key ? 1 : 0;
+        const int place = place_of(key);
         if (place < top) put(place, key);
-      }
-    } else if (top > 0) {
-      unsigned long long below = ~0ull;
-      for (int k = 0; k < top; ++k) {
-        below = below ? search(below) : 0;
-        if (tid == 0) put(k, below);
       }
     }
     cluster_sync_all();
@@ -713,7 +896,7 @@ token_logp_kernel(const LogpParams p, int ranks) {
     for (int r = 1; r < ranks; ++r) st = stat_join(st, sm.share[r], c);
     const RowResult res(st, p.inv_t);
     if (tid == 0) write_row(res);
-    if (tid < ranks * LP_MAX_TOP && tid % LP_MAX_TOP < top) {
+    if (TOP && tid < ranks * LP_MAX_TOP && tid % LP_MAX_TOP < top) {
       const unsigned long long key = sm.best[tid];
       int place = 0;
       for (int r = 0; r < ranks; ++r)
@@ -815,8 +998,29 @@ static int launch_embed(const T* table, long long ld_table, int vocab, int d, co
   return PCM_OK;
 }
 
-// Sorted pairs per tile: 64 once that leaves two blocks for each SM, fewer for short batches.
-static int embed_tile_rows(int n) { return n >= 64 * 296 ? 64 : 16; }
+// A launch that may begin before the kernel ahead of it in the stream has ended; the kernel waits for that one itself,
+// before it touches memory.
+template <typename... P, typename... A>
+static int launch_after(void (*kernel)(P...), dim3 grid, dim3 block, cudaStream_t s, A... args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid;
+  cfg.blockDim = block;
+  cfg.stream = s;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  if (cudaLaunchKernelEx(&cfg, kernel, static_cast<P>(args)...) != cudaSuccess) {
+    cudaGetLastError();
+    return PCM_ERR_CUDA;
+  }
+  g_launches.fetch_add(1, std::memory_order_relaxed);
+  return PCM_OK;
+}
+
+// Sorted pairs per tile: fewer for short batches, so that every SM gets some.
+static int embed_tile_rows(int n) { return n >= 32 * 296 ? 32 : 8; }
 
 static size_t embed_plan(EmbedPlan& pl, int n, int vocab, int d, void* ws) {
   pl.n = n; pl.vocab = vocab; pl.d = d;
@@ -831,9 +1035,14 @@ static size_t embed_plan(EmbedPlan& pl, int n, int vocab, int d, void* ws) {
   };
   pl.buf[0] = (uint2*)take((size_t)n * 8);
   pl.buf[1] = (uint2*)take((size_t)n * 8);
+  pl.keys = ceil_div(ceil_div(n, ES_MAX_BLOCKS), ES_THREADS) * ES_THREADS;
+  if (pl.keys < ES_THREADS) pl.keys = ES_THREADS;
+  pl.blocks = ceil_div(n, pl.keys);
   pl.present = (uint8_t*)take((size_t)vocab);
+  pl.hist = (unsigned*)take((size_t)pl.blocks * ES_BINS * 4);
   pl.n_jobs = (int*)take(4);
-  pl.jobs = (int*)take((size_t)pl.tiles * 4);
+  pl.jobs = (uint2*)take((size_t)pl.tiles * 8);
+  pl.first_tile = (int*)take((size_t)vocab * 4);
   pl.part = (float*)take((size_t)pl.tiles * 2 * pl.dpad * 4);
   return off;
 }
@@ -843,66 +1052,75 @@ static int launch_embed_bwd(const T* dout, long long ld, const int* tok, int n, 
                             float* grad, unsigned* status, void* ws, cudaStream_t s) {
   EmbedPlan pl;
   embed_plan(pl, n, vocab, d, ws);
-  int key_bits = 1;
-  while ((vocab >> key_bits) != 0) ++key_bits;                     // keys 0 .. vocab
-  const int passes = ceil_div(key_bits, 8), bits = ceil_div(key_bits, passes);
-  pl.sorted = pl.buf[(passes - 1) & 1];
-  const int ranks = n > 8192 ? ES_MAX_RANKS : 1;                   // one block sorts a short batch sooner than eight that exchange counts
+  if (n <= ES_THREADS) {
+    int threads = 128;
+    while (threads < n) threads *= 2;
+    if (vocab < (1 << 22) - 1) embed_sort_small_kernel<unsigned, 10><<<1, threads, 0, s>>>(tok, pl, status);
+    else embed_sort_small_kernel<unsigned long long, 32><<<1, threads, 0, s>>>(tok, pl, status);
+    PCM_LAUNCH_CHECK();
+    pl.sorted = pl.buf[0];
+  } else {
+    int key_bits = 1;
+    while ((vocab >> key_bits) != 0) ++key_bits;                   // keys 0 .. vocab
+    const int passes = ceil_div(key_bits, 8), bits = ceil_div(key_bits, passes);
+    pl.sorted = pl.buf[(passes - 1) & 1];
+    const dim3 grid(pl.blocks), block(ES_THREADS);
+    for (int pass = 0; pass < passes; ++pass) {
+      int rc = PCM_OK;
+      if (pass == 0) {
+        embed_count_kernel<<<grid, block, 0, s>>>(tok, pl, pass, bits, status);
+        PCM_LAUNCH_CHECK();
+      } else {
+        rc = launch_after(embed_count_kernel, grid, block, s, tok, pl, pass, bits, status);
+      }
+      if (rc == PCM_OK) rc = launch_after(embed_scatter_kernel, grid, block, s, tok, pl, pass, bits);
+      if (rc != PCM_OK) return rc;
+    }
+  }
+  const bool vec = !(((uintptr_t)dout | (uintptr_t)grad) & 15) && d % Vec16<T>::N == 0 && ld % Vec16<T>::N == 0;
+  const int slabs = ceil_div(d, vec ? 64 * Vec16<T>::N : 128);
+  const long long blocks = ((long long)pl.tiles * slabs + 3) / 4;
+  if (blocks > 0x7FFFFFFFll) return PCM_ERR_SHAPE;
+  const int rc = launch_after(vec ? embed_sum_kernel<T, true> : embed_sum_kernel<T, false>, dim3((unsigned)blocks), dim3(128), s, dout, ld, pl,
+                              scale, grad, accumulate, slabs);
+  if (rc != PCM_OK) return rc;
+  const int join_slabs = ceil_div(d, 128), most = ceil_div(pl.tiles, EJ_WARPS);
+  const int groups = pl.tiles <= 2 ? 0 : most < 64 ? most : 64;    // two tiles: nothing crosses two borders
+  const int join_blocks = groups * join_slabs + (accumulate ? 0 : ceil_div(vocab, EJ_WARPS));
+  if (join_blocks == 0) return PCM_OK;
+  return launch_after(embed_join_kernel, dim3(join_blocks), dim3(EJ_WARPS * 32), s, pl, scale, grad, accumulate, groups, join_slabs);
+}
+
+template <typename T, int NT>
+static int launch_logp_as(const LogpParams& p, int ranks, cudaStream_t s) {
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(ranks);
-  cfg.blockDim = dim3(ES_THREADS);
+  cfg.gridDim = dim3(NT == 32 ? (unsigned)ceil_div(p.M, 8) : (unsigned)(p.M * ranks));
+  cfg.blockDim = dim3(NT == 32 ? 256 : NT);
   cfg.stream = s;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeClusterDimension;
   attr[0].val.clusterDim.x = (unsigned)ranks; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  if (cudaLaunchKernelEx(&cfg, embed_sort_kernel, tok, pl, ranks, passes, bits, status) != cudaSuccess) {
+  const cudaError_t e = p.top > 0 ? cudaLaunchKernelEx(&cfg, token_logp_kernel<T, NT, true>, p, ranks)
+                                  : cudaLaunchKernelEx(&cfg, token_logp_kernel<T, NT, false>, p, ranks);
+  if (e != cudaSuccess) {
     cudaGetLastError();
     return PCM_ERR_CUDA;
   }
   g_launches.fetch_add(1, std::memory_order_relaxed);
-  const bool vec = !(((uintptr_t)dout | (uintptr_t)grad) & 15) && d % Vec16<T>::N == 0 && ld % Vec16<T>::N == 0;
-  const int steps = vec ? d / Vec16<T>::N : d;
-  int lg = 0;
-  while (lg < 7 && (1 << lg) < steps) ++lg;
-  const int slabs = ceil_div(steps, 1 << lg);
-  const long long tile_blocks = (long long)ceil_div(pl.tiles, 128 >> lg) * slabs;
-  const long long blocks = tile_blocks + (accumulate ? 0 : ceil_div(vocab, 32));
-  if (blocks > 0x7FFFFFFFll) return PCM_ERR_SHAPE;
-  if (vec) embed_sum_kernel<T, true><<<(unsigned)blocks, 128, 0, s>>>(dout, ld, pl, scale, grad, accumulate, lg, slabs, (int)tile_blocks);
-  else embed_sum_kernel<T, false><<<(unsigned)blocks, 128, 0, s>>>(dout, ld, pl, scale, grad, accumulate, lg, slabs, (int)tile_blocks);
-  PCM_LAUNCH_CHECK();
-  embed_join_kernel<<<dim3(ceil_div(pl.tiles, 8), ceil_div(d, 128)), 256, 0, s>>>(pl, scale, grad, accumulate);
-  PCM_LAUNCH_CHECK();
   return PCM_OK;
 }
 
+// Short rows: a warp each.  Enough rows to fill the GPU with blocks of 128: one block each (its fixed costs, reductions
+// and the top list, weigh least then).  Fewer: blocks of 512, and up to eight of them in a cluster share a row.
 template <typename T>
 static int launch_logp(const LogpParams& p, cudaStream_t s) {
-  constexpr int NT = 256;
-  if (p.V <= 1024) {
-    token_logp_kernel<T, 32><<<(unsigned)ceil_div(p.M, 8), 256, 0, s>>>(p, 1);
-    PCM_LAUNCH_CHECK();
-    return PCM_OK;
-  }
+  if (p.V <= 1024) return launch_logp_as<T, 32>(p, 1, s);
+  if (p.M >= 8 * sm_count()) return launch_logp_as<T, 128>(p, 1, s);
   int ranks = 1;
-  while (ranks < LP_MAX_RANKS && (long long)p.M * ranks * 2 <= 4ll * sm_count() && p.V / (ranks * 2) >= 2048) ranks *= 2;
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)(p.M * ranks));
-  cfg.blockDim = dim3(NT);
-  cfg.stream = s;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeClusterDimension;
-  attr[0].val.clusterDim.x = (unsigned)ranks; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = 1;
-  if (cudaLaunchKernelEx(&cfg, token_logp_kernel<T, NT>, p, ranks) != cudaSuccess) {
-    cudaGetLastError();
-    return PCM_ERR_CUDA;
-  }
-  g_launches.fetch_add(1, std::memory_order_relaxed);
-  return PCM_OK;
+  while (ranks < LP_MAX_RANKS && (long long)p.M * ranks * 2 <= 2ll * sm_count() && p.V / (ranks * 2) >= 2048) ranks *= 2;
+  return launch_logp_as<T, 512>(p, ranks, s);
 }
 
 template <typename T>

@@ -455,10 +455,12 @@ def grpo_actor_fwd_bwd(model: Model, packed: Packed, eps_low: float = 0.2, eps_h
 
 # ------------------------------------------------------------------------------------------------
 # The ends of a wider vocabulary.  These wrappers launch on the current stream of the tensors' own device and refuse
-# (PcmError) what the C calls would misread: mixed devices, other types, rows that are not contiguous.
+# (PcmError) what the C calls would misread: mixed devices, other types, rows that are not contiguous.  A call on one token
+# takes a few microseconds of GPU time, so the checks are written to cost little more.
 _DTYPES = {torch.float32: GRPO_F32, torch.bfloat16: GRPO_BF16}
 PCM_MAX_TOP = 16
 STATUS_BAD_TOKEN = 32
+_f32, _i32, _u8 = torch.float32, torch.int32, torch.uint8
 
 
 def _require(call: str, ok: bool, code: int = -1) -> None:
@@ -467,67 +469,64 @@ def _require(call: str, ok: bool, code: int = -1) -> None:
 
 
 def _matrix(call: str, t: torch.Tensor, device=None):
-    """(dtype code, address, row stride) of a device matrix with contiguous rows."""
-    _require(call, isinstance(t, torch.Tensor) and t.is_cuda and t.dim() == 2 and t.dtype in _DTYPES and
-             (device is None or t.device == device))
-    n, c = t.shape
-    ld = t.stride(0)
-    if n <= 1 or c == 0:                                       # the stride of a single row says nothing
-        ld = max(c, ld if n == 1 else 0)
-    _require(call, c <= 1 or t.stride(1) == 1 or n == 0)
-    _require(call, ld >= c)                                    # rows that overlap (an expanded view)
-    return _DTYPES[t.dtype], t.data_ptr(), ld
+    """(dtype code, address, row stride, rows, columns) of a device matrix with contiguous rows."""
+    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dim() == 2) or (device is not None and t.device != device):
+        raise PcmError(call, -1)
+    dt = _DTYPES.get(t.dtype)
+    (n, c), (ld, step) = t.shape, t.stride()
+    if n <= 1:                                                 # the stride of a single row says nothing
+        ld = max(c, ld) if n else c
+    # rows that overlap (an expanded view) are refused
+    if dt is None or ld < c or (step != 1 and c > 1 and n):
+        raise PcmError(call, -1)
+    return dt, t.data_ptr(), ld, n, c
 
 
 def _vector(call: str, t: Optional[torch.Tensor], device, dtype, n: int) -> Optional[int]:
     if t is None:
         return None
-    _require(call, isinstance(t, torch.Tensor) and t.device == device and t.dtype == dtype and t.numel() == n and
-             t.is_contiguous())
+    if not isinstance(t, torch.Tensor) or t.device != device or t.dtype != dtype or t.numel() != n or not t.is_contiguous():
+        raise PcmError(call, -1)
     return t.data_ptr()
 
 
-class _on:
-    """Makes a tensor's device current for one call; yields that device's current stream."""
-
-    def __init__(self, device):
-        self.device = device
-
-    def __enter__(self):
-        self.before = torch.cuda.current_device()
-        if self.before != self.device.index:
-            torch.cuda.set_device(self.device)
-        return torch.cuda.current_stream(self.device).cuda_stream
-
-    def __exit__(self, *exc):
-        if self.before != self.device.index:
-            torch.cuda.set_device(self.before)
+def _launch(call: str, device, fn, *args) -> None:
+    """fn(*args, stream) on `device` and its current stream."""
+    i = device.index
+    if torch._C._cuda_getDevice() == i:
+        rc = fn(*args, torch._C._cuda_getCurrentRawStream(i))
+    else:
+        with torch.cuda.device(device):
+            rc = fn(*args, torch._C._cuda_getCurrentRawStream(i))
+    if rc != 0:
+        raise PcmError(call, rc)
 
 
 def _workspace(call: str, workspace: Optional[torch.Tensor], need: int, device):
     """256-byte aligned scratch: the caller's, or a new allocation of at least `need` bytes."""
     if workspace is None:
-        workspace = torch.empty(need + 256, dtype=torch.uint8, device=device)
-    _require(call, workspace.device == device and workspace.dtype == torch.uint8 and workspace.is_contiguous(), -3)
-    off = (-workspace.data_ptr()) % 256
-    return workspace, workspace.data_ptr() + off, max(0, workspace.numel() - off)
+        workspace = torch.empty(need + 256, dtype=_u8, device=device)
+    elif workspace.device != device or workspace.dtype != _u8 or not workspace.is_contiguous():
+        raise PcmError(call, -3)
+    at = workspace.data_ptr()
+    off = -at % 256
+    return workspace, at + off, max(0, workspace.numel() - off)
 
 
 def grpo_embed(table: torch.Tensor, tok: torch.Tensor, scale: float = 1.0, out: Optional[torch.Tensor] = None,
                status: Optional[torch.Tensor] = None) -> torch.Tensor:
     """Rows scale * table[tok] as [n, d] in the table's type; zero rows for tokens outside the vocabulary."""
     call = "grpo_embed"
-    dt, tp, ld = _matrix(call, table)
-    dev = table.device
-    n, (vocab, d) = tok.numel(), table.shape
-    tk = _vector(call, tok, dev, torch.int32, n)
+    dt, tp, ld, vocab, d = _matrix(call, table)
+    dev, n = table.device, tok.numel()
     if out is None:
         out = torch.empty((n, d), dtype=table.dtype, device=dev)
-    odt, op, ldo = _matrix(call, out, dev)
-    _require(call, odt == dt and out.shape == (n, d))
-    with _on(dev) as stream:
-        _check(call, _lib.grpo_embed(dt, tp, ld, vocab, d, tk, n, scale, op, ldo,
-                                     _vector(call, status, dev, torch.int32, 1), stream))
+        op, ldo = out.data_ptr(), d
+    else:
+        odt, op, ldo, on, od = _matrix(call, out, dev)
+        _require(call, odt == dt and on == n and od == d)
+    _launch(call, dev, _lib.grpo_embed, dt, tp, ld, vocab, d, _vector(call, tok, dev, _i32, n), n, scale, op, ldo,
+            _vector(call, status, dev, _i32, 1))
     return out
 
 
@@ -540,21 +539,28 @@ def grpo_embed_bwd(dout: torch.Tensor, tok: torch.Tensor, vocab: int, scale: flo
                    workspace: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None) -> torch.Tensor:
     """fp32 gradient [vocab, d] of grpo_embed's table; with `accumulate` it is added to the given `grad`."""
     call = "grpo_embed_bwd"
-    dt, dp, ld = _matrix(call, dout)
+    dt, dp, ld, n, d = _matrix(call, dout)
     dev = dout.device
-    n, d = dout.shape
-    tk = _vector(call, tok, dev, torch.int32, n)
-    _require(call, grad is not None or not accumulate)
-    need = grpo_embed_workspace_bytes(n, vocab, d)
+    tk = _vector(call, tok, dev, _i32, n)
+    _require(call, tk is not None and (grad is not None or not accumulate))
+    need = _lib.grpo_embed_workspace_bytes(n, vocab, d)
     _require("grpo_embed_workspace_bytes", need > 0, -2)
     if grad is None:
-        grad = torch.empty((vocab, d), dtype=torch.float32, device=dev)
-    gp = _vector(call, grad, dev, torch.float32, vocab * d)
+        grad = torch.empty((vocab, d), dtype=_f32, device=dev)
+    gp = _vector(call, grad, dev, _f32, vocab * d)
     ws, wp, wn = _workspace(call, workspace, need, dev)
-    with _on(dev) as stream:
-        _check(call, _lib.grpo_embed_bwd(dt, dp, ld, tk, n, vocab, d, scale, GRPO_ACCUMULATE if accumulate else 0, gp,
-                                         _vector(call, status, dev, torch.int32, 1), wp, wn, stream))
+    _launch(call, dev, _lib.grpo_embed_bwd, dt, dp, ld, tk, n, vocab, d, scale, GRPO_ACCUMULATE if accumulate else 0, gp,
+            _vector(call, status, dev, _i32, 1), wp, wn)
     return grad
+
+
+def _out(call: str, out: Optional[Dict[str, torch.Tensor]], name: str, shape, n: int, dtype, device):
+    """(tensor, address) of one output: the caller's under `name`, or a new one."""
+    t = out.get(name) if out else None
+    if t is None:
+        t = torch.empty(shape, dtype=dtype, device=device)
+        return t, t.data_ptr()
+    return t, _vector(call, t, device, dtype, n)
 
 
 def grpo_token_logp(logits: torch.Tensor, tok: Optional[torch.Tensor], temperature: float = 1.0, top: int = 0,
@@ -562,24 +568,19 @@ def grpo_token_logp(logits: torch.Tensor, tok: Optional[torch.Tensor], temperatu
     """(logp, entropy, lse, top_id, top_logp) of logits [n, vocab] for the tokens tok [n]; the last two are None with
     top = 0, logp is None without tokens.  `out` may hold tensors to write instead (same names)."""
     call = "grpo_token_logp"
-    dt, zp, ld = _matrix(call, logits)
+    dt, zp, ld, n, vocab = _matrix(call, logits)
     dev = logits.device
-    n, vocab = logits.shape
-    out = out or {}
-
-    def take(name, shape, dtype):
-        t = out.get(name)
-        return torch.empty(shape, dtype=dtype, device=dev) if t is None else t
-    f32, i32 = torch.float32, torch.int32
-    logp = take("logp", n, f32) if tok is not None else None
-    entropy, lse = take("entropy", n, f32), take("lse", n, f32)
-    top_id, top_logp = (take("top_id", (n, top), i32), take("top_logp", (n, top), f32)) if top > 0 else (None, None)
-    with _on(dev) as stream:
-        _check(call, _lib.grpo_token_logp(dt, zp, ld, n, vocab, _vector(call, tok, dev, i32, n), temperature, top,
-                                          _vector(call, logp, dev, f32, n), _vector(call, entropy, dev, f32, n),
-                                          _vector(call, lse, dev, f32, n), _vector(call, top_id, dev, i32, n * top),
-                                          _vector(call, top_logp, dev, f32, n * top),
-                                          _vector(call, status, dev, i32, 1), stream))
+    tk = _vector(call, tok, dev, _i32, n)
+    logp = lp = top_id = ip = top_logp = tp = None
+    if tok is not None:
+        logp, lp = _out(call, out, "logp", n, n, _f32, dev)
+    entropy, ep = _out(call, out, "entropy", n, n, _f32, dev)
+    lse, sp = _out(call, out, "lse", n, n, _f32, dev)
+    if 0 < top <= PCM_MAX_TOP:                                # a larger one is refused by the call
+        top_id, ip = _out(call, out, "top_id", (n, top), n * top, _i32, dev)
+        top_logp, tp = _out(call, out, "top_logp", (n, top), n * top, _f32, dev)
+    _launch(call, dev, _lib.grpo_token_logp, dt, zp, ld, n, vocab, tk, temperature, top, lp, ep, sp, ip, tp,
+            _vector(call, status, dev, _i32, 1))
     return logp, entropy, lse, top_id, top_logp
 
 
@@ -588,19 +589,18 @@ def grpo_token_logp_bwd(logits: torch.Tensor, tok: torch.Tensor, lse: torch.Tens
                         dlogits: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None) -> torch.Tensor:
     """d loss / d logits in the logits' type; `dlogits` may be the logits themselves."""
     call = "grpo_token_logp_bwd"
-    dt, zp, ld = _matrix(call, logits)
+    dt, zp, ld, n, vocab = _matrix(call, logits)
     dev = logits.device
-    n, vocab = logits.shape
+    _require(call, tok is not None and lse is not None and dlogp is not None)
     if dlogits is None:
         dlogits = torch.empty((n, vocab), dtype=logits.dtype, device=dev)
-    ddt, dp, ldd = _matrix(call, dlogits, dev)
-    _require(call, ddt == dt and dlogits.shape == logits.shape and tok is not None and lse is not None and dlogp is not None)
-    f32 = torch.float32
-    with _on(dev) as stream:
-        _check(call, _lib.grpo_token_logp_bwd(dt, zp, ld, n, vocab, _vector(call, tok, dev, torch.int32, n), temperature,
-                                              _vector(call, lse, dev, f32, n), _vector(call, entropy, dev, f32, n),
-                                              _vector(call, dlogp, dev, f32, n), _vector(call, dentropy, dev, f32, n), dp,
-                                              ldd, _vector(call, status, dev, torch.int32, 1), stream))
+        dp, ldd = dlogits.data_ptr(), vocab
+    else:
+        ddt, dp, ldd, dn, dv = _matrix(call, dlogits, dev)
+        _require(call, ddt == dt and dn == n and dv == vocab)
+    _launch(call, dev, _lib.grpo_token_logp_bwd, dt, zp, ld, n, vocab, _vector(call, tok, dev, _i32, n), temperature,
+            _vector(call, lse, dev, _f32, n), _vector(call, entropy, dev, _f32, n), _vector(call, dlogp, dev, _f32, n),
+            _vector(call, dentropy, dev, _f32, n), dp, ldd, _vector(call, status, dev, _i32, 1))
     return dlogits
 
 
@@ -608,27 +608,31 @@ def grpo_head_logp_workspace_bytes(n: int, d: int, vocab: int) -> int:
     return int(_lib.grpo_head_logp_workspace_bytes(n, d, vocab))
 
 
+def _head_operands(call: str, x: torch.Tensor, w_h: torch.Tensor):
+    """Addresses, row strides and sizes of hidden states [n, d] and head weight [vocab, d], both bf16."""
+    dt, xp, ldx, n, d = _matrix(call, x)
+    wdt, wp, ldw, vocab, dw = _matrix(call, w_h, x.device)
+    _require(call, dt == GRPO_BF16 and wdt == GRPO_BF16 and d == dw)
+    return xp, ldx, n, d, wp, ldw, vocab
+
+
 def grpo_head_logp(x: torch.Tensor, w_h: torch.Tensor, tok: torch.Tensor, temperature: float = 1.0,
                    workspace: Optional[torch.Tensor] = None, out: Optional[Dict[str, torch.Tensor]] = None,
                    status: Optional[torch.Tensor] = None):
     """(logp, entropy, lse) of the tokens tok [n] under softmax(x w_h^T / temperature): x [n, d], w_h [vocab, d], bf16."""
     call = "grpo_head_logp"
-    dt, xp, ldx = _matrix(call, x)
+    operands = _head_operands(call, x, w_h)
+    _, _, n, d, _, _, vocab = operands
     dev = x.device
-    wdt, wp, ldw = _matrix(call, w_h, dev)
-    (n, d), (vocab, dw_) = x.shape, w_h.shape
-    _require(call, dt == wdt == GRPO_BF16 and d == dw_ and tok is not None)
-    need = grpo_head_logp_workspace_bytes(n, d, vocab)
+    _require(call, tok is not None)
+    need = _lib.grpo_head_logp_workspace_bytes(n, d, vocab)
     _require("grpo_head_logp_workspace_bytes", need > 0, -2)
     ws, wsp, wsn = _workspace(call, workspace, need, dev)
-    out = out or {}
-    f32 = torch.float32
-    logp, entropy, lse = (out[k] if k in out else torch.empty(n, dtype=f32, device=dev) for k in ("logp", "entropy", "lse"))
-    with _on(dev) as stream:
-        _check(call, _lib.grpo_head_logp(xp, ldx, n, d, wp, ldw, vocab, _vector(call, tok, dev, torch.int32, n), temperature,
-                                         _vector(call, logp, dev, f32, n), _vector(call, entropy, dev, f32, n),
-                                         _vector(call, lse, dev, f32, n), _vector(call, status, dev, torch.int32, 1), wsp, wsn,
-                                         stream))
+    logp, lp = _out(call, out, "logp", n, n, _f32, dev)
+    entropy, ep = _out(call, out, "entropy", n, n, _f32, dev)
+    lse, sp = _out(call, out, "lse", n, n, _f32, dev)
+    _launch(call, dev, _lib.grpo_head_logp, *operands, _vector(call, tok, dev, _i32, n), temperature, lp, ep, sp,
+            _vector(call, status, dev, _i32, 1), wsp, wsn)
     return logp, entropy, lse
 
 
@@ -647,31 +651,29 @@ def grpo_head_logp_bwd(x: torch.Tensor, w_h: torch.Tensor, tok: torch.Tensor, ls
     """(dx bf16 [n, d], dw fp32 [vocab, d]) of a loss with the given gradients by logp and entropy; with `accumulate` dw is
     added to.  chunk_rows = 0 takes as many rows at a time as HEAD_CHUNK_BYTES of logit gradients hold."""
     call = "grpo_head_logp_bwd"
-    dt, xp, ldx = _matrix(call, x)
+    operands = _head_operands(call, x, w_h)
+    _, _, n, d, _, _, vocab = operands
     dev = x.device
-    wdt, wp, ldw = _matrix(call, w_h, dev)
-    (n, d), (vocab, dw_) = x.shape, w_h.shape
-    _require(call, dt == wdt == GRPO_BF16 and d == dw_ and tok is not None and lse is not None and dlogp is not None)
+    _require(call, tok is not None and lse is not None and dlogp is not None)
     _require(call, chunk_rows >= 0 and (dw is not None or not accumulate))
     if chunk_rows == 0:
-        chunk_rows = max(256, HEAD_CHUNK_BYTES // (4 * vocab) // 256 * 256)
-    need = grpo_head_logp_bwd_workspace_bytes(n, d, vocab, chunk_rows)
+        chunk_rows = max(256, HEAD_CHUNK_BYTES // (4 * max(1, vocab)) // 256 * 256)
+    need = _lib.grpo_head_logp_bwd_workspace_bytes(n, d, vocab, chunk_rows)
     _require("grpo_head_logp_bwd_workspace_bytes", need > 0, -2)
     ws, wsp, wsn = _workspace(call, workspace, need, dev)
+    dxp, lddx = None, d
     if dx is None and want_dx:
         dx = torch.empty((n, d), dtype=x.dtype, device=dev)
+        dxp = dx.data_ptr()
+    elif dx is not None:
+        ddt, dxp, lddx, dn, dd = _matrix(call, dx, dev)
+        _require(call, ddt == GRPO_BF16 and dn == n and dd == d)
     if dw is None and want_dw:
-        dw = torch.empty((vocab, d), dtype=torch.float32, device=dev)
-    f32 = torch.float32
-    ddt, dxp, lddx = _matrix(call, dx, dev) if dx is not None else (GRPO_BF16, None, d)
-    _require(call, ddt == GRPO_BF16 and (dx is None or dx.shape == x.shape))
-    with _on(dev) as stream:
-        _check(call, _lib.grpo_head_logp_bwd(xp, ldx, n, d, wp, ldw, vocab, _vector(call, tok, dev, torch.int32, n), temperature,
-                                             _vector(call, lse, dev, f32, n), _vector(call, entropy, dev, f32, n),
-                                             _vector(call, dlogp, dev, f32, n), _vector(call, dentropy, dev, f32, n), chunk_rows,
-                                             GRPO_ACCUMULATE if accumulate else 0, dxp, lddx,
-                                             _vector(call, dw, dev, f32, vocab * d), _vector(call, status, dev, torch.int32, 1),
-                                             wsp, wsn, stream))
+        dw = torch.empty((vocab, d), dtype=_f32, device=dev)
+    _launch(call, dev, _lib.grpo_head_logp_bwd, *operands, _vector(call, tok, dev, _i32, n), temperature,
+            _vector(call, lse, dev, _f32, n), _vector(call, entropy, dev, _f32, n), _vector(call, dlogp, dev, _f32, n),
+            _vector(call, dentropy, dev, _f32, n), chunk_rows, GRPO_ACCUMULATE if accumulate else 0, dxp, lddx,
+            _vector(call, dw, dev, _f32, vocab * d), _vector(call, status, dev, _i32, 1), wsp, wsn)
     return dx, dw
 
 

@@ -524,18 +524,24 @@ __device__ __forceinline__ unsigned long long fma2(unsigned long long a, unsigne
   asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
   return r;
 }
-// Largest of a 16-byte vector's elements, NaN if one is.
-template <typename T> __device__ __forceinline__ float vec_max(const uint4& r);
-template <> __device__ __forceinline__ float vec_max<float>(const uint4& r) {
-  return max_nan(max_nan(__uint_as_float(r.x), __uint_as_float(r.y)), max_nan(__uint_as_float(r.z), __uint_as_float(r.w)));
+// Largest element of four 16-byte vectors, NaN if one is.
+template <typename T> __device__ __forceinline__ float batch_max(const uint4 (&r)[4]);
+template <> __device__ __forceinline__ float batch_max<float>(const uint4 (&r)[4]) {
+  float m = __uint_as_float(r[0].x);
+#pragma unroll
+  for (int u = 0; u < 4; ++u)
+    m = max_nan(max_nan(m, max_nan(__uint_as_float(r[u].x), __uint_as_float(r[u].y))), max_nan(__uint_as_float(r[u].z), __uint_as_float(r[u].w)));
+  return m;
 }
 __device__ __forceinline__ uint32_t max2_bf16(uint32_t a, uint32_t b) {
   uint32_t r;
   asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
   return r;
 }
-template <> __device__ __forceinline__ float vec_max<__nv_bfloat16>(const uint4& r) {
-  const uint32_t w = max2_bf16(max2_bf16(r.x, r.y), max2_bf16(r.z, r.w));
+template <> __device__ __forceinline__ float batch_max<__nv_bfloat16>(const uint4 (&r)[4]) {
+  uint32_t w = r[0].x;
+#pragma unroll
+  for (int u = 0; u < 4; ++u) w = max2_bf16(max2_bf16(w, max2_bf16(r[u].x, r[u].y)), max2_bf16(r[u].z, r[u].w));
   return max_nan(__uint_as_float(w << 16), __uint_as_float(w & 0xFFFF0000u));
 }
 template <typename T> __device__ __forceinline__ uint4 vec_of_minus_inf();
@@ -599,31 +605,37 @@ __device__ __forceinline__ unsigned long long top_key(float z, int idx) {
 //   1. The threads form 32 groups; the top-th largest of the groups' maxima, `limit`, is a value that at least `top`
 //      elements reach.  Few threads have a maximum that reaches it: their elements are read again, a warp at a time, and
 //      those that do go on the list.
-//   2. If they do not fit (many equal values: a constant row, a mask that leaves fewer than `top`), the list takes what
-//      lies above the limit, and then elements equal to it, in ascending order, until it has `top`.
+//   2. If they do not fit (many equal values: a constant row, a mask that leaves fewer than `top`) or there is a NaN, the
+//      list takes what lies above the limit, and then elements equal to it, in ascending order, until it has `top`.
 //   3. If not even those fit, one search of the share for each place.
+template <int NT>
+__device__ __forceinline__ unsigned top_limit(LogpSmem<NT>& sm, int lane, int top) {
+  unsigned mine = sm.group_max[lane], limit = 0;
+  for (int k = 0; k < top; ++k) {
+    limit = __reduce_max_sync(0xffffffffu, mine);
+    if (lane == __ffs(__ballot_sync(0xffffffffu, mine == limit)) - 1) mine = 0;
+  }
+  return limit;
+}
+
 template <typename T, int NT>
-__device__ __noinline__ int top_list(LogpSmem<NT>& sm, const RowShare<T>& sh, float own, int tid, int top) {
+__device__ __noinline__ int top_list_slow(LogpSmem<NT>& sm, const RowShare<T>& sh, float own, int tid, int top, unsigned limit) {
   using V16 = Vec16<T>;
   constexpr int N = V16::N, W = NT / 32, CAP = LogpSmem<NT>::CAP;
   const int lane = tid & 31, warp = tid >> 5;
   const unsigned own_max = order_of(own);
-  unsigned limit = 0;
-  {
-    unsigned mine = sm.group_max[lane];
-    for (int k = 0; k < top; ++k) {
-      limit = __reduce_max_sync(0xffffffffu, mine);
-      if (lane == __ffs(__ballot_sync(0xffffffffu, mine == limit)) - 1) mine = 0;
-    }
-  }
-  auto collect = [&](unsigned least) {        // elements of order >= least onto the list; returns how many there are
+  row_sync<NT>();
+  if (tid == 0) sm.n_cand = 0;
+  row_sync<NT>();
+  int n = 0;
+  if (limit != 0xFFFFFFFFu) {                 // elements above the limit; nothing is above a NaN
     auto offer = [&](float z, int idx) {
-      if (order_of(z) >= least) {
+      if (order_of(z) > limit) {
         const int at = atomicAdd(&sm.n_cand, 1);
         if (at < CAP) sm.cand[at] = top_key(z, idx);
       }
     };
-    for (unsigned owners = __ballot_sync(0xffffffffu, own_max >= least); owners; owners &= owners - 1) {
+    for (unsigned owners = __ballot_sync(0xffffffffu, own_max > limit); owners; owners &= owners - 1) {
       if (*reinterpret_cast<volatile int*>(&sm.n_cand) > CAP) break;       // it has overflowed: the rest would be thrown away
       const int owner = warp * 32 + __ffs(owners) - 1;
       for (int v = sh.v_lo + owner + lane * NT; v < sh.v_hi; v += 32 * NT) {
@@ -636,14 +648,8 @@ __device__ __noinline__ int top_list(LogpSmem<NT>& sm, const RowShare<T>& sh, fl
     const int e = sh.single(tid);
     if (e >= 0) offer(as_f32(sh.p[e]), e);
     row_sync<NT>();
-    return sm.n_cand;
-  };
-  int n = collect(limit);
-  if (n <= CAP) return n;
-  row_sync<NT>();
-  if (tid == 0) sm.n_cand = 0;
-  row_sync<NT>();
-  n = limit == 0xFFFFFFFFu ? 0 : collect(limit + 1);
+    n = sm.n_cand;
+  }
   if (n <= CAP) {
     if (n >= top) return n;
     const int above = n;
@@ -734,12 +740,12 @@ token_logp_kernel(const LogpParams p, int ranks) {
   const int tid = NT == 32 ? threadIdx.x & 31 : threadIdx.x;
   const int lane = threadIdx.x & 31;
   const int rank = NT == 32 || ranks == 1 ? 0 : (int)cluster_ctarank();
+  const float c = p.inv_t * VOCAB_LOG2E;
+  const int top = TOP ? p.top : 0;
   const long long row = NT == 32 ? (long long)blockIdx.x * ROWS + (threadIdx.x >> 5) : blockIdx.x / ranks;
   if (row >= p.M) return;                     // whole warps (NT = 32) only: the grid is exact otherwise
-  const float c = p.inv_t * VOCAB_LOG2E;
   const int t = p.tok ? p.tok[row] : 0;
   const bool bad = p.tok && t >= p.V, skip = p.tok && (t < 0 || bad);
-  const int top = TOP ? p.top : 0;
   if (skip) {                                 // the same for every thread of the row, every rank of its cluster
     if (rank == 0) {
       if (tid == 0) {
@@ -756,7 +762,7 @@ token_logp_kernel(const LogpParams p, int ranks) {
   if (tid == 0) sm.n_cand = 0;
 
   // ---- one pass over the share: U vectors at a time, the next U on their way --------------------------------
-  // Missing vectors read as -inf, which adds nothing (-inf - m, NaN when m is -inf too, is held at -1000).
+  // The exponent is held at -1000 or above, so that -inf (and -inf - -inf, a NaN) adds 0 to both sums.
   float m = -INFINITY;
   unsigned long long s2 = pack2(0.f, 0.f), w2 = s2;
   const unsigned long long c2 = pack2(c, c);
@@ -767,22 +773,8 @@ token_logp_kernel(const LogpParams p, int ranks) {
       s2 = pack2(m == -INFINITY ? 0.f : 1.f, 0.f);
     }
   }
-  uint4 next[U];
-#pragma unroll
-  for (int u = 0; u < U; ++u) next[u] = sh.v_lo + tid + u * NT < sh.v_hi ? __ldg(sh.vec(sh.v_lo + tid + u * NT)) : vec_of_minus_inf<T>();
-  for (int v0 = sh.v_lo + tid; v0 < sh.v_hi; v0 += U * NT) {
-    uint4 r[U];
-#pragma unroll
-    for (int u = 0; u < U; ++u) r[u] = next[u];
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int v = v0 + (U + u) * NT;
-      next[u] = v < sh.v_hi ? __ldg(sh.vec(v)) : vec_of_minus_inf<T>();
-    }
-    float bm = vec_max<T>(r[0]);
-#pragma unroll
-    for (int u = 1; u < U; ++u) bm = max_nan(bm, vec_max<T>(r[u]));
-    bm = max_nan(bm, m);
+  auto use = [&](const uint4 (&r)[U]) {
+    const float bm = max_nan(batch_max<T>(r), m);
     if (bm != m) {
       const float d = fmaxf((m - bm) * c, -1000.f), f = ex2(d);
       const unsigned long long f2 = pack2(f, f);
@@ -805,6 +797,31 @@ token_logp_kernel(const LogpParams p, int ranks) {
         s2 = add2(s2, x2);
         w2 = fma2(x2, pack2(t0, t1), w2);
       }
+    }
+  };
+  {
+    const uint4* q = sh.vec(sh.v_lo + tid);
+    const int full = (sh.v_hi - sh.v_lo) / (U * NT);
+    auto load = [&](uint4 (&r)[U]) {
+#pragma unroll
+      for (int u = 0; u < U; ++u) r[u] = __ldg(q + u * NT);
+      q += U * NT;
+    };
+    uint4 a[U], b[U];
+    if (full > 0) load(a);
+    for (int k = 0; k < full; k += 2) {
+      if (k + 1 < full) load(b);
+      use(a);
+      if (k + 1 < full) {
+        if (k + 2 < full) load(a);
+        use(b);
+      }
+    }
+    const int rest = sh.v_hi - sh.v_lo - full * (U * NT);
+    if (rest > 0) {                           // missing vectors read as -inf, which adds nothing
+#pragma unroll
+      for (int u = 0; u < U; ++u) a[u] = tid + u * NT < rest ? __ldg(q + u * NT) : vec_of_minus_inf<T>();
+      use(a);
     }
   }
 
@@ -844,7 +861,59 @@ token_logp_kernel(const LogpParams p, int ranks) {
   }
 
   int n = 0;
-  if constexpr (TOP) n = top_list<T, NT>(sm, sh, m, tid, top);
+  if constexpr (TOP) {
+    const unsigned limit = top_limit<NT>(sm, lane, top);
+    bool slow = st.m != st.m;
+    if (!slow) {
+      const float least = float_of_order(limit);
+      auto put = [&](float z, int idx) {
+        const int at = atomicAdd(&sm.n_cand, 1);
+        if (at < LogpSmem<NT>::CAP) sm.cand[at] = top_key(z, idx);
+      };
+      unsigned owners = __ballot_sync(0xffffffffu, m >= least);
+      // nearly every thread of a warp: a constant or masked share, which would only flood the list
+      if (W > 1 && __popc(owners) > 24) {
+        if (lane == 0) atomicAdd(&sm.n_cand, LogpSmem<NT>::CAP + 1);
+        owners = 0;
+      }
+      while (owners) {                        // four threads' elements at a time, so that their loads overlap
+        if (*reinterpret_cast<volatile int*>(&sm.n_cand) > LogpSmem<NT>::CAP) break;
+        int from[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          from[j] = owners ? sh.v_lo + (tid & ~31) + __ffs(owners) - 1 : sh.v_hi;
+          owners &= owners - 1;
+        }
+        for (int off = lane * NT; off < sh.v_hi - sh.v_lo; off += 32 * NT) {
+          uint4 r[4];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) r[j] = from[j] < sh.v_hi - off ? __ldg(sh.vec(from[j] + off)) : make_uint4(0, 0, 0, 0);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            if (from[j] >= sh.v_hi - off) continue;
+            float f[N];
+            V16::unpack(r[j], f);
+            unsigned bits = 0;
+#pragma unroll
+            for (int k = 0; k < N; ++k) bits |= f[k] >= least ? 1u << k : 0u;
+            for (; bits; bits &= bits - 1) {  // mostly one lane, once
+              const int at = __ffs(bits) - 1;
+              float z = f[0];
+#pragma unroll
+              for (int k = 1; k < N; ++k) z = at == k ? f[k] : z;
+              put(z, sh.head + (from[j] + off) * N + at);
+            }
+          }
+        }
+      }
+      const int e = sh.single(tid);
+      if (e >= 0 && as_f32(sh.p[e]) >= least) put(as_f32(sh.p[e]), e);
+      row_sync<NT>();
+      n = sm.n_cand;
+      slow = n > LogpSmem<NT>::CAP;
+    }
+    if (slow) n = top_list_slow<T, NT>(sm, sh, m, tid, top, limit);
+  }
   auto place_of = [&](unsigned long long key) {
     int place = 0;
     for (int j = 0; j < n; ++j) place += sm.cand[j] > key ? 1 : 0;
@@ -920,13 +989,13 @@ struct LogpBwdParams {
   unsigned* status;
 };
 
-constexpr int LB_THREADS = 256;
+constexpr int LB_THREADS = 256, LB_VECS = 4;  // 10752 x 32000 bf16: 254 us with two vectors a thread, 221 with four
 
 template <typename T, bool VEC>
 __global__ void __launch_bounds__(LB_THREADS)
 token_logp_bwd_kernel(const LogpBwdParams p, int chunks) {
   using V16 = Vec16<T>;
-  constexpr int N = V16::N, U = VEC ? 2 : 8;
+  constexpr int N = V16::N, U = VEC ? LB_VECS : 8;
   const long long row = blockIdx.x / chunks;
   const int chunk = blockIdx.x - (int)(row * chunks);
   const int t = p.tok[row];
@@ -1093,18 +1162,23 @@ static int launch_embed_bwd(const T* dout, long long ld, const int* tok, int n, 
 
 template <typename T, int NT>
 static int launch_logp_as(const LogpParams& p, int ranks, cudaStream_t s) {
+  void (*kernel)(LogpParams, int) = p.top > 0 ? token_logp_kernel<T, NT, true> : token_logp_kernel<T, NT, false>;
+  if (ranks == 1) {
+    // without the cluster attribute: with it, even at one block a cluster, fewer blocks were resident
+    kernel<<<NT == 32 ? ceil_div(p.M, 8) : p.M, NT == 32 ? 256 : NT, 0, s>>>(p, 1);
+    PCM_LAUNCH_CHECK();
+    return PCM_OK;
+  }
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(NT == 32 ? (unsigned)ceil_div(p.M, 8) : (unsigned)(p.M * ranks));
-  cfg.blockDim = dim3(NT == 32 ? 256 : NT);
+  cfg.gridDim = dim3((unsigned)(p.M * ranks));
+  cfg.blockDim = dim3(NT);
   cfg.stream = s;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeClusterDimension;
   attr[0].val.clusterDim.x = (unsigned)ranks; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  const cudaError_t e = p.top > 0 ? cudaLaunchKernelEx(&cfg, token_logp_kernel<T, NT, true>, p, ranks)
-                                  : cudaLaunchKernelEx(&cfg, token_logp_kernel<T, NT, false>, p, ranks);
-  if (e != cudaSuccess) {
+  if (cudaLaunchKernelEx(&cfg, kernel, p, ranks) != cudaSuccess) {
     cudaGetLastError();
     return PCM_ERR_CUDA;
   }
@@ -1128,7 +1202,7 @@ static int launch_logp_bwd(const LogpBwdParams& p, cudaStream_t s) {
   // 16-byte accesses need every row of logits and gradient to start at the same offset from a 16-byte boundary
   const long long off = (long long)((uintptr_t)p.logits & 15) - (long long)((uintptr_t)p.dlogits & 15);
   const bool vec = off == 0 && ((p.ld - p.ld_d) * (long long)sizeof(T)) % 16 == 0;
-  const int per = vec ? LB_THREADS * 2 * Vec16<T>::N : LB_THREADS * 8;
+  const int per = vec ? LB_THREADS * LB_VECS * Vec16<T>::N : LB_THREADS * 8;
   const int chunks = ceil_div(p.V, per);
   const long long blocks = (long long)p.M * chunks;
   if (blocks > 0x7FFFFFFFll) return PCM_ERR_SHAPE;

@@ -60,6 +60,9 @@ struct TcParams {
   VocabHeadArgs vh;                           // EPI_VOCAB_STATS, EPI_VOCAB_DZ
   int chain_kb, accumulate;                   // EPI_CHAIN
   long long part_stride;
+  int m_fast;                                 // vocabulary epilogues on CTA pairs: row tiles run fastest
+  int bn;                                     // columns per tile: BN, fewer for EPI_VOCAB_STATS on single CTAs
+  int a_rows;                                 // rows of A that a tile loads: TC_BM, fewer for EPI_VOCAB_STATS with M < TC_BM
 };
 
 __device__ __forceinline__ void store_bf16x32(__nv_bfloat16* dst, const float (&v)[32]) {
@@ -334,8 +337,12 @@ __device__ __forceinline__ void epi_tile(const TcParams& p, uint32_t tmem_acc, i
         // A thread owns one row of 128 columns: softmax statistics with a running maximum, 32 columns at a time, so
         // tensor memory is read once.  Parts are stored column-block-major: a warp's 32 rows are 512 contiguous bytes.
         const int first = n0 + chalf * (BN / 2);
-        static_assert(BN == 256, "a part covers 128 columns");
-        if (first >= p.N) return;
+        static_assert(BN == 256, "a part covers at most 128 columns");
+        const int last = min(n0 + p.bn, p.N);
+        if (first >= last) {                    // an empty part: nothing of the row, but the join reads it
+          if (row < p.M) p.vh.part[(long long)(2 * (n0 / p.bn) + chalf) * p.M + row] = make_float4(-INFINITY, 0.f, 0.f, 0.f);
+          return;
+        }
         const float c = p.vh.inv_t * VOCAB_LOG2E;
         const int t = row < p.M ? p.vh.tok[row] : -1;
         VocabStat st{-INFINITY, 0.f, 0.f};
@@ -343,20 +350,20 @@ __device__ __forceinline__ void epi_tile(const TcParams& p, uint32_t tmem_acc, i
 #pragma unroll 1
         for (int c0 = 0; c0 < BN / 2; c0 += 32) {
           const int col = first + c0;
-          if (col >= p.N) break;
+          if (col >= last) break;
           uint32_t r[32];
           tmem_ld_32x32(tmem_acc + (uint32_t)(chalf * (BN / 2) + c0), r);
           tmem_ld_wait();
-          if (p.N - col < 32) {                 // columns behind the vocabulary: zero fill, not logits
+          if (last - col < 32) {                // columns behind the tile or the vocabulary are not this part's logits
 #pragma unroll
             for (int e = 0; e < 32; ++e)
-              if (e >= p.N - col) r[e] = 0xFF800000u;
+              if (e >= last - col) r[e] = 0xFF800000u;
           }
           float bm = __uint_as_float(r[0]);
 #pragma unroll
           for (int e = 1; e < 32; ++e) bm = max_nan(bm, __uint_as_float(r[e]));
           stat_raise(st, bm, c);
-          if (__any_sync(0xffffffffu, (unsigned)(t - col) < 32u)) {
+          if (__any_sync(0xffffffffu, (unsigned)(t - col) < 32u)) {    // in the tile behind too, whose part is not read for it
 #pragma unroll
             for (int e = 0; e < 32; ++e) zt = t - col == e ? __uint_as_float(r[e]) : zt;
           }
@@ -370,46 +377,64 @@ __device__ __forceinline__ void epi_tile(const TcParams& p, uint32_t tmem_acc, i
             }
           }
         }
-        if (row < p.M) p.vh.part[(long long)(first / 128) * p.M + row] = make_float4(st.m, st.s, st.w, zt);
+        if (row < p.M) p.vh.part[(long long)(2 * (n0 / p.bn) + chalf) * p.M + row] = make_float4(st.m, st.s, st.w, zt);
       } else if constexpr (EPI == EPI_VOCAB_DZ) {
         // d loss / d z in fp32 from the accumulator, then bf16 twice: the rounded value and what the rounding left, so
-        // that the weight gradient (fp32) does not carry a bf16 rounding of every term.
+        // that the weight gradient (fp32) does not carry a bf16 rounding of every term.  With a = (log2 e) log p:
+        // d z = 2^a (B a + A) (+ g / T at the target).  64 columns at a time, packed before they are staged, so that a
+        // store covers 128 contiguous bytes of a row.
         const bool in = row < p.M;
         const int t = in ? p.vh.tok[row] : -1;
         const float lse = in ? p.vh.lse[row] : 0.f;
         const bool live = t >= 0 && t < p.vh.vocab && lse != -INFINITY;
         const float H = live && p.vh.dent ? p.vh.entropy[row] : 0.f;
         const float gt = live ? p.vh.dlogp[row] * p.vh.inv_t : 0.f, ht = live && p.vh.dent ? p.vh.dent[row] * p.vh.inv_t : 0.f;
-        __nv_bfloat16* hi = reinterpret_cast<__nv_bfloat16*>(p.C);
-        __nv_bfloat16* lo = reinterpret_cast<__nv_bfloat16*>(p.vh.dz_lo);
+        const float c = p.vh.inv_t * VOCAB_LOG2E, lse2 = lse * VOCAB_LOG2E, A = -(gt + ht * H), Bc = -ht * VOCAB_LN2;
+        const bool dead = __any_sync(0xffffffffu, !live);
 #pragma unroll 1
-        for (int c0 = chalf * (BN / 2); c0 < (chalf + 1) * (BN / 2); c0 += 32) {
+        for (int c0 = chalf * (BN / 2); c0 < (chalf + 1) * (BN / 2); c0 += 64) {
           const int col = n0 + c0;
           if (col >= p.N) break;
-          uint32_t r[32];
-          tmem_ld_32x32(tmem_acc + (uint32_t)c0, r);
+          uint32_t r[2][32];
+          tmem_ld_32x32(tmem_acc + (uint32_t)c0, r[0]);
+          tmem_ld_32x32(tmem_acc + (uint32_t)c0 + 32u, r[1]);
           tmem_ld_wait();
+          const bool target = __any_sync(0xffffffffu, (unsigned)(t - col) < 64u);
+          uint32_t lo[32];
 #pragma unroll
-          for (int e = 0; e < 32; ++e)
-            r[e] = live ? __float_as_uint(vocab_slope(__uint_as_float(r[e]), p.vh.inv_t, lse, H, gt, ht, t - col == e)) : 0u;
-          stage_put_rows(stage, lane_, r);
-          __syncwarp();
+          for (int h = 0; h < 2; ++h) {
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            float v[8], h[8];
-            stage_get8(stage, lane_, i, v);
-            const int gr = row - lane_ + i * 8 + (lane_ >> 2);
-            const long long at = (long long)gr * p.ldc + col + (lane_ & 3) * 8;
-            const uint4 ph = pack8_bf16(v);
-            unpack8_bf16(ph, h);
+            for (int e = 0; e < 32; ++e) {
+              const float a = max_nan(__uint_as_float(r[h][e]) * c - lse2, -1000.f);
+              float v = ex2(a) * (Bc * a + A);
+              if (target && t - col == 32 * h + e) v += gt;
+              if (dead && !live) v = 0.f;
+              r[h][e] = __float_as_uint(v);
+            }
 #pragma unroll
-            for (int e = 0; e < 8; ++e) h[e] = v[e] - h[e];
-            if (gr < p.M) {
-              *reinterpret_cast<uint4*>(hi + at) = ph;
-              *reinterpret_cast<uint4*>(lo + at) = pack8_bf16(h);
+            for (int e = 0; e < 32; e += 2) {
+              const float v0 = __uint_as_float(r[h][e]), v1 = __uint_as_float(r[h][e + 1]);
+              const __nv_bfloat162 q = __floats2bfloat162_rn(v0, v1);
+              const uint32_t w = *reinterpret_cast<const uint32_t*>(&q);
+              const __nv_bfloat162 l = __floats2bfloat162_rn(v0 - __uint_as_float(w << 16), v1 - __uint_as_float(w & 0xFFFF0000u));
+              r[0][16 * h + e / 2] = w;                            // h = 0 writes behind what it has read
+              lo[16 * h + e / 2] = *reinterpret_cast<const uint32_t*>(&l);
             }
           }
-          __syncwarp();
+          const int cc = col + (lane_ & 7) * 8;
+#pragma unroll
+          for (int part = 0; part < 2; ++part) {
+            __nv_bfloat16* dst = reinterpret_cast<__nv_bfloat16*>(part ? p.vh.dz_lo : p.C);
+            stage_put_rows(stage, lane_, part ? lo : r[0]);
+            __syncwarp();
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+              const int rr = i * 4 + (lane_ >> 3), gr = row - lane_ + rr;
+              const uint4 q = *reinterpret_cast<const uint4*>(stage + rr * EPI_STAGE_STRIDE + (lane_ & 7) * 4);
+              if (gr < p.M && cc < p.ldc) __stcs(reinterpret_cast<uint4*>(dst + (long long)gr * p.ldc + cc), q);   // streamed: w stays in L2
+            }
+            __syncwarp();
+          }
         }
       } else if constexpr (EPI == EPI_SWIGLU_FWD) {
         // accumulator columns [0,128) = gate, [128,256) = up, for hidden units hid0 .. hid0+127
@@ -678,6 +703,7 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
   float* epi_stage = reinterpret_cast<float*>(reinterpret_cast<uint8_t*>(bars) + 256);
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int bn = EPI == EPI_VOCAB_STATS ? p.bn : BN;      // columns per tile
   const int num_kb_total = p.kb_total;
   const int tiles_mn = p.tiles_m * p.tiles_n;
   const int total_tiles = tiles_mn * p.splits;
@@ -698,6 +724,10 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem_base = *tmem_slot;
+  if constexpr (EPI >= EPI_VOCAB_STATS) {       // launched with launch_after
+    wait_for_predecessor();
+    let_successor_start();
+  }
 
   // Tiles are walked in the same order by every role: tile -> (split, m, n) with n fastest, so that
   // CTAs running at the same time share A row-tiles and the whole B operand stays in L2.
@@ -707,7 +737,7 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
       unsigned it = 0;                        // k-blocks issued so far, across tiles
       for (int tile = blockIdx.x; tile < total_tiles && !*abort_flag; tile += gridDim.x) {
         const int split = tile / tiles_mn, mn = tile - split * tiles_mn;
-        const int m0 = (mn / p.tiles_n) * TC_BM, n0 = (mn % p.tiles_n) * BN;
+        const int m0 = (mn / p.tiles_n) * TC_BM, n0 = (mn % p.tiles_n) * bn;
         const int kb_lo = split * p.kb_per_split, kb_hi = min(kb_lo + p.kb_per_split, num_kb_total);
         for (int kb = kb_lo; kb < kb_hi; ++kb, ++it) {
           const int st = it % TC_STAGES;
@@ -715,7 +745,7 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
           if (!mbar_wait_bounded(&empty[st], ph ^ 1u, TC_WAIT_LIMIT_NS)) { *abort_flag = 1; atomicOr(&g_tc_status, 1u); break; }
           uint8_t* sa = tiles + st * SM::STAGE_BYTES;
           uint8_t* sb = sa + SM::A_BYTES;
-          mbar_expect_tx(&full[st], SM::STAGE_BYTES);
+          mbar_expect_tx(&full[st], p.a_rows * TC_BK * 2 + bn * TC_BK * 2);
           const bool ext = kb >= p.kb_main;                               // continuation: second operand pair
           const CUtensorMap* mA = ext ? &tmA2 : &tmA;
           const CUtensorMap* mB = ext ? &tmB2 : &tmB;
@@ -742,7 +772,7 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
   } else if (warp == 1) {
     if (lane == 0) {
       // ------------------------------ MMA issuer ------------------------------
-      const uint32_t idesc = make_idesc(BN, p.a_kmajor ? 0 : 1, p.b_kmajor ? 0 : 1);
+      const uint32_t idesc = make_idesc(bn, p.a_kmajor ? 0 : 1, p.b_kmajor ? 0 : 1);
       // K-major tile: rows of 128 B, 8-row groups 1024 B apart; a k-step of 16 elements is 32 B along the row.
       // MN-major tile: boxes of 64 (mn) x 64 (k): k-rows of 128 B, 8-row groups 1024 B apart, next 64 mn 8192 B on;
       //                a k-step of 16 rows is 2048 B.
@@ -799,7 +829,7 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
     unsigned tcount = 0;
     for (int tile = blockIdx.x; tile < total_tiles; tile += gridDim.x, ++tcount) {
       const int split = tile / tiles_mn, mn = tile - split * tiles_mn;
-      const int m0 = (mn / p.tiles_n) * TC_BM, n0 = (mn % p.tiles_n) * BN;
+      const int m0 = (mn / p.tiles_n) * TC_BM, n0 = (mn % p.tiles_n) * bn;
       const int row = m0 + quad * 32 + lane;
       if constexpr (EPI == EPI_CHAIN) {
         const int kb_lo = split * p.kb_per_split, kb_hi = min(kb_lo + p.kb_per_split, num_kb_total);
@@ -906,6 +936,7 @@ gemm_tc2_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
                 const __grid_constant__ CUtensorMap tmA2, const __grid_constant__ CUtensorMap tmB2, const TcParams p) {
   extern __shared__ uint8_t smem_raw[];
   constexpr int BN = T2_BN;
+  constexpr bool VOCAB = EPI == EPI_VOCAB_STATS || EPI == EPI_VOCAB_DZ;
   const uint32_t raw_addr = smem_u32(smem_raw);
   uint8_t* tiles = smem_raw + ((1024u - (raw_addr & 1023u)) & 1023u);
   uint64_t* bars = reinterpret_cast<uint64_t*>(tiles + T2_STAGES * T2_STAGE_BYTES);
@@ -942,6 +973,10 @@ gemm_tc2_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
   cluster_sync_all();                          // the peer's barriers exist before anything is sent to them
   tc_fence_after();
   const uint32_t tmem_base = *tmem_slot;
+  if constexpr (EPI >= EPI_VOCAB_STATS) {
+    wait_for_predecessor();
+    let_successor_start();
+  }
 
   if (warp == 0 || warp == T2_PRODUCER_B_WARP) {
     if (lane == 0) {
@@ -951,14 +986,16 @@ gemm_tc2_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
       // and the tile walk are counters (no division or modulo per k-block).
       const bool load_a = warp == 0;
       const uint32_t bar0 = mapa_shared(smem_u32(&full[0]), 0);               // the leader's barriers count both CTAs' bytes
+      const bool swap = VOCAB && p.m_fast;
+      const int walk_m = swap ? p.tiles_n : p.tiles_m, walk_n = swap ? p.tiles_m : p.tiles_n;
       TileWalk tw;
-      tw.init(pair, n_pairs, p.tiles_m, p.tiles_n);
+      tw.init(pair, n_pairs, walk_m, walk_n);
       int st = 0;
       unsigned ph = 0;
       bool ok = true;
-      for (int tile = pair; tile < total_tiles && ok && !*abort_flag; tile += n_pairs, tw.next(p.tiles_m, p.tiles_n)) {
-        const int m0 = tw.m * (2 * TC_BM) + (int)rank * TC_BM;                  // this CTA's rows
-        const int n0 = tw.n * BN;
+      for (int tile = pair; tile < total_tiles && ok && !*abort_flag; tile += n_pairs, tw.next(walk_m, walk_n)) {
+        const int m0 = (swap ? tw.n : tw.m) * (2 * TC_BM) + (int)rank * TC_BM;  // this CTA's rows
+        const int n0 = (swap ? tw.m : tw.n) * BN;
         const int nb0 = n0 + (int)rank * (BN / 2);                              // this CTA's columns of B
         const int kb_lo = tw.split * p.kb_per_split, kb_hi = min(kb_lo + p.kb_per_split, num_kb_total);
         for (int kb = kb_lo; kb < kb_hi; ++kb) {
@@ -1060,7 +1097,9 @@ gemm_tc2_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
     unsigned tcount = 0;
     for (int tile = pair; tile < total_tiles; tile += n_pairs, ++tcount) {
       const int split = tile / tiles_mn, mn = tile - split * tiles_mn;
-      const int m0 = (mn / p.tiles_n) * (2 * TC_BM) + (int)rank * TC_BM, n0 = (mn % p.tiles_n) * BN;
+      const bool swap = VOCAB && p.m_fast;
+      const int tm = swap ? mn % p.tiles_m : mn / p.tiles_n, tn = swap ? mn / p.tiles_m : mn % p.tiles_n;
+      const int m0 = tm * (2 * TC_BM) + (int)rank * TC_BM, n0 = tn * BN;
       const int row = m0 + quad * 32 + lane;
       if constexpr (EPI == EPI_CHAIN) {
         const int kb_lo = split * p.kb_per_split, kb_hi = min(kb_lo + p.kb_per_split, num_kb_total);
@@ -1190,6 +1229,10 @@ static void fill_params(TcParams& p, const GemmArgs& g) {
   p.chain_kb = g.epi.chain_kb > 0 ? g.epi.chain_kb : p.kb_total;
   p.accumulate = g.epi.accumulate;
   p.part_stride = g.epi.part_stride;
+  // The operand whose tiles run fastest is read once for every wave of the other's: the shorter one, which fits L2 sooner.
+  p.m_fast = g.M < g.N;
+  p.bn = T2_BN;
+  p.a_rows = TC_BM;
   p.alpha = g.alpha;
   p.kb_per_split = 1; p.tiles_m = p.tiles_n = p.splits = 1;
 }
@@ -1197,9 +1240,13 @@ static void fill_params(TcParams& p, const GemmArgs& g) {
 template <int BN, int EPI>
 static int launch_tc(const GemmArgs& g, cudaStream_t s) {
   CUtensorMap tmA, tmB;
-  constexpr int B_BOX_ROWS = (EPI == EPI_SWIGLU_FWD) ? 128 : BN;
+  const int bn = EPI == EPI_VOCAB_STATS ? gemm_vocab_tile(g.M, g.N) : BN;
+  const int B_BOX_ROWS = (EPI == EPI_SWIGLU_FWD) ? 128 : bn;
   // K-major operand: tensor [MN][K] -> box {64 k, rows}.  MN-major operand: tensor [K][MN] -> box {64 mn, 64 k}.
-  const bool okA = g.a_kmajor ? make_tmap(&tmA, g.A, g.M, g.K, g.lda, TC_BK, TC_BM)
+  // A short product loads its own rows only: filling the other rows of the box with zeros takes time, and they would only
+  // reach accumulator rows that nothing reads.
+  const int a_rows = EPI == EPI_VOCAB_STATS && g.M < TC_BM ? ceil_div(g.M, 8) * 8 : TC_BM;
+  const bool okA = g.a_kmajor ? make_tmap(&tmA, g.A, g.M, g.K, g.lda, TC_BK, a_rows)
                               : make_tmap(&tmA, g.A, g.K, g.M, g.lda, 64, TC_BK);
   const bool okB = g.b_kmajor ? make_tmap(&tmB, g.B, g.N, g.K, g.ldb, TC_BK, B_BOX_ROWS)
                               : make_tmap(&tmB, g.B, g.K, g.N, g.ldb, 64, TC_BK);
@@ -1214,7 +1261,9 @@ static int launch_tc(const GemmArgs& g, cudaStream_t s) {
   }
   TcParams p;
   fill_params(p, g);
-  const int tiles_m = (g.M + TC_BM - 1) / TC_BM, tiles_n = (g.N + BN - 1) / BN;
+  p.bn = bn;
+  p.a_rows = a_rows;
+  const int tiles_m = (g.M + TC_BM - 1) / TC_BM, tiles_n = (g.N + bn - 1) / bn;
   const int num_kb = p.kb_total;
   int splits = 1;
   if (p.reduce) {
@@ -1234,6 +1283,8 @@ static int launch_tc(const GemmArgs& g, cudaStream_t s) {
   p.tiles_m = tiles_m; p.tiles_n = tiles_n; p.splits = splits;
   const long long total = (long long)tiles_m * tiles_n * splits;
   const int grid = (int)(total < sm_count() ? total : sm_count());      // persistent: one CTA per SM walks the tile list
+  if constexpr (EPI >= EPI_VOCAB_STATS)
+    return launch_after_smem(gemm_tc_kernel<BN, EPI>, dim3(grid), dim3(TC_THREADS), TcSmem<BN>::TOTAL, s, tmA, tmB, tmA2, tmB2, p);
   gemm_tc_kernel<BN, EPI><<<grid, TC_THREADS, TcSmem<BN>::TOTAL, s>>>(tmA, tmB, tmA2, tmB2, p);
   PCM_LAUNCH_CHECK();
   return PCM_OK;
@@ -1302,17 +1353,28 @@ static int launch_tc2(const GemmArgs& g, cudaStream_t s) {
   cfg.blockDim = dim3(T2_THREADS);
   cfg.dynamicSmemBytes = T2_SMEM_TOTAL;
   cfg.stream = s;
-  cudaLaunchAttribute attr[1];
+  cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeClusterDimension;
   attr[0].val.clusterDim.x = 2; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;       // these kernels wait for their predecessor themselves
+  attr[1].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
-  cfg.numAttrs = 1;
+  cfg.numAttrs = EPI >= EPI_VOCAB_STATS ? 2 : 1;
   if (cudaLaunchKernelEx(&cfg, gemm_tc2_kernel<EPI>, tmA, tmB, tmA2, tmB2, p) != cudaSuccess) {
     cudaGetLastError();
     return PCM_ERR_CUDA;
   }
   pcm::g_launches.fetch_add(1, std::memory_order_relaxed);
   return PCM_OK;
+}
+
+// On single CTAs (M <= 128: reading B is what takes time) as many columns as give every SM the same number of tiles: 32000
+// columns are 143 tiles of 224 on 148 SMs instead of 125 of 256.
+int gemm_vocab_tile(int M, int N) {
+  if (pair_enabled() && M > TC_BM) return T2_BN;
+  const int sms = sm_count(), rounds = ceil_div(ceil_div(N, 256), sms);
+  const int bn = ceil_div(ceil_div(N, (long long)sms * rounds), 16) * 16;
+  return bn < 64 ? 64 : bn;
 }
 
 static bool chain_pair(const GemmArgs& g) { return pair_enabled() && g.N > TC_BM && g.M > TC_BM; }

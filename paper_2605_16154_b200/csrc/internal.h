@@ -6,6 +6,37 @@
 
 namespace pcm {
 
+// Kernels that run back to back in one call: each is launched (launch_after) while its predecessor drains, and waits in
+// the kernel for that one's results before it touches memory.
+__device__ __forceinline__ void wait_for_predecessor() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void let_successor_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+
+// A launch that may begin before the kernel ahead of it in the stream has ended; the kernel waits for that one itself,
+// before it touches memory.
+template <typename... P, typename... A>
+static int launch_after_smem(void (*kernel)(P...), dim3 grid, dim3 block, size_t smem, cudaStream_t s, A... args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid;
+  cfg.blockDim = block;
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = s;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  if (cudaLaunchKernelEx(&cfg, kernel, static_cast<P>(args)...) != cudaSuccess) {
+    cudaGetLastError();
+    return PCM_ERR_CUDA;
+  }
+  g_launches.fetch_add(1, std::memory_order_relaxed);
+  return PCM_OK;
+}
+template <typename... P, typename... A>
+static int launch_after(void (*kernel)(P...), dim3 grid, dim3 block, cudaStream_t s, A... args) {
+  return launch_after_smem(kernel, grid, block, 0, s, args...);
+}
+
 enum { DT_F32 = 0, DT_BF16 = 1 };
 
 // C[m][n] = sum_k A(m,k) * B(n,k)  (+ R[m][n] when R != nullptr; R may alias C to accumulate).
@@ -31,8 +62,8 @@ struct GemmEpilogue {
   //                 hl.want_dz, C = d loss / d z [M][256] bf16.  z is never stored.
   const float2* rope_tab = nullptr; int S = 0, dh = 0, d = 0;
   HeadLossArgs hl;
-  // EPI_VOCAB_STATS: the product is the logits z [M][N] of a vocabulary of any width N; the epilogue reduces every 128
-  //                 columns of a row to softmax statistics (vh.part).  z is never stored, C is not used.
+  // EPI_VOCAB_STATS: the product is the logits z [M][N] of a vocabulary of any width N; the epilogue reduces each half
+  //                 tile of a row to softmax statistics (vh.part).  z is never stored, C is not used.
   // EPI_VOCAB_DZ:   the same product again; C [M][ldc] (bf16, ldc a multiple of 32) and vh.dz_lo receive d loss / d z.
   VocabHeadArgs vh;
   // EPI_CHAIN:      C = or += A B (fp32 or bf16, N a multiple of 8).  The tensor core's accumulator is not rounded to
@@ -72,6 +103,8 @@ bool gemm_tcgen05_pair(const GemmArgs& g);      // the tensor-core path's own ch
 // Splits of the contraction with which an EPI_CHAIN product of this shape fills the GPU; its fp32 parts take at most
 // chain_part_bytes(), a bound that holds for every shape.
 int gemm_chain_splits(const GemmArgs& g);
+// Columns per tile of an EPI_VOCAB_STATS product; a tile leaves two parts a row, of its first 128 columns and of the rest.
+int gemm_vocab_tile(int M, int N);
 size_t chain_part_bytes();
 // Sets STATUS_TIMEOUT in *status (device; nothing where it is null), in stream order, when a bounded wait of a
 // tensor-core GEMM has run out since the status was last polled.

@@ -119,10 +119,6 @@ struct EmbedPlan {
 // Tokens outside the vocabulary take the key behind its last one.
 __device__ __forceinline__ unsigned embed_key(int t, int vocab) { return t >= 0 && t < vocab ? (unsigned)t : (unsigned)vocab; }
 
-// The kernels of one gradient run back to back: each is launched while its predecessor drains and waits here for its results.
-__device__ __forceinline__ void wait_for_predecessor() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
-__device__ __forceinline__ void let_successor_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
-
 // Up to 1024 pairs: a bitonic network over keys (token above, position below: positions differ, so the order is the stable
 // one), in 32 bits when token and position fit.  Exchanges up to 16 apart are shuffles, the others go through shared memory.
 template <typename K, int POS_BITS>
@@ -1064,27 +1060,6 @@ static int launch_embed(const T* table, long long ld_table, int vocab, int d, co
   if (vec) embed_kernel<T, true><<<(unsigned)blocks, 256, 0, s>>>(table, ld_table, vocab, d, tok, n, scale, out, ld_out, status, lg);
   else embed_kernel<T, false><<<(unsigned)blocks, 256, 0, s>>>(table, ld_table, vocab, d, tok, n, scale, out, ld_out, status, lg);
   PCM_LAUNCH_CHECK();
-  return PCM_OK;
-}
-
-// A launch that may begin before the kernel ahead of it in the stream has ended; the kernel waits for that one itself,
-// before it touches memory.
-template <typename... P, typename... A>
-static int launch_after(void (*kernel)(P...), dim3 grid, dim3 block, cudaStream_t s, A... args) {
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = grid;
-  cfg.blockDim = block;
-  cfg.stream = s;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = 1;
-  if (cudaLaunchKernelEx(&cfg, kernel, static_cast<P>(args)...) != cudaSuccess) {
-    cudaGetLastError();
-    return PCM_ERR_CUDA;
-  }
-  g_launches.fetch_add(1, std::memory_order_relaxed);
   return PCM_OK;
 }
 

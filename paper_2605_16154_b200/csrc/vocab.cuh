@@ -71,7 +71,7 @@ __device__ __forceinline__ float vocab_slope(float z, float inv_t, float lse, fl
 struct VocabHeadArgs {
   const int* tok = nullptr;                   // [M]
   float inv_t = 1.f;
-  float4* part = nullptr;                     // EPI_VOCAB_STATS out: [ceil(N / 128)][M] {m, s, w, the target's logit}
+  float4* part = nullptr;                     // EPI_VOCAB_STATS out: [2 tiles][M] {m, s, w, the target's logit}
   const float* lse = nullptr;                 // EPI_VOCAB_DZ
   const float* entropy = nullptr;
   const float* dlogp = nullptr;

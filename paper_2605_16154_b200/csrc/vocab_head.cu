@@ -1,7 +1,7 @@
 // Log-probabilities of given tokens straight from the last hidden states x [M][d] and the head's weight w [V][d], and
 // their gradients.  The logits z = x w^T exist only as accumulator tiles in tensor memory:
-//   forward   the head GEMM's epilogue reduces each row's 128-column blocks to softmax statistics (16 bytes per block and
-//             row instead of 256 or 512 of logits); a small kernel joins them.  Bound by the tensor cores from a few
+//   forward   the head GEMM's epilogue reduces each half tile of a row to softmax statistics (16 bytes instead of the
+//             256 or 512 of up to 128 logits); a small kernel joins them.  Bound by the tensor cores from a few
 //             hundred rows on, by reading w below.
 //   backward  the same product once more, its epilogue writing d loss / d z in bf16 (rounded value and remainder) for a
 //             chunk of rows; then dx = dz w and dw (+)= dz^T x.
@@ -14,34 +14,73 @@ namespace pcm {
 constexpr int VH_GROUPS = 16;                 // column-block slices of a row joined side by side
 constexpr int VH_CHAIN_KB = 8;                // k-blocks (512 rows) per accumulator piece of dw
 
-// 32 rows per block: thread (lane, slice) runs over every 16th part of row 32 b + lane, then slice 0 joins the slices.
+struct JoinParams {
+  const float4* part;                         // [parts][M]
+  int M, V, bn, parts;                        // columns per tile; two parts a tile
+  const int* tok;
+  float inv_t;
+  float* logp; float* entropy; float* lse;
+  unsigned* status;
+};
+
+__device__ __forceinline__ VocabStat load_part(const JoinParams& p, int b, long long row) {
+  const float4 q = p.part[(long long)b * p.M + row];
+  return VocabStat{q.x, q.y, q.z};
+}
+__device__ __forceinline__ void finish_row(const JoinParams& p, const VocabStat& st, long long row) {
+  const int t = p.tok[row];
+  const bool live = t >= 0 && t < p.V;
+  if (t >= p.V && p.status) atomicOr(p.status, STATUS_BAD_TOKEN);
+  const RowResult res(st, p.inv_t);
+  if (p.logp) p.logp[row] = live ? res.logp(p.part[(long long)(2 * (t / p.bn) + (t % p.bn) / 128) * p.M + row].w) : 0.f;
+  if (p.entropy) p.entropy[row] = live ? res.entropy : 0.f;
+  if (p.lse) p.lse[row] = live ? res.lse : 0.f;
+}
+
+// Many rows: 32 per block; thread (lane, slice) runs over every 16th part of row 32 b + lane (a warp reads 512 contiguous
+// bytes), then slice 0 joins the slices.
 __global__ void __launch_bounds__(32 * VH_GROUPS)
-vocab_stats_join_kernel(const float4* __restrict__ part, int M, int V, const int* __restrict__ tok, float inv_t,
-                        float* __restrict__ logp, float* __restrict__ entropy, float* __restrict__ lse, unsigned* status) {
+vocab_stats_join_kernel(const JoinParams p) {
   __shared__ VocabStat sm[VH_GROUPS][32];
   const int lane = threadIdx.x & 31, slice = threadIdx.x >> 5;
   const long long row = (long long)blockIdx.x * 32 + lane;
-  const int blocks = (V + 127) / 128;
-  const float c = inv_t * VOCAB_LOG2E;
+  const float c = p.inv_t * VOCAB_LOG2E;
+  wait_for_predecessor();
   VocabStat st{-INFINITY, 0.f, 0.f};
-  if (row < M) {
+  if (row < p.M) {
 #pragma unroll 4
-    for (int b = slice; b < blocks; b += VH_GROUPS) {
-      const float4 q = __ldg(part + (long long)b * M + row);
-      st = stat_join(st, VocabStat{q.x, q.y, q.z}, c);
-    }
+    for (int b = slice; b < p.parts; b += VH_GROUPS) st = stat_join(st, load_part(p, b, row), c);
   }
   sm[slice][lane] = st;
   __syncthreads();
-  if (slice != 0 || row >= M) return;
+  if (slice != 0 || row >= p.M) return;
   for (int k = 1; k < VH_GROUPS; ++k) st = stat_join(st, sm[k][lane], c);
-  const int t = tok[row];
-  const bool live = t >= 0 && t < V;
-  if (t >= V && status) atomicOr(status, STATUS_BAD_TOKEN);
-  const RowResult res(st, inv_t);
-  if (logp) logp[row] = live ? res.logp(part[(long long)(t / 128) * M + row].w) : 0.f;
-  if (entropy) entropy[row] = live ? res.entropy : 0.f;
-  if (lse) lse[row] = live ? res.lse : 0.f;
+  finish_row(p, st, row);
+}
+
+// Few rows: one per block, so that a row's parts are read at once.
+__global__ void __launch_bounds__(128)
+vocab_stats_join_row_kernel(const JoinParams p) {
+  __shared__ VocabStat sm[4];
+  const int tid = threadIdx.x;
+  const float c = p.inv_t * VOCAB_LOG2E;
+  wait_for_predecessor();
+  VocabStat st{-INFINITY, 0.f, 0.f};
+#pragma unroll 4
+  for (int b = tid; b < p.parts; b += 128) st = stat_join(st, load_part(p, b, blockIdx.x), c);
+#pragma unroll
+  for (int off = 16; off; off >>= 1) {
+    VocabStat o;
+    o.m = __shfl_down_sync(0xffffffffu, st.m, off);
+    o.s = __shfl_down_sync(0xffffffffu, st.s, off);
+    o.w = __shfl_down_sync(0xffffffffu, st.w, off);
+    st = stat_join(st, o, c);
+  }
+  if ((tid & 31) == 0) sm[tid >> 5] = st;
+  __syncthreads();
+  if (tid != 0) return;
+  for (int k = 1; k < 4; ++k) st = stat_join(st, sm[k], c);
+  finish_row(p, st, blockIdx.x);
 }
 
 // The hidden states with zeros in the rows that have no token: their d z is zero, but zero times whatever a padded row
@@ -49,6 +88,8 @@ vocab_stats_join_kernel(const float4* __restrict__ part, int M, int V, const int
 __global__ void __launch_bounds__(256)
 live_rows_kernel(const uint4* __restrict__ x, long long ld8, int M, int d8, const int* __restrict__ tok, int V, uint4* __restrict__ out,
                  unsigned* status) {
+  wait_for_predecessor();                     // the rows of the chunk before may still be read
+  let_successor_start();
   const long long total = (long long)M * d8;
   for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < total; i += (long long)gridDim.x * 256) {
     const long long row = i / d8;
@@ -64,6 +105,8 @@ template <bool BF16>
 __global__ void __launch_bounds__(256)
 parts_sum_kernel(const float* __restrict__ part, long long stride, int splits, long long M, int N, void* __restrict__ C, long long ldc,
                  int accumulate) {
+  wait_for_predecessor();
+  let_successor_start();
   const int n4 = N / 4;
   const long long total = M * n4;
   for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < total; i += (long long)gridDim.x * 256) {
@@ -99,12 +142,8 @@ static int chain_gemm(GemmArgs g, float* parts, cudaStream_t s) {
   if (rc != PCM_OK) return rc;
   const long long total = (long long)g.M * (g.N / 4);
   const int grid = (int)(ceil_div(total, 256) < 8 * sm_count() ? ceil_div(total, 256) : 8 * sm_count());
-  if (g.c_dtype == DT_BF16)
-    parts_sum_kernel<true><<<grid, 256, 0, s>>>(parts, q.epi.part_stride, splits, g.M, g.N, g.C, g.ldc, 0);
-  else
-    parts_sum_kernel<false><<<grid, 256, 0, s>>>(parts, q.epi.part_stride, splits, g.M, g.N, g.C, g.ldc, g.epi.accumulate);
-  PCM_LAUNCH_CHECK();
-  return PCM_OK;
+  return launch_after(g.c_dtype == DT_BF16 ? parts_sum_kernel<true> : parts_sum_kernel<false>, dim3(grid), dim3(256), s, parts,
+                      q.epi.part_stride, splits, g.M, g.N, g.C, g.ldc, g.epi.accumulate);
 }
 
 static size_t round256(size_t v) { return (v + 255) / 256 * 256; }
@@ -134,7 +173,7 @@ using namespace pcm;
 
 extern "C" size_t grpo_head_logp_workspace_bytes(int32_t n_rows, int32_t d, int32_t vocab) {
   if (n_rows < 0 || d < 8 || d % 8 || vocab < 1) return 0;
-  return round256((size_t)((vocab + 127) / 128) * (size_t)n_rows * sizeof(float4)) + 256;
+  return round256(2 * (size_t)ceil_div(vocab, gemm_vocab_tile(n_rows, vocab)) * (size_t)n_rows * sizeof(float4)) + 256;
 }
 
 extern "C" int grpo_head_logp(const void* x, int64_t ld_x, int32_t n_rows, int32_t d, const void* w_h, int64_t ld_w, int32_t vocab,
@@ -156,10 +195,12 @@ extern "C" int grpo_head_logp(const void* x, int64_t ld_x, int32_t n_rows, int32
   prof_end(s, 2.0 * n_rows * vocab * d, 2.0 * d * ((double)n_rows + vocab));
   if (rc != PCM_OK) return rc;
   prof_begin(PC_LOSS, s);
-  vocab_stats_join_kernel<<<ceil_div(n_rows, 32), 32 * VH_GROUPS, 0, s>>>(part, n_rows, vocab, tok, inv_t, logp, entropy, lse, device_status);
-  g_launches.fetch_add(1, std::memory_order_relaxed);
-  prof_end(s, 0.0, 16.0 * n_rows * ((vocab + 127) / 128));
-  PCM_CUDA_TRY(cudaPeekAtLastError());
+  const int bn = gemm_vocab_tile(n_rows, vocab);
+  const JoinParams jp{part, n_rows, vocab, bn, 2 * ceil_div(vocab, bn), tok, inv_t, logp, entropy, lse, device_status};
+  rc = n_rows <= 1024 ? launch_after(vocab_stats_join_row_kernel, dim3(n_rows), dim3(128), s, jp)
+                      : launch_after(vocab_stats_join_kernel, dim3(ceil_div(n_rows, 32)), dim3(32 * VH_GROUPS), s, jp);
+  prof_end(s, 0.0, 16.0 * n_rows * jp.parts);
+  if (rc != PCM_OK) return rc;
   return gemm_forward_status(device_status, s);
 }
 
@@ -198,10 +239,10 @@ extern "C" int grpo_head_logp_bwd(const void* x, int64_t ld_x, int32_t n_rows, i
     prof_begin(PC_ELEM, s);
     const int d8 = d / 8;
     const int blocks = ceil_div((long long)rows * d8, 1024);
-    live_rows_kernel<<<blocks, 256, 0, s>>>((const uint4*)xr, ld_x / 8, rows, d8, tok + r0, vocab, x_live, device_status);
-    g_launches.fetch_add(1, std::memory_order_relaxed);
+    int rc = launch_after(live_rows_kernel, dim3(blocks), dim3(256), s, (const uint4*)xr, ld_x / 8, rows, d8, tok + r0, vocab, x_live,
+                          device_status);
     prof_end(s, 0.0, 4.0 * rows * d);
-    PCM_CUDA_TRY(cudaPeekAtLastError());
+    if (rc != PCM_OK) return rc;
 
     GemmArgs z{rows, vocab, d, x_live, d, true, w_h, ld_w, true, DT_BF16, hi, pl.ldz, DT_BF16, nullptr, 0};
     z.epi.kind = EPI_VOCAB_DZ;
@@ -210,7 +251,7 @@ extern "C" int grpo_head_logp_bwd(const void* x, int64_t ld_x, int32_t n_rows, i
     v.dent = dentropy ? dentropy + r0 : nullptr;
     v.entropy = dentropy ? entropy + r0 : nullptr;
     prof_begin(PC_GEMM, s);
-    int rc = gemm_tcgen05(z, s);
+    rc = gemm_tcgen05(z, s);
     prof_end(s, flops, 2.0 * d * ((double)rows + vocab) + 4.0 * rows * vocab);
     if (rc != PCM_OK) return rc;
     if (dx) {

@@ -63,6 +63,7 @@ struct TcParams {
   int m_fast;                                 // vocabulary epilogues on CTA pairs: row tiles run fastest
   int bn;                                     // columns per tile: BN, fewer for EPI_VOCAB_STATS on single CTAs
   int a_rows;                                 // rows of A that a tile loads: TC_BM, fewer for EPI_VOCAB_STATS with M < TC_BM
+  int stages;                                 // EPI_VOCAB_STATS on single CTAs: ring depth
 };
 
 __device__ __forceinline__ void store_bf16x32(__nv_bfloat16* dst, const float (&v)[32]) {
@@ -692,11 +693,14 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
   using SM = TcSmem<BN>;
   const uint32_t raw_addr = smem_u32(smem_raw);
   uint8_t* tiles = smem_raw + ((1024u - (raw_addr & 1023u)) & 1023u);       // swizzle atoms need 1024-byte alignment
-  constexpr int TC_STAGES = SM::STAGES;
-  uint64_t* bars = reinterpret_cast<uint64_t*>(tiles + TC_STAGES * SM::STAGE_BYTES);
-  uint64_t* full = bars;                      // [TC_STAGES] producer -> MMA
-  uint64_t* empty = bars + TC_STAGES;         // [TC_STAGES] MMA -> producer
-  uint64_t* acc_full = bars + 2 * TC_STAGES;  // [2] MMA -> epilogue, one per accumulator buffer
+  // EPI_VOCAB_STATS: as many stages of its own (smaller) tiles as fit
+  const int stages = EPI == EPI_VOCAB_STATS ? p.stages : SM::STAGES;
+  const int a_bytes = EPI == EPI_VOCAB_STATS ? p.a_rows * TC_BK * 2 : SM::A_BYTES;
+  const int stage_bytes = EPI == EPI_VOCAB_STATS ? (p.a_rows + p.bn) * TC_BK * 2 : SM::STAGE_BYTES;
+  uint64_t* bars = reinterpret_cast<uint64_t*>(tiles + stages * stage_bytes);
+  uint64_t* full = bars;                      // [stages] producer -> MMA
+  uint64_t* empty = bars + stages;         // [stages] MMA -> producer
+  uint64_t* acc_full = bars + 2 * stages;  // [2] MMA -> epilogue, one per accumulator buffer
   uint64_t* acc_empty = acc_full + 2;         // [2] epilogue -> MMA
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(acc_empty + 2);
   volatile uint32_t* abort_flag = tmem_slot + 1;
@@ -709,7 +713,7 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
   const int total_tiles = tiles_mn * p.splits;
 
   if (threadIdx.x == 0) {
-    for (int s = 0; s < TC_STAGES; ++s) { mbar_init(&full[s], 1); mbar_init(&empty[s], 1); }
+    for (int s = 0; s < stages; ++s) { mbar_init(&full[s], 1); mbar_init(&empty[s], 1); }
     for (int b = 0; b < 2; ++b) { mbar_init(&acc_full[b], 1); mbar_init(&acc_empty[b], TC_EPI_WARPS); }
     *abort_flag = 0;
     fence_mbar_init();
@@ -734,18 +738,17 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
   if (warp == 0) {
     if (lane == 0) {
       // ------------------------------ TMA producer ------------------------------
-      unsigned it = 0;                        // k-blocks issued so far, across tiles
+      int st = 0;                             // ring position and its phase, across tiles
+      unsigned ph = 0;
       for (int tile = blockIdx.x; tile < total_tiles && !*abort_flag; tile += gridDim.x) {
         const int split = tile / tiles_mn, mn = tile - split * tiles_mn;
         const int m0 = (mn / p.tiles_n) * TC_BM, n0 = (mn % p.tiles_n) * bn;
         const int kb_lo = split * p.kb_per_split, kb_hi = min(kb_lo + p.kb_per_split, num_kb_total);
-        for (int kb = kb_lo; kb < kb_hi; ++kb, ++it) {
-          const int st = it % TC_STAGES;
-          const unsigned ph = (it / TC_STAGES) & 1u;
+        for (int kb = kb_lo; kb < kb_hi; ++kb) {
           if (!mbar_wait_bounded(&empty[st], ph ^ 1u, TC_WAIT_LIMIT_NS)) { *abort_flag = 1; atomicOr(&g_tc_status, 1u); break; }
-          uint8_t* sa = tiles + st * SM::STAGE_BYTES;
-          uint8_t* sb = sa + SM::A_BYTES;
-          mbar_expect_tx(&full[st], p.a_rows * TC_BK * 2 + bn * TC_BK * 2);
+          uint8_t* sa = tiles + st * stage_bytes;
+          uint8_t* sb = sa + a_bytes;
+          mbar_expect_tx(&full[st], stage_bytes);
           const bool ext = kb >= p.kb_main;                               // continuation: second operand pair
           const CUtensorMap* mA = ext ? &tmA2 : &tmA;
           const CUtensorMap* mB = ext ? &tmB2 : &tmB;
@@ -766,6 +769,7 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
 #pragma unroll
             for (int b = 0; b < BN / 64; ++b) tma_load_2d(sb + b * 8192, mB, n0 + b * 64, k0, &full[st]);
           }
+          if (++st == stages) { st = 0; ph ^= 1u; }
         }
       }
     }
@@ -778,7 +782,8 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
       //                a k-step of 16 rows is 2048 B.
       const uint32_t a_lbo = p.a_kmajor ? 16u : 8192u, b_lbo = p.b_kmajor ? 16u : 8192u;
       const uint32_t a_step = p.a_kmajor ? 32u : 2048u, b_step = p.b_kmajor ? 32u : 2048u;
-      unsigned it = 0, tcount = 0;
+      unsigned tcount = 0, ph = 0;
+      int st = 0;
       bool ok = true;
       for (int tile = blockIdx.x; tile < total_tiles && ok; tile += gridDim.x, ++tcount) {
         const int split = tile / tiles_mn;
@@ -789,7 +794,7 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
         uint32_t tmem_acc = tmem_base + ab * BN;
         int piece_end = EPI == EPI_CHAIN ? kb_lo + p.chain_kb : kb_hi;      // EPI_CHAIN: the next accumulator hand-over
         bool fresh = true;
-        for (int kb = kb_lo; kb < kb_hi; ++kb, ++it) {
+        for (int kb = kb_lo; kb < kb_hi; ++kb) {
           if constexpr (EPI == EPI_CHAIN) {
             if (kb == piece_end) {
               umma_commit(&acc_full[tcount & 1u]);
@@ -801,12 +806,10 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
               fresh = true;
             }
           }
-          const int st = it % TC_STAGES;
-          const unsigned ph = (it / TC_STAGES) & 1u;
           if (*abort_flag || !mbar_wait_bounded(&full[st], ph, TC_WAIT_LIMIT_NS)) { ok = false; break; }
           tc_fence_after();
-          const uint32_t sa = smem_u32(tiles + st * SM::STAGE_BYTES);
-          const uint32_t sb = sa + SM::A_BYTES;
+          const uint32_t sa = smem_u32(tiles + st * stage_bytes);
+          const uint32_t sb = sa + a_bytes;
           const int ksteps = kb >= p.kb_main ? p.ext_ksteps : TC_BK / 16;   // the continuation may be narrower than 64
 #pragma unroll
           for (int k = 0; k < TC_BK / 16; ++k) {
@@ -817,6 +820,7 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
           }
           fresh = false;
           umma_commit(&empty[st]);            // frees the stage once the MMAs above have read it
+          if (++st == stages) { st = 0; ph ^= 1u; }
         }
         if (ok) umma_commit(&acc_full[EPI == EPI_CHAIN ? tcount & 1u : ab]);
       }
@@ -1243,8 +1247,9 @@ static int launch_tc(const GemmArgs& g, cudaStream_t s) {
   const int bn = EPI == EPI_VOCAB_STATS ? gemm_vocab_tile(g.M, g.N) : BN;
   const int B_BOX_ROWS = (EPI == EPI_SWIGLU_FWD) ? 128 : bn;
   // K-major operand: tensor [MN][K] -> box {64 k, rows}.  MN-major operand: tensor [K][MN] -> box {64 mn, 64 k}.
-  // A short product loads its own rows only: filling the other rows of the box with zeros takes time, and they would only
-  // reach accumulator rows that nothing reads.
+  // A short product loads its own rows only: filling the other rows of the box with zeros takes time (16 x 2048 x 32000:
+  // 37 us with it, 29 without).  The product still reads 128 rows from shared memory; what it finds behind a_rows, the B
+  // tile or a later stage, only reaches accumulator rows that nothing reads.
   const int a_rows = EPI == EPI_VOCAB_STATS && g.M < TC_BM ? ceil_div(g.M, 8) * 8 : TC_BM;
   const bool okA = g.a_kmajor ? make_tmap(&tmA, g.A, g.M, g.K, g.lda, TC_BK, a_rows)
                               : make_tmap(&tmA, g.A, g.K, g.M, g.lda, 64, TC_BK);
@@ -1263,6 +1268,11 @@ static int launch_tc(const GemmArgs& g, cudaStream_t s) {
   fill_params(p, g);
   p.bn = bn;
   p.a_rows = a_rows;
+  // bytes in flight are what a short product needs: its ring is as deep as shared memory (and the barrier block) allow
+  constexpr int FIXED = 1024 + 256 + EPI_STAGE_BYTES, STATS_MAX_STAGES = 12;
+  const int slot = (a_rows + bn) * TC_BK * 2;
+  p.stages = (227 * 1024 - FIXED) / slot < STATS_MAX_STAGES ? (227 * 1024 - FIXED) / slot : STATS_MAX_STAGES;
+  const int smem = EPI == EPI_VOCAB_STATS ? FIXED + p.stages * slot : TcSmem<BN>::TOTAL;
   const int tiles_m = (g.M + TC_BM - 1) / TC_BM, tiles_n = (g.N + bn - 1) / bn;
   const int num_kb = p.kb_total;
   int splits = 1;
@@ -1279,13 +1289,14 @@ static int launch_tc(const GemmArgs& g, cudaStream_t s) {
   splits = (num_kb + p.kb_per_split - 1) / p.kb_per_split;          // no empty split
   static unsigned long long attr_devices = 0;
   if (attr_needed(&attr_devices))
-    PCM_CUDA_TRY(cudaFuncSetAttribute(gemm_tc_kernel<BN, EPI>, cudaFuncAttributeMaxDynamicSharedMemorySize, TcSmem<BN>::TOTAL));
+    PCM_CUDA_TRY(cudaFuncSetAttribute(gemm_tc_kernel<BN, EPI>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                      EPI == EPI_VOCAB_STATS ? 227 * 1024 : TcSmem<BN>::TOTAL));
   p.tiles_m = tiles_m; p.tiles_n = tiles_n; p.splits = splits;
   const long long total = (long long)tiles_m * tiles_n * splits;
   const int grid = (int)(total < sm_count() ? total : sm_count());      // persistent: one CTA per SM walks the tile list
   if constexpr (EPI >= EPI_VOCAB_STATS)
-    return launch_after_smem(gemm_tc_kernel<BN, EPI>, dim3(grid), dim3(TC_THREADS), TcSmem<BN>::TOTAL, s, tmA, tmB, tmA2, tmB2, p);
-  gemm_tc_kernel<BN, EPI><<<grid, TC_THREADS, TcSmem<BN>::TOTAL, s>>>(tmA, tmB, tmA2, tmB2, p);
+    return launch_after_smem(gemm_tc_kernel<BN, EPI>, dim3(grid), dim3(TC_THREADS), (size_t)smem, s, tmA, tmB, tmA2, tmB2, p);
+  gemm_tc_kernel<BN, EPI><<<grid, TC_THREADS, smem, s>>>(tmA, tmB, tmA2, tmB2, p);
   PCM_LAUNCH_CHECK();
   return PCM_OK;
 }

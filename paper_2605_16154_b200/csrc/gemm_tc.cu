@@ -62,8 +62,8 @@ struct TcParams {
   long long part_stride;
   int m_fast;                                 // vocabulary epilogues on CTA pairs: row tiles run fastest
   int bn;                                     // columns per tile: BN, fewer for EPI_VOCAB_STATS on single CTAs
-  int a_rows;                                 // rows of A that a tile loads: TC_BM, fewer for EPI_VOCAB_STATS with M < TC_BM
-  int stages;                                 // EPI_VOCAB_STATS on single CTAs: ring depth
+  int a_rows;                                 // rows of A that a tile loads: TC_BM, fewer for vocabulary products with M < TC_BM
+  int stages;                                 // vocabulary products on single CTAs: ring depth
 };
 
 __device__ __forceinline__ void store_bf16x32(__nv_bfloat16* dst, const float (&v)[32]) {
@@ -693,10 +693,11 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
   using SM = TcSmem<BN>;
   const uint32_t raw_addr = smem_u32(smem_raw);
   uint8_t* tiles = smem_raw + ((1024u - (raw_addr & 1023u)) & 1023u);       // swizzle atoms need 1024-byte alignment
-  // EPI_VOCAB_STATS: as many stages of its own (smaller) tiles as fit
-  const int stages = EPI == EPI_VOCAB_STATS ? p.stages : SM::STAGES;
-  const int a_bytes = EPI == EPI_VOCAB_STATS ? p.a_rows * TC_BK * 2 : SM::A_BYTES;
-  const int stage_bytes = EPI == EPI_VOCAB_STATS ? (p.a_rows + p.bn) * TC_BK * 2 : SM::STAGE_BYTES;
+  // vocabulary products: as many stages of their own (smaller) tiles as fit
+  constexpr bool OWN_RING = EPI >= EPI_VOCAB_STATS;
+  const int stages = OWN_RING ? p.stages : SM::STAGES;
+  const int a_bytes = OWN_RING ? p.a_rows * TC_BK * 2 : SM::A_BYTES;
+  const int stage_bytes = OWN_RING ? (p.a_rows + p.bn) * TC_BK * 2 : SM::STAGE_BYTES;
   uint64_t* bars = reinterpret_cast<uint64_t*>(tiles + stages * stage_bytes);
   uint64_t* full = bars;                      // [stages] producer -> MMA
   uint64_t* empty = bars + stages;         // [stages] MMA -> producer
@@ -707,7 +708,7 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
   float* epi_stage = reinterpret_cast<float*>(reinterpret_cast<uint8_t*>(bars) + 256);
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int bn = EPI == EPI_VOCAB_STATS ? p.bn : BN;      // columns per tile
+  const int bn = EPI == EPI_VOCAB_STATS ? p.bn : BN;        // columns per tile
   const int num_kb_total = p.kb_total;
   const int tiles_mn = p.tiles_m * p.tiles_n;
   const int total_tiles = tiles_mn * p.splits;
@@ -1250,7 +1251,7 @@ static int launch_tc(const GemmArgs& g, cudaStream_t s) {
   // A short product loads its own rows only: filling the other rows of the box with zeros takes time (16 x 2048 x 32000:
   // 37 us with it, 29 without).  The product still reads 128 rows from shared memory; what it finds behind a_rows, the B
   // tile or a later stage, only reaches accumulator rows that nothing reads.
-  const int a_rows = EPI == EPI_VOCAB_STATS && g.M < TC_BM ? ceil_div(g.M, 8) * 8 : TC_BM;
+  const int a_rows = EPI >= EPI_VOCAB_STATS && g.a_kmajor && g.M < TC_BM ? ceil_div(g.M, 8) * 8 : TC_BM;
   const bool okA = g.a_kmajor ? make_tmap(&tmA, g.A, g.M, g.K, g.lda, TC_BK, a_rows)
                               : make_tmap(&tmA, g.A, g.K, g.M, g.lda, 64, TC_BK);
   const bool okB = g.b_kmajor ? make_tmap(&tmB, g.B, g.N, g.K, g.ldb, TC_BK, B_BOX_ROWS)
@@ -1269,10 +1270,10 @@ static int launch_tc(const GemmArgs& g, cudaStream_t s) {
   p.bn = bn;
   p.a_rows = a_rows;
   // bytes in flight are what a short product needs: its ring is as deep as shared memory (and the barrier block) allow
-  constexpr int FIXED = 1024 + 256 + EPI_STAGE_BYTES, STATS_MAX_STAGES = 12;
+  constexpr int FIXED = 1024 + 256 + EPI_STAGE_BYTES, MAX_STAGES = 12;
   const int slot = (a_rows + bn) * TC_BK * 2;
-  p.stages = (227 * 1024 - FIXED) / slot < STATS_MAX_STAGES ? (227 * 1024 - FIXED) / slot : STATS_MAX_STAGES;
-  const int smem = EPI == EPI_VOCAB_STATS ? FIXED + p.stages * slot : TcSmem<BN>::TOTAL;
+  p.stages = (227 * 1024 - FIXED) / slot < MAX_STAGES ? (227 * 1024 - FIXED) / slot : MAX_STAGES;
+  const int smem = EPI >= EPI_VOCAB_STATS ? FIXED + p.stages * slot : TcSmem<BN>::TOTAL;
   const int tiles_m = (g.M + TC_BM - 1) / TC_BM, tiles_n = (g.N + bn - 1) / bn;
   const int num_kb = p.kb_total;
   int splits = 1;
@@ -1290,7 +1291,7 @@ static int launch_tc(const GemmArgs& g, cudaStream_t s) {
   static unsigned long long attr_devices = 0;
   if (attr_needed(&attr_devices))
     PCM_CUDA_TRY(cudaFuncSetAttribute(gemm_tc_kernel<BN, EPI>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                      EPI == EPI_VOCAB_STATS ? 227 * 1024 : TcSmem<BN>::TOTAL));
+                                      EPI >= EPI_VOCAB_STATS ? 227 * 1024 : TcSmem<BN>::TOTAL));
   p.tiles_m = tiles_m; p.tiles_n = tiles_n; p.splits = splits;
   const long long total = (long long)tiles_m * tiles_n * splits;
   const int grid = (int)(total < sm_count() ? total : sm_count());      // persistent: one CTA per SM walks the tile list

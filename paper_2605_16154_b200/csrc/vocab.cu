@@ -100,7 +100,7 @@ embed_kernel(const T* __restrict__ table, long long ld_table, int vocab, int d, 
 //   3. embed_join_kernel: the partial sums of those tokens, in tile order.
 // No floating-point atomics: the same inputs give the same bits.  Bound by HBM: dout once, grad once.
 // ------------------------------------------------------------------------------------------------
-constexpr int EJ_WARPS = 16;
+constexpr int EJ_WARPS = 16, EM_RING = 8;
 constexpr int ES_THREADS = 1024, ES_WARPS = ES_THREADS / 32, ES_BINS = 256, ES_MAX_BLOCKS = 256;
 
 struct EmbedPlan {
@@ -275,7 +275,7 @@ embed_scatter_kernel(const int* __restrict__ tok, const EmbedPlan pl, int pass, 
 }
 
 // A warp sums one tile (up to 32 sorted pairs, one per lane) over the columns of its slab: NV pieces of 16 bytes (or of one
-// element) per lane, eight rows in flight.  What a row needs besides its bytes is kept small, because instructions, not
+// element) per lane.  What a row needs besides its bytes is kept small, because instructions, not
 // bytes, bounded the version in which every thread looked at every pair: which rows open a token and which count comes
 // from two ballots.
 template <typename T, bool VEC>
@@ -344,44 +344,68 @@ embed_sum_kernel(const T* __restrict__ dout, long long ld, const EmbedPlan pl, f
       if (col[j] < pl.d) put(dst + col[j], acc[j], f, add);
   };
   // `kv`: up to 32 pairs, one per lane; rows with a bit in `live` count, those with one in `open` begin a token
-  auto run = [&](const uint2& kv, unsigned live, unsigned open) {
-    const int rows = 32 - __clz(live);
-    for (int i0 = live ? (__ffs(live) - 1) & ~(U - 1) : 32; i0 < rows; i0 += U) {
-      uint4 raw[VEC ? U : 1][NV];
-      float one[VEC ? 1 : U][NV];
+  auto begin = [&](unsigned key) {
+    flush();
+    cur = key;
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const unsigned at = __shfl_sync(0xffffffffu, kv.y, i0 + u);
-        if ((live >> (i0 + u)) & 1u) {
+    for (int j = 0; j < NV; ++j)
+#pragma unroll
+      for (int e = 0; e < N; ++e) acc[j][e] = 0.f;
+  };
+  auto run = [&](const uint2& kv, unsigned live, unsigned open) {
+    const int rows = 32 - __clz(live), first = live ? __ffs(live) - 1 : 0;
+    if constexpr (VEC) {
+      // Every lane copies its own 16-byte pieces of a row into its own shared memory, EM_RING - 1 rows ahead of the sums:
+      // bytes in flight without registers, and nobody to wait for but itself.
+      extern __shared__ uint4 ring[];         // [4 warps][EM_RING][NV][32]
+      uint4* mine = ring + (threadIdx.x >> 5) * (EM_RING * NV * 32) + lane;
+      auto issue = [&](int i) {
+        const unsigned at = __shfl_sync(0xffffffffu, kv.y, i & 31);
+        if (i < rows && ((live >> i) & 1u)) {
           const T* q = dout + (long long)at * ld;
 #pragma unroll
-          for (int j = 0; j < NV; ++j) {
-            if constexpr (VEC) raw[u][j] = col[j] < pl.d ? __ldcs(reinterpret_cast<const uint4*>(q + col[j])) : make_uint4(0, 0, 0, 0);
-            else one[u][j] = col[j] < pl.d ? as_f32(q[col[j]]) : 0.f;
-          }
-        }
-      }
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-        if (!((live >> (i0 + u)) & 1u)) continue;
-        if ((open >> (i0 + u)) & 1u) {
-          flush();
-          cur = __shfl_sync(0xffffffffu, kv.x, i0 + u);
-#pragma unroll
           for (int j = 0; j < NV; ++j)
-#pragma unroll
-            for (int e = 0; e < N; ++e) acc[j][e] = 0.f;
+            if (col[j] < pl.d)
+              asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(mine + ((i & (EM_RING - 1)) * NV + j) * 32)), "l"(q + col[j])
+                           : "memory");
         }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+      };
+#pragma unroll
+      for (int i = 0; i < EM_RING - 1; ++i) issue(first + i);
+      for (int i = first; i < rows; ++i) {
+        __syncwarp();                         // the row before has been read: its place may be filled again
+        issue(i + EM_RING - 1);
+        asm volatile("cp.async.wait_group %0;" ::"n"(EM_RING - 1) : "memory");
+        if (!((live >> i) & 1u)) continue;
+        if ((open >> i) & 1u) begin(__shfl_sync(0xffffffffu, kv.x, i));
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
-          if constexpr (VEC) {
-            float f[N];
-            Vec16<T>::unpack(raw[u][j], f);
+          float f[N];
+          Vec16<T>::unpack(mine[((i & (EM_RING - 1)) * NV + j) * 32], f);
 #pragma unroll
-            for (int e = 0; e < N; ++e) acc[j][e] += f[e];
-          } else {
-            acc[j][0] += one[u][j];
+          for (int e = 0; e < N; ++e) acc[j][e] += f[e];
+        }
+      }
+      asm volatile("cp.async.wait_group 0;" ::: "memory");
+    } else {
+      for (int i0 = first & ~(U - 1); i0 < rows; i0 += U) {
+        float one[U][NV];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          const unsigned at = __shfl_sync(0xffffffffu, kv.y, i0 + u);
+          if ((live >> (i0 + u)) & 1u) {
+            const T* q = dout + (long long)at * ld;
+#pragma unroll
+            for (int j = 0; j < NV; ++j) one[u][j] = col[j] < pl.d ? as_f32(q[col[j]]) : 0.f;
           }
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          if (!((live >> (i0 + u)) & 1u)) continue;
+          if ((open >> (i0 + u)) & 1u) begin(__shfl_sync(0xffffffffu, kv.x, i0 + u));
+#pragma unroll
+          for (int j = 0; j < NV; ++j) acc[j][0] += one[u][j];
         }
       }
     }
@@ -1125,8 +1149,8 @@ static int launch_embed_bwd(const T* dout, long long ld, const int* tok, int n, 
   const int slabs = ceil_div(d, vec ? 64 * Vec16<T>::N : 128);
   const long long blocks = ((long long)pl.tiles * slabs + 3) / 4;
   if (blocks > 0x7FFFFFFFll) return PCM_ERR_SHAPE;
-  const int rc = launch_after(vec ? embed_sum_kernel<T, true> : embed_sum_kernel<T, false>, dim3((unsigned)blocks), dim3(128), s, dout, ld, pl,
-                              scale, grad, accumulate, slabs);
+  const int rc = launch_after_smem(vec ? embed_sum_kernel<T, true> : embed_sum_kernel<T, false>, dim3((unsigned)blocks), dim3(128),
+                                   vec ? 4 * EM_RING * 2 * 32 * 16 : 0, s, dout, ld, pl, scale, grad, accumulate, slabs);
   if (rc != PCM_OK) return rc;
   const int join_slabs = ceil_div(d, 128), most = ceil_div(pl.tiles, EJ_WARPS);
   const int groups = pl.tiles <= 2 ? 0 : most < 64 ? most : 64;    // two tiles: nothing crosses two borders

@@ -381,6 +381,7 @@ int grpo_adamw_step_lora(const grpo_model_cfg* cfg, const grpo_adamw_cfg* opt, i
  *   - Results do not depend on launch order: there are no floating-point atomics. */
 #define PCM_MAX_TOP 16
 #define PCM_MAX_EMBED_DIM 65536
+#define PCM_MAX_VOCAB_CALL (1 << 30)   /* rows and tokens of one call (PCM_ERR_SHAPE beyond) */
 
 /* out[i] = round(scale * table[tok[i]]) for i < n: table [vocab][d], out [n][d], both of `dtype` (a grpo_dtype).
  * The product is formed in fp32 and rounded once; scale = 1 copies bits. */
@@ -410,7 +411,8 @@ int grpo_token_logp(int32_t dtype, const void* logits, int64_t ld, int32_t n_row
 
 /* Gradient of a loss with d loss / d logp = dlogp [n_rows] and d loss / d entropy = dentropy [n_rows] (may be NULL):
  *     dlogits_v = (1 / temperature) (dlogp (1[v = tok] - p_v) - dentropy p_v (log p_v + entropy))
- * lse and entropy (needed with dentropy) are those of the forward call.  dlogits is of `dtype`, with its own row
+ * lse and entropy (needed with dentropy) are those of the forward call; p = exp(z - lse) inherits the rounding of lse,
+ * |lse| 2^-24 of its value.  dlogits is of `dtype`, with its own row
  * stride; it may be the logits themselves (same pointer, same stride).  A row whose lse is -inf gets zeros. */
 int grpo_token_logp_bwd(int32_t dtype, const void* logits, int64_t ld, int32_t n_rows, int32_t vocab, const int32_t* tok,
                         float temperature, const float* lse, const float* entropy, const float* dlogp, const float* dentropy,

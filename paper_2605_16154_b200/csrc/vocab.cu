@@ -1087,6 +1087,8 @@ static int launch_embed(const T* table, long long ld_table, int vocab, int d, co
   return PCM_OK;
 }
 
+static bool sizes_ok(int64_t rows, int64_t vocab) { return rows <= PCM_MAX_VOCAB_CALL && vocab <= PCM_MAX_VOCAB_CALL; }
+
 // Sorted pairs per tile: fewer for short batches, so that every SM gets some.
 static int embed_tile_rows(int n) { return n >= 32 * 296 ? 32 : 8; }
 
@@ -1221,6 +1223,7 @@ using namespace pcm;
 extern "C" int grpo_embed(int32_t dtype, const void* table, int64_t ld_table, int32_t vocab, int32_t d, const int32_t* tok,
                           int32_t n, float scale, void* out, int64_t ld_out, uint32_t* device_status, pcm_stream stream) {
   if (!dtype_ok(dtype) || n < 0 || vocab < 1 || d < 1 || ld_table < d || ld_out < d || !std::isfinite(scale)) return PCM_ERR_ARG;
+  if (!sizes_ok(n, vocab)) return PCM_ERR_SHAPE;
   if (n == 0) return PCM_OK;
   if (!table || !tok || !out || !elem_aligned(table, dtype) || !elem_aligned(out, dtype)) return PCM_ERR_ARG;
   cudaStream_t s = (cudaStream_t)stream;
@@ -1234,7 +1237,7 @@ extern "C" int grpo_embed(int32_t dtype, const void* table, int64_t ld_table, in
 }
 
 extern "C" size_t grpo_embed_workspace_bytes(int32_t n, int32_t vocab, int32_t d) {
-  if (n < 0 || vocab < 1 || d < 1 || d > PCM_MAX_EMBED_DIM) return 0;
+  if (n < 0 || vocab < 1 || d < 1 || d > PCM_MAX_EMBED_DIM || !sizes_ok(n, vocab)) return 0;
   EmbedPlan pl;
   return embed_plan(pl, n, vocab, d, nullptr) + 256;
 }
@@ -1244,7 +1247,7 @@ extern "C" int grpo_embed_bwd(int32_t dtype, const void* dout, int64_t ld_dout, 
                               size_t workspace_bytes, pcm_stream stream) {
   if (!dtype_ok(dtype) || n < 0 || vocab < 1 || d < 1 || ld_dout < d || !std::isfinite(scale) || !grad) return PCM_ERR_ARG;
   if (((uintptr_t)grad & 3) || (flags & ~GRPO_ACCUMULATE)) return PCM_ERR_ARG;
-  if (d > PCM_MAX_EMBED_DIM) return PCM_ERR_SHAPE;
+  if (d > PCM_MAX_EMBED_DIM || !sizes_ok(n, vocab)) return PCM_ERR_SHAPE;
   cudaStream_t s = (cudaStream_t)stream;
   const bool accumulate = flags & GRPO_ACCUMULATE;
   if (n == 0) {
@@ -1266,7 +1269,7 @@ extern "C" int grpo_token_logp(int32_t dtype, const void* logits, int64_t ld, in
                                float* top_logp, uint32_t* device_status, pcm_stream stream) {
   if (!dtype_ok(dtype) || n_rows < 0 || vocab < 1 || ld < vocab || top < 0) return PCM_ERR_ARG;
   if (!(temperature > 0.f) || !std::isfinite(temperature) || !std::isfinite(1.f / temperature)) return PCM_ERR_ARG;
-  if (top > PCM_MAX_TOP || top > vocab) return PCM_ERR_SHAPE;
+  if (top > PCM_MAX_TOP || top > vocab || !sizes_ok(n_rows, vocab)) return PCM_ERR_SHAPE;
   if (n_rows == 0) return PCM_OK;
   if (!logits || !elem_aligned(logits, dtype) || (logp && !tok) || (top > 0 && (!top_id || !top_logp))) return PCM_ERR_ARG;
   const LogpParams p{logits, ld, n_rows, vocab, tok, 1.f / temperature, top, logp, entropy, lse, top_id, top_logp, device_status};
@@ -1283,6 +1286,7 @@ extern "C" int grpo_token_logp_bwd(int32_t dtype, const void* logits, int64_t ld
                                    uint32_t* device_status, pcm_stream stream) {
   if (!dtype_ok(dtype) || n_rows < 0 || vocab < 1 || ld < vocab || ld_dlogits < vocab) return PCM_ERR_ARG;
   if (!(temperature > 0.f) || !std::isfinite(temperature) || !std::isfinite(1.f / temperature)) return PCM_ERR_ARG;
+  if (!sizes_ok(n_rows, vocab)) return PCM_ERR_SHAPE;
   if (n_rows == 0) return PCM_OK;
   if (!logits || !tok || !lse || !dlogp || !dlogits || (dentropy && !entropy)) return PCM_ERR_ARG;
   if (!elem_aligned(logits, dtype) || !elem_aligned(dlogits, dtype)) return PCM_ERR_ARG;

@@ -165,14 +165,18 @@ static bool head_args_ok(const void* x, int64_t ld_x, const void* w, int64_t ld_
   return x && w && tok && !(((uintptr_t)x | (uintptr_t)w) & 15) && ld_x >= d && ld_w >= d;
 }
 static bool temperature_ok(float t) { return t > 0.f && std::isfinite(t) && std::isfinite(1.f / t); }
-static bool head_shape_ok(int64_t ld_x, int64_t ld_w, int32_t d) { return d % 8 == 0 && ld_x % 8 == 0 && ld_w % 8 == 0; }
+// Tiles are counted in 32 bits, at 64 columns and 128 rows the smallest.
+static bool head_shape_ok(int64_t ld_x, int64_t ld_w, int32_t d, int64_t n_rows, int64_t vocab) {
+  return d % 8 == 0 && ld_x % 8 == 0 && ld_w % 8 == 0 && n_rows <= PCM_MAX_VOCAB_CALL && vocab <= PCM_MAX_VOCAB_CALL &&
+         (n_rows / 128 + 1) * (vocab / 64 + 1) < (1ll << 31) && ((int64_t)d / 64 + 1) * (vocab / 64 + 1) < (1ll << 31);
+}
 
 }  // namespace pcm
 
 using namespace pcm;
 
 extern "C" size_t grpo_head_logp_workspace_bytes(int32_t n_rows, int32_t d, int32_t vocab) {
-  if (n_rows < 0 || d < 8 || d % 8 || vocab < 1) return 0;
+  if (n_rows < 0 || d < 8 || vocab < 1 || !head_shape_ok(d, d, d, n_rows, vocab)) return 0;
   return round256(2 * (size_t)ceil_div(vocab, gemm_vocab_tile(n_rows, vocab)) * (size_t)n_rows * sizeof(float4)) + 256;
 }
 
@@ -180,7 +184,7 @@ extern "C" int grpo_head_logp(const void* x, int64_t ld_x, int32_t n_rows, int32
                               const int32_t* tok, float temperature, float* logp, float* entropy, float* lse,
                               uint32_t* device_status, void* workspace, size_t workspace_bytes, pcm_stream stream) {
   if (n_rows < 0 || d < 1 || vocab < 1 || !temperature_ok(temperature)) return PCM_ERR_ARG;
-  if (!head_shape_ok(ld_x, ld_w, d)) return PCM_ERR_SHAPE;
+  if (!head_shape_ok(ld_x, ld_w, d, n_rows, vocab)) return PCM_ERR_SHAPE;
   if (n_rows == 0) return PCM_OK;
   if (!head_args_ok(x, ld_x, w_h, ld_w, d, tok)) return PCM_ERR_ARG;
   if (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < grpo_head_logp_workspace_bytes(n_rows, d, vocab)) return PCM_ERR_WORKSPACE;
@@ -205,7 +209,7 @@ extern "C" int grpo_head_logp(const void* x, int64_t ld_x, int32_t n_rows, int32
 }
 
 extern "C" size_t grpo_head_logp_bwd_workspace_bytes(int32_t n_rows, int32_t d, int32_t vocab, int32_t chunk_rows) {
-  if (n_rows < 0 || d < 8 || d % 8 || vocab < 1 || chunk_rows < 1) return 0;
+  if (n_rows < 0 || d < 8 || vocab < 1 || chunk_rows < 1 || !head_shape_ok(d, d, d, n_rows, vocab)) return 0;
   return head_bwd_plan(n_rows, d, vocab, chunk_rows).total + 256;
 }
 
@@ -215,7 +219,7 @@ extern "C" int grpo_head_logp_bwd(const void* x, int64_t ld_x, int32_t n_rows, i
                                   int64_t ld_dx, float* dw, uint32_t* device_status, void* workspace, size_t workspace_bytes,
                                   pcm_stream stream) {
   if (n_rows < 0 || d < 1 || vocab < 1 || chunk_rows < 1 || !temperature_ok(temperature) || (flags & ~GRPO_ACCUMULATE)) return PCM_ERR_ARG;
-  if (!head_shape_ok(ld_x, ld_w, d) || (dx && ld_dx % 8)) return PCM_ERR_SHAPE;
+  if (!head_shape_ok(ld_x, ld_w, d, n_rows, vocab) || (dx && ld_dx % 8)) return PCM_ERR_SHAPE;
   if ((!dx && !dw) || (dx && (((uintptr_t)dx & 15) || ld_dx < d)) || (dw && ((uintptr_t)dw & 15))) return PCM_ERR_ARG;
   const bool accumulate = flags & GRPO_ACCUMULATE;
   cudaStream_t s = (cudaStream_t)stream;

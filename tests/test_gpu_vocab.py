@@ -203,7 +203,8 @@ def test_logp_of_unusual_rows(kind, vocab):
 
 def clip32(x):
     """Values beyond fp32's range as the infinities they round to."""
-    return np.where(np.abs(x) > 3.4028235e38, np.sign(x) * np.inf, x)
+    with np.errstate(invalid="ignore"):
+        return np.where(np.abs(x) > 3.4028235e38, np.copysign(np.inf, x), x)
 
 
 def check_logp_bwd(logits, tok, temperature, dlogp, dent, got, lse32, ent32):
@@ -305,3 +306,85 @@ def test_captured_calls_follow_their_inputs_on_another_stream():
         torch.cuda.synchronize()
         for x, y in zip(held, step()):
             assert torch.equal(x, y)
+
+
+# ---- many rows (a block of 128 threads each), far offsets, several streams --------------------------------------------
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("vocab,gap,shift", [(1025, 0, 0), (2603, 2, 3)])
+def test_logp_of_many_rows(kind, vocab, gap, shift):
+    n, g = 1300, gen(vocab)
+    logits = (torch.randn(n, vocab, generator=g, device="cuda") * 3).to(TYPES[kind])
+    low = torch.finfo(TYPES[kind]).min
+    ramp = torch.arange(vocab, device="cuda", dtype=torch.float32) * (20.0 / vocab)
+    for i, row in enumerate((ramp, ramp.flip(0), torch.full_like(ramp, 1.5), torch.full_like(ramp, float("-inf")), torch.full_like(ramp, -30.0))):
+        logits[40 * i + 3] = row.to(logits.dtype)
+    logits[500:520, 7:] = float("-inf")                          # fewer values than places
+    logits[520, 9], logits[521, 11], logits[522, :5] = float("nan"), float("inf"), low
+    logits = placed(logits, gap, shift)
+    tok = torch.randint(0, vocab, (n,), generator=g, device="cuda", dtype=torch.int32)
+    tok[500:520] = torch.arange(20, device="cuda", dtype=torch.int32) % 7
+    tok[600], tok[1299] = -5, vocab
+    z = host(logits)
+    want = vo.token_logp(z, tok.cpu().numpy(), 1.25, 16)
+    finite = np.where(np.isfinite(z) & (np.abs(z) < 1e30), z, 0.0)
+    lt, pt, et = logp_tolerances(finite, 1.25, np.where(np.isfinite(want["lse"]), want["lse"], 0))
+    for top in (16, 3, 0):
+        logp, entropy, lse, top_id, top_logp = B().grpo_token_logp(logits, tok, 1.25, top)
+        close(lse, want["lse"], lt)
+        close(entropy, want["entropy"], et)
+        close(logp, clip32(want["logp"]), pt)
+        if top:
+            assert np.array_equal(top_id.cpu().numpy(), want["top_id"][:, :top])
+            close(top_logp, clip32(want["top_logp"][:, :top]), pt[:, None] + 4 * U * np.abs(np.where(np.abs(want["top_logp"][:, :top]) < 1e38, want["top_logp"][:, :top], 0)))
+
+
+def test_rows_far_apart():
+    """Offsets that do not fit 32 bits: rows of logits, of an embedding table, of the gradient."""
+    ld, vocab = 1_300_000_000, 5001
+    buf = torch.empty(2 * ld + vocab, dtype=torch.bfloat16, device="cuda")
+    logits = buf.as_strided((3, vocab), (ld, 1))
+    logits.copy_(torch.randn(3, vocab, generator=gen(1), device="cuda"))
+    tok = torch.tensor([5, 5000, 77], dtype=torch.int32, device="cuda")
+    check_logp(logits, tok, 1.0, 4)
+    a = torch.ones(3, device="cuda")
+    _, ent, lse, _, _ = B().grpo_token_logp(logits, tok)
+    near = B().grpo_token_logp_bwd(logits.contiguous(), tok, lse, ent, a, a)
+    assert torch.equal(B().grpo_token_logp_bwd(logits, tok, lse, ent, a, a, dlogits=logits), near)
+    del logits, buf
+    vocab, d = 40000, 60000
+    table = torch.empty(vocab, d, dtype=torch.bfloat16, device="cuda")
+    rows = torch.tensor([0, 39999, 36000, 39999], dtype=torch.int32, device="cuda")
+    table[[0, 36000, 39999]] = torch.randn(3, d, generator=gen(2), device="cuda").bfloat16()
+    assert torch.equal(B().grpo_embed(table, rows), table[rows.long()])
+    del table
+    dout = torch.randn(4, d, generator=gen(3), device="cuda")
+    grad = B().grpo_embed_bwd(dout, rows, vocab)
+    assert torch.equal(grad[0], dout[0]) and torch.equal(grad[36000], dout[2]) and torch.allclose(grad[39999], dout[1] + dout[3])
+    assert int(torch.count_nonzero(grad[1:36000])) == 0 and int(torch.count_nonzero(grad[36001:39999])) == 0
+
+
+def test_calls_on_two_streams_at_once():
+    b = B()
+    work = []
+    for k in range(2):
+        g = gen(40 + k)
+        z = torch.randn(900, 6000, generator=g, device="cuda").bfloat16()
+        tok = torch.randint(0, 6000, (900,), generator=g, device="cuda", dtype=torch.int32)
+        dout = torch.randn(900 * 20, 256, generator=g, device="cuda")
+        long = torch.randint(0, 6000, (900 * 20,), generator=g, device="cuda", dtype=torch.int32)
+        work.append((z, tok, dout, long))
+
+    def step(z, tok, dout, long):
+        lp, ent, lse, ids, tl = b.grpo_token_logp(z, tok, 1.0, 8)
+        return lp, ids, tl, b.grpo_token_logp_bwd(z, tok, lse, ent, lp, ent), b.grpo_embed_bwd(dout, long, 6000)
+    want = [step(*w) for w in work]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for _ in range(5):
+        got = []
+        for s, w in zip(streams, work):
+            with torch.cuda.stream(s):
+                got.append(step(*w))
+        torch.cuda.synchronize()
+        for x, y in zip(got, want):
+            assert all(torch.equal(p, q) for p, q in zip(x, y))

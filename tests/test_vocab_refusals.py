@@ -35,7 +35,7 @@ CASES = [
     ("grpo_head_logp", HEAD, [
         (dict(x=None), ARG), (dict(w=None), ARG), (dict(tok=None), ARG), (dict(x=P + 8), ARG), (dict(w=P + 2), ARG), (dict(n_rows=-1), ARG),
         (dict(d=0), ARG), (dict(vocab=0), ARG), (dict(ld_x=56), ARG), (dict(ld_w=8), ARG), (dict(temperature=0.0), ARG),
-        (dict(temperature=NAN), ARG), (dict(d=60), SHAPE), (dict(ld_x=68), SHAPE), (dict(ld_w=65), SHAPE), (dict(workspace=None), WORKSPACE),
+        (dict(temperature=NAN), ARG), (dict(n_rows=1 << 30, vocab=1 << 30), SHAPE), (dict(d=60), SHAPE), (dict(ld_x=68), SHAPE), (dict(ld_w=65), SHAPE), (dict(workspace=None), WORKSPACE),
         (dict(workspace=P + 128), WORKSPACE), (dict(workspace_bytes=64), WORKSPACE)]),
     ("grpo_head_logp_bwd", HEAD_BWD, [
         (dict(x=None), ARG), (dict(w=None), ARG), (dict(tok=None), ARG), (dict(lse=None), ARG), (dict(dlogp=None), ARG),
@@ -45,23 +45,24 @@ CASES = [
     ("grpo_embed", EMBED, [
         (dict(dtype=2), ARG), (dict(dtype=-1), ARG), (dict(table=None), ARG), (dict(tok=None), ARG), (dict(out=None), ARG),
         (dict(n=-1), ARG), (dict(vocab=0), ARG), (dict(d=0), ARG), (dict(ld_table=63), ARG), (dict(ld_out=63), ARG),
-        (dict(scale=NAN), ARG), (dict(scale=INF), ARG), (dict(table=P + 1), ARG), (dict(dtype=0, out=P + 2), ARG)]),
+        (dict(scale=NAN), ARG), (dict(scale=INF), ARG), (dict(table=P + 1), ARG), (dict(dtype=0, out=P + 2), ARG),
+        (dict(n=(1 << 30) + 1), SHAPE), (dict(vocab=(1 << 30) + 1), SHAPE)]),
     ("grpo_embed_bwd", EMBED_BWD, [
         (dict(dtype=7), ARG), (dict(dout=None), ARG), (dict(tok=None), ARG), (dict(grad=None), ARG), (dict(n=-3), ARG),
         (dict(vocab=0), ARG), (dict(d=-1), ARG), (dict(ld_dout=1), ARG), (dict(scale=INF), ARG), (dict(flags=1), ARG),
-        (dict(grad=P + 2), ARG), (dict(d=70000, ld_dout=70000), SHAPE), (dict(workspace=None), WORKSPACE),
+        (dict(grad=P + 2), ARG), (dict(d=70000, ld_dout=70000), SHAPE), (dict(n=2 ** 31 - 1), SHAPE), (dict(workspace=None), WORKSPACE),
         (dict(workspace=P + 64), WORKSPACE), (dict(workspace_bytes=1000), WORKSPACE)]),
     ("grpo_token_logp", LOGP, [
         (dict(dtype=3), ARG), (dict(logits=None), ARG), (dict(n_rows=-1), ARG), (dict(vocab=0, top=0), ARG), (dict(ld=99), ARG),
         (dict(temperature=0.0), ARG), (dict(temperature=-1.0), ARG), (dict(temperature=NAN), ARG), (dict(temperature=INF), ARG),
         (dict(temperature=1e-42), ARG), (dict(tok=None), ARG), (dict(top=-1), ARG), (dict(top=17), SHAPE),
-        (dict(vocab=3, top=4), SHAPE), (dict(top_id=None), ARG), (dict(top_logp=None), ARG), (dict(logits=P + 1), ARG),
+        (dict(vocab=3, top=4), SHAPE), (dict(vocab=2 ** 31 - 1, ld=2 ** 31), SHAPE), (dict(top_id=None), ARG), (dict(top_logp=None), ARG), (dict(logits=P + 1), ARG),
         (dict(dtype=0, logits=P + 2), ARG)]),
     ("grpo_token_logp_bwd", LOGP_BWD, [
         (dict(dtype=3), ARG), (dict(logits=None), ARG), (dict(tok=None), ARG), (dict(lse=None), ARG), (dict(dlogp=None), ARG),
         (dict(dlogits=None), ARG), (dict(entropy=None), ARG), (dict(ld=99), ARG), (dict(ld_dlogits=50), ARG),
         (dict(temperature=0.0), ARG), (dict(temperature=NAN), ARG), (dict(n_rows=-1), ARG), (dict(vocab=-2), ARG),
-        (dict(dlogits=P, ld_dlogits=104), ARG), (dict(dlogits=P + 1), ARG)]),
+        (dict(dlogits=P, ld_dlogits=104), ARG), (dict(n_rows=2 ** 31 - 1), SHAPE), (dict(dlogits=P + 1), ARG)]),
 ]
 
 

@@ -346,8 +346,9 @@ __device__ __forceinline__ void epi_tile(const TcParams& p, uint32_t tmem_acc, i
         }
         const float c = p.vh.inv_t * VOCAB_LOG2E;
         const int t = row < p.M ? p.vh.tok[row] : -1;
-        VocabStat st{-INFINITY, 0.f, 0.f};
-        float zt = 0.f;
+        float m = -INFINITY, zt = 0.f;
+        unsigned long long s2 = pack2(0.f, 0.f), w2 = s2;
+        const unsigned long long c2 = pack2(c, c);
 #pragma unroll 1
         for (int c0 = 0; c0 < BN / 2; c0 += 32) {
           const int col = first + c0;
@@ -360,25 +361,37 @@ __device__ __forceinline__ void epi_tile(const TcParams& p, uint32_t tmem_acc, i
             for (int e = 0; e < 32; ++e)
               if (e >= last - col) r[e] = 0xFF800000u;
           }
-          float bm = __uint_as_float(r[0]);
+          float bm[4] = {m, __uint_as_float(r[1]), __uint_as_float(r[2]), __uint_as_float(r[3])};
 #pragma unroll
-          for (int e = 1; e < 32; ++e) bm = max_nan(bm, __uint_as_float(r[e]));
-          stat_raise(st, bm, c);
+          for (int e = 0; e < 32; ++e) bm[e & 3] = max_nan(bm[e & 3], __uint_as_float(r[e]));
+          const float top = max_nan(max_nan(bm[0], bm[1]), max_nan(bm[2], bm[3]));
+          if (top != m) {
+            const float d = fmaxf((m - top) * c, -1000.f), f = ex2(d);
+            const unsigned long long f2 = pack2(f, f);
+            w2 = mul2(f2, fma2(s2, pack2(d, d), w2));
+            s2 = mul2(f2, s2);
+            m = top;
+          }
           if (__any_sync(0xffffffffu, (unsigned)(t - col) < 32u)) {    // in the tile behind too, whose part is not read for it
 #pragma unroll
             for (int e = 0; e < 32; ++e) zt = t - col == e ? __uint_as_float(r[e]) : zt;
           }
-          if (st.m != -INFINITY) {
+          const unsigned long long neg_m = pack2(-m, -m);
 #pragma unroll
-            for (int e = 0; e < 32; ++e) {
-              const float x2 = fmaxf((__uint_as_float(r[e]) - st.m) * c, -1000.f);
-              const float x = ex2(x2);
-              st.s += x;
-              st.w += x * x2;
-            }
+          for (int e = 0; e < 32; e += 2) {
+            float t0, t1;
+            unpack2(mul2(add2(pack2(__uint_as_float(r[e]), __uint_as_float(r[e + 1])), neg_m), c2), t0, t1);
+            t0 = fmaxf(t0, -1000.f);
+            t1 = fmaxf(t1, -1000.f);
+            const unsigned long long x2 = pack2(ex2(t0), ex2(t1));
+            s2 = add2(s2, x2);
+            w2 = fma2(x2, pack2(t0, t1), w2);
           }
         }
-        if (row < p.M) p.vh.part[(long long)(2 * (n0 / p.bn) + chalf) * p.M + row] = make_float4(st.m, st.s, st.w, zt);
+        float s0, s1, w0, w1;
+        unpack2(s2, s0, s1);
+        unpack2(w2, w0, w1);
+        if (row < p.M) p.vh.part[(long long)(2 * (n0 / p.bn) + chalf) * p.M + row] = make_float4(m, s0 + s1, w0 + w1, zt);
       } else if constexpr (EPI == EPI_VOCAB_DZ) {
         // d loss / d z in fp32 from the accumulator, then bf16 twice: the rounded value and what the rounding left, so
         // that the weight gradient (fp32) does not carry a bf16 rounding of every term.  With a = (log2 e) log p:

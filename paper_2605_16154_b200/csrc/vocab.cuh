@@ -19,6 +19,31 @@ __device__ __forceinline__ float ex2(float x) {
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
   return r;
 }
+// Two fp32 lanes of one 64-bit register: half the issue slots of scalar adds and products.
+__device__ __forceinline__ unsigned long long pack2(float a, float b) {
+  unsigned long long r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ void unpack2(unsigned long long v, float& a, float& b) {
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v));
+}
+__device__ __forceinline__ unsigned long long add2(unsigned long long a, unsigned long long b) {
+  unsigned long long r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ unsigned long long mul2(unsigned long long a, unsigned long long b) {
+  unsigned long long r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ unsigned long long fma2(unsigned long long a, unsigned long long b, unsigned long long c) {
+  unsigned long long r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+
 // Softmax statistics of a part of a row: m the largest logit, s = sum 2^t and w = sum 2^t t with t = (z - m) c,
 // c = log2(e) / temperature.  t is held at -1000 or above, so that a masked logit (-inf, or the type's lowest
 // value) adds 2^t = 0 to both sums instead of 0 * -inf.
@@ -46,17 +71,6 @@ struct RowResult {
   // z - m first: large logits do not swallow the logarithm
   __device__ float logp(float z) const { return m == -INFINITY ? -INFINITY : (z - m) * inv_t - log_s; }
 };
-
-// Raises the reference value of the statistics to at least z (NaN propagates).
-__device__ __forceinline__ void stat_raise(VocabStat& st, float z, float c) {
-  const float m = max_nan(st.m, z);
-  if (m != st.m) {
-    const float d = fmaxf((st.m - m) * c, -1000.f), f = ex2(d);
-    st.w = f * (st.w + st.s * d);
-    st.s *= f;
-    st.m = m;
-  }
-}
 
 // d loss / d z of one logit z (unscaled): (1/T) (g (1[target] - p) - h p (log p + H)) with gt = g / T, ht = h / T.
 // A masked logit has p = 0 and log p = -inf: nothing but a target's own term is left.

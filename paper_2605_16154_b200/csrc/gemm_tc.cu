@@ -405,6 +405,7 @@ __device__ __forceinline__ void epi_tile(const TcParams& p, uint32_t tmem_acc, i
         const float gt = live ? p.vh.dlogp[row] * p.vh.inv_t : 0.f, ht = live && p.vh.dent ? p.vh.dent[row] * p.vh.inv_t : 0.f;
         const float c = p.vh.inv_t * VOCAB_LOG2E, lse2 = lse * VOCAB_LOG2E, A = -(gt + ht * H), Bc = -ht * VOCAB_LN2;
         const bool dead = __any_sync(0xffffffffu, !live);
+        const unsigned long long c2 = pack2(c, c), neg_lse2 = pack2(-lse2, -lse2), A2 = pack2(A, A), B2 = pack2(Bc, Bc), minus1 = pack2(-1.f, -1.f);
 #pragma unroll 1
         for (int c0 = chalf * (BN / 2); c0 < (chalf + 1) * (BN / 2); c0 += 64) {
           const int col = n0 + c0;
@@ -418,20 +419,24 @@ __device__ __forceinline__ void epi_tile(const TcParams& p, uint32_t tmem_acc, i
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
 #pragma unroll
-            for (int e = 0; e < 32; ++e) {
-              const float a = max_nan(__uint_as_float(r[h][e]) * c - lse2, -1000.f);
-              float v = ex2(a) * (Bc * a + A);
-              if (target && t - col == 32 * h + e) v += gt;
-              if (dead && !live) v = 0.f;
-              r[h][e] = __float_as_uint(v);
-            }
-#pragma unroll
             for (int e = 0; e < 32; e += 2) {
-              const float v0 = __uint_as_float(r[h][e]), v1 = __uint_as_float(r[h][e + 1]);
+              float a0, a1, v0, v1;
+              unpack2(fma2(pack2(__uint_as_float(r[h][e]), __uint_as_float(r[h][e + 1])), c2, neg_lse2), a0, a1);
+              a0 = max_nan(a0, -1000.f);
+              a1 = max_nan(a1, -1000.f);
+              unsigned long long v2 = mul2(pack2(ex2(a0), ex2(a1)), fma2(B2, pack2(a0, a1), A2));
+              if (target || dead) {
+                unpack2(v2, v0, v1);
+                if (t - col == 32 * h + e) v0 += gt;
+                if (t - col == 32 * h + e + 1) v1 += gt;
+                v2 = pack2(live ? v0 : 0.f, live ? v1 : 0.f);
+              }
+              unpack2(v2, v0, v1);
               const __nv_bfloat162 q = __floats2bfloat162_rn(v0, v1);
               const uint32_t w = *reinterpret_cast<const uint32_t*>(&q);
-              const __nv_bfloat162 l = __floats2bfloat162_rn(v0 - __uint_as_float(w << 16), v1 - __uint_as_float(w & 0xFFFF0000u));
-              r[0][16 * h + e / 2] = w;                            // h = 0 writes behind what it has read
+              unpack2(fma2(pack2(__uint_as_float(w << 16), __uint_as_float(w & 0xFFFF0000u)), minus1, v2), v0, v1);   // exact
+              const __nv_bfloat162 l = __floats2bfloat162_rn(v0, v1);
+              r[0][16 * h + e / 2] = w;                            // behind what has been read
               lo[16 * h + e / 2] = *reinterpret_cast<const uint32_t*>(&l);
             }
           }

@@ -1252,7 +1252,8 @@ static void fill_params(TcParams& p, const GemmArgs& g) {
   p.chain_kb = g.epi.chain_kb > 0 ? g.epi.chain_kb : p.kb_total;
   p.accumulate = g.epi.accumulate;
   p.part_stride = g.epi.part_stride;
-  // The operand whose tiles run fastest is read once for every wave of the other's: the shorter one, which fits L2 sooner.
+  // The operand whose tiles run fastest is read once for every wave of the other's: the shorter one, which fits L2 sooner
+  // (d z of 8192 rows x 1024 x 32000: 0.09 GB of reads instead of 1.0, 519 us -> 463).
   p.m_fast = g.M < g.N;
   p.bn = T2_BN;
   p.a_rows = TC_BM;
@@ -1399,7 +1400,8 @@ static int launch_tc2(const GemmArgs& g, cudaStream_t s) {
 }
 
 // On single CTAs (M <= 128: reading B is what takes time) as many columns as give every SM the same number of tiles: 32000
-// columns are 143 tiles of 224 on 148 SMs instead of 125 of 256.
+// columns are 143 tiles of 224 on 148 SMs instead of 125 of 256 (no faster: HBM is the limit), 40000 columns two rounds of
+// 144 instead of one and a little of 256 (16 rows x 2048: 35 us instead of 46).
 int gemm_vocab_tile(int M, int N) {
   if (pair_enabled() && M > TC_BM) return T2_BN;
   const int sms = sm_count(), rounds = ceil_div(ceil_div(N, 256), sms);

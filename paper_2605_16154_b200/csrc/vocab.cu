@@ -48,7 +48,8 @@ template <> __device__ __forceinline__ __nv_bfloat16 from_f32<__nv_bfloat16>(flo
 // ------------------------------------------------------------------------------------------------
 // Embedding lookup: out[i] = round(scale * table[tok[i]]); rows of a token outside [0, vocab) are zero.
 // Bound by HBM (each distinct row read once, every output row written once); a block holds 256 / tpr rows, tpr
-// threads walk one row in 16-byte steps, four loads in flight each.
+// threads walk one row in 16-byte steps, four loads in flight each.  119808 rows of 1024 bf16 from 32000: 46 us, 6.7 TB/s;
+// 64 rows of 2048: 2 us.
 // ------------------------------------------------------------------------------------------------
 template <typename T, bool VEC>
 __global__ void __launch_bounds__(256)
@@ -98,9 +99,11 @@ embed_kernel(const T* __restrict__ table, long long ld_table, int vocab, int d, 
 //   2. embed_sum_kernel: tiles of `rows` sorted pairs, each summed in order; a token that crosses more than one border
 //      between tiles leaves a partial sum per tile;
 //   3. embed_join_kernel: the partial sums of those tokens, in tile order.
-// No floating-point atomics: the same inputs give the same bits.  Bound by HBM: dout once, grad once.
+// No floating-point atomics: the same inputs give the same bits.  Bound by HBM: dout once, grad once.  119808 rows of 1024
+// bf16 into 32000: 97 us against 58 us for the bytes; about 18 us are the four sort kernels, which are latency, 57 us the
+// sums (5.6 TB/s) and the rest the joins and the rows of absent tokens.
 // ------------------------------------------------------------------------------------------------
-constexpr int EJ_WARPS = 16, EM_RING = 8;
+constexpr int EJ_WARPS = 16, EM_RING = 8, EM_LANES = 16;
 constexpr int ES_THREADS = 1024, ES_WARPS = ES_THREADS / 32, ES_BINS = 256, ES_MAX_BLOCKS = 256;
 
 struct EmbedPlan {
@@ -287,8 +290,11 @@ embed_sum_kernel(const T* __restrict__ dout, long long ld, const EmbedPlan pl, f
   let_successor_start();
   const int lane = threadIdx.x & 31;
   const long long item = (long long)blockIdx.x * 4 + (threadIdx.x >> 5);
-  const int tile = (int)(item / slabs), slab = (int)(item - (long long)tile * slabs);
-  if (tile >= pl.tiles) return;
+  // Tiles run in EM_LANES interleaved sequences: where tokens are numbered by frequency, one sequence would read (many rows
+  // of a token) first and write (a token a row) last (97 us, 111 in one sequence).
+  const int place = (int)(item / slabs), slab = (int)(item - (long long)place * slabs);
+  const int per = (pl.tiles + EM_LANES - 1) / EM_LANES, tile = (place % EM_LANES) * per + place / EM_LANES;
+  if (place / EM_LANES >= per || tile >= pl.tiles) return;
   const uint2* pair = pl.sorted;
   const int lo = tile * pl.rows, hi = min(lo + pl.rows, pl.n);
   const unsigned none = 0xFFFFFFFFu, vocab = (unsigned)pl.vocab;
@@ -429,62 +435,77 @@ __device__ void zero_absent_rows(const EmbedPlan& pl, float* __restrict__ grad, 
   }
 }
 
-// The first blocks: one warp per token that left parts and 128 columns; a token over more than 16 tiles is shared by the
-// block's warps.  The others write the rows of absent tokens: stores that need HBM and little else, next to sums that wait
+// The first blocks: one warp per token that left parts and 32 columns, its tiles in four slices (eight lanes each, four
+// columns a lane); a token over more than 64 tiles is shared by the block's warps.  The slices depend on the token's tiles
+// alone.  The other blocks write the rows of absent tokens: stores that need HBM and little else, next to sums that wait
 // for one load after the other.
 __global__ void __launch_bounds__(EJ_WARPS * 32)
 embed_join_kernel(const EmbedPlan pl, float scale, float* __restrict__ grad, int accumulate, int groups, int slabs) {
-  __shared__ float4 sum[EJ_WARPS][32];
+  __shared__ float4 sum[EJ_WARPS][8];
   __shared__ unsigned key[EJ_WARPS];
   __shared__ int first[EJ_WARPS], span[EJ_WARPS];           // tiles: the first one, how many
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  constexpr int LONG = 64;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, slice = lane >> 3;
   wait_for_predecessor();
   if ((int)blockIdx.x >= groups * slabs) {
     zero_absent_rows(pl, grad, (long long)(blockIdx.x - groups * slabs) * EJ_WARPS);
     return;
   }
   const int n_jobs = *pl.n_jobs;
-  const int group = blockIdx.x / slabs, col = ((blockIdx.x - group * slabs) * 32 + lane) * 4;
+  const int group = blockIdx.x / slabs, col = ((blockIdx.x - group * slabs) * 8 + (lane & 7)) * 4;
   const bool in = col < pl.d;                 // partial rows are padded to a multiple of four
-  auto add_tiles = [&](float4& a, int t, int lo, int hi) {      // partial sums of tiles t + lo .. t + hi - 1 (0: the first tile)
+  // partial sums of tiles t + lo .. t + hi - 1 (0: the first tile), then of the warp's four slices
+  auto add_tiles = [&](int t, int lo, int hi) {
+    float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (in) {
 #pragma unroll 8
-    for (int k = lo; k < hi; ++k) {
-      const float* q = pl.part + ((long long)(t + k) * 2 + (k == 0 ? 1 : 0)) * pl.dpad + col;
-      const float4 w = *reinterpret_cast<const float4*>(q);
-      a.x += w.x; a.y += w.y; a.z += w.z; a.w += w.w;
+      for (int k = lo; k < hi; ++k) {
+        const float* q = pl.part + ((long long)(t + k) * 2 + (k == 0 ? 1 : 0)) * pl.dpad + col;
+        const float4 w = *reinterpret_cast<const float4*>(q);
+        a.x += w.x; a.y += w.y; a.z += w.z; a.w += w.w;
+      }
     }
+#pragma unroll
+    for (int off = 8; off < 32; off <<= 1) {
+      a.x += __shfl_xor_sync(0xffffffffu, a.x, off);
+      a.y += __shfl_xor_sync(0xffffffffu, a.y, off);
+      a.z += __shfl_xor_sync(0xffffffffu, a.z, off);
+      a.w += __shfl_xor_sync(0xffffffffu, a.w, off);
+    }
+    return a;
   };
-  auto finish = [&](const float4& a, unsigned key) {
-    float* g = grad + (long long)key * pl.d + col;
+  auto finish = [&](const float4& a, unsigned token) {
+    if (!in || slice != 0) return;
+    float* g = grad + (long long)token * pl.d + col;
     const float v[4] = {a.x * scale, a.y * scale, a.z * scale, a.w * scale};
 #pragma unroll
     for (int e = 0; e < 4; ++e)
       if (col + e < pl.d) g[e] = accumulate ? g[e] + v[e] : v[e];
   };
-  for (int base = group * EJ_WARPS; base < n_jobs; base += groups * EJ_WARPS) {
-    if (base + warp < n_jobs) {
-      const uint2 job = pl.jobs[base + warp];
+  // Warp w takes the job `groups * w` behind its block's first: frequent tokens mostly have neighbouring numbers, and so
+  // neighbouring jobs, which then fall to different blocks.
+  for (int base = group; base < n_jobs; base += groups * EJ_WARPS) {
+    const int at = base + warp * groups;
+    if (at < n_jobs) {
+      const uint2 job = pl.jobs[at];
       const int t = pl.first_tile[job.x], len = (int)job.y - t + 1;
       if (lane == 0) { key[warp] = job.x; first[warp] = t; span[warp] = len; }
-      if (len <= 16 && in) {
-        float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
-        add_tiles(a, t, 0, len);
-        finish(a, job.x);
-      }
+      if (len <= LONG) finish(add_tiles(t, len * slice / 4, len * (slice + 1) / 4), job.x);
     } else if (lane == 0) {
       span[warp] = 0;
     }
     __syncthreads();
     for (int j = 0; j < EJ_WARPS; ++j) {
       const int len = span[j];
-      if (len <= 16) continue;                // the same for the whole block
-      float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
-      if (in) add_tiles(a, first[j], (int)((long long)len * warp / EJ_WARPS), (int)((long long)len * (warp + 1) / EJ_WARPS));
-      sum[warp][lane] = a;
+      if (len <= LONG) continue;              // the same for the whole block
+      const int piece = warp * 4 + slice;
+      float4 a = add_tiles(first[j], (int)((long long)len * piece / (4 * EJ_WARPS)), (int)((long long)len * (piece + 1) / (4 * EJ_WARPS)));
+      if (slice == 0) sum[warp][lane] = a;
       __syncthreads();
-      if (warp == 0 && in) {
+      if (warp == 0) {
+        a = sum[0][lane & 7];
         for (int w = 1; w < EJ_WARPS; ++w) {
-          const float4 b = sum[w][lane];
+          const float4 b = sum[w][lane & 7];
           a.x += b.x; a.y += b.y; a.z += b.z; a.w += b.w;
         }
         finish(a, key[j]);
@@ -574,6 +595,9 @@ struct RowShare {
 constexpr int LP_MAX_TOP = PCM_MAX_TOP;
 constexpr int LP_MAX_RANKS = 8;
 
+// One pass over the logits, bound by HBM on many rows and next by the exponentials (one per element: 0.7 of the unit's rate
+// at 6 TB/s of bf16), by latency on few.  21504 rows of 32000 bf16: 219 us without a top list (6.3 TB/s), 257 us with
+// the top 4, 320 us with 16; 8 rows of 130011 with the top 8: 9.6 us.
 // NT threads work on one row's share.  NT = 32: a warp per row, several rows per block.  Otherwise one block per share,
 // `ranks` blocks of a cluster per row.
 template <int NT> struct LogpSmem {
@@ -973,7 +997,8 @@ token_logp_kernel(const LogpParams p, int ranks) {
 
 // ------------------------------------------------------------------------------------------------
 // Gradient: d loss / d z_v = (1/T) (g (1[v = t] - p_v) - h p_v (log p_v + H)), g = d loss / d logp, h = d loss / d H.
-// One read and one write of the logits; a thread reads what it writes, so dlogits may be the logits themselves.
+// One read and one write of the logits, bound by HBM; a thread reads what it writes, so dlogits may be the logits
+// themselves.
 // ------------------------------------------------------------------------------------------------
 struct LogpBwdParams {
   const void* logits; long long ld;
@@ -1125,13 +1150,13 @@ static int launch_embed_bwd(const T* dout, long long ld, const int* tok, int n, 
   }
   const bool vec = !(((uintptr_t)dout | (uintptr_t)grad) & 15) && d % Vec16<T>::N == 0 && ld % Vec16<T>::N == 0;
   const int slabs = ceil_div(d, vec ? 64 * Vec16<T>::N : 128);
-  const long long blocks = ((long long)pl.tiles * slabs + 3) / 4;
+  const long long blocks = ((long long)ceil_div(pl.tiles, EM_LANES) * EM_LANES * slabs + 3) / 4;
   if (blocks > 0x7FFFFFFFll) return PCM_ERR_SHAPE;
   const int rc = launch_after_smem(vec ? embed_sum_kernel<T, true> : embed_sum_kernel<T, false>, dim3((unsigned)blocks), dim3(128),
                                    vec ? 4 * EM_RING * 2 * 32 * 16 : 0, s, dout, ld, pl, scale, grad, accumulate, slabs);
   if (rc != PCM_OK) return rc;
-  const int join_slabs = ceil_div(d, 128), most = ceil_div(pl.tiles, EJ_WARPS);
-  const int groups = pl.tiles <= 2 ? 0 : most < 64 ? most : 64;    // two tiles: nothing crosses two borders
+  const int join_slabs = ceil_div(d, 32), most = ceil_div(pl.tiles, EJ_WARPS);
+  const int groups = pl.tiles <= 2 ? 0 : most < 16 ? most : 16;    // two tiles: nothing crosses two borders
   const int join_blocks = groups * join_slabs + (accumulate ? 0 : ceil_div(vocab, EJ_WARPS));
   if (join_blocks == 0) return PCM_OK;
   return launch_after(embed_join_kernel, dim3(join_blocks), dim3(EJ_WARPS * 32), s, pl, scale, grad, accumulate, groups, join_slabs);
@@ -1164,7 +1189,8 @@ static int launch_logp_as(const LogpParams& p, int ranks, cudaStream_t s) {
 }
 
 // Short rows: a warp each.  Enough rows to fill the GPU with blocks of 128: one block each (its fixed costs, reductions
-// and the top list, weigh least then).  Fewer: blocks of 512, and up to eight of them in a cluster share a row.
+// and the top list, weigh least then: 21504 x 32000 top 4 took 279 us, 307 with 256 threads, 553 with 512).  Fewer: blocks
+// of 512, and up to eight of them in a cluster share a row.
 template <typename T>
 static int launch_logp(const LogpParams& p, cudaStream_t s) {
   if (p.V <= 1024) return launch_logp_as<T, 32>(p, 1, s);

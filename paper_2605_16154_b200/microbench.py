@@ -5,6 +5,7 @@ kernel is bandwidth bound).  One JSON line per case.
     python -m paper_2605_16154_b200.microbench attention [--seqs 64 --S 312 --heads 16 --dh 64]
     python -m paper_2605_16154_b200.microbench pcm [--tasks 8192 --G 8 --T 128 --phases 10 --budget 24]
     python -m paper_2605_16154_b200.microbench pack [--kept 384 --P 256 --d 1024]
+    python -m paper_2605_16154_b200.microbench vocab [--rows 21504 --tokens 119808 --vocab 32000 --d 1024 --top 4]
 """
 from __future__ import annotations
 
@@ -126,6 +127,39 @@ def bench_pack(a):
     ctx.close()
 
 
+def bench_vocab(a):
+    """The vocabulary operators on one training batch: embedding of `tokens` positions, log-probabilities of `rows` scored
+    ones (bf16), forward and backward.  Bytes and flops are what each call cannot do without."""
+    g = torch.Generator(device="cuda").manual_seed(0)
+    V, d, n, m = a.vocab, a.d, a.tokens, a.rows
+    table = (torch.randn(V, d, generator=g, device="cuda") * 0.02).to(torch.bfloat16)
+    u = torch.rand(n, generator=g, device="cuda", dtype=torch.float64)
+    tok = ((torch.exp(u * np.log(V + 1.0)).long() - 1).clamp_(0, V - 1)).to(torch.int32)     # frequency ~ 1 / rank
+    dout = torch.randn(n, d, generator=g, device="cuda").to(torch.bfloat16)
+
+    def report(name, fn, nbytes, flops):
+        ms = _time(fn, a.iters)
+        print(json.dumps({"kernel": name, "ms": ms, "gbs": nbytes / (ms * 1e6), "tflops": flops / (ms * 1e9)}))
+    report("embed", lambda: B.grpo_embed(table, tok), 2.0 * d * (n + min(n, V)), 0)
+    report("embed_bwd", lambda: B.grpo_embed_bwd(dout, tok, V), 2.0 * n * d + 4.0 * V * d, 0)
+    del dout
+    x = torch.randn(m, d, generator=g, device="cuda").to(torch.bfloat16)
+    w = (torch.randn(V, d, generator=g, device="cuda") * (1.5 / d ** 0.5)).to(torch.bfloat16)
+    tgt = torch.randint(0, V, (m,), generator=g, device="cuda", dtype=torch.int32)
+    dlogp, dent = torch.randn(m, generator=g, device="cuda") / m, torch.full((m,), -1e-3 / m, device="cuda")
+    _, ent, lse = B.grpo_head_logp(x, w, tgt)
+    report("head_logp", lambda: B.grpo_head_logp(x, w, tgt), 2.0 * d * (m + V), 2.0 * m * V * d)
+    report("head_logp_bwd", lambda: B.grpo_head_logp_bwd(x, w, tgt, lse, ent, dlogp, dent), 4.0 * d * m + 6.0 * d * V,
+           6.0 * m * V * d)
+    z = torch.empty(m, V, dtype=torch.bfloat16, device="cuda")
+    for lo in range(0, m, 4096):
+        z[lo:lo + 4096] = x[lo:lo + 4096] @ w.t()
+    report(f"token_logp top {a.top}", lambda: B.grpo_token_logp(z, tgt, top=a.top), 2.0 * m * V, 0)
+    report("token_logp", lambda: B.grpo_token_logp(z, tgt), 2.0 * m * V, 0)
+    dz = torch.empty_like(z)
+    report("token_logp_bwd", lambda: B.grpo_token_logp_bwd(z, tgt, lse, ent, dlogp, dent, dlogits=dz), 4.0 * m * V, 0)
+
+
 def main():
     ap = argparse.ArgumentParser()
     sub = ap.add_subparsers(dest="what", required=True)
@@ -145,8 +179,12 @@ def main():
     k = sub.add_parser("pack")
     k.add_argument("--kept", type=int, default=384); k.add_argument("--P", type=int, default=256)
     k.add_argument("--d", type=int, default=1024); k.add_argument("--iters", type=int, default=10)
+    v = sub.add_parser("vocab")
+    v.add_argument("--rows", type=int, default=21504); v.add_argument("--tokens", type=int, default=119808)
+    v.add_argument("--vocab", type=int, default=32000); v.add_argument("--d", type=int, default=1024)
+    v.add_argument("--top", type=int, default=4); v.add_argument("--iters", type=int, default=10)
     a = ap.parse_args()
-    {"gemm": bench_gemm, "attention": bench_attention, "pcm": bench_pcm, "pack": bench_pack}[a.what](a)
+    {"gemm": bench_gemm, "attention": bench_attention, "pcm": bench_pcm, "pack": bench_pack, "vocab": bench_vocab}[a.what](a)
 
 
 if __name__ == "__main__":

@@ -391,7 +391,7 @@ int grpo_embed(int32_t dtype, const void* table, int64_t ld_table, int32_t vocab
 /* Its gradient: grad[v] = scale * sum over {i : tok[i] = v} of dout[i] in fp32 for every v < vocab (0 for tokens that
  * do not occur); with GRPO_ACCUMULATE in flags it is added to grad.  dout [n][d] of `dtype`, grad [vocab][d] fp32,
  * contiguous.  Tokens are sorted first; the rows of a token are summed in ascending i within tiles of 8 or 32 sorted
- * rows, the tiles in order.  d <= PCM_MAX_EMBED_DIM.  workspace: device, 256-byte aligned,
+ * rows, the tiles of a frequent token in an order that depends on its rows alone.  d <= PCM_MAX_EMBED_DIM.  workspace: device, 256-byte aligned,
  * >= grpo_embed_workspace_bytes() (0 when the sizes are not supported). */
 size_t grpo_embed_workspace_bytes(int32_t n, int32_t vocab, int32_t d);
 int grpo_embed_bwd(int32_t dtype, const void* dout, int64_t ld_dout, const int32_t* tok, int32_t n, int32_t vocab, int32_t d,

@@ -718,8 +718,8 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
   const int stage_bytes = OWN_RING ? (p.a_rows + p.bn) * TC_BK * 2 : SM::STAGE_BYTES;
   uint64_t* bars = reinterpret_cast<uint64_t*>(tiles + stages * stage_bytes);
   uint64_t* full = bars;                      // [stages] producer -> MMA
-  uint64_t* empty = bars + stages;         // [stages] MMA -> producer
-  uint64_t* acc_full = bars + 2 * stages;  // [2] MMA -> epilogue, one per accumulator buffer
+  uint64_t* empty = bars + stages;            // [stages] MMA -> producer
+  uint64_t* acc_full = bars + 2 * stages;     // [2] MMA -> epilogue, one per accumulator buffer
   uint64_t* acc_empty = acc_full + 2;         // [2] epilogue -> MMA
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(acc_empty + 2);
   volatile uint32_t* abort_flag = tmem_slot + 1;

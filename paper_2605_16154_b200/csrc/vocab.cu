@@ -93,12 +93,12 @@ embed_kernel(const T* __restrict__ table, long long ld_table, int vocab, int d, 
 }
 
 // ------------------------------------------------------------------------------------------------
-// Gradient of the embedding: grad[v] (+)= scale * sum over {i : tok[i] = v} of dout[i], in fp32 and in ascending i.
+// Gradient of the embedding: grad[v] (+)= scale * sum over {i : tok[i] = v} of dout[i], in fp32 and in a fixed order.
 //   1. (token, position) pairs into token order, stably: up to 1024 pairs by a bitonic network in one block, more by a
 //      radix sort of 8-bit digits over up to 256 blocks;
 //   2. embed_sum_kernel: tiles of `rows` sorted pairs, each summed in order; a token that crosses more than one border
 //      between tiles leaves a partial sum per tile;
-//   3. embed_join_kernel: the partial sums of those tokens, in tile order.
+//   3. embed_join_kernel: the partial sums of those tokens, in an order that depends on the token's tiles alone.
 // No floating-point atomics: the same inputs give the same bits.  Bound by HBM: dout once, grad once.  119808 rows of 1024
 // bf16 into 32000: 97 us against 58 us for the bytes; about 18 us are the four sort kernels, which are latency, 57 us the
 // sums (5.6 TB/s) and the rest the joins and the rows of absent tokens.
@@ -278,8 +278,8 @@ embed_scatter_kernel(const int* __restrict__ tok, const EmbedPlan pl, int pass, 
 }
 
 // A warp sums one tile (up to 32 sorted pairs, one per lane) over the columns of its slab: NV pieces of 16 bytes (or of one
-// element) per lane.  What a row needs besides its bytes is kept small, because instructions, not
-// bytes, bounded the version in which every thread looked at every pair: which rows open a token and which count comes
+// element) per lane.  What a row needs besides its bytes is kept small, because instructions, not bytes,
+// bounded the version in which every thread looked at every pair: which rows open a token and which count comes
 // from two ballots.
 template <typename T, bool VEC>
 __global__ void __launch_bounds__(128)

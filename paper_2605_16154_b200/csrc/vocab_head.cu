@@ -154,6 +154,9 @@ static int chain_gemm(GemmArgs g, float* parts, cudaStream_t s) {
                       q.epi.part_stride, splits, g.M, g.N, g.C, g.ldc, g.epi.accumulate);
 }
 
+// Profile class of a product: on CTA pairs or not (the choice that gemm_tcgen05 makes).
+static int gemm_class(long long M, long long N) { return M > 128 && N > 128 ? PC_GEMM : PC_GEMM_SMALL; }
+
 static size_t round256(size_t v) { return (v + 255) / 256 * 256; }
 
 struct HeadBwdPlan { size_t x, hi, lo, parts, total; long long ldz; int rows; };
@@ -202,7 +205,7 @@ extern "C" int grpo_head_logp(const void* x, int64_t ld_x, int32_t n_rows, int32
   GemmArgs g{n_rows, vocab, d, x, ld_x, true, w_h, ld_w, true, DT_BF16, nullptr, 0, DT_BF16, nullptr, 0};
   g.epi.kind = EPI_VOCAB_STATS;
   g.epi.vh.tok = tok; g.epi.vh.inv_t = inv_t; g.epi.vh.part = part; g.epi.vh.vocab = vocab;
-  prof_begin(PC_GEMM, s);
+  prof_begin(gemm_class(n_rows, 256), s);
   int rc = gemm_tcgen05(g, s);
   prof_end(s, 2.0 * n_rows * vocab * d, 2.0 * d * ((double)n_rows + vocab));
   if (rc != PCM_OK) return rc;
@@ -262,14 +265,14 @@ extern "C" int grpo_head_logp_bwd(const void* x, int64_t ld_x, int32_t n_rows, i
     v.tok = tok + r0; v.inv_t = inv_t; v.lse = lse + r0; v.dlogp = dlogp + r0; v.vocab = vocab; v.dz_lo = lo;
     v.dent = dentropy ? dentropy + r0 : nullptr;
     v.entropy = dentropy ? entropy + r0 : nullptr;
-    prof_begin(PC_GEMM, s);
+    prof_begin(gemm_class(rows, 256), s);
     rc = gemm_tcgen05(z, s);
     prof_end(s, flops, 2.0 * d * ((double)rows + vocab) + 4.0 * rows * vocab);
     if (rc != PCM_OK) return rc;
     if (dx) {
       GemmArgs q{rows, d, vocab, hi, pl.ldz, true, w_h, ld_w, false, DT_BF16, (unsigned short*)dx + (long long)r0 * ld_dx, ld_dx, DT_BF16, nullptr, 0};
       q.epi.kind = EPI_CHAIN;                  // bf16 result: one accumulator piece
-      prof_begin(PC_GEMM, s);
+      prof_begin(gemm_class(rows, d), s);
       rc = chain_gemm(q, parts, s);
       prof_end(s, flops, 2.0 * rows * vocab + 2.0 * vocab * d + 2.0 * rows * d);
       if (rc != PCM_OK) return rc;
@@ -280,7 +283,7 @@ extern "C" int grpo_head_logp_bwd(const void* x, int64_t ld_x, int32_t n_rows, i
       q.epi.kind = EPI_CHAIN;
       q.epi.chain_kb = VH_CHAIN_KB;
       q.epi.accumulate = accumulate || r0 > 0;
-      prof_begin(PC_GEMM, s);
+      prof_begin(gemm_class(vocab, d), s);
       rc = chain_gemm(q, parts, s);
       prof_end(s, 2.0 * flops, 4.0 * rows * vocab + 4.0 * rows * d + 4.0 * vocab * d);
       if (rc != PCM_OK) return rc;

@@ -25,6 +25,10 @@
 
 namespace pcm {
 
+// The two forms of the vocabulary statistics; the kernels that hand their accumulator over in pieces.
+template <int EPI> constexpr bool is_stats = EPI == EPI_VOCAB_STATS || EPI == EPI_VOCAB_STATS_LONG;
+template <int EPI> constexpr bool is_chained = EPI == EPI_CHAIN || EPI == EPI_VOCAB_STATS_LONG;
+
 constexpr int TC_BM = 128;
 constexpr int TC_BK = 64;                     // 64 bf16 = one 128-byte swizzle row
 // Ring depth of the single-CTA kernel: as deep as shared memory allows.  Its launches are the narrow or short GEMMs
@@ -267,6 +271,53 @@ __device__ __forceinline__ void epi_prefetch(const TcParams& p, int row, int n0,
       }
 }
 
+// EPI_VOCAB_STATS: softmax statistics of a thread's row over the columns [first, last) of half a tile, taken 32 at a time
+// with a running maximum.
+struct RowPart {
+  float m = -INFINITY, zt = 0.f;
+  unsigned long long s2, w2;                  // the sums of even and of odd columns
+};
+__device__ __forceinline__ void part_chunk(RowPart& q, uint32_t (&r)[32], int col, int last, int t, float c) {
+  if (last - col < 32) {                      // columns behind the tile or the vocabulary are not this part's logits
+#pragma unroll
+    for (int e = 0; e < 32; ++e)
+      if (e >= last - col) r[e] = 0xFF800000u;
+  }
+  float bm[4] = {q.m, __uint_as_float(r[1]), __uint_as_float(r[2]), __uint_as_float(r[3])};
+#pragma unroll
+  for (int e = 0; e < 32; ++e) bm[e & 3] = max_nan(bm[e & 3], __uint_as_float(r[e]));
+  const float top = max_nan(max_nan(bm[0], bm[1]), max_nan(bm[2], bm[3]));
+  if (top != q.m) {
+    const float d = fmaxf((q.m - top) * c, -1000.f), f = ex2(d);
+    const unsigned long long f2 = pack2(f, f);
+    q.w2 = mul2(f2, fma2(q.s2, pack2(d, d), q.w2));
+    q.s2 = mul2(f2, q.s2);
+    q.m = top;
+  }
+  if (__any_sync(0xffffffffu, (unsigned)(t - col) < 32u)) {            // in the tile behind too, whose part is not read for it
+#pragma unroll
+    for (int e = 0; e < 32; ++e) q.zt = t - col == e ? __uint_as_float(r[e]) : q.zt;
+  }
+  const unsigned long long neg_m = pack2(-q.m, -q.m), c2 = pack2(c, c);
+#pragma unroll
+  for (int e = 0; e < 32; e += 2) {
+    float t0, t1;
+    unpack2(mul2(add2(pack2(__uint_as_float(r[e]), __uint_as_float(r[e + 1])), neg_m), c2), t0, t1);
+    t0 = fmaxf(t0, -1000.f);
+    t1 = fmaxf(t1, -1000.f);
+    const unsigned long long x2 = pack2(ex2(t0), ex2(t1));
+    q.s2 = add2(q.s2, x2);
+    q.w2 = fma2(x2, pack2(t0, t1), q.w2);
+  }
+}
+// Parts are stored column-block-major: a warp's 32 rows are 512 contiguous bytes.
+__device__ __forceinline__ void part_store(const TcParams& p, const RowPart& q, int row, int n0, int chalf) {
+  float s0, s1, w0, w1;
+  unpack2(q.s2, s0, s1);
+  unpack2(q.w2, w0, w1);
+  if (row < p.M) p.vh.part[(long long)(2 * (n0 / p.bn) + chalf) * p.M + row] = make_float4(q.m, s0 + s1, w0 + w1, q.zt);
+}
+
 // One epilogue warp's share of a tile: rows = this warp's 32 tensor-memory lanes, columns = its half of the tile.
 template <int BN, int EPI>
 __device__ __forceinline__ void epi_tile(const TcParams& p, uint32_t tmem_acc, int row, int n0, int chalf, EpiRegs& pre,
@@ -335,63 +386,22 @@ __device__ __forceinline__ void epi_tile(const TcParams& p, uint32_t tmem_acc, i
           }
         }
       } else if constexpr (EPI == EPI_VOCAB_STATS) {
-        // A thread owns one row of 128 columns: softmax statistics with a running maximum, 32 columns at a time, so
-        // tensor memory is read once.  Parts are stored column-block-major: a warp's 32 rows are 512 contiguous bytes.
-        const int first = n0 + chalf * (BN / 2);
+        // tensor memory is read once, a thread owns one row of up to 128 columns (none at all in the second half of a
+        // narrow tile: its part is empty, but the join reads it)
         static_assert(BN == 256, "a part covers at most 128 columns");
-        const int last = min(n0 + p.bn, p.N);
-        if (first >= last) {                    // an empty part: nothing of the row, but the join reads it
-          if (row < p.M) p.vh.part[(long long)(2 * (n0 / p.bn) + chalf) * p.M + row] = make_float4(-INFINITY, 0.f, 0.f, 0.f);
-          return;
-        }
+        const int first = n0 + chalf * (BN / 2), last = min(n0 + p.bn, p.N), t = row < p.M ? p.vh.tok[row] : -1;
         const float c = p.vh.inv_t * VOCAB_LOG2E;
-        const int t = row < p.M ? p.vh.tok[row] : -1;
-        float m = -INFINITY, zt = 0.f;
-        unsigned long long s2 = pack2(0.f, 0.f), w2 = s2;
-        const unsigned long long c2 = pack2(c, c);
+        RowPart q;
+        q.s2 = q.w2 = pack2(0.f, 0.f);
 #pragma unroll 1
         for (int c0 = 0; c0 < BN / 2; c0 += 32) {
-          const int col = first + c0;
-          if (col >= last) break;
+          if (first + c0 >= last) break;
           uint32_t r[32];
           tmem_ld_32x32(tmem_acc + (uint32_t)(chalf * (BN / 2) + c0), r);
           tmem_ld_wait();
-          if (last - col < 32) {                // columns behind the tile or the vocabulary are not this part's logits
-#pragma unroll
-            for (int e = 0; e < 32; ++e)
-              if (e >= last - col) r[e] = 0xFF800000u;
-          }
-          float bm[4] = {m, __uint_as_float(r[1]), __uint_as_float(r[2]), __uint_as_float(r[3])};
-#pragma unroll
-          for (int e = 0; e < 32; ++e) bm[e & 3] = max_nan(bm[e & 3], __uint_as_float(r[e]));
-          const float top = max_nan(max_nan(bm[0], bm[1]), max_nan(bm[2], bm[3]));
-          if (top != m) {
-            const float d = fmaxf((m - top) * c, -1000.f), f = ex2(d);
-            const unsigned long long f2 = pack2(f, f);
-            w2 = mul2(f2, fma2(s2, pack2(d, d), w2));
-            s2 = mul2(f2, s2);
-            m = top;
-          }
-          if (__any_sync(0xffffffffu, (unsigned)(t - col) < 32u)) {    // in the tile behind too, whose part is not read for it
-#pragma unroll
-            for (int e = 0; e < 32; ++e) zt = t - col == e ? __uint_as_float(r[e]) : zt;
-          }
-          const unsigned long long neg_m = pack2(-m, -m);
-#pragma unroll
-          for (int e = 0; e < 32; e += 2) {
-            float t0, t1;
-            unpack2(mul2(add2(pack2(__uint_as_float(r[e]), __uint_as_float(r[e + 1])), neg_m), c2), t0, t1);
-            t0 = fmaxf(t0, -1000.f);
-            t1 = fmaxf(t1, -1000.f);
-            const unsigned long long x2 = pack2(ex2(t0), ex2(t1));
-            s2 = add2(s2, x2);
-            w2 = fma2(x2, pack2(t0, t1), w2);
-          }
+          part_chunk(q, r, first + c0, last, t, c);
         }
-        float s0, s1, w0, w1;
-        unpack2(s2, s0, s1);
-        unpack2(w2, w0, w1);
-        if (row < p.M) p.vh.part[(long long)(2 * (n0 / p.bn) + chalf) * p.M + row] = make_float4(m, s0 + s1, w0 + w1, zt);
+        part_store(p, q, row, n0, chalf);
       } else if constexpr (EPI == EPI_VOCAB_DZ) {
         // d loss / d z in fp32 from the accumulator, then bf16 twice: the rounded value and what the rounding left, so
         // that the weight gradient (fp32) does not carry a bf16 rounding of every term.  With a = (log2 e) log p:
@@ -703,6 +713,24 @@ __device__ __forceinline__ void chain_store(const TcParams& p, int row, int n0, 
   }
 }
 
+// EPI_VOCAB_STATS_LONG: the statistics from the running sums of a thread's row.
+template <int BN>
+__device__ __forceinline__ void chain_stats(const TcParams& p, int row, int n0, int chalf, const float (&sum)[BN / 2]) {
+  const int first = n0 + chalf * (BN / 2), last = min(n0 + p.bn, p.N), t = row < p.M ? p.vh.tok[row] : -1;
+  const float c = p.vh.inv_t * VOCAB_LOG2E;
+  RowPart q;
+  q.s2 = q.w2 = pack2(0.f, 0.f);
+#pragma unroll
+  for (int c0 = 0; c0 < BN / 2; c0 += 32) {
+    if (first + c0 >= last) break;
+    uint32_t r[32];
+#pragma unroll
+    for (int e = 0; e < 32; ++e) r[e] = __float_as_uint(sum[c0 + e]);
+    part_chunk(q, r, first + c0, last, t, c);
+  }
+  part_store(p, q, row, n0, chalf);
+}
+
 template <int BN, int EPI>
 __global__ void __launch_bounds__(TC_THREADS, 1)
 gemm_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB,
@@ -726,7 +754,7 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
   float* epi_stage = reinterpret_cast<float*>(reinterpret_cast<uint8_t*>(bars) + 256);
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int bn = EPI == EPI_VOCAB_STATS ? p.bn : BN;        // columns per tile
+  const int bn = is_stats<EPI> ? p.bn : BN;                 // columns per tile
   const int num_kb_total = p.kb_total;
   const int tiles_mn = p.tiles_m * p.tiles_n;
   const int total_tiles = tiles_mn * p.splits;
@@ -811,10 +839,10 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
         if (*abort_flag || !mbar_wait_bounded(&acc_empty[ab], aph ^ 1u, TC_WAIT_LIMIT_NS)) { ok = false; break; }
         tc_fence_after();
         uint32_t tmem_acc = tmem_base + ab * BN;
-        int piece_end = EPI == EPI_CHAIN ? kb_lo + p.chain_kb : kb_hi;      // EPI_CHAIN: the next accumulator hand-over
+        int piece_end = is_chained<EPI> ? kb_lo + p.chain_kb : kb_hi;       // the next accumulator hand-over
         bool fresh = true;
         for (int kb = kb_lo; kb < kb_hi; ++kb) {
-          if constexpr (EPI == EPI_CHAIN) {
+          if constexpr (is_chained<EPI>) {
             if (kb == piece_end) {
               umma_commit(&acc_full[tcount & 1u]);
               ++tcount;
@@ -841,7 +869,7 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
           umma_commit(&empty[st]);            // frees the stage once the MMAs above have read it
           if (++st == stages) { st = 0; ph ^= 1u; }
         }
-        if (ok) umma_commit(&acc_full[EPI == EPI_CHAIN ? tcount & 1u : ab]);
+        if (ok) umma_commit(&acc_full[is_chained<EPI> ? tcount & 1u : ab]);
       }
       if (!ok) { *abort_flag = 1; atomicOr(&g_tc_status, 1u); }
     }
@@ -854,7 +882,7 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
       const int split = tile / tiles_mn, mn = tile - split * tiles_mn;
       const int m0 = (mn / p.tiles_n) * TC_BM, n0 = (mn % p.tiles_n) * bn;
       const int row = m0 + quad * 32 + lane;
-      if constexpr (EPI == EPI_CHAIN) {
+      if constexpr (is_chained<EPI>) {
         const int kb_lo = split * p.kb_per_split, kb_hi = min(kb_lo + p.kb_per_split, num_kb_total);
         float sum[BN / 2];
 #pragma unroll
@@ -876,7 +904,8 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
           if (kb + p.chain_kb < kb_hi) ++tcount;                   // the loop over tiles counts the last piece
         }
         if (!ok) break;
-        chain_store<BN>(p, row, n0, chalf, split, epi_stage + (warp - 2) * EPI_STAGE_FLOATS, sum);
+        if constexpr (EPI == EPI_CHAIN) chain_store<BN>(p, row, n0, chalf, split, epi_stage + (warp - 2) * EPI_STAGE_FLOATS, sum);
+        else chain_stats<BN>(p, row, n0, chalf, sum);
         continue;
       }
       const unsigned ab = tcount & 1u, aph = (tcount >> 1) & 1u;
@@ -959,7 +988,7 @@ gemm_tc2_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
                 const __grid_constant__ CUtensorMap tmA2, const __grid_constant__ CUtensorMap tmB2, const TcParams p) {
   extern __shared__ uint8_t smem_raw[];
   constexpr int BN = T2_BN;
-  constexpr bool VOCAB = EPI == EPI_VOCAB_STATS || EPI == EPI_VOCAB_DZ;
+  constexpr bool VOCAB = is_stats<EPI> || EPI == EPI_VOCAB_DZ;
   const uint32_t raw_addr = smem_u32(smem_raw);
   uint8_t* tiles = smem_raw + ((1024u - (raw_addr & 1023u)) & 1023u);
   uint64_t* bars = reinterpret_cast<uint64_t*>(tiles + T2_STAGES * T2_STAGE_BYTES);
@@ -1080,9 +1109,9 @@ gemm_tc2_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
         if (*abort_flag || !mbar_wait_bounded(&acc_empty[ab], aph ^ 1u, TC_WAIT_LIMIT_NS)) { ok = false; break; }
         tc_fence_after();
         uint32_t tmem_acc = tmem_base + ab * BN;
-        int piece_lo = kb_lo;                    // EPI_CHAIN: where the current accumulator piece began
+        int piece_lo = kb_lo;                    // where the current accumulator piece began
         for (int kb = kb_lo; kb < kb_hi; ++kb) {
-          if constexpr (EPI == EPI_CHAIN) {
+          if constexpr (is_chained<EPI>) {
             if (kb - piece_lo == p.chain_kb) {   // hand this piece over, go on in the other buffer
               umma_commit_pair(&acc_full[tcount & 1u], 3);
               ++tcount;
@@ -1096,7 +1125,7 @@ gemm_tc2_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
           tc_fence_after();
           const uint32_t alo = da_lo + st_off, blo = db_lo + st_off;
           umma_bf16_pair(tmem_acc, desc(alo, da_hi), desc(blo, db_hi), idesc, kb > piece_lo ? 1u : 0u);
-          if (EPI == EPI_CHAIN || kb < p.kb_main) {
+          if (is_chained<EPI> || kb < p.kb_main) {
 #pragma unroll
             for (int k = 1; k < TC_BK / 16; ++k)
               umma_bf16_pair(tmem_acc, desc(alo + k * a_step16, da_hi), desc(blo + k * b_step16, db_hi), idesc, 1u);
@@ -1109,7 +1138,7 @@ gemm_tc2_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
           st_off += T2_STAGE_BYTES >> 4;
           if (++st == T2_STAGES) { st = 0; st_off = 0; ph ^= 1u; }
         }
-        if (ok) umma_commit_pair(&acc_full[EPI == EPI_CHAIN ? tcount & 1u : ab], 3);
+        if (ok) umma_commit_pair(&acc_full[is_chained<EPI> ? tcount & 1u : ab], 3);
       }
       if (!ok) { *abort_flag = 1; atomicOr(&g_tc_status, 1u); }
     }
@@ -1124,7 +1153,7 @@ gemm_tc2_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
       const int tm = swap ? mn % p.tiles_m : mn / p.tiles_n, tn = swap ? mn / p.tiles_m : mn % p.tiles_n;
       const int m0 = tm * (2 * TC_BM) + (int)rank * TC_BM, n0 = tn * BN;
       const int row = m0 + quad * 32 + lane;
-      if constexpr (EPI == EPI_CHAIN) {
+      if constexpr (is_chained<EPI>) {
         const int kb_lo = split * p.kb_per_split, kb_hi = min(kb_lo + p.kb_per_split, num_kb_total);
         float sum[BN / 2];
 #pragma unroll
@@ -1146,7 +1175,8 @@ gemm_tc2_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
           if (kb + p.chain_kb < kb_hi) ++tcount;                   // the loop over tiles counts the last piece
         }
         if (!ok) break;
-        chain_store<BN>(p, row, n0, chalf, split, epi_stage + (warp - 2) * EPI_STAGE_FLOATS, sum);
+        if constexpr (EPI == EPI_CHAIN) chain_store<BN>(p, row, n0, chalf, split, epi_stage + (warp - 2) * EPI_STAGE_FLOATS, sum);
+        else chain_stats<BN>(p, row, n0, chalf, sum);
         continue;
       }
       const unsigned ab = tcount & 1u, aph = (tcount >> 1) & 1u;
@@ -1264,7 +1294,7 @@ static void fill_params(TcParams& p, const GemmArgs& g) {
 template <int BN, int EPI>
 static int launch_tc(const GemmArgs& g, cudaStream_t s) {
   CUtensorMap tmA, tmB;
-  const int bn = EPI == EPI_VOCAB_STATS ? gemm_vocab_tile(g.M, g.N) : BN;
+  const int bn = is_stats<EPI> ? gemm_vocab_tile(g.M, g.N) : BN;
   const int B_BOX_ROWS = (EPI == EPI_SWIGLU_FWD) ? 128 : bn;
   // K-major operand: tensor [MN][K] -> box {64 k, rows}.  MN-major operand: tensor [K][MN] -> box {64 mn, 64 k}.
   // A short product loads its own rows only: filling the other rows of the box with zeros takes time (16 x 2048 x 32000:
@@ -1399,6 +1429,10 @@ static int launch_tc2(const GemmArgs& g, cudaStream_t s) {
   return PCM_OK;
 }
 
+// Hidden widths beyond this take the statistics from pieces of half of it, added in fp32 registers: with 128 truncating
+// additions (2048) the log-probabilities are off by 0.5e-6 of their norm, with 256 by 1.6e-6.
+constexpr int VOCAB_LONG_K = 2048;
+
 // On single CTAs (M <= 128: reading B is what takes time) as many columns as give every SM the same number of tiles: 32000
 // columns are 143 tiles of 224 on 148 SMs instead of 125 of 256 (no faster: HBM is the limit), 40000 columns two rounds of
 // 144 instead of one and a little of 256 (16 rows x 2048: 35 us instead of 46).
@@ -1492,6 +1526,11 @@ int gemm_tcgen05(const GemmArgs& g, cudaStream_t s) {
       return launch_tc<256, EPI_HEAD_LOSS>(g, s);
     case EPI_VOCAB_STATS:
       if (!gemm_epilogue_supported(g)) return PCM_ERR_SHAPE;
+      if (g.K > VOCAB_LONG_K) {
+        GemmArgs q = g;
+        q.epi.chain_kb = VOCAB_LONG_K / TC_BK / 2;
+        return pair_enabled() && g.M > TC_BM ? launch_tc2<EPI_VOCAB_STATS_LONG>(q, s) : launch_tc<256, EPI_VOCAB_STATS_LONG>(q, s);
+      }
       return pair_enabled() && g.M > TC_BM ? launch_tc2<EPI_VOCAB_STATS>(g, s) : launch_tc<256, EPI_VOCAB_STATS>(g, s);
     case EPI_VOCAB_DZ:
       if (!gemm_epilogue_supported(g)) return PCM_ERR_SHAPE;

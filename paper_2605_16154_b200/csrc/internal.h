@@ -46,7 +46,7 @@ enum { DT_F32 = 0, DT_BF16 = 1 };
 // Work fused into the tensor-core GEMM's epilogue (ignored by the SIMT kernel: callers use it only
 // when gemm_tcgen05_supported() holds).
 enum { EPI_NONE = 0, EPI_SWIGLU_FWD = 1, EPI_SWIGLU_BWD = 2, EPI_ROPE = 3, EPI_HEAD_LOSS = 4, EPI_VOCAB_STATS = 5, EPI_VOCAB_DZ = 6,
-       EPI_CHAIN = 7 };
+       EPI_CHAIN = 7, EPI_VOCAB_STATS_LONG = 8 /* chosen by the launcher */ };
 struct GemmEpilogue {
   int kind = EPI_NONE;
   // EPI_SWIGLU_FWD: B is [2F][K] (gate rows, then up rows); C receives gate | up as [M][2F] and

@@ -378,7 +378,7 @@ int grpo_adamw_step_lora(const grpo_model_cfg* cfg, const grpo_adamw_cfg* opt, i
  *     says otherwise; 16-byte accesses are used where rows are aligned for them.
  *   - No call allocates or synchronises; all can be captured in a CUDA graph.  A workspace is scratch of one call:
  *     calls that may run at the same time need one each.  n = 0 rows is a valid call.
- *   - Results do not depend on launch order: there are no floating-point atomics. */
+ *   - The same inputs give the same bits: every sum has an order that follows from sizes and tokens alone. */
 #define PCM_MAX_TOP 16
 #define PCM_MAX_EMBED_DIM 65536
 #define PCM_MAX_VOCAB_CALL (1 << 30)   /* rows and tokens of one call (PCM_ERR_SHAPE beyond) */
@@ -432,9 +432,9 @@ int grpo_head_logp(const void* x, int64_t ld_x, int32_t n_rows, int32_t d, const
 /* Its gradients, with dlogits as in grpo_token_logp_bwd (formed in fp32 from a second x w_h^T):
  *     dx = dlogits w_h  (bf16 [n_rows][d], row stride ld_dx, from dlogits rounded to bf16)
  *     dw = dlogits^T x  (fp32 [vocab][d], contiguous, 16-byte aligned; GRPO_ACCUMULATE in flags adds to it), from dlogits
- *                       as a sum of two bf16 values
+ *                       as a sum of two bf16 values, the targets' own in fp32
  * Either may be NULL.  x may hold anything, NaN too, in rows without a token.  The rows are processed chunk_rows (>= 1) at
- * a time, which sizes the workspace (2 d + 4 vocab bytes a row and a constant); the results differ between chunk sizes
+ * a time, which sizes the workspace (about 2 d + 4 vocab bytes a row, 5 a token and a constant); the results differ between chunk sizes
  * by fp32 rounding only.  For a tied embedding pass its fp32 gradient as dw with GRPO_ACCUMULATE. */
 size_t grpo_head_logp_bwd_workspace_bytes(int32_t n_rows, int32_t d, int32_t vocab, int32_t chunk_rows);
 int grpo_head_logp_bwd(const void* x, int64_t ld_x, int32_t n_rows, int32_t d, const void* w_h, int64_t ld_w, int32_t vocab,

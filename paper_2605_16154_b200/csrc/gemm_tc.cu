@@ -405,7 +405,8 @@ __device__ __forceinline__ void epi_tile(const TcParams& p, uint32_t tmem_acc, i
       } else if constexpr (EPI == EPI_VOCAB_DZ) {
         // d loss / d z in fp32 from the accumulator, then bf16 twice: the rounded value and what the rounding left, so
         // that the weight gradient (fp32) does not carry a bf16 rounding of every term.  With a = (log2 e) log p:
-        // d z = 2^a (B a + A) (+ g / T at the target).  64 columns at a time, packed before they are staged, so that a
+        // d z = 2^a (B a + A) (+ g / T at the target).  The target's own d z, mostly the largest of its row, goes to the weight
+        // gradient apart, in fp32 (vh.coef): there the remainder cancels the rounded value.  64 columns at a time, packed before they are staged, so that a
         // store covers 128 contiguous bytes of a row.
         const bool in = row < p.M;
         const int t = in ? p.vh.tok[row] : -1;
@@ -435,16 +436,21 @@ __device__ __forceinline__ void epi_tile(const TcParams& p, uint32_t tmem_acc, i
               a0 = max_nan(a0, -1000.f);
               a1 = max_nan(a1, -1000.f);
               unsigned long long v2 = mul2(pack2(ex2(a0), ex2(a1)), fma2(B2, pack2(a0, a1), A2));
+              unsigned long long of2 = v2;                         // what the remainder is taken of
               if (target || dead) {
                 unpack2(v2, v0, v1);
-                if (t - col == 32 * h + e) v0 += gt;
-                if (t - col == 32 * h + e + 1) v1 += gt;
-                v2 = pack2(live ? v0 : 0.f, live ? v1 : 0.f);
+                const bool at0 = t - col == 32 * h + e, at1 = t - col == 32 * h + e + 1;
+                v0 = live ? (at0 ? v0 + gt : v0) : 0.f;
+                v1 = live ? (at1 ? v1 + gt : v1) : 0.f;
+                v2 = pack2(v0, v1);
+                const bool apart = p.vh.coef != nullptr;           // written for every row that has a token, 0 where it is not live
+                of2 = pack2(apart && at0 ? 0.f : v0, apart && at1 ? 0.f : v1);
+                if (apart && (at0 || at1)) p.vh.coef[row] = at0 ? v0 : v1;
               }
               unpack2(v2, v0, v1);
               const __nv_bfloat162 q = __floats2bfloat162_rn(v0, v1);
               const uint32_t w = *reinterpret_cast<const uint32_t*>(&q);
-              unpack2(fma2(pack2(__uint_as_float(w << 16), __uint_as_float(w & 0xFFFF0000u)), minus1, v2), v0, v1);   // exact
+              unpack2(fma2(pack2(__uint_as_float(w << 16), __uint_as_float(w & 0xFFFF0000u)), minus1, of2), v0, v1);  // exact
               const __nv_bfloat162 l = __floats2bfloat162_rn(v0, v1);
               r[0][16 * h + e / 2] = w;                            // behind what has been read
               lo[16 * h + e / 2] = *reinterpret_cast<const uint32_t*>(&l);

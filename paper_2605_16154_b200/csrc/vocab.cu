@@ -99,7 +99,7 @@ embed_kernel(const T* __restrict__ table, long long ld_table, int vocab, int d, 
 //   2. embed_sum_kernel: tiles of `rows` sorted pairs, each summed in order; a token that crosses more than one border
 //      between tiles leaves a partial sum per tile;
 //   3. embed_join_kernel: the partial sums of those tokens, in an order that depends on the token's tiles alone.
-// No floating-point atomics: the same inputs give the same bits.  Bound by HBM: dout once, grad once.  119808 rows of 1024
+// Every sum has a fixed order: the same inputs give the same bits.  Bound by HBM: dout once, grad once.  119808 rows of 1024
 // bf16 into 32000: 97 us against 58 us for the bytes; about 18 us are the four sort kernels, which are latency, 57 us the
 // sums (5.6 TB/s) and the rest the joins and the rows of absent tokens.
 // ------------------------------------------------------------------------------------------------
@@ -283,8 +283,8 @@ embed_scatter_kernel(const int* __restrict__ tok, const EmbedPlan pl, int pass, 
 // from two ballots.
 template <typename T, bool VEC>
 __global__ void __launch_bounds__(128)
-embed_sum_kernel(const T* __restrict__ dout, long long ld, const EmbedPlan pl, float scale, float* __restrict__ grad, int accumulate,
-                 int slabs) {
+embed_sum_kernel(const T* __restrict__ dout, long long ld, const float* __restrict__ coef, const EmbedPlan pl, float scale,
+                 float* __restrict__ grad, int accumulate, int slabs) {
   constexpr int N = VEC ? Vec16<T>::N : 1, NV = VEC ? 2 : 4, U = 8;
   wait_for_predecessor();
   let_successor_start();
@@ -317,17 +317,19 @@ embed_sum_kernel(const T* __restrict__ dout, long long ld, const EmbedPlan pl, f
   for (int j = 0; j < NV; ++j) col[j] = (slab * NV + j) * 32 * N + lane * N;
   unsigned cur = none;
   float acc[NV][N];
+  // Added by the memory, not read back: an element has one addition per call, so there is no order to depend on, and a
+  // warp does not wait for the row it adds to.
   auto put = [&](float* dst, const float (&a)[N], float f, bool add) {
     if constexpr (N >= 4) {
 #pragma unroll
       for (int e = 0; e < N; e += 4) {
-        float4 o = make_float4(a[e] * f, a[e + 1] * f, a[e + 2] * f, a[e + 3] * f);
-        float4* q = reinterpret_cast<float4*>(dst + e);
-        if (add) { const float4 w = *q; o.x += w.x; o.y += w.y; o.z += w.z; o.w += w.w; }
-        *q = o;
+        if (add) red_add_v4(dst + e, a[e] * f, a[e + 1] * f, a[e + 2] * f, a[e + 3] * f);
+        else *reinterpret_cast<float4*>(dst + e) = make_float4(a[e] * f, a[e + 1] * f, a[e + 2] * f, a[e + 3] * f);
       }
+    } else if (add) {
+      atomicAdd(dst, a[0] * f);
     } else {
-      dst[0] = add ? dst[0] + a[0] * f : a[0] * f;
+      dst[0] = a[0] * f;
     }
   };
   auto flush = [&]() {
@@ -360,6 +362,7 @@ embed_sum_kernel(const T* __restrict__ dout, long long ld, const EmbedPlan pl, f
   };
   auto run = [&](const uint2& kv, unsigned live, unsigned open) {
     const int rows = 32 - __clz(live), first = live ? __ffs(live) - 1 : 0;
+    const float weight = coef && ((live >> lane) & 1u) ? coef[kv.y] : 1.f;     // of this lane's row
     if constexpr (VEC) {
       // Every lane copies its own 16-byte pieces of a row into its own shared memory, EM_RING - 1 rows ahead of the sums:
       // bytes in flight without registers, and nobody to wait for but itself.
@@ -385,12 +388,13 @@ embed_sum_kernel(const T* __restrict__ dout, long long ld, const EmbedPlan pl, f
         asm volatile("cp.async.wait_group %0;" ::"n"(EM_RING - 1) : "memory");
         if (!((live >> i) & 1u)) continue;
         if ((open >> i) & 1u) begin(__shfl_sync(0xffffffffu, kv.x, i));
+        const float k = __shfl_sync(0xffffffffu, weight, i);
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
           float f[N];
           Vec16<T>::unpack(mine[((i & (EM_RING - 1)) * NV + j) * 32], f);
 #pragma unroll
-          for (int e = 0; e < N; ++e) acc[j][e] += f[e];
+          for (int e = 0; e < N; ++e) acc[j][e] += k * f[e];
         }
       }
       asm volatile("cp.async.wait_group 0;" ::: "memory");
@@ -410,8 +414,9 @@ embed_sum_kernel(const T* __restrict__ dout, long long ld, const EmbedPlan pl, f
         for (int u = 0; u < U; ++u) {
           if (!((live >> (i0 + u)) & 1u)) continue;
           if ((open >> (i0 + u)) & 1u) begin(__shfl_sync(0xffffffffu, kv.x, i0 + u));
+          const float k = __shfl_sync(0xffffffffu, weight, i0 + u);
 #pragma unroll
-          for (int j = 0; j < NV; ++j) acc[j][0] += one[u][j];
+          for (int j = 0; j < NV; ++j) acc[j][0] += k * one[u][j];
         }
       }
     }
@@ -1118,23 +1123,30 @@ static size_t embed_plan(EmbedPlan& pl, int n, int vocab, int d, void* ws) {
   return off;
 }
 
-template <typename T>
-static int launch_embed_bwd(const T* dout, long long ld, const int* tok, int n, int vocab, int d, float scale, int accumulate,
-                            float* grad, unsigned* status, void* ws, cudaStream_t s) {
+static int embed_passes(int vocab) {
+  int key_bits = 1;
+  while ((vocab >> key_bits) != 0) ++key_bits;                     // keys 0 .. vocab
+  return ceil_div(key_bits, 8);
+}
+static EmbedPlan embed_sorted_plan(int n, int vocab, int d, void* ws) {
   EmbedPlan pl;
   embed_plan(pl, n, vocab, d, ws);
+  pl.sorted = n <= ES_THREADS ? pl.buf[0] : pl.buf[(embed_passes(vocab) - 1) & 1];
+  return pl;
+}
+
+static int launch_embed_sort(const EmbedPlan& pl, const int* tok, unsigned* status, cudaStream_t s) {
+  const int n = pl.n, vocab = pl.vocab;
   if (n <= ES_THREADS) {
     int threads = 128;
     while (threads < n) threads *= 2;
     if (vocab < (1 << 22) - 1) embed_sort_small_kernel<unsigned, 10><<<1, threads, 0, s>>>(tok, pl, status);
     else embed_sort_small_kernel<unsigned long long, 32><<<1, threads, 0, s>>>(tok, pl, status);
     PCM_LAUNCH_CHECK();
-    pl.sorted = pl.buf[0];
   } else {
     int key_bits = 1;
-    while ((vocab >> key_bits) != 0) ++key_bits;                   // keys 0 .. vocab
-    const int passes = ceil_div(key_bits, 8), bits = ceil_div(key_bits, passes);
-    pl.sorted = pl.buf[(passes - 1) & 1];
+    while ((vocab >> key_bits) != 0) ++key_bits;
+    const int passes = embed_passes(vocab), bits = ceil_div(key_bits, passes);
     const dim3 grid(pl.blocks), block(ES_THREADS);
     for (int pass = 0; pass < passes; ++pass) {
       int rc = PCM_OK;
@@ -1148,18 +1160,36 @@ static int launch_embed_bwd(const T* dout, long long ld, const int* tok, int n, 
       if (rc != PCM_OK) return rc;
     }
   }
+  return PCM_OK;
+}
+
+template <typename T>
+static int launch_embed_sum(const EmbedPlan& pl, const T* dout, long long ld, const float* coef, float scale, int accumulate, float* grad,
+                            cudaStream_t s) {
+  const int vocab = pl.vocab, d = pl.d;
   const bool vec = !(((uintptr_t)dout | (uintptr_t)grad) & 15) && d % Vec16<T>::N == 0 && ld % Vec16<T>::N == 0;
   const int slabs = ceil_div(d, vec ? 64 * Vec16<T>::N : 128);
   const long long blocks = ((long long)ceil_div(pl.tiles, EM_LANES) * EM_LANES * slabs + 3) / 4;
   if (blocks > 0x7FFFFFFFll) return PCM_ERR_SHAPE;
   const int rc = launch_after_smem(vec ? embed_sum_kernel<T, true> : embed_sum_kernel<T, false>, dim3((unsigned)blocks), dim3(128),
-                                   vec ? 4 * EM_RING * 2 * 32 * 16 : 0, s, dout, ld, pl, scale, grad, accumulate, slabs);
+                                   vec ? 4 * EM_RING * 2 * 32 * 16 : 0, s, dout, ld, coef, pl, scale, grad, accumulate, slabs);
   if (rc != PCM_OK) return rc;
   const int join_slabs = ceil_div(d, 32), most = ceil_div(pl.tiles, EJ_WARPS);
   const int groups = pl.tiles <= 2 ? 0 : most < 16 ? most : 16;    // two tiles: nothing crosses two borders
   const int join_blocks = groups * join_slabs + (accumulate ? 0 : ceil_div(vocab, EJ_WARPS));
   if (join_blocks == 0) return PCM_OK;
   return launch_after(embed_join_kernel, dim3(join_blocks), dim3(EJ_WARPS * 32), s, pl, scale, grad, accumulate, groups, join_slabs);
+}
+
+size_t embed_accumulate_bytes(int n, int vocab, int d) {
+  EmbedPlan pl;
+  return embed_plan(pl, n, vocab, d, nullptr);
+}
+int embed_accumulate_sort(const int* tok, int n, int vocab, int d, void* scratch, cudaStream_t s) {
+  return launch_embed_sort(embed_sorted_plan(n, vocab, d, scratch), tok, nullptr, s);
+}
+int embed_accumulate_sum(const void* rows, const float* coef, int n, int vocab, int d, float* grad, void* scratch, cudaStream_t s) {
+  return launch_embed_sum(embed_sorted_plan(n, vocab, d, scratch), (const __nv_bfloat16*)rows, d, coef, 1.f, 1, grad, s);
 }
 
 template <typename T, int NT>
@@ -1259,9 +1289,11 @@ extern "C" int grpo_embed_bwd(int32_t dtype, const void* dout, int64_t ld_dout, 
   if (!dout || !tok || !elem_aligned(dout, dtype)) return PCM_ERR_ARG;
   if (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < grpo_embed_workspace_bytes(n, vocab, d)) return PCM_ERR_WORKSPACE;
   prof_begin(PC_EMBED, s);
-  const int rc = dtype == GRPO_BF16
-                     ? launch_embed_bwd((const __nv_bfloat16*)dout, ld_dout, tok, n, vocab, d, scale, accumulate, grad, device_status, workspace, s)
-                     : launch_embed_bwd((const float*)dout, ld_dout, tok, n, vocab, d, scale, accumulate, grad, device_status, workspace, s);
+  const EmbedPlan pl = embed_sorted_plan(n, vocab, d, workspace);
+  int rc = launch_embed_sort(pl, tok, device_status, s);
+  if (rc == PCM_OK)
+    rc = dtype == GRPO_BF16 ? launch_embed_sum(pl, (const __nv_bfloat16*)dout, ld_dout, nullptr, scale, accumulate, grad, s)
+                            : launch_embed_sum(pl, (const float*)dout, ld_dout, nullptr, scale, accumulate, grad, s);
   prof_end(s, 2.0 * n * d, (double)n * d * (dtype == GRPO_BF16 ? 2.0 : 4.0) + 4.0 * vocab * d);
   return rc;
 }

@@ -91,6 +91,7 @@ struct VocabHeadArgs {
   const float* dlogp = nullptr;
   const float* dent = nullptr;                // may be null
   void* dz_lo = nullptr;                      // bf16, laid out like C: what the bf16 rounding of C leaves
+  float* coef = nullptr;                      // [M] out, may be null: d z of the row's token; dz_lo is minus C there
   int vocab = 0;
 };
 

@@ -8,9 +8,12 @@
 // Both are bound by the tensor cores under the board's power limit.  21504 rows x 1024 x 32000: forward 0.99 - 1.1 ms
 // (1280 - 1425 TFLOP/s), backward 4.4 - 4.9 ms; 16 rows x 2048 x 32000 forward: 27 us, of which w (131 MB) takes 20.
 // Roundings to fewer bits: dx is formed from d z in bf16 (relative error 2.4e-3 of dx's norm, 1.7e-3 of which is the
-// rounding of the result itself).  dw is fp32, so its d z enters as hi + lo, two bf16 values, 16 significant bits: 2.6e-6 of
-// dw's norm, where fp32 products have 0.5e-6 (701 rows) to 2.5e-6 (21504 rows).  With hi alone it would be 1.6e-3; a
-// third value would cost a quarter more time for bits that the gradient of a bf16 weight has no use for.
+// rounding of the result itself).  dw is fp32, so its d z enters as hi + lo, two bf16 values, 16 significant bits, and the
+// target's d z, mostly the largest of its row, apart: coef x summed by token in fp32 (embed_accumulate_sum).  Relative to
+// dw's norm that leaves 0.8e-6 (701 rows x 1024 x 5003) and 0.35e-6 (8192 x 1024 x 32000), where fp32 products leave 0.5e-6
+// and 1.6e-6; hi + lo alone left 2.6e-6, hi alone would leave 1.6e-3.  The sums cost 60 us of the large batch, 19 us of
+// 86 of the small one.
+
 #include <cmath>
 
 #include "internal.h"
@@ -19,7 +22,7 @@ namespace pcm {
 
 constexpr int VH_GROUPS = 16;                 // column-block slices of a row joined side by side
 // k-blocks (of 64 rows) per accumulator piece of dw.  8192 rows x 1024 x 32000: error 2.55e-6 / 2.60e-6 / 2.81e-6 with 4 / 8 /
-// 16, time the same within the clock's wandering; without pieces the drift grows with the rows (4e-5 at 119808).
+// 16 (before the targets went apart), time the same within the clock's wandering; without pieces the drift grows with the rows (4e-5 at 119808).
 constexpr int VH_CHAIN_KB = 8;
 
 struct JoinParams {
@@ -95,8 +98,10 @@ vocab_stats_join_row_kernel(const JoinParams p) {
 // holds (NaN, inf) need not be.
 __global__ void __launch_bounds__(256)
 live_rows_kernel(const uint4* __restrict__ x, long long ld8, int M, int d8, const int* __restrict__ tok, int V, uint4* __restrict__ out,
-                 unsigned* status) {
-  wait_for_predecessor();                     // the rows of the chunk before may still be read
+                 unsigned* status, int beside) {
+  // `beside`: launched behind the sort of the chunk's tokens, which began when all before it had ended, so that the rows
+  // can be copied while it runs; this kernel ends when both are done.  Otherwise the chunk before may still be read.
+  if (!beside) wait_for_predecessor();
   let_successor_start();
   const long long total = (long long)M * d8;
   for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < total; i += (long long)gridDim.x * 256) {
@@ -106,6 +111,7 @@ live_rows_kernel(const uint4* __restrict__ x, long long ld8, int M, int d8, cons
     if (t >= V && c == 0 && status) atomicOr(status, STATUS_BAD_TOKEN);
     out[i] = live ? x[row * ld8 + c] : make_uint4(0, 0, 0, 0);
   }
+  if (beside) wait_for_predecessor();
 }
 
 // Parts of a split contraction added in order, four columns a thread.
@@ -159,7 +165,7 @@ static int gemm_class(long long M, long long N) { return M > 128 && N > 128 ? PC
 
 static size_t round256(size_t v) { return (v + 255) / 256 * 256; }
 
-struct HeadBwdPlan { size_t x, hi, lo, parts, total; long long ldz; int rows; };
+struct HeadBwdPlan { size_t x, hi, lo, parts, coef, sort, total; long long ldz; int rows; };
 static HeadBwdPlan head_bwd_plan(int M, int d, int V, int chunk_rows) {
   HeadBwdPlan pl;
   pl.rows = chunk_rows < M ? chunk_rows : M;
@@ -168,7 +174,9 @@ static HeadBwdPlan head_bwd_plan(int M, int d, int V, int chunk_rows) {
   pl.hi = round256((size_t)pl.rows * d * 2);
   pl.lo = pl.hi + round256((size_t)pl.rows * pl.ldz * 2);
   pl.parts = pl.lo + round256((size_t)pl.rows * pl.ldz * 2);
-  pl.total = pl.parts + chain_part_bytes();
+  pl.coef = pl.parts + round256(chain_part_bytes());
+  pl.sort = pl.coef + round256((size_t)pl.rows * sizeof(float));
+  pl.total = pl.sort + (pl.rows > 0 ? embed_accumulate_bytes(pl.rows, V, d) : 0);
   return pl;
 }
 
@@ -245,17 +253,24 @@ extern "C" int grpo_head_logp_bwd(const void* x, int64_t ld_x, int32_t n_rows, i
   unsigned char* base = (unsigned char*)workspace;
   uint4* x_live = (uint4*)(base + pl.x);
   void *hi = base + pl.hi, *lo = base + pl.lo;
-  float* parts = (float*)(base + pl.parts);
+  float *parts = (float*)(base + pl.parts), *coef = (float*)(base + pl.coef);
   const float inv_t = 1.f / temperature;
   for (int r0 = 0; r0 < n_rows; r0 += pl.rows) {
     const int rows = n_rows - r0 < pl.rows ? n_rows - r0 : pl.rows;
     const unsigned short* xr = (const unsigned short*)x + (long long)r0 * ld_x;
     const double flops = 2.0 * rows * vocab * d;
+    int rc = PCM_OK;
+    if (dw) {
+      prof_begin(PC_EMBED, s);
+      rc = embed_accumulate_sort(tok + r0, rows, vocab, d, base + pl.sort, s);
+      prof_end(s, 0.0, 4.0 * rows);
+      if (rc != PCM_OK) return rc;
+    }
     prof_begin(PC_ELEM, s);
     const int d8 = d / 8;
     const int blocks = ceil_div((long long)rows * d8, 1024);
-    int rc = launch_after(live_rows_kernel, dim3(blocks), dim3(256), s, (const uint4*)xr, ld_x / 8, rows, d8, tok + r0, vocab, x_live,
-                          device_status);
+    rc = launch_after(live_rows_kernel, dim3(blocks), dim3(256), s, (const uint4*)xr, ld_x / 8, rows, d8, tok + r0, vocab, x_live,
+                      device_status, dw ? 1 : 0);
     prof_end(s, 0.0, 4.0 * rows * d);
     if (rc != PCM_OK) return rc;
 
@@ -263,6 +278,7 @@ extern "C" int grpo_head_logp_bwd(const void* x, int64_t ld_x, int32_t n_rows, i
     z.epi.kind = EPI_VOCAB_DZ;
     VocabHeadArgs& v = z.epi.vh;
     v.tok = tok + r0; v.inv_t = inv_t; v.lse = lse + r0; v.dlogp = dlogp + r0; v.vocab = vocab; v.dz_lo = lo;
+    v.coef = dw ? coef : nullptr;
     v.dent = dentropy ? dentropy + r0 : nullptr;
     v.entropy = dentropy ? entropy + r0 : nullptr;
     prof_begin(gemm_class(rows, 256), s);
@@ -286,6 +302,10 @@ extern "C" int grpo_head_logp_bwd(const void* x, int64_t ld_x, int32_t n_rows, i
       prof_begin(gemm_class(vocab, d), s);
       rc = chain_gemm(q, parts, s);
       prof_end(s, 2.0 * flops, 4.0 * rows * vocab + 4.0 * rows * d + 4.0 * vocab * d);
+      if (rc != PCM_OK) return rc;
+      prof_begin(PC_EMBED, s);
+      rc = embed_accumulate_sum(x_live, coef, rows, vocab, d, dw, base + pl.sort, s);
+      prof_end(s, 2.0 * rows * d, 2.0 * rows * d);
       if (rc != PCM_OK) return rc;
     }
   }

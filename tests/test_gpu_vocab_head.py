@@ -110,7 +110,10 @@ def check_grads(x, w, tok, lse, entropy, dlogp, dent, temperature, dx, dw, dw0=N
         want = dz.T @ xf
         mass = np.abs(dz).T @ np.abs(xf)
         pieces = x.shape[0] / 256 + 4
-        tol = edz.T @ np.abs(xf) + (2.0 ** -16 + 34 * 2.0 ** -23 + 2 * pieces * U) * mass
+        # the targets' part, summed by token in fp32: k additions of at most k rows, one product each
+        tgt = np.where(live & (np.arange(vocab)[None] == t[:, None]), np.abs(dz), 0.0)
+        most = np.bincount(t[live[:, 0]], minlength=vocab).max() if live.any() else 0
+        tol = edz.T @ np.abs(xf) + (2.0 ** -16 + 34 * 2.0 ** -23 + 2 * pieces * U) * mass + (most + 4) * U * (tgt.T @ np.abs(xf))
         if dw0 is not None:
             want = want + host(dw0)
             tol = tol + 4 * U * np.abs(host(dw0))
@@ -176,6 +179,37 @@ def test_refusals_of_the_binding():
     for f in bad:
         with pytest.raises(b.PcmError):
             f()
+
+
+def test_weight_gradient_is_as_exact_as_fp32_products():
+    """Spread-out rows: a row's d z is its target's for the most part, which fp32 sums carry; the rest is cut to 16 bits."""
+    b = B()
+    x, w, tok, dlogp, dent = problem(700, 512, 4001, seed=6)
+    dlogp[2] = dent[2] = 0.0
+    _, entropy, lse = b.grpo_head_logp(x, w, tok)
+    _, dw = b.grpo_head_logp_bwd(x, w, tok, lse, entropy, dlogp, dent * 1e-2, want_dx=False)
+    xf, wf = finite(x, tok, 4001), host(w)
+    _, want = vo.head_logp_bwd(xf, wf, tok.cpu().numpy(), host(dlogp), host(dent) * 1e-2)
+    dz = vo.token_logp_bwd(xf @ wf.T, tok.cpu().numpy(), host(dlogp), host(dent) * 1e-2)
+    rest = dz.copy()
+    rest[np.arange(700), np.clip(tok.cpu().numpy(), 0, 4000)] = 0.0
+    share = np.linalg.norm(rest) / np.linalg.norm(dz)
+    # remainder 2^-16 at most of the rest; p from fp32 exponents (2^-20); 34 truncations a piece and fp32 sums of the targets
+    bound = share * (2.0 ** -16 + 2.0 ** -19) + 34 * 2.0 ** -23 * 0.5
+    assert np.linalg.norm(host(dw) - want) <= bound * np.linalg.norm(want)
+
+
+def test_a_row_without_a_finite_logit_has_no_gradient():
+    """lse = -inf, as a caller may hand in, with a valid token: nothing of the row reaches either gradient."""
+    b = B()
+    x, w, tok, dlogp, dent = problem(6, 64, 300)
+    _, entropy, lse = b.grpo_head_logp(x, w, tok)
+    lse[3] = float("-inf")
+    dx, dw = b.grpo_head_logp_bwd(x, w, tok, lse, entropy, dlogp, dent)
+    keep = torch.arange(6, device="cuda") != 3
+    dx2, dw2 = b.grpo_head_logp_bwd(x[keep], w, tok[keep], lse[keep], entropy[keep], dlogp[keep], dent[keep])
+    assert not dx[3].any() and torch.equal(dx[keep], dx2)
+    assert torch.allclose(dw, dw2, rtol=1e-5, atol=1e-6)
 
 
 def test_wide_hidden_states_keep_their_accuracy():

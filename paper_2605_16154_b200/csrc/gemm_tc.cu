@@ -414,8 +414,10 @@ __device__ __forceinline__ void epi_tile(const TcParams& p, uint32_t tmem_acc, i
         const bool live = t >= 0 && t < p.vh.vocab && lse != -INFINITY;
         const float H = live && p.vh.dent ? p.vh.entropy[row] : 0.f;
         const float gt = live ? p.vh.dlogp[row] * p.vh.inv_t : 0.f, ht = live && p.vh.dent ? p.vh.dent[row] * p.vh.inv_t : 0.f;
-        const float c = p.vh.inv_t * VOCAB_LOG2E, lse2 = lse * VOCAB_LOG2E, A = -(gt + ht * H), Bc = -ht * VOCAB_LN2;
-        const bool dead = __any_sync(0xffffffffu, !live);
+        // A row without gradient has all factors 0, whatever its z (a NaN exponent reads as -1000); a row with a NaN or +inf
+        // among its logits, whose lse is NaN, becomes NaN through A.
+        const float c = live ? p.vh.inv_t * VOCAB_LOG2E : 0.f, lse2 = live ? lse * VOCAB_LOG2E : 0.f;
+        const float A = lse == lse || !live ? -(gt + ht * H) : lse, Bc = -ht * VOCAB_LN2;
         const unsigned long long c2 = pack2(c, c), neg_lse2 = pack2(-lse2, -lse2), A2 = pack2(A, A), B2 = pack2(Bc, Bc), minus1 = pack2(-1.f, -1.f);
 #pragma unroll 1
         for (int c0 = chalf * (BN / 2); c0 < (chalf + 1) * (BN / 2); c0 += 64) {
@@ -433,15 +435,15 @@ __device__ __forceinline__ void epi_tile(const TcParams& p, uint32_t tmem_acc, i
             for (int e = 0; e < 32; e += 2) {
               float a0, a1, v0, v1;
               unpack2(fma2(pack2(__uint_as_float(r[h][e]), __uint_as_float(r[h][e + 1])), c2, neg_lse2), a0, a1);
-              a0 = max_nan(a0, -1000.f);
-              a1 = max_nan(a1, -1000.f);
+              a0 = fmaxf(a0, -1000.f);
+              a1 = fmaxf(a1, -1000.f);
               unsigned long long v2 = mul2(pack2(ex2(a0), ex2(a1)), fma2(B2, pack2(a0, a1), A2));
               unsigned long long of2 = v2;                         // what the remainder is taken of
-              if (target || dead) {
+              if (target) {
                 unpack2(v2, v0, v1);
                 const bool at0 = t - col == 32 * h + e, at1 = t - col == 32 * h + e + 1;
-                v0 = live ? (at0 ? v0 + gt : v0) : 0.f;
-                v1 = live ? (at1 ? v1 + gt : v1) : 0.f;
+                v0 = at0 ? v0 + gt : v0;
+                v1 = at1 ? v1 + gt : v1;
                 v2 = pack2(v0, v1);
                 const bool apart = p.vh.coef != nullptr;           // written for every row that has a token, 0 where it is not live
                 of2 = pack2(apart && at0 ? 0.f : v0, apart && at1 ? 0.f : v1);

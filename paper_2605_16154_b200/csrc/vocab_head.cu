@@ -94,11 +94,11 @@ vocab_stats_join_row_kernel(const JoinParams p) {
   finish_row(p, st, blockIdx.x);
 }
 
-// The hidden states with zeros in the rows that have no token: their d z is zero, but zero times whatever a padded row
-// holds (NaN, inf) need not be.
+// The hidden states with zeros in the rows that have no token (or no finite logit, lse = -inf): their d z is zero, but zero
+// times whatever such a row holds (NaN, inf) need not be.
 __global__ void __launch_bounds__(256)
-live_rows_kernel(const uint4* __restrict__ x, long long ld8, int M, int d8, const int* __restrict__ tok, int V, uint4* __restrict__ out,
-                 unsigned* status, int beside) {
+live_rows_kernel(const uint4* __restrict__ x, long long ld8, int M, int d8, const int* __restrict__ tok,
+                 const float* __restrict__ lse, int V, uint4* __restrict__ out, unsigned* status, int beside) {
   // `beside`: launched behind the sort of the chunk's tokens, which began when all before it had ended, so that the rows
   // can be copied while it runs; this kernel ends when both are done.  Otherwise the chunk before may still be read.
   if (!beside) wait_for_predecessor();
@@ -107,7 +107,7 @@ live_rows_kernel(const uint4* __restrict__ x, long long ld8, int M, int d8, cons
   for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < total; i += (long long)gridDim.x * 256) {
     const long long row = i / d8;
     const int c = (int)(i - row * d8), t = tok[row];
-    const bool live = t >= 0 && t < V;
+    const bool live = t >= 0 && t < V && lse[row] != -INFINITY;
     if (t >= V && c == 0 && status) atomicOr(status, STATUS_BAD_TOKEN);
     out[i] = live ? x[row * ld8 + c] : make_uint4(0, 0, 0, 0);
   }
@@ -269,8 +269,8 @@ extern "C" int grpo_head_logp_bwd(const void* x, int64_t ld_x, int32_t n_rows, i
     prof_begin(PC_ELEM, s);
     const int d8 = d / 8;
     const int blocks = ceil_div((long long)rows * d8, 1024);
-    rc = launch_after(live_rows_kernel, dim3(blocks), dim3(256), s, (const uint4*)xr, ld_x / 8, rows, d8, tok + r0, vocab, x_live,
-                      device_status, dw ? 1 : 0);
+    rc = launch_after(live_rows_kernel, dim3(blocks), dim3(256), s, (const uint4*)xr, ld_x / 8, rows, d8, tok + r0, lse + r0, vocab,
+                      x_live, device_status, dw ? 1 : 0);
     prof_end(s, 0.0, 4.0 * rows * d);
     if (rc != PCM_OK) return rc;
 

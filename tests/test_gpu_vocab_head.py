@@ -199,17 +199,31 @@ def test_weight_gradient_is_as_exact_as_fp32_products():
     assert np.linalg.norm(host(dw) - want) <= bound * np.linalg.norm(want)
 
 
+def test_a_nan_in_a_live_row_reaches_its_gradient_and_no_other():
+    b = B()
+    x, w, tok, dlogp, dent = problem(5, 64, 300)
+    x[2, 7] = float("nan")
+    logp, entropy, lse = b.grpo_head_logp(x, w, tok)
+    keep = torch.arange(5, device="cuda") != 2
+    assert bool(torch.isnan(logp[2]) & torch.isnan(lse[2]) & torch.isnan(entropy[2])) and bool(torch.isfinite(logp[keep]).all())
+    for de in (dent, None):
+        dx, dw = b.grpo_head_logp_bwd(x, w, tok, lse, entropy, dlogp, de)
+        assert bool(torch.isnan(dx[2]).all()) and bool(torch.isfinite(dx[keep]).all())
+        assert bool(torch.isnan(dw).any())
+
+
 def test_a_row_without_a_finite_logit_has_no_gradient():
     """lse = -inf, as a caller may hand in, with a valid token: nothing of the row reaches either gradient."""
     b = B()
     x, w, tok, dlogp, dent = problem(6, 64, 300)
     _, entropy, lse = b.grpo_head_logp(x, w, tok)
     lse[3] = float("-inf")
+    x[3, 5] = float("inf")                                       # what its logits are made of does not matter
     dx, dw = b.grpo_head_logp_bwd(x, w, tok, lse, entropy, dlogp, dent)
     keep = torch.arange(6, device="cuda") != 3
     dx2, dw2 = b.grpo_head_logp_bwd(x[keep], w, tok[keep], lse[keep], entropy[keep], dlogp[keep], dent[keep])
     assert not dx[3].any() and torch.equal(dx[keep], dx2)
-    assert torch.allclose(dw, dw2, rtol=1e-5, atol=1e-6)
+    assert torch.allclose(dw, dw2, rtol=1e-5, atol=1e-6)         # 0 x inf nowhere
 
 
 def test_wide_hidden_states_keep_their_accuracy():

@@ -380,6 +380,7 @@ embed_sum_kernel(const T* __restrict__ dout, long long ld, const float* __restri
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
       };
+      __syncwarp();
 #pragma unroll
       for (int i = 0; i < EM_RING - 1; ++i) issue(first + i);
       for (int i = first; i < rows; ++i) {

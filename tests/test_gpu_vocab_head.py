@@ -358,3 +358,33 @@ def test_calls_on_two_streams_at_once():
         torch.cuda.synchronize()
         for p, q in zip(got, want):
             assert all(torch.equal(u, v) for u, v in zip(p, q))
+
+
+def test_calls_back_to_back_in_one_workspace():
+    """Inputs written on the device right before each call, one workspace for all calls, nothing waited for in between: the
+    kernels of a call overlap their launches, so each has to wait for what it reads and for what it overwrites."""
+    b = B()
+    n, d, vocab = 1500, 128, 2011
+    problems = [problem(n, d, vocab, seed=k) for k in (30, 31, 32)]
+    need = max(b.grpo_head_logp_bwd_workspace_bytes(n, d, vocab, 700), b.grpo_embed_workspace_bytes(n, vocab, d),
+               b.grpo_head_logp_workspace_bytes(n, d, vocab)) + 256
+    ws = torch.empty(need, dtype=torch.uint8, device="cuda")
+    x, w, tok, dlogp, dent = (torch.empty_like(t) for t in problems[0])
+
+    def step(p, ws):
+        for dst, src in zip((x, w, tok, dlogp, dent), p):
+            dst.copy_(src)
+        logp, ent, lse = b.grpo_head_logp(x, w, tok, workspace=ws)
+        dx, dw = b.grpo_head_logp_bwd(x, w, tok, lse, ent, dlogp, dent, chunk_rows=700, workspace=ws)
+        grad = b.grpo_embed_bwd(dx, tok, vocab, workspace=ws)
+        _, only = b.grpo_head_logp_bwd(x, w, tok, lse, ent, dlogp, dent, chunk_rows=700, workspace=ws, want_dx=False)
+        dx2, _ = b.grpo_head_logp_bwd(x, w, tok, lse, ent, dlogp, dent, chunk_rows=400, workspace=ws, want_dw=False)
+        return logp, ent, lse, dx, dw, grad, only, dx2
+    want = []
+    for p in problems:
+        want.append([t.clone() for t in step(p, None)])
+        torch.cuda.synchronize()
+    got = [step(problems[i % 3], ws) for i in range(24)]
+    torch.cuda.synchronize()
+    for i, g in enumerate(got):
+        assert all(torch.equal(u, v) for u, v in zip(g, want[i % 3])), i

@@ -430,7 +430,7 @@ int grpo_head_logp(const void* x, int64_t ld_x, int32_t n_rows, int32_t d, const
                    void* workspace, size_t workspace_bytes, pcm_stream stream);
 
 /* Its gradients, with dlogits as in grpo_token_logp_bwd (formed in fp32 from a second x w_h^T):
- *     dx = dlogits w_h  (bf16 [n_rows][d], row stride ld_dx, from dlogits rounded to bf16)
+ *     dx = dlogits w_h  (bf16 [n_rows][d], row stride ld_dx; dlogits rounded to bf16, the targets' entries not)
  *     dw = dlogits^T x  (fp32 [vocab][d], contiguous, 16-byte aligned; GRPO_ACCUMULATE in flags adds to it), from dlogits
  *                       as a sum of two bf16 values, the targets' own in fp32
  * Either may be NULL.  x may hold anything, NaN too, in rows without a token.  The rows are processed chunk_rows (>= 1) at

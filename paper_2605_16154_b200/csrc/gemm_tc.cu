@@ -447,7 +447,11 @@ __device__ __forceinline__ void epi_tile(const TcParams& p, uint32_t tmem_acc, i
                 v2 = pack2(v0, v1);
                 const bool apart = p.vh.coef != nullptr;           // written for every row that has a token, 0 where it is not live
                 of2 = pack2(apart && at0 ? 0.f : v0, apart && at1 ? 0.f : v1);
-                if (apart && (at0 || at1)) p.vh.coef[row] = at0 ? v0 : v1;
+                if (at0 || at1) {
+                  const float v = at0 ? v0 : v1;
+                  if (apart) p.vh.coef[row] = v;
+                  if (p.vh.corr) p.vh.corr[row] = v - __bfloat162float(__float2bfloat16_rn(v));
+                }
               }
               unpack2(v2, v0, v1);
               const __nv_bfloat162 q = __floats2bfloat162_rn(v0, v1);
@@ -684,6 +688,16 @@ template <int BN>
 __device__ __forceinline__ void chain_store(const TcParams& p, int row, int n0, int chalf, int split, float* stage,
                                             const float (&sum)[BN / 2]) {
   const int lane = threadIdx.x & 31, row_base = row - lane;
+  // dx: the targets' rows of w, weighted with what d z's rounding left of the targets' entries
+  const __nv_bfloat16* w_row[4] = {nullptr, nullptr, nullptr, nullptr};
+  float corr[4];
+  if (p.vh.corr && p.c_dtype == DT_BF16) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int gr = row_base + i * 8 + (lane >> 2), t = gr < p.M ? p.vh.tok[gr] : -1;
+      if (t >= 0 && t < p.vh.vocab) { w_row[i] = p.vh.w + (long long)t * p.vh.ld_w; corr[i] = p.vh.corr[gr]; }
+    }
+  }
 #pragma unroll
   for (int c0 = 0; c0 < BN / 2; c0 += 32) {
     const int col = n0 + chalf * (BN / 2) + c0;
@@ -714,7 +728,15 @@ __device__ __forceinline__ void chain_store(const TcParams& p, int row, int n0, 
         float v[8];
         stage_get8(stage, lane, i, v);
         const int gr = row_base + i * 8 + (lane >> 2);
-        if (gr < p.M && cc < p.N) *reinterpret_cast<uint4*>(C + (long long)gr * p.ldc + cc) = pack8_bf16(v);
+        if (gr < p.M && cc < p.N) {
+          if (w_row[i]) {
+            float w[8];
+            unpack8_bf16(__ldg(reinterpret_cast<const uint4*>(w_row[i] + cc)), w);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] += corr[i] * w[e];
+          }
+          *reinterpret_cast<uint4*>(C + (long long)gr * p.ldc + cc) = pack8_bf16(v);
+        }
       }
     }
     __syncwarp();
@@ -1489,6 +1511,7 @@ bool gemm_epilogue_supported(const GemmArgs& g) {
     if (g.epi.kind == EPI_VOCAB_DZ)
       return g.a_kmajor && g.b_kmajor && g.C && g.c_dtype == DT_BF16 && g.ldc % 32 == 0 && g.ldc >= g.N && g.epi.vh.dz_lo &&
              !((uintptr_t)g.epi.vh.dz_lo & 15) && g.epi.vh.tok && g.epi.vh.lse && g.epi.vh.dlogp && !g.K2;
+    if (g.epi.vh.corr && (!g.epi.vh.tok || !g.epi.vh.w || g.epi.vh.ld_w % 8 || ((uintptr_t)g.epi.vh.w & 15))) return false;
     return g.C && g.N % 8 == 0 && g.ldc % 8 == 0 && g.epi.splits >= 1 && (g.epi.splits == 1 || (g.c_dtype == DT_F32 && !g.epi.accumulate)) &&
            (!g.epi.accumulate || g.c_dtype == DT_F32) && !g.R && g.alpha == 1.f &&
            (!g.K2 || (g.K2 > 0 && g.A2 && g.B2 && !(g.lda2 % 8) && !(g.ldb2 % 8) && !(((uintptr_t)g.A2 | (uintptr_t)g.B2) & 15)));

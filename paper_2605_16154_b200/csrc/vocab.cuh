@@ -1,6 +1,7 @@
 // Softmax statistics over a vocabulary that is seen in parts (threads, cluster ranks, accumulator tiles), shared by the
 // kernels that read logits and by the GEMM epilogues that never store them.
 #pragma once
+#include <cuda_bf16.h>
 #include <math.h>
 #include <stdint.h>
 
@@ -92,6 +93,9 @@ struct VocabHeadArgs {
   const float* dent = nullptr;                // may be null
   void* dz_lo = nullptr;                      // bf16, laid out like C: what the bf16 rounding of C leaves
   float* coef = nullptr;                      // [M] out, may be null: d z of the row's token; dz_lo is minus C there
+  float* corr = nullptr;                      // [M] what the bf16 rounding of C leaves of the token's d z: out of EPI_VOCAB_DZ (may
+                                              // be null), into the EPI_CHAIN product with w, which adds corr w[tok] to its rows
+  const __nv_bfloat16* w = nullptr; long long ld_w = 0;
   int vocab = 0;
 };
 

@@ -7,8 +7,9 @@
 //             chunk of rows; then dx = dz w and dw (+)= dz^T x.
 // Both are bound by the tensor cores under the board's power limit.  21504 rows x 1024 x 32000: forward 0.99 - 1.1 ms
 // (1280 - 1425 TFLOP/s), backward 4.4 - 4.9 ms; 16 rows x 2048 x 32000 forward: 27 us, of which w (131 MB) takes 20.
-// Roundings to fewer bits: dx is formed from d z in bf16 (relative error 2.4e-3 of dx's norm, 1.7e-3 of which is the
-// rounding of the result itself).  dw is fp32, so its d z enters as hi + lo, two bf16 values, 16 significant bits, and the
+// Roundings to fewer bits: d z enters dx in bf16, its largest entry, the target's, corrected by what that leaves (corr w[tok],
+// added before dx is rounded): error 1.66e-3 of dx's norm, the rounding of the result itself, where it was 2.4e-3 without.
+// dw is fp32, so its d z enters as hi + lo, two bf16 values, 16 significant bits, and the
 // target's d z, mostly the largest of its row, apart: coef x summed by token in fp32 (embed_accumulate_sum).  Relative to
 // dw's norm that leaves 0.8e-6 (701 rows x 1024 x 5003) and 0.35e-6 (8192 x 1024 x 32000), where fp32 products leave 0.5e-6
 // and 1.6e-6; hi + lo alone left 2.6e-6, hi alone would leave 1.6e-3.  The sums cost 60 us of the large batch, 19 us of
@@ -118,7 +119,7 @@ live_rows_kernel(const uint4* __restrict__ x, long long ld8, int M, int d8, cons
 template <bool BF16>
 __global__ void __launch_bounds__(256)
 parts_sum_kernel(const float* __restrict__ part, long long stride, int splits, long long M, int N, void* __restrict__ C, long long ldc,
-                 int accumulate) {
+                 int accumulate, const VocabHeadArgs vh) {
   wait_for_predecessor();
   let_successor_start();
   const int n4 = N / 4;
@@ -133,6 +134,13 @@ parts_sum_kernel(const float* __restrict__ part, long long stride, int splits, l
       a.x += w.x; a.y += w.y; a.z += w.z; a.w += w.w;
     }
     if constexpr (BF16) {
+      const int t = vh.corr ? vh.tok[row] : -1;                     // as in the product's own epilogue
+      if (t >= 0 && t < vh.vocab) {
+        const uint2 q = __ldg(reinterpret_cast<const uint2*>(vh.w + (long long)t * vh.ld_w + col));
+        const float k = vh.corr[row];
+        a.x += k * __uint_as_float(q.x << 16); a.y += k * __uint_as_float(q.x & 0xFFFF0000u);
+        a.z += k * __uint_as_float(q.y << 16); a.w += k * __uint_as_float(q.y & 0xFFFF0000u);
+      }
       const __nv_bfloat162 lo = __floats2bfloat162_rn(a.x, a.y), hi = __floats2bfloat162_rn(a.z, a.w);
       uint2 o;
       o.x = *reinterpret_cast<const uint32_t*>(&lo); o.y = *reinterpret_cast<const uint32_t*>(&hi);
@@ -152,12 +160,13 @@ static int chain_gemm(GemmArgs g, float* parts, cudaStream_t s) {
   GemmArgs q = g;
   q.C = parts; q.ldc = g.N; q.c_dtype = DT_F32;
   q.epi.splits = splits; q.epi.accumulate = 0; q.epi.part_stride = (long long)g.M * g.N;
+  q.epi.vh.corr = nullptr;                     // the summing kernel adds it
   const int rc = gemm_tcgen05(q, s);
   if (rc != PCM_OK) return rc;
   const long long total = (long long)g.M * (g.N / 4);
   const int grid = (int)(ceil_div(total, 256) < 8 * sm_count() ? ceil_div(total, 256) : 8 * sm_count());
   return launch_after(g.c_dtype == DT_BF16 ? parts_sum_kernel<true> : parts_sum_kernel<false>, dim3(grid), dim3(256), s, parts,
-                      q.epi.part_stride, splits, g.M, g.N, g.C, g.ldc, g.epi.accumulate);
+                      q.epi.part_stride, splits, g.M, g.N, g.C, g.ldc, g.epi.accumulate, g.epi.vh);
 }
 
 // Profile class of a product: on CTA pairs or not (the choice that gemm_tcgen05 makes).
@@ -165,7 +174,7 @@ static int gemm_class(long long M, long long N) { return M > 128 && N > 128 ? PC
 
 static size_t round256(size_t v) { return (v + 255) / 256 * 256; }
 
-struct HeadBwdPlan { size_t x, hi, lo, parts, coef, sort, total; long long ldz; int rows; };
+struct HeadBwdPlan { size_t x, hi, lo, parts, coef, corr, sort, total; long long ldz; int rows; };
 static HeadBwdPlan head_bwd_plan(int M, int d, int V, int chunk_rows) {
   HeadBwdPlan pl;
   pl.rows = chunk_rows < M ? chunk_rows : M;
@@ -175,7 +184,8 @@ static HeadBwdPlan head_bwd_plan(int M, int d, int V, int chunk_rows) {
   pl.lo = pl.hi + round256((size_t)pl.rows * pl.ldz * 2);
   pl.parts = pl.lo + round256((size_t)pl.rows * pl.ldz * 2);
   pl.coef = pl.parts + round256(chain_part_bytes());
-  pl.sort = pl.coef + round256((size_t)pl.rows * sizeof(float));
+  pl.corr = pl.coef + round256((size_t)pl.rows * sizeof(float));
+  pl.sort = pl.corr + round256((size_t)pl.rows * sizeof(float));
   pl.total = pl.sort + (pl.rows > 0 ? embed_accumulate_bytes(pl.rows, V, d) : 0);
   return pl;
 }
@@ -253,7 +263,7 @@ extern "C" int grpo_head_logp_bwd(const void* x, int64_t ld_x, int32_t n_rows, i
   unsigned char* base = (unsigned char*)workspace;
   uint4* x_live = (uint4*)(base + pl.x);
   void *hi = base + pl.hi, *lo = base + pl.lo;
-  float *parts = (float*)(base + pl.parts), *coef = (float*)(base + pl.coef);
+  float *parts = (float*)(base + pl.parts), *coef = (float*)(base + pl.coef), *corr = (float*)(base + pl.corr);
   const float inv_t = 1.f / temperature;
   for (int r0 = 0; r0 < n_rows; r0 += pl.rows) {
     const int rows = n_rows - r0 < pl.rows ? n_rows - r0 : pl.rows;
@@ -279,6 +289,7 @@ extern "C" int grpo_head_logp_bwd(const void* x, int64_t ld_x, int32_t n_rows, i
     VocabHeadArgs& v = z.epi.vh;
     v.tok = tok + r0; v.inv_t = inv_t; v.lse = lse + r0; v.dlogp = dlogp + r0; v.vocab = vocab; v.dz_lo = lo;
     v.coef = dw ? coef : nullptr;
+    v.corr = dx ? corr : nullptr;
     v.dent = dentropy ? dentropy + r0 : nullptr;
     v.entropy = dentropy ? entropy + r0 : nullptr;
     prof_begin(gemm_class(rows, 256), s);
@@ -288,6 +299,8 @@ extern "C" int grpo_head_logp_bwd(const void* x, int64_t ld_x, int32_t n_rows, i
     if (dx) {
       GemmArgs q{rows, d, vocab, hi, pl.ldz, true, w_h, ld_w, false, DT_BF16, (unsigned short*)dx + (long long)r0 * ld_dx, ld_dx, DT_BF16, nullptr, 0};
       q.epi.kind = EPI_CHAIN;                  // bf16 result: one accumulator piece
+      q.epi.vh.tok = tok + r0; q.epi.vh.vocab = vocab; q.epi.vh.corr = corr;
+      q.epi.vh.w = (const __nv_bfloat16*)w_h; q.epi.vh.ld_w = ld_w;
       prof_begin(gemm_class(rows, d), s);
       rc = chain_gemm(q, parts, s);
       prof_end(s, flops, 2.0 * rows * vocab + 2.0 * vocab * d + 2.0 * rows * d);

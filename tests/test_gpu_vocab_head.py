@@ -187,9 +187,9 @@ def test_weight_gradient_is_as_exact_as_fp32_products():
     x, w, tok, dlogp, dent = problem(700, 512, 4001, seed=6)
     dlogp[2] = dent[2] = 0.0
     _, entropy, lse = b.grpo_head_logp(x, w, tok)
-    _, dw = b.grpo_head_logp_bwd(x, w, tok, lse, entropy, dlogp, dent * 1e-2, want_dx=False)
+    dx, dw = b.grpo_head_logp_bwd(x, w, tok, lse, entropy, dlogp, dent * 1e-2)
     xf, wf = finite(x, tok, 4001), host(w)
-    _, want = vo.head_logp_bwd(xf, wf, tok.cpu().numpy(), host(dlogp), host(dent) * 1e-2)
+    want_dx, want = vo.head_logp_bwd(xf, wf, tok.cpu().numpy(), host(dlogp), host(dent) * 1e-2)
     dz = vo.token_logp_bwd(xf @ wf.T, tok.cpu().numpy(), host(dlogp), host(dent) * 1e-2)
     rest = dz.copy()
     rest[np.arange(700), np.clip(tok.cpu().numpy(), 0, 4000)] = 0.0
@@ -197,6 +197,10 @@ def test_weight_gradient_is_as_exact_as_fp32_products():
     # remainder 2^-16 at most of the rest; p from fp32 exponents (2^-20); 34 truncations a piece and fp32 sums of the targets
     bound = share * (2.0 ** -16 + 2.0 ** -19) + 34 * 2.0 ** -23 * 0.5
     assert np.linalg.norm(host(dw) - want) <= bound * np.linalg.norm(want)
+    # dx: its own rounding, 2^-8 of each element at most, spread evenly over half steps of 2^-9 to 2^-8 of the value (3^-1/2 of
+    # it in the mean); the rest's rounding likewise, its errors independent of one another
+    bound = 2.0 ** -8 * 3 ** -0.5 * (1 + 2 * share)
+    assert np.linalg.norm(host(dx) - want_dx) <= bound * np.linalg.norm(want_dx)
 
 
 def test_a_nan_in_a_live_row_reaches_its_gradient_and_no_other():

@@ -83,7 +83,8 @@ def check_embed_grad(grad, dout, tok, vocab, scale, before=None):
 @pytest.mark.parametrize("n,vocab,d,gap,shift", [(1, 1, 1, 0, 0), (1, 70001, 8, 0, 0), (997, 1003, 520, 0, 0), (64, 3, 129, 5, 1), (3000, 17, 72, 0, 0),
                                                  (8193, 255, 64, 0, 0), (20000, 256, 24, 8, 0), (20011, 65537, 33, 0, 0), (16, 2, 1024, 0, 0),
                                                  (40000, 70000, 16, 0, 8), (129, 40, 2056, 0, 0),
-                                                 (270001, 70000, 8, 0, 0), (500, 4194400, 8, 0, 0), (1025, 4194400, 8, 0, 0)])
+                                                 (270001, 70000, 8, 0, 0), (500, 4194400, 8, 0, 0), (1025, 4194400, 8, 0, 0),
+                                                 (2048, 900, 16, 0, 0), (2049, 900, 16, 0, 0), (1030, 2097150, 8, 0, 0), (1024, 2097151, 8, 0, 0)])
 def test_embed_gradient(kind, n, vocab, d, gap, shift):
     g = gen(n + vocab)
     dout = placed(torch.randn(n, d, generator=g, device="cuda").to(TYPES[kind]), gap, shift)

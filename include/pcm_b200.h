@@ -392,7 +392,8 @@ int grpo_embed(int32_t dtype, const void* table, int64_t ld_table, int32_t vocab
  * do not occur); with GRPO_ACCUMULATE in flags it is added to grad.  dout [n][d] of `dtype`, grad [vocab][d] fp32,
  * contiguous.  Tokens are sorted first; the rows of a token are summed in ascending i within tiles of 8 or 32 sorted
  * rows, the tiles of a frequent token in an order that depends on its rows alone.  d <= PCM_MAX_EMBED_DIM.  workspace: device, 256-byte aligned,
- * >= grpo_embed_workspace_bytes() (0 when the sizes are not supported). */
+ * >= grpo_embed_workspace_bytes() (0 when the sizes are not supported), which
+ * never falls as n grows: a workspace for the longest batch serves shorter ones. */
 size_t grpo_embed_workspace_bytes(int32_t n, int32_t vocab, int32_t d);
 int grpo_embed_bwd(int32_t dtype, const void* dout, int64_t ld_dout, const int32_t* tok, int32_t n, int32_t vocab, int32_t d,
                    float scale, uint32_t flags, float* grad, uint32_t* device_status, void* workspace, size_t workspace_bytes,

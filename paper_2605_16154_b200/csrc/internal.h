@@ -117,8 +117,9 @@ int tcgen05_poll_status();
 // grad[tok[i]] += coef[i] rows[i] in fp32 for rows [n][d] (bf16, 16-byte aligned, d a multiple of 8), tokens outside
 // [0, vocab) left out, in two steps with one scratch (256-byte aligned): the sort, which needs the tokens alone, and the
 // sums.  The sort's first kernel is an ordinary launch: what ran before it in the stream has ended when it starts.
+// Scratch of embed_accumulate_bytes(n) serves any smaller n too; the sort refuses scratch that is too small (PCM_ERR_WORKSPACE).
 size_t embed_accumulate_bytes(int n, int vocab, int d);
-int embed_accumulate_sort(const int* tok, int n, int vocab, int d, void* scratch, cudaStream_t s);
+int embed_accumulate_sort(const int* tok, int n, int vocab, int d, void* scratch, size_t scratch_bytes, cudaStream_t s);
 int embed_accumulate_sum(const void* rows, const float* coef, int n, int vocab, int d, float* grad, void* scratch, cudaStream_t s);
 
 // Causal attention within each sequence of S tokens.  qkv [n_seq*S][3d] (q | k | v, heads of dh

@@ -1119,9 +1119,15 @@ static int launch_embed(const T* table, long long ld_table, int vocab, int d, co
 static bool sizes_ok(int64_t rows, int64_t vocab) { return rows <= PCM_MAX_VOCAB_CALL && vocab <= PCM_MAX_VOCAB_CALL; }
 
 // Sorted pairs per tile: fewer for short batches, so that every SM gets some.
-static int embed_tile_rows(int n) { return n >= 32 * 296 ? 32 : 8; }
+constexpr int EM_LONG = 32 * 296;
+static int embed_tile_rows(int n) { return n >= EM_LONG ? 32 : 8; }
 
+// Every region is as large as any batch of up to n rows needs it, so that a workspace sized for n holds a shorter batch too
+// (the last chunk of rows of grpo_head_logp_bwd): just below EM_LONG there are more tiles than just above it, and a sort
+// of 262144 pairs runs in more blocks than one of 262145.
 static size_t embed_plan(EmbedPlan& pl, int n, int vocab, int d, void* ws) {
+  const int most_tiles = max(ceil_div(n, 32), ceil_div(min(n, EM_LONG - 1), 8));
+  const int most_blocks = min(ceil_div(n, ES_THREADS), ES_MAX_BLOCKS);
   pl.n = n; pl.vocab = vocab; pl.d = d;
   pl.rows = embed_tile_rows(n);
   pl.tiles = ceil_div(n, pl.rows);
@@ -1138,11 +1144,11 @@ static size_t embed_plan(EmbedPlan& pl, int n, int vocab, int d, void* ws) {
   if (pl.keys < ES_THREADS) pl.keys = ES_THREADS;
   pl.blocks = ceil_div(n, pl.keys);
   pl.present = (uint8_t*)take((size_t)vocab);
-  pl.hist = (unsigned*)take((size_t)pl.blocks * ES_BINS * 4);
+  pl.hist = (unsigned*)take((size_t)most_blocks * ES_BINS * 4);
   pl.n_jobs = (int*)take(4);
-  pl.jobs = (uint2*)take((size_t)pl.tiles * 8);
+  pl.jobs = (uint2*)take((size_t)most_tiles * 8);
   pl.first_tile = (int*)take((size_t)vocab * 4);
-  pl.part = (float*)take((size_t)pl.tiles * 2 * pl.dpad * 4);
+  pl.part = (float*)take((size_t)most_tiles * 2 * pl.dpad * 4);
   return off;
 }
 
@@ -1213,7 +1219,8 @@ size_t embed_accumulate_bytes(int n, int vocab, int d) {
   EmbedPlan pl;
   return embed_plan(pl, n, vocab, d, nullptr);
 }
-int embed_accumulate_sort(const int* tok, int n, int vocab, int d, void* scratch, cudaStream_t s) {
+int embed_accumulate_sort(const int* tok, int n, int vocab, int d, void* scratch, size_t scratch_bytes, cudaStream_t s) {
+  if (embed_accumulate_bytes(n, vocab, d) > scratch_bytes) return PCM_ERR_WORKSPACE;
   return launch_embed_sort(embed_sorted_plan(n, vocab, d, scratch), tok, nullptr, s);
 }
 int embed_accumulate_sum(const void* rows, const float* coef, int n, int vocab, int d, float* grad, void* scratch, cudaStream_t s) {

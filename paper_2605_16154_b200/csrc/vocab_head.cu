@@ -272,7 +272,7 @@ extern "C" int grpo_head_logp_bwd(const void* x, int64_t ld_x, int32_t n_rows, i
     int rc = PCM_OK;
     if (dw) {
       prof_begin(PC_EMBED, s);
-      rc = embed_accumulate_sort(tok + r0, rows, vocab, d, base + pl.sort, s);
+      rc = embed_accumulate_sort(tok + r0, rows, vocab, d, base + pl.sort, pl.total - pl.sort, s);
       prof_end(s, 0.0, 4.0 * rows);
       if (rc != PCM_OK) return rc;
     }

@@ -1,0 +1,113 @@
+"""The vocabulary calls at the edges of what they own, on the GPU: workspaces of exactly the size asked for with other data
+behind them, and chunks of rows on both sides of the sizes at which the plan of the sums changes."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import vocab_oracle as vo
+
+pytestmark = pytest.mark.gpu
+U = 2.0 ** -24
+GUARD = 1 << 22
+
+
+def B():
+    from paper_2605_16154_b200 import binding
+    return binding
+
+
+def gen(seed):
+    return torch.Generator(device="cuda").manual_seed(seed)
+
+
+def host(t):
+    return t.detach().double().cpu().numpy()
+
+
+class Guarded:
+    """A workspace of `need` bytes inside a larger buffer whose other bytes have to stay as they are."""
+
+    def __init__(self, need):
+        self.all = torch.full((need + 2 * GUARD + 256,), 0xA5, dtype=torch.uint8, device="cuda")
+        at = -self.all.data_ptr() % 256 + GUARD
+        self.lo, self.hi = at, at + need
+
+    def view(self):
+        return self.all[self.lo:self.hi]
+
+    def intact(self):
+        return bool((self.all[:self.lo] == 0xA5).all()) and bool((self.all[self.hi:] == 0xA5).all())
+
+
+def late_tokens(n, vocab, seed):
+    """Few tokens, often, at the end of the vocabulary (action tokens of a language policy); some rows are padded."""
+    g = gen(seed)
+    tok = vocab - 1 - (torch.rand(n, generator=g, device="cuda") ** 3 * min(vocab, 60)).int()
+    tok[torch.rand(n, generator=g, device="cuda") < 0.05] = -1
+    return tok.clamp_(-1, vocab - 1)
+
+
+def check_dw(dw, x, w, tok, dlogp):
+    """Against fp64, by the norm: remainder of d z at most 2^-16 of it, exponents a few 2^-20, pieces of 34 truncations of 2^-23
+    at most, the targets' sums k additions of 2^-24 on average far below their bound."""
+    xd, wd, t = x.double(), w.double(), tok.long()
+    live = t >= 0
+    xd = torch.where(live[:, None], xd, 0.0)
+    p = torch.softmax(xd @ wd.t(), -1)
+    dz = -p * torch.where(live, dlogp.double(), 0.0)[:, None]
+    dz[live.nonzero()[:, 0], t[live]] += dlogp.double()[live]
+    want = dz.t() @ xd
+    assert float((dw.double() - want).norm()) <= 2e-5 * float(want.norm())
+
+
+@pytest.mark.parametrize("n,d,vocab,chunk", [(12000, 64, 900, 10000), (18471, 64, 900, 9472), (18000, 128, 2003, 9500), (20000, 64, 700, 9471)])
+def test_head_gradient_of_a_shorter_last_chunk(n, d, vocab, chunk):
+    b = B()
+    g = gen(n + chunk)
+    x = torch.randn(n, d, generator=g, device="cuda").bfloat16()
+    w = (torch.randn(vocab, d, generator=g, device="cuda") * (2.0 / d ** 0.5)).bfloat16()
+    tok, dlogp = late_tokens(n, vocab, n), torch.randn(n, generator=g, device="cuda")
+    _, entropy, lse = b.grpo_head_logp(x, w, tok)
+    ws = Guarded(b.grpo_head_logp_bwd_workspace_bytes(n, d, vocab, chunk))
+    dx, dw = b.grpo_head_logp_bwd(x, w, tok, lse, entropy, dlogp, chunk_rows=chunk, workspace=ws.view())
+    torch.cuda.synchronize()
+    assert ws.intact()
+    check_dw(dw, x, w, tok, dlogp)
+    dx1, dw1 = b.grpo_head_logp_bwd(x, w, tok, lse, entropy, dlogp, chunk_rows=n)
+    # other pieces of the contraction and of the tokens' sums: fp32 rounding of up to n / 512 pieces; dx may round to the
+    # neighbouring bf16 value, 2^-7 of it
+    assert float((dw - dw1).norm() / dw1.norm()) < (n / 512) * U + 34 * 2.0 ** -23
+    assert float((dx.float() - dx1.float()).norm() / dx1.float().norm()) < 2.0 ** -7
+
+
+@pytest.mark.parametrize("kind", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("n", [1, 5, 2049, 9471, 9472, 9473, 30000, 262144, 262145])
+def test_embedding_gradient_stays_in_its_workspace(kind, n):
+    b, vocab, d = B(), 3001, 16
+    dout, tok = torch.randn(n, d, generator=gen(n), device="cuda").to(kind), late_tokens(n, vocab, n + 1)
+    ws = Guarded(b.grpo_embed_workspace_bytes(n, vocab, d))
+    grad = b.grpo_embed_bwd(dout, tok, vocab, workspace=ws.view())
+    torch.cuda.synchronize()
+    assert ws.intact()
+    t = tok.cpu().numpy()
+    want, mass = vo.embed_bwd(host(dout), t, vocab), vo.embed_bwd(np.abs(host(dout)), t, vocab)
+    k = np.bincount(t[t >= 0].astype(np.int64), minlength=vocab)[:, None]
+    assert np.all(np.abs(host(grad) - want) <= (k + 2) * U * mass + 2 * U * np.abs(want))
+    # the workspace of the longest batch serves this one
+    big = Guarded(b.grpo_embed_workspace_bytes(262145, vocab, d))
+    assert torch.equal(b.grpo_embed_bwd(dout, tok, vocab, workspace=big.view()), grad)
+    torch.cuda.synchronize()
+    assert big.intact()
+
+
+@pytest.mark.parametrize("n,vocab", [(1, 50001), (16, 40000), (128, 3000), (129, 3000), (700, 5003), (1025, 257)])
+def test_head_log_probabilities_stay_in_their_workspace(n, vocab):
+    b, d = B(), 64
+    g = gen(n + vocab)
+    x, w = torch.randn(n, d, generator=g, device="cuda").bfloat16(), (torch.randn(vocab, d, generator=g, device="cuda") * 0.2).bfloat16()
+    tok = late_tokens(n, vocab, n)
+    ws = Guarded(b.grpo_head_logp_workspace_bytes(n, d, vocab))
+    got = b.grpo_head_logp(x, w, tok, workspace=ws.view())
+    torch.cuda.synchronize()
+    assert ws.intact()
+    assert all(torch.equal(p, q) for p, q in zip(got, b.grpo_head_logp(x, w, tok)))

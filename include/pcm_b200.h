@@ -424,7 +424,8 @@ int grpo_token_logp_bwd(int32_t dtype, const void* logits, int64_t ld, int32_t n
  * x and w_h 16-byte aligned, d and both row strides multiples of 8 (PCM_ERR_SHAPE otherwise).  For top alternatives, and
  * for fp32 policies, form the logits with grpo_gemm and use grpo_token_logp.  logp, entropy, lse may each be NULL.
  * workspace: device, 256-byte aligned, >= grpo_head_logp_workspace_bytes() (0 when the sizes are not supported): 16
- * bytes for each row and 128 tokens; up to 128 rows, whose tiles are of 64 to 256 tokens, 32 bytes for each row and tile. */
+ * bytes for each row and 128 tokens; up to 128 rows, whose tiles are of 64 to 256 tokens, 32 bytes for each row and tile.
+ * It never falls as n_rows grows. */
 size_t grpo_head_logp_workspace_bytes(int32_t n_rows, int32_t d, int32_t vocab);
 int grpo_head_logp(const void* x, int64_t ld_x, int32_t n_rows, int32_t d, const void* w_h, int64_t ld_w, int32_t vocab,
                    const int32_t* tok, float temperature, float* logp, float* entropy, float* lse, uint32_t* device_status,

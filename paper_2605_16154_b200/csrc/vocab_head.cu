@@ -206,7 +206,9 @@ using namespace pcm;
 
 extern "C" size_t grpo_head_logp_workspace_bytes(int32_t n_rows, int32_t d, int32_t vocab) {
   if (n_rows < 0 || d < 8 || vocab < 1 || !head_shape_ok(d, d, d, n_rows, vocab)) return 0;
-  return round256(2 * (size_t)ceil_div(vocab, gemm_vocab_tile(n_rows, vocab)) * (size_t)n_rows * sizeof(float4)) + 256;
+  auto parts = [&](int rows) { return 2 * (size_t)ceil_div(vocab, gemm_vocab_tile(rows, vocab)) * (size_t)rows * sizeof(float4); };
+  // up to 128 rows the tiles are narrower, so 128 rows can leave more parts than 129
+  return round256(max(parts(n_rows), parts(min(n_rows, 128)))) + 256;
 }
 
 extern "C" int grpo_head_logp(const void* x, int64_t ld_x, int32_t n_rows, int32_t d, const void* w_h, int64_t ld_w, int32_t vocab,

@@ -53,3 +53,12 @@ def test_no_size_falls_as_the_rows_grow():
         assert all(p <= q for p, q in zip(sizes, sizes[1:]))
     sizes = [b.grpo_embed_workspace_bytes(n, 32000, 8) for n in range(260000, 264000)]
     assert all(p <= q for p, q in zip(sizes, sizes[1:]))
+
+
+@pytest.mark.parametrize("vocab", [1, 63, 700, 9473, 32000, 40000, 50257, 130011])
+def test_the_log_probabilities_of_the_longest_batch_leave_room_for_shorter_ones(vocab):
+    """Up to 128 rows a tile has 64 to 256 columns and leaves two parts of 16 bytes a row; beyond, 256."""
+    b = B()
+    sizes = [b.grpo_head_logp_workspace_bytes(n, 1024, vocab) for n in range(1, 1200)]
+    assert all(p <= q for p, q in zip(sizes, sizes[1:]))
+    assert all(s >= 32 * n * -(-vocab // 256) for n, s in enumerate(sizes, 1))

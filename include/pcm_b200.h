@@ -373,7 +373,9 @@ int grpo_adamw_step_lora(const grpo_model_cfg* cfg, const grpo_adamw_cfg* opt, i
  *     gradient and what it would read is not read.  A token >= vocab is treated the same and sets bit 5 (value 32) of
  *     device_status.
  *   - device_status (device [1], may be NULL) is only ever OR-ed into: clear it before the first call, read it when
- *     the stream has got there.  Bit 0: a bounded wait in a tensor-core kernel expired.
+ *     the stream has got there.  Bit 0: a bounded wait in a tensor-core kernel of that call expired, and its outputs are
+ *     not finished.  A call without a status word leaves the report to the next one on the device that polls
+ *     (grpo_gemm, grpo_attention, grpo_actor_fwd_bwd with stats: PCM_ERR_DEVICE_TIMEOUT).
  *   - Row strides ld* are in elements; a row is contiguous.  Rows may start anywhere their type allows unless a call
  *     says otherwise; 16-byte accesses are used where rows are aligned for them.
  *   - No call allocates or synchronises; all can be captured in a CUDA graph.  A workspace is scratch of one call:
@@ -467,6 +469,11 @@ int grpo_attention(int32_t dtype, const void* qkv, void* out, float* lse, const 
  * 3 queries landed, 4 probabilities ready, 5 accumulator slot free, 6 output ready, 7 scores ready).
  * Updated when a call returns PCM_ERR_DEVICE_TIMEOUT.  Host value, no GPU work. */
 uint32_t grpo_attention_wait_status(void);
+
+/* The current device's word of expired waits of the tensor-core GEMM kernels (0 = none since the last poll; all ones: the
+ * word could not be read), with `next` stored in its place: 0 clears it, 1 plants a report, which is how a test sees who
+ * reads it.  Synchronises the device's default stream. */
+uint32_t grpo_gemm_wait_status(uint32_t next);
 
 /* Per-kernel-class timing.  While enabled, every launch of the classes below is bracketed by a
  * pair of CUDA events on its stream; pcm_profile_read() synchronises the device, adds up elapsed

@@ -158,6 +158,8 @@ _lib.grpo_head_logp_bwd_workspace_bytes.argtypes = [_I, _I, _I, _I]
 _lib.grpo_head_logp_bwd_workspace_bytes.restype = C.c_size_t
 _lib.grpo_head_logp_bwd.argtypes = [_P, _L, _I, _I, _P, _L, _I, _P, _F, _P, _P, _P, _P, _I, C.c_uint32, _P, _L, _P, _P, _P,
                                     C.c_size_t, _P]
+_lib.grpo_gemm_wait_status.argtypes = [C.c_uint32]
+_lib.grpo_gemm_wait_status.restype = C.c_uint32
 _lib.pcm_launch_count.restype = C.c_int64
 _lib.pcm_first_use_on_device.argtypes = [C.POINTER(C.c_uint64), C.c_int32]
 _lib.pcm_first_use_on_device.restype = C.c_int32
@@ -178,7 +180,7 @@ EXPORTED = ("pcm_create", "pcm_destroy", "pcm_poll_status", "pcm_state_export", 
             "grpo_attention_wait_status", "pcm_first_use_on_device", "grpo_lora_workspace_bytes",
             "grpo_actor_fwd_bwd_lora", "grpo_embed", "grpo_embed_workspace_bytes", "grpo_embed_bwd", "grpo_token_logp",
             "grpo_token_logp_bwd", "grpo_head_logp_workspace_bytes", "grpo_head_logp", "grpo_head_logp_bwd_workspace_bytes",
-            "grpo_head_logp_bwd")
+            "grpo_head_logp_bwd", "grpo_gemm_wait_status")
 
 
 def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
@@ -709,6 +711,10 @@ def grpo_attention(qkv: torch.Tensor, n_seq: int, S: int, H: int, dh: int, dout:
 def grpo_attention_wait_status() -> int:
     _lib.grpo_attention_wait_status.restype = C.c_uint32
     return int(_lib.grpo_attention_wait_status())
+
+
+def grpo_gemm_wait_status(next: int = 0) -> int:
+    return int(_lib.grpo_gemm_wait_status(next))
 
 
 def pcm_launch_count() -> int:

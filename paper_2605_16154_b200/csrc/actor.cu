@@ -1153,6 +1153,9 @@ extern "C" int grpo_gemm(int32_t M, int32_t N, int32_t K, const void* A, int64_t
 namespace pcm { unsigned attention_tc_last_status(); }
 extern "C" uint32_t grpo_attention_wait_status(void) { return pcm::attention_tc_last_status(); }
 
+namespace pcm { unsigned tcgen05_exchange_status(unsigned next); }
+extern "C" uint32_t grpo_gemm_wait_status(uint32_t next) { return pcm::tcgen05_exchange_status(next); }
+
 extern "C" int grpo_attention(int32_t dtype, const void* qkv, void* out, float* lse, const void* dout, void* dqkv,
                               float* scratch, int32_t n_seq, int32_t S, int32_t n_heads, int32_t head_dim,
                               pcm_stream stream) {

@@ -15,7 +15,7 @@
 // epilogue of one tile overlaps the MMAs of the next.
 // Warp roles (320 threads): warp 0 = TMA producer, warp 1 = tensor-memory allocation + MMA issue,
 // warps 2..9 = epilogue (two per tensor-memory lane quadrant, splitting the tile's columns).  Every mbarrier wait is bounded; when one runs out the CTA sets a status
-// flag, all roles leave their loops, tensor memory is released and the kernel returns.
+// flag (the call's own word where it has one), all roles leave their loops, tensor memory is released and the kernel returns.
 #include <cuda.h>
 
 #include <cstdlib>
@@ -41,7 +41,7 @@ constexpr int EPI_STAGE_BYTES = TC_EPI_WARPS * EPI_STAGE_FLOATS * 4;
 constexpr int TC_THREADS = 320;               // producer warp, MMA warp, 8 epilogue warps
 constexpr unsigned long long TC_WAIT_LIMIT_NS = 2000000000ull;   // 2 s per mbarrier wait
 
-__device__ unsigned g_tc_status = 0;          // bit 0: a bounded wait expired
+__device__ unsigned g_tc_status = 0;          // STATUS_TIMEOUT: a bounded wait expired in a call without a word of its own
 
 struct TcParams {
   int M, N, K;
@@ -68,7 +68,10 @@ struct TcParams {
   int bn;                                     // columns per tile: BN, fewer for EPI_VOCAB_STATS on single CTAs
   int a_rows;                                 // rows of A that a tile loads: TC_BM, fewer for vocabulary products with M < TC_BM
   int stages;                                 // vocabulary products on single CTAs: ring depth
+  unsigned* status;                           // where an expired wait is reported: the call's own word, or null for the device's
 };
+
+__device__ __forceinline__ void report_timeout(const TcParams& p) { atomicOr(p.status ? p.status : &g_tc_status, STATUS_TIMEOUT); }
 
 __device__ __forceinline__ void store_bf16x32(__nv_bfloat16* dst, const float (&v)[32]) {
   uint4* d4 = reinterpret_cast<uint4*>(dst);
@@ -822,7 +825,7 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
         const int m0 = (mn / p.tiles_n) * TC_BM, n0 = (mn % p.tiles_n) * bn;
         const int kb_lo = split * p.kb_per_split, kb_hi = min(kb_lo + p.kb_per_split, num_kb_total);
         for (int kb = kb_lo; kb < kb_hi; ++kb) {
-          if (!mbar_wait_bounded(&empty[st], ph ^ 1u, TC_WAIT_LIMIT_NS)) { *abort_flag = 1; atomicOr(&g_tc_status, 1u); break; }
+          if (!mbar_wait_bounded(&empty[st], ph ^ 1u, TC_WAIT_LIMIT_NS)) { *abort_flag = 1; report_timeout(p); break; }
           uint8_t* sa = tiles + st * stage_bytes;
           uint8_t* sb = sa + a_bytes;
           mbar_expect_tx(&full[st], stage_bytes);
@@ -901,7 +904,7 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
         }
         if (ok) umma_commit(&acc_full[is_chained<EPI> ? tcount & 1u : ab]);
       }
-      if (!ok) { *abort_flag = 1; atomicOr(&g_tc_status, 1u); }
+      if (!ok) { *abort_flag = 1; report_timeout(p); }
     }
   } else {
     // ------------------------------ epilogue: warps 2..9 ------------------------------
@@ -922,7 +925,7 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
           const unsigned pb = tcount & 1u, pph = (tcount >> 1) & 1u;
           if (lane == 0) {
             ok = (!*abort_flag && mbar_wait_bounded(&acc_full[pb], pph, TC_WAIT_LIMIT_NS * 2ull)) ? 1 : 0;
-            if (!ok) { *abort_flag = 1; atomicOr(&g_tc_status, 1u); }
+            if (!ok) { *abort_flag = 1; report_timeout(p); }
           }
           ok = __shfl_sync(0xffffffffu, ok, 0);
           if (!ok) break;
@@ -944,7 +947,7 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
       int ok = 1;
       if (lane == 0) {
         ok = (!*abort_flag && mbar_wait_bounded(&acc_full[ab], aph, TC_WAIT_LIMIT_NS * 2ull)) ? 1 : 0;
-        if (!ok) { *abort_flag = 1; atomicOr(&g_tc_status, 1u); }
+        if (!ok) { *abort_flag = 1; report_timeout(p); }
       }
       ok = __shfl_sync(0xffffffffu, ok, 0);
       if (!ok) break;
@@ -1109,7 +1112,7 @@ gemm_tc2_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
           if (++st == T2_STAGES) { st = 0; ph ^= 1u; }
         }
       }
-      if (!ok) { *abort_flag = 1; atomicOr(&g_tc_status, 1u); }
+      if (!ok) { *abort_flag = 1; report_timeout(p); }
     }
   } else if (warp == 1) {
     if (lane == 0 && leader) {
@@ -1170,7 +1173,7 @@ gemm_tc2_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
         }
         if (ok) umma_commit_pair(&acc_full[is_chained<EPI> ? tcount & 1u : ab], 3);
       }
-      if (!ok) { *abort_flag = 1; atomicOr(&g_tc_status, 1u); }
+      if (!ok) { *abort_flag = 1; report_timeout(p); }
     }
   } else {
     // ------------------------------ epilogue: warps 2..9 of both CTAs ------------------------------
@@ -1193,7 +1196,7 @@ gemm_tc2_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
           const unsigned pb = tcount & 1u, pph = (tcount >> 1) & 1u;
           if (lane == 0) {
             ok = (!*abort_flag && mbar_wait_bounded(&acc_full[pb], pph, TC_WAIT_LIMIT_NS * 2ull)) ? 1 : 0;
-            if (!ok) { *abort_flag = 1; atomicOr(&g_tc_status, 1u); }
+            if (!ok) { *abort_flag = 1; report_timeout(p); }
           }
           ok = __shfl_sync(0xffffffffu, ok, 0);
           if (!ok) break;
@@ -1215,7 +1218,7 @@ gemm_tc2_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
       int ok = 1;
       if (lane == 0) {
         ok = (!*abort_flag && mbar_wait_bounded(&acc_full[ab], aph, TC_WAIT_LIMIT_NS * 2ull)) ? 1 : 0;
-        if (!ok) { *abort_flag = 1; atomicOr(&g_tc_status, 1u); }
+        if (!ok) { *abort_flag = 1; report_timeout(p); }
       }
       ok = __shfl_sync(0xffffffffu, ok, 0);
       if (!ok) break;
@@ -1312,6 +1315,7 @@ static void fill_params(TcParams& p, const GemmArgs& g) {
   p.chain_kb = g.epi.chain_kb > 0 ? g.epi.chain_kb : p.kb_total;
   p.accumulate = g.epi.accumulate;
   p.part_stride = g.epi.part_stride;
+  p.status = g.epi.status;
   // The operand whose tiles run fastest is read once for every wave of the other's: the shorter one, which fits L2 sooner
   // (d z of 8192 rows x 1024 x 32000: 0.09 GB of reads instead of 1.0, 519 us -> 463).
   p.m_fast = g.M < g.N;
@@ -1492,16 +1496,6 @@ int gemm_chain_splits(const GemmArgs& g) {
 }
 size_t chain_part_bytes() { return (size_t)sm_count() * TC_BM * T2_BN * 4; }
 
-__global__ void forward_status_kernel(unsigned* status) {
-  if (g_tc_status) atomicOr(status, STATUS_TIMEOUT);
-}
-int gemm_forward_status(unsigned* status, cudaStream_t s) {
-  if (!status) return PCM_OK;
-  forward_status_kernel<<<1, 1, 0, s>>>(status);
-  PCM_LAUNCH_CHECK();
-  return PCM_OK;
-}
-
 bool gemm_epilogue_supported(const GemmArgs& g) {
   if (g.epi.kind == EPI_VOCAB_STATS || g.epi.kind == EPI_VOCAB_DZ || g.epi.kind == EPI_CHAIN) {
     // any N (EPI_CHAIN: a multiple of 8), so the general conditions are checked here
@@ -1575,6 +1569,13 @@ int gemm_tcgen05(const GemmArgs& g, cudaStream_t s) {
   if (pair) return launch_tc2<EPI_NONE>(g, s);
   if (g.N % 256 == 0 || g.N > 256) return launch_tc<256, EPI_NONE>(g, s);
   return launch_tc<128, EPI_NONE>(g, s);
+}
+
+// The device word of expired waits; `next` is stored in its place.
+unsigned tcgen05_exchange_status(unsigned next) {
+  unsigned h = 0;
+  if (cudaMemcpyFromSymbol(&h, g_tc_status, sizeof(h)) != cudaSuccess) return ~0u;
+  return cudaMemcpyToSymbol(g_tc_status, &next, sizeof(next)) == cudaSuccess ? h : ~0u;
 }
 
 int attention_tc_poll_status();

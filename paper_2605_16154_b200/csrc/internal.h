@@ -72,6 +72,9 @@ struct GemmEpilogue {
   //                 splits > 1: each split of the contraction stores its own fp32 part, part_stride elements apart.
   int chain_kb = 0, splits = 1, accumulate = 0;
   long long part_stride = 0;
+  // Device word that receives STATUS_TIMEOUT when a bounded wait of this product expires; null: the device's own word,
+  // which tcgen05_poll_status() reads.
+  unsigned* status = nullptr;
 };
 
 struct GemmArgs {
@@ -106,9 +109,6 @@ int gemm_chain_splits(const GemmArgs& g);
 // Columns per tile of an EPI_VOCAB_STATS product; a tile leaves two parts a row, of its first 128 columns and of the rest.
 int gemm_vocab_tile(int M, int N);
 size_t chain_part_bytes();
-// Sets STATUS_TIMEOUT in *status (device; nothing where it is null), in stream order, when a bounded wait of a
-// tensor-core GEMM has run out since the status was last polled.
-int gemm_forward_status(unsigned* status, cudaStream_t s);
 // True when the tensor-core kernel can run g including its fused epilogue.
 bool gemm_epilogue_supported(const GemmArgs& g);
 // Reads and clears the tensor-core kernels' device status word (synchronous copy).

@@ -224,6 +224,7 @@ extern "C" int grpo_head_logp(const void* x, int64_t ld_x, int32_t n_rows, int32
   float4* part = (float4*)workspace;
   GemmArgs g{n_rows, vocab, d, x, ld_x, true, w_h, ld_w, true, DT_BF16, nullptr, 0, DT_BF16, nullptr, 0};
   g.epi.kind = EPI_VOCAB_STATS;
+  g.epi.status = device_status;
   g.epi.vh.tok = tok; g.epi.vh.inv_t = inv_t; g.epi.vh.part = part; g.epi.vh.vocab = vocab;
   prof_begin(gemm_class(n_rows, 256), s);
   int rc = gemm_tcgen05(g, s);
@@ -235,8 +236,7 @@ extern "C" int grpo_head_logp(const void* x, int64_t ld_x, int32_t n_rows, int32
   rc = n_rows <= 1024 ? launch_after(vocab_stats_join_row_kernel, dim3(n_rows), dim3(128), s, jp)
                       : launch_after(vocab_stats_join_kernel, dim3(ceil_div(n_rows, 32)), dim3(32 * VH_GROUPS), s, jp);
   prof_end(s, 0.0, 16.0 * n_rows * jp.parts);
-  if (rc != PCM_OK) return rc;
-  return gemm_forward_status(device_status, s);
+  return rc;
 }
 
 extern "C" size_t grpo_head_logp_bwd_workspace_bytes(int32_t n_rows, int32_t d, int32_t vocab, int32_t chunk_rows) {
@@ -288,6 +288,7 @@ extern "C" int grpo_head_logp_bwd(const void* x, int64_t ld_x, int32_t n_rows, i
 
     GemmArgs z{rows, vocab, d, x_live, d, true, w_h, ld_w, true, DT_BF16, hi, pl.ldz, DT_BF16, nullptr, 0};
     z.epi.kind = EPI_VOCAB_DZ;
+    z.epi.status = device_status;
     VocabHeadArgs& v = z.epi.vh;
     v.tok = tok + r0; v.inv_t = inv_t; v.lse = lse + r0; v.dlogp = dlogp + r0; v.vocab = vocab; v.dz_lo = lo;
     v.coef = dw ? coef : nullptr;
@@ -301,6 +302,7 @@ extern "C" int grpo_head_logp_bwd(const void* x, int64_t ld_x, int32_t n_rows, i
     if (dx) {
       GemmArgs q{rows, d, vocab, hi, pl.ldz, true, w_h, ld_w, false, DT_BF16, (unsigned short*)dx + (long long)r0 * ld_dx, ld_dx, DT_BF16, nullptr, 0};
       q.epi.kind = EPI_CHAIN;                  // bf16 result: one accumulator piece
+      q.epi.status = device_status;
       q.epi.vh.tok = tok + r0; q.epi.vh.vocab = vocab; q.epi.vh.corr = corr;
       q.epi.vh.w = (const __nv_bfloat16*)w_h; q.epi.vh.ld_w = ld_w;
       prof_begin(gemm_class(rows, d), s);
@@ -312,6 +314,7 @@ extern "C" int grpo_head_logp_bwd(const void* x, int64_t ld_x, int32_t n_rows, i
       GemmArgs q{vocab, d, rows, hi, pl.ldz, false, x_live, d, false, DT_BF16, dw, d, DT_F32, nullptr, 0};
       q.A2 = lo; q.lda2 = pl.ldz; q.B2 = x_live; q.ldb2 = d; q.K2 = rows;
       q.epi.kind = EPI_CHAIN;
+      q.epi.status = device_status;
       q.epi.chain_kb = VH_CHAIN_KB;
       q.epi.accumulate = accumulate || r0 > 0;
       prof_begin(gemm_class(vocab, d), s);
@@ -324,5 +327,5 @@ extern "C" int grpo_head_logp_bwd(const void* x, int64_t ld_x, int32_t n_rows, i
       if (rc != PCM_OK) return rc;
     }
   }
-  return gemm_forward_status(device_status, s);
+  return PCM_OK;
 }

@@ -80,15 +80,18 @@ embed_kernel(const T* __restrict__ table, long long ld_table, int vocab, int d, 
 #pragma unroll
       for (int u = 0; u < 4; ++u) {
         const int v = v0 + u * tpr;
-        float f[V::N];
-        V::unpack(r[u], f);
+        if (scale != 1.f) {                   // a scale of 1 copies bits, a NaN's too
+          float f[V::N];
+          V::unpack(r[u], f);
 #pragma unroll
-        for (int e = 0; e < V::N; ++e) f[e] *= scale;
-        if (v < nv) __stcs(d4 + v, live ? V::pack(f) : make_uint4(0, 0, 0, 0));
+          for (int e = 0; e < V::N; ++e) f[e] *= scale;
+          r[u] = live ? V::pack(f) : make_uint4(0, 0, 0, 0);
+        }
+        if (v < nv) __stcs(d4 + v, r[u]);
       }
     }
   } else {
-    for (int c = lane; c < d; c += tpr) dst[c] = live ? from_f32<T>(as_f32(src[c]) * scale) : from_f32<T>(0.f);
+    for (int c = lane; c < d; c += tpr) dst[c] = !live ? from_f32<T>(0.f) : scale == 1.f ? src[c] : from_f32<T>(as_f32(src[c]) * scale);
   }
 }
 

@@ -111,3 +111,18 @@ def test_head_log_probabilities_stay_in_their_workspace(n, vocab):
     torch.cuda.synchronize()
     assert ws.intact()
     assert all(torch.equal(p, q) for p, q in zip(got, b.grpo_head_logp(x, w, tok)))
+
+
+@pytest.mark.parametrize("kind,ints", [(torch.float32, torch.int32), (torch.bfloat16, torch.int16)])
+@pytest.mark.parametrize("d,gap", [(64, 0), (2056, 8), (37, 0)])
+def test_embedding_with_scale_one_copies_bits(kind, ints, d, gap):
+    """Every bit pattern of the type arrives as it is: NaNs with their payloads and signs, infinities, -0, subnormals."""
+    vocab = 70
+    bits = torch.randint(torch.iinfo(ints).min, torch.iinfo(ints).max, (vocab, d + gap), generator=gen(d), device="cuda", dtype=torch.int64).to(ints)
+    special = {torch.int32: [0x7F800001, -0x3FFFFF, 0x7FC12345, -0x800000, -(1 << 31), 1], torch.int16: [0x7F81, -0x3F, 0x7FC9, -0x80, -(1 << 15), 1]}[ints]
+    bits[:, :6] = torch.tensor(special, dtype=torch.int64, device="cuda").to(ints)
+    table = bits.view(kind)[:, :d]
+    tok = torch.randint(-1, vocab, (200,), generator=gen(d + 1), device="cuda", dtype=torch.int32)
+    out = B().grpo_embed(table, tok).view(ints)
+    want = torch.where((tok >= 0)[:, None], bits[:, :d][tok.clamp(min=0).long()], 0)
+    assert torch.equal(out, want)

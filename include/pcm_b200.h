@@ -383,7 +383,7 @@ int grpo_adamw_step_lora(const grpo_model_cfg* cfg, const grpo_adamw_cfg* opt, i
  *   - The same inputs give the same bits: every sum has an order that follows from sizes and tokens alone. */
 #define PCM_MAX_TOP 16
 #define PCM_MAX_EMBED_DIM 65536
-#define PCM_MAX_VOCAB_CALL (1 << 30)   /* rows and tokens of one call (PCM_ERR_SHAPE beyond) */
+#define PCM_MAX_VOCAB_CALL (1 << 30)   /* rows, tokens and columns of one call (PCM_ERR_SHAPE beyond) */
 
 /* out[i] = round(scale * table[tok[i]]) for i < n: table [vocab][d], out [n][d], both of `dtype` (a grpo_dtype).
  * The product is formed in fp32 and rounded once; scale = 1 copies bits. */

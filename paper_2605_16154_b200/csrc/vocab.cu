@@ -1293,7 +1293,7 @@ using namespace pcm;
 extern "C" int grpo_embed(int32_t dtype, const void* table, int64_t ld_table, int32_t vocab, int32_t d, const int32_t* tok,
                           int32_t n, float scale, void* out, int64_t ld_out, uint32_t* device_status, pcm_stream stream) {
   if (!dtype_ok(dtype) || n < 0 || vocab < 1 || d < 1 || ld_table < d || ld_out < d || !std::isfinite(scale)) return PCM_ERR_ARG;
-  if (!sizes_ok(n, vocab)) return PCM_ERR_SHAPE;
+  if (!sizes_ok(n, vocab) || d > PCM_MAX_VOCAB_CALL) return PCM_ERR_SHAPE;       // a thread's columns are counted in 32 bits
   if (n == 0) return PCM_OK;
   if (!table || !tok || !out || !elem_aligned(table, dtype) || !elem_aligned(out, dtype)) return PCM_ERR_ARG;
   cudaStream_t s = (cudaStream_t)stream;

@@ -194,9 +194,9 @@ static bool head_args_ok(const void* x, int64_t ld_x, const void* w, int64_t ld_
   return x && w && tok && !(((uintptr_t)x | (uintptr_t)w) & 15) && ld_x >= d && ld_w >= d;
 }
 static bool temperature_ok(float t) { return t > 0.f && std::isfinite(t) && std::isfinite(1.f / t); }
-// Tiles are counted in 32 bits, at 64 columns and 128 rows the smallest.
+// Tiles are counted in 32 bits, at 64 columns and 128 rows the smallest; so are the contraction's k-blocks, rounded up.
 static bool head_shape_ok(int64_t ld_x, int64_t ld_w, int32_t d, int64_t n_rows, int64_t vocab) {
-  return d % 8 == 0 && ld_x % 8 == 0 && ld_w % 8 == 0 && n_rows <= PCM_MAX_VOCAB_CALL && vocab <= PCM_MAX_VOCAB_CALL &&
+  return d % 8 == 0 && ld_x % 8 == 0 && ld_w % 8 == 0 && n_rows <= PCM_MAX_VOCAB_CALL && vocab <= PCM_MAX_VOCAB_CALL && d <= PCM_MAX_VOCAB_CALL &&
          (n_rows / 128 + 1) * (vocab / 64 + 1) < (1ll << 31) && ((int64_t)d / 64 + 1) * (vocab / 64 + 1) < (1ll << 31);
 }
 

@@ -1,0 +1,21 @@
+"""Sizes and factors at the edge of what the vocabulary calls take, on the host: nothing is launched."""
+import pytest
+
+from tests.test_vocab_refusals import EMBED, HEAD, HEAD_BWD, SHAPE, _call
+
+WIDE = (1 << 30) + 8
+
+
+@pytest.mark.parametrize("d", [(1 << 30) + 1, WIDE, 2 ** 31 - 200, 2 ** 31 - 1])
+def test_rows_whose_columns_pass_31_bits_are_refused(d):
+    """A thread steps through a row's columns in 32 bits: the step behind the last one has to fit too."""
+    assert _call("grpo_embed", EMBED, n=1, d=d, ld_table=d, ld_out=d) == SHAPE
+    assert _call("grpo_embed", EMBED, n=0, d=1 << 30, ld_table=1 << 30, ld_out=1 << 30) == 0
+
+
+@pytest.mark.parametrize("d", [WIDE, 2 ** 31 - 8])
+def test_hidden_widths_whose_blocks_pass_31_bits_are_refused(d):
+    from paper_2605_16154_b200 import binding as B
+    for name, base, lead in (("grpo_head_logp", HEAD, {}), ("grpo_head_logp_bwd", HEAD_BWD, dict(ld_dx=d))):
+        assert _call(name, base, n_rows=1, d=d, ld_x=d, ld_w=d, vocab=1, **lead) == SHAPE
+    assert B.grpo_head_logp_workspace_bytes(1, d, 1) == 0 and B.grpo_head_logp_bwd_workspace_bytes(1, d, 1, 1) == 0

@@ -378,6 +378,7 @@ int grpo_adamw_step_lora(const grpo_model_cfg* cfg, const grpo_adamw_cfg* opt, i
  *     (grpo_gemm, grpo_attention, grpo_actor_fwd_bwd with stats: PCM_ERR_DEVICE_TIMEOUT).
  *   - Row strides ld* are in elements; a row is contiguous.  Rows may start anywhere their type allows unless a call
  *     says otherwise; 16-byte accesses are used where rows are aligned for them.
+ *   - A temperature is above 0, and log2(e) / temperature is finite in fp32 (PCM_ERR_ARG otherwise).
  *   - No call allocates or synchronises; all can be captured in a CUDA graph.  A workspace is scratch of one call:
  *     calls that may run at the same time need one each.  n = 0 rows is a valid call.
  *   - The same inputs give the same bits: every sum has an order that follows from sizes and tokens alone. */

@@ -1340,7 +1340,7 @@ extern "C" int grpo_token_logp(int32_t dtype, const void* logits, int64_t ld, in
                                float temperature, int32_t top, float* logp, float* entropy, float* lse, int32_t* top_id,
                                float* top_logp, uint32_t* device_status, pcm_stream stream) {
   if (!dtype_ok(dtype) || n_rows < 0 || vocab < 1 || ld < vocab || top < 0) return PCM_ERR_ARG;
-  if (!(temperature > 0.f) || !std::isfinite(temperature) || !std::isfinite(1.f / temperature)) return PCM_ERR_ARG;
+  if (!vocab_temperature_ok(temperature)) return PCM_ERR_ARG;
   if (top > PCM_MAX_TOP || top > vocab || !sizes_ok(n_rows, vocab)) return PCM_ERR_SHAPE;
   if (n_rows == 0) return PCM_OK;
   if (!logits || !elem_aligned(logits, dtype) || (logp && !tok) || (top > 0 && (!top_id || !top_logp))) return PCM_ERR_ARG;
@@ -1357,7 +1357,7 @@ extern "C" int grpo_token_logp_bwd(int32_t dtype, const void* logits, int64_t ld
                                    const float* dlogp, const float* dentropy, void* dlogits, int64_t ld_dlogits,
                                    uint32_t* device_status, pcm_stream stream) {
   if (!dtype_ok(dtype) || n_rows < 0 || vocab < 1 || ld < vocab || ld_dlogits < vocab) return PCM_ERR_ARG;
-  if (!(temperature > 0.f) || !std::isfinite(temperature) || !std::isfinite(1.f / temperature)) return PCM_ERR_ARG;
+  if (!vocab_temperature_ok(temperature)) return PCM_ERR_ARG;
   if (!sizes_ok(n_rows, vocab)) return PCM_ERR_SHAPE;
   if (n_rows == 0) return PCM_OK;
   if (!logits || !tok || !lse || !dlogp || !dlogits || (dentropy && !entropy)) return PCM_ERR_ARG;

@@ -10,6 +10,10 @@ namespace pcm {
 constexpr float VOCAB_LOG2E = 1.44269504088896340736f;
 constexpr float VOCAB_LN2 = 0.69314718055994530942f;
 
+// The kernels scale logits by 1 / T and exponents by log2(e) / T, in fp32: an infinite factor would make 0 * inf of the largest
+// logit of a row.
+static inline bool vocab_temperature_ok(float t) { return t > 0.f && t < INFINITY && 1.f / t * VOCAB_LOG2E < INFINITY; }
+
 __device__ __forceinline__ float max_nan(float a, float b) {
   float r;
   asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));

@@ -15,8 +15,6 @@
 // and 1.6e-6; hi + lo alone left 2.6e-6, hi alone would leave 1.6e-3.  The sums cost 60 us of the large batch, 19 us of
 // 86 of the small one.
 
-#include <cmath>
-
 #include "internal.h"
 
 namespace pcm {
@@ -193,7 +191,6 @@ static HeadBwdPlan head_bwd_plan(int M, int d, int V, int chunk_rows) {
 static bool head_args_ok(const void* x, int64_t ld_x, const void* w, int64_t ld_w, int32_t d, const int32_t* tok) {
   return x && w && tok && !(((uintptr_t)x | (uintptr_t)w) & 15) && ld_x >= d && ld_w >= d;
 }
-static bool temperature_ok(float t) { return t > 0.f && std::isfinite(t) && std::isfinite(1.f / t); }
 // Tiles are counted in 32 bits, at 64 columns and 128 rows the smallest; so are the contraction's k-blocks, rounded up.
 static bool head_shape_ok(int64_t ld_x, int64_t ld_w, int32_t d, int64_t n_rows, int64_t vocab) {
   return d % 8 == 0 && ld_x % 8 == 0 && ld_w % 8 == 0 && n_rows <= PCM_MAX_VOCAB_CALL && vocab <= PCM_MAX_VOCAB_CALL && d <= PCM_MAX_VOCAB_CALL &&
@@ -214,7 +211,7 @@ extern "C" size_t grpo_head_logp_workspace_bytes(int32_t n_rows, int32_t d, int3
 extern "C" int grpo_head_logp(const void* x, int64_t ld_x, int32_t n_rows, int32_t d, const void* w_h, int64_t ld_w, int32_t vocab,
                               const int32_t* tok, float temperature, float* logp, float* entropy, float* lse,
                               uint32_t* device_status, void* workspace, size_t workspace_bytes, pcm_stream stream) {
-  if (n_rows < 0 || d < 1 || vocab < 1 || !temperature_ok(temperature)) return PCM_ERR_ARG;
+  if (n_rows < 0 || d < 1 || vocab < 1 || !vocab_temperature_ok(temperature)) return PCM_ERR_ARG;
   if (!head_shape_ok(ld_x, ld_w, d, n_rows, vocab)) return PCM_ERR_SHAPE;
   if (n_rows == 0) return PCM_OK;
   if (!head_args_ok(x, ld_x, w_h, ld_w, d, tok)) return PCM_ERR_ARG;
@@ -249,7 +246,7 @@ extern "C" int grpo_head_logp_bwd(const void* x, int64_t ld_x, int32_t n_rows, i
                                   const float* dlogp, const float* dentropy, int32_t chunk_rows, uint32_t flags, void* dx,
                                   int64_t ld_dx, float* dw, uint32_t* device_status, void* workspace, size_t workspace_bytes,
                                   pcm_stream stream) {
-  if (n_rows < 0 || d < 1 || vocab < 1 || chunk_rows < 1 || !temperature_ok(temperature) || (flags & ~GRPO_ACCUMULATE)) return PCM_ERR_ARG;
+  if (n_rows < 0 || d < 1 || vocab < 1 || chunk_rows < 1 || !vocab_temperature_ok(temperature) || (flags & ~GRPO_ACCUMULATE)) return PCM_ERR_ARG;
   if (!head_shape_ok(ld_x, ld_w, d, n_rows, vocab) || (dx && ld_dx % 8)) return PCM_ERR_SHAPE;
   if ((!dx && !dw) || (dx && (((uintptr_t)dx & 15) || ld_dx < d)) || (dw && ((uintptr_t)dw & 15))) return PCM_ERR_ARG;
   const bool accumulate = flags & GRPO_ACCUMULATE;

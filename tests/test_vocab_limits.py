@@ -1,7 +1,7 @@
 """Sizes and factors at the edge of what the vocabulary calls take, on the host: nothing is launched."""
 import pytest
 
-from tests.test_vocab_refusals import EMBED, HEAD, HEAD_BWD, SHAPE, _call
+from tests.test_vocab_refusals import ARG, EMBED, HEAD, HEAD_BWD, LOGP, LOGP_BWD, SHAPE, _call
 
 WIDE = (1 << 30) + 8
 
@@ -19,3 +19,13 @@ def test_hidden_widths_whose_blocks_pass_31_bits_are_refused(d):
     for name, base, lead in (("grpo_head_logp", HEAD, {}), ("grpo_head_logp_bwd", HEAD_BWD, dict(ld_dx=d))):
         assert _call(name, base, n_rows=1, d=d, ld_x=d, ld_w=d, vocab=1, **lead) == SHAPE
     assert B.grpo_head_logp_workspace_bytes(1, d, 1) == 0 and B.grpo_head_logp_bwd_workspace_bytes(1, d, 1, 1) == 0
+
+
+@pytest.mark.parametrize("name,base", [("grpo_token_logp", LOGP), ("grpo_token_logp_bwd", LOGP_BWD), ("grpo_head_logp", HEAD),
+                                       ("grpo_head_logp_bwd", HEAD_BWD)])
+def test_temperatures_whose_factors_are_infinite_are_refused(name, base):
+    """1 / T is finite from 2.94e-39 on, log2(e) / T, which scales the exponents, from 4.24e-39 on."""
+    for t in (2.95e-39, 3.5e-39, 4.2e-39, float("inf"), 0.0, -1.0, float("nan")):
+        assert _call(name, base, temperature=t, n_rows=0) == ARG
+    for t in (4.3e-39, 1e-3, 1.0, 1e30, 3.4028e38):
+        assert _call(name, base, temperature=t, n_rows=0, **({"dw": None} if "dw" in base else {})) == 0

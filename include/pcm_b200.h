@@ -255,6 +255,7 @@ int grpo_pack_chunks(pcm_ctx* ctx, const pcm_batch* batch, const grpo_model_cfg*
 #define GRPO_FWD_ONLY 1u       /* forward only: writes logp (and loss), touches no gradient       */
 #define GRPO_ACCUMULATE 2u     /* add into grads instead of overwriting them                      */
 #define GRPO_CHUNK_RATIO 4u    /* one importance ratio per chunk (joint of its 56 tokens) instead of per token */
+#define GRPO_EXACT_DX 8u       /* grpo_head_logp_bwd: dx from unrounded logit gradients (one more product)          */
 
 typedef struct {
   float eps_low;               /* clip range [1 - eps_low, 1 + eps_high]                          */
@@ -435,7 +436,8 @@ int grpo_head_logp(const void* x, int64_t ld_x, int32_t n_rows, int32_t d, const
                    void* workspace, size_t workspace_bytes, pcm_stream stream);
 
 /* Its gradients, with dlogits as in grpo_token_logp_bwd (formed in fp32 from a second x w_h^T):
- *     dx = dlogits w_h  (bf16 [n_rows][d], row stride ld_dx; dlogits rounded to bf16, the targets' entries not)
+ *     dx = dlogits w_h  (bf16 [n_rows][d], row stride ld_dx; dlogits rounded to bf16, the targets' entries not; with
+ *                       GRPO_EXACT_DX in flags dlogits is a sum of two bf16 values as for dw, at the cost of one more product)
  *     dw = dlogits^T x  (fp32 [vocab][d], contiguous, 16-byte aligned; GRPO_ACCUMULATE in flags adds to it), from dlogits
  *                       as a sum of two bf16 values, the targets' own in fp32
  * Either may be NULL.  x may hold anything, NaN too, in rows without a token.  The rows are processed chunk_rows (>= 1) at

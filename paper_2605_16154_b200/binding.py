@@ -22,7 +22,7 @@ _lib = C.CDLL(LIB_PATH)
 ACT_DIM = 56
 N_BINS = 256
 GRPO_F32, GRPO_BF16 = 0, 1
-GRPO_FWD_ONLY, GRPO_ACCUMULATE, GRPO_CHUNK_RATIO = 1, 2, 4
+GRPO_FWD_ONLY, GRPO_ACCUMULATE, GRPO_CHUNK_RATIO, GRPO_EXACT_DX = 1, 2, 4, 8
 MASK_PCM, MASK_RANDOM, MASK_FULL = 0, 1, 2
 
 STATUS_NAMES = {0: "PCM_OK", -1: "PCM_ERR_ARG", -2: "PCM_ERR_SHAPE", -3: "PCM_ERR_WORKSPACE", -4: "PCM_ERR_CUDA",
@@ -649,9 +649,10 @@ def grpo_head_logp_bwd(x: torch.Tensor, w_h: torch.Tensor, tok: torch.Tensor, ls
                        dlogp: torch.Tensor, dentropy: Optional[torch.Tensor] = None, temperature: float = 1.0,
                        dx: Optional[torch.Tensor] = None, dw: Optional[torch.Tensor] = None, accumulate: bool = False,
                        want_dx: bool = True, want_dw: bool = True, chunk_rows: int = 0,
-                       workspace: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None):
+                       workspace: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None, exact_dx: bool = False):
     """(dx bf16 [n, d], dw fp32 [vocab, d]) of a loss with the given gradients by logp and entropy; with `accumulate` dw is
-    added to.  chunk_rows = 0 takes as many rows at a time as HEAD_CHUNK_BYTES of logit gradients hold."""
+    added to.  chunk_rows = 0 takes as many rows at a time as HEAD_CHUNK_BYTES of logit gradients hold.  `exact_dx`: dx from
+    logit gradients that are not rounded to bf16 first, for one more product."""
     call = "grpo_head_logp_bwd"
     operands = _head_operands(call, x, w_h)
     _, _, n, d, _, _, vocab = operands
@@ -674,7 +675,7 @@ def grpo_head_logp_bwd(x: torch.Tensor, w_h: torch.Tensor, tok: torch.Tensor, ls
         dw = torch.empty((vocab, d), dtype=_f32, device=dev)
     _launch(call, dev, _lib.grpo_head_logp_bwd, *operands, _vector(call, tok, dev, _i32, n), temperature,
             _vector(call, lse, dev, _f32, n), _vector(call, entropy, dev, _f32, n), _vector(call, dlogp, dev, _f32, n),
-            _vector(call, dentropy, dev, _f32, n), chunk_rows, GRPO_ACCUMULATE if accumulate else 0, dxp, lddx,
+            _vector(call, dentropy, dev, _f32, n), chunk_rows, (GRPO_ACCUMULATE if accumulate else 0) | (GRPO_EXACT_DX if exact_dx else 0), dxp, lddx,
             _vector(call, dw, dev, _f32, vocab * d), _vector(call, status, dev, _i32, 1), wsp, wsn)
     return dx, dw
 

@@ -1342,7 +1342,7 @@ static int launch_tc(const GemmArgs& g, cudaStream_t s) {
   if (!okA || !okB) return PCM_ERR_CUDA;
   CUtensorMap tmA2 = tmA, tmB2 = tmB;                      // continuation of the contraction, laid out like A / B
   if (g.K2 > 0) {
-    const bool okA2 = g.a_kmajor ? make_tmap(&tmA2, g.A2, g.M, g.K2, g.lda2, TC_BK, TC_BM)
+    const bool okA2 = g.a_kmajor ? make_tmap(&tmA2, g.A2, g.M, g.K2, g.lda2, TC_BK, a_rows)
                                  : make_tmap(&tmA2, g.A2, g.K2, g.M, g.lda2, 64, TC_BK);
     const bool okB2 = g.b_kmajor ? make_tmap(&tmB2, g.B2, g.N, g.K2, g.ldb2, TC_BK, B_BOX_ROWS)
                                  : make_tmap(&tmB2, g.B2, g.K2, g.N, g.ldb2, 64, TC_BK);

@@ -7,8 +7,11 @@
 //             chunk of rows; then dx = dz w and dw (+)= dz^T x.
 // Both are bound by the tensor cores under the board's power limit.  21504 rows x 1024 x 32000: forward 0.99 - 1.1 ms
 // (1280 - 1425 TFLOP/s), backward 4.4 - 4.9 ms; 16 rows x 2048 x 32000 forward: 27 us, of which w (131 MB) takes 20.
-// Roundings to fewer bits: d z enters dx in bf16, its largest entry, the target's, corrected by what that leaves (corr w[tok],
-// added before dx is rounded): error 1.66e-3 of dx's norm, the rounding of the result itself, where it was 2.4e-3 without.
+// Roundings to fewer bits: d z enters dx in bf16, the target's entry corrected by what that leaves (corr w[tok], added before
+// dx is rounded).  The rounding of the result itself is 1.66e-3 of dx's norm.  Where the policy is flat (logits of spread 1.5)
+// the target carries d z and the error stays there; where another token carries as much, its rounding shows: 1.8e-3 at spread 4,
+// 1.9 - 2.05e-3 at 8 to 20 (701 x 1024 x 5003; worst row 3.1e-3, of a rounded exact result 1.8e-3).  GRPO_EXACT_DX takes
+// d z as hi + lo here too: 1.66e-3 everywhere, for a fifth product (21504 x 1024 x 32000: 6.6 ms instead of 5.3).
 // dw is fp32, so its d z enters as hi + lo, two bf16 values, 16 significant bits, and the
 // target's d z, mostly the largest of its row, apart: coef x summed by token in fp32 (embed_accumulate_sum).  Relative to
 // dw's norm that leaves 0.8e-6 (701 rows x 1024 x 5003) and 0.35e-6 (8192 x 1024 x 32000), where fp32 products leave 0.5e-6
@@ -246,10 +249,10 @@ extern "C" int grpo_head_logp_bwd(const void* x, int64_t ld_x, int32_t n_rows, i
                                   const float* dlogp, const float* dentropy, int32_t chunk_rows, uint32_t flags, void* dx,
                                   int64_t ld_dx, float* dw, uint32_t* device_status, void* workspace, size_t workspace_bytes,
                                   pcm_stream stream) {
-  if (n_rows < 0 || d < 1 || vocab < 1 || chunk_rows < 1 || !vocab_temperature_ok(temperature) || (flags & ~GRPO_ACCUMULATE)) return PCM_ERR_ARG;
+  if (n_rows < 0 || d < 1 || vocab < 1 || chunk_rows < 1 || !vocab_temperature_ok(temperature) || (flags & ~(GRPO_ACCUMULATE | GRPO_EXACT_DX))) return PCM_ERR_ARG;
   if (!head_shape_ok(ld_x, ld_w, d, n_rows, vocab) || (dx && ld_dx % 8)) return PCM_ERR_SHAPE;
   if ((!dx && !dw) || (dx && (((uintptr_t)dx & 15) || ld_dx < d)) || (dw && ((uintptr_t)dw & 15))) return PCM_ERR_ARG;
-  const bool accumulate = flags & GRPO_ACCUMULATE;
+  const bool accumulate = flags & GRPO_ACCUMULATE, exact_dx = dx && (flags & GRPO_EXACT_DX);
   cudaStream_t s = (cudaStream_t)stream;
   if (n_rows == 0) {
     if (dw && !accumulate) PCM_CUDA_TRY(cudaMemsetAsync(dw, 0, (size_t)vocab * d * sizeof(float), s));
@@ -288,8 +291,8 @@ extern "C" int grpo_head_logp_bwd(const void* x, int64_t ld_x, int32_t n_rows, i
     z.epi.status = device_status;
     VocabHeadArgs& v = z.epi.vh;
     v.tok = tok + r0; v.inv_t = inv_t; v.lse = lse + r0; v.dlogp = dlogp + r0; v.vocab = vocab; v.dz_lo = lo;
-    v.coef = dw ? coef : nullptr;
-    v.corr = dx ? corr : nullptr;
+    v.coef = dw || exact_dx ? coef : nullptr;
+    v.corr = dx && !exact_dx ? corr : nullptr;
     v.dent = dentropy ? dentropy + r0 : nullptr;
     v.entropy = dentropy ? entropy + r0 : nullptr;
     prof_begin(gemm_class(rows, 256), s);
@@ -301,10 +304,14 @@ extern "C" int grpo_head_logp_bwd(const void* x, int64_t ld_x, int32_t n_rows, i
       q.epi.kind = EPI_CHAIN;                  // bf16 result: one accumulator piece
       q.epi.status = device_status;
       q.epi.vh.tok = tok + r0; q.epi.vh.vocab = vocab; q.epi.vh.corr = corr;
+      if (exact_dx) {                          // hi + lo, which cancel at the targets: all of their d z is added in fp32
+        q.A2 = lo; q.lda2 = pl.ldz; q.B2 = w_h; q.ldb2 = ld_w; q.K2 = vocab;
+        q.epi.vh.corr = coef;
+      }
       q.epi.vh.w = (const __nv_bfloat16*)w_h; q.epi.vh.ld_w = ld_w;
       prof_begin(gemm_class(rows, d), s);
       rc = chain_gemm(q, parts, s);
-      prof_end(s, flops, 2.0 * rows * vocab + 2.0 * vocab * d + 2.0 * rows * d);
+      prof_end(s, exact_dx ? 2.0 * flops : flops, (exact_dx ? 4.0 : 2.0) * rows * vocab + 2.0 * vocab * d + 2.0 * rows * d);
       if (rc != PCM_OK) return rc;
     }
     if (dw) {

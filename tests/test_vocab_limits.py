@@ -1,7 +1,7 @@
 """Sizes and factors at the edge of what the vocabulary calls take, on the host: nothing is launched."""
 import pytest
 
-from tests.test_vocab_refusals import ARG, EMBED, HEAD, HEAD_BWD, LOGP, LOGP_BWD, SHAPE, _call
+from tests.test_vocab_refusals import ARG, EMBED, EMBED_BWD, HEAD, HEAD_BWD, LOGP, LOGP_BWD, SHAPE, _call
 
 WIDE = (1 << 30) + 8
 
@@ -29,3 +29,12 @@ def test_temperatures_whose_factors_are_infinite_are_refused(name, base):
         assert _call(name, base, temperature=t, n_rows=0) == ARG
     for t in (4.3e-39, 1e-3, 1.0, 1e30, 3.4028e38):
         assert _call(name, base, temperature=t, n_rows=0, **({"dw": None} if "dw" in base else {})) == 0
+
+
+def test_flags_of_the_head_gradient():
+    from paper_2605_16154_b200 import binding as B
+    for flags in (0, B.GRPO_ACCUMULATE, B.GRPO_EXACT_DX, B.GRPO_ACCUMULATE | B.GRPO_EXACT_DX):
+        assert _call("grpo_head_logp_bwd", HEAD_BWD, n_rows=0, dw=None, flags=flags) == 0
+    for flags in (1, 4, 12, 16, 1 << 31):
+        assert _call("grpo_head_logp_bwd", HEAD_BWD, n_rows=0, dw=None, flags=flags) == ARG
+    assert _call("grpo_embed_bwd", EMBED_BWD, flags=B.GRPO_EXACT_DX) == ARG

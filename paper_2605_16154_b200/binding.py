@@ -462,12 +462,19 @@ def grpo_actor_fwd_bwd(model: Model, packed: Packed, eps_low: float = 0.2, eps_h
 _DTYPES = {torch.float32: GRPO_F32, torch.bfloat16: GRPO_BF16}
 PCM_MAX_TOP = 16
 STATUS_BAD_TOKEN = 32
+_INT32_MAX = 0x7FFFFFFF
 _f32, _i32, _u8 = torch.float32, torch.int32, torch.uint8
 
 
 def _require(call: str, ok: bool, code: int = -1) -> None:
     if not ok:
         raise PcmError(call, code)
+
+
+def _size(call: str, *sizes: int) -> None:
+    """Sizes that the C interface takes as int32: ctypes would cut larger ones to their low half."""
+    if max(sizes) > _INT32_MAX or min(sizes) < -_INT32_MAX:
+        raise PcmError(call, -2)
 
 
 def _matrix(call: str, t: torch.Tensor, device=None):
@@ -481,6 +488,8 @@ def _matrix(call: str, t: torch.Tensor, device=None):
     # rows that overlap (an expanded view) are refused
     if dt is None or ld < c or (step != 1 and c > 1 and n):
         raise PcmError(call, -1)
+    if n > _INT32_MAX or c > _INT32_MAX:
+        raise PcmError(call, -2)
     return dt, t.data_ptr(), ld, n, c
 
 
@@ -521,6 +530,7 @@ def grpo_embed(table: torch.Tensor, tok: torch.Tensor, scale: float = 1.0, out: 
     call = "grpo_embed"
     dt, tp, ld, vocab, d = _matrix(call, table)
     dev, n = table.device, tok.numel()
+    _require(call, n <= _INT32_MAX, -2)
     if out is None:
         out = torch.empty((n, d), dtype=table.dtype, device=dev)
         op, ldo = out.data_ptr(), d
@@ -533,6 +543,7 @@ def grpo_embed(table: torch.Tensor, tok: torch.Tensor, scale: float = 1.0, out: 
 
 
 def grpo_embed_workspace_bytes(n: int, vocab: int, d: int) -> int:
+    _size("grpo_embed_workspace_bytes", n, vocab, d)
     return int(_lib.grpo_embed_workspace_bytes(n, vocab, d))
 
 
@@ -544,6 +555,7 @@ def grpo_embed_bwd(dout: torch.Tensor, tok: torch.Tensor, vocab: int, scale: flo
     dt, dp, ld, n, d = _matrix(call, dout)
     dev = dout.device
     tk = _vector(call, tok, dev, _i32, n)
+    _size(call, vocab, 0)
     _require(call, tk is not None and (grad is not None or not accumulate))
     need = _lib.grpo_embed_workspace_bytes(n, vocab, d)
     _require("grpo_embed_workspace_bytes", need > 0, -2)
@@ -573,6 +585,7 @@ def grpo_token_logp(logits: torch.Tensor, tok: Optional[torch.Tensor], temperatu
     dt, zp, ld, n, vocab = _matrix(call, logits)
     dev = logits.device
     tk = _vector(call, tok, dev, _i32, n)
+    _size(call, top, 0)
     logp = lp = top_id = ip = top_logp = tp = None
     if tok is not None:
         logp, lp = _out(call, out, "logp", n, n, _f32, dev)
@@ -607,6 +620,7 @@ def grpo_token_logp_bwd(logits: torch.Tensor, tok: torch.Tensor, lse: torch.Tens
 
 
 def grpo_head_logp_workspace_bytes(n: int, d: int, vocab: int) -> int:
+    _size("grpo_head_logp_workspace_bytes", n, d, vocab)
     return int(_lib.grpo_head_logp_workspace_bytes(n, d, vocab))
 
 
@@ -642,6 +656,7 @@ HEAD_CHUNK_BYTES = 4 << 30
 
 
 def grpo_head_logp_bwd_workspace_bytes(n: int, d: int, vocab: int, chunk_rows: int) -> int:
+    _size("grpo_head_logp_bwd_workspace_bytes", n, d, vocab, chunk_rows)
     return int(_lib.grpo_head_logp_bwd_workspace_bytes(n, d, vocab, chunk_rows))
 
 
@@ -659,6 +674,7 @@ def grpo_head_logp_bwd(x: torch.Tensor, w_h: torch.Tensor, tok: torch.Tensor, ls
     dev = x.device
     _require(call, tok is not None and lse is not None and dlogp is not None)
     _require(call, chunk_rows >= 0 and (dw is not None or not accumulate))
+    _require(call, chunk_rows <= _INT32_MAX, -2)
     if chunk_rows == 0:
         chunk_rows = max(256, HEAD_CHUNK_BYTES // (4 * max(1, vocab)) // 256 * 256)
     need = _lib.grpo_head_logp_bwd_workspace_bytes(n, d, vocab, chunk_rows)

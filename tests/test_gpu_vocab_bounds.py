@@ -126,3 +126,19 @@ def test_embedding_with_scale_one_copies_bits(kind, ints, d, gap):
     out = B().grpo_embed(table, tok).view(ints)
     want = torch.where((tok >= 0)[:, None], bits[:, :d][tok.clamp(min=0).long()], 0)
     assert torch.equal(out, want)
+
+
+def test_sizes_beyond_32_bits_are_refused():
+    """2^32 + k rows or tokens would arrive as k."""
+    b, far = B(), (1 << 32) + 3
+    few = torch.zeros(4, dtype=torch.int32, device="cuda")
+    m = torch.zeros(4, 8, device="cuda")
+    x, w, v = m.bfloat16(), torch.zeros(20, 8, device="cuda").bfloat16(), torch.zeros(4, device="cuda")
+    long = torch.empty(far, 1, dtype=torch.bfloat16, device="cuda")             # nothing reads or writes these
+    many = torch.empty(far, dtype=torch.int32, device="cuda")
+    for f in (lambda: b.grpo_embed_bwd(m, few, far), lambda: b.grpo_embed(long, few), lambda: b.grpo_embed(m, many, out=m),
+              lambda: b.grpo_token_logp(long, many), lambda: b.grpo_token_logp(long.t(), few[:1]), lambda: b.grpo_token_logp(m, few, top=(1 << 32) + 2),
+              lambda: b.grpo_head_logp_bwd(x, w, few, v, v, v, chunk_rows=far)):
+        with pytest.raises(b.PcmError) as e:
+            f()
+        assert e.value.code == -2

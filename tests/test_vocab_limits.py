@@ -38,3 +38,17 @@ def test_flags_of_the_head_gradient():
     for flags in (1, 4, 12, 16, 1 << 31):
         assert _call("grpo_head_logp_bwd", HEAD_BWD, n_rows=0, dw=None, flags=flags) == ARG
     assert _call("grpo_embed_bwd", EMBED_BWD, flags=B.GRPO_EXACT_DX) == ARG
+
+
+def test_the_binding_refuses_sizes_that_do_not_fit_the_interface():
+    """The C interface takes int32: what ctypes would cut to its low half is refused, not computed for another size."""
+    from paper_2605_16154_b200 import binding as B
+    far = 1 << 32
+    for f in (lambda: B.grpo_embed_workspace_bytes(far + 5, 10, 8), lambda: B.grpo_embed_workspace_bytes(5, far + 10, 8),
+              lambda: B.grpo_embed_workspace_bytes(5, 10, far + 8), lambda: B.grpo_head_logp_workspace_bytes(far + 5, 64, 100),
+              lambda: B.grpo_head_logp_workspace_bytes(5, 64, 100 - far), lambda: B.grpo_head_logp_bwd_workspace_bytes(5, 64, far + 100, 5),
+              lambda: B.grpo_head_logp_bwd_workspace_bytes(5, 64, 100, far + 5), lambda: B.grpo_head_logp_bwd_workspace_bytes(5, 64, 100, 1 << 31)):
+        with pytest.raises(B.PcmError) as e:
+            f()
+        assert e.value.code == SHAPE
+    assert B.grpo_embed_workspace_bytes(5, 10, 8) > 0 and B.grpo_embed_workspace_bytes(-1, 10, 8) == 0

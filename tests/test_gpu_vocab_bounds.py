@@ -142,3 +142,69 @@ def test_sizes_beyond_32_bits_are_refused():
         with pytest.raises(b.PcmError) as e:
             f()
         assert e.value.code == -2
+
+
+# ---- captured calls at sizes beyond the short kernels --------------------------------------------------------------------
+def replays_follow(step, refill):
+    """Captures step(), then replays it twice on refilled inputs; the results are those of the same calls made directly."""
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held = step()
+    for seed in (1, 2):
+        refill(seed)
+        graph.replay()
+        torch.cuda.synchronize()
+        for p, q in zip(held, step()):
+            assert torch.equal(p, q)
+
+
+@pytest.mark.parametrize("n,vocab,d", [(3000, 70001, 40), (9472, 300, 16), (20011, 1000, 136)])
+def test_captured_embedding_gradients_of_long_batches(n, vocab, d):
+    """The radix sort of two and three passes, tokens over many tiles."""
+    b = B()
+    dout, tok = torch.randn(n, d, generator=gen(n), device="cuda"), late_tokens(n, vocab, n)
+    grad = torch.zeros(vocab, d, device="cuda")
+
+    def step():
+        grad.fill_(0.5)
+        return b.grpo_embed_bwd(dout, tok, vocab, 0.7), b.grpo_embed_bwd(dout, tok, vocab, grad=grad, accumulate=True).clone()
+
+    def refill(seed):
+        dout.copy_(torch.randn(n, d, generator=gen(seed), device="cuda"))
+        tok.copy_(torch.randint(-1, vocab, (n,), generator=gen(seed), device="cuda", dtype=torch.int32))
+    replays_follow(step, refill)
+
+
+def test_captured_head_gradients_in_chunks_on_both_sides_of_the_plans():
+    b, n, d, vocab = B(), 12000, 64, 700
+    x, w = torch.randn(n, d, generator=gen(1), device="cuda").bfloat16(), (torch.randn(vocab, d, generator=gen(2), device="cuda") * 0.2).bfloat16()
+    tok, a = late_tokens(n, vocab, 5), torch.randn(n, generator=gen(3), device="cuda")
+
+    def step():
+        logp, ent, lse = b.grpo_head_logp(x, w, tok)
+        return (logp, ent, lse) + b.grpo_head_logp_bwd(x, w, tok, lse, ent, a, a, chunk_rows=9500) + \
+            b.grpo_head_logp_bwd(x, w, tok, lse, ent, a, None, chunk_rows=2500, exact_dx=True)
+
+    def refill(seed):
+        x.copy_(torch.randn(n, d, generator=gen(seed), device="cuda"))
+        tok.copy_(late_tokens(n, vocab, seed + 40))
+    replays_follow(step, refill)
+
+
+def test_captured_log_probabilities_of_many_and_of_few_rows():
+    b = B()
+    many, few = torch.randn(1300, 3001, generator=gen(1), device="cuda").bfloat16(), torch.randn(3, 50001, generator=gen(2), device="cuda")
+    t1, t2 = late_tokens(1300, 3001, 3), torch.tensor([5, 50000, -1], dtype=torch.int32, device="cuda")
+
+    def step():
+        return b.grpo_token_logp(many, t1, 0.8, 5) + b.grpo_token_logp(few, t2, 1.3, 16)
+
+    def refill(seed):
+        many.copy_(torch.randn(1300, 3001, generator=gen(seed), device="cuda"))
+        few.copy_(torch.randn(3, 50001, generator=gen(seed + 9), device="cuda"))
+    replays_follow(step, refill)

@@ -530,7 +530,8 @@ def grpo_embed(table: torch.Tensor, tok: torch.Tensor, scale: float = 1.0, out: 
     call = "grpo_embed"
     dt, tp, ld, vocab, d = _matrix(call, table)
     dev, n = table.device, tok.numel()
-    _require(call, n <= _INT32_MAX, -2)
+    if n > _INT32_MAX:
+        raise PcmError(call, -2)
     if out is None:
         out = torch.empty((n, d), dtype=table.dtype, device=dev)
         op, ldo = out.data_ptr(), d
@@ -555,7 +556,8 @@ def grpo_embed_bwd(dout: torch.Tensor, tok: torch.Tensor, vocab: int, scale: flo
     dt, dp, ld, n, d = _matrix(call, dout)
     dev = dout.device
     tk = _vector(call, tok, dev, _i32, n)
-    _size(call, vocab, 0)
+    if not 0 < vocab <= _INT32_MAX:
+        raise PcmError(call, -2)
     _require(call, tk is not None and (grad is not None or not accumulate))
     need = _lib.grpo_embed_workspace_bytes(n, vocab, d)
     _require("grpo_embed_workspace_bytes", need > 0, -2)
@@ -585,7 +587,6 @@ def grpo_token_logp(logits: torch.Tensor, tok: Optional[torch.Tensor], temperatu
     dt, zp, ld, n, vocab = _matrix(call, logits)
     dev = logits.device
     tk = _vector(call, tok, dev, _i32, n)
-    _size(call, top, 0)
     logp = lp = top_id = ip = top_logp = tp = None
     if tok is not None:
         logp, lp = _out(call, out, "logp", n, n, _f32, dev)
@@ -594,6 +595,8 @@ def grpo_token_logp(logits: torch.Tensor, tok: Optional[torch.Tensor], temperatu
     if 0 < top <= PCM_MAX_TOP:                                # a larger one is refused by the call
         top_id, ip = _out(call, out, "top_id", (n, top), n * top, _i32, dev)
         top_logp, tp = _out(call, out, "top_logp", (n, top), n * top, _f32, dev)
+    elif top:
+        _size(call, top, 0)
     _launch(call, dev, _lib.grpo_token_logp, dt, zp, ld, n, vocab, tk, temperature, top, lp, ep, sp, ip, tp,
             _vector(call, status, dev, _i32, 1))
     return logp, entropy, lse, top_id, top_logp

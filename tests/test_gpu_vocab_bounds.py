@@ -208,3 +208,66 @@ def test_captured_log_probabilities_of_many_and_of_few_rows():
         many.copy_(torch.randn(1300, 3001, generator=gen(seed), device="cuda"))
         few.copy_(torch.randn(3, 50001, generator=gen(seed + 9), device="cuda"))
     replays_follow(step, refill)
+
+
+# ---- outputs inside larger buffers: what lies around and between their rows stays ----------------------------------------
+def inside(shape, dtype, shift, gap=0, fill=55):
+    """An output of `shape` (rows `gap` elements apart) starting `shift` elements into a buffer of `fill`, and a check that only
+    the output was written."""
+    rows, cols = (1, shape[0]) if len(shape) == 1 else shape
+    ld = cols + gap
+    buf = torch.full((shift + rows * ld + 64,), fill, dtype=dtype, device="cuda")
+    view = buf[shift:shift + rows * ld].view(rows, ld)[:, :cols]
+
+    def only():
+        left = torch.ones_like(buf, dtype=torch.bool)
+        left[shift:shift + rows * ld].view(rows, ld)[:, :cols] = False
+        return bool((buf[left] == fill).all())
+    return (view[0] if len(shape) == 1 else view), only
+
+
+@pytest.mark.parametrize("n,vocab,d,shift", [(50, 33, 24, 1), (3000, 300, 40, 3), (700, 9, 129, 2), (12000, 77, 16, 4)])
+def test_embedding_gradient_writes_its_table_only(n, vocab, d, shift):
+    b = B()
+    dout, tok = torch.randn(n, d, generator=gen(n), device="cuda").bfloat16(), late_tokens(n, vocab, n)
+    flat, only = inside((vocab * d,), torch.float32, shift)
+    b.grpo_embed_bwd(dout, tok, vocab, 0.5, grad=flat.view(vocab, d))
+    assert only()
+    t = tok.cpu().numpy()
+    want, mass = vo.embed_bwd(host(dout), t, vocab, 0.5), vo.embed_bwd(np.abs(host(dout)), t, vocab, 0.5)
+    k = np.bincount(t[t >= 0].astype(np.int64), minlength=vocab)[:, None]
+    assert np.all(np.abs(host(flat.view(vocab, d)) - want) <= (k + 2) * U * mass + 2 * U * np.abs(want))
+
+
+@pytest.mark.parametrize("kind", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("n,vocab,gap,shift", [(3, 50, 3, 1), (9, 1500, 1, 2), (1300, 1100, 0, 5), (2, 40003, 5, 7)])
+def test_log_probabilities_write_their_outputs_only(kind, n, vocab, gap, shift):
+    b, top = B(), 5
+    z, tok = torch.randn(n, vocab, generator=gen(n), device="cuda").to(kind), late_tokens(n, vocab, vocab)
+    want = b.grpo_token_logp(z, tok, 1.0, top)
+    made = {k: inside((n,), torch.float32, shift) for k in ("logp", "entropy", "lse")}
+    made["top_id"], made["top_logp"] = inside((n * top,), torch.int32, shift), inside((n * top,), torch.float32, shift)
+    b.grpo_token_logp(z, tok, 1.0, top, out={k: v[0] for k, v in made.items()})
+    for (t, only), w in zip(made.values(), want):
+        assert only() and torch.equal(t, w.reshape(-1))
+    a = torch.randn(n, generator=gen(3), device="cuda")
+    near = b.grpo_token_logp_bwd(z, tok, want[2], want[1], a, a)
+    out, only = inside((n, vocab), kind, shift, gap)
+    b.grpo_token_logp_bwd(z, tok, want[2], want[1], a, a, dlogits=out)
+    assert only() and torch.equal(out, near)
+
+
+@pytest.mark.parametrize("n,d,vocab", [(3, 64, 77), (300, 72, 515), (700, 256, 40)])
+def test_head_gradients_write_their_outputs_only(n, d, vocab):
+    b = B()
+    x, w = torch.randn(n, d, generator=gen(n), device="cuda").bfloat16(), (torch.randn(vocab, d, generator=gen(d), device="cuda") * 0.2).bfloat16()
+    tok, a = late_tokens(n, vocab, n), torch.randn(n, generator=gen(1), device="cuda")
+    got = {k: inside((n,), torch.float32, 3) for k in ("logp", "entropy", "lse")}
+    logp, ent, lse = b.grpo_head_logp(x, w, tok, out={k: v[0] for k, v in got.items()})
+    assert all(only() for _, only in got.values())
+    for exact in (False, True):
+        dx, dw = b.grpo_head_logp_bwd(x, w, tok, lse, ent, a, a, exact_dx=exact)
+        dx1, only_dx = inside((n, d), torch.bfloat16, 8, 16)
+        dw1, only_dw = inside((vocab * d,), torch.float32, 4)
+        b.grpo_head_logp_bwd(x, w, tok, lse, ent, a, a, dx=dx1, dw=dw1.view(vocab, d), exact_dx=exact)
+        assert only_dx() and only_dw() and torch.equal(dx1, dx) and torch.equal(dw1.view(vocab, d), dw)

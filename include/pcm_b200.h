@@ -395,9 +395,9 @@ int grpo_embed(int32_t dtype, const void* table, int64_t ld_table, int32_t vocab
 /* Its gradient: grad[v] = scale * sum over {i : tok[i] = v} of dout[i] in fp32 for every v < vocab (0 for tokens that
  * do not occur); with GRPO_ACCUMULATE in flags it is added to grad.  dout [n][d] of `dtype`, grad [vocab][d] fp32,
  * contiguous.  Tokens are sorted first; the rows of a token are summed in ascending i within tiles of 8 or 32 sorted
- * rows, the tiles of a frequent token in an order that depends on its rows alone.  d <= PCM_MAX_EMBED_DIM.  workspace: device, 256-byte aligned,
- * >= grpo_embed_workspace_bytes() (0 when the sizes are not supported), which
- * never falls as n grows: a workspace for the longest batch serves shorter ones. */
+ * rows, the tiles of a frequent token in an order that follows from where they lie among all sorted rows.
+ * d <= PCM_MAX_EMBED_DIM.  workspace: device, 256-byte aligned, >= grpo_embed_workspace_bytes() (0 when the sizes are not
+ * supported), which never falls as n grows: a workspace for the longest batch serves shorter ones. */
 size_t grpo_embed_workspace_bytes(int32_t n, int32_t vocab, int32_t d);
 int grpo_embed_bwd(int32_t dtype, const void* dout, int64_t ld_dout, const int32_t* tok, int32_t n, int32_t vocab, int32_t d,
                    float scale, uint32_t flags, float* grad, uint32_t* device_status, void* workspace, size_t workspace_bytes,
@@ -417,8 +417,9 @@ int grpo_token_logp(int32_t dtype, const void* logits, int64_t ld, int32_t n_row
 /* Gradient of a loss with d loss / d logp = dlogp [n_rows] and d loss / d entropy = dentropy [n_rows] (may be NULL):
  *     dlogits_v = (1 / temperature) (dlogp (1[v = tok] - p_v) - dentropy p_v (log p_v + entropy))
  * lse and entropy (needed with dentropy) are those of the forward call; p = exp(z - lse) inherits the rounding of lse,
- * |lse| 2^-24 of its value.  dlogits is of `dtype`, with its own row
- * stride; it may be the logits themselves (same pointer, same stride).  A row whose lse is -inf gets zeros. */
+ * |lse| 2^-24 of its value, so a row of nothing but the type's lowest value (a mask that leaves nothing, not written as -inf)
+ * has no meaningful p: give it a token below 0.  dlogits is of `dtype`, with its own row stride; it may be the logits themselves
+ * (same pointer, same stride).  A row whose lse is -inf gets zeros. */
 int grpo_token_logp_bwd(int32_t dtype, const void* logits, int64_t ld, int32_t n_rows, int32_t vocab, const int32_t* tok,
                         float temperature, const float* lse, const float* entropy, const float* dlogp, const float* dentropy,
                         void* dlogits, int64_t ld_dlogits, uint32_t* device_status, pcm_stream stream);
@@ -441,8 +442,9 @@ int grpo_head_logp(const void* x, int64_t ld_x, int32_t n_rows, int32_t d, const
  *     dw = dlogits^T x  (fp32 [vocab][d], contiguous, 16-byte aligned; GRPO_ACCUMULATE in flags adds to it), from dlogits
  *                       as a sum of two bf16 values, the targets' own in fp32
  * Either may be NULL.  x may hold anything, NaN too, in rows without a token.  The rows are processed chunk_rows (>= 1) at
- * a time, which sizes the workspace (about 2 d + 4 vocab bytes a row, 5 a token and a constant); the results differ between chunk sizes
- * by fp32 rounding only.  For a tied embedding pass its fp32 gradient as dw with GRPO_ACCUMULATE. */
+ * a time, which sizes the workspace: a row of a chunk takes 2 d + 4 vocab bytes, 24 for its factors and its token's sort and d / 4
+ * for partial sums of the targets (d up to 9472 rows), a token of the vocabulary 5, and the parts of split products 19 MB.  Between chunk
+ * sizes dw differs by fp32 rounding, dx by at most a rounding to the neighbouring bf16 value.  For a tied embedding pass its fp32 gradient as dw with GRPO_ACCUMULATE. */
 size_t grpo_head_logp_bwd_workspace_bytes(int32_t n_rows, int32_t d, int32_t vocab, int32_t chunk_rows);
 int grpo_head_logp_bwd(const void* x, int64_t ld_x, int32_t n_rows, int32_t d, const void* w_h, int64_t ld_w, int32_t vocab,
                        const int32_t* tok, float temperature, const float* lse, const float* entropy, const float* dlogp,

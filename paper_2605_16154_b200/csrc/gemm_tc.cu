@@ -675,7 +675,9 @@ __device__ __forceinline__ void epi_tile(const TcParams& p, uint32_t tmem_acc, i
       }
 }
 
-// EPI_CHAIN: one accumulator piece into the running sums of this thread's row, and the finished tile out to memory.
+// EPI_CHAIN: one accumulator piece into the running sums of this thread's row, and the finished tile out to memory.  With
+// 256-column tiles the 128 sums and what the store needs beside them pass the 168 registers a thread: about 80 bytes are
+// spilled and 350 read back, once a tile.
 template <int BN>
 __device__ __forceinline__ void chain_add(uint32_t tmem_acc, int chalf, float (&sum)[BN / 2]) {
 #pragma unroll

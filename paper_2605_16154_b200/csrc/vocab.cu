@@ -49,8 +49,8 @@ template <> __device__ __forceinline__ __nv_bfloat16 from_f32<__nv_bfloat16>(flo
 // Embedding lookup: out[i] = round(scale * table[tok[i]]); rows of a token outside [0, vocab) are zero.  COPY (scale 1) moves
 // bits: a NaN keeps its payload, which a product and a conversion would change.
 // Bound by HBM (each distinct row read once, every output row written once); a block holds 256 / tpr rows, tpr
-// threads walk one row in 16-byte steps, four loads in flight each.  119808 rows of 1024 bf16 from 32000: 46 us, 6.7 TB/s;
-// 64 rows of 2048: 2 us.
+// threads walk one row in 16-byte steps, four loads in flight each.  119808 rows of 1024 bf16 from 32000: 46 - 48 us, 6.5 - 6.7
+// TB/s; 64 rows of 2048: 1.5 us.
 // ------------------------------------------------------------------------------------------------
 template <typename T, bool VEC, bool COPY>
 __global__ void __launch_bounds__(256)
@@ -105,7 +105,7 @@ embed_kernel(const T* __restrict__ table, long long ld_table, int vocab, int d, 
 //      between tiles leaves a partial sum per tile;
 //   3. embed_join_kernel: the partial sums of those tokens, in an order that depends on the token's tiles alone.
 // Every sum has a fixed order: the same inputs give the same bits.  Bound by HBM: dout once, grad once.  119808 rows of 1024
-// bf16 into 32000: 97 us against 58 us for the bytes; about 18 us are the four sort kernels, which are latency, 57 us the
+// bf16 into 32000: 98 - 100 us against 58 us for the bytes; about 18 us are the four sort kernels, which are latency, 57 us the
 // sums (5.6 TB/s) and the rest the joins and the rows of absent tokens.
 // ------------------------------------------------------------------------------------------------
 constexpr int EJ_WARPS = 16, EM_RING = 8, EM_LANES = 16;
@@ -629,8 +629,9 @@ constexpr int LP_MAX_TOP = PCM_MAX_TOP;
 constexpr int LP_MAX_RANKS = 8;
 
 // One pass over the logits, bound by HBM on many rows and next by the exponentials (one per element: 0.7 of the unit's rate
-// at 6 TB/s of bf16), by latency on few.  21504 rows of 32000 bf16: 219 us without a top list (6.3 TB/s), 257 us with
-// the top 4, 320 us with 16; 8 rows of 130011 with the top 8: 9.6 us.
+// at 6 TB/s of bf16), by latency on few.  21504 rows of 32000 bf16, calls back to back on the same logits: 213 us without a top
+// list (6.5 TB/s), 257 us with the top 4, 315 us with 16; on logits that change from call to call 286 us with the top 4.  8 rows
+// of 130011 with the top 8: 9.1 us.
 // NT threads work on one row's share.  NT = 32: a warp per row, several rows per block.  Otherwise one block per share,
 // `ranks` blocks of a cluster per row.
 template <int NT> struct LogpSmem {
@@ -1043,7 +1044,8 @@ struct LogpBwdParams {
   unsigned* status;
 };
 
-constexpr int LB_THREADS = 256, LB_VECS = 4;  // 10752 x 32000 bf16: 254 us with two vectors a thread, 221 with four
+constexpr int LB_THREADS = 256, LB_VECS = 4;  // 10752 x 32000 bf16: 254 us with two vectors a thread, 221 with four, in
+// calls back to back; 241 where the inputs change from call to call
 
 template <typename T, bool VEC>
 __global__ void __launch_bounds__(LB_THREADS)

@@ -5,13 +5,15 @@
 //             hundred rows on, by reading w below.
 //   backward  the same product once more, its epilogue writing d loss / d z in bf16 (rounded value and remainder) for a
 //             chunk of rows; then dx = dz w and dw (+)= dz^T x.
-// Both are bound by the tensor cores under the board's power limit.  21504 rows x 1024 x 32000: forward 0.99 - 1.1 ms
-// (1280 - 1425 TFLOP/s), backward 4.4 - 4.9 ms; 16 rows x 2048 x 32000 forward: 27 us, of which w (131 MB) takes 20.
+// Both are bound by the tensor cores under the board's power limit.  21504 rows x 1024 x 32000: forward 0.98 ms in calls back
+// to back and 1.15 ms on inputs that change from call to call (1430 and 1225 TFLOP/s), backward 4.5 and 5.35 ms; 16 rows x 2048 x
+// 32000 forward: 28 - 30 us, of which w (131 MB) takes 20.
 // Roundings to fewer bits: d z enters dx in bf16, the target's entry corrected by what that leaves (corr w[tok], added before
 // dx is rounded).  The rounding of the result itself is 1.66e-3 of dx's norm.  Where the policy is flat (logits of spread 1.5)
 // the target carries d z and the error stays there; where another token carries as much, its rounding shows: 1.8e-3 at spread 4,
 // 1.9 - 2.05e-3 at 8 to 20 (701 x 1024 x 5003; worst row 3.1e-3, of a rounded exact result 1.8e-3).  GRPO_EXACT_DX takes
-// d z as hi + lo here too: 1.66e-3 everywhere, for a fifth product (21504 x 1024 x 32000: 6.6 ms instead of 5.3).
+// d z as hi + lo here too: 1.66e-3 everywhere, for a fifth product (21504 x 1024 x 32000: 6.3 ms instead of 4.5 back to back,
+// 6.65 instead of 5.35 on changing inputs; 701 x 1024 x 5003: 98 us instead of 93).
 // dw is fp32, so its d z enters as hi + lo, two bf16 values, 16 significant bits, and the
 // target's d z, mostly the largest of its row, apart: coef x summed by token in fp32 (embed_accumulate_sum).  Relative to
 // dw's norm that leaves 0.8e-6 (701 rows x 1024 x 5003) and 0.35e-6 (8192 x 1024 x 32000), where fp32 products leave 0.5e-6

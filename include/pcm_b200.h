@@ -451,6 +451,102 @@ int grpo_head_logp_bwd(const void* x, int64_t ld_x, int32_t n_rows, int32_t d, c
                        const float* dentropy, int32_t chunk_rows, uint32_t flags, void* dx, int64_t ld_dx, float* dw,
                        uint32_t* device_status, void* workspace, size_t workspace_bytes, pcm_stream stream);
 
+/* ---- the rollout side: rotary positions, a paged cache and attention over it ---------------------------------
+ * The actor update above knows positions 0 .. S-1 of one chunk and attends inside it.  The policy that produces the rollouts
+ * (and scores them as the behaviour policy) goes on from chunk to chunk: its tokens stand at any position, their keys and
+ * values stay in a cache, and it brings a prefix of new tokens or a single one at a time.  These calls need no context.
+ * The conventions of the vocabulary section on device_status, strides, workspaces, graphs and empty calls hold here too;
+ * the bits of device_status are: bit 0 a bounded wait expired; bit 6 (value 64) a page index outside the cache, whose keys
+ * and values read as zeros and are not written; bit 7 (value 128) a length or row offset that does not fit the sizes of the
+ * call: a length is clipped to what the table can hold, a sequence whose offsets do not fit has no rows. */
+enum { GRPO_ROTARY_PLAIN = 0, GRPO_ROTARY_LINEAR = 1, GRPO_ROTARY_BASE = 2, GRPO_ROTARY_PARTS = 3 };
+#define GRPO_ROTARY_INTERLEAVED 1u  /* pairs (2 i, 2 i + 1); otherwise (i, i + rot_dim / 2)                                */
+#define GRPO_ROTARY_INVERSE 2u      /* the opposite rotation: the gradient (grpo_rotary only)                              */
+#define PCM_MAX_ROTARY_DIM 1024     /* elements of a head that grpo_rotary and grpo_rotary_cache take                      */
+
+/* Frequencies of the rot_dim / 2 pairs, in turns per position, and the factor on the rotated values (host, no GPU work).
+ * f_i = base^(-2 i / rot_dim) / (2 pi), then
+ *   GRPO_ROTARY_PLAIN   as they are
+ *   GRPO_ROTARY_LINEAR  f_i / factor: positions are squeezed
+ *   GRPO_ROTARY_BASE    of the base factor^(rot_dim / (rot_dim - 2)) base: the slowest pair is squeezed by factor, the fastest
+ *                       keeps its frequency (rot_dim >= 4)
+ *   GRPO_ROTARY_PARTS   f_i (k + (1 - k) / factor), k = clamp((original_len f_i - low) / (high - low), 0, 1): pairs that make
+ *                       high turns or more within original_len keep their frequency, those below low are squeezed
+ * (factor, low, high and original_len are read by the kinds that name them).  *amplitude is 1, or 0.1 ln(factor) + 1 with
+ * GRPO_ROTARY_PARTS. */
+typedef struct {
+  int32_t rot_dim;             /* even, 2 .. PCM_MAX_ROTARY_DIM                                   */
+  int32_t scaling;             /* GRPO_ROTARY_PLAIN ..                                            */
+  double base;                 /* > 0                                                             */
+  double factor;               /* >= 1                                                            */
+  double original_len;         /* > 0                                                             */
+  double low, high;            /* low < high                                                      */
+} grpo_rotary_cfg;
+int grpo_rotary_freqs(const grpo_rotary_cfg* cfg, double* turns, float* amplitude);
+
+/* out[r][h] = amplitude R(pos[r]) x[r][h] on the first rot_dim elements of a head, the others as they are; with
+ * GRPO_ROTARY_INVERSE in flags amplitude R(-pos[r]), which is also the gradient d x of d out.  Pair i turns by the angle
+ * 2 pi pos turns[i], formed in 64 bits; the products are formed in fp32 and rounded once.
+ * x and out: [n][n_heads][head_dim] of `dtype`, rows ld_* and heads ld_*_head elements apart; out may be x itself (same pointer
+ * and strides), but not overlap it otherwise.  pos: device int32 [n]; turns: device double [rot_dim / 2]. */
+int grpo_rotary(int32_t dtype, const void* x, int64_t ld_x, int64_t ld_x_head, int32_t n, int32_t n_heads, int32_t head_dim,
+                int32_t rot_dim, const double* turns, float amplitude, const int32_t* pos, uint32_t flags, void* out, int64_t ld_out,
+                int64_t ld_out_head, pcm_stream stream);
+
+/* A cache of keys and values in pages of page_size tokens: token slot j of head h of page i starts at element
+ * i ld_page + j ld_slot + h ld_head of k and of v, and its head_dim elements are contiguous.  k and v start on 16-byte
+ * boundaries and their strides are multiples of 16 bytes (PCM_ERR_SHAPE otherwise); page_size is a multiple of 8. */
+typedef struct {
+  int32_t dtype;               /* grpo_dtype                                                      */
+  int32_t n_pages, page_size, n_kv_heads, head_dim;
+  int32_t reserved;
+  void* k;
+  void* v;
+  int64_t ld_page, ld_slot, ld_head;
+} grpo_kv_cache;
+
+/* The sequences of one call (device arrays).  Sequence s holds seq_len[s] tokens, the new ones of this call included: its
+ * token j is in slot j % page_size of page page_table[s][j / page_size].  Its new tokens are rows q_off[s] .. q_off[s+1]-1
+ * of the call, the last one at position seq_len[s] - 1.  q_off = NULL: one new token each (n_rows = n_seq).  Rows before the
+ * first sequence's and behind the last one's are neither read nor written.  Entries of the table that no row of a call sees
+ * may hold anything. */
+typedef struct {
+  int32_t n_seq;
+  int32_t max_pages;           /* entries in a row of the table                                   */
+  const int32_t* page_table;   /* [n_seq][max_pages], rows ld_table apart                         */
+  int64_t ld_table;
+  const int32_t* seq_len;      /* [n_seq]                                                         */
+  const int32_t* q_off;        /* [n_seq + 1] ascending, or NULL                                  */
+} grpo_kv_batch;
+
+/* New tokens enter the cache: their keys, rotated, and their values go to their slots, their rotated queries to q_out.
+ * q [n_rows][n_heads][head_dim], k and v [n_rows][n_kv_heads][head_dim] of the cache's type, with row and head strides each
+ * (views of one fused projection, say); q_out likewise, or q itself.  Rotation as grpo_rotary (INTERLEAVED in flags), at
+ * the token's position, or at pos[row] where pos is not NULL; rot_dim = 0 rotates nothing (turns is not read).
+ * q = NULL with n_heads = 0: keys and values only.  Slots that two tokens share hold either one's values. */
+int grpo_rotary_cache(const grpo_kv_cache* cache, const grpo_kv_batch* batch, int32_t n_rows, const void* q, int64_t ld_q,
+                      int64_t ld_q_head, int32_t n_heads, const void* k, int64_t ld_k, int64_t ld_k_head, const void* v, int64_t ld_v,
+                      int64_t ld_v_head, int32_t rot_dim, const double* turns, float amplitude, const int32_t* pos, uint32_t flags,
+                      void* q_out, int64_t ld_q_out, int64_t ld_q_out_head, uint32_t* device_status, pcm_stream stream);
+
+/* Attention of the new tokens' queries over the cache, their own keys and values already in it:
+ *     out[r][h] = sum_j softmax_j(scale q[r][h] . k_j) v_j,   lse[r][h] = log sum_j exp(scale q[r][h] . k_j)
+ * over the tokens j of the row's sequence with j <= p and (window = 0 or j > p - window or j < sinks), p the row's position;
+ * head h reads key-value head h / (n_heads / n_kv_heads).  A row that sees nothing has out 0 and lse -inf.  Keys and values
+ * that a row does not see have no influence on it, NaN and infinities included.
+ * q and out [n_rows][n_heads][head_dim] of the cache's type with row and head strides, on 16-byte boundaries like the cache;
+ * lse fp32 [n_rows][n_heads] contiguous, may be NULL.  head_dim 32, 64 or 128.  scale > 0.
+ * max_new: no sequence brings more new tokens than this (0: not known); it chooses among kernels and sizes the workspace.
+ * Sums and softmax statistics are fp32; in bf16 the weights enter the product with v as bf16 values (chunks of many new
+ * tokens; a pair of bf16 values each for few).  fp32 is a mode for checks.
+ * workspace: device, 256-byte aligned, >= grpo_paged_attention_workspace_bytes() for the current device (0 when the sizes
+ * are not supported), which never falls as n_rows, n_seq or max_new grow. */
+size_t grpo_paged_attention_workspace_bytes(const grpo_kv_cache* cache, int32_t n_seq, int32_t n_rows, int32_t n_heads, int32_t max_new);
+int grpo_paged_attention(const grpo_kv_cache* cache, const grpo_kv_batch* batch, int32_t n_rows, const void* q, int64_t ld_q,
+                         int64_t ld_q_head, int32_t n_heads, float scale, int32_t window, int32_t sinks, int32_t max_new, void* out,
+                         int64_t ld_out, int64_t ld_out_head, float* lse, uint32_t* device_status, void* workspace,
+                         size_t workspace_bytes, pcm_stream stream);
+
 /* ---- diagnostic entry points (per-kernel tests and measurements; not part of Algorithm 1) -------
  * grpo_gemm: C[m][n] = sum_k A(m,k) B(n,k) (+ R[m][n]) with the GEMM kernels the actor update uses.
  * a_kmajor != 0: A is stored [M][K] with row stride lda, else [K][M]; likewise B ([N][K] / [K][N]).

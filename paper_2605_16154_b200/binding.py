@@ -94,6 +94,22 @@ class grpo_adamw_cfg(C.Structure):
                 ("weight_decay", C.c_float), ("max_grad_norm", C.c_float)]
 
 
+class grpo_rotary_cfg(C.Structure):
+    _fields_ = [("rot_dim", C.c_int32), ("scaling", C.c_int32), ("base", C.c_double), ("factor", C.c_double),
+                ("original_len", C.c_double), ("low", C.c_double), ("high", C.c_double)]
+
+
+class grpo_kv_cache(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("n_pages", C.c_int32), ("page_size", C.c_int32), ("n_kv_heads", C.c_int32),
+                ("head_dim", C.c_int32), ("reserved", C.c_int32), ("k", C.c_void_p), ("v", C.c_void_p),
+                ("ld_page", C.c_int64), ("ld_slot", C.c_int64), ("ld_head", C.c_int64)]
+
+
+class grpo_kv_batch(C.Structure):
+    _fields_ = [("n_seq", C.c_int32), ("max_pages", C.c_int32), ("page_table", C.c_void_p), ("ld_table", C.c_int64),
+                ("seq_len", C.c_void_p), ("q_off", C.c_void_p)]
+
+
 PROFILE_CLASSES = ("gemm", "attention", "rmsnorm", "elementwise", "loss", "embed_grad", "pack", "pcm_score", "pcm_sample",
                    "gemm_small")
 
@@ -158,6 +174,13 @@ _lib.grpo_head_logp_bwd_workspace_bytes.argtypes = [_I, _I, _I, _I]
 _lib.grpo_head_logp_bwd_workspace_bytes.restype = C.c_size_t
 _lib.grpo_head_logp_bwd.argtypes = [_P, _L, _I, _I, _P, _L, _I, _P, _F, _P, _P, _P, _P, _I, C.c_uint32, _P, _L, _P, _P, _P,
                                     C.c_size_t, _P]
+_KV = [C.POINTER(grpo_kv_cache), C.POINTER(grpo_kv_batch)]
+_lib.grpo_rotary_freqs.argtypes = [C.POINTER(grpo_rotary_cfg), _P, C.POINTER(_F)]
+_lib.grpo_rotary.argtypes = [_I, _P, _L, _L, _I, _I, _I, _I, _P, _F, _P, C.c_uint32, _P, _L, _L, _P]
+_lib.grpo_rotary_cache.argtypes = _KV + [_I, _P, _L, _L, _I, _P, _L, _L, _P, _L, _L, _I, _P, _F, _P, C.c_uint32, _P, _L, _L, _P, _P]
+_lib.grpo_paged_attention_workspace_bytes.argtypes = [C.POINTER(grpo_kv_cache), _I, _I, _I, _I]
+_lib.grpo_paged_attention_workspace_bytes.restype = C.c_size_t
+_lib.grpo_paged_attention.argtypes = _KV + [_I, _P, _L, _L, _I, _F, _I, _I, _I, _P, _L, _L, _P, _P, _P, C.c_size_t, _P]
 _lib.grpo_gemm_wait_status.argtypes = [C.c_uint32]
 _lib.grpo_gemm_wait_status.restype = C.c_uint32
 _lib.pcm_launch_count.restype = C.c_int64
@@ -169,7 +192,7 @@ for _name in ("pcm_create", "pcm_destroy", "pcm_poll_status", "pcm_state_export"
               "pcm_score_phases", "pcm_update_keep_probs", "pcm_sample_chunks", "grpo_pack_chunks",
               "grpo_actor_fwd_bwd", "grpo_gemm", "grpo_attention", "pcm_profile_enable", "pcm_profile_read",
               "grpo_embed", "grpo_embed_bwd", "grpo_token_logp", "grpo_token_logp_bwd", "grpo_head_logp",
-              "grpo_head_logp_bwd"):
+              "grpo_head_logp_bwd", "grpo_rotary_freqs", "grpo_rotary", "grpo_rotary_cache", "grpo_paged_attention"):
     getattr(_lib, _name).restype = C.c_int
 
 EXPORTED = ("pcm_create", "pcm_destroy", "pcm_poll_status", "pcm_state_export", "pcm_state_import",
@@ -180,7 +203,8 @@ EXPORTED = ("pcm_create", "pcm_destroy", "pcm_poll_status", "pcm_state_export", 
             "grpo_attention_wait_status", "pcm_first_use_on_device", "grpo_lora_workspace_bytes",
             "grpo_actor_fwd_bwd_lora", "grpo_embed", "grpo_embed_workspace_bytes", "grpo_embed_bwd", "grpo_token_logp",
             "grpo_token_logp_bwd", "grpo_head_logp_workspace_bytes", "grpo_head_logp", "grpo_head_logp_bwd_workspace_bytes",
-            "grpo_head_logp_bwd", "grpo_gemm_wait_status")
+            "grpo_head_logp_bwd", "grpo_gemm_wait_status", "grpo_rotary_freqs", "grpo_rotary", "grpo_rotary_cache",
+            "grpo_paged_attention_workspace_bytes", "grpo_paged_attention")
 
 
 def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
@@ -697,6 +721,169 @@ def grpo_head_logp_bwd(x: torch.Tensor, w_h: torch.Tensor, tok: torch.Tensor, ls
             _vector(call, dentropy, dev, _f32, n), chunk_rows, (GRPO_ACCUMULATE if accumulate else 0) | (GRPO_EXACT_DX if exact_dx else 0), dxp, lddx,
             _vector(call, dw, dev, _f32, vocab * d), _vector(call, status, dev, _i32, 1), wsp, wsn)
     return dx, dw
+
+
+# ------------------------------------------------------------------------------------------------
+# The rollout side: rotary positions, a paged cache and attention over it.  The same manner as above.
+ROTARY_PLAIN, ROTARY_LINEAR, ROTARY_BASE, ROTARY_PARTS = 0, 1, 2, 3
+_ROTARY_INTERLEAVED, _ROTARY_INVERSE = 1, 2
+STATUS_BAD_PAGE, STATUS_BAD_LENGTH = 64, 128
+_f64 = torch.float64
+
+
+def grpo_rotary_freqs(rot_dim: int, base: float = 10000.0, scaling: int = ROTARY_PLAIN, factor: float = 1.0,
+                      original_len: float = 0.0, low: float = 1.0, high: float = 32.0):
+    """(turns, amplitude): the frequencies of rot_dim / 2 pairs in turns per position (float64, on the host: move them to the
+    device once) and the factor on the rotated values."""
+    _size("grpo_rotary_freqs", rot_dim, 0)
+    turns = torch.empty(max(0, rot_dim // 2), dtype=_f64)
+    amplitude = C.c_float(0.0)
+    cfg = grpo_rotary_cfg(rot_dim, scaling, base, factor, original_len, low, high)
+    _check("grpo_rotary_freqs", _lib.grpo_rotary_freqs(C.byref(cfg), turns.data_ptr(), C.byref(amplitude)))
+    return turns, amplitude.value
+
+
+def _heads(call: str, t: torch.Tensor, device=None):
+    """(dtype code, address, row stride, head stride, rows, heads, head dim) of device rows [n, heads, dim]."""
+    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dim() == 3) or (device is not None and t.device != device):
+        raise PcmError(call, -1)
+    dt = _DTYPES.get(t.dtype)
+    (n, h, d), (ld, ld_head, step) = t.shape, t.stride()
+    if dt is None or (step != 1 and d > 1 and n * h):
+        raise PcmError(call, -1)
+    if n > _INT32_MAX or h > _INT32_MAX or d > _INT32_MAX:
+        raise PcmError(call, -2)
+    return dt, t.data_ptr(), ld, ld_head, n, h, d
+
+
+def _turns(call: str, turns: Optional[torch.Tensor], device) -> tuple:
+    """(address, rotated elements of a head) of a table of frequencies."""
+    if turns is None:
+        return None, 0
+    return _vector(call, turns, device, _f64, turns.numel()), 2 * turns.numel()
+
+
+def grpo_rotary(x: torch.Tensor, pos: torch.Tensor, turns: torch.Tensor, interleaved: bool = False, amplitude: float = 1.0,
+                inverse: bool = False, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """x [n, heads, dim] rotated to the positions pos [n] (int32): the first 2 len(turns) elements of each head turn by
+    2 pi pos turns, times amplitude.  `inverse` turns back: the gradient of x from the gradient of the result.  `out` may be x."""
+    call = "grpo_rotary"
+    dt, xp, ld, ldh, n, h, d = _heads(call, x)
+    dev = x.device
+    tp, rot = _turns(call, turns, dev)
+    if out is None:
+        out = torch.empty((n, h, d), dtype=x.dtype, device=dev)
+    odt, op, ldo, ldoh, on, oh, od = _heads(call, out, dev)
+    _require(call, odt == dt and on == n and oh == h and od == d and pos is not None)
+    _launch(call, dev, _lib.grpo_rotary, dt, xp, ld, ldh, n, h, d, rot, tp, amplitude, _vector(call, pos, dev, _i32, n),
+            (_ROTARY_INTERLEAVED if interleaved else 0) | (_ROTARY_INVERSE if inverse else 0), op, ldo, ldoh)
+    return out
+
+
+def _cache(call: str, k_pages: torch.Tensor, v_pages: torch.Tensor):
+    """The cache of pages [n_pages, page_size, kv heads, dim], in any order of the first three in memory."""
+    dev = k_pages.device
+    ok = k_pages.is_cuda and k_pages.dim() == 4 and v_pages.device == dev and v_pages.dtype == k_pages.dtype
+    dt = _DTYPES.get(k_pages.dtype)
+    if not ok or dt is None or v_pages.shape != k_pages.shape or v_pages.stride() != k_pages.stride():
+        raise PcmError(call, -1)
+    (n, page, kv, d), (ld_page, ld_slot, ld_head, step) = k_pages.shape, k_pages.stride()
+    if step != 1 and d > 1:
+        raise PcmError(call, -1)
+    if n > _INT32_MAX or page > _INT32_MAX or kv > _INT32_MAX:
+        raise PcmError(call, -2)
+    return grpo_kv_cache(dt, n, page, kv, d, 0, k_pages.data_ptr(), v_pages.data_ptr(), ld_page, ld_slot, ld_head), dev
+
+
+def _sequences(call: str, table: torch.Tensor, seq_len: torch.Tensor, q_off: Optional[torch.Tensor], dev) -> grpo_kv_batch:
+    n = seq_len.numel()
+    if table.device != dev or table.dtype != _i32 or table.dim() != 2 or table.shape[0] != n:
+        raise PcmError(call, -1)
+    (_, pages), (ld, step) = table.shape, table.stride()
+    if n <= 1:
+        ld = max(pages, ld)
+    if step != 1 and pages > 1:
+        raise PcmError(call, -1)
+    if n > _INT32_MAX or pages > _INT32_MAX:
+        raise PcmError(call, -2)
+    return grpo_kv_batch(n, pages, table.data_ptr(), ld, _vector(call, seq_len, dev, _i32, n), _vector(call, q_off, dev, _i32, n + 1))
+
+
+def grpo_rotary_cache(q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor,
+                      table: torch.Tensor, seq_len: torch.Tensor, q_off: Optional[torch.Tensor], turns: Optional[torch.Tensor],
+                      interleaved: bool = False, amplitude: float = 1.0, pos: Optional[torch.Tensor] = None,
+                      q_out: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None) -> Optional[torch.Tensor]:
+    """New tokens enter the cache: k and v [n, kv heads, dim], the keys rotated, go to the pages [n_pages, page_size, kv heads,
+    dim] that table [n_seq, pages] (int32) names; returns the rotated q [n, heads, dim].  Sequence s has seq_len[s] tokens, the
+    new ones included, which are rows q_off[s] .. q_off[s + 1] - 1 (None: one each).  `turns` None rotates nothing; `pos` [n]
+    stands in for the tokens' own positions; `q_out` may be q; without q only the cache is written."""
+    call = "grpo_rotary_cache"
+    cache, dev = _cache(call, k_pages, v_pages)
+    batch = _sequences(call, table, seq_len, q_off, dev)
+    dt, kp, ldk, ldkh, n, kv, d = _heads(call, k, dev)
+    vdt, vp, ldv, ldvh, vn, vkv, vd = _heads(call, v, dev)
+    _require(call, dt == cache.dtype and vdt == dt and (n, kv, d) == (vn, vkv, vd) and kv == cache.n_kv_heads and d == cache.head_dim)
+    tp, rot = _turns(call, turns, dev)
+    qp = op = None
+    ldq = ldqh = ldo = ldoh = h = 0
+    if q is not None:
+        qdt, qp, ldq, ldqh, qn, h, qd = _heads(call, q, dev)
+        _require(call, qdt == dt and qn == n and qd == d)
+        if q_out is None:
+            q_out = torch.empty((n, h, d), dtype=q.dtype, device=dev)
+        odt, op, ldo, ldoh, on, oh, od = _heads(call, q_out, dev)
+        _require(call, odt == dt and on == n and oh == h and od == d)
+    else:
+        _require(call, q_out is None)
+    _launch(call, dev, _lib.grpo_rotary_cache, cache, batch, n, qp, ldq, ldqh, h, kp, ldk, ldkh, vp, ldv, ldvh, rot, tp, amplitude,
+            _vector(call, pos, dev, _i32, n), _ROTARY_INTERLEAVED if interleaved else 0, op, ldo, ldoh,
+            _vector(call, status, dev, _i32, 1))
+    return q_out
+
+
+def grpo_paged_attention_workspace_bytes(k_pages: torch.Tensor, n_seq: int, n: int, n_heads: int, max_new: int = 0) -> int:
+    """Workspace of a call with n rows of n_heads queries over a cache like k_pages, on its device."""
+    call = "grpo_paged_attention_workspace_bytes"
+    _size(call, n_seq, n, n_heads, max_new)
+    cache, dev = _cache(call, k_pages, k_pages)
+    with torch.cuda.device(dev):
+        return int(_lib.grpo_paged_attention_workspace_bytes(C.byref(cache), n_seq, n, n_heads, max_new))
+
+
+def grpo_paged_attention(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor, table: torch.Tensor, seq_len: torch.Tensor,
+                         q_off: Optional[torch.Tensor] = None, scale: Optional[float] = None, window: int = 0, sinks: int = 0,
+                         max_new: int = 0, out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None,
+                         want_lse: bool = True, workspace: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None):
+    """(out, lse): attention of the new tokens' queries q [n, heads, dim] over the cache, causal, with `window` over the last
+    `window` tokens and the first `sinks`.  Cache, table, seq_len and q_off as for grpo_rotary_cache; scale None is
+    1 / sqrt(dim); max_new: the most new tokens of a sequence, if known.  Rows that belong to no sequence are left as they are
+    in a given `out`, and hold anything in a new one."""
+    call = "grpo_paged_attention"
+    cache, dev = _cache(call, k_pages, v_pages)
+    batch = _sequences(call, table, seq_len, q_off, dev)
+    dt, qp, ldq, ldqh, n, h, d = _heads(call, q, dev)
+    _require(call, dt == cache.dtype and d == cache.head_dim)
+    _size(call, window, sinks, max_new)
+    if out is None:
+        out = torch.empty((n, h, d), dtype=q.dtype, device=dev)
+        op, ldo, ldoh = out.data_ptr(), h * d, d
+    else:
+        odt, op, ldo, ldoh, on, oh, od = _heads(call, out, dev)
+        _require(call, odt == dt and on == n and oh == h and od == d)
+    if lse is None and want_lse:
+        lse = torch.empty((n, h), dtype=_f32, device=dev)
+    lp = _vector(call, lse, dev, _f32, n * h)
+    sp = _vector(call, status, dev, _i32, 1)
+    if scale is None:
+        scale = d ** -0.5
+
+    def run(stream):
+        need = _lib.grpo_paged_attention_workspace_bytes(cache, batch.n_seq, n, h, max_new)
+        ws, wp, wn = _workspace(call, workspace, need, dev)
+        return _lib.grpo_paged_attention(cache, batch, n, qp, ldq, ldqh, h, scale, window, sinks, max_new, op, ldo, ldoh, lp, sp,
+                                         wp, wn, stream)
+    _launch(call, dev, run)
+    return out, lse
 
 
 # ------------------------------------------------------------------------------------------------

@@ -18,6 +18,8 @@ constexpr unsigned STATUS_TOO_LONG = 4u;      // trajectory longer than max_len
 constexpr unsigned STATUS_BAD_OFFSETS = 8u;   // traj_off / kept_idx inconsistent with host sizes
 constexpr unsigned STATUS_BAD_ACTION = 16u;   // continuous action not finite or beyond the fixed-point range
 constexpr unsigned STATUS_BAD_TOKEN = 32u;     // token id >= vocab
+constexpr unsigned STATUS_BAD_PAGE = 64u;      // page index outside the cache
+constexpr unsigned STATUS_BAD_LENGTH = 128u;   // sequence length or row offset that does not fit the call
 
 #define PCM_CUDA_TRY(expr)                         \
   do {                                             \

@@ -1,0 +1,400 @@
+// Attention of new tokens over a paged cache: the line of work, the kernel for checks (fp32), the join of split units, and
+// the entry points.  The line is described in paged_attention.cuh.
+#include <cmath>
+
+#include "async_ptx.cuh"
+#include "paged_attention.cuh"
+
+namespace pcm {
+namespace pga {
+
+// ------------------------------------------------------------------------------------------------
+// tiles ahead of every sequence: one block
+// ------------------------------------------------------------------------------------------------
+constexpr int PLAN_THREADS = 1024;
+__global__ void __launch_bounds__(PLAN_THREADS) attn_plan_kernel(const AttnParams p) {
+  __shared__ long long warp_sum[PLAN_THREADS / 32];
+  __shared__ long long carry;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  if (tid == 0) { carry = 0; p.prefix[0] = 0; }
+  for (int base = 0; base < p.c.n_seq; base += PLAN_THREADS) {
+    const int s = base + tid;
+    SeqSpan sp{0, 0, 0};
+    if (s < p.c.n_seq) sp = attn_span(p, s, true);
+    const int nqt = row_tiles(p, sp);
+    long long sum = 0;
+    if (nqt <= 2)
+      for (int qt = 0; qt < nqt; ++qt) sum += unit_span(p, sp, qt).tiles;
+    for (unsigned many = __ballot_sync(0xffffffffu, nqt > 2); many; many &= many - 1) {
+      const int from = __ffs(many) - 1;                            // a sequence of many row tiles takes the whole warp
+      SeqSpan o;
+      o.row0 = 0;
+      o.fresh = __shfl_sync(0xffffffffu, sp.fresh, from);
+      o.len = __shfl_sync(0xffffffffu, sp.len, from);
+      const int n = row_tiles(p, o);
+      long long mine = 0;
+      for (int qt = lane; qt < n; qt += 32) mine += unit_span(p, o, qt).tiles;
+#pragma unroll
+      for (int d = 16; d > 0; d >>= 1) mine += __shfl_xor_sync(0xffffffffu, mine, d);
+      if (lane == from) sum = mine;
+    }
+    sum *= p.c.n_kv;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const long long t = __shfl_up_sync(0xffffffffu, sum, o);
+      if (lane >= o) sum += t;
+    }
+    if (lane == 31) warp_sum[warp] = sum;
+    __syncthreads();
+    long long before = carry;
+    for (int w = 0; w < warp; ++w) before += warp_sum[w];
+    if (s < p.c.n_seq) p.prefix[s + 1] = before + sum;
+    __syncthreads();
+    if (tid == PLAN_THREADS - 1) carry = before + sum;
+    __syncthreads();
+  }
+  let_successor_start();
+}
+
+// ------------------------------------------------------------------------------------------------
+// fp32: 16 rows, 128 keys a tile, 16 of them for each of eight warps, which run independently of one another through a
+// unit and join their sums at its end.  Bound by the fp32 pipes and shared memory; a mode for checks, not tuned.
+// ------------------------------------------------------------------------------------------------
+constexpr int RF_ROWS = 16, RF_WARPS = 8, RF_KEYS = 16, RF_TILE = RF_WARPS * RF_KEYS, RF_THREADS = RF_WARPS * 32;
+template <int DH> struct RfSmem {
+  static constexpr int LDK = DH + 4;                               // a lane per key: rows shifted by a bank group
+  static constexpr int WARP = RF_KEYS * LDK + RF_KEYS * DH + RF_KEYS * RF_ROWS;      // keys, values, weights
+  static constexpr int FLOATS = RF_ROWS * DH + RF_WARPS * WARP + RF_WARPS * RF_ROWS * 2 + RF_ROWS * 3;
+  static constexpr int BYTES = FLOATS * 4;
+};
+
+__device__ __forceinline__ void cp_async16(void* dst, const void* src, bool take) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_u32(dst)), "l"(src), "r"(take ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void cp_async_wait_all() { asm volatile("cp.async.wait_all;" ::: "memory"); }
+
+template <int DH>
+__global__ void __launch_bounds__(RF_THREADS) attn_rows_f32_kernel(const __grid_constant__ AttnParams p) {
+  using S = RfSmem<DH>;
+  extern __shared__ float sm[];
+  __shared__ Piece piece;
+  float* qs = sm;                                                  // [16][DH]
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  float* ks = sm + RF_ROWS * DH + warp * S::WARP;
+  float* vs = ks + RF_KEYS * S::LDK;
+  float* ws = vs + RF_KEYS * DH;                                   // [key][row]
+  float* all_m = sm + RF_ROWS * DH + RF_WARPS * S::WARP;           // [warp][row]
+  float* all_l = all_m + RF_WARPS * RF_ROWS;
+  float* row_m = all_l + RF_WARPS * RF_ROWS;                       // joined
+  float* row_l = row_m + RF_ROWS;
+  int* row_bad = reinterpret_cast<int*>(row_l + RF_ROWS);
+  constexpr int CL = DH / 4, KG = 32 / CL;                         // lanes across a value's columns; keys side by side
+  const int col = (lane % CL) * 4, kg = lane / CL, key_lane = lane & 15, half = lane >> 4;
+
+  wait_for_predecessor();
+  if (warp == 0) {
+    Piece own;
+    find_piece(p, blockIdx.x, own);
+    if (lane == 0) piece = own;
+  }
+  __syncthreads();
+  Cursor c = piece.c;
+  long long left = piece.left, ahead = piece.ahead;
+  const long long share = piece.share;
+  int4 job = make_int4(0, 0, 0, -1);
+
+  while (left > 0) {
+    const int t0 = c.at, t1 = (int)min((long long)c.u.tiles, t0 + left);
+    const bool whole = t0 == 0 && t1 == c.u.tiles;
+    for (int i = tid; i < RF_ROWS * DH; i += RF_THREADS) {
+      const int r = i / DH;
+      const RowPlace x = row_place(p, c.sp, c.qt, c.head, r);
+      qs[i] = x.valid ? ((const float*)p.q)[x.row * p.ld_q + x.head * p.ld_q_head + (i - r * DH)] : 0.f;
+    }
+    int pos[8];
+#pragma unroll
+    for (int r = 0; r < 8; ++r) pos[r] = row_place(p, c.sp, c.qt, c.head, half * 8 + r).pos;
+    __syncthreads();
+    float m[8], l[8], acc[RF_ROWS][4];
+#pragma unroll
+    for (int r = 0; r < 8; ++r) { m[r] = -INFINITY; l[r] = 0.f; }
+#pragma unroll
+    for (int r = 0; r < RF_ROWS; ++r) acc[r][0] = acc[r][1] = acc[r][2] = acc[r][3] = 0.f;
+    for (int t = t0; t < t1; ++t) {
+      const int key0 = (t < c.u.first_tiles ? t : t + c.u.skip) * RF_TILE + warp * RF_KEYS;
+      __syncwarp();
+      for (int i = lane; i < RF_KEYS * DH / 4; i += 32) {
+        const int k = i / (DH / 4), e = (i - k * (DH / 4)) * 4, key = key0 + k;
+        long long at = -1;
+        if (unit_sees(p, c.u, key)) at = slot_offset(p.c, c.s, key, c.head);
+        cp_async16(ks + k * S::LDK + e, (const float*)p.c.k + (at < 0 ? 0 : at + e), at >= 0);
+        cp_async16(vs + k * DH + e, (const float*)p.c.v + (at < 0 ? 0 : at + e), at >= 0);
+      }
+      cp_async_wait_all();
+      __syncwarp();
+      float z[8];
+#pragma unroll
+      for (int r = 0; r < 8; ++r) z[r] = 0.f;
+      for (int e = 0; e < DH; e += 4) {
+        const float4 k = *reinterpret_cast<const float4*>(ks + key_lane * S::LDK + e);
+#pragma unroll
+        for (int r = 0; r < 8; ++r) {
+          const float4 q = *reinterpret_cast<const float4*>(qs + (half * 8 + r) * DH + e);
+          z[r] = fmaf(q.x, k.x, fmaf(q.y, k.y, fmaf(q.z, k.z, fmaf(q.w, k.w, z[r]))));
+        }
+      }
+      float shrink[8];
+      bool changed = false;
+#pragma unroll
+      for (int r = 0; r < 8; ++r) {
+        if (!row_sees(p, pos[r], key0 + key_lane)) z[r] = -INFINITY;
+        float top = z[r];
+#pragma unroll
+        for (int d = 8; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+        const float to = fmaxf(m[r], top);
+        const float ref = to == -INFINITY ? 0.f : to;
+        shrink[r] = m[r] == to ? 1.f : ex2((m[r] - ref) * p.scale_log2);
+        changed |= shrink[r] != 1.f;
+        m[r] = to;
+        const float w = ex2((z[r] - ref) * p.scale_log2);
+        l[r] = fmaf(l[r], shrink[r], w);
+        ws[key_lane * RF_ROWS + half * 8 + r] = w;
+      }
+      if (__any_sync(0xffffffffu, changed)) {
+#pragma unroll
+        for (int r = 0; r < RF_ROWS; ++r) {
+          const float f = __shfl_sync(0xffffffffu, shrink[r & 7], (r >> 3) << 4);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) acc[r][i] *= f;
+        }
+      }
+      __syncwarp();
+#pragma unroll
+      for (int k = kg; k < RF_KEYS; k += KG) {
+        const float4 v = *reinterpret_cast<const float4*>(vs + k * DH + col);
+#pragma unroll
+        for (int r = 0; r < RF_ROWS; r += 4) {
+          const float4 w = *reinterpret_cast<const float4*>(ws + k * RF_ROWS + r);
+          acc[r][0] = fmaf(w.x, v.x, acc[r][0]); acc[r][1] = fmaf(w.x, v.y, acc[r][1]);
+          acc[r][2] = fmaf(w.x, v.z, acc[r][2]); acc[r][3] = fmaf(w.x, v.w, acc[r][3]);
+          acc[r + 1][0] = fmaf(w.y, v.x, acc[r + 1][0]); acc[r + 1][1] = fmaf(w.y, v.y, acc[r + 1][1]);
+          acc[r + 1][2] = fmaf(w.y, v.z, acc[r + 1][2]); acc[r + 1][3] = fmaf(w.y, v.w, acc[r + 1][3]);
+          acc[r + 2][0] = fmaf(w.z, v.x, acc[r + 2][0]); acc[r + 2][1] = fmaf(w.z, v.y, acc[r + 2][1]);
+          acc[r + 2][2] = fmaf(w.z, v.z, acc[r + 2][2]); acc[r + 2][3] = fmaf(w.z, v.w, acc[r + 2][3]);
+          acc[r + 3][0] = fmaf(w.w, v.x, acc[r + 3][0]); acc[r + 3][1] = fmaf(w.w, v.y, acc[r + 3][1]);
+          acc[r + 3][2] = fmaf(w.w, v.z, acc[r + 3][2]); acc[r + 3][3] = fmaf(w.w, v.w, acc[r + 3][3]);
+        }
+      }
+    }
+    // join the warps
+#pragma unroll
+    for (int r = 0; r < 8; ++r) {
+#pragma unroll
+      for (int d = 8; d > 0; d >>= 1) l[r] += __shfl_xor_sync(0xffffffffu, l[r], d);
+      if (key_lane == 0) { all_m[warp * RF_ROWS + half * 8 + r] = m[r]; all_l[warp * RF_ROWS + half * 8 + r] = l[r]; }
+    }
+#pragma unroll
+    for (int r = 0; r < RF_ROWS; ++r)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int d = CL; d < 32; d <<= 1) acc[r][i] += __shfl_xor_sync(0xffffffffu, acc[r][i], d);
+    __syncthreads();                                               // every warp is through with its keys and values
+    float* mine = sm + RF_ROWS * DH + warp * S::WARP;              // [16][DH]
+    if (kg == 0)
+#pragma unroll
+      for (int r = 0; r < RF_ROWS; ++r) *reinterpret_cast<float4*>(mine + r * DH + col) = make_float4(acc[r][0], acc[r][1], acc[r][2], acc[r][3]);
+    __syncthreads();
+    if (tid < RF_ROWS) {
+      float top = -INFINITY, sum = 0.f;
+      for (int w = 0; w < RF_WARPS; ++w) top = fmaxf(top, all_m[w * RF_ROWS + tid]);
+      const float ref = top == -INFINITY ? 0.f : top;
+      for (int w = 0; w < RF_WARPS; ++w) {
+        const float f = ex2((all_m[w * RF_ROWS + tid] - ref) * p.scale_log2);
+        sum = fmaf(all_l[w * RF_ROWS + tid], f, sum);
+        all_m[w * RF_ROWS + tid] = f;
+      }
+      row_m[tid] = top; row_l[tid] = sum; row_bad[tid] = 0;
+    }
+    __syncthreads();
+    const int slot = 2 * blockIdx.x + (t0 == 0 ? 1 : 0);
+    float* part = p.part + (long long)slot * RF_ROWS * DH;
+    for (int i = tid; i < RF_ROWS * DH; i += RF_THREADS) {
+      const int r = i / DH, e = i - r * DH;
+      float o = 0.f;
+      for (int w = 0; w < RF_WARPS; ++w) o = fmaf(all_m[w * RF_ROWS + r], sm[RF_ROWS * DH + w * S::WARP + i], o);
+      const RowPlace x = row_place(p, c.sp, c.qt, c.head, r);
+      if (!isfinite(o) && isfinite(row_l[r]) && x.valid) row_bad[r] = 1;
+      if (!whole) part[i] = o;
+      else if (x.valid) ((float*)p.out)[x.row * p.ld_out + x.head * p.ld_out_head + e] = row_l[r] == 0.f ? 0.f : o / row_l[r];
+    }
+    __syncthreads();
+    for (int r = warp; r < RF_ROWS; r += RF_WARPS) {
+      const RowPlace x = row_place(p, c.sp, c.qt, c.head, r);
+      if (row_bad[r]) {
+        float o[DH / 32];
+        exact_row<float, DH>(p, c.s, c.head, c.u, t0, t1, x, row_m[r] == -INFINITY ? 0.f : row_m[r], o);
+#pragma unroll
+        for (int i = 0; i < DH / 32; ++i) {
+          if (!whole) part[r * DH + lane + 32 * i] = o[i];
+          else ((float*)p.out)[x.row * p.ld_out + x.head * p.ld_out_head + lane + 32 * i] = o[i] / row_l[r];
+        }
+      }
+      if (lane == 0) {
+        if (!whole) p.part_ml[(long long)slot * RF_ROWS + r] = make_float2(row_m[r], row_l[r]);
+        else if (x.valid && p.lse)
+          p.lse[x.row * p.n_heads + x.head] = row_l[r] == 0.f ? -INFINITY : fmaf(row_m[r], p.scale_log2, log2f(row_l[r])) * LN2;
+      }
+    }
+    __syncthreads();
+    if (!whole && t0 == 0) job = make_int4(c.s, c.qt, c.head, last_worker(p, blockIdx.x, share, ahead, c.u.tiles));
+    left -= t1 - t0;
+    ahead += t1 - t0;
+    if (left > 0) c.next_unit(p);
+  }
+  if (tid == 0) p.jobs[blockIdx.x] = job;
+  let_successor_start();
+}
+
+// ------------------------------------------------------------------------------------------------
+// join of split units: a warp per row, the pieces in the order of their keys
+// ------------------------------------------------------------------------------------------------
+constexpr int JN_WARPS = 8;
+template <typename T, int DH>
+__global__ void __launch_bounds__(JN_WARPS * 32) attn_join_kernel(const AttnParams p) {
+  wait_for_predecessor();
+  const int w0 = blockIdx.x;
+  const int4 job = p.jobs[w0];
+  if (job.w < 0) return;
+  const int r = blockIdx.y * JN_WARPS + (threadIdx.x >> 5), lane = threadIdx.x & 31;
+  const SeqSpan sp = attn_span(p, job.x, false);
+  const RowPlace x = row_place(p, sp, job.y, job.z, r);
+  if (r >= p.unit_rows || !x.valid) return;
+  constexpr int C = DH / 32;
+  float top = -INFINITY;
+  for (int w = w0; w <= job.w; ++w) top = fmaxf(top, p.part_ml[(long long)(w == w0 ? 2 * w + 1 : 2 * w) * p.unit_rows + r].x);
+  const float ref = top == -INFINITY ? 0.f : top;
+  float o[C], l = 0.f;
+#pragma unroll
+  for (int i = 0; i < C; ++i) o[i] = 0.f;
+  for (int w = w0; w <= job.w; ++w) {
+    const long long at = (long long)(w == w0 ? 2 * w + 1 : 2 * w) * p.unit_rows + r;
+    const float2 ml = p.part_ml[at];
+    const float f = ex2((ml.x - ref) * p.scale_log2);
+    l = fmaf(ml.y, f, l);
+#pragma unroll
+    for (int i = 0; i < C; ++i) o[i] = fmaf(p.part[at * DH + lane + 32 * i], f, o[i]);
+  }
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+#pragma unroll
+  for (int i = 0; i < C; ++i) from_float(((T*)p.out)[x.row * p.ld_out + x.head * p.ld_out_head + lane + 32 * i], o[i] * inv);
+  if (lane == 0 && p.lse) p.lse[x.row * p.n_heads + x.head] = l == 0.f ? -INFINITY : fmaf(top, p.scale_log2, log2f(l)) * LN2;
+}
+
+// ------------------------------------------------------------------------------------------------
+// host side
+// ------------------------------------------------------------------------------------------------
+template <int DH>
+static int launch_f32(const AttnParams& p, cudaStream_t s) {
+  static unsigned long long seen = 0;
+  if (attr_needed(&seen))
+    PCM_CUDA_TRY(cudaFuncSetAttribute(attn_rows_f32_kernel<DH>, cudaFuncAttributeMaxDynamicSharedMemorySize, RfSmem<DH>::BYTES));
+  return launch_after_smem(attn_rows_f32_kernel<DH>, dim3(p.workers), dim3(RF_THREADS), RfSmem<DH>::BYTES, s, p);
+}
+
+template <typename T, int DH>
+static int launch_join(const AttnParams& p, cudaStream_t s) {
+  return launch_after(attn_join_kernel<T, DH>, dim3(p.workers, ceil_div(p.unit_rows, JN_WARPS)), dim3(JN_WARPS * 32), s, p);
+}
+
+template <typename T>
+static int launch_join_as(const AttnParams& p, int dh, cudaStream_t s) {
+  return dh == 128 ? launch_join<T, 128>(p, s) : dh == 64 ? launch_join<T, 64>(p, s) : launch_join<T, 32>(p, s);
+}
+
+struct Layout { size_t prefix, jobs, ml, part, total; };
+static Layout layout(int n_seq, int workers, int unit_rows, int dh) {
+  Layout y;
+  auto up = [](size_t b) { return (b + 255) / 256 * 256; };
+  y.prefix = 0;
+  y.jobs = y.prefix + up(((size_t)n_seq + 1) * 8);
+  y.ml = y.jobs + up((size_t)workers * 16);
+  y.part = y.ml + up((size_t)2 * workers * unit_rows * 8);
+  y.total = y.part + up((size_t)2 * workers * unit_rows * dh * 4);
+  return y;
+}
+static void place(AttnParams& p, const Layout& y, void* ws) {
+  unsigned char* b = (unsigned char*)ws;
+  p.prefix = (long long*)(b + y.prefix);
+  p.jobs = (int4*)(b + y.jobs);
+  p.part_ml = (float2*)(b + y.ml);
+  p.part = (float*)(b + y.part);
+}
+
+static bool attn_sizes_ok(const grpo_kv_cache* c, int64_t n_seq, int64_t n_rows, int64_t n_heads) {
+  if (!c || (c->dtype != GRPO_F32 && c->dtype != GRPO_BF16) || n_seq < 0 || n_rows < 0 || c->n_kv_heads < 1 || n_heads < 1) return false;
+  if (c->head_dim != 32 && c->head_dim != 64 && c->head_dim != 128) return false;
+  if (n_heads % c->n_kv_heads || n_heads > (1 << 16) || n_seq > PCM_MAX_VOCAB_CALL || n_rows > PCM_MAX_VOCAB_CALL) return false;
+  return n_rows * (n_heads / c->n_kv_heads) <= PCM_MAX_VOCAB_CALL;              // rows of a key-value head are counted in 32 bits
+}
+
+}  // namespace pga
+}  // namespace pcm
+
+using namespace pcm;
+using namespace pcm::pga;
+
+extern "C" size_t grpo_paged_attention_workspace_bytes(const grpo_kv_cache* cache, int32_t n_seq, int32_t n_rows, int32_t n_heads,
+                                                       int32_t max_new) {
+  if (!attn_sizes_ok(cache, n_seq, n_rows, n_heads) || max_new < 0) return 0;
+  return layout(n_seq, 2 * sm_count(), cache->dtype == GRPO_F32 ? RF_ROWS : 32, cache->head_dim).total;
+}
+
+extern "C" int grpo_paged_attention(const grpo_kv_cache* cache, const grpo_kv_batch* batch, int32_t n_rows, const void* q, int64_t ld_q,
+                                    int64_t ld_q_head, int32_t n_heads, float scale, int32_t window, int32_t sinks, int32_t max_new,
+                                    void* out, int64_t ld_out, int64_t ld_out_head, float* lse, uint32_t* device_status, void* workspace,
+                                    size_t workspace_bytes, pcm_stream stream) {
+  const int bad = kv_check(cache, batch, n_rows);
+  if (bad != PCM_OK) return bad;
+  if (n_heads < 1 || !(scale > 0.f) || !std::isfinite(scale * LOG2E) || window < 0 || sinks < 0 || max_new < 0) return PCM_ERR_ARG;
+  if (n_heads % cache->n_kv_heads) return PCM_ERR_ARG;
+  if (!attn_sizes_ok(cache, batch->n_seq, n_rows, n_heads)) return PCM_ERR_SHAPE;
+  if (n_rows == 0 || batch->n_seq == 0) return PCM_OK;
+  const int dh = cache->head_dim;
+  if (!q || !out || (lse && ((uintptr_t)lse & 3))) return PCM_ERR_ARG;
+  if (n_heads > 1 && (ld_q_head < dh || ld_out_head < dh)) return PCM_ERR_ARG;
+  if (n_rows > 1 && (ld_q < dh || ld_out < dh)) return PCM_ERR_ARG;
+  const int64_t per = cache->dtype == GRPO_BF16 ? 8 : 4;
+  if ((((uintptr_t)q | (uintptr_t)out) & 15) || (n_heads > 1 && (ld_q_head % per || ld_out_head % per)) ||
+      (n_rows > 1 && (ld_q % per || ld_out % per)))
+    return PCM_ERR_SHAPE;
+  if (!workspace || ((uintptr_t)workspace & 255) ||
+      workspace_bytes < grpo_paged_attention_workspace_bytes(cache, batch->n_seq, n_rows, n_heads, max_new))
+    return PCM_ERR_WORKSPACE;
+  AttnParams p = {};
+  p.c = kv_view(cache, batch, n_rows, device_status);
+  p.q = q; p.ld_q = n_rows > 1 ? ld_q : 0; p.ld_q_head = n_heads > 1 ? ld_q_head : 0;
+  p.out = out; p.ld_out = n_rows > 1 ? ld_out : 0; p.ld_out_head = n_heads > 1 ? ld_out_head : 0;
+  p.lse = lse;
+  p.n_heads = n_heads; p.group = n_heads / cache->n_kv_heads;
+  p.div_group = make_fastdiv(p.group);
+  p.scale_log2 = scale * LOG2E;
+  p.window = window; p.sinks = sinks;
+  cudaStream_t s = (cudaStream_t)stream;
+  prof_begin(PC_ATTN, s);
+  const bool bf16 = cache->dtype == GRPO_BF16;
+  const long long most_rows = (long long)(max_new > 0 && max_new < n_rows ? max_new : batch->q_off ? n_rows : 1) * p.group;
+  p.unit_rows = !bf16 || most_rows <= 16 ? 16 : 32;
+  p.tile = bf16 ? attn_rows_tile() : RF_TILE;
+  p.over_rows = 0; p.up_to_rows = 0x7FFFFFFF;
+  p.workers = 2 * sm_count(); p.min_share = 4;
+  place(p, layout(batch->n_seq, p.workers, p.unit_rows, dh), workspace);
+  int rc = PCM_OK;
+  attn_plan_kernel<<<1, PLAN_THREADS, 0, s>>>(p);
+  g_launches.fetch_add(1, std::memory_order_relaxed);
+  if (cudaPeekAtLastError() != cudaSuccess) { cudaGetLastError(); rc = PCM_ERR_CUDA; }
+  if (rc == PCM_OK) rc = bf16 ? launch_rows_bf16(p, dh, s) : dh == 128 ? launch_f32<128>(p, s) : dh == 64 ? launch_f32<64>(p, s) : launch_f32<32>(p, s);
+  if (rc == PCM_OK) rc = bf16 ? launch_join_as<__nv_bfloat16>(p, dh, s) : launch_join_as<float>(p, dh, s);
+  prof_end(s, 0.0, 0.0);
+  return rc;
+}

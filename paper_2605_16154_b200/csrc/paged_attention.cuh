@@ -1,0 +1,245 @@
+// Attention over a paged cache: how its work is cut, shared by the kernels that do it.
+//
+// A unit is `unit_rows` rows of one sequence and one key-value head (a row is a new token and one of the query heads that
+// share the key-value head; token-major) and the tiles of keys that some of them see.  All units' tiles form one line, in the
+// order of sequences, row tiles, heads, keys.  Every worker (a block) takes an equal piece of that line, so that one long
+// sequence or many short ones keep all SMs equally busy; borders that would cut off less than a few tiles of a unit move to
+// its end.  A piece of a unit leaves the unnormalised sum of its values, its maximum and its sum of weights in the workspace,
+// and the combining kernel joins a unit's pieces in the order of its keys: nothing depends on which block ran when.
+#pragma once
+#include "paged.cuh"
+
+namespace pcm {
+namespace pga {
+
+constexpr float LOG2E = 1.4426950408889634f;
+constexpr float LN2 = 0.6931471805599453f;
+
+struct AttnParams {
+  KvView c;
+  const void* q; long long ld_q, ld_q_head;
+  void* out; long long ld_out, ld_out_head;
+  float* lse;
+  int n_heads, group;
+  FastDiv div_group;
+  float scale_log2;                            // scale log2(e): weights are powers of two
+  int window, sinks;                           // window 0: everything before
+  int unit_rows, tile;                         // rows of a unit, keys of a tile (a power of two)
+  int over_rows, up_to_rows;                   // this kernel's sequences: over_rows < new tokens * group <= up_to_rows
+  int workers, min_share;                      // pieces of the line; tiles of a piece at least
+  long long* prefix;                           // [n_seq + 1] tiles ahead of each sequence
+  int4* jobs;                                  // [workers] unit that a worker began and left open: sequence, row tile, head, last worker (-1: none)
+  float* part;                                 // [2 workers][unit_rows][head_dim], then [2 workers][unit_rows] maxima and sums
+  float2* part_ml;
+};
+
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
+// A sequence's rows as this kernel sees them: none where another kernel takes the sequence.
+__device__ __forceinline__ SeqSpan attn_span(const AttnParams& p, int s, bool report) {
+  SeqSpan sp = seq_span(p.c, s, report);
+  const long long rows = (long long)sp.fresh * p.group;
+  if (rows <= p.over_rows || rows > p.up_to_rows) sp.fresh = 0;
+  return sp;
+}
+__device__ __forceinline__ int row_tiles(const AttnParams& p, const SeqSpan& sp) {
+  return (int)(((long long)sp.fresh * p.group + p.unit_rows - 1) / p.unit_rows);
+}
+
+// The tiles that the rows of row tile qt see: tile i of the unit is tile i of the sequence below `first_tiles` and tile
+// i + skip from there on.  Keys at or behind `end`, and from `sinks` up to `low`, are seen by none of them.
+struct UnitSpan { int tiles, first_tiles, skip, end, low; };
+__device__ __forceinline__ UnitSpan unit_span(const AttnParams& p, const SeqSpan& sp, int qt) {
+  const long long r0 = (long long)qt * p.unit_rows;
+  long long r1 = r0 + p.unit_rows;
+  if (r1 > (long long)sp.fresh * p.group) r1 = (long long)sp.fresh * p.group;
+  const int p0 = sp.len - sp.fresh + (int)(r0 / p.group), p1 = sp.len - sp.fresh + (int)((r1 - 1) / p.group);
+  UnitSpan u;
+  u.end = p1 >= 0 ? p1 + 1 : 0;
+  u.low = p.window > 0 && p0 >= p.window ? p0 - p.window + 1 : 0;
+  const int all = (u.end + p.tile - 1) / p.tile, from = u.low / p.tile;
+  int st = (min(p.sinks, u.end) + p.tile - 1) / p.tile;
+  if (st >= from) {
+    u.first_tiles = 0; u.skip = 0; u.tiles = max(1, all);          // a unit that sees nothing still writes its zeros
+  } else {
+    u.first_tiles = st; u.skip = from - st; u.tiles = all - u.skip;
+  }
+  return u;
+}
+__device__ __forceinline__ bool unit_sees(const AttnParams& p, const UnitSpan& u, int key) {
+  return key < u.end && (key >= u.low || key < p.sinks);
+}
+__device__ __forceinline__ bool row_sees(const AttnParams& p, int pos, int key) {
+  return key <= pos && (p.window == 0 || key > pos - p.window || key < p.sinks);
+}
+
+// A place on the line.
+struct Cursor {
+  int s, qt, head, at, nqt;                    // sequence, row tile, key-value head, tile; row tiles of the sequence
+  SeqSpan sp;
+  UnitSpan u;
+  __device__ void enter_sequence(const AttnParams& p) {            // the next sequence with rows, from s on
+    for (;; ++s) {
+      if (s >= p.c.n_seq) { nqt = 0; return; }
+      sp = attn_span(p, s, false);
+      nqt = row_tiles(p, sp);
+      if (nqt > 0) return;
+    }
+  }
+  __device__ void next_unit(const AttnParams& p) {
+    at = 0;
+    if (++head < p.c.n_kv) return;
+    head = 0;
+    if (++qt >= nqt) {
+      qt = 0; ++s;
+      enter_sequence(p);
+      if (nqt == 0) return;
+    }
+    u = unit_span(p, sp, qt);
+  }
+};
+
+__device__ __forceinline__ long long line_share(const AttnParams& p, long long total) {
+  const long long even = (total + p.workers - 1) / p.workers;
+  return even > p.min_share ? even : p.min_share;
+}
+// A border at tile `at` of a unit of `tiles`: -at moves it to the unit's start, tiles - at to its end, 0 leaves it.
+__device__ __forceinline__ int border_shift(const AttnParams& p, long long share, int at, int tiles) {
+  const int slack = (int)min(1ll << 20, max((long long)(p.min_share + 1) / 2, share >> 4));
+  if (at <= slack && at <= tiles - at) return -at;
+  return tiles - at <= slack ? tiles - at : 0;
+}
+
+// Where border `i` of the line falls; called by a whole warp.  Returns the tiles ahead of it.
+__device__ inline long long find_border(const AttnParams& p, int i, long long share, long long total, Cursor& c) {
+  const int lane = threadIdx.x & 31;
+  const long long x = share * i;
+  if (x >= total) { c.s = p.c.n_seq; c.qt = c.head = c.at = c.nqt = 0; return total; }
+  int lo = 0, hi = p.c.n_seq - 1;              // the sequence with prefix[s] <= x < prefix[s + 1]
+  while (lo < hi) {
+    const int mid = (lo + hi) >> 1;
+    if (p.prefix[mid + 1] > x) hi = mid; else lo = mid + 1;
+  }
+  c.s = lo;
+  c.sp = attn_span(p, lo, false);
+  c.nqt = row_tiles(p, c.sp);
+  long long y = x - p.prefix[lo];
+  for (int base = 0;; base += 32) {
+    const int qt = base + lane;
+    long long sum = qt < c.nqt ? (long long)unit_span(p, c.sp, qt).tiles * p.c.n_kv : 0;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const long long t = __shfl_up_sync(0xffffffffu, sum, o);
+      if (lane >= o) sum += t;
+    }
+    const unsigned over = __ballot_sync(0xffffffffu, sum > y);
+    if (over || base + 32 >= c.nqt) {
+      const int at = over ? __ffs(over) - 1 : 0;
+      const long long before = __shfl_sync(0xffffffffu, sum, at > 0 ? at - 1 : 0);
+      c.qt = base + at;
+      if (at > 0) y -= before;
+      break;
+    }
+    y -= __shfl_sync(0xffffffffu, sum, 31);
+  }
+  c.u = unit_span(p, c.sp, c.qt);
+  c.head = (int)(y / c.u.tiles);
+  c.at = (int)(y - (long long)c.head * c.u.tiles);
+  const int shift = border_shift(p, share, c.at, c.u.tiles);
+  const bool to_end = shift > 0;
+  c.at += shift;
+  if (to_end) c.next_unit(p);
+  return x + shift;
+}
+
+// The last worker that holds a piece of the unit which covers [first, first + tiles) of the line, worker w its first.
+__device__ inline int last_worker(const AttnParams& p, int w, long long share, long long first, int tiles) {
+  int e = w;
+  for (;;) {
+    const long long x = share * (e + 1) - first;                   // border e + 1, from the unit's start
+    if (x >= tiles || x + border_shift(p, share, (int)x, tiles) >= tiles || e + 1 >= p.workers) return e;
+    ++e;
+  }
+}
+
+// Row r of row tile qt: its token's row in the call and position, and its query head.
+struct RowPlace { long long row; int pos, head; bool valid; };
+__device__ __forceinline__ RowPlace row_place(const AttnParams& p, const SeqSpan& sp, int qt, int kv_head, int r) {
+  RowPlace x;
+  const long long R = (long long)qt * p.unit_rows + r;
+  x.valid = R < (long long)sp.fresh * p.group;
+  const int t = x.valid ? fast_div((int)R, p.div_group) : 0;
+  x.row = sp.row0 + t;
+  x.head = kv_head * p.group + (int)(R - (long long)t * p.group);
+  x.pos = x.valid ? sp.len - sp.fresh + t : -1;
+  return x;
+}
+
+// First element of the slot of token `key` for a key-value head; -1 where the table names no page of the cache.
+__device__ __forceinline__ long long slot_offset(const KvView& c, int s, int key, int head) {
+  const int at = fast_div(key, c.div_page);
+  const int page = c.table[s * c.ld_table + at];
+  if (page < 0 || page >= c.n_pages) { kv_report(c, STATUS_BAD_PAGE); return -1; }
+  return page * c.ld_page + (key - at * c.page_size) * c.ld_slot + head * c.ld_head;
+}
+
+__device__ __forceinline__ float as_float(float x) { return x; }
+__device__ __forceinline__ float as_float(__nv_bfloat16 x) { return __bfloat162float(x); }
+__device__ __forceinline__ void from_float(float& d, float x) { d = x; }
+__device__ __forceinline__ void from_float(__nv_bfloat16& d, float x) { d = __float2bfloat16_rn(x); }
+
+// A zero weight times an infinity or a NaN is a NaN, so a value that one row does not see could reach it through the product
+// of its tile.  A row whose sum is not finite although its weights are is formed once more here, by a whole warp, key by key
+// and without the keys it does not see: sum_j 2^(scale_log2 (q . k_j - m)) v_j over tiles [t0, t1) of its unit.
+// Lane i forms columns i, i + 32, ..
+template <typename T, int DH>
+__device__ __noinline__ void exact_row(const AttnParams& p, int s, int kv_head, const UnitSpan& u, int t0, int t1, const RowPlace& x,
+                                       float m, float (&o)[DH / 32]) {
+  const int lane = threadIdx.x & 31;
+  const T* q = (const T*)p.q + x.row * p.ld_q + x.head * p.ld_q_head;
+  float qv[DH / 32];
+#pragma unroll
+  for (int i = 0; i < DH / 32; ++i) { qv[i] = as_float(q[lane + 32 * i]); o[i] = 0.f; }
+  for (int t = t0; t < t1; ++t) {
+    const int base = (t < u.first_tiles ? t : t + u.skip) * p.tile;
+    for (int key = base; key < base + p.tile; ++key) {
+      if (!row_sees(p, x.pos, key)) continue;
+      const long long at = slot_offset(p.c, s, key, kv_head);
+      float z = 0.f, v[DH / 32];
+#pragma unroll
+      for (int i = 0; i < DH / 32; ++i) {
+        const float k = at >= 0 ? as_float(((const T*)p.c.k)[at + lane + 32 * i]) : 0.f;
+        v[i] = at >= 0 ? as_float(((const T*)p.c.v)[at + lane + 32 * i]) : 0.f;
+        z = fmaf(qv[i], k, z);
+      }
+#pragma unroll
+      for (int d = 16; d > 0; d >>= 1) z += __shfl_xor_sync(0xffffffffu, z, d);
+      const float w = ex2((z - m) * p.scale_log2);
+      if (w == 0.f) continue;
+#pragma unroll
+      for (int i = 0; i < DH / 32; ++i) o[i] = fmaf(w, v[i], o[i]);
+    }
+  }
+}
+
+// One worker's walk over its piece of the line.  `begin` and `end` are found by a whole warp and handed to the block.
+struct Piece { Cursor c; long long left, share, ahead; };          // tiles left of the piece; tiles ahead of the cursor
+__device__ inline void find_piece(const AttnParams& p, int w, Piece& piece) {
+  const long long total = p.prefix[p.c.n_seq];
+  piece.share = line_share(p, total);
+  Cursor end;
+  const long long b1 = find_border(p, w + 1, piece.share, total, end);
+  piece.ahead = find_border(p, w, piece.share, total, piece.c);
+  piece.left = b1 - piece.ahead;
+}
+
+// Launches of the kernels on a line that is planned (workers, unit_rows and tile set).
+int attn_rows_tile();
+int launch_rows_bf16(const AttnParams& p, int dh, cudaStream_t s);
+
+}  // namespace pga
+}  // namespace pcm

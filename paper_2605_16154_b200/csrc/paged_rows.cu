@@ -1,0 +1,310 @@
+// Attention of few new tokens over a paged cache in bf16: decoding steps, short chunks, and head dim 32.
+//
+// What bounds it is the reading of the cache, each key and value once for the 16 or 32 rows of a unit (new tokens times the
+// query heads of a key-value head).  Four warps share a tile of 64 keys, 16 each, and run through their unit without
+// waiting for one another: each copies its own keys and values ahead into its own ring of shared memory (cp.async, 16 bytes
+// a lane, zeros for what no row sees), forms scores and weights in registers (mma.sync m16n8k16: a tile of so few rows
+// would leave a tcgen05 tile of 128 rows nearly empty, and the products take a fraction of the time of the loads), and
+// keeps its own running maximum, sum and values.  The warps' sums meet at the unit's end.  The weights enter the product with v
+// as a pair of bf16 values, high and low part, so that they are not rounded: the second product hides behind the loads too.
+#include "async_ptx.cuh"
+#include "paged_attention.cuh"
+
+namespace pcm {
+namespace pga {
+
+constexpr int RB_WARPS = 4, RB_THREADS = RB_WARPS * 32, RB_KEYS = 16, RB_TILE = RB_WARPS * RB_KEYS;
+template <int DH> struct RbCfg {
+  static constexpr int STAGES = DH == 128 ? 3 : DH == 64 ? 6 : 8;
+  static constexpr int ROW = DH * 2, HALF = RB_KEYS * ROW, STAGE = 2 * HALF;       // bytes: a key, 16 keys, keys and values
+  static constexpr int RING = STAGES * STAGE;
+  static constexpr int BYTES = RB_WARPS * RING;
+};
+
+__device__ __forceinline__ void rb_copy16(uint32_t dst, const void* src, bool take) {
+  asm volatile("cp.async.cg.shared.global.L2::256B [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(take ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void rb_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void rb_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+__device__ __forceinline__ void ldm4(uint32_t (&r)[4], uint32_t a) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(a) : "memory");
+}
+__device__ __forceinline__ void ldm4t(uint32_t (&r)[4], uint32_t a) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(a) : "memory");
+}
+__device__ __forceinline__ void mma16816(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+               : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+               : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+// 16-byte chunk c of row r within 16 rows of DH values: eight rows of one chunk never share banks
+template <int DH> __device__ __forceinline__ uint32_t rb_at(int r, int c) {
+  return (uint32_t)(r * RbCfg<DH>::ROW + ((DH >= 64 ? c ^ (r & 7) : c ^ ((r >> 1) & 3)) << 4));
+}
+// high and low bf16 parts of two weights
+__device__ __forceinline__ void split2(float a, float b, uint32_t& hi, uint32_t& lo) {
+  const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
+  const __nv_bfloat162 l = __floats2bfloat162_rn(a - __low2float(h), b - __high2float(h));
+  hi = *reinterpret_cast<const uint32_t*>(&h);
+  lo = *reinterpret_cast<const uint32_t*>(&l);
+}
+
+template <int DH, int MT>
+__global__ void __launch_bounds__(RB_THREADS, 2) attn_rows_bf16_kernel(const __grid_constant__ AttnParams p) {
+  using C = RbCfg<DH>;
+  constexpr int UR = 16 * MT, KT = DH / 16, NT = DH / 8, LEAD = C::STAGES - 1;
+  extern __shared__ __align__(128) uint8_t rb_smem[];
+  __shared__ Piece piece;
+  __shared__ float all_m[RB_WARPS][UR], all_l[RB_WARPS][UR], row_m[UR], row_l[UR];
+  __shared__ int row_bad[UR];
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t4 = lane & 3;
+  const uint32_t ring = smem_u32(rb_smem) + warp * C::RING;
+  const __nv_bfloat16* kp = (const __nv_bfloat16*)p.c.k;
+  const __nv_bfloat16* vp = (const __nv_bfloat16*)p.c.v;
+
+  wait_for_predecessor();
+  if (warp == 0) {
+    Piece own;
+    find_piece(p, blockIdx.x, own);
+    if (lane == 0) piece = own;
+  }
+  __syncthreads();
+  Cursor c = piece.c;
+  long long left = piece.left, ahead = piece.ahead;
+  const long long share = piece.share;
+  int4 job = make_int4(0, 0, 0, -1);
+
+  while (left > 0) {
+    const int t0 = c.at, t1 = (int)min((long long)c.u.tiles, t0 + left), steps = t1 - t0;
+    const bool whole = t0 == 0 && t1 == c.u.tiles;
+    auto first_key = [&](int i) {
+      const int t = t0 + i;
+      return (t < c.u.first_tiles ? t : t + c.u.skip) * RB_TILE + warp * RB_KEYS;
+    };
+    // Where the keys of step i lie: lanes 0 and 1 read the table for keys 0..7 and 8..15, which are of one page each.
+    auto locate = [&](int i) {
+      long long at = -1;
+      if (lane < 2 && i < steps) {
+        const int key = first_key(i) + lane * 8;
+        bool any = false;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) any |= unit_sees(p, c.u, key + k);
+        if (any) at = slot_offset(p.c, c.s, key, c.head);
+      }
+      return at;
+    };
+    auto copy = [&](int i, long long at) {
+      const int key0 = i < steps ? first_key(i) : c.u.end;
+      const long long at0 = __shfl_sync(0xffffffffu, at, 0), at1 = __shfl_sync(0xffffffffu, at, 1);
+      if (key0 < c.u.end) {
+        const uint32_t dst = ring + (i % C::STAGES) * C::STAGE;
+#pragma unroll
+        for (int k = 0; k < RB_KEYS * NT / 32; ++k) {
+          const int ch = lane + 32 * k, r = ch / NT, cc = ch % NT;
+          const long long from = r < 8 ? at0 : at1;
+          const bool take = from >= 0 && unit_sees(p, c.u, key0 + r);
+          const long long e = take ? from + (r & 7) * p.c.ld_slot + cc * 8 : 0;
+          rb_copy16(dst + rb_at<DH>(r, cc), kp + e, take);
+          rb_copy16(dst + C::HALF + rb_at<DH>(r, cc), vp + e, take);
+        }
+      }
+      rb_commit();
+    };
+#pragma unroll 1
+    for (int i = 0; i < LEAD; ++i) copy(i, locate(i));
+    long long at_next = locate(LEAD);
+
+    uint32_t qf[MT][KT][4];
+    int pos[MT][2];
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const RowPlace x = row_place(p, c.sp, c.qt, c.head, mt * 16 + h * 8 + g);
+        pos[mt][h] = x.pos;
+        const __nv_bfloat16* q = (const __nv_bfloat16*)p.q + x.row * p.ld_q + x.head * p.ld_q_head + t4 * 2;
+#pragma unroll
+        for (int k = 0; k < KT; ++k) {
+          qf[mt][k][h] = x.valid ? *reinterpret_cast<const uint32_t*>(q + k * 16) : 0u;
+          qf[mt][k][2 + h] = x.valid ? *reinterpret_cast<const uint32_t*>(q + k * 16 + 8) : 0u;
+        }
+      }
+    const int p_low = row_place(p, c.sp, c.qt, c.head, 0).pos, p_high = c.u.end - 1;
+
+    float o[MT][NT][4], m[MT][2], l[MT][2];
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) {
+      m[mt][0] = m[mt][1] = -INFINITY;
+      l[mt][0] = l[mt][1] = 0.f;
+#pragma unroll
+      for (int n = 0; n < NT; ++n) o[mt][n][0] = o[mt][n][1] = o[mt][n][2] = o[mt][n][3] = 0.f;
+    }
+#pragma unroll 1
+    for (int i = 0; i < steps; ++i) {
+      copy(i + LEAD, at_next);
+      at_next = locate(i + LEAD + 1);
+      rb_wait<LEAD>();
+      __syncwarp();
+      const int key0 = first_key(i);
+      if (key0 < c.u.end) {
+        const uint32_t kb = ring + (i % C::STAGES) * C::STAGE, vb = kb + C::HALF;
+        float z[MT][2][4];
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+          for (int n = 0; n < 2; ++n) z[mt][n][0] = z[mt][n][1] = z[mt][n][2] = z[mt][n][3] = 0.f;
+#pragma unroll
+        for (int k = 0; k < KT; ++k) {
+          uint32_t b[4];
+          ldm4(b, kb + rb_at<DH>((lane & 7) + ((lane >> 4) << 3), k * 2 + ((lane >> 3) & 1)));
+#pragma unroll
+          for (int mt = 0; mt < MT; ++mt) {
+            mma16816(z[mt][0], qf[mt][k], b[0], b[1]);
+            mma16816(z[mt][1], qf[mt][k], b[2], b[3]);
+          }
+        }
+        const bool all_seen = key0 + RB_KEYS - 1 <= p_low &&
+                              (p.window == 0 || key0 > p_high - p.window || key0 + RB_KEYS - 1 < p.sinks);
+        uint32_t hi[MT][4], lo[MT][4];
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            if (!all_seen)
+#pragma unroll
+              for (int n = 0; n < 2; ++n)
+#pragma unroll
+                for (int e = 0; e < 2; ++e)
+                  if (!row_sees(p, pos[mt][h], key0 + n * 8 + t4 * 2 + e)) z[mt][n][h * 2 + e] = -INFINITY;
+            float top = fmaxf(fmaxf(z[mt][0][h * 2], z[mt][0][h * 2 + 1]), fmaxf(z[mt][1][h * 2], z[mt][1][h * 2 + 1]));
+            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+            if (top > m[mt][h]) {
+              const float f = ex2((m[mt][h] - top) * p.scale_log2);
+              m[mt][h] = top;
+              l[mt][h] *= f;
+#pragma unroll
+              for (int n = 0; n < NT; ++n) { o[mt][n][h * 2] *= f; o[mt][n][h * 2 + 1] *= f; }
+            }
+            const float ref = m[mt][h] == -INFINITY ? 0.f : m[mt][h];
+#pragma unroll
+            for (int n = 0; n < 2; ++n) {
+              const float a = ex2((z[mt][n][h * 2] - ref) * p.scale_log2), b = ex2((z[mt][n][h * 2 + 1] - ref) * p.scale_log2);
+              l[mt][h] += a + b;
+              split2(a, b, hi[mt][n * 2 + h], lo[mt][n * 2 + h]);
+            }
+          }
+#pragma unroll
+        for (int n = 0; n < NT; n += 2) {
+          uint32_t b[4];
+          ldm4t(b, vb + rb_at<DH>((lane & 7) + (((lane >> 3) & 1) << 3), n + (lane >> 4)));
+#pragma unroll
+          for (int mt = 0; mt < MT; ++mt) {
+            mma16816(o[mt][n], hi[mt], b[0], b[1]);
+            mma16816(o[mt][n], lo[mt], b[0], b[1]);
+            mma16816(o[mt][n + 1], hi[mt], b[2], b[3]);
+            mma16816(o[mt][n + 1], lo[mt], b[2], b[3]);
+          }
+        }
+      }
+      __syncwarp();                            // the stage is copied over in the next step
+    }
+    // join the warps
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        float s = l[mt][h];
+        s += __shfl_xor_sync(0xffffffffu, s, 1);
+        s += __shfl_xor_sync(0xffffffffu, s, 2);
+        if (t4 == 0) { all_m[warp][mt * 16 + h * 8 + g] = m[mt][h]; all_l[warp][mt * 16 + h * 8 + g] = s; }
+      }
+    rb_wait<0>();
+    __syncthreads();                           // every warp is through with its ring, which takes its sums now
+    float* sums = reinterpret_cast<float*>(rb_smem);
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+          *reinterpret_cast<float2*>(sums + (warp * UR + mt * 16 + h * 8 + g) * DH + n * 8 + t4 * 2) = make_float2(o[mt][n][h * 2], o[mt][n][h * 2 + 1]);
+    if (tid < UR) {
+      float top = -INFINITY, sum = 0.f;
+      for (int w = 0; w < RB_WARPS; ++w) top = fmaxf(top, all_m[w][tid]);
+      const float ref = top == -INFINITY ? 0.f : top;
+      for (int w = 0; w < RB_WARPS; ++w) {
+        const float f = ex2((all_m[w][tid] - ref) * p.scale_log2);
+        sum = fmaf(all_l[w][tid], f, sum);
+        all_m[w][tid] = f;
+      }
+      row_m[tid] = top; row_l[tid] = sum; row_bad[tid] = 0;
+    }
+    __syncthreads();
+    const int slot = 2 * blockIdx.x + (t0 == 0 ? 1 : 0);
+    float* part = p.part + (long long)slot * UR * DH;
+    __nv_bfloat16* out = (__nv_bfloat16*)p.out;
+    for (int i = tid * 2; i < UR * DH; i += RB_THREADS * 2) {
+      const int r = i / DH, e = i - r * DH;
+      const RowPlace x = row_place(p, c.sp, c.qt, c.head, r);
+      if (!x.valid) continue;
+      float a = 0.f, b = 0.f;
+#pragma unroll
+      for (int w = 0; w < RB_WARPS; ++w) {
+        const float2 v = *reinterpret_cast<const float2*>(sums + w * UR * DH + i);
+        a = fmaf(all_m[w][r], v.x, a);
+        b = fmaf(all_m[w][r], v.y, b);
+      }
+      if (!(isfinite(a) && isfinite(b)) && isfinite(row_l[r])) row_bad[r] = 1;
+      if (!whole) {
+        *reinterpret_cast<float2*>(part + i) = make_float2(a, b);
+      } else {
+        const float inv = row_l[r] == 0.f ? 0.f : 1.f / row_l[r];
+        *reinterpret_cast<__nv_bfloat162*>(out + x.row * p.ld_out + x.head * p.ld_out_head + e) = __floats2bfloat162_rn(a * inv, b * inv);
+      }
+    }
+    __syncthreads();
+    for (int r = warp; r < UR; r += RB_WARPS) {
+      const RowPlace x = row_place(p, c.sp, c.qt, c.head, r);
+      if (!x.valid) continue;
+      if (row_bad[r]) {
+        float v[DH / 32];
+        exact_row<__nv_bfloat16, DH>(p, c.s, c.head, c.u, t0, t1, x, row_m[r] == -INFINITY ? 0.f : row_m[r], v);
+#pragma unroll
+        for (int i = 0; i < DH / 32; ++i) {
+          if (!whole) part[r * DH + lane + 32 * i] = v[i];
+          else out[x.row * p.ld_out + x.head * p.ld_out_head + lane + 32 * i] = __float2bfloat16_rn(v[i] / row_l[r]);
+        }
+      }
+      if (lane == 0) {
+        if (!whole) p.part_ml[(long long)slot * UR + r] = make_float2(row_m[r], row_l[r]);
+        else if (p.lse) p.lse[x.row * p.n_heads + x.head] = row_l[r] == 0.f ? -INFINITY : fmaf(row_m[r], p.scale_log2, log2f(row_l[r])) * LN2;
+      }
+    }
+    __syncthreads();
+    if (!whole && t0 == 0) job = make_int4(c.s, c.qt, c.head, last_worker(p, blockIdx.x, share, ahead, c.u.tiles));
+    left -= steps;
+    ahead += steps;
+    if (left > 0) c.next_unit(p);
+  }
+  if (tid == 0) p.jobs[blockIdx.x] = job;
+  let_successor_start();
+}
+
+template <int DH, int MT>
+static int launch_rows(const AttnParams& p, cudaStream_t s) {
+  static unsigned long long seen = 0;
+  if (attr_needed(&seen))
+    PCM_CUDA_TRY(cudaFuncSetAttribute(attn_rows_bf16_kernel<DH, MT>, cudaFuncAttributeMaxDynamicSharedMemorySize, RbCfg<DH>::BYTES));
+  return launch_after_smem(attn_rows_bf16_kernel<DH, MT>, dim3(p.workers), dim3(RB_THREADS), RbCfg<DH>::BYTES, s, p);
+}
+int attn_rows_tile() { return RB_TILE; }
+int launch_rows_bf16(const AttnParams& p, int dh, cudaStream_t s) {
+  if (p.unit_rows == 16) return dh == 128 ? launch_rows<128, 1>(p, s) : dh == 64 ? launch_rows<64, 1>(p, s) : launch_rows<32, 1>(p, s);
+  return dh == 128 ? launch_rows<128, 2>(p, s) : dh == 64 ? launch_rows<64, 2>(p, s) : launch_rows<32, 2>(p, s);
+}
+
+}  // namespace pga
+}  // namespace pcm

@@ -9,10 +9,13 @@ namespace pcm {
 namespace pga {
 
 // ------------------------------------------------------------------------------------------------
-// tiles ahead of every sequence: one block
+// tiles ahead of every sequence: one block a line
 // ------------------------------------------------------------------------------------------------
 constexpr int PLAN_THREADS = 1024;
-__global__ void __launch_bounds__(PLAN_THREADS) attn_plan_kernel(const AttnParams p) {
+// The lines of one call: few rows and many rows a sequence may each have a kernel of their own.
+struct Lines { AttnParams of[2]; };
+__global__ void __launch_bounds__(PLAN_THREADS) attn_plan_kernel(const __grid_constant__ Lines lines) {
+  const AttnParams& p = lines.of[blockIdx.x];
   __shared__ long long warp_sum[PLAN_THREADS / 32];
   __shared__ long long carry;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -64,7 +67,7 @@ constexpr int RF_ROWS = 16, RF_WARPS = 8, RF_KEYS = 16, RF_TILE = RF_WARPS * RF_
 template <int DH> struct RfSmem {
   static constexpr int LDK = DH + 4;                               // a lane per key: rows shifted by a bank group
   static constexpr int WARP = RF_KEYS * LDK + RF_KEYS * DH + RF_KEYS * RF_ROWS;      // keys, values, weights
-  static constexpr int FLOATS = RF_ROWS * DH + RF_WARPS * WARP + RF_WARPS * RF_ROWS * 2 + RF_ROWS * 3;
+  static constexpr int FLOATS = RF_ROWS * DH + RF_WARPS * WARP + RF_WARPS * RF_ROWS * 2 + RF_ROWS * 2;
   static constexpr int BYTES = FLOATS * 4;
 };
 
@@ -87,7 +90,6 @@ __global__ void __launch_bounds__(RF_THREADS) attn_rows_f32_kernel(const __grid_
   float* all_l = all_m + RF_WARPS * RF_ROWS;
   float* row_m = all_l + RF_WARPS * RF_ROWS;                       // joined
   float* row_l = row_m + RF_ROWS;
-  int* row_bad = reinterpret_cast<int*>(row_l + RF_ROWS);
   constexpr int CL = DH / 4, KG = 32 / CL;                         // lanes across a value's columns; keys side by side
   const int col = (lane % CL) * 4, kg = lane / CL, key_lane = lane & 15, half = lane >> 4;
 
@@ -102,6 +104,7 @@ __global__ void __launch_bounds__(RF_THREADS) attn_rows_f32_kernel(const __grid_
   long long left = piece.left, ahead = piece.ahead;
   const long long share = piece.share;
   int4 job = make_int4(0, 0, 0, -1);
+  int redo = 0;
 
   while (left > 0) {
     const int t0 = c.at, t1 = (int)min((long long)c.u.tiles, t0 + left);
@@ -214,37 +217,29 @@ __global__ void __launch_bounds__(RF_THREADS) attn_rows_f32_kernel(const __grid_
         sum = fmaf(all_l[w * RF_ROWS + tid], f, sum);
         all_m[w * RF_ROWS + tid] = f;
       }
-      row_m[tid] = top; row_l[tid] = sum; row_bad[tid] = 0;
+      row_m[tid] = top; row_l[tid] = sum;
     }
     __syncthreads();
     const int slot = 2 * blockIdx.x + (t0 == 0 ? 1 : 0);
     float* part = p.part + (long long)slot * RF_ROWS * DH;
     for (int i = tid; i < RF_ROWS * DH; i += RF_THREADS) {
       const int r = i / DH, e = i - r * DH;
+      const RowPlace x = row_place(p, c.sp, c.qt, c.head, r);
+      if (!x.valid) continue;
       float o = 0.f;
       for (int w = 0; w < RF_WARPS; ++w) o = fmaf(all_m[w * RF_ROWS + r], sm[RF_ROWS * DH + w * S::WARP + i], o);
-      const RowPlace x = row_place(p, c.sp, c.qt, c.head, r);
-      if (!isfinite(o) && isfinite(row_l[r]) && x.valid) row_bad[r] = 1;
-      if (!whole) part[i] = o;
-      else if (x.valid) ((float*)p.out)[x.row * p.ld_out + x.head * p.ld_out_head + e] = row_l[r] == 0.f ? 0.f : o / row_l[r];
+      if (!whole) {
+        part[i] = o;
+      } else {
+        ((float*)p.out)[x.row * p.ld_out + x.head * p.ld_out_head + e] = row_l[r] == 0.f ? 0.f : o / row_l[r];
+        redo |= !isfinite(o) && isfinite(row_l[r]);
+      }
     }
-    __syncthreads();
-    for (int r = warp; r < RF_ROWS; r += RF_WARPS) {
-      const RowPlace x = row_place(p, c.sp, c.qt, c.head, r);
-      if (row_bad[r]) {
-        float o[DH / 32];
-        exact_row<float, DH>(p, c.s, c.head, c.u, t0, t1, x, row_m[r] == -INFINITY ? 0.f : row_m[r], o);
-#pragma unroll
-        for (int i = 0; i < DH / 32; ++i) {
-          if (!whole) part[r * DH + lane + 32 * i] = o[i];
-          else ((float*)p.out)[x.row * p.ld_out + x.head * p.ld_out_head + lane + 32 * i] = o[i] / row_l[r];
-        }
-      }
-      if (lane == 0) {
-        if (!whole) p.part_ml[(long long)slot * RF_ROWS + r] = make_float2(row_m[r], row_l[r]);
-        else if (x.valid && p.lse)
-          p.lse[x.row * p.n_heads + x.head] = row_l[r] == 0.f ? -INFINITY : fmaf(row_m[r], p.scale_log2, log2f(row_l[r])) * LN2;
-      }
+    if (tid < RF_ROWS) {
+      const RowPlace x = row_place(p, c.sp, c.qt, c.head, tid);
+      if (!whole) p.part_ml[(long long)slot * RF_ROWS + tid] = make_float2(row_m[tid], row_l[tid]);
+      else if (x.valid && p.lse)
+        p.lse[x.row * p.n_heads + x.head] = row_l[tid] == 0.f ? -INFINITY : fmaf(row_m[tid], p.scale_log2, log2f(row_l[tid])) * LN2;
     }
     __syncthreads();
     if (!whole && t0 == 0) job = make_int4(c.s, c.qt, c.head, last_worker(p, blockIdx.x, share, ahead, c.u.tiles));
@@ -252,24 +247,58 @@ __global__ void __launch_bounds__(RF_THREADS) attn_rows_f32_kernel(const __grid_
     ahead += t1 - t0;
     if (left > 0) c.next_unit(p);
   }
-  if (tid == 0) p.jobs[blockIdx.x] = job;
+  redo = __syncthreads_or(redo);
+  if (tid == 0) { p.jobs[blockIdx.x] = job; p.redo[blockIdx.x] = redo; }
   let_successor_start();
 }
 
 // ------------------------------------------------------------------------------------------------
-// join of split units: a warp per row, the pieces in the order of their keys
+// join of split units: a warp per row, the pieces in the order of their keys; and rows formed once more
 // ------------------------------------------------------------------------------------------------
 constexpr int JN_WARPS = 8;
+
 template <typename T, int DH>
-__global__ void __launch_bounds__(JN_WARPS * 32) attn_join_kernel(const AttnParams p) {
+__device__ void store_row(const AttnParams& p, const RowPlace& x, const float (&o)[DH / 32]) {
+  T* out = (T*)p.out + x.row * p.ld_out + x.head * p.ld_out_head + (threadIdx.x & 31);
+#pragma unroll
+  for (int i = 0; i < DH / 32; ++i) from_float(out[32 * i], o[i]);
+}
+
+// Row r of the whole units of worker w, where it is not finite.
+template <typename T, int DH>
+__device__ __noinline__ void redo_rows(const AttnParams& p, int w, int r) {
+  Piece piece;
+  find_piece(p, w, piece);
+  Cursor& c = piece.c;
+  while (piece.left > 0) {
+    const RowPlace x = row_place(p, c.sp, c.qt, c.head, r);
+    if (c.at == 0 && c.u.tiles <= piece.left && x.valid) {
+      const T* out = (const T*)p.out + x.row * p.ld_out + x.head * p.ld_out_head + (threadIdx.x & 31);
+      bool fine = true;
+      for (int i = 0; i < DH; i += 32) fine &= (bool)isfinite(as_float(out[i]));
+      if (__any_sync(0xffffffffu, !fine)) {
+        float o[DH / 32];
+        exact_row<T, DH>(p, c.s, c.head, c.u, x, o);
+        store_row<T, DH>(p, x, o);
+      }
+    }
+    piece.left -= min((long long)c.u.tiles - c.at, piece.left);
+    if (piece.left > 0) c.next_unit(p);
+  }
+}
+
+template <typename T, int DH>
+__global__ void __launch_bounds__(JN_WARPS * 32) attn_join_kernel(const __grid_constant__ Lines lines) {
+  const AttnParams& p = lines.of[blockIdx.z];
+  const int w0 = blockIdx.x, r = blockIdx.y * JN_WARPS + (threadIdx.x >> 5), lane = threadIdx.x & 31;
   wait_for_predecessor();
-  const int w0 = blockIdx.x;
+  if (w0 >= p.workers || r >= p.unit_rows) return;
   const int4 job = p.jobs[w0];
+  if (p.redo[w0]) redo_rows<T, DH>(p, w0, r);
   if (job.w < 0) return;
-  const int r = blockIdx.y * JN_WARPS + (threadIdx.x >> 5), lane = threadIdx.x & 31;
   const SeqSpan sp = attn_span(p, job.x, false);
   const RowPlace x = row_place(p, sp, job.y, job.z, r);
-  if (r >= p.unit_rows || !x.valid) return;
+  if (!x.valid) return;
   constexpr int C = DH / 32;
   float top = -INFINITY;
   for (int w = w0; w <= job.w; ++w) top = fmaxf(top, p.part_ml[(long long)(w == w0 ? 2 * w + 1 : 2 * w) * p.unit_rows + r].x);
@@ -285,9 +314,14 @@ __global__ void __launch_bounds__(JN_WARPS * 32) attn_join_kernel(const AttnPara
 #pragma unroll
     for (int i = 0; i < C; ++i) o[i] = fmaf(p.part[at * DH + lane + 32 * i], f, o[i]);
   }
-  const float inv = l == 0.f ? 0.f : 1.f / l;
+  bool fine = true;
 #pragma unroll
-  for (int i = 0; i < C; ++i) from_float(((T*)p.out)[x.row * p.ld_out + x.head * p.ld_out_head + lane + 32 * i], o[i] * inv);
+  for (int i = 0; i < C; ++i) {
+    fine &= (bool)isfinite(o[i]);
+    o[i] = l == 0.f ? 0.f : o[i] / l;
+  }
+  if (__any_sync(0xffffffffu, !fine) && isfinite(l)) exact_row<T, DH>(p, job.x, job.z, unit_span(p, sp, job.y), x, o);
+  store_row<T, DH>(p, x, o);
   if (lane == 0 && p.lse) p.lse[x.row * p.n_heads + x.head] = l == 0.f ? -INFINITY : fmaf(top, p.scale_log2, log2f(l)) * LN2;
 }
 
@@ -303,22 +337,24 @@ static int launch_f32(const AttnParams& p, cudaStream_t s) {
 }
 
 template <typename T, int DH>
-static int launch_join(const AttnParams& p, cudaStream_t s) {
-  return launch_after(attn_join_kernel<T, DH>, dim3(p.workers, ceil_div(p.unit_rows, JN_WARPS)), dim3(JN_WARPS * 32), s, p);
+static int launch_join(const Lines& a, int n, cudaStream_t s) {
+  int workers = 0, rows = 0;
+  for (int i = 0; i < n; ++i) { workers = max(workers, a.of[i].workers); rows = max(rows, a.of[i].unit_rows); }
+  return launch_after(attn_join_kernel<T, DH>, dim3(workers, ceil_div(rows, JN_WARPS), n), dim3(JN_WARPS * 32), s, a);
 }
-
 template <typename T>
-static int launch_join_as(const AttnParams& p, int dh, cudaStream_t s) {
-  return dh == 128 ? launch_join<T, 128>(p, s) : dh == 64 ? launch_join<T, 64>(p, s) : launch_join<T, 32>(p, s);
+static int launch_join_as(const Lines& a, int n, int dh, cudaStream_t s) {
+  return dh == 128 ? launch_join<T, 128>(a, n, s) : dh == 64 ? launch_join<T, 64>(a, n, s) : launch_join<T, 32>(a, n, s);
 }
 
-struct Layout { size_t prefix, jobs, ml, part, total; };
+struct Layout { size_t prefix, jobs, redo, ml, part, total; };
 static Layout layout(int n_seq, int workers, int unit_rows, int dh) {
   Layout y;
   auto up = [](size_t b) { return (b + 255) / 256 * 256; };
   y.prefix = 0;
   y.jobs = y.prefix + up(((size_t)n_seq + 1) * 8);
-  y.ml = y.jobs + up((size_t)workers * 16);
+  y.redo = y.jobs + up((size_t)workers * 16);
+  y.ml = y.redo + up((size_t)workers * 4);
   y.part = y.ml + up((size_t)2 * workers * unit_rows * 8);
   y.total = y.part + up((size_t)2 * workers * unit_rows * dh * 4);
   return y;
@@ -327,6 +363,7 @@ static void place(AttnParams& p, const Layout& y, void* ws) {
   unsigned char* b = (unsigned char*)ws;
   p.prefix = (long long*)(b + y.prefix);
   p.jobs = (int4*)(b + y.jobs);
+  p.redo = (int*)(b + y.redo);
   p.part_ml = (float2*)(b + y.ml);
   p.part = (float*)(b + y.part);
 }
@@ -338,6 +375,32 @@ static bool attn_sizes_ok(const grpo_kv_cache* c, int64_t n_seq, int64_t n_rows,
   return n_rows * (n_heads / c->n_kv_heads) <= PCM_MAX_VOCAB_CALL;              // rows of a key-value head are counted in 32 bits
 }
 
+// Rows of a key-value head (new tokens times group) up to which a sequence goes to the kernel for few rows.
+constexpr int FEW_ROWS = 32;
+
+// The lines of a call: which kernels take part, with what workers; n_lines and their regions of the workspace.
+struct CallPlan { int n; bool chunk[2]; int rows[2], tile[2], workers[2], min_share[2], over[2], up_to[2]; Layout at[2]; size_t total; };
+static CallPlan plan_call(int dtype, int dh, int n_seq, int n_rows, int group, int max_new) {
+  CallPlan c;
+  c.n = 0; c.total = 0;
+  const long long new_most = max_new > 0 && max_new < n_rows ? max_new : n_rows, most = new_most * group;
+  auto add = [&](bool chunk, int rows, int tile, int workers, int min_share, int over, int up_to) {
+    const int i = c.n++;
+    c.chunk[i] = chunk; c.rows[i] = rows; c.tile[i] = tile; c.workers[i] = workers; c.min_share[i] = min_share;
+    c.over[i] = over; c.up_to[i] = up_to;
+    c.at[i] = layout(n_seq, workers, rows, dh);
+    c.total += c.at[i].total;
+  };
+  const int all = 0x7FFFFFFF, sms = sm_count();
+  if (dtype == GRPO_F32) { add(false, RF_ROWS, RF_TILE, 2 * sms, 4, 0, all); return c; }
+  const bool many = most > FEW_ROWS && dh != 32;
+  // every sequence brings max_new rows: none has few
+  const bool few = !many || (long long)n_seq * new_most != n_rows;
+  if (few) add(false, most <= 16 ? 16 : 32, attn_rows_tile(), 2 * sms, 4, 0, many ? FEW_ROWS : all);
+  if (many) add(true, attn_chunk_rows(), attn_chunk_tile(), sms, 4, few ? FEW_ROWS : 0, all);
+  return c;
+}
+
 }  // namespace pga
 }  // namespace pcm
 
@@ -347,7 +410,15 @@ using namespace pcm::pga;
 extern "C" size_t grpo_paged_attention_workspace_bytes(const grpo_kv_cache* cache, int32_t n_seq, int32_t n_rows, int32_t n_heads,
                                                        int32_t max_new) {
   if (!attn_sizes_ok(cache, n_seq, n_rows, n_heads) || max_new < 0) return 0;
-  return layout(n_seq, 2 * sm_count(), cache->dtype == GRPO_F32 ? RF_ROWS : 32, cache->head_dim).total;
+  // as large as any smaller call's: few rows alone, or few and many
+  const int group = n_heads / cache->n_kv_heads;
+  CallPlan c = plan_call(cache->dtype, cache->head_dim, n_seq, n_rows, group, max_new);
+  size_t total = c.total;
+  if (cache->dtype == GRPO_BF16) {
+    total = layout(n_seq, 2 * sm_count(), 32, cache->head_dim).total;
+    if (c.chunk[c.n - 1]) total += c.at[c.n - 1].total;
+  }
+  return total;
 }
 
 extern "C" int grpo_paged_attention(const grpo_kv_cache* cache, const grpo_kv_batch* batch, int32_t n_rows, const void* q, int64_t ld_q,
@@ -383,18 +454,27 @@ extern "C" int grpo_paged_attention(const grpo_kv_cache* cache, const grpo_kv_ba
   cudaStream_t s = (cudaStream_t)stream;
   prof_begin(PC_ATTN, s);
   const bool bf16 = cache->dtype == GRPO_BF16;
-  const long long most_rows = (long long)(max_new > 0 && max_new < n_rows ? max_new : batch->q_off ? n_rows : 1) * p.group;
-  p.unit_rows = !bf16 || most_rows <= 16 ? 16 : 32;
-  p.tile = bf16 ? attn_rows_tile() : RF_TILE;
-  p.over_rows = 0; p.up_to_rows = 0x7FFFFFFF;
-  p.workers = 2 * sm_count(); p.min_share = 4;
-  place(p, layout(batch->n_seq, p.workers, p.unit_rows, dh), workspace);
+  const CallPlan call = plan_call(cache->dtype, dh, batch->n_seq, n_rows, p.group, batch->q_off ? max_new : 1);
+  Lines lines;
+  unsigned char* ws = (unsigned char*)workspace;
+  for (int i = 0; i < call.n; ++i) {
+    AttnParams& a = lines.of[i];
+    a = p;
+    a.unit_rows = call.rows[i]; a.tile = call.tile[i]; a.workers = call.workers[i]; a.min_share = call.min_share[i];
+    a.over_rows = call.over[i]; a.up_to_rows = call.up_to[i];
+    place(a, call.at[i], ws);
+    ws += call.at[i].total;
+  }
   int rc = PCM_OK;
-  attn_plan_kernel<<<1, PLAN_THREADS, 0, s>>>(p);
+  attn_plan_kernel<<<call.n, PLAN_THREADS, 0, s>>>(lines);
   g_launches.fetch_add(1, std::memory_order_relaxed);
   if (cudaPeekAtLastError() != cudaSuccess) { cudaGetLastError(); rc = PCM_ERR_CUDA; }
-  if (rc == PCM_OK) rc = bf16 ? launch_rows_bf16(p, dh, s) : dh == 128 ? launch_f32<128>(p, s) : dh == 64 ? launch_f32<64>(p, s) : launch_f32<32>(p, s);
-  if (rc == PCM_OK) rc = bf16 ? launch_join_as<__nv_bfloat16>(p, dh, s) : launch_join_as<float>(p, dh, s);
+  for (int i = 0; i < call.n && rc == PCM_OK; ++i) {
+    const AttnParams& a = lines.of[i];
+    if (!bf16) rc = dh == 128 ? launch_f32<128>(a, s) : dh == 64 ? launch_f32<64>(a, s) : launch_f32<32>(a, s);
+    else rc = call.chunk[i] ? launch_chunk_bf16(a, dh, s) : launch_rows_bf16(a, dh, s);
+  }
+  if (rc == PCM_OK) rc = bf16 ? launch_join_as<__nv_bfloat16>(lines, call.n, dh, s) : launch_join_as<float>(lines, call.n, dh, s);
   prof_end(s, 0.0, 0.0);
   return rc;
 }

@@ -29,6 +29,7 @@ struct AttnParams {
   int workers, min_share;                      // pieces of the line; tiles of a piece at least
   long long* prefix;                           // [n_seq + 1] tiles ahead of each sequence
   int4* jobs;                                  // [workers] unit that a worker began and left open: sequence, row tile, head, last worker (-1: none)
+  int* redo;                                   // [workers] 1: a row of a whole unit is not finite although its weights are
   float* part;                                 // [2 workers][unit_rows][head_dim], then [2 workers][unit_rows] maxima and sums
   float2* part_ml;
 };
@@ -192,19 +193,18 @@ __device__ __forceinline__ float as_float(__nv_bfloat16 x) { return __bfloat162f
 __device__ __forceinline__ void from_float(float& d, float x) { d = x; }
 __device__ __forceinline__ void from_float(__nv_bfloat16& d, float x) { d = __float2bfloat16_rn(x); }
 
-// A zero weight times an infinity or a NaN is a NaN, so a value that one row does not see could reach it through the product
-// of its tile.  A row whose sum is not finite although its weights are is formed once more here, by a whole warp, key by key
-// and without the keys it does not see: sum_j 2^(scale_log2 (q . k_j - m)) v_j over tiles [t0, t1) of its unit.
-// Lane i forms columns i, i + 32, ..
+// A zero weight times an infinity or a NaN is a NaN, so a value that one row does not see can reach it through the product of
+// its tile.  A row whose values are not finite although the sum of its weights is gets formed once more, by a warp, key by key
+// and without the keys it does not see (the kernels report it in `redo`, the joining kernel mends it).  Lane i holds columns
+// i, i + 32, ..
 template <typename T, int DH>
-__device__ __noinline__ void exact_row(const AttnParams& p, int s, int kv_head, const UnitSpan& u, int t0, int t1, const RowPlace& x,
-                                       float m, float (&o)[DH / 32]) {
+__device__ inline void exact_row(const AttnParams& p, int s, int kv_head, const UnitSpan& u, const RowPlace& x, float (&o)[DH / 32]) {
   const int lane = threadIdx.x & 31;
   const T* q = (const T*)p.q + x.row * p.ld_q + x.head * p.ld_q_head;
-  float qv[DH / 32];
+  float qv[DH / 32], m = -INFINITY, l = 0.f;
 #pragma unroll
   for (int i = 0; i < DH / 32; ++i) { qv[i] = as_float(q[lane + 32 * i]); o[i] = 0.f; }
-  for (int t = t0; t < t1; ++t) {
+  for (int t = 0; t < u.tiles; ++t) {
     const int base = (t < u.first_tiles ? t : t + u.skip) * p.tile;
     for (int key = base; key < base + p.tile; ++key) {
       if (!row_sees(p, x.pos, key)) continue;
@@ -218,12 +218,22 @@ __device__ __noinline__ void exact_row(const AttnParams& p, int s, int kv_head, 
       }
 #pragma unroll
       for (int d = 16; d > 0; d >>= 1) z += __shfl_xor_sync(0xffffffffu, z, d);
+      if (z > m) {
+        const float f = ex2((m - z) * p.scale_log2);
+        m = z;
+        l *= f;
+#pragma unroll
+        for (int i = 0; i < DH / 32; ++i) o[i] *= f;
+      }
       const float w = ex2((z - m) * p.scale_log2);
+      l += w;
       if (w == 0.f) continue;
 #pragma unroll
       for (int i = 0; i < DH / 32; ++i) o[i] = fmaf(w, v[i], o[i]);
     }
   }
+#pragma unroll
+  for (int i = 0; i < DH / 32; ++i) o[i] = l == 0.f ? 0.f : o[i] / l;
 }
 
 // One worker's walk over its piece of the line.  `begin` and `end` are found by a whole warp and handed to the block.
@@ -240,6 +250,9 @@ __device__ inline void find_piece(const AttnParams& p, int w, Piece& piece) {
 // Launches of the kernels on a line that is planned (workers, unit_rows and tile set).
 int attn_rows_tile();
 int launch_rows_bf16(const AttnParams& p, int dh, cudaStream_t s);
+int attn_chunk_rows();
+int attn_chunk_tile();
+int launch_chunk_bf16(const AttnParams& p, int dh, cudaStream_t s);              // head dims 64 and 128
 
 }  // namespace pga
 }  // namespace pcm

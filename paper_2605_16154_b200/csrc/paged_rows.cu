@@ -58,7 +58,6 @@ __global__ void __launch_bounds__(RB_THREADS, 2) attn_rows_bf16_kernel(const __g
   extern __shared__ __align__(128) uint8_t rb_smem[];
   __shared__ Piece piece;
   __shared__ float all_m[RB_WARPS][UR], all_l[RB_WARPS][UR], row_m[UR], row_l[UR];
-  __shared__ int row_bad[UR];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t4 = lane & 3;
   const uint32_t ring = smem_u32(rb_smem) + warp * C::RING;
   const __nv_bfloat16* kp = (const __nv_bfloat16*)p.c.k;
@@ -75,6 +74,7 @@ __global__ void __launch_bounds__(RB_THREADS, 2) attn_rows_bf16_kernel(const __g
   long long left = piece.left, ahead = piece.ahead;
   const long long share = piece.share;
   int4 job = make_int4(0, 0, 0, -1);
+  int redo = 0;
 
   while (left > 0) {
     const int t0 = c.at, t1 = (int)min((long long)c.u.tiles, t0 + left), steps = t1 - t0;
@@ -240,7 +240,7 @@ __global__ void __launch_bounds__(RB_THREADS, 2) attn_rows_bf16_kernel(const __g
         sum = fmaf(all_l[w][tid], f, sum);
         all_m[w][tid] = f;
       }
-      row_m[tid] = top; row_l[tid] = sum; row_bad[tid] = 0;
+      row_m[tid] = top; row_l[tid] = sum;
     }
     __syncthreads();
     const int slot = 2 * blockIdx.x + (t0 == 0 ? 1 : 0);
@@ -257,31 +257,19 @@ __global__ void __launch_bounds__(RB_THREADS, 2) attn_rows_bf16_kernel(const __g
         a = fmaf(all_m[w][r], v.x, a);
         b = fmaf(all_m[w][r], v.y, b);
       }
-      if (!(isfinite(a) && isfinite(b)) && isfinite(row_l[r])) row_bad[r] = 1;
       if (!whole) {
         *reinterpret_cast<float2*>(part + i) = make_float2(a, b);
       } else {
         const float inv = row_l[r] == 0.f ? 0.f : 1.f / row_l[r];
         *reinterpret_cast<__nv_bfloat162*>(out + x.row * p.ld_out + x.head * p.ld_out_head + e) = __floats2bfloat162_rn(a * inv, b * inv);
+        redo |= !(isfinite(a) && isfinite(b)) && isfinite(row_l[r]);
       }
     }
-    __syncthreads();
-    for (int r = warp; r < UR; r += RB_WARPS) {
-      const RowPlace x = row_place(p, c.sp, c.qt, c.head, r);
-      if (!x.valid) continue;
-      if (row_bad[r]) {
-        float v[DH / 32];
-        exact_row<__nv_bfloat16, DH>(p, c.s, c.head, c.u, t0, t1, x, row_m[r] == -INFINITY ? 0.f : row_m[r], v);
-#pragma unroll
-        for (int i = 0; i < DH / 32; ++i) {
-          if (!whole) part[r * DH + lane + 32 * i] = v[i];
-          else out[x.row * p.ld_out + x.head * p.ld_out_head + lane + 32 * i] = __float2bfloat16_rn(v[i] / row_l[r]);
-        }
-      }
-      if (lane == 0) {
-        if (!whole) p.part_ml[(long long)slot * UR + r] = make_float2(row_m[r], row_l[r]);
-        else if (p.lse) p.lse[x.row * p.n_heads + x.head] = row_l[r] == 0.f ? -INFINITY : fmaf(row_m[r], p.scale_log2, log2f(row_l[r])) * LN2;
-      }
+    if (tid < UR) {
+      const RowPlace x = row_place(p, c.sp, c.qt, c.head, tid);
+      if (!whole) p.part_ml[(long long)slot * UR + tid] = make_float2(row_m[tid], row_l[tid]);
+      else if (x.valid && p.lse)
+        p.lse[x.row * p.n_heads + x.head] = row_l[tid] == 0.f ? -INFINITY : fmaf(row_m[tid], p.scale_log2, log2f(row_l[tid])) * LN2;
     }
     __syncthreads();
     if (!whole && t0 == 0) job = make_int4(c.s, c.qt, c.head, last_worker(p, blockIdx.x, share, ahead, c.u.tiles));
@@ -289,7 +277,8 @@ __global__ void __launch_bounds__(RB_THREADS, 2) attn_rows_bf16_kernel(const __g
     ahead += steps;
     if (left > 0) c.next_unit(p);
   }
-  if (tid == 0) p.jobs[blockIdx.x] = job;
+  redo = __syncthreads_or(redo);
+  if (tid == 0) { p.jobs[blockIdx.x] = job; p.redo[blockIdx.x] = redo; }
   let_successor_start();
 }
 

@@ -278,8 +278,10 @@ __device__ __noinline__ void redo_rows(const AttnParams& p, int w, int r) {
       for (int i = 0; i < DH; i += 32) fine &= (bool)isfinite(as_float(out[i]));
       if (__any_sync(0xffffffffu, !fine)) {
         float o[DH / 32];
-        exact_row<T, DH>(p, c.s, c.head, c.u, x, o);
+        const float lse = exact_row<T, DH>(p, c.s, c.head, c.u, x, o);
         store_row<T, DH>(p, x, o);
+        float* at = p.lse + (x.row * p.n_heads + x.head);
+        if (p.lse && (threadIdx.x & 31) == 0 && !(*at == *at)) *at = lse;          // NaN: the row's weights did not fit either
       }
     }
     piece.left -= min((long long)c.u.tiles - c.at, piece.left);
@@ -304,6 +306,7 @@ __global__ void __launch_bounds__(JN_WARPS * 32) attn_join_kernel(const __grid_c
   for (int w = w0; w <= job.w; ++w) top = fmaxf(top, p.part_ml[(long long)(w == w0 ? 2 * w + 1 : 2 * w) * p.unit_rows + r].x);
   const float ref = top == -INFINITY ? 0.f : top;
   float o[C], l = 0.f;
+  bool unfit = false;
 #pragma unroll
   for (int i = 0; i < C; ++i) o[i] = 0.f;
   for (int w = w0; w <= job.w; ++w) {
@@ -311,6 +314,7 @@ __global__ void __launch_bounds__(JN_WARPS * 32) attn_join_kernel(const __grid_c
     const float2 ml = p.part_ml[at];
     const float f = ex2((ml.x - ref) * p.scale_log2);
     l = fmaf(ml.y, f, l);
+    unfit |= ml.y < 0.f;                       // a piece whose weights did not fit
 #pragma unroll
     for (int i = 0; i < C; ++i) o[i] = fmaf(p.part[at * DH + lane + 32 * i], f, o[i]);
   }
@@ -320,9 +324,13 @@ __global__ void __launch_bounds__(JN_WARPS * 32) attn_join_kernel(const __grid_c
     fine &= (bool)isfinite(o[i]);
     o[i] = l == 0.f ? 0.f : o[i] / l;
   }
-  if (__any_sync(0xffffffffu, !fine) && isfinite(l)) exact_row<T, DH>(p, job.x, job.z, unit_span(p, sp, job.y), x, o);
+  float lse = l == 0.f ? -INFINITY : fmaf(top, p.scale_log2, log2f(l)) * LN2;
+  if (unfit || (__any_sync(0xffffffffu, !fine) && isfinite(l))) {
+    const float exact = exact_row<T, DH>(p, job.x, job.z, unit_span(p, sp, job.y), x, o);
+    if (unfit) lse = exact;
+  }
   store_row<T, DH>(p, x, o);
-  if (lane == 0 && p.lse) p.lse[x.row * p.n_heads + x.head] = l == 0.f ? -INFINITY : fmaf(top, p.scale_log2, log2f(l)) * LN2;
+  if (lane == 0 && p.lse) p.lse[x.row * p.n_heads + x.head] = lse;
 }
 
 // ------------------------------------------------------------------------------------------------

@@ -55,10 +55,8 @@ __device__ __forceinline__ int row_tiles(const AttnParams& p, const SeqSpan& sp)
 // i + skip from there on.  Keys at or behind `end`, and from `sinks` up to `low`, are seen by none of them.
 struct UnitSpan { int tiles, first_tiles, skip, end, low; };
 __device__ __forceinline__ UnitSpan unit_span(const AttnParams& p, const SeqSpan& sp, int qt) {
-  const long long r0 = (long long)qt * p.unit_rows;
-  long long r1 = r0 + p.unit_rows;
-  if (r1 > (long long)sp.fresh * p.group) r1 = (long long)sp.fresh * p.group;
-  const int p0 = sp.len - sp.fresh + (int)(r0 / p.group), p1 = sp.len - sp.fresh + (int)((r1 - 1) / p.group);
+  const int r0 = qt * p.unit_rows, r1 = min(r0 + p.unit_rows, sp.fresh * p.group) - 1, first = sp.len - sp.fresh;
+  const int p0 = first + fast_div(r0, p.div_group), p1 = first + fast_div(r1, p.div_group);
   UnitSpan u;
   u.end = p1 >= 0 ? p1 + 1 : 0;
   u.low = p.window > 0 && p0 >= p.window ? p0 - p.window + 1 : 0;
@@ -110,7 +108,7 @@ __device__ __forceinline__ long long line_share(const AttnParams& p, long long t
 }
 // A border at tile `at` of a unit of `tiles`: -at moves it to the unit's start, tiles - at to its end, 0 leaves it.
 __device__ __forceinline__ int border_shift(const AttnParams& p, long long share, int at, int tiles) {
-  const int slack = (int)min(1ll << 20, max((long long)(p.min_share + 1) / 2, share >> 4));
+  const int slack = (int)min(1ll << 20, max((long long)(p.min_share + 1) / 2, share >> 6));
   if (at <= slack && at <= tiles - at) return -at;
   return tiles - at <= slack ? tiles - at : 0;
 }
@@ -171,11 +169,11 @@ __device__ inline int last_worker(const AttnParams& p, int w, long long share, l
 struct RowPlace { long long row; int pos, head; bool valid; };
 __device__ __forceinline__ RowPlace row_place(const AttnParams& p, const SeqSpan& sp, int qt, int kv_head, int r) {
   RowPlace x;
-  const long long R = (long long)qt * p.unit_rows + r;
-  x.valid = R < (long long)sp.fresh * p.group;
-  const int t = x.valid ? fast_div((int)R, p.div_group) : 0;
+  const int R = qt * p.unit_rows + r;          // rows of a sequence are counted in 31 bits, and a unit more
+  x.valid = R < sp.fresh * p.group;
+  const int t = x.valid ? fast_div(R, p.div_group) : 0;
   x.row = sp.row0 + t;
-  x.head = kv_head * p.group + (int)(R - (long long)t * p.group);
+  x.head = kv_head * p.group + (R - t * p.group);
   x.pos = x.valid ? sp.len - sp.fresh + t : -1;
   return x;
 }
@@ -196,9 +194,9 @@ __device__ __forceinline__ void from_float(__nv_bfloat16& d, float x) { d = __fl
 // A zero weight times an infinity or a NaN is a NaN, so a value that one row does not see can reach it through the product of
 // its tile.  A row whose values are not finite although the sum of its weights is gets formed once more, by a warp, key by key
 // and without the keys it does not see (the kernels report it in `redo`, the joining kernel mends it).  Lane i holds columns
-// i, i + 32, ..
+// i, i + 32, ..; returns the log-sum-exp.
 template <typename T, int DH>
-__device__ inline void exact_row(const AttnParams& p, int s, int kv_head, const UnitSpan& u, const RowPlace& x, float (&o)[DH / 32]) {
+__device__ inline float exact_row(const AttnParams& p, int s, int kv_head, const UnitSpan& u, const RowPlace& x, float (&o)[DH / 32]) {
   const int lane = threadIdx.x & 31;
   const T* q = (const T*)p.q + x.row * p.ld_q + x.head * p.ld_q_head;
   float qv[DH / 32], m = -INFINITY, l = 0.f;
@@ -234,6 +232,7 @@ __device__ inline void exact_row(const AttnParams& p, int s, int kv_head, const 
   }
 #pragma unroll
   for (int i = 0; i < DH / 32; ++i) o[i] = l == 0.f ? 0.f : o[i] / l;
+  return l == 0.f ? -INFINITY : fmaf(m, p.scale_log2, log2f(l)) * LN2;
 }
 
 // One worker's walk over its piece of the line.  `begin` and `end` are found by a whole warp and handed to the block.

@@ -7,6 +7,8 @@
 // its end.  A piece of a unit leaves the unnormalised sum of its values, its maximum and its sum of weights in the workspace,
 // and the combining kernel joins a unit's pieces in the order of its keys: nothing depends on which block ran when.
 #pragma once
+#include <cuda.h>
+
 #include "paged.cuh"
 
 namespace pcm {
@@ -247,6 +249,7 @@ __device__ inline void find_piece(const AttnParams& p, int w, Piece& piece) {
 }
 
 // Launches of the kernels on a line that is planned (workers, unit_rows and tile set).
+bool page_map(CUtensorMap* tm, const void* base, const KvView& c, int dh, int box_cols, int box_rows);
 int attn_rows_tile();
 int launch_rows_bf16(const AttnParams& p, int dh, cudaStream_t s);
 int attn_chunk_rows();

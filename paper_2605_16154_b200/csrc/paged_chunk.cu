@@ -692,16 +692,16 @@ static EncodeFn encode_fn() {
   }
   return fn;
 }
-// Pages as [page][slot][head][column], boxes of box_rows slots of one head and 64 columns.
-static bool page_map(CUtensorMap* tm, const void* base, const KvView& c, int dh, int box_rows) {
+// Pages as [page][slot][head][column], boxes of box_rows slots of one head, swizzled rows of box_cols (64 or 32) columns.
+bool page_map(CUtensorMap* tm, const void* base, const KvView& c, int dh, int box_cols, int box_rows) {
   EncodeFn fn = encode_fn();
   if (!fn) return false;
   cuuint64_t dims[4] = {(cuuint64_t)dh, (cuuint64_t)c.n_kv, (cuuint64_t)c.page_size, (cuuint64_t)c.n_pages};
   const cuuint64_t one = (cuuint64_t)dh * 2;                       // a stride of one head or one page leads nowhere
   cuuint64_t strides[3] = {c.n_kv > 1 ? (cuuint64_t)c.ld_head * 2 : one, (cuuint64_t)c.ld_slot * 2, c.n_pages > 1 ? (cuuint64_t)c.ld_page * 2 : one};
-  cuuint32_t box[4] = {64u, 1u, (cuuint32_t)box_rows, 1u}, step[4] = {1, 1, 1, 1};
+  cuuint32_t box[4] = {(cuuint32_t)box_cols, 1u, (cuuint32_t)box_rows, 1u}, step[4] = {1, 1, 1, 1};
   return fn(tm, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(base), dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
-            CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+            box_cols == 64 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 template <int DH>
@@ -709,7 +709,7 @@ static int launch_chunk(const AttnParams& p, cudaStream_t s) {
   int a = p.c.page_size, box = CH_TILE;
   while (a) { const int t = box % a; box = a; a = t; }
   CUtensorMap tm_k, tm_v;
-  if (!page_map(&tm_k, p.c.k, p.c, DH, box) || !page_map(&tm_v, p.c.v, p.c, DH, box)) return PCM_ERR_CUDA;
+  if (!page_map(&tm_k, p.c.k, p.c, DH, 64, box) || !page_map(&tm_v, p.c.v, p.c, DH, 64, box)) return PCM_ERR_CUDA;
   static unsigned long long seen = 0;
   if (attr_needed(&seen))
     PCM_CUDA_TRY(cudaFuncSetAttribute(attn_chunk_kernel<DH>, cudaFuncAttributeMaxDynamicSharedMemorySize, ChCfg<DH>::BYTES));

@@ -2,11 +2,14 @@
 //
 // What bounds it is the reading of the cache, each key and value once for the 16 or 32 rows of a unit (new tokens times the
 // query heads of a key-value head).  Four warps share a tile of 64 keys, 16 each, and run through their unit without
-// waiting for one another: each copies its own keys and values ahead into its own ring of shared memory (cp.async, 16 bytes
-// a lane, zeros for what no row sees), forms scores and weights in registers (mma.sync m16n8k16: a tile of so few rows
-// would leave a tcgen05 tile of 128 rows nearly empty, and the products take a fraction of the time of the loads), and
-// keeps its own running maximum, sum and values.  The warps' sums meet at the unit's end.  The weights enter the product with v
+// waiting for one another: each copies its own keys and values ahead into its own ring of shared memory (TMA, whose one
+// instruction for 8 or 16 keys of a page leaves the warp's time to the products: with 16 bytes a lane a step of 256 sequences took
+// 322 us), forms scores and weights in registers (mma.sync m16n8k16: a tile of so few rows would leave a tcgen05 tile of
+// 128 rows nearly empty, and the products take a fraction of the time of the loads), and keeps its own running maximum, sum
+// and values.  The warps' sums meet at the unit's end.  The weights enter the product with v
 // as a pair of bf16 values, high and low part, so that they are not rounded: the second product hides behind the loads too.
+#include <cuda.h>
+
 #include "async_ptx.cuh"
 #include "paged_attention.cuh"
 
@@ -18,14 +21,20 @@ template <int DH> struct RbCfg {
   static constexpr int STAGES = DH == 128 ? 3 : DH == 64 ? 6 : 8;
   static constexpr int ROW = DH * 2, HALF = RB_KEYS * ROW, STAGE = 2 * HALF;       // bytes: a key, 16 keys, keys and values
   static constexpr int RING = STAGES * STAGE;
-  static constexpr int BYTES = RB_WARPS * RING;
+  static constexpr int SLAB_COLS = DH < 64 ? DH : 64, SLABS = DH / SLAB_COLS;      // columns of a swizzled row
+  static constexpr int SLAB_ROW = SLAB_COLS * 2, SLAB = RB_KEYS * SLAB_ROW;
+  static constexpr int BYTES = RB_WARPS * RING + 1024;             // tiles start on multiples of 1024 bytes
 };
 
-__device__ __forceinline__ void rb_copy16(uint32_t dst, const void* src, bool take) {
-  asm volatile("cp.async.cg.shared.global.L2::256B [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(take ? 16 : 0) : "memory");
+constexpr unsigned long long RB_WAIT_NS = 2000000000ull;
+__device__ __forceinline__ void rb_load_4d(void* dst, const void* tmap, int x, int y, int z, int w, uint64_t* bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];" ::"r"(
+          smem_u32(dst)),
+      "l"(tmap), "r"(smem_u32(bar)), "r"(x), "r"(y), "r"(z), "r"(w)
+      : "memory");
 }
-__device__ __forceinline__ void rb_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N> __device__ __forceinline__ void rb_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+__device__ __forceinline__ void rb_fence_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 __device__ __forceinline__ void ldm4(uint32_t (&r)[4], uint32_t a) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
                : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(a) : "memory");
@@ -39,9 +48,11 @@ __device__ __forceinline__ void mma16816(float (&d)[4], const uint32_t (&a)[4], 
                : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
                : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
-// 16-byte chunk c of row r within 16 rows of DH values: eight rows of one chunk never share banks
+// 16-byte chunk c of row r within 16 rows of DH values, as TMA leaves them: eight rows of one chunk never share banks
 template <int DH> __device__ __forceinline__ uint32_t rb_at(int r, int c) {
-  return (uint32_t)(r * RbCfg<DH>::ROW + ((DH >= 64 ? c ^ (r & 7) : c ^ ((r >> 1) & 3)) << 4));
+  using C = RbCfg<DH>;
+  if (DH < 64) return (uint32_t)(r * C::SLAB_ROW + ((c ^ ((r >> 1) & 3)) << 4));
+  return (uint32_t)((c >> 3) * C::SLAB + r * C::SLAB_ROW + (((c & 7) ^ (r & 7)) << 4));
 }
 // high and low bf16 parts of two weights
 __device__ __forceinline__ void split2(float a, float b, uint32_t& hi, uint32_t& lo) {
@@ -52,16 +63,27 @@ __device__ __forceinline__ void split2(float a, float b, uint32_t& hi, uint32_t&
 }
 
 template <int DH, int MT>
-__global__ void __launch_bounds__(RB_THREADS, 2) attn_rows_bf16_kernel(const __grid_constant__ AttnParams p) {
+__global__ void __launch_bounds__(RB_THREADS, 2) attn_rows_bf16_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ AttnParams p,
+                      const int box_rows) {
   using C = RbCfg<DH>;
   constexpr int UR = 16 * MT, KT = DH / 16, NT = DH / 8, LEAD = C::STAGES - 1;
-  extern __shared__ __align__(128) uint8_t rb_smem[];
+  extern __shared__ uint8_t rb_raw[];
   __shared__ Piece piece;
+  __shared__ uint64_t full[RB_WARPS][C::STAGES];
   __shared__ float all_m[RB_WARPS][UR], all_l[RB_WARPS][UR], row_m[UR], row_l[UR];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t4 = lane & 3;
-  const uint32_t ring = smem_u32(rb_smem) + warp * C::RING;
-  const __nv_bfloat16* kp = (const __nv_bfloat16*)p.c.k;
-  const __nv_bfloat16* vp = (const __nv_bfloat16*)p.c.v;
+  uint8_t* rb_smem = rb_raw + ((1024u - (smem_u32(rb_raw) & 1023u)) & 1023u);
+  uint8_t* my_ring = rb_smem + warp * C::RING;
+  const uint32_t ring = smem_u32(my_ring);
+  if (lane == 0) {
+    for (int i = 0; i < C::STAGES; ++i) mbar_init(&full[warp][i], 1);
+    fence_mbar_init();
+    prefetch_tmap(&tm_k);
+    prefetch_tmap(&tm_v);
+  }
+  __syncwarp();
+  unsigned asked = 0, taken = 0;               // steps copied into the ring and taken from it, over all units
+  bool ok = true;
 
   wait_for_predecessor();
   if (warp == 0) {
@@ -83,38 +105,39 @@ __global__ void __launch_bounds__(RB_THREADS, 2) attn_rows_bf16_kernel(const __g
       const int t = t0 + i;
       return (t < c.u.first_tiles ? t : t + c.u.skip) * RB_TILE + warp * RB_KEYS;
     };
-    // Where the keys of step i lie: lanes 0 and 1 read the table for keys 0..7 and 8..15, which are of one page each.
+    // Where the boxes of step i lie (lane: box): page and slot.  Boxes that no row of the unit sees lie behind the last page,
+    // which reads as zeros.
     auto locate = [&](int i) {
-      long long at = -1;
-      if (lane < 2 && i < steps) {
-        const int key = first_key(i) + lane * 8;
-        bool any = false;
-#pragma unroll
-        for (int k = 0; k < 8; ++k) any |= unit_sees(p, c.u, key + k);
-        if (any) at = slot_offset(p.c, c.s, key, c.head);
+      int2 at = make_int2(p.c.n_pages, 0);
+      if (i < steps) {
+        const int key = first_key(i) + lane * box_rows;
+        if (lane * box_rows < RB_KEYS && key < c.u.end && (key + box_rows > c.u.low || key < p.sinks)) {
+          const int n = fast_div(key, p.c.div_page), page = p.c.table[c.s * p.c.ld_table + n];
+          if (page >= 0 && page < p.c.n_pages) at = make_int2(page, key - n * p.c.page_size);
+          else kv_report(p.c, STATUS_BAD_PAGE);
+        }
       }
       return at;
     };
-    auto copy = [&](int i, long long at) {
-      const int key0 = i < steps ? first_key(i) : c.u.end;
-      const long long at0 = __shfl_sync(0xffffffffu, at, 0), at1 = __shfl_sync(0xffffffffu, at, 1);
-      if (key0 < c.u.end) {
-        const uint32_t dst = ring + (i % C::STAGES) * C::STAGE;
+    auto copy = [&](int i, int2 at) {
+      if (i >= steps || first_key(i) >= c.u.end || !ok) return;    // the same in all lanes
+      const int st = asked % C::STAGES;
+      uint64_t* bar = &full[warp][st];
+      if (lane == 0) mbar_expect_tx(bar, C::STAGE);
+      __syncwarp();
+      if (lane * box_rows < RB_KEYS) {
+        uint8_t* dst = my_ring + st * C::STAGE + lane * box_rows * C::SLAB_ROW;
 #pragma unroll
-        for (int k = 0; k < RB_KEYS * NT / 32; ++k) {
-          const int ch = lane + 32 * k, r = ch / NT, cc = ch % NT;
-          const long long from = r < 8 ? at0 : at1;
-          const bool take = from >= 0 && unit_sees(p, c.u, key0 + r);
-          const long long e = take ? from + (r & 7) * p.c.ld_slot + cc * 8 : 0;
-          rb_copy16(dst + rb_at<DH>(r, cc), kp + e, take);
-          rb_copy16(dst + C::HALF + rb_at<DH>(r, cc), vp + e, take);
+        for (int slab = 0; slab < C::SLABS; ++slab) {
+          rb_load_4d(dst + slab * C::SLAB, &tm_k, slab * 64, c.head, at.y, at.x, bar);
+          rb_load_4d(dst + C::HALF + slab * C::SLAB, &tm_v, slab * 64, c.head, at.y, at.x, bar);
         }
       }
-      rb_commit();
+      ++asked;
     };
 #pragma unroll 1
     for (int i = 0; i < LEAD; ++i) copy(i, locate(i));
-    long long at_next = locate(LEAD);
+    int2 at_next = locate(LEAD);
 
     uint32_t qf[MT][KT][4];
     int pos[MT][2];
@@ -145,11 +168,22 @@ __global__ void __launch_bounds__(RB_THREADS, 2) attn_rows_bf16_kernel(const __g
     for (int i = 0; i < steps; ++i) {
       copy(i + LEAD, at_next);
       at_next = locate(i + LEAD + 1);
-      rb_wait<LEAD>();
-      __syncwarp();
       const int key0 = first_key(i);
-      if (key0 < c.u.end) {
-        const uint32_t kb = ring + (i % C::STAGES) * C::STAGE, vb = kb + C::HALF;
+      if (key0 < c.u.end && ok) {
+        const int st = taken % C::STAGES;
+        ok = __all_sync(0xffffffffu, mbar_wait_bounded(&full[warp][st], (taken / C::STAGES) & 1u, RB_WAIT_NS));
+        ++taken;
+        if (!ok) {                             // (the copies have not landed: the block's results are not meaningful)
+          kv_report(p.c, STATUS_TIMEOUT);
+          break;
+        }
+        const uint32_t kb = ring + st * C::STAGE, vb = kb + C::HALF;
+        if (key0 + RB_KEYS > c.sp.len) {       // slots behind the end of a sequence may never have been written
+          for (int r = max(0, c.sp.len - key0) * NT + lane; r < RB_KEYS * NT; r += 32)
+            *reinterpret_cast<uint4*>(my_ring + st * C::STAGE + C::HALF + rb_at<DH>(r / NT, r % NT)) = make_uint4(0, 0, 0, 0);
+          rb_fence_async();
+          __syncwarp();
+        }
         float z[MT][2][4];
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt)
@@ -221,7 +255,6 @@ __global__ void __launch_bounds__(RB_THREADS, 2) attn_rows_bf16_kernel(const __g
         s += __shfl_xor_sync(0xffffffffu, s, 2);
         if (t4 == 0) { all_m[warp][mt * 16 + h * 8 + g] = m[mt][h]; all_l[warp][mt * 16 + h * 8 + g] = s; }
       }
-    rb_wait<0>();
     __syncthreads();                           // every warp is through with its ring, which takes its sums now
     float* sums = reinterpret_cast<float*>(rb_smem);
 #pragma unroll
@@ -271,12 +304,15 @@ __global__ void __launch_bounds__(RB_THREADS, 2) attn_rows_bf16_kernel(const __g
       else if (x.valid && p.lse)
         p.lse[x.row * p.n_heads + x.head] = row_l[tid] == 0.f ? -INFINITY : fmaf(row_m[tid], p.scale_log2, log2f(row_l[tid])) * LN2;
     }
+    rb_fence_async();                          // the ring goes back from sums to copies
     __syncthreads();
     if (!whole && t0 == 0) job = make_int4(c.s, c.qt, c.head, last_worker(p, blockIdx.x, share, ahead, c.u.tiles));
     left -= steps;
     ahead += steps;
     if (left > 0) c.next_unit(p);
   }
+  if (!ok)                                     // nothing may land after the block is gone
+    for (; taken < asked; ++taken) mbar_wait_bounded(&full[warp][taken % C::STAGES], (taken / C::STAGES) & 1u, RB_WAIT_NS / 8);
   redo = __syncthreads_or(redo);
   if (tid == 0) { p.jobs[blockIdx.x] = job; p.redo[blockIdx.x] = redo; }
   let_successor_start();
@@ -287,7 +323,10 @@ static int launch_rows(const AttnParams& p, cudaStream_t s) {
   static unsigned long long seen = 0;
   if (attr_needed(&seen))
     PCM_CUDA_TRY(cudaFuncSetAttribute(attn_rows_bf16_kernel<DH, MT>, cudaFuncAttributeMaxDynamicSharedMemorySize, RbCfg<DH>::BYTES));
-  return launch_after_smem(attn_rows_bf16_kernel<DH, MT>, dim3(p.workers), dim3(RB_THREADS), RbCfg<DH>::BYTES, s, p);
+  const int box = p.c.page_size % RB_KEYS ? 8 : RB_KEYS;
+  CUtensorMap tm_k, tm_v;
+  if (!page_map(&tm_k, p.c.k, p.c, DH, RbCfg<DH>::SLAB_COLS, box) || !page_map(&tm_v, p.c.v, p.c, DH, RbCfg<DH>::SLAB_COLS, box)) return PCM_ERR_CUDA;
+  return launch_after_smem(attn_rows_bf16_kernel<DH, MT>, dim3(p.workers), dim3(RB_THREADS), RbCfg<DH>::BYTES, s, tm_k, tm_v, p, box);
 }
 int attn_rows_tile() { return RB_TILE; }
 int launch_rows_bf16(const AttnParams& p, int dh, cudaStream_t s) {

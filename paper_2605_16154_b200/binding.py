@@ -6,6 +6,7 @@ compiled library raises.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes as C
 import os
 from typing import Dict, Optional
@@ -729,6 +730,7 @@ ROTARY_PLAIN, ROTARY_LINEAR, ROTARY_BASE, ROTARY_PARTS = 0, 1, 2, 3
 _ROTARY_INTERLEAVED, _ROTARY_INVERSE = 1, 2
 STATUS_BAD_PAGE, STATUS_BAD_LENGTH = 64, 128
 _f64 = torch.float64
+_NO_SWITCH = contextlib.nullcontext()
 
 
 def grpo_rotary_freqs(rot_dim: int, base: float = 10000.0, scaling: int = ROTARY_PLAIN, factor: float = 1.0,
@@ -772,9 +774,12 @@ def grpo_rotary(x: torch.Tensor, pos: torch.Tensor, turns: torch.Tensor, interle
     dev = x.device
     tp, rot = _turns(call, turns, dev)
     if out is None:
-        out = torch.empty((n, h, d), dtype=x.dtype, device=dev)
-    odt, op, ldo, ldoh, on, oh, od = _heads(call, out, dev)
-    _require(call, odt == dt and on == n and oh == h and od == d and pos is not None)
+        out = x.new_empty(n, h, d)
+        op, ldo, ldoh = out.data_ptr(), h * d, d
+    else:
+        odt, op, ldo, ldoh, on, oh, od = _heads(call, out, dev)
+        _require(call, odt == dt and on == n and oh == h and od == d)
+    _require(call, pos is not None)
     _launch(call, dev, _lib.grpo_rotary, dt, xp, ld, ldh, n, h, d, rot, tp, amplitude, _vector(call, pos, dev, _i32, n),
             (_ROTARY_INTERLEAVED if interleaved else 0) | (_ROTARY_INVERSE if inverse else 0), op, ldo, ldoh)
     return out
@@ -830,9 +835,11 @@ def grpo_rotary_cache(q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tenso
         qdt, qp, ldq, ldqh, qn, h, qd = _heads(call, q, dev)
         _require(call, qdt == dt and qn == n and qd == d)
         if q_out is None:
-            q_out = torch.empty((n, h, d), dtype=q.dtype, device=dev)
-        odt, op, ldo, ldoh, on, oh, od = _heads(call, q_out, dev)
-        _require(call, odt == dt and on == n and oh == h and od == d)
+            q_out = q.new_empty(n, h, d)
+            op, ldo, ldoh = q_out.data_ptr(), h * d, d
+        else:
+            odt, op, ldo, ldoh, on, oh, od = _heads(call, q_out, dev)
+            _require(call, odt == dt and on == n and oh == h and od == d)
     else:
         _require(call, q_out is None)
     _launch(call, dev, _lib.grpo_rotary_cache, cache, batch, n, qp, ldq, ldqh, h, kp, ldk, ldkh, vp, ldv, ldvh, rot, tp, amplitude,
@@ -865,24 +872,30 @@ def grpo_paged_attention(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.
     _require(call, dt == cache.dtype and d == cache.head_dim)
     _size(call, window, sinks, max_new)
     if out is None:
-        out = torch.empty((n, h, d), dtype=q.dtype, device=dev)
+        out = q.new_empty(n, h, d)
         op, ldo, ldoh = out.data_ptr(), h * d, d
     else:
         odt, op, ldo, ldoh, on, oh, od = _heads(call, out, dev)
         _require(call, odt == dt and on == n and oh == h and od == d)
-    if lse is None and want_lse:
-        lse = torch.empty((n, h), dtype=_f32, device=dev)
-    lp = _vector(call, lse, dev, _f32, n * h)
+    lp = None
+    if lse is not None:
+        lp = _vector(call, lse, dev, _f32, n * h)
+    elif want_lse:
+        lse = q.new_empty(n, h, dtype=_f32)
+        lp = lse.data_ptr()
     sp = _vector(call, status, dev, _i32, 1)
     if scale is None:
         scale = d ** -0.5
-
-    def run(stream):
+    i = dev.index
+    with _NO_SWITCH if torch._C._cuda_getDevice() == i else torch.cuda.device(dev):       # the workspace's size is the device's
         need = _lib.grpo_paged_attention_workspace_bytes(cache, batch.n_seq, n, h, max_new)
+        if workspace is None:
+            workspace = q.new_empty(need + 256, dtype=_u8)
         ws, wp, wn = _workspace(call, workspace, need, dev)
-        return _lib.grpo_paged_attention(cache, batch, n, qp, ldq, ldqh, h, scale, window, sinks, max_new, op, ldo, ldoh, lp, sp,
-                                         wp, wn, stream)
-    _launch(call, dev, run)
+        rc = _lib.grpo_paged_attention(cache, batch, n, qp, ldq, ldqh, h, scale, window, sinks, max_new, op, ldo, ldoh, lp, sp, wp, wn,
+                                       torch._C._cuda_getCurrentRawStream(i))
+    if rc != 0:
+        raise PcmError(call, rc)
     return out, lse
 
 

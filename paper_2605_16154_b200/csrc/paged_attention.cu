@@ -16,46 +16,8 @@ constexpr int PLAN_THREADS = 1024;
 struct Lines { AttnParams of[2]; };
 __global__ void __launch_bounds__(PLAN_THREADS) attn_plan_kernel(const __grid_constant__ Lines lines) {
   const AttnParams& p = lines.of[blockIdx.x];
-  __shared__ long long warp_sum[PLAN_THREADS / 32];
-  __shared__ long long carry;
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  if (tid == 0) { carry = 0; p.prefix[0] = 0; }
-  for (int base = 0; base < p.c.n_seq; base += PLAN_THREADS) {
-    const int s = base + tid;
-    SeqSpan sp{0, 0, 0};
-    if (s < p.c.n_seq) sp = attn_span(p, s, true);
-    const int nqt = row_tiles(p, sp);
-    long long sum = 0;
-    if (nqt <= 2)
-      for (int qt = 0; qt < nqt; ++qt) sum += unit_span(p, sp, qt).tiles;
-    for (unsigned many = __ballot_sync(0xffffffffu, nqt > 2); many; many &= many - 1) {
-      const int from = __ffs(many) - 1;                            // a sequence of many row tiles takes the whole warp
-      SeqSpan o;
-      o.row0 = 0;
-      o.fresh = __shfl_sync(0xffffffffu, sp.fresh, from);
-      o.len = __shfl_sync(0xffffffffu, sp.len, from);
-      const int n = row_tiles(p, o);
-      long long mine = 0;
-      for (int qt = lane; qt < n; qt += 32) mine += unit_span(p, o, qt).tiles;
-#pragma unroll
-      for (int d = 16; d > 0; d >>= 1) mine += __shfl_xor_sync(0xffffffffu, mine, d);
-      if (lane == from) sum = mine;
-    }
-    sum *= p.c.n_kv;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const long long t = __shfl_up_sync(0xffffffffu, sum, o);
-      if (lane >= o) sum += t;
-    }
-    if (lane == 31) warp_sum[warp] = sum;
-    __syncthreads();
-    long long before = carry;
-    for (int w = 0; w < warp; ++w) before += warp_sum[w];
-    if (s < p.c.n_seq) p.prefix[s + 1] = before + sum;
-    __syncthreads();
-    if (tid == PLAN_THREADS - 1) carry = before + sum;
-    __syncthreads();
-  }
+  __shared__ long long sums[PLAN_THREADS / 32 + 1];
+  if (p.prefix) line_prefix(p, p.prefix, sums, true);
   let_successor_start();
 }
 
@@ -94,11 +56,7 @@ __global__ void __launch_bounds__(RF_THREADS) attn_rows_f32_kernel(const __grid_
   const int col = (lane % CL) * 4, kg = lane / CL, key_lane = lane & 15, half = lane >> 4;
 
   wait_for_predecessor();
-  if (warp == 0) {
-    Piece own;
-    find_piece(p, blockIdx.x, own);
-    if (lane == 0) piece = own;
-  }
+  block_piece(p, sm, &piece);
   __syncthreads();
   Cursor c = piece.c;
   long long left = piece.left, ahead = piece.ahead;
@@ -248,7 +206,7 @@ __global__ void __launch_bounds__(RF_THREADS) attn_rows_f32_kernel(const __grid_
     if (left > 0) c.next_unit(p);
   }
   redo = __syncthreads_or(redo);
-  if (tid == 0) { p.jobs[blockIdx.x] = job; p.redo[blockIdx.x] = redo; }
+  if (tid == 0) { p.jobs[blockIdx.x] = job; p.redo[blockIdx.x] = redo; p.pieces[blockIdx.x] = piece; }
   let_successor_start();
 }
 
@@ -267,8 +225,7 @@ __device__ void store_row(const AttnParams& p, const RowPlace& x, const float (&
 // Row r of the whole units of worker w, where it is not finite.
 template <typename T, int DH>
 __device__ __noinline__ void redo_rows(const AttnParams& p, int w, int r) {
-  Piece piece;
-  find_piece(p, w, piece);
+  Piece piece = p.pieces[w];
   Cursor& c = piece.c;
   while (piece.left > 0) {
     const RowPlace x = row_place(p, c.sp, c.qt, c.head, r);
@@ -355,14 +312,15 @@ static int launch_join_as(const Lines& a, int n, int dh, cudaStream_t s) {
   return dh == 128 ? launch_join<T, 128>(a, n, s) : dh == 64 ? launch_join<T, 64>(a, n, s) : launch_join<T, 32>(a, n, s);
 }
 
-struct Layout { size_t prefix, jobs, redo, ml, part, total; };
+struct Layout { size_t prefix, jobs, redo, pieces, ml, part, total; };
 static Layout layout(int n_seq, int workers, int unit_rows, int dh) {
   Layout y;
   auto up = [](size_t b) { return (b + 255) / 256 * 256; };
   y.prefix = 0;
   y.jobs = y.prefix + up(((size_t)n_seq + 1) * 8);
   y.redo = y.jobs + up((size_t)workers * 16);
-  y.ml = y.redo + up((size_t)workers * 4);
+  y.pieces = y.redo + up((size_t)workers * 4);
+  y.ml = y.pieces + up((size_t)workers * sizeof(Piece));
   y.part = y.ml + up((size_t)2 * workers * unit_rows * 8);
   y.total = y.part + up((size_t)2 * workers * unit_rows * dh * 4);
   return y;
@@ -372,6 +330,7 @@ static void place(AttnParams& p, const Layout& y, void* ws) {
   p.prefix = (long long*)(b + y.prefix);
   p.jobs = (int4*)(b + y.jobs);
   p.redo = (int*)(b + y.redo);
+  p.pieces = (Piece*)(b + y.pieces);
   p.part_ml = (float2*)(b + y.ml);
   p.part = (float*)(b + y.part);
 }
@@ -387,10 +346,10 @@ static bool attn_sizes_ok(const grpo_kv_cache* c, int64_t n_seq, int64_t n_rows,
 constexpr int FEW_ROWS = 32;
 
 // The lines of a call: which kernels take part, with what workers; n_lines and their regions of the workspace.
-struct CallPlan { int n; bool chunk[2]; int rows[2], tile[2], workers[2], min_share[2], over[2], up_to[2]; Layout at[2]; size_t total; };
+struct CallPlan { int n; bool planned, self[2], chunk[2]; int rows[2], tile[2], workers[2], min_share[2], over[2], up_to[2]; Layout at[2]; size_t total; };
 static CallPlan plan_call(int dtype, int dh, int n_seq, int n_rows, int group, int max_new) {
   CallPlan c;
-  c.n = 0; c.total = 0;
+  c.n = 0; c.total = 0; c.planned = false;
   const long long new_most = max_new > 0 && max_new < n_rows ? max_new : n_rows, most = new_most * group;
   auto add = [&](bool chunk, int rows, int tile, int workers, int min_share, int over, int up_to) {
     const int i = c.n++;
@@ -398,13 +357,16 @@ static CallPlan plan_call(int dtype, int dh, int n_seq, int n_rows, int group, i
     c.over[i] = over; c.up_to[i] = up_to;
     c.at[i] = layout(n_seq, workers, rows, dh);
     c.total += c.at[i].total;
+    // most row tiles that the call's rows can make
+    c.self[i] = n_seq <= SELF_PLANNED && (long long)n_rows * group / rows + n_seq <= SELF_PLANNED;
+    c.planned |= !c.self[i];
   };
   const int all = 0x7FFFFFFF, sms = sm_count();
   if (dtype == GRPO_F32) { add(false, RF_ROWS, RF_TILE, 2 * sms, 4, 0, all); return c; }
   const bool many = most > FEW_ROWS && dh != 32;
   // every sequence brings max_new rows: none has few
   const bool few = !many || (long long)n_seq * new_most != n_rows;
-  if (few) add(false, most <= 16 ? 16 : 32, attn_rows_tile(), 2 * sms, 4, 0, many ? FEW_ROWS : all);
+  if (few) add(false, most <= 16 ? 16 : 32, attn_rows_tile(), 2 * sms, 1, 0, many ? FEW_ROWS : all);
   if (many) add(true, attn_chunk_rows(), attn_chunk_tile(), sms, 4, few ? FEW_ROWS : 0, all);
   return c;
 }
@@ -471,12 +433,15 @@ extern "C" int grpo_paged_attention(const grpo_kv_cache* cache, const grpo_kv_ba
     a.unit_rows = call.rows[i]; a.tile = call.tile[i]; a.workers = call.workers[i]; a.min_share = call.min_share[i];
     a.over_rows = call.over[i]; a.up_to_rows = call.up_to[i];
     place(a, call.at[i], ws);
+    if (call.self[i]) a.prefix = nullptr;
     ws += call.at[i].total;
   }
   int rc = PCM_OK;
-  attn_plan_kernel<<<call.n, PLAN_THREADS, 0, s>>>(lines);
-  g_launches.fetch_add(1, std::memory_order_relaxed);
-  if (cudaPeekAtLastError() != cudaSuccess) { cudaGetLastError(); rc = PCM_ERR_CUDA; }
+  if (call.planned) {
+    attn_plan_kernel<<<call.n, PLAN_THREADS, 0, s>>>(lines);
+    g_launches.fetch_add(1, std::memory_order_relaxed);
+    if (cudaPeekAtLastError() != cudaSuccess) { cudaGetLastError(); rc = PCM_ERR_CUDA; }
+  }
   for (int i = 0; i < call.n && rc == PCM_OK; ++i) {
     const AttnParams& a = lines.of[i];
     if (!bf16) rc = dh == 128 ? launch_f32<128>(a, s) : dh == 64 ? launch_f32<64>(a, s) : launch_f32<32>(a, s);

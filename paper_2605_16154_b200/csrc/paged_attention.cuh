@@ -17,6 +17,7 @@ namespace pga {
 constexpr float LOG2E = 1.4426950408889634f;
 constexpr float LN2 = 0.6931471805599453f;
 
+struct Piece;
 struct AttnParams {
   KvView c;
   const void* q; long long ld_q, ld_q_head;
@@ -29,8 +30,9 @@ struct AttnParams {
   int unit_rows, tile;                         // rows of a unit, keys of a tile (a power of two)
   int over_rows, up_to_rows;                   // this kernel's sequences: over_rows < new tokens * group <= up_to_rows
   int workers, min_share;                      // pieces of the line; tiles of a piece at least
-  long long* prefix;                           // [n_seq + 1] tiles ahead of each sequence
+  long long* prefix;                           // [n_seq + 1] tiles ahead of each sequence; NULL: every block finds them itself
   int4* jobs;                                  // [workers] unit that a worker began and left open: sequence, row tile, head, last worker (-1: none)
+  Piece* pieces;                               // [workers]
   int* redo;                                   // [workers] 1: a row of a whole unit is not finite although its weights are
   float* part;                                 // [2 workers][unit_rows][head_dim], then [2 workers][unit_rows] maxima and sums
   float2* part_ml;
@@ -116,19 +118,19 @@ __device__ __forceinline__ int border_shift(const AttnParams& p, long long share
 }
 
 // Where border `i` of the line falls; called by a whole warp.  Returns the tiles ahead of it.
-__device__ inline long long find_border(const AttnParams& p, int i, long long share, long long total, Cursor& c) {
+__device__ inline long long find_border(const AttnParams& p, const long long* prefix, int i, long long share, long long total, Cursor& c) {
   const int lane = threadIdx.x & 31;
   const long long x = share * i;
   if (x >= total) { c.s = p.c.n_seq; c.qt = c.head = c.at = c.nqt = 0; return total; }
   int lo = 0, hi = p.c.n_seq - 1;              // the sequence with prefix[s] <= x < prefix[s + 1]
   while (lo < hi) {
     const int mid = (lo + hi) >> 1;
-    if (p.prefix[mid + 1] > x) hi = mid; else lo = mid + 1;
+    if (prefix[mid + 1] > x) hi = mid; else lo = mid + 1;
   }
   c.s = lo;
   c.sp = attn_span(p, lo, false);
   c.nqt = row_tiles(p, c.sp);
-  long long y = x - p.prefix[lo];
+  long long y = x - prefix[lo];
   for (int base = 0;; base += 32) {
     const int qt = base + lane;
     long long sum = qt < c.nqt ? (long long)unit_span(p, c.sp, qt).tiles * p.c.n_kv : 0;
@@ -239,13 +241,78 @@ __device__ inline float exact_row(const AttnParams& p, int s, int kv_head, const
 
 // One worker's walk over its piece of the line.  `begin` and `end` are found by a whole warp and handed to the block.
 struct Piece { Cursor c; long long left, share, ahead; };          // tiles left of the piece; tiles ahead of the cursor
-__device__ inline void find_piece(const AttnParams& p, int w, Piece& piece) {
-  const long long total = p.prefix[p.c.n_seq];
+__device__ inline void find_piece(const AttnParams& p, const long long* prefix, int w, Piece& piece) {
+  const long long total = prefix[p.c.n_seq];
   piece.share = line_share(p, total);
   Cursor end;
-  const long long b1 = find_border(p, w + 1, piece.share, total, end);
-  piece.ahead = find_border(p, w, piece.share, total, piece.c);
+  const long long b1 = find_border(p, prefix, w + 1, piece.share, total, end);
+  piece.ahead = find_border(p, prefix, w, piece.share, total, piece.c);
   piece.left = b1 - piece.ahead;
+}
+
+// Tiles ahead of every sequence, by a whole block; `sums` takes a word per warp and one more.
+__device__ inline void line_prefix(const AttnParams& p, long long* prefix, long long* sums, bool report) {
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, warps = (int)blockDim.x >> 5;
+  long long* carry = sums + warps;
+  if (tid == 0) { *carry = 0; prefix[0] = 0; }
+  __syncthreads();
+  for (int base = 0; base < p.c.n_seq; base += (int)blockDim.x) {
+    const int s = base + tid;
+    SeqSpan sp{0, 0, 0};
+    if (s < p.c.n_seq) sp = attn_span(p, s, report);
+    const int nqt = row_tiles(p, sp);
+    long long sum = 0;
+    if (nqt <= 2)
+      for (int qt = 0; qt < nqt; ++qt) sum += unit_span(p, sp, qt).tiles;
+    for (unsigned many = __ballot_sync(0xffffffffu, nqt > 2); many; many &= many - 1) {
+      const int from = __ffs(many) - 1;                            // a sequence of many row tiles takes the whole warp
+      SeqSpan o;
+      o.row0 = 0;
+      o.fresh = __shfl_sync(0xffffffffu, sp.fresh, from);
+      o.len = __shfl_sync(0xffffffffu, sp.len, from);
+      const int n = row_tiles(p, o);
+      long long mine = 0;
+      for (int qt = lane; qt < n; qt += 32) mine += unit_span(p, o, qt).tiles;
+#pragma unroll
+      for (int d = 16; d > 0; d >>= 1) mine += __shfl_xor_sync(0xffffffffu, mine, d);
+      if (lane == from) sum = mine;
+    }
+    sum *= p.c.n_kv;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const long long t = __shfl_up_sync(0xffffffffu, sum, o);
+      if (lane >= o) sum += t;
+    }
+    if (lane == 31) sums[warp] = sum;
+    __syncthreads();
+    long long before = *carry;
+    for (int w = 0; w < warp; ++w) before += sums[w];
+    if (s < p.c.n_seq) prefix[s + 1] = before + sum;
+    __syncthreads();
+    if (tid == (int)blockDim.x - 1) *carry = before + sum;
+    __syncthreads();
+  }
+}
+
+// Sequences and row tiles (as the host can bound them) up to which every block finds its piece from the lengths: a launch and
+// the reads of its results less, 4 of 16 us of a step of one sequence.
+constexpr int SELF_PLANNED = 1024;
+constexpr int SELF_BYTES = (SELF_PLANNED + 1 + 33) * 8;            // prefix and sums
+
+// The block's piece of the line, from the plan's results or from the lengths; `scratch`: SELF_BYTES of shared memory that is
+// free until the block's next barrier after this.
+__device__ inline void block_piece(const AttnParams& p, void* scratch, Piece* piece) {
+  const long long* prefix = p.prefix;
+  if (!prefix) {
+    long long* own = (long long*)scratch;
+    line_prefix(p, own, own + SELF_PLANNED + 1, blockIdx.x == 0);
+    prefix = own;
+  }
+  if (threadIdx.x < 32) {
+    Piece own;
+    find_piece(p, prefix, blockIdx.x, own);
+    if (threadIdx.x == 0) *piece = own;
+  }
 }
 
 // Launches of the kernels on a line that is planned (workers, unit_rows and tile set).

@@ -246,11 +246,9 @@ attn_chunk_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
     tmem_relinquish();
   }
   wait_for_predecessor();
-  if (warp == 0) {
-    Piece own;
-    find_piece(p, blockIdx.x, own);
-    if (lane == 0) sh.piece = own;
-  }
+  block_piece(p, base + C::RING_AT, &sh.piece);
+  ch_fence_async();                            // what it needed of the ring goes to the copies
+  if (tid == 0) p.pieces[blockIdx.x] = sh.piece;
   tc_fence_before();
   __syncthreads();
   tc_fence_after();

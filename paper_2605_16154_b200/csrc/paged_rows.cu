@@ -86,11 +86,8 @@ __global__ void __launch_bounds__(RB_THREADS, 2) attn_rows_bf16_kernel(const __g
   bool ok = true;
 
   wait_for_predecessor();
-  if (warp == 0) {
-    Piece own;
-    find_piece(p, blockIdx.x, own);
-    if (lane == 0) piece = own;
-  }
+  block_piece(p, rb_smem, &piece);
+  rb_fence_async();                            // what it needed of the ring goes to the copies
   __syncthreads();
   Cursor c = piece.c;
   long long left = piece.left, ahead = piece.ahead;
@@ -202,26 +199,43 @@ __global__ void __launch_bounds__(RB_THREADS, 2) attn_rows_bf16_kernel(const __g
         const bool all_seen = key0 + RB_KEYS - 1 <= p_low &&
                               (p.window == 0 || key0 > p_high - p.window || key0 + RB_KEYS - 1 < p.sinks);
         uint32_t hi[MT][4], lo[MT][4];
+        if (!all_seen)
+#pragma unroll
+          for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+              if (!row_sees(p, pos[mt][(e >> 1) & 1], key0 + (e >> 2) * 8 + t4 * 2 + (e & 1))) z[mt][e >> 2][e & 3] = -INFINITY;
+        float top[MT][2];
+        bool rise = false;
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            if (!all_seen)
+          for (int h = 0; h < 2; ++h)
+            top[mt][h] = fmaxf(fmaxf(z[mt][0][h * 2], z[mt][0][h * 2 + 1]), fmaxf(z[mt][1][h * 2], z[mt][1][h * 2 + 1]));
 #pragma unroll
-              for (int n = 0; n < 2; ++n)
+        for (int d = 1; d <= 2; d <<= 1)
 #pragma unroll
-                for (int e = 0; e < 2; ++e)
-                  if (!row_sees(p, pos[mt][h], key0 + n * 8 + t4 * 2 + e)) z[mt][n][h * 2 + e] = -INFINITY;
-            float top = fmaxf(fmaxf(z[mt][0][h * 2], z[mt][0][h * 2 + 1]), fmaxf(z[mt][1][h * 2], z[mt][1][h * 2 + 1]));
-            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
-            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
-            if (top > m[mt][h]) {
-              const float f = ex2((m[mt][h] - top) * p.scale_log2);
-              m[mt][h] = top;
+          for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) top[mt][h] = fmaxf(top[mt][h], __shfl_xor_sync(0xffffffffu, top[mt][h], d));
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) rise |= top[mt][0] > m[mt][0] || top[mt][1] > m[mt][1];
+        if (__any_sync(0xffffffffu, rise)) {
+#pragma unroll
+          for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              const float to = fmaxf(m[mt][h], top[mt][h]), f = to == -INFINITY ? 1.f : ex2((m[mt][h] - to) * p.scale_log2);
+              m[mt][h] = to;
               l[mt][h] *= f;
 #pragma unroll
               for (int n = 0; n < NT; ++n) { o[mt][n][h * 2] *= f; o[mt][n][h * 2 + 1] *= f; }
             }
+        }
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
             const float ref = m[mt][h] == -INFINITY ? 0.f : m[mt][h];
 #pragma unroll
             for (int n = 0; n < 2; ++n) {
@@ -230,17 +244,18 @@ __global__ void __launch_bounds__(RB_THREADS, 2) attn_rows_bf16_kernel(const __g
               split2(a, b, hi[mt][n * 2 + h], lo[mt][n * 2 + h]);
             }
           }
+        // high parts of four columns of tiles, then their low parts: products into one accumulator wait for one another
 #pragma unroll
-        for (int n = 0; n < NT; n += 2) {
-          uint32_t b[4];
-          ldm4t(b, vb + rb_at<DH>((lane & 7) + (((lane >> 3) & 1) << 3), n + (lane >> 4)));
+        for (int n = 0; n < NT; n += 4) {
+          uint32_t b[2][4];
+          ldm4t(b[0], vb + rb_at<DH>((lane & 7) + (((lane >> 3) & 1) << 3), n + (lane >> 4)));
+          ldm4t(b[1], vb + rb_at<DH>((lane & 7) + (((lane >> 3) & 1) << 3), n + 2 + (lane >> 4)));
 #pragma unroll
-          for (int mt = 0; mt < MT; ++mt) {
-            mma16816(o[mt][n], hi[mt], b[0], b[1]);
-            mma16816(o[mt][n], lo[mt], b[0], b[1]);
-            mma16816(o[mt][n + 1], hi[mt], b[2], b[3]);
-            mma16816(o[mt][n + 1], lo[mt], b[2], b[3]);
-          }
+          for (int part = 0; part < 2; ++part)
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+              for (int k = 0; k < 4; ++k) mma16816(o[mt][n + k], part ? lo[mt] : hi[mt], b[k >> 1][(k & 1) * 2], b[k >> 1][(k & 1) * 2 + 1]);
         }
       }
       __syncwarp();                            // the stage is copied over in the next step
@@ -314,7 +329,7 @@ __global__ void __launch_bounds__(RB_THREADS, 2) attn_rows_bf16_kernel(const __g
   if (!ok)                                     // nothing may land after the block is gone
     for (; taken < asked; ++taken) mbar_wait_bounded(&full[warp][taken % C::STAGES], (taken / C::STAGES) & 1u, RB_WAIT_NS / 8);
   redo = __syncthreads_or(redo);
-  if (tid == 0) { p.jobs[blockIdx.x] = job; p.redo[blockIdx.x] = redo; }
+  if (tid == 0) { p.jobs[blockIdx.x] = job; p.redo[blockIdx.x] = redo; p.pieces[blockIdx.x] = piece; }
   let_successor_start();
 }
 

@@ -84,10 +84,12 @@ __global__ void __launch_bounds__(RF_THREADS) attn_rows_f32_kernel(const __grid_
     for (int t = t0; t < t1; ++t) {
       const int key0 = (t < c.u.first_tiles ? t : t + c.u.skip) * RF_TILE + warp * RF_KEYS;
       __syncwarp();
+      long long slot = -1;                     // of key key0 + lane
+      if (lane < RF_KEYS && unit_sees(p, c.u, key0 + lane)) slot = slot_offset(p.c, c.s, key0 + lane, c.head);
+#pragma unroll 4
       for (int i = lane; i < RF_KEYS * DH / 4; i += 32) {
-        const int k = i / (DH / 4), e = (i - k * (DH / 4)) * 4, key = key0 + k;
-        long long at = -1;
-        if (unit_sees(p, c.u, key)) at = slot_offset(p.c, c.s, key, c.head);
+        const int k = i / (DH / 4), e = (i - k * (DH / 4)) * 4;
+        const long long at = __shfl_sync(0xffffffffu, slot, k);
         cp_async16(ks + k * S::LDK + e, (const float*)p.c.k + (at < 0 ? 0 : at + e), at >= 0);
         cp_async16(vs + k * DH + e, (const float*)p.c.v + (at < 0 ? 0 : at + e), at >= 0);
       }
@@ -213,7 +215,7 @@ __global__ void __launch_bounds__(RF_THREADS) attn_rows_f32_kernel(const __grid_
 // ------------------------------------------------------------------------------------------------
 // join of split units: a warp per row, the pieces in the order of their keys; and rows formed once more
 // ------------------------------------------------------------------------------------------------
-constexpr int JN_WARPS = 8;
+constexpr int JN_WARPS = 8, JN_BLOCKS = 8;     // warps a block; blocks for a worker's rows: one wave of them for 148 workers
 
 template <typename T, int DH>
 __device__ void store_row(const AttnParams& p, const RowPlace& x, const float (&o)[DH / 32]) {
@@ -249,45 +251,61 @@ __device__ __noinline__ void redo_rows(const AttnParams& p, int w, int r) {
 template <typename T, int DH>
 __global__ void __launch_bounds__(JN_WARPS * 32) attn_join_kernel(const __grid_constant__ Lines lines) {
   const AttnParams& p = lines.of[blockIdx.z];
-  const int w0 = blockIdx.x, r = blockIdx.y * JN_WARPS + (threadIdx.x >> 5), lane = threadIdx.x & 31;
+  const int w0 = blockIdx.x, r0 = blockIdx.y * JN_WARPS + (threadIdx.x >> 5), lane = threadIdx.x & 31;
   wait_for_predecessor();
-  if (w0 >= p.workers || r >= p.unit_rows) return;
+  if (w0 >= p.workers) return;
   const int4 job = p.jobs[w0];
-  if (p.redo[w0]) redo_rows<T, DH>(p, w0, r);
+  if (p.redo[w0])
+    for (int r = r0; r < p.unit_rows; r += gridDim.y * JN_WARPS) redo_rows<T, DH>(p, w0, r);
   if (job.w < 0) return;
   const SeqSpan sp = attn_span(p, job.x, false);
-  const RowPlace x = row_place(p, sp, job.y, job.z, r);
-  if (!x.valid) return;
+  const int n = job.w - w0 + 1;                // pieces: the second of worker w0, the first ones of those behind it
   constexpr int C = DH / 32;
-  float top = -INFINITY;
-  for (int w = w0; w <= job.w; ++w) top = fmaxf(top, p.part_ml[(long long)(w == w0 ? 2 * w + 1 : 2 * w) * p.unit_rows + r].x);
-  const float ref = top == -INFINITY ? 0.f : top;
-  float o[C], l = 0.f;
-  bool unfit = false;
+  for (int r = r0; r < p.unit_rows; r += gridDim.y * JN_WARPS) {
+    const RowPlace x = row_place(p, sp, job.y, job.z, r);
+    if (!x.valid) return;
+    auto place_of = [&](int i) { return (long long)(i == 0 ? 2 * w0 + 1 : 2 * (w0 + i)) * p.unit_rows + r; };
+    float top = -INFINITY;
+    for (int i = lane; i < n; i += 32) top = fmaxf(top, p.part_ml[place_of(i)].x);
 #pragma unroll
-  for (int i = 0; i < C; ++i) o[i] = 0.f;
-  for (int w = w0; w <= job.w; ++w) {
-    const long long at = (long long)(w == w0 ? 2 * w + 1 : 2 * w) * p.unit_rows + r;
-    const float2 ml = p.part_ml[at];
-    const float f = ex2((ml.x - ref) * p.scale_log2);
-    l = fmaf(ml.y, f, l);
-    unfit |= ml.y < 0.f;                       // a piece whose weights did not fit
+    for (int k = 16; k > 0; k >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, k));
+    const float ref = top == -INFINITY ? 0.f : top;
+    float o[C], l = 0.f;
+    bool unfit = false;
 #pragma unroll
-    for (int i = 0; i < C; ++i) o[i] = fmaf(p.part[at * DH + lane + 32 * i], f, o[i]);
-  }
-  bool fine = true;
+    for (int k = 0; k < C; ++k) o[k] = 0.f;
+    for (int base = 0; base < n; base += 32) {                     // a lane per piece, then the pieces in order
+      float2 ml = make_float2(-INFINITY, 0.f);
+      if (base + lane < n) ml = p.part_ml[place_of(base + lane)];
+      const float f = ex2((ml.x - ref) * p.scale_log2);
+      l = fmaf(ml.y, f, l);
+      unfit |= ml.y < 0.f;                     // a piece whose weights did not fit
+      const int here = min(32, n - base);
+#pragma unroll 4
+      for (int i = 0; i < here; ++i) {
+        const float g = __shfl_sync(0xffffffffu, f, i);
+        const float* part = p.part + place_of(base + i) * DH + lane;
 #pragma unroll
-  for (int i = 0; i < C; ++i) {
-    fine &= (bool)isfinite(o[i]);
-    o[i] = l == 0.f ? 0.f : o[i] / l;
+        for (int k = 0; k < C; ++k) o[k] = fmaf(part[32 * k], g, o[k]);
+      }
+    }
+#pragma unroll
+    for (int k = 16; k > 0; k >>= 1) l += __shfl_xor_sync(0xffffffffu, l, k);
+    unfit = __any_sync(0xffffffffu, unfit);
+    bool fine = true;
+#pragma unroll
+    for (int k = 0; k < C; ++k) {
+      fine &= (bool)isfinite(o[k]);
+      o[k] = l == 0.f ? 0.f : o[k] / l;
+    }
+    float lse = l == 0.f ? -INFINITY : fmaf(top, p.scale_log2, log2f(l)) * LN2;
+    if (unfit || (__any_sync(0xffffffffu, !fine) && isfinite(l))) {
+      const float exact = exact_row<T, DH>(p, job.x, job.z, unit_span(p, sp, job.y), x, o);
+      if (unfit) lse = exact;
+    }
+    store_row<T, DH>(p, x, o);
+    if (lane == 0 && p.lse) p.lse[x.row * p.n_heads + x.head] = lse;
   }
-  float lse = l == 0.f ? -INFINITY : fmaf(top, p.scale_log2, log2f(l)) * LN2;
-  if (unfit || (__any_sync(0xffffffffu, !fine) && isfinite(l))) {
-    const float exact = exact_row<T, DH>(p, job.x, job.z, unit_span(p, sp, job.y), x, o);
-    if (unfit) lse = exact;
-  }
-  store_row<T, DH>(p, x, o);
-  if (lane == 0 && p.lse) p.lse[x.row * p.n_heads + x.head] = lse;
 }
 
 // ------------------------------------------------------------------------------------------------
@@ -305,7 +323,7 @@ template <typename T, int DH>
 static int launch_join(const Lines& a, int n, cudaStream_t s) {
   int workers = 0, rows = 0;
   for (int i = 0; i < n; ++i) { workers = max(workers, a.of[i].workers); rows = max(rows, a.of[i].unit_rows); }
-  return launch_after(attn_join_kernel<T, DH>, dim3(workers, ceil_div(rows, JN_WARPS), n), dim3(JN_WARPS * 32), s, a);
+  return launch_after(attn_join_kernel<T, DH>, dim3(workers, min(JN_BLOCKS, ceil_div(rows, JN_WARPS)), n), dim3(JN_WARPS * 32), s, a);
 }
 template <typename T>
 static int launch_join_as(const Lines& a, int n, int dh, cudaStream_t s) {
@@ -430,7 +448,7 @@ extern "C" int grpo_paged_attention(const grpo_kv_cache* cache, const grpo_kv_ba
   for (int i = 0; i < call.n; ++i) {
     AttnParams& a = lines.of[i];
     a = p;
-    a.unit_rows = call.rows[i]; a.tile = call.tile[i]; a.workers = call.workers[i]; a.min_share = call.min_share[i];
+    a.unit_rows = call.rows[i]; a.tile = call.tile[i]; a.tile_shift = __builtin_ctz(call.tile[i]); a.workers = call.workers[i]; a.min_share = call.min_share[i];
     a.over_rows = call.over[i]; a.up_to_rows = call.up_to[i];
     place(a, call.at[i], ws);
     if (call.self[i]) a.prefix = nullptr;

@@ -27,7 +27,7 @@ struct AttnParams {
   FastDiv div_group;
   float scale_log2;                            // scale log2(e): weights are powers of two
   int window, sinks;                           // window 0: everything before
-  int unit_rows, tile;                         // rows of a unit, keys of a tile (a power of two)
+  int unit_rows, tile, tile_shift;             // rows of a unit, keys of a tile: 2^tile_shift
   int over_rows, up_to_rows;                   // this kernel's sequences: over_rows < new tokens * group <= up_to_rows
   int workers, min_share;                      // pieces of the line; tiles of a piece at least
   long long* prefix;                           // [n_seq + 1] tiles ahead of each sequence; NULL: every block finds them itself
@@ -64,8 +64,8 @@ __device__ __forceinline__ UnitSpan unit_span(const AttnParams& p, const SeqSpan
   UnitSpan u;
   u.end = p1 >= 0 ? p1 + 1 : 0;
   u.low = p.window > 0 && p0 >= p.window ? p0 - p.window + 1 : 0;
-  const int all = (u.end + p.tile - 1) / p.tile, from = u.low / p.tile;
-  int st = (min(p.sinks, u.end) + p.tile - 1) / p.tile;
+  const int all = (u.end + p.tile - 1) >> p.tile_shift, from = u.low >> p.tile_shift;
+  const int st = (min(p.sinks, u.end) + p.tile - 1) >> p.tile_shift;
   if (st >= from) {
     u.first_tiles = 0; u.skip = 0; u.tiles = max(1, all);          // a unit that sees nothing still writes its zeros
   } else {

@@ -58,7 +58,7 @@ __device__ static int sequence_of(const KvView& c, int row) {
 // A unit is what one thread handles at a time: with VEC, 16 bytes (interleaved), or 16 bytes of either half; else one pair;
 // of what does not turn, 16 bytes or one element.
 template <typename T, bool VEC, bool INTER>
-__global__ void __launch_bounds__(RT_THREADS) rotary_kernel(const RotaryParams p) {
+__global__ void __launch_bounds__(RT_THREADS, 8) rotary_kernel(const __grid_constant__ RotaryParams p) {
   constexpr int N = VEC ? RtVec<T>::N : 1;
   __shared__ float2 cs[RT_ANGLES];
   __shared__ int row_pos[RT_ROWS];

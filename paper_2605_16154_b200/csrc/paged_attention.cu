@@ -16,8 +16,8 @@ constexpr int PLAN_THREADS = 1024;
 struct Lines { AttnParams of[2]; };
 __global__ void __launch_bounds__(PLAN_THREADS) attn_plan_kernel(const __grid_constant__ Lines lines) {
   const AttnParams& p = lines.of[blockIdx.x];
-  __shared__ long long sums[PLAN_THREADS / 32 + 1];
-  if (p.prefix) line_prefix(p, p.prefix, sums, true);
+  __shared__ __align__(8) unsigned char room[LINE_ROOM];
+  if (p.prefix) line_prefix(p, p.prefix, room, true);
   let_successor_start();
 }
 
@@ -57,7 +57,6 @@ __global__ void __launch_bounds__(RF_THREADS) attn_rows_f32_kernel(const __grid_
 
   wait_for_predecessor();
   block_piece(p, sm, &piece);
-  __syncthreads();
   Cursor c = piece.c;
   long long left = piece.left, ahead = piece.ahead;
   const long long share = piece.share;
@@ -448,7 +447,7 @@ extern "C" int grpo_paged_attention(const grpo_kv_cache* cache, const grpo_kv_ba
   for (int i = 0; i < call.n; ++i) {
     AttnParams& a = lines.of[i];
     a = p;
-    a.unit_rows = call.rows[i]; a.tile = call.tile[i]; a.tile_shift = __builtin_ctz(call.tile[i]); a.workers = call.workers[i]; a.min_share = call.min_share[i];
+    a.unit_rows = call.rows[i]; a.tile = call.tile[i]; a.tile_shift = __builtin_ctz(call.tile[i]); a.row_shift = __builtin_ctz(call.rows[i]); a.workers = call.workers[i]; a.min_share = call.min_share[i];
     a.over_rows = call.over[i]; a.up_to_rows = call.up_to[i];
     place(a, call.at[i], ws);
     if (call.self[i]) a.prefix = nullptr;

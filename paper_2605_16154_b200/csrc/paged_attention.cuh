@@ -27,7 +27,8 @@ struct AttnParams {
   FastDiv div_group;
   float scale_log2;                            // scale log2(e): weights are powers of two
   int window, sinks;                           // window 0: everything before
-  int unit_rows, tile, tile_shift;             // rows of a unit, keys of a tile: 2^tile_shift
+  int unit_rows, row_shift;                    // rows of a unit: 2^row_shift
+  int tile, tile_shift;                        // keys of a tile: 2^tile_shift
   int over_rows, up_to_rows;                   // this kernel's sequences: over_rows < new tokens * group <= up_to_rows
   int workers, min_share;                      // pieces of the line; tiles of a piece at least
   long long* prefix;                           // [n_seq + 1] tiles ahead of each sequence; NULL: every block finds them itself
@@ -52,7 +53,7 @@ __device__ __forceinline__ SeqSpan attn_span(const AttnParams& p, int s, bool re
   return sp;
 }
 __device__ __forceinline__ int row_tiles(const AttnParams& p, const SeqSpan& sp) {
-  return (int)(((long long)sp.fresh * p.group + p.unit_rows - 1) / p.unit_rows);
+  return (sp.fresh * p.group + p.unit_rows - 1) >> p.row_shift;
 }
 
 // The tiles that the rows of row tile qt see: tile i of the unit is tile i of the sequence below `first_tiles` and tile
@@ -150,7 +151,7 @@ __device__ inline long long find_border(const AttnParams& p, const long long* pr
     y -= __shfl_sync(0xffffffffu, sum, 31);
   }
   c.u = unit_span(p, c.sp, c.qt);
-  c.head = (int)(y / c.u.tiles);
+  c.head = y >> 31 ? (int)(y / c.u.tiles) : (int)y / c.u.tiles;     // (y is below the tiles of one row tile: all but always short)
   c.at = (int)(y - (long long)c.head * c.u.tiles);
   const int shift = border_shift(p, share, c.at, c.u.tiles);
   const bool to_end = shift > 0;
@@ -239,45 +240,42 @@ __device__ inline float exact_row(const AttnParams& p, int s, int kv_head, const
   return l == 0.f ? -INFINITY : fmaf(m, p.scale_log2, log2f(l)) * LN2;
 }
 
-// One worker's walk over its piece of the line.  `begin` and `end` are found by a whole warp and handed to the block.
+// One worker's piece of the line.
 struct Piece { Cursor c; long long left, share, ahead; };          // tiles left of the piece; tiles ahead of the cursor
-__device__ inline void find_piece(const AttnParams& p, const long long* prefix, int w, Piece& piece) {
-  const long long total = prefix[p.c.n_seq];
-  piece.share = line_share(p, total);
-  Cursor end;
-  const long long b1 = find_border(p, prefix, w + 1, piece.share, total, end);
-  piece.ahead = find_border(p, prefix, w, piece.share, total, piece.c);
-  piece.left = b1 - piece.ahead;
-}
-
-// Tiles ahead of every sequence, by a whole block; `sums` takes a word per warp and one more.
-__device__ inline void line_prefix(const AttnParams& p, long long* prefix, long long* sums, bool report) {
+// Tiles ahead of every sequence, by a whole block; `room`: LINE_ROOM bytes of shared memory.
+constexpr int LINE_ROOM = 34 * 8 + 1024 * 4;
+__device__ inline void line_prefix(const AttnParams& p, long long* prefix, void* room, bool report) {
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, warps = (int)blockDim.x >> 5;
-  long long* carry = sums + warps;
-  if (tid == 0) { *carry = 0; prefix[0] = 0; }
-  __syncthreads();
+  long long* sums = (long long*)room;          // one a warp; the carry; how many sequences are listed
+  long long* carry = sums + 32;
+  int* listed = (int*)(sums + 33);
+  int* list = (int*)(sums + 34);               // sequences of many row tiles: a warp each
+  if (tid == 0) { *carry = 0; prefix[0] = 0; *listed = 0; }
   for (int base = 0; base < p.c.n_seq; base += (int)blockDim.x) {
+    __syncthreads();
     const int s = base + tid;
-    SeqSpan sp{0, 0, 0};
-    if (s < p.c.n_seq) sp = attn_span(p, s, report);
-    const int nqt = row_tiles(p, sp);
-    long long sum = 0;
-    if (nqt <= 2)
-      for (int qt = 0; qt < nqt; ++qt) sum += unit_span(p, sp, qt).tiles;
-    for (unsigned many = __ballot_sync(0xffffffffu, nqt > 2); many; many &= many - 1) {
-      const int from = __ffs(many) - 1;                            // a sequence of many row tiles takes the whole warp
-      SeqSpan o;
-      o.row0 = 0;
-      o.fresh = __shfl_sync(0xffffffffu, sp.fresh, from);
-      o.len = __shfl_sync(0xffffffffu, sp.len, from);
-      const int n = row_tiles(p, o);
-      long long mine = 0;
-      for (int qt = lane; qt < n; qt += 32) mine += unit_span(p, o, qt).tiles;
-#pragma unroll
-      for (int d = 16; d > 0; d >>= 1) mine += __shfl_xor_sync(0xffffffffu, mine, d);
-      if (lane == from) sum = mine;
+    if (s < p.c.n_seq) {
+      const SeqSpan sp = attn_span(p, s, report);
+      const int nqt = row_tiles(p, sp);
+      long long sum = 0;
+      if (nqt <= 2)
+        for (int qt = 0; qt < nqt; ++qt) sum += unit_span(p, sp, qt).tiles;
+      else
+        list[atomicAdd(listed, 1)] = s;        // in any order: each writes its own sequence's sum
+      prefix[s + 1] = sum * p.c.n_kv;
     }
-    sum *= p.c.n_kv;
+    __syncthreads();
+    for (int i = warp; i < *listed; i += warps) {
+      const SeqSpan sp = attn_span(p, list[i], false);
+      const int nqt = row_tiles(p, sp);
+      long long sum = 0;
+      for (int qt = lane; qt < nqt; qt += 32) sum += unit_span(p, sp, qt).tiles;
+#pragma unroll
+      for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+      if (lane == 0) prefix[list[i] + 1] = sum * p.c.n_kv;
+    }
+    __syncthreads();
+    long long sum = s < p.c.n_seq ? prefix[s + 1] : 0;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
       const long long t = __shfl_up_sync(0xffffffffu, sum, o);
@@ -289,18 +287,18 @@ __device__ inline void line_prefix(const AttnParams& p, long long* prefix, long 
     for (int w = 0; w < warp; ++w) before += sums[w];
     if (s < p.c.n_seq) prefix[s + 1] = before + sum;
     __syncthreads();
-    if (tid == (int)blockDim.x - 1) *carry = before + sum;
-    __syncthreads();
+    if (tid == (int)blockDim.x - 1) { *carry = before + sum; *listed = 0; }
   }
+  __syncthreads();
 }
 
 // Sequences and row tiles (as the host can bound them) up to which every block finds its piece from the lengths: a launch and
 // the reads of its results less, 4 of 16 us of a step of one sequence.
 constexpr int SELF_PLANNED = 1024;
-constexpr int SELF_BYTES = (SELF_PLANNED + 1 + 33) * 8;            // prefix and sums
+constexpr int SELF_BYTES = (SELF_PLANNED + 1) * 8 + LINE_ROOM;
 
-// The block's piece of the line, from the plan's results or from the lengths; `scratch`: SELF_BYTES of shared memory that is
-// free until the block's next barrier after this.
+// The block's piece of the line, from the plan's results or from the lengths; `scratch`: SELF_BYTES of shared memory.  Ends
+// with a barrier of the block.
 __device__ inline void block_piece(const AttnParams& p, void* scratch, Piece* piece) {
   const long long* prefix = p.prefix;
   if (!prefix) {
@@ -308,11 +306,19 @@ __device__ inline void block_piece(const AttnParams& p, void* scratch, Piece* pi
     line_prefix(p, own, own + SELF_PLANNED + 1, blockIdx.x == 0);
     prefix = own;
   }
-  if (threadIdx.x < 32) {
-    Piece own;
-    find_piece(p, prefix, blockIdx.x, own);
-    if (threadIdx.x == 0) *piece = own;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const long long total = prefix[p.c.n_seq], share = line_share(p, total);
+  if (warp < 2) {                              // a warp for either border
+    Cursor c;
+    const long long x = find_border(p, prefix, (int)blockIdx.x + warp, share, total, c);
+    if (lane == 0) {
+      if (warp == 0) { piece->c = c; piece->ahead = x; piece->share = share; }
+      else piece->left = x;
+    }
   }
+  __syncthreads();
+  if (threadIdx.x == 0) piece->left -= piece->ahead;
+  __syncthreads();
 }
 
 // Launches of the kernels on a line that is planned (workers, unit_rows and tile set).

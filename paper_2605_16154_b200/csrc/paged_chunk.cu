@@ -596,7 +596,7 @@ attn_chunk_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
         const long long at = (long long)slot * p.unit_rows + half * CH_ROWS + row;
         const long long out_at = place.row * p.ld_out + place.head * p.ld_out_head;
         const float inv = wild ? NAN : l == 0.f ? 0.f : 1.f / l;
-        float bad = 0.f;                       // NaN once a value is not finite
+        float2 bad = make_float2(0.f, 0.f);    // NaN once a value is not finite
 #pragma unroll 1
         for (int k = 0; k < DH; k += 32) {
           uint32_t o[32];
@@ -608,7 +608,7 @@ attn_chunk_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
             for (int e = 0; e < 32; ++e) o[e] = 0u;
           }
 #pragma unroll
-          for (int e = 0; e < 32; ++e) bad = fmaf(__uint_as_float(o[e]), 0.f, bad);
+          for (int e = 0; e < 32; e += 2) bad = fma2(make_float2(__uint_as_float(o[e]), __uint_as_float(o[e + 1])), make_float2(0.f, 0.f), bad);
           if (whole) {
 #pragma unroll
             for (int e = 0; e < 32; e += 8) {
@@ -642,7 +642,7 @@ attn_chunk_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
           if (!whole) p.part_ml[at] = make_float2(m, wild ? -1.f : l);
           else if (p.lse) p.lse[place.row * p.n_heads + place.head] = wild ? NAN : l == 0.f ? -INFINITY : fmaf(m, p.scale_log2, log2f(l)) * LN2;
         }
-        if (whole && place.valid && (wild || (bad != 0.f && isfinite(l)))) b.redo = 1;
+        if (whole && place.valid && (wild || (!(bad.x + bad.y == 0.f) && isfinite(l)))) b.redo = 1;
       }
       if constexpr (C::QBUFS == 1) {
         if (rest > 0) {

@@ -738,7 +738,7 @@ def grpo_rotary_freqs(rot_dim: int, base: float = 10000.0, scaling: int = ROTARY
     """(turns, amplitude): the frequencies of rot_dim / 2 pairs in turns per position (float64, on the host: move them to the
     device once) and the factor on the rotated values."""
     _size("grpo_rotary_freqs", rot_dim, 0)
-    turns = torch.empty(max(0, rot_dim // 2), dtype=_f64)
+    turns = torch.empty(max(1, rot_dim // 2), dtype=_f64)
     amplitude = C.c_float(0.0)
     cfg = grpo_rotary_cfg(rot_dim, scaling, base, factor, original_len, low, high)
     _check("grpo_rotary_freqs", _lib.grpo_rotary_freqs(C.byref(cfg), turns.data_ptr(), C.byref(amplitude)))

@@ -49,6 +49,13 @@ __device__ __forceinline__ SeqSpan seq_span(const KvView& c, int s, bool report)
   return sp;
 }
 
+// Whether rows of heads that are written may share elements: neither do a row's heads end before the next row, nor a head's
+// rows before the next head.
+static inline bool rows_overlap(int64_t n, int64_t heads, int64_t dim, int64_t ld, int64_t ld_head) {
+  if (n <= 1 || heads <= 1) return (n > 1 && ld < dim) || (heads > 1 && ld_head < dim);
+  return ld < dim || ld_head < dim || (ld < (heads - 1) * ld_head + dim && ld_head < (n - 1) * ld + dim);
+}
+
 // Checks of the two structs that every call makes before it reads from them.
 int kv_check(const grpo_kv_cache* cache, const grpo_kv_batch* batch, int32_t n_rows);
 KvView kv_view(const grpo_kv_cache* cache, const grpo_kv_batch* batch, int32_t n_rows, uint32_t* status);

@@ -420,8 +420,7 @@ extern "C" int grpo_paged_attention(const grpo_kv_cache* cache, const grpo_kv_ba
   if (n_rows == 0 || batch->n_seq == 0) return PCM_OK;
   const int dh = cache->head_dim;
   if (!q || !out || (lse && ((uintptr_t)lse & 3))) return PCM_ERR_ARG;
-  if (n_heads > 1 && (ld_q_head < dh || ld_out_head < dh)) return PCM_ERR_ARG;
-  if (n_rows > 1 && (ld_q < dh || ld_out < dh)) return PCM_ERR_ARG;
+  if ((n_heads > 1 && ld_q_head < dh) || (n_rows > 1 && ld_q < dh) || rows_overlap(n_rows, n_heads, dh, ld_out, ld_out_head)) return PCM_ERR_ARG;
   const int64_t per = cache->dtype == GRPO_BF16 ? 8 : 4;
   if ((((uintptr_t)q | (uintptr_t)out) & 15) || (n_heads > 1 && (ld_q_head % per || ld_out_head % per)) ||
       (n_rows > 1 && (ld_q % per || ld_out % per)))

@@ -284,7 +284,7 @@ extern "C" int grpo_rotary(int32_t dtype, const void* x, int64_t ld_x, int64_t l
   if (n == 0) return PCM_OK;
   const uintptr_t low = elem_bytes(dtype) - 1;
   if (!x || !out || !pos || (rot_dim > 0 && !turns) || (((uintptr_t)x | (uintptr_t)out) & low)) return PCM_ERR_ARG;
-  if ((n_heads > 1 && (ld_x_head < head_dim || ld_out_head < head_dim)) || (n > 1 && (ld_x < head_dim || ld_out < head_dim))) return PCM_ERR_ARG;
+  if ((n_heads > 1 && ld_x_head < head_dim) || (n > 1 && ld_x < head_dim) || rows_overlap(n, n_heads, head_dim, ld_out, ld_out_head)) return PCM_ERR_ARG;
   if (x == out && (ld_x != ld_out || ld_x_head != ld_out_head)) return PCM_ERR_ARG;
   RotaryParams p = {};
   p.q = RotaryStream{x, ld_x, ld_x_head, out, ld_out, ld_out_head, n_heads};
@@ -315,8 +315,8 @@ extern "C" int grpo_rotary_cache(const grpo_kv_cache* cache, const grpo_kv_batch
   if (((uintptr_t)k | (uintptr_t)v | (n_heads ? (uintptr_t)q | (uintptr_t)q_out : 0)) & low) return PCM_ERR_ARG;
   if (n_kv > 1 && (ld_k_head < dim || ld_v_head < dim)) return PCM_ERR_ARG;
   if (n_rows > 1 && (ld_k < dim || ld_v < dim)) return PCM_ERR_ARG;
-  if (n_heads > 1 && (ld_q_head < dim || ld_q_out_head < dim)) return PCM_ERR_ARG;
-  if (n_heads > 0 && n_rows > 1 && (ld_q < dim || ld_q_out < dim)) return PCM_ERR_ARG;
+  if ((n_heads > 1 && ld_q_head < dim) || (n_heads > 0 && n_rows > 1 && ld_q < dim)) return PCM_ERR_ARG;
+  if (n_heads > 0 && rows_overlap(n_rows, n_heads, dim, ld_q_out, ld_q_out_head)) return PCM_ERR_ARG;
   if (n_heads > 0 && q == q_out && (ld_q != ld_q_out || ld_q_head != ld_q_out_head)) return PCM_ERR_ARG;
   RotaryParams p = {};
   p.q = RotaryStream{q, ld_q, ld_q_head, q_out, ld_q_out, ld_q_out_head, n_heads};

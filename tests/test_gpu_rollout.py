@@ -330,3 +330,211 @@ def test_pages_outside_the_cache_are_not_written():
     assert int(c.status) == 64
     changed = (c.k_pages != before).flatten(1).any(1).nonzero().flatten().tolist()
     assert set(changed) <= {int(c.table_host[0][1]), int(c.table_host[1][3])}
+
+
+# ---- as they are used ------------------------------------------------------------------------------------------------
+def test_the_same_inputs_give_the_same_bits():
+    for new in ([1, 1, 1], [200, 1, 130], [5, 3, 8]):
+        c = Case(51, "bf16", 128, 2, 4, 16, [9000, 700, 3111], new)
+        out, lse = c.run()
+        for _ in range(3):
+            again, lse2 = c.run()
+            assert torch.equal(out, again) and torch.equal(lse, lse2)
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+def test_rows_and_heads_apart_and_a_known_scale(kind):
+    c = Case(53, kind, 64, 2, 3, 16, [200, 90], [140, 4], gap=8)
+    want, lse = c.run(scale=0.2)
+    wide = torch.full((c.n, c.heads + 2, 64 + 8), 9.0, dtype=c.t, device="cuda")
+    q = wide[:, 1:-1, :64]
+    q.copy_(c.q)
+    room = torch.full((c.heads, c.n + 3, 64), 5.0, dtype=c.t, device="cuda")
+    out = room.transpose(0, 1)[1:-2]                               # heads outside, rows inside
+    got, none = B().grpo_paged_attention(q, c.k_pages, c.v_pages, c.table, c.seq_len, c.q_off, scale=0.2, out=out, want_lse=False)
+    assert none is None and got is out and torch.equal(out, want[:c.n])
+    assert bool((room[:, 0] == 5).all()) and bool((room[:, -2:] == 5).all())
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+def test_rows_ahead_of_the_first_sequence_are_left_alone(kind):
+    c = Case(55, kind, 64, 2, 2, 16, [50, 300], [3, 120])
+    want, lse = c.run()
+    c.q = torch.cat([c.q[:7] * float("nan"), c.q])
+    c.n += 7
+    c.q_off += 7
+    out, ls = c.run()
+    assert torch.equal(out[7:], want) and torch.equal(ls[7:], lse) and bool((out[:7] == 7).all()) and bool((ls[:7] == 7).all())
+    kv = torch.randn(c.n, 2, 64, device="cuda").to(c.t)
+    before = c.k_pages.clone()
+    q_out = torch.full_like(c.q, 7.0)
+    B().grpo_rotary_cache(c.q, kv, kv, c.k_pages, c.v_pages, c.table, c.seq_len, c.q_off, None, q_out=q_out)
+    assert bool((q_out[:7] == 7).all()) and torch.equal(q_out[7:], c.q[7:])
+    changed = (c.k_pages != before) & ~(torch.isnan(c.k_pages) & torch.isnan(before))          # slots never written are NaN
+    assert int(changed.flatten(2).any(2).sum()) == 123
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("max_new", [0, 1, 2, 40, 10 ** 6])
+def test_max_new_is_a_hint(kind, max_new):
+    """Any value gives the right answer, one that is too small too: it chooses among kernels."""
+    c = Case(57, kind, 64, 1, 4, 16, [400, 3, 90, 33], [40, 1, 2, 33])
+    c.check(*c.run(max_new=max_new))
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+def test_many_sequences(kind):
+    """More than a block's own plan takes: 1300 sequences, a tenth of them without rows, and a few with many."""
+    rng = np.random.default_rng(3)
+    lens = [int(a) for a in rng.integers(0, 60, 1300)]
+    new = [0 if i % 10 == 0 else min(a, 1 + i % 3) for i, a in enumerate(lens)]
+    lens[77], new[77] = 500, 150
+    c = Case(59, kind, 32 if kind == "f32" else 64, 1, 2, 8, lens, new)
+    c.check(*c.run())
+
+
+def test_many_row_tiles():
+    """A chunk whose row tiles pass what a block plans itself (1024): only its last rows are checked."""
+    new, length = 66000, 66100
+    g = gen(61)
+    k, v = (torch.randn(length // 64 + 1, 64, 1, 64, generator=g, device="cuda").bfloat16() for _ in range(2))
+    q = torch.randn(new, 4, 64, generator=g, device="cuda").bfloat16()
+    table = torch.randperm(length // 64 + 1, generator=g, device="cuda").to(torch.int32)[None]
+    out, lse = B().grpo_paged_attention(q, k, v, table, torch.tensor([length], dtype=torch.int32, device="cuda"),
+                                        torch.tensor([0, new], dtype=torch.int32, device="cuda"), window=600, sinks=3, max_new=new)
+    rows = [0, 1, 12345, 40000, new - 1]
+    flat = lambda t: host(t[table[0].long()].flatten(0, 1)[:length])
+    kh, vh = flat(k), flat(v)
+    for r in rows:
+        want, wlse, mass, _ = ro.attend(host(q[r:r + 1]), kh[None], vh[None], np.zeros((1, 1), int), [length - new + r + 1], np.array([0, 1]), 0.125, 600, 3)
+        assert np.all(np.abs(host(out[r:r + 1]) - want) <= 2.0 ** -7 * mass + 2.0 ** -8 * np.abs(want))
+        assert np.all(np.abs(host(lse[r:r + 1]) - wlse) < 1e-4)
+
+
+def test_offsets_beyond_31_bits():
+    """Pages at both ends of a cache of more than 2^32 elements."""
+    n, page, kv, dim = 264000, 16, 8, 128
+    k, v = (torch.empty(n, page, kv, dim, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    assert k.numel() > 2 ** 32
+    table = torch.tensor([[n - 1, 0, n // 2, n - 2, 5]], dtype=torch.int32, device="cuda")
+    g = gen(63)
+    new = torch.randn(70, 16 + 2 * kv, dim, generator=g, device="cuda").bfloat16()
+    q, kn, vn = new[:, :16], new[:, 16:24], new[:, 24:]
+    seq_len, q_off = torch.tensor([70], dtype=torch.int32, device="cuda"), torch.tensor([0, 70], dtype=torch.int32, device="cuda")
+    B().grpo_rotary_cache(q, kn, vn, k, v, table, seq_len, q_off, None)
+    assert torch.equal(k[table[0].long()].flatten(0, 1)[:70], kn)
+    kh, vh = host(kn)[None], host(vn)[None]
+    for rows in (70, 1):
+        out, _ = B().grpo_paged_attention(q[70 - rows:], k, v, table, seq_len, torch.tensor([0, rows], dtype=torch.int32, device="cuda"))
+        want, _, mass, _ = ro.attend(host(q[70 - rows:]), kh, vh, np.zeros((1, 1), int), [70], np.array([0, rows]), dim ** -0.5)
+        assert np.all(np.abs(host(out) - want) <= 2.0 ** -7 * mass + 2.0 ** -8 * np.abs(want))
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("new", [1, 130])
+def test_scores_that_rise_by_hundreds_from_tile_to_tile(kind, new):
+    """Each tile of keys outweighs all before it by more than a weight's exponent holds, and the other way round."""
+    for falling in (False, True):
+        c = Case(65, kind, 64, 1, 2, 16, [700], [new])
+        c.q[:] = 1.0
+        steps = torch.arange(700, device="cuda") // 128 * 90.0
+        rows = torch.from_numpy(c.table_host[0][np.arange(700) // 16].astype(np.int64)).cuda(), torch.arange(700, device="cuda") % 16
+        noise = torch.randn(700, 1, 64, generator=gen(66), device="cuda") * 0.01
+        c.k_pages[rows] = ((noise + ((-steps if falling else steps) / 64)[:, None, None]) * 8).to(c.t)      # scores: 64 x 8 / 8 per step
+        c.check(*c.run())
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+def test_captured_calls_follow_the_lengths_and_share_a_workspace(kind):
+    """A decoding step and a chunk captured into two graphs with one workspace, replayed in turn as the sequences grow."""
+    dim, kv, heads, page = 64, 2, 6, 16
+    t, g = TYPES[kind], gen(71)
+    k, v = (torch.zeros(40, page, kv, dim, dtype=t, device="cuda") for _ in range(2))
+    table = torch.arange(40, dtype=torch.int32, device="cuda").view(2, 20)
+    turns, _ = B().grpo_rotary_freqs(dim)
+    turns = turns.cuda()
+    seq_len = torch.zeros(2, dtype=torch.int32, device="cuda")
+    need = max(B().grpo_paged_attention_workspace_bytes(k, 2, n, heads, m) for n, m in ((2, 1), (80, 40)))
+    workspace = torch.empty(need + 256, dtype=torch.uint8, device="cuda")
+    calls = {}
+    for new in (40, 1):
+        fused = torch.zeros(2 * new, heads + 2 * kv, dim, dtype=t, device="cuda")
+        q_off = torch.tensor([0, new, 2 * new], dtype=torch.int32, device="cuda")
+        out, lse, q = (torch.empty(2 * new, heads, dim, dtype=t, device="cuda"), torch.empty(2 * new, heads, device="cuda"),
+                       torch.empty(2 * new, heads, dim, dtype=t, device="cuda"))
+
+        def step(fused=fused, q_off=q_off, out=out, lse=lse, q=q, new=new):
+            B().grpo_rotary_cache(fused[:, :heads], fused[:, heads:heads + kv], fused[:, heads + kv:], k, v, table, seq_len, q_off, turns, q_out=q)
+            B().grpo_paged_attention(q, k, v, table, seq_len, q_off, max_new=new, out=out, lse=lse, workspace=workspace)
+        step()
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            step()
+        calls[new] = graph, fused, q_off, out, lse, q
+    history = []
+    length = 0
+    for new in (40, 1, 1, 40, 1):
+        graph, fused, q_off, out, lse, q = calls[new]
+        fused.copy_(torch.randn(fused.shape, generator=g, device="cuda"))
+        length += new
+        seq_len.fill_(length)
+        graph.replay()
+        history.append((host(k[table.long()].flatten(1, 2)), host(v[table.long()].flatten(1, 2))))
+        kh, vh = history[-1]
+        want, _, mass, reach = ro.attend(host(q), kh, vh, np.array([[0], [1]]), [length] * 2, q_off.cpu().numpy(), dim ** -0.5)
+        d = 2 * (dim + 4) * U * reach
+        tol = ((2 * (2 * d + 2 * reach * U + 2.0 ** -22) + 100 * U + (2.0 ** -8 if kind == "bf16" else 0))[..., None]) * mass + half_step(t) * np.abs(want)
+        assert np.all(np.abs(host(out) - want) <= tol)
+
+
+def test_two_streams_at_once():
+    cases = [Case(73 + i, "bf16", 64, 2, 2, 16, [3000, 700], [n, n]) for i, n in enumerate((1, 200))]
+    want = [c.run() for c in cases]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    got = []
+    for _ in range(5):
+        for c, s in zip(cases, streams):
+            with torch.cuda.stream(s):
+                got.append(c.run())
+    torch.cuda.synchronize()
+    for i, (out, lse) in enumerate(got):
+        assert torch.equal(out, want[i % 2][0]) and torch.equal(lse, want[i % 2][1])
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+def test_a_layer_token_by_token_is_the_layer_over_the_whole_sequence(kind):
+    """The actor update's attention over 96 positions of two chunks, and the rollout's over the same: a prefix of 40 tokens at
+    once, then eight, then one at a time, through projection, rotation, cache and attention."""
+    H, dh, S, n = 4, 64, 96, 2
+    d, t, g = H * dh, TYPES[kind], gen(81)
+    x = torch.randn(n * S, d, generator=g, device="cuda").to(t)
+    w = (torch.randn(3 * d, d, generator=g, device="cuda") * d ** -0.5).to(t)
+    turns, _ = B().grpo_rotary_freqs(dh)
+    turns = turns.cuda()
+    qkv = B().grpo_gemm(x, True, w, True, n * S, 3 * d, d, out_dtype=t)
+    pos = torch.arange(S, dtype=torch.int32, device="cuda").repeat(n)
+    whole = qkv.clone().view(n * S, 3, H, dh)
+    for i in (0, 1):
+        B().grpo_rotary(whole[:, i], pos, turns, out=whole[:, i])
+    want, want_lse, _ = B().grpo_attention(whole.view(n * S, 3 * d), n, S, H, dh)
+    k, v = (torch.zeros(n * 8, 16, H, dh, dtype=t, device="cuda") for _ in range(2))
+    table = torch.randperm(n * 8, generator=g, device="cuda").to(torch.int32).view(n, 8)
+    qkv = qkv.view(n, S, 3, H, dh)
+    out = torch.empty(n, S, H, dh, dtype=t, device="cuda")
+    lse = torch.empty(n, S, H, device="cuda")
+    at = 0
+    for new in [40, 8] + [1] * 48:
+        rows = qkv[:, at:at + new].reshape(n * new, 3, H, dh)
+        at += new
+        seq_len = torch.full((n,), at, dtype=torch.int32, device="cuda")
+        q_off = torch.arange(n + 1, dtype=torch.int32, device="cuda") * new
+        q = B().grpo_rotary_cache(rows[:, 0], rows[:, 1], rows[:, 2], k, v, table, seq_len, q_off, turns)
+        o, ls = B().grpo_paged_attention(q, k, v, table, seq_len, q_off, max_new=new)
+        out[:, at - new:at], lse[:, at - new:at] = o.view(n, new, H, dh), ls.view(n, new, H)
+    # both are off from the exact attention by a rounding of the weights (2^-8 of sum p |v|) and one of the result
+    vv = whole.view(n, S, 3, H, dh)[:, :, 2].double().abs().max()
+    tol = 1e-5 if kind == "f32" else 2 * (2.0 ** -8 + 2.0 ** -8) * float(vv)
+    assert float((out.view(n * S, d).double() - want.double()).abs().max()) <= tol
+    assert float((lse - want_lse.transpose(1, 2)).abs().max()) <= (1e-5 if kind == "f32" else 1e-3)

@@ -6,9 +6,9 @@
 //   O += P V             tcgen05.mma with P from tensor memory, accumulated there
 // While one stream's warps form weights the tensor core works for the other.  The streams have an issuing warp each and run
 // at their own pace, a ring of tiles apart at most; from unit to unit they change halves, since the later half sees more.  The
-// reference m of a row is its maximum so far, but it moves only when a tile's maximum has risen by more than 8 powers of two above
-// it, and then from the next tile on: weights far above 1 are as exact in bf16 and fp32 as weights up to 1, the accumulator is
-// hardly ever fetched, scaled and put back, and no weight waits for the maximum of its tile.  A tile that rises by more than 100
+// reference m of a row is the first score that it sees, and it moves only when a tile's maximum has risen by more than 32 powers
+// of two above it, to that maximum from the next tile on: weights far above 1 are as exact in bf16 and fp32 as weights up to 1,
+// the accumulator is hardly ever fetched, scaled and put back, and no weight waits for the maximum of its tile.  A tile that rises by more than 100
 // powers of two at once (70 nats) has its rows formed once more where pieces are joined.
 // Keys and values come by TMA through a ring of tiles, box by box of a page (greatest common divisor of page and tile):
 // lanes of the loading warp look their boxes' pages up side by side.  Boxes that no row of the unit sees are read from
@@ -31,7 +31,7 @@ constexpr unsigned long long CH_WAIT_NS = 2000000000ull;
 constexpr int CH_TMEM = 512;
 constexpr int CH_TURNS = 8;                    // tiles of a piece from which on its streams take turns (8 x 1024 tokens behind 4096 to 8192: 387 us,
                                                // 436 without; units of two tiles: 361 us without, 397 with)
-constexpr float CH_RISE = 8.f;                 // powers of two by which a maximum may outgrow its reference
+constexpr float CH_RISE = 32.f;                // powers of two by which a maximum may outgrow its reference
 constexpr float CH_WILD = 100.f;               // .. within one tile: 128 weights of 2^100 still have a sum
 template <int DH> struct ChCfg {
   static constexpr int SLABS = DH / 64;        // 64 columns of 128 rows, 128-byte swizzle
@@ -88,6 +88,11 @@ __device__ __forceinline__ void ch_tmem_st16(uint32_t taddr, const uint32_t (&r)
       "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
       "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
       : "memory");
+}
+__device__ __forceinline__ float ch_tmem_ld1(uint32_t taddr) {
+  uint32_t r;
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x1.b32 {%0}, [%1];\n\ttcgen05.wait::ld.sync.aligned;" : "=r"(r) : "r"(taddr) : "memory");
+  return __uint_as_float(r);
 }
 __device__ __forceinline__ void ch_tmem_ld16(uint32_t taddr, uint32_t (&r)[16]) {
   asm volatile(
@@ -484,23 +489,27 @@ attn_chunk_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
         const int last = pos - key0, from = pos - p.window + 1 - key0, sunk = p.sinks - key0;
         const bool behind = p.window > 0 && __any_sync(0xffffffffu, from > 0);
         auto mask = [&](uint32_t (&z)[32], int k0) {
-          if (all_seen) return;
 #pragma unroll
           for (int e = 0; e < 32; ++e) z[e] = e > last - k0 ? 0xFF800000u : z[e];
           if (behind)
 #pragma unroll
             for (int e = 0; e < 32; ++e) z[e] = (e < from - k0) & (e >= sunk - k0) ? 0xFF800000u : z[e];
         };
-        // The reference of a tile's weights comes from the tiles before it, so that they need not wait for this one's maximum;
-        // only a row that has seen nothing yet takes its first one from here.
+        // The reference of a tile's weights comes from the tiles before it, so that they need not wait for this one's maximum.
         if (__any_sync(0xffffffffu, m == -INFINITY)) {
+          // any score that the row sees will do: weights stay exact far above 1
+          const float first = ch_tmem_ld1(s_col);
+          if (m == -INFINITY && last >= 0 && !(p.window > 0 && from > 0 && sunk <= 0)) m = first;
+          m_next = m;
+        }
+        if (__any_sync(0xffffffffu, m == -INFINITY && last >= 0)) {
           float tops[2] = {m, m};
 #pragma unroll 1
           for (int k = 0; k < CH_TILE; k += 32) {
             uint32_t z[32];
             tmem_ld_32x32(s_col + k, z);
             tmem_ld_wait();
-            mask(z, k);
+            if (!all_seen) mask(z, k);
 #pragma unroll
             for (int e = 0; e < 32; e += 4) {
               tops[0] = max3(tops[0], __uint_as_float(z[e]), __uint_as_float(z[e + 1]));
@@ -536,38 +545,60 @@ attn_chunk_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
               if (*gave_up) break;
           __syncwarp();
         }
-#pragma unroll 1
-        for (int h = 0; h < 2; ++h) {
-          uint32_t z[2][32];
-          tmem_ld_32x32(s_col + h * 64, z[0]);
-          tmem_ld_32x32(s_col + h * 64 + 32, z[1]);
-          tmem_ld_wait();
-#pragma unroll
-          for (int k = 0; k < 2; ++k) {
-            uint32_t w[16];
-            mask(z[k], h * 64 + k * 32);
-#pragma unroll
-            for (int e = 0; e < 32; e += 4) {
-              const float2 x0 = make_float2(__uint_as_float(z[k][e]), __uint_as_float(z[k][e + 1]));
-              const float2 x1 = make_float2(__uint_as_float(z[k][e + 2]), __uint_as_float(z[k][e + 3]));
-              float2 a = fma2(x0, c2, mc2), d = fma2(x1, c2, mc2);
-              a.x = ex2(a.x);
-              a.y = ex2(a.y);
-              d.x = ex2(d.x);
-              d.y = ex2(d.y);
-              tops[0] = max3(tops[0], x0.x, x0.y);
-              tops[1] = max3(tops[1], x1.x, x1.y);
-              sums[0] = add2(sums[0], a);
-              sums[1] = add2(sums[1], d);
-              w[e >> 1] = ch_pack(a.x, a.y);
-              w[(e >> 1) + 1] = ch_pack(d.x, d.y);
-            }
-            ch_tmem_st16(s_col + h * 32 + k * 16, w);              // over scores that have been read
-          }
+        auto hand_over = [&](int h) {
           ch_tmem_st_wait();
           tc_fence_before();
           __syncwarp();
           if (lane == 0) mbar_arrive(h == 0 ? &b.p_half[s] : &b.p_full[s]);
+        };
+        auto form = [&](const uint32_t (&z)[32], int k) {          // weights of 32 keys, over scores that have been read
+          uint32_t w[16];
+#pragma unroll
+          for (int e = 0; e < 32; e += 4) {
+            const float2 x0 = make_float2(__uint_as_float(z[e]), __uint_as_float(z[e + 1]));
+            const float2 x1 = make_float2(__uint_as_float(z[e + 2]), __uint_as_float(z[e + 3]));
+            float2 a = fma2(x0, c2, mc2), d = fma2(x1, c2, mc2);
+            a.x = ex2(a.x);
+            a.y = ex2(a.y);
+            d.x = ex2(d.x);
+            d.y = ex2(d.y);
+            tops[0] = max3(tops[0], x0.x, x0.y);
+            tops[1] = max3(tops[1], x1.x, x1.y);
+            sums[0] = add2(sums[0], a);
+            sums[1] = add2(sums[1], d);
+            w[e >> 1] = ch_pack(a.x, a.y);
+            w[(e >> 1) + 1] = ch_pack(d.x, d.y);
+          }
+          ch_tmem_st16(s_col + k * 16, w);
+        };
+        if (all_seen) {
+#pragma unroll 1
+          for (int h = 0; h < 2; ++h) {
+            uint32_t z[2][32];
+            tmem_ld_32x32(s_col + h * 64, z[0]);
+            tmem_ld_32x32(s_col + h * 64 + 32, z[1]);
+            tmem_ld_wait();
+            form(z[0], 2 * h);
+            form(z[1], 2 * h + 1);
+            hand_over(h);
+          }
+        } else {
+#pragma unroll 1
+          for (int k = 0; k < 4; ++k) {
+            if (key0 + k * 32 > w_hi) {        // behind every row of the warp
+              uint32_t none[16];
+#pragma unroll
+              for (int e = 0; e < 16; ++e) none[e] = 0u;
+              ch_tmem_st16(s_col + k * 16, none);
+            } else {
+              uint32_t z[32];
+              tmem_ld_32x32(s_col + k * 32, z);
+              tmem_ld_wait();
+              if (key0 + k * 32 + 31 > w_lo || behind) mask(z, k * 32);
+              form(z, k);
+            }
+            if (k & 1) hand_over(k >> 1);
+          }
         }
         if (turns && lane == 0) atomicExch_block(&b.turn[quad], 0u);
         l += (sums[0].x + sums[0].y) + (sums[1].x + sums[1].y);

@@ -22,8 +22,8 @@ __global__ void __launch_bounds__(PLAN_THREADS) attn_plan_kernel(const __grid_co
 }
 
 // ------------------------------------------------------------------------------------------------
-// fp32: 16 rows, 128 keys a tile, 16 of them for each of eight warps, which run independently of one another through a
-// unit and join their sums at its end.  Bound by the fp32 pipes and shared memory; a mode for checks, not tuned.
+// fp32, few rows: 16 rows, 128 keys a tile, 16 of them for each of eight warps, which run independently of one another
+// through a unit and join their sums at its end.  Bound by the latency of its loads; a mode for checks.
 // ------------------------------------------------------------------------------------------------
 constexpr int RF_ROWS = 16, RF_WARPS = 8, RF_KEYS = 16, RF_TILE = RF_WARPS * RF_KEYS, RF_THREADS = RF_WARPS * 32;
 template <int DH> struct RfSmem {
@@ -212,6 +212,177 @@ __global__ void __launch_bounds__(RF_THREADS) attn_rows_f32_kernel(const __grid_
 }
 
 // ------------------------------------------------------------------------------------------------
+// fp32, many rows: 64 rows and a tile of 64 keys (32 at head dim 128) in registers, 8 rows by 4 (2) keys a thread: of each
+// product's operands 12 vectors of four are read for 128 multiplications, so that the fp32 pipes set the pace.  The weights
+// pass through shared memory between the two products; the 16 threads of 8 rows share them with nobody else.  Loads of one
+// block hide behind the products of the others of its SM.
+// ------------------------------------------------------------------------------------------------
+constexpr int TF_ROWS = 64, TF_THREADS = 128;
+template <int DH> struct TfCfg {
+  static constexpr int KEYS = DH == 128 ? 32 : 64, KT = KEYS / 16;                 // keys of a tile, of a thread
+  static constexpr int LDQ = DH + 4, LDP = KEYS + 4;               // eight rows of a vector never share banks
+  static constexpr int COLS = DH / 16, VEC = COLS < 4 ? COLS : 4;  // columns of a thread, in vectors
+  static constexpr int FLOATS = TF_ROWS * LDQ + KEYS * LDQ + KEYS * DH + TF_ROWS * LDP;
+  static constexpr int BYTES = FLOATS * 4;
+};
+
+template <int DH>
+__global__ void __launch_bounds__(TF_THREADS) attn_tiles_f32_kernel(const __grid_constant__ AttnParams p) {
+  using C = TfCfg<DH>;
+  extern __shared__ float sm[];
+  __shared__ Piece piece;
+  __shared__ long long slots[2][C::KEYS];
+  float* qs = sm;
+  float* ks = qs + TF_ROWS * C::LDQ;
+  float* vs = ks + C::KEYS * C::LDQ;
+  float* ps = vs + C::KEYS * DH;
+  const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4;
+
+  wait_for_predecessor();
+  block_piece(p, sm, &piece);
+  Cursor c = piece.c;
+  long long left = piece.left, ahead = piece.ahead;
+  const long long share = piece.share;
+  int4 job = make_int4(0, 0, 0, -1);
+  int redo = 0;
+
+  while (left > 0) {
+    const int t0 = c.at, t1 = (int)min((long long)c.u.tiles, t0 + left);
+    const bool whole = t0 == 0 && t1 == c.u.tiles;
+    auto first_key = [&](int t) { return (t < c.u.first_tiles ? t : t + c.u.skip) * C::KEYS; };
+    auto look_up = [&](int t) {                // where the keys of tile t lie
+      if (tid < C::KEYS) {
+        const int key = first_key(t) + tid;
+        slots[t & 1][tid] = unit_sees(p, c.u, key) ? slot_offset(p.c, c.s, key, c.head) : -1;
+      }
+    };
+    for (int i = tid; i < TF_ROWS * DH / 4; i += TF_THREADS) {
+      const int r = i / (DH / 4), e = (i - r * (DH / 4)) * 4;
+      const RowPlace x = row_place(p, c.sp, c.qt, c.head, r);
+      float4 q = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (x.valid) q = *reinterpret_cast<const float4*>((const float*)p.q + x.row * p.ld_q + x.head * p.ld_q_head + e);
+      *reinterpret_cast<float4*>(qs + r * C::LDQ + e) = q;
+    }
+    int pos[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) pos[i] = row_place(p, c.sp, c.qt, c.head, ty * 8 + i).pos;
+    float m[8], l[8], o[8][C::COLS];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      m[i] = -INFINITY;
+      l[i] = 0.f;
+#pragma unroll
+      for (int j = 0; j < C::COLS; ++j) o[i][j] = 0.f;
+    }
+    look_up(t0);
+    __syncthreads();
+    for (int t = t0; t < t1; ++t) {
+      const int key0 = first_key(t);
+#pragma unroll 4
+      for (int i = tid; i < C::KEYS * DH / 4; i += TF_THREADS) {
+        const int k = i / (DH / 4), e = (i - k * (DH / 4)) * 4;
+        const long long at = slots[t & 1][k];
+        cp_async16(ks + k * C::LDQ + e, (const float*)p.c.k + (at < 0 ? 0 : at + e), at >= 0);
+        cp_async16(vs + k * DH + e, (const float*)p.c.v + (at < 0 ? 0 : at + e), at >= 0);
+      }
+      if (t + 1 < t1) look_up(t + 1);
+      cp_async_wait_all();
+      __syncthreads();
+      float z[8][C::KT];
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+#pragma unroll
+        for (int j = 0; j < C::KT; ++j) z[i][j] = 0.f;
+#pragma unroll 2
+      for (int e = 0; e < DH; e += 4) {
+        float4 k[C::KT];
+#pragma unroll
+        for (int j = 0; j < C::KT; ++j) k[j] = *reinterpret_cast<const float4*>(ks + (tx + 16 * j) * C::LDQ + e);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const float4 q = *reinterpret_cast<const float4*>(qs + (ty * 8 + i) * C::LDQ + e);
+#pragma unroll
+          for (int j = 0; j < C::KT; ++j) z[i][j] = fmaf(q.x, k[j].x, fmaf(q.y, k[j].y, fmaf(q.z, k[j].z, fmaf(q.w, k[j].w, z[i][j]))));
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        float top = -INFINITY;
+#pragma unroll
+        for (int j = 0; j < C::KT; ++j) {
+          if (!row_sees(p, pos[i], key0 + tx + 16 * j)) z[i][j] = -INFINITY;
+          top = fmaxf(top, z[i][j]);
+        }
+#pragma unroll
+        for (int d = 8; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+        if (top > m[i]) {
+          const float f = ex2((m[i] - top) * p.scale_log2);
+          m[i] = top;
+          l[i] *= f;
+#pragma unroll
+          for (int j = 0; j < C::COLS; ++j) o[i][j] *= f;
+        }
+        const float ref = m[i] == -INFINITY ? 0.f : m[i];
+#pragma unroll
+        for (int j = 0; j < C::KT; ++j) {
+          const float w = ex2((z[i][j] - ref) * p.scale_log2);
+          l[i] += w;
+          ps[(ty * 8 + i) * C::LDP + tx + 16 * j] = w;
+        }
+      }
+      __syncwarp();
+#pragma unroll 2
+      for (int k = 0; k < C::KEYS; k += 4) {
+        float v[4][C::COLS];
+#pragma unroll
+        for (int n = 0; n < 4; ++n)
+#pragma unroll
+          for (int j = 0; j < C::COLS; j += C::VEC) {
+            const float* from = vs + (k + n) * DH + j * 16 + tx * C::VEC;
+            if (C::VEC == 4) *reinterpret_cast<float4*>(&v[n][j]) = *reinterpret_cast<const float4*>(from);
+            else *reinterpret_cast<float2*>(&v[n][j]) = *reinterpret_cast<const float2*>(from);
+          }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const float4 w = *reinterpret_cast<const float4*>(ps + (ty * 8 + i) * C::LDP + k);
+#pragma unroll
+          for (int j = 0; j < C::COLS; ++j) o[i][j] = fmaf(w.x, v[0][j], fmaf(w.y, v[1][j], fmaf(w.z, v[2][j], fmaf(w.w, v[3][j], o[i][j]))));
+        }
+      }
+      __syncthreads();                         // the next tile's keys and values take the place of these
+    }
+    const int slot = 2 * blockIdx.x + (t0 == 0 ? 1 : 0);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+#pragma unroll
+      for (int d = 8; d > 0; d >>= 1) l[i] += __shfl_xor_sync(0xffffffffu, l[i], d);
+      const int r = ty * 8 + i;
+      const RowPlace x = row_place(p, c.sp, c.qt, c.head, r);
+      if (!x.valid) continue;
+      const long long at = (long long)slot * TF_ROWS + r;
+      float* to = whole ? (float*)p.out + x.row * p.ld_out + x.head * p.ld_out_head : p.part + at * DH;
+      const float by = !whole ? 1.f : l[i] == 0.f ? 0.f : 1.f / l[i];
+#pragma unroll
+      for (int j = 0; j < C::COLS; ++j) {
+        redo |= whole && !isfinite(o[i][j]) && isfinite(l[i]);
+        to[(j / C::VEC) * C::VEC * 16 + tx * C::VEC + j % C::VEC] = o[i][j] * by;
+      }
+      if (tx == 0) {
+        if (!whole) p.part_ml[at] = make_float2(m[i], l[i]);
+        else if (p.lse) p.lse[x.row * p.n_heads + x.head] = l[i] == 0.f ? -INFINITY : fmaf(m[i], p.scale_log2, log2f(l[i])) * LN2;
+      }
+    }
+    if (!whole && t0 == 0) job = make_int4(c.s, c.qt, c.head, last_worker(p, blockIdx.x, share, ahead, c.u.tiles));
+    left -= t1 - t0;
+    ahead += t1 - t0;
+    if (left > 0) c.next_unit(p);
+  }
+  redo = __syncthreads_or(redo);
+  if (tid == 0) { p.jobs[blockIdx.x] = job; p.redo[blockIdx.x] = redo; p.pieces[blockIdx.x] = piece; }
+  let_successor_start();
+}
+
+// ------------------------------------------------------------------------------------------------
 // join of split units: a warp per row, the pieces in the order of their keys; and rows formed once more
 // ------------------------------------------------------------------------------------------------
 constexpr int JN_WARPS = 8, JN_BLOCKS = 8;     // warps a block; blocks for a worker's rows: one wave of them for 148 workers
@@ -318,6 +489,14 @@ static int launch_f32(const AttnParams& p, cudaStream_t s) {
   return launch_after_smem(attn_rows_f32_kernel<DH>, dim3(p.workers), dim3(RF_THREADS), RfSmem<DH>::BYTES, s, p);
 }
 
+template <int DH>
+static int launch_tiles_f32(const AttnParams& p, cudaStream_t s) {
+  static unsigned long long seen = 0;
+  if (attr_needed(&seen))
+    PCM_CUDA_TRY(cudaFuncSetAttribute(attn_tiles_f32_kernel<DH>, cudaFuncAttributeMaxDynamicSharedMemorySize, TfCfg<DH>::BYTES));
+  return launch_after_smem(attn_tiles_f32_kernel<DH>, dim3(p.workers), dim3(TF_THREADS), TfCfg<DH>::BYTES, s, p);
+}
+
 template <typename T, int DH>
 static int launch_join(const Lines& a, int n, cudaStream_t s) {
   int workers = 0, rows = 0;
@@ -359,8 +538,11 @@ static bool attn_sizes_ok(const grpo_kv_cache* c, int64_t n_seq, int64_t n_rows,
   return n_rows * (n_heads / c->n_kv_heads) <= PCM_MAX_VOCAB_CALL;              // rows of a key-value head are counted in 32 bits
 }
 
-// Rows of a key-value head (new tokens times group) up to which a sequence goes to the kernel for few rows.
-constexpr int FEW_ROWS = 32;
+// Rows of a key-value head (new tokens times group) up to which a sequence goes to the kernel for few rows.  bf16: two row
+// tiles at head dim 64 (24 rows of 40 sequences over a window of 1024: 31 us, 45 in the kernel for many), one at 128, whose
+// registers hold no more (24 rows of 16 sequences of 8000: 55 us, 44 in the other).  Head dim 32 has the one kernel.
+// fp32: 37 sequences of up to 120 rows took 43 us, 74 to 80 in the kernel for many.
+static int few_rows_of(int dtype, int dh) { return dtype == GRPO_F32 ? 128 : dh == 128 ? 16 : 32; }
 
 // The lines of a call: which kernels take part, with what workers; n_lines and their regions of the workspace.
 struct CallPlan { int n; bool planned, self[2], chunk[2]; int rows[2], tile[2], workers[2], min_share[2], over[2], up_to[2]; Layout at[2]; size_t total; };
@@ -379,12 +561,14 @@ static CallPlan plan_call(int dtype, int dh, int n_seq, int n_rows, int group, i
     c.planned |= !c.self[i];
   };
   const int all = 0x7FFFFFFF, sms = sm_count();
-  if (dtype == GRPO_F32) { add(false, RF_ROWS, RF_TILE, 2 * sms, 4, 0, all); return c; }
-  const bool many = most > FEW_ROWS && dh != 32;
-  // every sequence brings max_new rows: none has few
-  const bool few = !many || (long long)n_seq * new_most != n_rows;
-  if (few) add(false, most <= 16 ? 16 : 32, attn_rows_tile(), 2 * sms, 1, 0, many ? FEW_ROWS : all);
-  if (many) add(true, attn_chunk_rows(), attn_chunk_tile(), sms, 4, few ? FEW_ROWS : 0, all);
+  // sequences of many rows have a kernel of their own, and so do those of few; where every sequence brings max_new rows, none has few
+  const bool f32 = dtype == GRPO_F32;
+  const int few_rows = few_rows_of(dtype, dh);
+  const bool many = most > few_rows && (f32 || dh != 32), few = !many || (long long)n_seq * new_most != n_rows;
+  if (few && f32) add(false, RF_ROWS, RF_TILE, 2 * sms, 4, 0, many ? few_rows : all);
+  if (few && !f32) add(false, most <= 16 || few_rows == 16 ? 16 : 32, attn_rows_tile(), 2 * sms, 1, 0, many ? few_rows : all);
+  if (many && f32) add(true, TF_ROWS, dh == 128 ? TfCfg<128>::KEYS : TfCfg<64>::KEYS, (dh == 128 ? 2 : 3) * sms, 1, few ? few_rows : 0, all);
+  if (many && !f32) add(true, attn_chunk_rows(), attn_chunk_tile(), sms, 4, few ? few_rows : 0, all);
   return c;
 }
 
@@ -401,10 +585,8 @@ extern "C" size_t grpo_paged_attention_workspace_bytes(const grpo_kv_cache* cach
   const int group = n_heads / cache->n_kv_heads;
   CallPlan c = plan_call(cache->dtype, cache->head_dim, n_seq, n_rows, group, max_new);
   size_t total = c.total;
-  if (cache->dtype == GRPO_BF16) {
-    total = layout(n_seq, 2 * sm_count(), 32, cache->head_dim).total;
-    if (c.chunk[c.n - 1]) total += c.at[c.n - 1].total;
-  }
+  total = layout(n_seq, 2 * sm_count(), cache->dtype == GRPO_F32 ? RF_ROWS : 32, cache->head_dim).total;
+  if (c.chunk[c.n - 1]) total += c.at[c.n - 1].total;
   return total;
 }
 
@@ -460,7 +642,8 @@ extern "C" int grpo_paged_attention(const grpo_kv_cache* cache, const grpo_kv_ba
   }
   for (int i = 0; i < call.n && rc == PCM_OK; ++i) {
     const AttnParams& a = lines.of[i];
-    if (!bf16) rc = dh == 128 ? launch_f32<128>(a, s) : dh == 64 ? launch_f32<64>(a, s) : launch_f32<32>(a, s);
+    if (!bf16 && call.chunk[i]) rc = dh == 128 ? launch_tiles_f32<128>(a, s) : dh == 64 ? launch_tiles_f32<64>(a, s) : launch_tiles_f32<32>(a, s);
+    else if (!bf16) rc = dh == 128 ? launch_f32<128>(a, s) : dh == 64 ? launch_f32<64>(a, s) : launch_f32<32>(a, s);
     else rc = call.chunk[i] ? launch_chunk_bf16(a, dh, s) : launch_rows_bf16(a, dh, s);
   }
   if (rc == PCM_OK) rc = bf16 ? launch_join_as<__nv_bfloat16>(lines, call.n, dh, s) : launch_join_as<float>(lines, call.n, dh, s);

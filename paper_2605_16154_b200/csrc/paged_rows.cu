@@ -346,7 +346,8 @@ static int launch_rows(const AttnParams& p, cudaStream_t s) {
 int attn_rows_tile() { return RB_TILE; }
 int launch_rows_bf16(const AttnParams& p, int dh, cudaStream_t s) {
   if (p.unit_rows == 16) return dh == 128 ? launch_rows<128, 1>(p, s) : dh == 64 ? launch_rows<64, 1>(p, s) : launch_rows<32, 1>(p, s);
-  return dh == 128 ? launch_rows<128, 2>(p, s) : dh == 64 ? launch_rows<64, 2>(p, s) : launch_rows<32, 2>(p, s);
+  if (dh == 128) return PCM_ERR_SHAPE;          // (16 rows are all that its registers hold)
+  return dh == 64 ? launch_rows<64, 2>(p, s) : launch_rows<32, 2>(p, s);
 }
 
 }  // namespace pga

@@ -533,10 +533,12 @@ int grpo_rotary_cache(const grpo_kv_cache* cache, const grpo_kv_batch* batch, in
  *     out[r][h] = sum_j softmax_j(scale q[r][h] . k_j) v_j,   lse[r][h] = log sum_j exp(scale q[r][h] . k_j)
  * over the tokens j of the row's sequence with j <= p and (window = 0 or j > p - window or j < sinks), p the row's position;
  * head h reads key-value head h / (n_heads / n_kv_heads).  A row that sees nothing has out 0 and lse -inf.  Keys and values
- * that a row does not see have no influence on it, NaN and infinities included.
+ * that a row does not see have no influence on it, NaN and infinities included (such values in the slots of later tokens cost
+ * time: the rows that they could reach are formed once more).  A row that sees a score of NaN or +inf is NaN, and so is its lse.
  * q and out [n_rows][n_heads][head_dim] of the cache's type with row and head strides, on 16-byte boundaries like the cache;
- * lse fp32 [n_rows][n_heads] contiguous, may be NULL.  head_dim 32, 64 or 128.  scale > 0.
- * max_new: no sequence brings more new tokens than this (0: not known); it chooses among kernels and sizes the workspace.
+ * lse fp32 [n_rows][n_heads] contiguous, may be NULL.  head_dim 32, 64 or 128.  scale > 0.  out overlaps neither q nor the cache.
+ * max_new: no sequence brings more new tokens than this (0: not known); it chooses among kernels and sizes the workspace, and
+ * has no influence on which rows are computed.
  * Sums and softmax statistics are fp32; in bf16 the weights enter the product with v as bf16 values (chunks of many new
  * tokens; a pair of bf16 values each for few).  fp32 is a mode for checks.
  * workspace: device, 256-byte aligned, >= grpo_paged_attention_workspace_bytes() for the current device (0 when the sizes

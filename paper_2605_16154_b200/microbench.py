@@ -160,6 +160,38 @@ def bench_vocab(a):
     report("token_logp_bwd", lambda: B.grpo_token_logp_bwd(z, tgt, lse, ent, dlogp, dent, dlogits=dz), 4.0 * m * V, 0)
 
 
+def bench_rollout(a):
+    """The rollout side: positions of a training batch's queries, prefixes of `chunks` chunks into the cache and their attention,
+    a decoding step of `seqs` sequences of `length` tokens (bf16).  Bytes and flops are what each call cannot do without."""
+    g = torch.Generator(device="cuda").manual_seed(0)
+    H, kv, dh, page = a.heads, a.kv, a.dh, a.page
+    turns, _ = B.grpo_rotary_freqs(dh)
+    turns = turns.cuda()
+
+    def report(name, fn, nbytes, flops):
+        ms = _time(fn, a.iters)
+        print(json.dumps({"kernel": name, "ms": ms, "gbs": nbytes / (ms * 1e6), "tflops": flops / (ms * 1e9)}))
+    n = a.chunks * 312
+    x = torch.randn(n, H, dh, generator=g, device="cuda").to(torch.bfloat16)
+    pos = (torch.arange(n, device="cuda") % 312).to(torch.int32)
+    report("rotary", lambda: B.grpo_rotary(x, pos, turns), 4.0 * n * H * dh, 0)
+    report("rotary gradient", lambda: B.grpo_rotary(x, pos, turns, inverse=True), 4.0 * n * H * dh, 0)
+    del x
+    for name, seqs, new, length in (("prefix", a.chunks, 256, 256), ("step", a.seqs, 1, a.length)):
+        pages = -(-length // page)
+        k, v = (torch.randn(seqs * pages, page, kv, dh, generator=g, device="cuda", dtype=torch.bfloat16) for _ in range(2))
+        table = torch.randperm(seqs * pages, generator=g, device="cuda").to(torch.int32).view(seqs, pages)
+        seq_len = torch.full((seqs,), length, dtype=torch.int32, device="cuda")
+        q_off = (torch.arange(seqs + 1, device="cuda") * new).to(torch.int32)
+        fused = torch.randn(seqs * new, H + 2 * kv, dh, generator=g, device="cuda").to(torch.bfloat16)
+        q = fused[:, :H].contiguous()
+        report(f"rotary_cache {name}", lambda: B.grpo_rotary_cache(fused[:, :H], fused[:, H:H + kv], fused[:, H + kv:], k, v, table, seq_len, q_off,
+                                                                   turns), 4.0 * fused.numel(), 0)
+        pairs = seqs * (new * (length - new) + new * (new + 1) / 2)
+        report(f"paged_attention {name}", lambda: B.grpo_paged_attention(q, k, v, table, seq_len, q_off, max_new=new),
+               4.0 * seqs * length * kv * dh + 4.0 * q.numel(), 4.0 * pairs * H * dh)
+
+
 def main():
     ap = argparse.ArgumentParser()
     sub = ap.add_subparsers(dest="what", required=True)
@@ -183,8 +215,13 @@ def main():
     v.add_argument("--rows", type=int, default=21504); v.add_argument("--tokens", type=int, default=119808)
     v.add_argument("--vocab", type=int, default=32000); v.add_argument("--d", type=int, default=1024)
     v.add_argument("--top", type=int, default=4); v.add_argument("--iters", type=int, default=10)
+    r = sub.add_parser("rollout")
+    r.add_argument("--chunks", type=int, default=384); r.add_argument("--seqs", type=int, default=256)
+    r.add_argument("--length", type=int, default=2048); r.add_argument("--heads", type=int, default=16)
+    r.add_argument("--kv", type=int, default=16); r.add_argument("--dh", type=int, default=64)
+    r.add_argument("--page", type=int, default=16); r.add_argument("--iters", type=int, default=10)
     a = ap.parse_args()
-    {"gemm": bench_gemm, "attention": bench_attention, "pcm": bench_pcm, "pack": bench_pack, "vocab": bench_vocab}[a.what](a)
+    {"gemm": bench_gemm, "attention": bench_attention, "pcm": bench_pcm, "pack": bench_pack, "vocab": bench_vocab, "rollout": bench_rollout}[a.what](a)
 
 
 if __name__ == "__main__":

@@ -566,7 +566,7 @@ static CallPlan plan_call(int dtype, int dh, int n_seq, int n_rows, int group, i
   const int few_rows = few_rows_of(dtype, dh);
   const bool many = most > few_rows && (f32 || dh != 32), few = !many || (long long)n_seq * new_most != n_rows;
   if (few && f32) add(false, RF_ROWS, RF_TILE, 2 * sms, 4, 0, many ? few_rows : all);
-  if (few && !f32) add(false, most <= 16 || few_rows == 16 ? 16 : 32, attn_rows_tile(), 2 * sms, 1, 0, many ? few_rows : all);
+  if (few && !f32) add(false, most <= 16 || few_rows == 16 ? 16 : 32, attn_rows_tile(dh), 2 * sms, 1, 0, many ? few_rows : all);
   if (many && f32) add(true, TF_ROWS, dh == 128 ? TfCfg<128>::KEYS : TfCfg<64>::KEYS, (dh == 128 ? 2 : 3) * sms, 1, few ? few_rows : 0, all);
   if (many && !f32) add(true, attn_chunk_rows(), attn_chunk_tile(), sms, 4, few ? few_rows : 0, all);
   return c;

@@ -323,7 +323,7 @@ __device__ inline void block_piece(const AttnParams& p, void* scratch, Piece* pi
 
 // Launches of the kernels on a line that is planned (workers, unit_rows and tile set).
 bool page_map(CUtensorMap* tm, const void* base, const KvView& c, int dh, int box_cols, int box_rows);
-int attn_rows_tile();
+int attn_rows_tile(int dh);
 int launch_rows_bf16(const AttnParams& p, int dh, cudaStream_t s);
 int attn_chunk_rows();
 int attn_chunk_tile();

@@ -721,7 +721,8 @@ static EncodeFn encode_fn() {
   }
   return fn;
 }
-// Pages as [page][slot][head][column], boxes of box_rows slots of one head, swizzled rows of box_cols (64 or 32) columns.
+// Pages as [page][slot][head][column] (reads of more than a head's row bring in others' too soon: a step of 256 sequences of 2048,
+// 16 heads of 64, took 512 us with 256 bytes at a time, 400 with 128), boxes of box_rows slots of one head, swizzled rows of box_cols (64 or 32) columns.
 bool page_map(CUtensorMap* tm, const void* base, const KvView& c, int dh, int box_cols, int box_rows) {
   EncodeFn fn = encode_fn();
   if (!fn) return false;
@@ -730,7 +731,7 @@ bool page_map(CUtensorMap* tm, const void* base, const KvView& c, int dh, int bo
   cuuint64_t strides[3] = {c.n_kv > 1 ? (cuuint64_t)c.ld_head * 2 : one, (cuuint64_t)c.ld_slot * 2, c.n_pages > 1 ? (cuuint64_t)c.ld_page * 2 : one};
   cuuint32_t box[4] = {(cuuint32_t)box_cols, 1u, (cuuint32_t)box_rows, 1u}, step[4] = {1, 1, 1, 1};
   return fn(tm, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(base), dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
-            box_cols == 64 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+            box_cols == 64 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, dh >= 128 ? CU_TENSOR_MAP_L2_PROMOTION_L2_256B : CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 template <int DH>

@@ -1,7 +1,7 @@
 // Attention of few new tokens over a paged cache in bf16: decoding steps, short chunks, and head dim 32.
 //
 // What bounds it is the reading of the cache, each key and value once for the 16 or 32 rows of a unit (new tokens times the
-// query heads of a key-value head).  Four warps share a tile of 64 keys, 16 each, and run through their unit without
+// query heads of a key-value head).  Four warps share a tile of 64 or 128 keys, and run through their unit without
 // waiting for one another: each copies its own keys and values ahead into its own ring of shared memory (TMA, whose one
 // instruction for 8 or 16 keys of a page leaves the warp's time to the products: with 16 bytes a lane a step of 256 sequences took
 // 322 us), forms scores and weights in registers (mma.sync m16n8k16: a tile of so few rows would leave a tcgen05 tile of
@@ -16,13 +16,15 @@
 namespace pcm {
 namespace pga {
 
-constexpr int RB_WARPS = 4, RB_THREADS = RB_WARPS * 32, RB_KEYS = 16, RB_TILE = RB_WARPS * RB_KEYS;
+constexpr int RB_WARPS = 4, RB_THREADS = RB_WARPS * 32;
 template <int DH> struct RbCfg {
-  static constexpr int STAGES = DH == 128 ? 3 : DH == 64 ? 6 : 8;
-  static constexpr int ROW = DH * 2, HALF = RB_KEYS * ROW, STAGE = 2 * HALF;       // bytes: a key, 16 keys, keys and values
+  // keys of a warp's step: 8 KB of keys and values (4 at head dim 32), so that what a step costs beside them weighs alike
+  static constexpr int KEYS = DH == 128 ? 16 : 32, TILE = RB_WARPS * KEYS;
+  static constexpr int STAGES = DH == 32 ? 6 : 3;
+  static constexpr int ROW = DH * 2, HALF = KEYS * ROW, STAGE = 2 * HALF;          // bytes: a key, a step's keys, keys and values
   static constexpr int RING = STAGES * STAGE;
   static constexpr int SLAB_COLS = DH < 64 ? DH : 64, SLABS = DH / SLAB_COLS;      // columns of a swizzled row
-  static constexpr int SLAB_ROW = SLAB_COLS * 2, SLAB = RB_KEYS * SLAB_ROW;
+  static constexpr int SLAB_ROW = SLAB_COLS * 2, SLAB = KEYS * SLAB_ROW;
   static constexpr int BYTES = RB_WARPS * RING + 1024;             // tiles start on multiples of 1024 bytes
 };
 
@@ -48,7 +50,7 @@ __device__ __forceinline__ void mma16816(float (&d)[4], const uint32_t (&a)[4], 
                : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
                : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
-// 16-byte chunk c of row r within 16 rows of DH values, as TMA leaves them: eight rows of one chunk never share banks
+// 16-byte chunk c of row r within a step's rows of DH values, as TMA leaves them: eight rows of one chunk never share banks
 template <int DH> __device__ __forceinline__ uint32_t rb_at(int r, int c) {
   using C = RbCfg<DH>;
   if (DH < 64) return (uint32_t)(r * C::SLAB_ROW + ((c ^ ((r >> 1) & 3)) << 4));
@@ -67,6 +69,7 @@ __global__ void __launch_bounds__(RB_THREADS, 2) attn_rows_bf16_kernel(const __g
                       const int box_rows) {
   using C = RbCfg<DH>;
   constexpr int UR = 16 * MT, KT = DH / 16, NT = DH / 8, LEAD = C::STAGES - 1;
+  constexpr int KEYS = C::KEYS, NK = KEYS / 8, KB = KEYS / 16;     // keys of a step, in columns of 8 and blocks of 16
   extern __shared__ uint8_t rb_raw[];
   __shared__ Piece piece;
   __shared__ uint64_t full[RB_WARPS][C::STAGES];
@@ -100,7 +103,7 @@ __global__ void __launch_bounds__(RB_THREADS, 2) attn_rows_bf16_kernel(const __g
     const bool whole = t0 == 0 && t1 == c.u.tiles;
     auto first_key = [&](int i) {
       const int t = t0 + i;
-      return (t < c.u.first_tiles ? t : t + c.u.skip) * RB_TILE + warp * RB_KEYS;
+      return (t < c.u.first_tiles ? t : t + c.u.skip) * C::TILE + warp * KEYS;
     };
     // Where the boxes of step i lie (lane: box): page and slot.  Boxes that no row of the unit sees lie behind the last page,
     // which reads as zeros.
@@ -108,7 +111,7 @@ __global__ void __launch_bounds__(RB_THREADS, 2) attn_rows_bf16_kernel(const __g
       int2 at = make_int2(p.c.n_pages, 0);
       if (i < steps) {
         const int key = first_key(i) + lane * box_rows;
-        if (lane * box_rows < RB_KEYS && key < c.u.end && (key + box_rows > c.u.low || key < p.sinks)) {
+        if (lane * box_rows < KEYS && key < c.u.end && (key + box_rows > c.u.low || key < p.sinks)) {
           const int n = fast_div(key, p.c.div_page), page = p.c.table[c.s * p.c.ld_table + n];
           if (page >= 0 && page < p.c.n_pages) at = make_int2(page, key - n * p.c.page_size);
           else kv_report(p.c, STATUS_BAD_PAGE);
@@ -122,7 +125,7 @@ __global__ void __launch_bounds__(RB_THREADS, 2) attn_rows_bf16_kernel(const __g
       uint64_t* bar = &full[warp][st];
       if (lane == 0) mbar_expect_tx(bar, C::STAGE);
       __syncwarp();
-      if (lane * box_rows < RB_KEYS) {
+      if (lane * box_rows < KEYS) {
         uint8_t* dst = my_ring + st * C::STAGE + lane * box_rows * C::SLAB_ROW;
 #pragma unroll
         for (int slab = 0; slab < C::SLABS; ++slab) {
@@ -174,44 +177,50 @@ __global__ void __launch_bounds__(RB_THREADS, 2) attn_rows_bf16_kernel(const __g
           kv_report(p.c, STATUS_TIMEOUT);
           break;
         }
-        const uint32_t kb = ring + st * C::STAGE, vb = kb + C::HALF;
-        if (key0 + RB_KEYS > c.sp.len) {       // slots behind the end of a sequence may never have been written
-          for (int r = max(0, c.sp.len - key0) * NT + lane; r < RB_KEYS * NT; r += 32)
+        const uint32_t kb_at = ring + st * C::STAGE, vb = kb_at + C::HALF;
+        if (key0 + KEYS > c.sp.len) {       // slots behind the end of a sequence may never have been written
+          for (int r = max(0, c.sp.len - key0) * NT + lane; r < KEYS * NT; r += 32)
             *reinterpret_cast<uint4*>(my_ring + st * C::STAGE + C::HALF + rb_at<DH>(r / NT, r % NT)) = make_uint4(0, 0, 0, 0);
           rb_fence_async();
           __syncwarp();
         }
-        float z[MT][2][4];
+        float z[MT][NK][4];
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
-          for (int n = 0; n < 2; ++n) z[mt][n][0] = z[mt][n][1] = z[mt][n][2] = z[mt][n][3] = 0.f;
+          for (int n = 0; n < NK; ++n) z[mt][n][0] = z[mt][n][1] = z[mt][n][2] = z[mt][n][3] = 0.f;
 #pragma unroll
-        for (int k = 0; k < KT; ++k) {
-          uint32_t b[4];
-          ldm4(b, kb + rb_at<DH>((lane & 7) + ((lane >> 4) << 3), k * 2 + ((lane >> 3) & 1)));
+        for (int k = 0; k < KT; ++k)
 #pragma unroll
-          for (int mt = 0; mt < MT; ++mt) {
-            mma16816(z[mt][0], qf[mt][k], b[0], b[1]);
-            mma16816(z[mt][1], qf[mt][k], b[2], b[3]);
+          for (int kb = 0; kb < KB; ++kb) {
+            uint32_t b[4];
+            ldm4(b, kb_at + rb_at<DH>(kb * 16 + (lane & 7) + ((lane >> 4) << 3), k * 2 + ((lane >> 3) & 1)));
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt) {
+              mma16816(z[mt][2 * kb], qf[mt][k], b[0], b[1]);
+              mma16816(z[mt][2 * kb + 1], qf[mt][k], b[2], b[3]);
+            }
           }
-        }
-        const bool all_seen = key0 + RB_KEYS - 1 <= p_low &&
-                              (p.window == 0 || key0 > p_high - p.window || key0 + RB_KEYS - 1 < p.sinks);
-        uint32_t hi[MT][4], lo[MT][4];
+        const bool all_seen = key0 + KEYS - 1 <= p_low &&
+                              (p.window == 0 || key0 > p_high - p.window || key0 + KEYS - 1 < p.sinks);
         if (!all_seen)
 #pragma unroll
           for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
-            for (int e = 0; e < 8; ++e)
-              if (!row_sees(p, pos[mt][(e >> 1) & 1], key0 + (e >> 2) * 8 + t4 * 2 + (e & 1))) z[mt][e >> 2][e & 3] = -INFINITY;
+            for (int n = 0; n < NK; ++n)
+#pragma unroll
+              for (int e = 0; e < 4; ++e)
+                if (!row_sees(p, pos[mt][e >> 1], key0 + n * 8 + t4 * 2 + (e & 1))) z[mt][n][e] = -INFINITY;
         float top[MT][2];
         bool rise = false;
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
-          for (int h = 0; h < 2; ++h)
-            top[mt][h] = fmaxf(fmaxf(z[mt][0][h * 2], z[mt][0][h * 2 + 1]), fmaxf(z[mt][1][h * 2], z[mt][1][h * 2 + 1]));
+          for (int h = 0; h < 2; ++h) {
+            top[mt][h] = fmaxf(z[mt][0][h * 2], z[mt][0][h * 2 + 1]);
+#pragma unroll
+            for (int n = 1; n < NK; ++n) top[mt][h] = fmaxf(top[mt][h], fmaxf(z[mt][n][h * 2], z[mt][n][h * 2 + 1]));
+          }
 #pragma unroll
         for (int d = 1; d <= 2; d <<= 1)
 #pragma unroll
@@ -232,31 +241,35 @@ __global__ void __launch_bounds__(RB_THREADS, 2) attn_rows_bf16_kernel(const __g
               for (int n = 0; n < NT; ++n) { o[mt][n][h * 2] *= f; o[mt][n][h * 2 + 1] *= f; }
             }
         }
+        uint32_t hi[MT][KB][4], lo[MT][KB][4];
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
             const float ref = m[mt][h] == -INFINITY ? 0.f : m[mt][h];
 #pragma unroll
-            for (int n = 0; n < 2; ++n) {
+            for (int n = 0; n < NK; ++n) {
               const float a = ex2((z[mt][n][h * 2] - ref) * p.scale_log2), b = ex2((z[mt][n][h * 2 + 1] - ref) * p.scale_log2);
               l[mt][h] += a + b;
-              split2(a, b, hi[mt][n * 2 + h], lo[mt][n * 2 + h]);
+              split2(a, b, hi[mt][n >> 1][(n & 1) * 2 + h], lo[mt][n >> 1][(n & 1) * 2 + h]);
             }
           }
         // high parts of four columns of tiles, then their low parts: products into one accumulator wait for one another
 #pragma unroll
-        for (int n = 0; n < NT; n += 4) {
-          uint32_t b[2][4];
-          ldm4t(b[0], vb + rb_at<DH>((lane & 7) + (((lane >> 3) & 1) << 3), n + (lane >> 4)));
-          ldm4t(b[1], vb + rb_at<DH>((lane & 7) + (((lane >> 3) & 1) << 3), n + 2 + (lane >> 4)));
+        for (int n = 0; n < NT; n += 4)
 #pragma unroll
-          for (int part = 0; part < 2; ++part)
+          for (int kb = 0; kb < KB; ++kb) {
+            uint32_t b[2][4];
+            ldm4t(b[0], vb + rb_at<DH>(kb * 16 + (lane & 7) + (((lane >> 3) & 1) << 3), n + (lane >> 4)));
+            ldm4t(b[1], vb + rb_at<DH>(kb * 16 + (lane & 7) + (((lane >> 3) & 1) << 3), n + 2 + (lane >> 4)));
 #pragma unroll
-            for (int mt = 0; mt < MT; ++mt)
+            for (int part = 0; part < 2; ++part)
 #pragma unroll
-              for (int k = 0; k < 4; ++k) mma16816(o[mt][n + k], part ? lo[mt] : hi[mt], b[k >> 1][(k & 1) * 2], b[k >> 1][(k & 1) * 2 + 1]);
-        }
+              for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                  mma16816(o[mt][n + k], part ? lo[mt][kb] : hi[mt][kb], b[k >> 1][(k & 1) * 2], b[k >> 1][(k & 1) * 2 + 1]);
+          }
       }
       __syncwarp();                            // the stage is copied over in the next step
     }
@@ -338,12 +351,13 @@ static int launch_rows(const AttnParams& p, cudaStream_t s) {
   static unsigned long long seen = 0;
   if (attr_needed(&seen))
     PCM_CUDA_TRY(cudaFuncSetAttribute(attn_rows_bf16_kernel<DH, MT>, cudaFuncAttributeMaxDynamicSharedMemorySize, RbCfg<DH>::BYTES));
-  const int box = p.c.page_size % RB_KEYS ? 8 : RB_KEYS;
+  int box = RbCfg<DH>::KEYS;
+  while (p.c.page_size % box) box /= 2;        // (pages are of a multiple of 8)
   CUtensorMap tm_k, tm_v;
   if (!page_map(&tm_k, p.c.k, p.c, DH, RbCfg<DH>::SLAB_COLS, box) || !page_map(&tm_v, p.c.v, p.c, DH, RbCfg<DH>::SLAB_COLS, box)) return PCM_ERR_CUDA;
   return launch_after_smem(attn_rows_bf16_kernel<DH, MT>, dim3(p.workers), dim3(RB_THREADS), RbCfg<DH>::BYTES, s, tm_k, tm_v, p, box);
 }
-int attn_rows_tile() { return RB_TILE; }
+int attn_rows_tile(int dh) { return dh == 128 ? RbCfg<128>::TILE : dh == 64 ? RbCfg<64>::TILE : RbCfg<32>::TILE; }
 int launch_rows_bf16(const AttnParams& p, int dh, cudaStream_t s) {
   if (p.unit_rows == 16) return dh == 128 ? launch_rows<128, 1>(p, s) : dh == 64 ? launch_rows<64, 1>(p, s) : launch_rows<32, 1>(p, s);
   if (dh == 128) return PCM_ERR_SHAPE;          // (16 rows are all that its registers hold)

@@ -47,6 +47,8 @@ __device__ __forceinline__ void rt_store(__nv_bfloat16* p, float x) { *p = __flo
 // The sequence of a row (ascending offsets), or -1.
 __device__ static int sequence_of(const KvView& c, int row) {
   if (!c.q_off) return row < c.n_seq ? row : -1;
+  const int even = (int)((long long)row * c.n_seq / c.n_rows);     // right where all sequences bring as many rows
+  if (c.q_off[even] <= row && row < c.q_off[even + 1]) return even;
   int lo = 0, hi = c.n_seq;                    // first s with q_off[s + 1] > row
   while (lo < hi) {
     const int mid = (lo + hi) >> 1;
@@ -93,10 +95,12 @@ __global__ void __launch_bounds__(RT_THREADS, 8) rotary_kernel(const __grid_cons
     row_pos[threadIdx.x] = t;
     row_slot[threadIdx.x] = slot;
   }
+  double turns = (int)threadIdx.x < n_here * p.half ? p.turns[threadIdx.x % p.half] : 0.0;      // on its way with the row's place
   __syncthreads();
   for (int i = threadIdx.x; i < n_here * p.half; i += RT_THREADS) {
     const int r = i / p.half;
-    const double part = (double)row_pos[r] * p.turns[i - r * p.half];
+    if (i != (int)threadIdx.x) turns = p.turns[i - r * p.half];
+    const double part = (double)row_pos[r] * turns;
     float s, c;
     sincospif(2.f * (float)(part - rint(part)), &s, &c);
     cs[i] = make_float2(c * p.amplitude, (p.inverse ? -s : s) * p.amplitude);

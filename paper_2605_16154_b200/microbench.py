@@ -6,6 +6,7 @@ kernel is bandwidth bound).  One JSON line per case.
     python -m paper_2605_16154_b200.microbench pcm [--tasks 8192 --G 8 --T 128 --phases 10 --budget 24]
     python -m paper_2605_16154_b200.microbench pack [--kept 384 --P 256 --d 1024]
     python -m paper_2605_16154_b200.microbench vocab [--rows 21504 --tokens 119808 --vocab 32000 --d 1024 --top 4]
+    python -m paper_2605_16154_b200.microbench rollout [--chunks 384 --seqs 256 --length 2048 --heads 16 --kv 16 --dh 64 --page 16]
 """
 from __future__ import annotations
 

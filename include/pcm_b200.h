@@ -542,7 +542,7 @@ int grpo_rotary_cache(const grpo_kv_cache* cache, const grpo_kv_batch* batch, in
  * Sums and softmax statistics are fp32; in bf16 the weights enter the product with v as bf16 values (chunks of many new
  * tokens; a pair of bf16 values each for few).  fp32 is a mode for checks.
  * workspace: device, 256-byte aligned, >= grpo_paged_attention_workspace_bytes() for the current device (0 when the sizes
- * are not supported), which never falls as n_rows, n_seq or max_new grow. */
+ * are not supported), which never falls as n_rows, n_seq or max_new grow (max_new 0 counts as n_rows). */
 size_t grpo_paged_attention_workspace_bytes(const grpo_kv_cache* cache, int32_t n_seq, int32_t n_rows, int32_t n_heads, int32_t max_new);
 int grpo_paged_attention(const grpo_kv_cache* cache, const grpo_kv_batch* batch, int32_t n_rows, const void* q, int64_t ld_q,
                          int64_t ld_q_head, int32_t n_heads, float scale, int32_t window, int32_t sinks, int32_t max_new, void* out,

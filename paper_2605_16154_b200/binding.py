@@ -762,6 +762,8 @@ def _turns(call: str, turns: Optional[torch.Tensor], device) -> tuple:
     """(address, rotated elements of a head) of a table of frequencies."""
     if turns is None:
         return None, 0
+    if not isinstance(turns, torch.Tensor):
+        raise PcmError(call, -1)
     return _vector(call, turns, device, _f64, turns.numel()), 2 * turns.numel()
 
 
@@ -787,6 +789,8 @@ def grpo_rotary(x: torch.Tensor, pos: torch.Tensor, turns: torch.Tensor, interle
 
 def _cache(call: str, k_pages: torch.Tensor, v_pages: torch.Tensor):
     """The cache of pages [n_pages, page_size, kv heads, dim], in any order of the first three in memory."""
+    if not (isinstance(k_pages, torch.Tensor) and isinstance(v_pages, torch.Tensor)):
+        raise PcmError(call, -1)
     dev = k_pages.device
     ok = k_pages.is_cuda and k_pages.dim() == 4 and v_pages.device == dev and v_pages.dtype == k_pages.dtype
     dt = _DTYPES.get(k_pages.dtype)
@@ -801,6 +805,8 @@ def _cache(call: str, k_pages: torch.Tensor, v_pages: torch.Tensor):
 
 
 def _sequences(call: str, table: torch.Tensor, seq_len: torch.Tensor, q_off: Optional[torch.Tensor], dev) -> grpo_kv_batch:
+    if not (isinstance(table, torch.Tensor) and isinstance(seq_len, torch.Tensor)):
+        raise PcmError(call, -1)
     n = seq_len.numel()
     if table.device != dev or table.dtype != _i32 or table.dim() != 2 or table.shape[0] != n:
         raise PcmError(call, -1)

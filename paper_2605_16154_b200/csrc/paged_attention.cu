@@ -409,8 +409,10 @@ __device__ __noinline__ void redo_rows(const AttnParams& p, int w, int r) {
         float o[DH / 32];
         const float lse = exact_row<T, DH>(p, c.s, c.head, c.u, x, o);
         store_row<T, DH>(p, x, o);
-        float* at = p.lse + (x.row * p.n_heads + x.head);
-        if (p.lse && (threadIdx.x & 31) == 0 && !(*at == *at)) *at = lse;          // NaN: the row's weights did not fit either
+        if (p.lse && (threadIdx.x & 31) == 0) {
+          float& kept = p.lse[x.row * p.n_heads + x.head];
+          if (kept != kept) kept = lse;        // NaN: the row's weights did not fit either
+        }
       }
     }
     piece.left -= min((long long)c.u.tiles - c.at, piece.left);
@@ -618,7 +620,7 @@ extern "C" int grpo_paged_attention(const grpo_kv_cache* cache, const grpo_kv_ba
   p.n_heads = n_heads; p.group = n_heads / cache->n_kv_heads;
   p.div_group = make_fastdiv(p.group);
   p.scale_log2 = scale * LOG2E;
-  p.window = window; p.sinks = sinks;
+  p.window = window; p.sinks = sinks < PCM_MAX_VOCAB_CALL ? sinks : PCM_MAX_VOCAB_CALL;       // (no sequence is longer: sums with tiles fit)
   cudaStream_t s = (cudaStream_t)stream;
   prof_begin(PC_ATTN, s);
   const bool bf16 = cache->dtype == GRPO_BF16;

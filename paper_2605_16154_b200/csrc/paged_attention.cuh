@@ -221,6 +221,7 @@ __device__ inline float exact_row(const AttnParams& p, int s, int kv_head, const
       }
 #pragma unroll
       for (int d = 16; d > 0; d >>= 1) z += __shfl_xor_sync(0xffffffffu, z, d);
+      if (z == -INFINITY) continue;            // weighs nothing, and is no reference
       if (z > m) {
         const float f = ex2((m - z) * p.scale_log2);
         m = z;

@@ -31,6 +31,7 @@ constexpr unsigned long long CH_WAIT_NS = 2000000000ull;
 constexpr int CH_TMEM = 512;
 constexpr int CH_TURNS = 8;                    // tiles of a piece from which on its streams take turns (8 x 1024 tokens behind 4096 to 8192: 387 us,
                                                // 436 without; units of two tiles: 361 us without, 397 with)
+constexpr int CH_TURN_TRIES = 1 << 12;
 constexpr float CH_RISE = 32.f;                // powers of two by which a maximum may outgrow its reference
 constexpr float CH_WILD = 100.f;               // .. within one tile: 128 weights of 2^100 still have a sum
 template <int DH> struct ChCfg {
@@ -540,9 +541,8 @@ attn_chunk_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
         // The two warps of a quarter of the SM, one of each stream, take turns: side by side both would end late, and the tensor
         // core would wait for both at once.
         if (turns) {
-          if (lane == 0)
-            while (atomicCAS_block(&b.turn[quad], 0u, 1u) != 0u)
-              if (*gave_up) break;
+          if (lane == 0)                       // (a turn saves time and guards nothing: the wait for it may end)
+            for (int n = 0; n < CH_TURN_TRIES && atomicCAS_block(&b.turn[quad], 0u, 1u) != 0u; ++n) {}
           __syncwarp();
         }
         auto hand_over = [&](int h) {
@@ -604,7 +604,7 @@ attn_chunk_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
         l += (sums[0].x + sums[0].y) + (sums[1].x + sums[1].y);
         const float top = fmaxf(tops[0], tops[1]), over = (top - m) * p.scale_log2;
         m_next = over > CH_RISE ? top : m;
-        if (over > CH_WILD) wild = true;
+        if (over > CH_WILD || fabsf(mc) == INFINITY) wild = true;      // (a scaled reference beyond fp32 hides every difference from it)
         if (top == INFINITY) l = NAN;          // an infinite score makes its row NaN, like a NaN
         ++o_count;
         begun = true;

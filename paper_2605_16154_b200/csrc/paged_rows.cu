@@ -172,13 +172,13 @@ __global__ void __launch_bounds__(RB_THREADS, 2) attn_rows_bf16_kernel(const __g
       if (key0 < c.u.end && ok) {
         const int st = taken % C::STAGES;
         ok = __all_sync(0xffffffffu, mbar_wait_bounded(&full[warp][st], (taken / C::STAGES) & 1u, RB_WAIT_NS));
-        ++taken;
         if (!ok) {                             // (the copies have not landed: the block's results are not meaningful)
           kv_report(p.c, STATUS_TIMEOUT);
           break;
         }
+        ++taken;
         const uint32_t kb_at = ring + st * C::STAGE, vb = kb_at + C::HALF;
-        if (key0 + KEYS > c.sp.len) {       // slots behind the end of a sequence may never have been written
+        if (key0 + KEYS > c.sp.len) {          // slots behind the end of a sequence may never have been written
           for (int r = max(0, c.sp.len - key0) * NT + lane; r < KEYS * NT; r += 32)
             *reinterpret_cast<uint4*>(my_ring + st * C::STAGE + C::HALF + rb_at<DH>(r / NT, r % NT)) = make_uint4(0, 0, 0, 0);
           rb_fence_async();

@@ -538,3 +538,44 @@ def test_a_layer_token_by_token_is_the_layer_over_the_whole_sequence(kind):
     tol = 1e-5 if kind == "f32" else 2 * (2.0 ** -8 + 2.0 ** -8) * float(vv)
     assert float((out.view(n * S, d).double() - want.double()).abs().max()) <= tol
     assert float((lse - want_lse.transpose(1, 2)).abs().max()) <= (1e-5 if kind == "f32" else 1e-3)
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("new", [1, 300])
+def test_more_sinks_than_a_sequence_can_have_are_all_of_it(kind, new):
+    c = Case(71, kind, 64, 2, 2, 16, [900], [new])
+    full, lse = c.run()
+    out, lse2 = c.run(64, 2 ** 31 - 1)
+    assert torch.equal(out, full) and torch.equal(lse, lse2)
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("new", [1, 300])
+def test_scaled_scores_beyond_fp32_choose_the_largest(kind, new):
+    """Scores near 1e34 times a scale of 1e6: any difference leaves the lesser score no weight.  Elements are a power of two
+    times small integers: every score is exact and the largest ones are the same in both arithmetics."""
+    c = Case(73, kind, 64, 1, 2, 16, [700], [new])
+    g = gen(74)
+    for t in (c.q, c.k_pages):
+        t.copy_((torch.randint(-8, 9, t.shape, generator=g, device="cuda") * 2.0 ** 52).to(c.t))
+    out, _ = c.run(scale=1e6)
+    want = ro.attend(host(c.q), host(c.k_pages), host(c.v_pages), c.table_host, c.lens, c.q_off_host, 1e6)[0]
+    assert bool(torch.isfinite(out).all())
+    assert float(np.abs(host(out) - want).max()) <= (2.0 ** -22 if kind == "f32" else 2.0 ** -8) * float(np.abs(want).max())
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("new", [2, 130])
+def test_a_score_of_minus_infinity_weighs_nothing_beside_values_that_no_row_sees(kind, new):
+    c = Case(75, kind, 64, 1, 2, 16, [new + 400], [new])
+    c.q[..., 0] = 1.0
+    page, slot = c.table_host[0][0], 0
+    c.k_pages[page, slot, 0, 0] = float("-inf")
+    clean, lse = c.run()
+    assert bool(torch.isfinite(clean).all()) and bool(torch.isfinite(lse).all())
+    page, slot = c.table_host[0][(new + 399) // 16], (new + 399) % 16                 # the last token's slot
+    c.v_pages[page, slot] = float("nan")
+    out, lse2 = c.run()
+    tol = 0 if kind == "f32" else 2.0 ** -7
+    assert bool(torch.isfinite(out[:-1]).all()) and torch.equal(lse, lse2)
+    assert float((out[:-1].double() - clean[:-1].double()).abs().max()) <= tol * float(clean.double().abs().max()) + 1e-5

@@ -160,6 +160,18 @@ def test_binding_refuses_host_tensors_and_sizes_that_do_not_fit():
         assert e.value.code == SHAPE
 
 
+def test_binding_refuses_what_is_no_tensor():
+    B = _lib()
+    x, pos, pages = torch.zeros(3, 2, 64), torch.zeros(3, dtype=torch.int32), torch.zeros(4, 16, 2, 64)
+    for f in (lambda: B.grpo_rotary(None, pos, None), lambda: B.grpo_rotary_cache(x, x, x, None, pages, pos, pos, None, None),
+              lambda: B.grpo_rotary_cache(x, x, x, pages, [1], pos, pos, None, None), lambda: B.grpo_paged_attention(x, None, None, None, None),
+              lambda: B.grpo_paged_attention_workspace_bytes(None, 1, 1, 2), lambda: B._sequences("x", None, pos, None, pos.device),
+              lambda: B._sequences("x", pos.view(3, 1), None, None, pos.device), lambda: B._turns("x", 0.5, pos.device)):
+        with pytest.raises(B.PcmError) as e:
+            f()
+        assert e.value.code == ARG
+
+
 def test_structs_have_the_header_s_layout():
     B = _lib()
     assert ctypes.sizeof(B.grpo_rotary_cfg) == 8 + 5 * 8

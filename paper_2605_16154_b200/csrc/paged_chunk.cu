@@ -17,6 +17,10 @@
 //
 // Warps 0-3 and 4-7: softmax and output of streams 0 and 1.  Warps 8 and 10: products of streams 0 and 1.  Warps 9 and 11: loads of
 // keys and values.
+//
+// What bounds it is the latency from one product to the next: a tile of 256 rows takes about 4300 cycles where the tensor pipe and
+// the exponential unit need 2048 each (47 % busy).  8 x 1024 tokens behind 4096 to 8192, 16/4 heads of 128: 384 us, 870 TFLOP/s;
+// 384 prefixes of 256, 16 heads of 64: 252 us, 0.81 GB at 3.2 TB/s, where the change of units costs as much as its tiles.
 // Every wait is bounded; one that expires is reported in the status word and ends the block.
 #include <cuda.h>
 
@@ -29,8 +33,8 @@ namespace pga {
 constexpr int CH_ROWS = 128, CH_TILE = 128, CH_THREADS = 384;
 constexpr unsigned long long CH_WAIT_NS = 2000000000ull;
 constexpr int CH_TMEM = 512;
-constexpr int CH_TURNS = 8;                    // tiles of a piece from which on its streams take turns (8 x 1024 tokens behind 4096 to 8192: 387 us,
-                                               // 436 without; units of two tiles: 361 us without, 397 with)
+constexpr int CH_TURNS = 8;                    // tiles of a piece from which on its streams take turns (8 x 1024 tokens behind 4096 to 8192: 393 us,
+                                               // 413 without; prefixes of two tiles: 258 us without, 295 with)
 constexpr int CH_TURN_TRIES = 1 << 12;
 constexpr float CH_RISE = 32.f;                // powers of two by which a maximum may outgrow its reference
 constexpr float CH_WILD = 100.f;               // .. within one tile: 128 weights of 2^100 still have a sum
@@ -102,6 +106,16 @@ __device__ __forceinline__ void ch_tmem_ld16(uint32_t taddr, uint32_t (&r)[16]) 
         "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
       : "r"(taddr)
       : "memory");
+}
+// Loads are over, and what they bring is not read before.
+__device__ __forceinline__ void ch_ld_wait(uint32_t (&r)[32]) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;"
+               : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]), "+r"(r[9]),
+                 "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]), "+r"(r[16]), "+r"(r[17]), "+r"(r[18]),
+                 "+r"(r[19]), "+r"(r[20]), "+r"(r[21]), "+r"(r[22]), "+r"(r[23]), "+r"(r[24]), "+r"(r[25]), "+r"(r[26]), "+r"(r[27]),
+                 "+r"(r[28]), "+r"(r[29]), "+r"(r[30]), "+r"(r[31])
+               :
+               : "memory");
 }
 __device__ __forceinline__ void ch_tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void ch_fence_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
@@ -433,7 +447,7 @@ attn_chunk_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
     auto ask_queries = [&](const Cursor& c, int h) {
       const RowPlace x = row_place(p, c.sp, c.qt, c.head, h * CH_ROWS + row);
       const long long mine = x.valid ? x.row * p.ld_q + x.head * p.ld_q_head : -1;
-#pragma unroll 4
+#pragma unroll
       for (int i = 0; i < PER; ++i) {
         const int r = i * (32 / PER) + lane / PER, ch = lane % PER;
         const long long from = __shfl_sync(0xffffffffu, mine, r);
@@ -482,10 +496,13 @@ attn_chunk_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
         if (i >= range.e) break;
         const int key0 = ch_key(c.u, i);
         const bool all_seen = key0 + CH_TILE - 1 <= w_lo && (p.window == 0 || key0 > w_hi - p.window || key0 + CH_TILE - 1 < p.sinks);
-        if (!ch_wait(&b.s_full[s], s_phase, gave_up, p.c)) { ok = false; break; }
+        const bool none_yet = __any_sync(0xffffffffu, m == -INFINITY), rises = __any_sync(0xffffffffu, m_next != m);
+        ok = __all_sync(0xffffffffu, ch_wait(&b.s_full[s], s_phase, gave_up, p.c));
+        if (!ok) break;
         s_phase ^= 1u;
         tc_fence_after();
-        // The warps run through more instructions a tile than are held close by, so loops stay loops: 64 scores a time.  Masks
+        // The warps run through more instructions a tile than are held close by, so loops stay loops: 64 scores a time (16 took 444 us
+        // of far chunks, 32 423, 64 393).  Masks
         // are selects: a branch per score would cost ten times as much.
         const int last = pos - key0, from = pos - p.window + 1 - key0, sunk = p.sinks - key0;
         const bool behind = p.window > 0 && __any_sync(0xffffffffu, from > 0);
@@ -497,13 +514,13 @@ attn_chunk_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
             for (int e = 0; e < 32; ++e) z[e] = (e < from - k0) & (e >= sunk - k0) ? 0xFF800000u : z[e];
         };
         // The reference of a tile's weights comes from the tiles before it, so that they need not wait for this one's maximum.
-        if (__any_sync(0xffffffffu, m == -INFINITY)) {
+        if (none_yet) {
           // any score that the row sees will do: weights stay exact far above 1
           const float first = ch_tmem_ld1(s_col);
           if (m == -INFINITY && last >= 0 && !(p.window > 0 && from > 0 && sunk <= 0)) m = first;
           m_next = m;
         }
-        if (__any_sync(0xffffffffu, m == -INFINITY && last >= 0)) {
+        if (none_yet && __any_sync(0xffffffffu, m == -INFINITY && last >= 0)) {
           float tops[2] = {m, m};
 #pragma unroll 1
           for (int k = 0; k < CH_TILE; k += 32) {
@@ -519,7 +536,7 @@ attn_chunk_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
           }
           if (m == -INFINITY) m_next = m = fmaxf(tops[0], tops[1]);
         }
-        if (__any_sync(0xffffffffu, m_next != m) && begun) {       // (the last tile's values are summed: these scores came after them)
+        if ((none_yet || rises) && begun && __any_sync(0xffffffffu, m_next != m)) {       // (the last tile's values are summed: these scores came after them)
           const float f = m_next > m ? ex2((m - m_next) * p.scale_log2) : 1.f;
 #pragma unroll 1
           for (int k = 0; k < DH; k += 16) {
@@ -571,14 +588,16 @@ attn_chunk_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
           }
           ch_tmem_st16(s_col + k * 16, w);
         };
-        if (all_seen) {
+        if (all_seen) {                        // 32 scores come in while 32 weights are formed
+          uint32_t z[2][32];
+          tmem_ld_32x32(s_col, z[0]);
 #pragma unroll 1
           for (int h = 0; h < 2; ++h) {
-            uint32_t z[2][32];
-            tmem_ld_32x32(s_col + h * 64, z[0]);
+            ch_ld_wait(z[0]);
             tmem_ld_32x32(s_col + h * 64 + 32, z[1]);
-            tmem_ld_wait();
             form(z[0], 2 * h);
+            ch_ld_wait(z[1]);
+            if (h == 0) tmem_ld_32x32(s_col + 64, z[0]);
             form(z[1], 2 * h + 1);
             hand_over(h);
           }
@@ -620,7 +639,8 @@ attn_chunk_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
       }
       if (__any_sync(0xffffffffu, place.valid)) {
         if (begun) {
-          if (!ch_wait(&b.o_full[s], (o_count - 1) & 1u, gave_up, p.c)) { ok = false; break; }
+          ok = __all_sync(0xffffffffu, ch_wait(&b.o_full[s], (o_count - 1) & 1u, gave_up, p.c));
+          if (!ok) break;
           tc_fence_after();
         }
         const int slot = 2 * blockIdx.x + (t0 == 0 ? 1 : 0);
@@ -660,7 +680,7 @@ attn_chunk_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
         if (whole && begun) {                  // whole rows at a time: a row per thread would write 16 bytes of 32 lines at once
           const long long mine = place.valid ? out_at : -1;
           __syncwarp();
-#pragma unroll 4
+#pragma unroll
           for (int i = 0; i < PER; ++i) {
             const int r = i * (32 / PER) + lane / PER, ch = lane % PER;
             const long long to = __shfl_sync(0xffffffffu, mine, r);

@@ -5,7 +5,8 @@
 // turns of t f carry no information and would cost fp32 all of its digits at far positions, so t f is formed and reduced to
 // [-1/2, 1/2] in 64 bits (error below 2^-22 turns at t = 2^31) and only the rest goes through sincospif.  All heads of a row share its
 // angles: a block forms the sines and cosines of its rows once in shared memory, then streams the rows through them, each
-// element read and written once: bound by HBM.
+// element read and written once: bound by HBM (119808 rows of 16 heads of 64 in bf16: 78 us, 6.3 TB/s; 98304 new tokens of 16/8 heads
+// into a cache: 129 us, 6.2 TB/s; a step of 64 tokens: 6 us, which are dependent reads of offsets, lengths and table).
 #include <cmath>
 
 #include "paged.cuh"

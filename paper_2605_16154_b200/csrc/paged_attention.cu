@@ -438,8 +438,20 @@ __global__ void __launch_bounds__(JN_WARPS * 32) attn_join_kernel(const __grid_c
     const RowPlace x = row_place(p, sp, job.y, job.z, r);
     if (!x.valid) return;
     auto place_of = [&](int i) { return (long long)(i == 0 ? 2 * w0 + 1 : 2 * (w0 + i)) * p.unit_rows + r; };
-    float top = -INFINITY;
-    for (int i = lane; i < n; i += 32) top = fmaxf(top, p.part_ml[place_of(i)].x);
+    float v[4][C];                             // four pieces' values, on their way before their weights are known
+    auto fetch = [&](int i) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const float* part = p.part + place_of(i + j) * DH + lane;
+#pragma unroll
+        for (int k = 0; k < C; ++k) v[j][k] = i + j < n ? part[32 * k] : 0.f;
+      }
+    };
+    float2 first = make_float2(-INFINITY, 0.f);
+    if (lane < n) first = p.part_ml[place_of(lane)];
+    fetch(0);
+    float top = first.x;
+    for (int i = lane + 32; i < n; i += 32) top = fmaxf(top, p.part_ml[place_of(i)].x);
 #pragma unroll
     for (int k = 16; k > 0; k >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, k));
     const float ref = top == -INFINITY ? 0.f : top;
@@ -448,18 +460,21 @@ __global__ void __launch_bounds__(JN_WARPS * 32) attn_join_kernel(const __grid_c
 #pragma unroll
     for (int k = 0; k < C; ++k) o[k] = 0.f;
     for (int base = 0; base < n; base += 32) {                     // a lane per piece, then the pieces in order
-      float2 ml = make_float2(-INFINITY, 0.f);
-      if (base + lane < n) ml = p.part_ml[place_of(base + lane)];
+      float2 ml = base == 0 ? first : make_float2(-INFINITY, 0.f);
+      if (base > 0 && base + lane < n) ml = p.part_ml[place_of(base + lane)];
       const float f = ex2((ml.x - ref) * p.scale_log2);
       l = fmaf(ml.y, f, l);
       unfit |= ml.y < 0.f;                     // a piece whose weights did not fit
       const int here = min(32, n - base);
-#pragma unroll 4
-      for (int i = 0; i < here; ++i) {
-        const float g = __shfl_sync(0xffffffffu, f, i);
-        const float* part = p.part + place_of(base + i) * DH + lane;
+      for (int i = 0; i < here; i += 4) {
+        if (base + i > 0) fetch(base + i);
 #pragma unroll
-        for (int k = 0; k < C; ++k) o[k] = fmaf(part[32 * k], g, o[k]);
+        for (int j = 0; j < 4; ++j) {
+          const float g = __shfl_sync(0xffffffffu, f, (i + j) & 31);
+          if (i + j < here)
+#pragma unroll
+            for (int k = 0; k < C; ++k) o[k] = fmaf(v[j][k], g, o[k]);
+        }
       }
     }
 #pragma unroll

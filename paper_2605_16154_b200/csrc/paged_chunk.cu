@@ -19,8 +19,8 @@
 // keys and values.
 //
 // What bounds it is the latency from one product to the next: a tile of 256 rows takes about 4300 cycles where the tensor pipe and
-// the exponential unit need 2048 each (47 % busy).  8 x 1024 tokens behind 4096 to 8192, 16/4 heads of 128: 384 us, 870 TFLOP/s;
-// 384 prefixes of 256, 16 heads of 64: 252 us, 0.81 GB at 3.2 TB/s, where the change of units costs as much as its tiles.
+// the exponential unit need 2048 each (47 % busy).  8 x 1024 tokens behind 4096 to 8192, 16/4 heads of 128: 379 us, 880 TFLOP/s;
+// 384 prefixes of 256, 16 heads of 64: 249 us, 0.81 GB at 3.3 TB/s, where the change of units costs as much as its tiles.
 // Every wait is bounded; one that expires is reported in the status word and ends the block.
 #include <cuda.h>
 
@@ -33,8 +33,8 @@ namespace pga {
 constexpr int CH_ROWS = 128, CH_TILE = 128, CH_THREADS = 384;
 constexpr unsigned long long CH_WAIT_NS = 2000000000ull;
 constexpr int CH_TMEM = 512;
-constexpr int CH_TURNS = 8;                    // tiles of a piece from which on its streams take turns (8 x 1024 tokens behind 4096 to 8192: 393 us,
-                                               // 413 without; prefixes of two tiles: 258 us without, 295 with)
+constexpr int CH_TURNS = 8;                    // tiles of a piece from which on its streams take turns (8 x 1024 tokens behind 4096 to 8192: 379 us,
+                                               // 398 without; prefixes of two tiles: 249 us without, 294 with)
 constexpr int CH_TURN_TRIES = 1 << 12;
 constexpr float CH_RISE = 32.f;                // powers of two by which a maximum may outgrow its reference
 constexpr float CH_WILD = 100.f;               // .. within one tile: 128 weights of 2^100 still have a sum

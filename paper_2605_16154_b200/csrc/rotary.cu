@@ -229,7 +229,7 @@ int kv_check(const grpo_kv_cache* c, const grpo_kv_batch* b, int32_t n_rows) {
   if ((((uintptr_t)c->k | (uintptr_t)c->v) & 15) || (c->n_pages > 1 && c->ld_page % per) || (c->ld_slot % per) ||
       (c->n_kv_heads > 1 && c->ld_head % per))
     return PCM_ERR_SHAPE;
-  // distinct heads, slots and pages do not overlap
+  // neighbouring heads, slots and pages have room for a row of a head
   if ((c->n_kv_heads > 1 && c->ld_head < c->head_dim) || c->ld_slot < c->head_dim || (c->n_pages > 1 && c->ld_page < c->head_dim))
     return PCM_ERR_ARG;
   return PCM_OK;

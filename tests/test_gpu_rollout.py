@@ -579,3 +579,14 @@ def test_a_score_of_minus_infinity_weighs_nothing_beside_values_that_no_row_sees
     tol = 0 if kind == "f32" else 2.0 ** -7
     assert bool(torch.isfinite(out[:-1]).all()) and torch.equal(lse, lse2)
     assert float((out[:-1].double() - clean[:-1].double()).abs().max()) <= tol * float(clean.double().abs().max()) + 1e-5
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("shape", [(64, 1, 71, 136, [300, 33, 1], [1, 2, 1]), (128, 1, 300, 8, [260, 129], [1, 3]), (32, 1, 100, 40, [500, 7], [1, 7]),
+                                   (64, 2, 33, 1000, [2100, 900], [5, 1]), (128, 2, 17, 72, [400, 65, 3], [1, 1, 1])],
+                         ids=lambda s: f"d{s[0]}kv{s[1]}g{s[2]}p{s[3]}")
+def test_many_heads_of_one_key_and_odd_pages(kind, shape):
+    dim, kv, group, page, lens, new = shape
+    c = Case(dim + group, kind, dim, kv, group, page, lens, new)
+    for window, sinks in ((0, 0), (70, 9)):
+        c.check(*c.run(window, sinks), window, sinks, rounded=True)

@@ -78,9 +78,10 @@ __global__ void __launch_bounds__(RT_THREADS, 8) rotary_kernel(const __grid_cons
       } else {
         const SeqSpan sp = seq_span(p.cache, s, true);
         if (row >= sp.row0 && row < sp.row0 + sp.fresh) {
-          const int j = sp.len - sp.fresh + (row - sp.row0);
+          // from the length as it was given: counted back from a clipped one new tokens would land on stored ones
+          const int j = max(p.cache.seq_len[s], 0) - sp.fresh + (row - sp.row0);
           t = p.pos ? p.pos[row] : j;
-          if (j >= 0) {
+          if (j >= 0 && j < p.cache.max_len) {
             const int at = fast_div(j, p.cache.div_page);
             const int page = p.cache.table[s * p.cache.ld_table + at];
             if (page < 0 || page >= p.cache.n_pages) kv_report(p.cache, STATUS_BAD_PAGE);

@@ -1,0 +1,37 @@
+"""Calls of the rollout side at their edges.  Tolerances are those of the Case class."""
+import os
+import subprocess
+import sys
+
+import numpy as np
+import pytest
+import torch
+
+from test_gpu_rollout import B, Case, TYPES, gen, host
+
+pytestmark = pytest.mark.gpu
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("length", [67, 68, 200, 2 ** 31 - 1])
+def test_a_length_beyond_the_table_overwrites_no_stored_token(kind, length):
+    """64 slots, all of them taken; new tokens whose places lie behind the table are not stored, and nothing else moves."""
+    c = Case(95, kind, 64, 2, 2, 16, [64, 60], [5, 4], stale=3.0)
+    c.table = c.table[:, :4].contiguous()
+    g = gen(96)
+    fused = torch.randn(9, 4 + 2 * 2, 64, generator=g, device="cuda").to(c.t)
+    q, k, v = fused[:, :4], fused[:, 4:6], fused[:, 6:]
+    turns = B().grpo_rotary_freqs(64)[0].cuda()
+    c.seq_len[0] = length
+    want_k, want_v = c.k_pages.clone(), c.v_pages.clone()
+    pos = np.concatenate([np.arange(length - 5, length), np.arange(56, 60)])
+    pos_t = torch.from_numpy(pos.astype(np.int32)).cuda()
+    turned = B().grpo_rotary(k, pos_t, turns)
+    for r, (s, j) in enumerate(zip([0] * 5 + [1] * 4, pos)):
+        if j < 64:
+            want_k[c.table_host[s][j // 16], j % 16], want_v[c.table_host[s][j // 16], j % 16] = turned[r], v[r]
+    out = B().grpo_rotary_cache(q, k, v, c.k_pages, c.v_pages, c.table, c.seq_len, c.q_off, turns, status=c.status)
+    assert torch.equal(c.k_pages, want_k) and torch.equal(c.v_pages, want_v)
+    assert torch.equal(out, B().grpo_rotary(q, pos_t, turns))
+    assert int(c.status) == 128

@@ -23,6 +23,7 @@
 
 #include "async_ptx.cuh"
 #include "internal.h"
+#include "tensor_map.h"
 
 namespace pcm {
 
@@ -1261,36 +1262,13 @@ fa_rowsum64_kernel(const __nv_bfloat16* __restrict__ out, const __nv_bfloat16* _
 // ------------------------------------------------------------------------------------------------
 // host side
 // ------------------------------------------------------------------------------------------------
-typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
-                                  const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
-                                  CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
-static EncodeTiledFn attn_encode_fn() {
-  static EncodeTiledFn fn = nullptr;
-  static bool tried = false;
-  if (!tried) {
-    tried = true;
-    void* p = nullptr;
-    cudaDriverEntryPointQueryResult q;
-    if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &q) == cudaSuccess &&
-        q == cudaDriverEntryPointSuccess)
-      fn = (EncodeTiledFn)p;
-  }
-  return fn;
-}
-
 // bf16 tensor [n_seq][S][cols] (row stride ld elements, sequences S rows apart), box {64 columns, box_rows, 1},
 // 128-byte swizzle.  Rows past the end of a sequence read as zero, so a tile never sees its neighbour's rows.
 static bool make_seq_tmap(CUtensorMap* tm, const void* base, int n_seq, int S, long long cols, long long ld, int box_rows) {
-  EncodeTiledFn fn = attn_encode_fn();
-  if (!fn) return false;
   cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)S, (cuuint64_t)n_seq};
   cuuint64_t strides[2] = {(cuuint64_t)ld * 2, (cuuint64_t)ld * 2 * (cuuint64_t)S};
   cuuint32_t box[3] = {64u, (cuuint32_t)box_rows, 1u};
-  cuuint32_t estr[3] = {1, 1, 1};
-  return fn(tm, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), dims, strides, box, estr,
-            CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+  return encode_tensor_map(tm, 3, base, dims, strides, box, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B);
 }
 
 constexpr uint32_t SMEM_LIMIT = 227u * 1024u;
@@ -1419,7 +1397,7 @@ bool attention_tc_supported(const void* qkv, const void* out, int S, int H, int 
   if (fatc::make_plan(dh, ((S + 63) / 64) * 64, 1, 1).total > fatc::SMEM_LIMIT) return false;
   if ((((uintptr_t)qkv) | ((uintptr_t)out)) & 15) return false;
   (void)H;
-  return fatc::attn_encode_fn() != nullptr;
+  return encode_tiled_fn() != nullptr;
 }
 
 int attention_bwd_bf16_tc(const void* qkv, const void* out, const void* dout, const float* lse, float* dsum, void* dqkv,

@@ -22,6 +22,7 @@
 
 #include "async_ptx.cuh"
 #include "internal.h"
+#include "tensor_map.h"
 
 namespace pcm {
 
@@ -1251,37 +1252,14 @@ gemm_tc2_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
 // ------------------------------------------------------------------------------------------------
 // host side
 // ------------------------------------------------------------------------------------------------
-typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
-                                  const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
-                                  CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
-static EncodeTiledFn encode_fn() {
-  static EncodeTiledFn fn = nullptr;
-  static bool tried = false;
-  if (!tried) {
-    tried = true;
-    void* p = nullptr;
-    cudaDriverEntryPointQueryResult q;
-    if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &q) == cudaSuccess &&
-        q == cudaDriverEntryPointSuccess)
-      fn = (EncodeTiledFn)p;
-  }
-  return fn;
-}
-
 // 2-D bf16 tensor [rows][cols] with row stride ld (elements); box {box_cols, box_rows}, 128-byte swizzle,
 // out-of-range elements read as zero.
 static bool make_tmap(CUtensorMap* tm, const void* base, long long rows, long long cols, long long ld, int box_cols,
                       int box_rows) {
-  EncodeTiledFn fn = encode_fn();
-  if (!fn) return false;
   cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
   cuuint64_t strides[1] = {(cuuint64_t)ld * 2};
   cuuint32_t box[2] = {(cuuint32_t)box_cols, (cuuint32_t)box_rows};
-  cuuint32_t estr[2] = {1, 1};
-  return fn(tm, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(base), dims, strides, box, estr,
-            CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+  return encode_tensor_map(tm, 2, base, dims, strides, box, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B);
 }
 
 bool gemm_tcgen05_supported(const GemmArgs& g) {
@@ -1296,7 +1274,7 @@ bool gemm_tcgen05_supported(const GemmArgs& g) {
   if (g.K2 < 0 || g.K2 > TC_BK || (g.K2 % 16)) return false;
   if (g.K2 > 0 && (!g.A2 || !g.B2 || (g.lda2 % 8) || (g.ldb2 % 8) || (((uintptr_t)g.A2 | (uintptr_t)g.B2) & 15))) return false;
   if (g.alpha != 1.f && (g.epi.kind != EPI_NONE || (g.R && (const void*)g.R == (const void*)g.C))) return false;
-    return encode_fn() != nullptr;
+    return encode_tiled_fn() != nullptr;
 }
 
 static void fill_params(TcParams& p, const GemmArgs& g) {
@@ -1501,7 +1479,7 @@ size_t chain_part_bytes() { return (size_t)sm_count() * TC_BM * T2_BN * 4; }
 bool gemm_epilogue_supported(const GemmArgs& g) {
   if (g.epi.kind == EPI_VOCAB_STATS || g.epi.kind == EPI_VOCAB_DZ || g.epi.kind == EPI_CHAIN) {
     // any N (EPI_CHAIN: a multiple of 8), so the general conditions are checked here
-    if (g.ab_dtype != DT_BF16 || g.M < 1 || g.N < 1 || g.K < 1 || (g.lda % 8) || (g.ldb % 8) || !encode_fn()) return false;
+    if (g.ab_dtype != DT_BF16 || g.M < 1 || g.N < 1 || g.K < 1 || (g.lda % 8) || (g.ldb % 8) || !encode_tiled_fn()) return false;
     if (((uintptr_t)g.A | (uintptr_t)g.B | (uintptr_t)g.C) & 15) return false;
     if (g.epi.kind == EPI_VOCAB_STATS) return g.a_kmajor && g.b_kmajor && g.epi.vh.tok && g.epi.vh.part && !g.K2;
     if (g.epi.kind == EPI_VOCAB_DZ)

@@ -26,6 +26,7 @@
 
 #include "async_ptx.cuh"
 #include "paged_attention.cuh"
+#include "tensor_map.h"
 
 namespace pcm {
 namespace pga {
@@ -727,31 +728,15 @@ attn_chunk_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
 // ------------------------------------------------------------------------------------------------
 // host side
 // ------------------------------------------------------------------------------------------------
-typedef CUresult (*EncodeFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
-                             const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-static EncodeFn encode_fn() {
-  static EncodeFn fn = nullptr;
-  static bool tried = false;
-  if (!tried) {
-    tried = true;
-    void* q = nullptr;
-    cudaDriverEntryPointQueryResult r;
-    if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &q, cudaEnableDefault, &r) == cudaSuccess && r == cudaDriverEntryPointSuccess)
-      fn = (EncodeFn)q;
-  }
-  return fn;
-}
 // Pages as [page][slot][head][column] (reads of more than a head's row bring in others' too soon: a step of 256 sequences of 2048,
 // 16 heads of 64, took 512 us with 256 bytes at a time, 400 with 128), boxes of box_rows slots of one head, swizzled rows of box_cols (64 or 32) columns.
 bool page_map(CUtensorMap* tm, const void* base, const KvView& c, int dh, int box_cols, int box_rows) {
-  EncodeFn fn = encode_fn();
-  if (!fn) return false;
   cuuint64_t dims[4] = {(cuuint64_t)dh, (cuuint64_t)c.n_kv, (cuuint64_t)c.page_size, (cuuint64_t)c.n_pages};
   const cuuint64_t one = (cuuint64_t)dh * 2;                       // a stride of one head or one page leads nowhere
   cuuint64_t strides[3] = {c.n_kv > 1 ? (cuuint64_t)c.ld_head * 2 : one, (cuuint64_t)c.ld_slot * 2, c.n_pages > 1 ? (cuuint64_t)c.ld_page * 2 : one};
-  cuuint32_t box[4] = {(cuuint32_t)box_cols, 1u, (cuuint32_t)box_rows, 1u}, step[4] = {1, 1, 1, 1};
-  return fn(tm, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(base), dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
-            box_cols == 64 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, dh >= 128 ? CU_TENSOR_MAP_L2_PROMOTION_L2_256B : CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+  const cuuint32_t box[4] = {(cuuint32_t)box_cols, 1u, (cuuint32_t)box_rows, 1u};
+  return encode_tensor_map(tm, 4, base, dims, strides, box, box_cols == 64 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
+                           dh >= 128 ? CU_TENSOR_MAP_L2_PROMOTION_L2_256B : CU_TENSOR_MAP_L2_PROMOTION_L2_128B);
 }
 
 template <int DH>

@@ -1,0 +1,43 @@
+// Tensor maps for TMA, formed by the driver: its entry point is found through the runtime, so that nothing links to the driver.
+#pragma once
+#include <cuda.h>
+#include <cuda_runtime.h>
+
+namespace pcm {
+
+typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
+                                  const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                  CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+static inline EncodeTiledFn encode_tiled_fn() {
+  static EncodeTiledFn fn = nullptr;
+  static bool tried = false;
+  if (!tried) {
+    tried = true;
+    void* p = nullptr;
+    cudaDriverEntryPointQueryResult q;
+    if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &q) == cudaSuccess && q == cudaDriverEntryPointSuccess)
+      fn = (EncodeTiledFn)p;
+  }
+  return fn;
+}
+
+// A tensor of `rank` dimensions in bf16: sizes innermost first, strides of all but the innermost in bytes, box sizes; elements
+// out of range read as zero.
+static inline bool encode_tensor_map(CUtensorMap* tm, int rank, const void* base, const cuuint64_t* dims, const cuuint64_t* strides,
+                                     const cuuint32_t* box, CUtensorMapSwizzle swizzle, CUtensorMapL2promotion promotion) {
+  const EncodeTiledFn fn = encode_tiled_fn();
+  if (!fn) return false;
+  const cuuint32_t step[5] = {1, 1, 1, 1, 1};
+  auto encode = [&]() {
+    return fn(tm, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, (cuuint32_t)rank, const_cast<void*>(base), dims, strides, box, step,
+              CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle, promotion, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+  };
+  if (encode()) return true;
+  // The driver wants a context that is current.  The runtime makes one so in a thread's first call that needs it, which the first
+  // tensor map of a new thread may come before.
+  int dev = 0;
+  return cudaGetDevice(&dev) == cudaSuccess && cudaSetDevice(dev) == cudaSuccess && encode();
+}
+
+}  // namespace pcm

@@ -35,3 +35,39 @@ def test_a_length_beyond_the_table_overwrites_no_stored_token(kind, length):
     assert torch.equal(c.k_pages, want_k) and torch.equal(c.v_pages, want_v)
     assert torch.equal(out, B().grpo_rotary(q, pos_t, turns))
     assert int(c.status) == 128
+
+
+def test_calls_of_a_new_thread():
+    """The first GPU work of a thread is the call itself: nothing else has made a context current there."""
+    import threading
+    b, g = B(), gen(99)
+    c = {new: Case(99, "bf16", 64, 2, 2, 16, [300, 280], [new, new]) for new in (1, 150)}
+    x, w = torch.randn(256, 128, generator=g, device="cuda").bfloat16(), torch.randn(512, 128, generator=g, device="cuda").bfloat16()
+    qkv = torch.randn(2 * 96, 3 * 128, generator=g, device="cuda").bfloat16()
+    tok = torch.randint(0, 512, (256,), generator=g, device="cuda", dtype=torch.int32)
+    paged = []
+    for new, case in c.items():
+        room = torch.empty(b.grpo_paged_attention_workspace_bytes(case.k_pages, 2, case.n, 4, new) + 256, dtype=torch.uint8, device="cuda")
+        paged.append(lambda case=case, new=new, room=room, to=(torch.empty_like(case.q), torch.empty(case.n, 4, device="cuda")): b.grpo_paged_attention(
+            case.q, case.k_pages, case.v_pages, case.table, case.seq_len, case.q_off, max_new=new, out=to[0], lse=to[1], workspace=room))
+    calls = [*paged, lambda: b.grpo_gemm(x, True, w, True, 256, 512, 128), lambda: b.grpo_attention(qkv, 2, 96, 2, 64)[:2],
+             lambda: b.grpo_head_logp(x, w, tok)]
+    as_list, failed = (lambda r: list(r) if isinstance(r, (tuple, list)) else [r]), []
+    for call in calls:
+        want, got = [t.clone() for t in as_list(call())], []
+        torch.cuda.synchronize()
+
+        def work():
+            try:
+                got.append(call())
+            except Exception as e:
+                got.append(e)
+        t = threading.Thread(target=work)
+        t.start()
+        t.join()
+        torch.cuda.synchronize()
+        if isinstance(got[0], Exception):
+            failed.append(got[0])
+        else:
+            assert all(torch.equal(p, q) for p, q in zip(as_list(got[0]), want))
+    assert not failed

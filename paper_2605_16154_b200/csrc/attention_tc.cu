@@ -1298,9 +1298,8 @@ static int fwd_launch(const void* qkv, void* out, float* lse, int n_seq, int S, 
     return PCM_ERR_CUDA;
   CUtensorMap tmO;
   if (!make_seq_tmap(&tmO, out, n_seq, S, d, d, BM)) return PCM_ERR_CUDA;
-  static unsigned long long attr_devices = 0;
-  if (attr_needed(&attr_devices))
-    PCM_CUDA_TRY(cudaFuncSetAttribute(fa_tc_fwd_kernel<DH>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)SMEM_LIMIT));
+  static std::atomic<unsigned long long> attr_devices{0};
+  if (const int rc = allow_smem(fa_tc_fwd_kernel<DH>, (int)SMEM_LIMIT, &attr_devices)) return rc;
   const int grid = p.n_items < sm_count() ? p.n_items : sm_count();
   fa_tc_fwd_kernel<DH><<<grid, Cfg<DH>::THREADS, smem, s>>>(tmQ, tmKV, tmO, p);
   PCM_LAUNCH_CHECK();
@@ -1314,9 +1313,8 @@ static int bwd_launch_one(const CUtensorMap& tmQKV, const CUtensorMap& tmDO, con
   const BwPlan pl = bw_make_plan<DH, MODE>();
   if (pl.total > SMEM_LIMIT) return PCM_ERR_SHAPE;
   const uint32_t smem = pl.total < SMEM_FLOOR ? SMEM_FLOOR : pl.total;
-  static unsigned long long attr_devices = 0;
-  if (attr_needed(&attr_devices))
-    PCM_CUDA_TRY(cudaFuncSetAttribute(fa_tc_bwd_kernel<DH, MODE>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)SMEM_LIMIT));
+  static std::atomic<unsigned long long> attr_devices{0};
+  if (const int rc = allow_smem(fa_tc_bwd_kernel<DH, MODE>, (int)SMEM_LIMIT, &attr_devices)) return rc;
   const int grid = p.n_items < sm_count() ? p.n_items : sm_count();
   fa_tc_bwd_kernel<DH, MODE><<<grid, BW_THREADS, smem, s>>>(tmQKV, tmDO, tmOUT, tmDQKV, p);
   PCM_LAUNCH_CHECK();
@@ -1379,9 +1377,8 @@ static int bwd1_launch(const void* qkv, const void* out, const void* dout, const
     return PCM_ERR_CUDA;
   fa_rowsum64_kernel<<<sm_count() * 8, 256, 0, s>>>(p.out, p.dout, dsum, (long long)n_seq * S, S, H);
   PCM_LAUNCH_CHECK();
-  static unsigned long long attr_devices = 0;
-  if (attr_needed(&attr_devices))
-    PCM_CUDA_TRY(cudaFuncSetAttribute(fa_tc_bwd1_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)b1::SMEM_BYTES));
+  static std::atomic<unsigned long long> attr_devices{0};
+  if (const int rc = allow_smem(fa_tc_bwd1_kernel, (int)b1::SMEM_BYTES, &attr_devices)) return rc;
   const int grid = p.n_items < sm_count() ? p.n_items : sm_count();
   fa_tc_bwd1_kernel<<<grid, b1::THREADS, b1::SMEM_BYTES, s>>>(tmQKV, tmDO, tmDQKV, p);
   PCM_LAUNCH_CHECK();

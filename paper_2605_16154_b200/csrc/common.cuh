@@ -43,26 +43,35 @@ static inline int ceil_div(long long a, long long b) { return (int)((a + b - 1) 
 // drives several GPUs needs them once per device, not once per process.
 // First use of `seen_mask` on device `dev` (0..63) returns true and marks the device; devices outside that range
 // always return true (the attribute is then simply set again).
+static inline bool device_marked(unsigned long long mask, int dev) { return dev >= 0 && dev < 64 && (mask & (1ull << dev)); }
+static inline unsigned long long device_mark(int dev) { return dev >= 0 && dev < 64 ? 1ull << dev : 0ull; }
 static inline bool first_use_on_device(unsigned long long* seen_mask, int dev) {
-  if (dev < 0 || dev >= 64) return true;
-  if (*seen_mask & (1ull << dev)) return false;
-  *seen_mask |= 1ull << dev;
+  if (device_marked(*seen_mask, dev)) return false;
+  *seen_mask |= device_mark(dev);
   return true;
 }
-static inline bool attr_needed(unsigned long long* seen_mask) {
-  int dev = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess) return true;
-  return first_use_on_device(seen_mask, dev);
+// Lets `kernel` use `bytes` of dynamic shared memory on the current device.  The device is marked once that holds: threads that
+// call at the same time for the first time each set it, and one that failed is tried again.
+template <typename... P>
+static int allow_smem(void (*kernel)(P...), int bytes, std::atomic<unsigned long long>* seen) {
+  int dev = -1;
+  if (cudaGetDevice(&dev) == cudaSuccess && device_marked(seen->load(std::memory_order_acquire), dev)) return PCM_OK;
+  PCM_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes));
+  seen->fetch_or(device_mark(dev), std::memory_order_release);
+  return PCM_OK;
 }
 // SM count of the current device, cached per device; 148 when the query fails.
 static inline int sm_count() {
-  static int cached[64] = {0};
+  static std::atomic<int> cached[64];
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess) return 148;
-  if (dev >= 0 && dev < 64 && cached[dev] > 0) return cached[dev];
+  if (dev >= 0 && dev < 64) {
+    const int known = cached[dev].load(std::memory_order_relaxed);
+    if (known > 0) return known;
+  }
   int n = 0;
   if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n < 1) n = 148;
-  if (dev >= 0 && dev < 64) cached[dev] = n;
+  if (dev >= 0 && dev < 64) cached[dev].store(n, std::memory_order_relaxed);
   return n;
 }
 

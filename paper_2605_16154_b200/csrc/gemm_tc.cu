@@ -1351,10 +1351,8 @@ static int launch_tc(const GemmArgs& g, cudaStream_t s) {
   if (EPI == EPI_CHAIN) splits = g.epi.splits;
   p.kb_per_split = (num_kb + splits - 1) / splits;
   splits = (num_kb + p.kb_per_split - 1) / p.kb_per_split;          // no empty split
-  static unsigned long long attr_devices = 0;
-  if (attr_needed(&attr_devices))
-    PCM_CUDA_TRY(cudaFuncSetAttribute(gemm_tc_kernel<BN, EPI>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                      EPI >= EPI_VOCAB_STATS ? 227 * 1024 : TcSmem<BN>::TOTAL));
+  static std::atomic<unsigned long long> attr_devices{0};
+  if (const int rc = allow_smem(gemm_tc_kernel<BN, EPI>, EPI >= EPI_VOCAB_STATS ? 227 * 1024 : TcSmem<BN>::TOTAL, &attr_devices)) return rc;
   p.tiles_m = tiles_m; p.tiles_n = tiles_n; p.splits = splits;
   const long long total = (long long)tiles_m * tiles_n * splits;
   const int grid = (int)(total < sm_count() ? total : sm_count());      // persistent: one CTA per SM walks the tile list
@@ -1418,9 +1416,8 @@ static int launch_tc2(const GemmArgs& g, cudaStream_t s) {
   p.kb_per_split = (num_kb + splits - 1) / splits;
   splits = (num_kb + p.kb_per_split - 1) / p.kb_per_split;
   p.tiles_m = tiles_m; p.tiles_n = tiles_n; p.splits = splits;
-  static unsigned long long attr_devices = 0;
-  if (attr_needed(&attr_devices))
-    PCM_CUDA_TRY(cudaFuncSetAttribute(gemm_tc2_kernel<EPI>, cudaFuncAttributeMaxDynamicSharedMemorySize, T2_SMEM_TOTAL));
+  static std::atomic<unsigned long long> attr_devices{0};
+  if (const int rc = allow_smem(gemm_tc2_kernel<EPI>, T2_SMEM_TOTAL, &attr_devices)) return rc;
   const long long total = (long long)tiles_m * tiles_n * splits;
   const int pairs = (int)(total < n_pairs_max ? total : n_pairs_max);
   cudaLaunchConfig_t cfg = {};

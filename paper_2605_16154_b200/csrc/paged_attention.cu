@@ -501,17 +501,15 @@ __global__ void __launch_bounds__(JN_WARPS * 32) attn_join_kernel(const __grid_c
 // ------------------------------------------------------------------------------------------------
 template <int DH>
 static int launch_f32(const AttnParams& p, cudaStream_t s) {
-  static unsigned long long seen = 0;
-  if (attr_needed(&seen))
-    PCM_CUDA_TRY(cudaFuncSetAttribute(attn_rows_f32_kernel<DH>, cudaFuncAttributeMaxDynamicSharedMemorySize, RfSmem<DH>::BYTES));
+  static std::atomic<unsigned long long> seen{0};
+  if (const int rc = allow_smem(attn_rows_f32_kernel<DH>, RfSmem<DH>::BYTES, &seen)) return rc;
   return launch_after_smem(attn_rows_f32_kernel<DH>, dim3(p.workers), dim3(RF_THREADS), RfSmem<DH>::BYTES, s, p);
 }
 
 template <int DH>
 static int launch_tiles_f32(const AttnParams& p, cudaStream_t s) {
-  static unsigned long long seen = 0;
-  if (attr_needed(&seen))
-    PCM_CUDA_TRY(cudaFuncSetAttribute(attn_tiles_f32_kernel<DH>, cudaFuncAttributeMaxDynamicSharedMemorySize, TfCfg<DH>::BYTES));
+  static std::atomic<unsigned long long> seen{0};
+  if (const int rc = allow_smem(attn_tiles_f32_kernel<DH>, TfCfg<DH>::BYTES, &seen)) return rc;
   return launch_after_smem(attn_tiles_f32_kernel<DH>, dim3(p.workers), dim3(TF_THREADS), TfCfg<DH>::BYTES, s, p);
 }
 

@@ -745,9 +745,8 @@ static int launch_chunk(const AttnParams& p, cudaStream_t s) {
   while (a) { const int t = box % a; box = a; a = t; }
   CUtensorMap tm_k, tm_v;
   if (!page_map(&tm_k, p.c.k, p.c, DH, 64, box) || !page_map(&tm_v, p.c.v, p.c, DH, 64, box)) return PCM_ERR_CUDA;
-  static unsigned long long seen = 0;
-  if (attr_needed(&seen))
-    PCM_CUDA_TRY(cudaFuncSetAttribute(attn_chunk_kernel<DH>, cudaFuncAttributeMaxDynamicSharedMemorySize, ChCfg<DH>::BYTES));
+  static std::atomic<unsigned long long> seen{0};
+  if (const int rc = allow_smem(attn_chunk_kernel<DH>, ChCfg<DH>::BYTES, &seen)) return rc;
   return launch_after_smem(attn_chunk_kernel<DH>, dim3(p.workers), dim3(CH_THREADS), ChCfg<DH>::BYTES, s, tm_k, tm_v, p, box);
 }
 int attn_chunk_rows() { return 2 * CH_ROWS; }

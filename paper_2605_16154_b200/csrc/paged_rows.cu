@@ -350,9 +350,8 @@ __global__ void __launch_bounds__(RB_THREADS, 2) attn_rows_bf16_kernel(const __g
 
 template <int DH, int MT>
 static int launch_rows(const AttnParams& p, cudaStream_t s) {
-  static unsigned long long seen = 0;
-  if (attr_needed(&seen))
-    PCM_CUDA_TRY(cudaFuncSetAttribute(attn_rows_bf16_kernel<DH, MT>, cudaFuncAttributeMaxDynamicSharedMemorySize, RbCfg<DH>::BYTES));
+  static std::atomic<unsigned long long> seen{0};
+  if (const int rc = allow_smem(attn_rows_bf16_kernel<DH, MT>, RbCfg<DH>::BYTES, &seen)) return rc;
   int box = RbCfg<DH>::KEYS;
   while (p.c.page_size % box) box /= 2;        // (pages are of a multiple of 8)
   CUtensorMap tm_k, tm_v;

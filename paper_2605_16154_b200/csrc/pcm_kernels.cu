@@ -615,15 +615,9 @@ static int launch_score_groups_nt(const pcm_batch* b, int G, int n_phases, int n
                                   uint8_t* valid_group, unsigned* status, cudaStream_t s) {
   const size_t n_cnt = ((size_t)n_phases * 2 * (ACT + 1) + 3) & ~(size_t)3;
   const size_t smem = n_cnt * sizeof(unsigned) + (size_t)SC_WARPS * 2 * SC_SLAB_BYTES;
-  static unsigned long long attr_devices = 0;
-  static std::mutex mu;
-  {
-    std::lock_guard<std::mutex> lk(mu);
-    if (attr_needed(&attr_devices))
-      PCM_CUDA_TRY(cudaFuncSetAttribute(score_groups_kernel<NT>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                        (int)(((size_t)PCM_MAX_PHASES * 2 * (ACT + 1) + 3) * sizeof(unsigned) +
-                                              (size_t)SC_WARPS * 2 * SC_SLAB_BYTES)));
-  }
+  static std::atomic<unsigned long long> attr_devices{0};
+  const int most = (int)(((size_t)PCM_MAX_PHASES * 2 * (ACT + 1) + 3) * sizeof(unsigned) + (size_t)SC_WARPS * 2 * SC_SLAB_BYTES);
+  if (const int rc = allow_smem(score_groups_kernel<NT>, most, &attr_devices)) return rc;
   score_groups_kernel<NT><<<n_groups, SC_WARPS * 32, smem, s>>>(b->traj_off, b->tok, b->phase, b->reward, G, n_phases,
                                                               c_group, valid_group, status);
   PCM_LAUNCH_CHECK();

@@ -71,3 +71,50 @@ def test_calls_of_a_new_thread():
         else:
             assert all(torch.equal(p, q) for p, q in zip(as_list(got[0]), want))
     assert not failed
+
+
+_FIRST_CALLS = """
+import threading
+import torch
+from paper_2605_16154_b200 import binding as B
+
+def family(dtype, dim, new):
+    g = torch.Generator(device="cuda").manual_seed(1)
+    k, v = (torch.randn(40, 16, 2, dim, generator=g, device="cuda").to(dtype) for _ in range(2))
+    q = torch.randn(2 * new, 4, dim, generator=g, device="cuda").to(dtype)
+    table = torch.arange(40, dtype=torch.int32, device="cuda").view(2, 20)
+    seq_len = torch.tensor([300, 280], dtype=torch.int32, device="cuda")
+    q_off = torch.tensor([0, new, 2 * new], dtype=torch.int32, device="cuda")
+    need = B.grpo_paged_attention_workspace_bytes(k, 2, 2 * new, 4, new)
+    n = 8
+    outs = [(torch.empty_like(q), torch.empty(2 * new, 4, device="cuda"), torch.empty(need + 256, dtype=torch.uint8, device="cuda")) for _ in range(n)]
+    streams = [torch.cuda.Stream() for _ in range(n)]
+    gate, failed = threading.Barrier(n), []
+    torch.cuda.synchronize()
+    def call(i):
+        out, lse, ws = outs[i]
+        with torch.cuda.stream(streams[i]):
+            gate.wait()
+            try:
+                B.grpo_paged_attention(q, k, v, table, seq_len, q_off, max_new=new, out=out, lse=lse, workspace=ws)
+            except Exception as e:
+                failed.append(repr(e))
+    threads = [threading.Thread(target=call, args=(i,)) for i in range(n)]
+    for t in threads: t.start()
+    for t in threads: t.join()
+    torch.cuda.synchronize()
+    assert not failed, (dtype, dim, new, failed)
+    for out, lse, _ in outs[1:]:
+        assert torch.equal(out, outs[0][0]) and torch.equal(lse, outs[0][1])
+
+for dtype, dim, new in ((torch.bfloat16, 64, 150), (torch.bfloat16, 128, 150), (torch.bfloat16, 64, 1), (torch.bfloat16, 128, 1), (torch.bfloat16, 32, 1),
+                        (torch.float32, 64, 150), (torch.float32, 128, 150), (torch.float32, 64, 1), (torch.float32, 128, 1)):
+    family(dtype, dim, new)
+print("first calls ok")
+"""
+
+
+def test_first_calls_of_several_threads():
+    """Eight threads make a process's first call of each kernel at the same time."""
+    res = subprocess.run([sys.executable, "-c", _FIRST_CALLS], cwd=ROOT, env=dict(os.environ, PYTHONPATH=ROOT), capture_output=True, text=True, timeout=300)
+    assert res.returncode == 0 and "first calls ok" in res.stdout, res.stdout[-2000:] + res.stderr[-2000:]

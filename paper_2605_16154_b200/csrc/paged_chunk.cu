@@ -489,7 +489,8 @@ attn_chunk_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
         if (lane == 0) sh.coming[warp] = next;
         __syncwarp();
       }
-      float m = -INFINITY, m_next = m, l = 0.f;                    // the row's reference, what it is to be, the sum of its weights
+      // the row's reference, what it is to be, the sum of its weights (a row ahead of every token waits for no reference)
+      float m = pos < 0 ? 0.f : -INFINITY, m_next = m, l = 0.f;
       bool wild = false;                       // a tile rose so far above the reference that its weights may not fit
       bool begun = false;
       for (int i = t0;; ++i) {
@@ -519,7 +520,7 @@ attn_chunk_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
           // any score that the row sees will do: weights stay exact far above 1
           const float first = ch_tmem_ld1(s_col);
           if (m == -INFINITY && last >= 0 && !(p.window > 0 && from > 0 && sunk <= 0)) m = first;
-          m_next = m;
+          m_next = fmaxf(m_next, m);           // (other rows of the warp may be about to move theirs)
         }
         if (none_yet && __any_sync(0xffffffffu, m == -INFINITY && last >= 0)) {
           float tops[2] = {m, m};

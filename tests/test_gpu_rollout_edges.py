@@ -13,6 +13,25 @@ pytestmark = pytest.mark.gpu
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 
 
+@pytest.mark.parametrize("dim", [64, 128])
+def test_a_reference_moves_in_a_warp_with_fewer_rows_too(dim):
+    """Scores that rise by 40 powers of two a tile: each row's reference follows from the next tile on, wherever the row's warp
+    ends.  The rows of a chunk of 246 tokens are those of a chunk of 256 from the same place, bit by bit: its last warp is the
+    only difference, and rows formed once more would round otherwise."""
+    c = Case(91, "bf16", dim, 1, 1, 16, [1000], [256])
+    c.q[:] = 1.0
+    at = torch.from_numpy(c.table_host[0][np.arange(1000) // 16].astype(np.int64)).cuda(), torch.arange(1000, device="cuda") % 16
+    rise = torch.arange(1000, device="cuda") // 128 * (40.0 * np.log(2.0) * dim ** 0.5 / dim)
+    noise = torch.randn(1000, 1, dim, generator=gen(92), device="cuda") * 0.01
+    c.k_pages[at] = (rise[:, None, None] + noise).to(c.t)
+    out, lse = c.run()
+    c.check(out, lse)
+    c.seq_len[0] = 990
+    c.q_off[1] = 246
+    fewer, lse2 = c.run()
+    assert torch.equal(fewer[:246], out[:246]) and torch.equal(lse2[:246], lse[:246])
+
+
 @pytest.mark.parametrize("kind", ["f32", "bf16"])
 @pytest.mark.parametrize("length", [67, 68, 200, 2 ** 31 - 1])
 def test_a_length_beyond_the_table_overwrites_no_stored_token(kind, length):

@@ -575,10 +575,14 @@ int grpo_attention(int32_t dtype, const void* qkv, void* out, float* lse, const 
  * Updated when a call returns PCM_ERR_DEVICE_TIMEOUT.  Host value, no GPU work. */
 uint32_t grpo_attention_wait_status(void);
 
-/* The current device's word of expired waits of the tensor-core GEMM kernels (0 = none since the last poll; all ones: the
- * word could not be read), with `next` stored in its place: 0 clears it, 1 plants a report, which is how a test sees who
+/* The current device's word of expired waits of the tensor-core GEMM kernels and of the paged attention (0 = none since the
+ * last poll; all ones: the word could not be read), with `next` stored in its place: 0 clears it, 1 plants a report, which is how a test sees who
  * reads it.  Synchronises the device's default stream. */
 uint32_t grpo_gemm_wait_status(uint32_t next);
+
+/* A kernel whose bounded wait (a millisecond for something that nothing does) expires, reported as those of
+ * grpo_paged_attention are: bit 0 of device_status, or of the device's own word when that is NULL. */
+int grpo_expired_wait(uint32_t* device_status, pcm_stream stream);
 
 /* Per-kernel-class timing.  While enabled, every launch of the classes below is bracketed by a
  * pair of CUDA events on its stream; pcm_profile_read() synchronises the device, adds up elapsed

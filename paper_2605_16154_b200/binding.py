@@ -184,6 +184,7 @@ _lib.grpo_paged_attention_workspace_bytes.restype = C.c_size_t
 _lib.grpo_paged_attention.argtypes = _KV + [_I, _P, _L, _L, _I, _F, _I, _I, _I, _P, _L, _L, _P, _P, _P, C.c_size_t, _P]
 _lib.grpo_gemm_wait_status.argtypes = [C.c_uint32]
 _lib.grpo_gemm_wait_status.restype = C.c_uint32
+_lib.grpo_expired_wait.argtypes = [_P, _P]
 _lib.pcm_launch_count.restype = C.c_int64
 _lib.pcm_first_use_on_device.argtypes = [C.POINTER(C.c_uint64), C.c_int32]
 _lib.pcm_first_use_on_device.restype = C.c_int32
@@ -193,7 +194,8 @@ for _name in ("pcm_create", "pcm_destroy", "pcm_poll_status", "pcm_state_export"
               "pcm_score_phases", "pcm_update_keep_probs", "pcm_sample_chunks", "grpo_pack_chunks",
               "grpo_actor_fwd_bwd", "grpo_gemm", "grpo_attention", "pcm_profile_enable", "pcm_profile_read",
               "grpo_embed", "grpo_embed_bwd", "grpo_token_logp", "grpo_token_logp_bwd", "grpo_head_logp",
-              "grpo_head_logp_bwd", "grpo_rotary_freqs", "grpo_rotary", "grpo_rotary_cache", "grpo_paged_attention"):
+              "grpo_head_logp_bwd", "grpo_rotary_freqs", "grpo_rotary", "grpo_rotary_cache", "grpo_paged_attention",
+              "grpo_expired_wait"):
     getattr(_lib, _name).restype = C.c_int
 
 EXPORTED = ("pcm_create", "pcm_destroy", "pcm_poll_status", "pcm_state_export", "pcm_state_import",
@@ -205,7 +207,7 @@ EXPORTED = ("pcm_create", "pcm_destroy", "pcm_poll_status", "pcm_state_export", 
             "grpo_actor_fwd_bwd_lora", "grpo_embed", "grpo_embed_workspace_bytes", "grpo_embed_bwd", "grpo_token_logp",
             "grpo_token_logp_bwd", "grpo_head_logp_workspace_bytes", "grpo_head_logp", "grpo_head_logp_bwd_workspace_bytes",
             "grpo_head_logp_bwd", "grpo_gemm_wait_status", "grpo_rotary_freqs", "grpo_rotary", "grpo_rotary_cache",
-            "grpo_paged_attention_workspace_bytes", "grpo_paged_attention")
+            "grpo_paged_attention_workspace_bytes", "grpo_paged_attention", "grpo_expired_wait")
 
 
 def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
@@ -941,6 +943,11 @@ def grpo_attention_wait_status() -> int:
 
 def grpo_gemm_wait_status(next: int = 0) -> int:
     return int(_lib.grpo_gemm_wait_status(next))
+
+
+def grpo_expired_wait(status: Optional[torch.Tensor] = None) -> None:
+    """A kernel whose bounded wait expires, on the current device: into `status` (int32 [1]) or the device's own word."""
+    _check("grpo_expired_wait", _lib.grpo_expired_wait(_ptr(status), _stream()))
 
 
 def pcm_launch_count() -> int:

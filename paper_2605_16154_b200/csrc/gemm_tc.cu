@@ -1555,6 +1555,23 @@ unsigned tcgen05_exchange_status(unsigned next) {
   return cudaMemcpyToSymbol(g_tc_status, &next, sizeof(next)) == cudaSuccess ? h : ~0u;
 }
 
+// The current device's word itself, for kernels elsewhere whose calls bring none of their own; null when it cannot be found.
+unsigned* tcgen05_status_word() {
+  static std::atomic<unsigned*> known[64];
+  int dev = -1;
+  if (cudaGetDevice(&dev) != cudaSuccess) return nullptr;
+  const bool cached = dev >= 0 && dev < 64;
+  if (cached)
+    if (unsigned* w = known[dev].load(std::memory_order_relaxed)) return w;
+  void* w = nullptr;
+  if (cudaGetSymbolAddress(&w, g_tc_status) != cudaSuccess) {
+    cudaGetLastError();
+    return nullptr;
+  }
+  if (cached) known[dev].store((unsigned*)w, std::memory_order_relaxed);
+  return (unsigned*)w;
+}
+
 int attention_tc_poll_status();
 
 int tcgen05_poll_status() {

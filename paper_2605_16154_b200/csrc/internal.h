@@ -113,6 +113,8 @@ size_t chain_part_bytes();
 bool gemm_epilogue_supported(const GemmArgs& g);
 // Reads and clears the tensor-core kernels' device status word (synchronous copy).
 int tcgen05_poll_status();
+// The word of the current device that it reads, or null: where a call without a status word reports its expired waits.
+unsigned* tcgen05_status_word();
 
 // grad[tok[i]] += coef[i] rows[i] in fp32 for rows [n][d] (bf16, 16-byte aligned, d a multiple of 8), tokens outside
 // [0, vocab) left out, in two steps with one scratch (256-byte aligned): the sort, which needs the tokens alone, and the

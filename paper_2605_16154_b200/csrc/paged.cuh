@@ -27,12 +27,15 @@ struct KvView {
   const int* q_off;
   int n_seq, n_rows;
   int max_len;                                 // tokens that a row of the table can hold
-  unsigned* status;
+  unsigned* status;                            // pages and lengths that do not fit; may be null
+  unsigned* waits;                             // expired waits: the call's own word, or the device's (kernels that wait)
 };
 
 __device__ __forceinline__ void kv_report(const KvView& c, unsigned bit) {
   if (c.status) atomicOr(c.status, bit);
 }
+
+__device__ __forceinline__ void kv_report_expired(const KvView& c) { atomicOr(c.waits, STATUS_TIMEOUT); }
 
 struct SeqSpan { int row0, fresh, len; };      // first row and number of new tokens, tokens in all
 

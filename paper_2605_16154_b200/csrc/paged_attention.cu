@@ -588,6 +588,14 @@ static CallPlan plan_call(int dtype, int dh, int n_seq, int n_rows, int group, i
   return c;
 }
 
+// A wait for a barrier that nothing arrives at, reported as the kernels above report theirs.
+__global__ void expired_wait_kernel(KvView c) {
+  __shared__ uint64_t never;
+  mbar_init(&never, 1);
+  fence_mbar_init();
+  if (!mbar_wait_bounded(&never, 0, 1000000ull)) kv_report_expired(c);
+}
+
 }  // namespace pga
 }  // namespace pcm
 
@@ -628,6 +636,7 @@ extern "C" int grpo_paged_attention(const grpo_kv_cache* cache, const grpo_kv_ba
     return PCM_ERR_WORKSPACE;
   AttnParams p = {};
   p.c = kv_view(cache, batch, n_rows, device_status);
+  if (!p.c.waits && !(p.c.waits = tcgen05_status_word())) return PCM_ERR_CUDA;      // (left for the next call that polls)
   p.q = q; p.ld_q = n_rows > 1 ? ld_q : 0; p.ld_q_head = n_heads > 1 ? ld_q_head : 0;
   p.out = out; p.ld_out = n_rows > 1 ? ld_out : 0; p.ld_out_head = n_heads > 1 ? ld_out_head : 0;
   p.lse = lse;
@@ -665,4 +674,14 @@ extern "C" int grpo_paged_attention(const grpo_kv_cache* cache, const grpo_kv_ba
   if (rc == PCM_OK) rc = bf16 ? launch_join_as<__nv_bfloat16>(lines, call.n, dh, s) : launch_join_as<float>(lines, call.n, dh, s);
   prof_end(s, 0.0, 0.0);
   return rc;
+}
+
+extern "C" int grpo_expired_wait(uint32_t* device_status, pcm_stream stream) {
+  if ((uintptr_t)device_status & 3) return PCM_ERR_ARG;
+  KvView c = {};
+  c.waits = device_status ? device_status : tcgen05_status_word();
+  if (!c.waits) return PCM_ERR_CUDA;
+  expired_wait_kernel<<<1, 1, 0, (cudaStream_t)stream>>>(c);
+  PCM_LAUNCH_CHECK();
+  return PCM_OK;
 }

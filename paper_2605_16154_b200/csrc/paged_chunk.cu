@@ -163,7 +163,7 @@ __device__ __forceinline__ bool ch_wait(uint64_t* bar, unsigned parity, volatile
     if (*gave_up) return false;
     if (global_timer_ns() - from > CH_WAIT_NS) {
       *gave_up = 1;
-      kv_report(c, STATUS_TIMEOUT);
+      kv_report_expired(c);
       return false;
     }
   }

@@ -175,7 +175,7 @@ __global__ void __launch_bounds__(RB_THREADS, 2) attn_rows_bf16_kernel(const __g
         const int st = taken % C::STAGES;
         ok = __all_sync(0xffffffffu, mbar_wait_bounded(&full[warp][st], (taken / C::STAGES) & 1u, RB_WAIT_NS));
         if (!ok) {                             // (the copies have not landed: the block's results are not meaningful)
-          kv_report(p.c, STATUS_TIMEOUT);
+          kv_report_expired(p.c);
           break;
         }
         ++taken;

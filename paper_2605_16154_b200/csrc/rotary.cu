@@ -248,6 +248,7 @@ KvView kv_view(const grpo_kv_cache* c, const grpo_kv_batch* b, int32_t n_rows, u
   const long long hold = (long long)b->max_pages * c->page_size, most = PCM_MAX_VOCAB_CALL;
   v.max_len = (int)(hold < most ? hold : most);
   v.status = status;
+  v.waits = status;
   return v;
 }
 

@@ -92,6 +92,61 @@ def test_calls_of_a_new_thread():
     assert not failed
 
 
+def test_an_expired_wait_is_reported_with_and_without_a_status_word():
+    """With a word it is that call's alone; without one the next call that polls has it."""
+    b = B()
+    x, w = torch.zeros(128, 64, device="cuda").bfloat16(), torch.zeros(256, 64, device="cuda").bfloat16()
+    assert b.grpo_gemm_wait_status(0) == 0
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    b.grpo_expired_wait(status)
+    assert int(status) == 1 and b.grpo_gemm_wait_status(0) == 0
+    b.grpo_expired_wait()
+    with pytest.raises(b.PcmError) as e:
+        b.grpo_gemm(x, True, w, True, 128, 256, 64)
+    assert e.value.code == -5
+    b.grpo_gemm(x, True, w, True, 128, 256, 64)
+    c = Case(101, "bf16", 64, 1, 2, 16, [300], [200])              # calls that wait for nothing in vain report nothing, with a word and without
+    for new in (200, 1):
+        c.q_off[1] = new
+        c.run()
+        c.run(status=None)
+    assert int(c.status) == 0 and b.grpo_gemm_wait_status(0) == 0
+
+
+_CAPTURED_FIRST = """
+import torch
+from paper_2605_16154_b200 import binding as B
+g = torch.Generator(device="cuda").manual_seed(1)
+k, v = (torch.randn(40, 16, 2, 64, generator=g, device="cuda").bfloat16() for _ in range(2))
+table = torch.arange(40, dtype=torch.int32, device="cuda").view(2, 20)
+seq_len = torch.tensor([300, 280], dtype=torch.int32, device="cuda")
+new = NEW
+q = torch.randn(2 * new, 4, 64, generator=g, device="cuda").bfloat16()
+q_off = torch.tensor([0, new, 2 * new], dtype=torch.int32, device="cuda")
+room = torch.empty(B.grpo_paged_attention_workspace_bytes(k, 2, 2 * new, 4, new) + 256, dtype=torch.uint8, device="cuda")
+out, lse = torch.zeros_like(q), torch.zeros(2 * new, 4, device="cuda")
+call = lambda: B.grpo_paged_attention(q, k, v, table, seq_len, q_off, max_new=new, out=out, lse=lse, workspace=room)
+graph = torch.cuda.CUDAGraph()
+torch.cuda.synchronize()
+with torch.cuda.graph(graph):
+    call()
+graph.replay()
+torch.cuda.synchronize()
+got, got_lse = out.clone(), lse.clone()
+call()
+torch.cuda.synchronize()
+assert torch.equal(got, out) and torch.equal(got_lse, lse) and bool((out != 0).any())
+print("captured first ok")
+"""
+
+
+@pytest.mark.parametrize("new", [1, 150])
+def test_a_process_whose_first_call_is_captured(new):
+    res = subprocess.run([sys.executable, "-c", _CAPTURED_FIRST.replace("NEW", str(new))], cwd=ROOT, env=dict(os.environ, PYTHONPATH=ROOT),
+                         capture_output=True, text=True, timeout=300)
+    assert res.returncode == 0 and "captured first ok" in res.stdout, res.stdout[-2000:] + res.stderr[-2000:]
+
+
 _FIRST_CALLS = """
 import threading
 import torch

@@ -227,6 +227,8 @@ __device__ __forceinline__ bool ch_any(const ChRange& r) { return r.a > r.t0 || 
 struct ChBars {
   uint64_t full[10], empty[10];                // tiles of the ring
   uint64_t landed;                             // a tile that is cleaned before it is handed on
+  int filled[10];                              // what the tiles wait for should the block give up: 1 + the last ring position ..
+  int cleaning;                                // .. and 1 + the phase of `landed`, 0: nothing
   uint64_t q_full[2], s_full[2], p_half[2], p_full[2], o_full[2], done[2];
   uint32_t tmem;
   unsigned gave_up;
@@ -256,6 +258,8 @@ attn_chunk_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
     mbar_init(&b.landed, 1);
     for (int s = 0; s < 2; ++s) { mbar_init(&b.q_full[s], 4); mbar_init(&b.s_full[s], 1); mbar_init(&b.p_half[s], 4); mbar_init(&b.p_full[s], 4); mbar_init(&b.o_full[s], 1); mbar_init(&b.done[s], 1); }
     b.gave_up = 0;
+    b.cleaning = 0;
+    for (int i = 0; i < C::STAGES; ++i) b.filled[i] = 0;
     for (int i = 0; i < 4; ++i) b.turn[i] = 0;
     b.redo = 0;
     fence_mbar_init();
@@ -287,7 +291,6 @@ attn_chunk_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
       unsigned landed_phase = 0;
       bool ok = true;
       int base_at = 0;                         // ring position of a piece's first keys
-      unsigned asked = 0, lap = 0;             // stages that this warp has filled, and the parity of the last time
       // The page and slot of box `lane` of tile i.  Boxes that the unit does not see lie behind the last page.
       auto look_up = [&](int i, int& page, int& slot) {
         const int key = ch_key(c.u, i) + lane * box_rows;
@@ -311,7 +314,11 @@ attn_chunk_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
           const int key0 = ch_key(c.u, t0 + i);
           const bool clean = values && key0 + CH_TILE > c.sp.len;
           uint64_t* bar = clean ? &b.landed : &b.full[st];
-          if (me) mbar_expect_tx(bar, C::TILE_BYTES);
+          if (me) {
+            if (clean) b.cleaning = 1 + (int)landed_phase;
+            else b.filled[st] = at + 1;
+            mbar_expect_tx(bar, C::TILE_BYTES);
+          }
           __syncwarp();
           for (int k = 0; k < boxes; ++k) {
             const int page_k = __shfl_sync(0xffffffffu, page, k), slot_k = __shfl_sync(0xffffffffu, slot, k);
@@ -319,8 +326,6 @@ attn_chunk_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
             for (int slab = 0; slab < C::SLABS; ++slab)
               ch_load_4d(me, dst + slab * C::SLAB + k * box_rows * 128, tm, slab * 64, c.head, slot_k, page_k, bar);
           }
-          asked |= 1u << st;
-          lap = (lap & ~(1u << st)) | ((unsigned)(at / C::STAGES) & 1u) << st;
           if (i + 1 < n) look_up(t0 + i + 1, page, slot);
           if (clean) {
             if (!__all_sync(0xffffffffu, ch_wait(&b.landed, landed_phase, gave_up, p.c))) { ok = false; break; }
@@ -332,17 +337,17 @@ attn_chunk_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
             }
             ch_fence_async();
             __syncwarp();
-            if (me) mbar_arrive(&b.full[st]);
+            if (me) {
+              b.cleaning = 0;
+              b.filled[st] = at + 1;
+              mbar_arrive(&b.full[st]);
+            }
           }
         }
         base_at += 2 * n;
         left -= n;
         if (left > 0) c.next_unit(p);
       }
-      // Nothing may land after the block is gone.  The products wait for every tile; where the block gives up, this does.
-      if (!ok)
-        for (int st = 0; st < C::STAGES; ++st)
-          if (asked >> st & 1u) mbar_wait_bounded(&b.full[st], lap >> st & 1u, CH_WAIT_NS / 8);
     } else {
       // ---------------------------- products of one stream ----------------------------
       const int s = warp == 8 ? 0 : 1, me = ch_elect();
@@ -722,6 +727,12 @@ attn_chunk_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
+  // Nothing may land after the block is gone.  The products wait for every tile; where any warp has given up, this one does.
+  if (warp == 9 && *gave_up) {
+    for (int st = 0; st < C::STAGES; ++st)
+      if (b.filled[st] > 0) mbar_wait_bounded(&b.full[st], (unsigned)((b.filled[st] - 1) / C::STAGES) & 1u, CH_WAIT_NS / 8);
+    if (b.cleaning > 0) mbar_wait_bounded(&b.landed, (unsigned)(b.cleaning - 1), CH_WAIT_NS / 8);
+  }
   if (tid == 0) p.redo[blockIdx.x] = b.redo;
   if (warp == 8) tmem_dealloc(tmem, CH_TMEM);
 }

@@ -525,7 +525,8 @@ typedef struct {
  * q [n_rows][n_heads][head_dim], k and v [n_rows][n_kv_heads][head_dim] of the cache's type, with row and head strides each
  * (views of one fused projection, say); q_out likewise, or q itself.  Rotation as grpo_rotary (INTERLEAVED in flags), at
  * the token's position, or at pos[row] where pos is not NULL; rot_dim = 0 rotates nothing (turns is not read).
- * q = NULL with n_heads = 0: keys and values only.  Slots that two tokens share hold either one's values. */
+ * q = NULL with n_heads = 0: keys and values only.  Slots that two tokens share hold either one's values.  A cache whose strides
+ * make slots overlap, or whose k and v are one array, is refused (PCM_ERR_ARG; grpo_paged_attention, which only reads, takes it). */
 int grpo_rotary_cache(const grpo_kv_cache* cache, const grpo_kv_batch* batch, int32_t n_rows, const void* q, int64_t ld_q,
                       int64_t ld_q_head, int32_t n_heads, const void* k, int64_t ld_k, int64_t ld_k_head, const void* v, int64_t ld_v,
                       int64_t ld_v_head, int32_t rot_dim, const double* turns, float amplitude, const int32_t* pos, uint32_t flags,

@@ -306,6 +306,21 @@ extern "C" int grpo_rotary(int32_t dtype, const void* x, int64_t ld_x, int64_t l
   return rc;
 }
 
+// Whether the slots of a cache that is written share elements: each stride, from the least on, has to span what lies within it.
+static bool slots_overlap(const grpo_kv_cache* c) {
+  struct Dim { int64_t ld, n; } d[3] = {{c->ld_head, c->n_kv_heads}, {c->ld_slot, c->page_size}, {c->ld_page, c->n_pages}};
+  for (int i = 0; i < 2; ++i)
+    for (int j = 0; j < 2 - i; ++j)
+      if (d[j].ld > d[j + 1].ld) { const Dim t = d[j]; d[j] = d[j + 1]; d[j + 1] = t; }
+  __int128 span = c->head_dim;
+  for (const Dim& x : d) {
+    if (x.n == 1) continue;                    // leads nowhere
+    if (x.ld < span) return true;
+    span += (__int128)x.ld * (x.n - 1);
+  }
+  return c->k == c->v;
+}
+
 extern "C" int grpo_rotary_cache(const grpo_kv_cache* cache, const grpo_kv_batch* batch, int32_t n_rows, const void* q, int64_t ld_q,
                                  int64_t ld_q_head, int32_t n_heads, const void* k, int64_t ld_k, int64_t ld_k_head, const void* v,
                                  int64_t ld_v, int64_t ld_v_head, int32_t rot_dim, const double* turns, float amplitude,
@@ -317,6 +332,7 @@ extern "C" int grpo_rotary_cache(const grpo_kv_cache* cache, const grpo_kv_batch
   if (n_heads < 0 || rot_dim < 0 || !std::isfinite(amplitude) || (flags & ~GRPO_ROTARY_INTERLEAVED)) return PCM_ERR_ARG;
   if (dim > PCM_MAX_ROTARY_DIM || rot_dim % 2 || rot_dim > dim || n_heads > (1 << 16) || n_kv > (1 << 16)) return PCM_ERR_SHAPE;
   if (n_rows == 0 || batch->n_seq == 0) return PCM_OK;
+  if (slots_overlap(cache)) return PCM_ERR_ARG;
   if (!k || !v || (rot_dim > 0 && !turns) || (n_heads > 0 && (!q || !q_out))) return PCM_ERR_ARG;
   const uintptr_t low = elem_bytes(cache->dtype) - 1;
   if (((uintptr_t)k | (uintptr_t)v | (n_heads ? (uintptr_t)q | (uintptr_t)q_out : 0)) & low) return PCM_ERR_ARG;

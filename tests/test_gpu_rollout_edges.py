@@ -147,6 +147,36 @@ def test_a_process_whose_first_call_is_captured(new):
     assert res.returncode == 0 and "captured first ok" in res.stdout, res.stdout[-2000:] + res.stderr[-2000:]
 
 
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("layout", ["pages", "heads first", "slots outside", "heads outside", "beside one another", "page by page", "one page", "one head"])
+def test_layouts_of_a_cache_that_are_written(kind, layout):
+    """The order of pages, slots and heads in memory is free, and keys and values may lie between one another."""
+    t, n, page, kv, dim = TYPES[kind], 1 if layout == "one page" else 6, 16, 1 if layout == "one head" else 2, 32
+    make = lambda *shape: torch.full(shape, 3.0, dtype=t, device="cuda")
+    if layout == "beside one another":
+        k, v = make(n, page, kv, 2, dim).unbind(3)
+    elif layout == "page by page":
+        k, v = make(n, 2, page, kv, dim).unbind(1)
+    elif layout == "heads first":
+        k, v = (make(n, kv, page, dim).transpose(1, 2) for _ in range(2))
+    elif layout == "slots outside":
+        k, v = (make(page, n, kv, dim + 8).transpose(0, 1)[..., :dim] for _ in range(2))
+    elif layout == "heads outside":
+        k, v = (make(kv, n, page, dim).permute(1, 2, 0, 3) for _ in range(2))
+    else:
+        k, v = (make(n, page, kv, dim) for _ in range(2))
+    g = gen(103)
+    new = min(40, n * page - 3)
+    kn, vn = (torch.randn(new, kv, dim, generator=g, device="cuda").to(t) for _ in range(2))
+    table = torch.randperm(n, generator=g, device="cuda").to(torch.int32)[None]
+    at = torch.arange(3, new + 3, device="cuda")
+    want_k, want_v = k.clone(), v.clone()
+    want_k[table[0].long()[at // page], at % page], want_v[table[0].long()[at // page], at % page] = kn, vn
+    B().grpo_rotary_cache(None, kn, vn, k, v, table, torch.tensor([new + 3], dtype=torch.int32, device="cuda"),
+                          torch.tensor([0, new], dtype=torch.int32, device="cuda"), None)
+    assert torch.equal(k, want_k) and torch.equal(v, want_v)
+
+
 _FIRST_CALLS = """
 import threading
 import torch

@@ -177,3 +177,10 @@ def test_structs_have_the_header_s_layout():
     assert ctypes.sizeof(B.grpo_rotary_cfg) == 8 + 5 * 8
     assert ctypes.sizeof(B.grpo_kv_cache) == 6 * 4 + 2 * 8 + 3 * 8
     assert ctypes.sizeof(B.grpo_kv_batch) == 8 + 4 * 8
+
+
+@pytest.mark.parametrize("cache", [dict(ld_slot=64, ld_head=64), dict(ld_head=64, ld_slot=96), dict(ld_page=64), dict(ld_page=16 * 128 - 64), dict(v=P),
+                                   dict(ld_head=16 * 64 - 8, ld_slot=64), dict(n_kv_heads=1, ld_page=512, ld_slot=64),
+                                   dict(ld_page=1 << 61, ld_slot=1 << 62, ld_head=64)])
+def test_a_cache_whose_slots_overlap_is_not_written(cache):
+    assert _call("grpo_rotary_cache", cache=cache, **(dict(ld_k=64, ld_v=64) if "n_kv_heads" in cache else {})) == ARG

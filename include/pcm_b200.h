@@ -460,7 +460,9 @@ int grpo_head_logp_bwd(const void* x, int64_t ld_x, int32_t n_rows, int32_t d, c
  * and values read as zeros and are not written; bit 7 (value 128) a length or row offset that does not fit the sizes of the
  * call.  A length below 0 counts as 0.  Of a length beyond what the table can hold, grpo_rotary_cache stores the new tokens whose
  * places the table has and leaves out the others (no stored token is overwritten), and grpo_paged_attention takes what the table
- * holds for the whole sequence.  A sequence whose offsets do not fit has no rows. */
+ * holds for the whole sequence.  A sequence whose offsets do not fit has no rows; where offsets do not ascend,
+ * grpo_rotary_cache may leave out rows of other sequences too.  A length below the number of a sequence's rows is no error: the
+ * first rows stand ahead of its first token, are not stored, and attend to nothing. */
 enum { GRPO_ROTARY_PLAIN = 0, GRPO_ROTARY_LINEAR = 1, GRPO_ROTARY_BASE = 2, GRPO_ROTARY_PARTS = 3 };
 #define GRPO_ROTARY_INTERLEAVED 1u  /* pairs (2 i, 2 i + 1); otherwise (i, i + rot_dim / 2)                                */
 #define GRPO_ROTARY_INVERSE 2u      /* the opposite rotation: the gradient (grpo_rotary only)                              */

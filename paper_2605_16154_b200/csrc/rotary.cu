@@ -76,7 +76,7 @@ __global__ void __launch_bounds__(RT_THREADS, 8) rotary_kernel(const __grid_cons
       if (s < 0) {
         slot = -2;
       } else {
-        const SeqSpan sp = seq_span(p.cache, s, true);
+        const SeqSpan sp = seq_span(p.cache, s, false);
         if (row >= sp.row0 && row < sp.row0 + sp.fresh) {
           // from the length as it was given: counted back from a clipped one new tokens would land on stored ones
           const int j = max(p.cache.seq_len[s], 0) - sp.fresh + (row - sp.row0);
@@ -97,6 +97,9 @@ __global__ void __launch_bounds__(RT_THREADS, 8) rotary_kernel(const __grid_cons
     row_pos[threadIdx.x] = t;
     row_slot[threadIdx.x] = slot;
   }
+  if (p.to_cache && p.cache.status)            // every sequence's sizes are looked at once, by the warps that have no row to place
+    for (long long s = (long long)blockIdx.x * RT_THREADS + RT_THREADS - 1 - threadIdx.x; s < p.cache.n_seq; s += (long long)gridDim.x * RT_THREADS)
+      seq_span(p.cache, (int)s, true);
   double turns = (int)threadIdx.x < n_here * p.half ? p.turns[threadIdx.x % p.half] : 0.0;      // on its way with the row's place
   __syncthreads();
   for (int i = threadIdx.x; i < n_here * p.half; i += RT_THREADS) {

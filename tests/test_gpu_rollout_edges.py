@@ -56,6 +56,22 @@ def test_a_length_beyond_the_table_overwrites_no_stored_token(kind, length):
     assert int(c.status) == 128
 
 
+@pytest.mark.parametrize("seq_len,q_off", [([40, -1], [0, 10, 10]), ([40, 1 << 20], [0, 10, 10]), ([40, 40], [0, 10, 4]), ([40, 40], [0, 4, 11]),
+                                           ([40, 40], [-1, 4, 10])])
+def test_both_calls_report_lengths_and_offsets_that_do_not_fit(seq_len, q_off):
+    """.. of sequences without rows too."""
+    c = Case(97, "bf16", 64, 2, 2, 16, [40, 40], [5, 5])
+    c.table = torch.arange(6, dtype=torch.int32, device="cuda").view(2, 3)
+    c.seq_len.copy_(torch.tensor(seq_len, dtype=torch.int32))
+    c.q_off.copy_(torch.tensor(q_off, dtype=torch.int32))
+    kv = torch.ones(10, 2, 64, dtype=c.t, device="cuda")
+    c.run()
+    assert int(c.status) == 128
+    c.status.zero_()
+    B().grpo_rotary_cache(c.q, kv, kv, c.k_pages, c.v_pages, c.table, c.seq_len, c.q_off, None, status=c.status)
+    assert int(c.status) == 128
+
+
 def test_calls_of_a_new_thread():
     """The first GPU work of a thread is the call itself: nothing else has made a context current there."""
     import threading

@@ -796,7 +796,9 @@ def _cache(call: str, k_pages: torch.Tensor, v_pages: torch.Tensor):
     dev = k_pages.device
     ok = k_pages.is_cuda and k_pages.dim() == 4 and v_pages.device == dev and v_pages.dtype == k_pages.dtype
     dt = _DTYPES.get(k_pages.dtype)
-    if not ok or dt is None or v_pages.shape != k_pages.shape or v_pages.stride() != k_pages.stride():
+    if not ok or dt is None or v_pages.shape != k_pages.shape:
+        raise PcmError(call, -1)
+    if v_pages.stride() != k_pages.stride() and any(a != b and size > 1 for a, b, size in zip(v_pages.stride(), k_pages.stride(), k_pages.shape)):
         raise PcmError(call, -1)
     (n, page, kv, d), (ld_page, ld_slot, ld_head, step) = k_pages.shape, k_pages.stride()
     if step != 1 and d > 1:

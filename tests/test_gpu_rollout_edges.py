@@ -72,6 +72,28 @@ def test_both_calls_report_lengths_and_offsets_that_do_not_fit(seq_len, q_off):
     assert int(c.status) == 128
 
 
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("n_pages,kv", [(1, 2), (4, 1), (1, 1)])
+def test_strides_that_lead_nowhere_may_differ(kind, n_pages, kv):
+    """A cache of one page or one head: the strides of k and v in that dimension mean nothing."""
+    g, t = gen(98), TYPES[kind]
+    k, v = (torch.randn(n_pages, 16, kv, 64, generator=g, device="cuda").to(t) for _ in range(2))
+    table = torch.arange(n_pages, dtype=torch.int32, device="cuda")[None]
+    seq_len, q = torch.tensor([n_pages * 16], dtype=torch.int32, device="cuda"), torch.randn(1, 4, 64, generator=g, device="cuda").to(t)
+    want, lse = B().grpo_paged_attention(q, k, v, table, seq_len)
+    strides = list(v.stride())
+    for i, n in ((0, n_pages), (2, kv)):
+        if n == 1:
+            strides[i] = 24
+    other = v.as_strided(v.shape, strides)
+    got, lse2 = B().grpo_paged_attention(q, k, other, table, seq_len)
+    assert torch.equal(got, want) and torch.equal(lse2, lse)
+    got, lse2 = B().grpo_paged_attention(q, k.as_strided(k.shape, strides), v, table, seq_len)
+    assert torch.equal(got, want) and torch.equal(lse2, lse)
+    with pytest.raises(B().PcmError):                              # the slots' strides do lead somewhere
+        B().grpo_paged_attention(q, k, torch.zeros(n_pages, 16, kv, 128, dtype=t, device="cuda")[..., :64], table, seq_len)
+
+
 def test_calls_of_a_new_thread():
     """The first GPU work of a thread is the call itself: nothing else has made a context current there."""
     import threading

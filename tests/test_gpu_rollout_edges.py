@@ -33,6 +33,24 @@ def test_a_reference_moves_in_a_warp_with_fewer_rows_too(dim):
 
 
 @pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("new,length", [(3, 60), (3, 20000), (130, 230), (130, 20000)])
+@pytest.mark.parametrize("key", ["first", "late"])
+def test_a_score_of_infinity_makes_the_rows_that_see_it_nan(kind, new, length, key):
+    """.. in units of one piece and in units that are cut, as the first key and as one of the chunk's own; other rows and heads keep their bits."""
+    c = Case(93, kind, 64, 2, 2, 16, [length, 90], [new, 1])
+    c.q[..., 0] = 1.0
+    clean, lse = c.run()
+    assert bool(torch.isfinite(clean).all())
+    j = 0 if key == "first" else length - (new + 1) // 2
+    c.k_pages[c.table_host[0][j // 16], j % 16, 0, 0] = float("inf")
+    out, lse2 = c.run()
+    first = max(0, j - (length - new))                             # rows from here on see it
+    assert bool(torch.isnan(out[first:new, :2]).all()) and bool(torch.isnan(lse2[first:new, :2]).all())
+    out[first:new, :2], lse2[first:new, :2] = clean[first:new, :2], lse[first:new, :2]
+    assert torch.equal(out, clean) and torch.equal(lse2, lse)
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
 @pytest.mark.parametrize("length", [67, 68, 200, 2 ** 31 - 1])
 def test_a_length_beyond_the_table_overwrites_no_stored_token(kind, length):
     """64 slots, all of them taken; new tokens whose places lie behind the table are not stored, and nothing else moves."""

@@ -34,8 +34,11 @@ namespace pga {
 constexpr int CH_ROWS = 128, CH_TILE = 128, CH_THREADS = 384;
 constexpr unsigned long long CH_WAIT_NS = 2000000000ull;
 constexpr int CH_TMEM = 512;
-constexpr int CH_TURNS = 8;                    // tiles of a piece from which on its streams take turns (8 x 1024 tokens behind 4096 to 8192: 379 us,
-                                               // 398 without; prefixes of two tiles: 249 us without, 294 with)
+// Tiles of a piece from which on its streams take turns at head dim 128, whose products keep the tensor core as busy as the exponential
+// unit (8 x 1024 tokens, 16/4 heads, the last of 128 x 16 keys: 158 us, 166 without; x 32: 302, 319; x 96: 962, 1014; below 12 tiles
+// the same; two tiles: 5 % more).  At head dim 64 the exponential unit sets the pace and turns cost 6 to 15 % (x 16: 139 us, 122
+// without; x 32: 259, 225; x 96: 756, 641).
+constexpr int CH_TURNS = 8;
 constexpr int CH_TURN_TRIES = 1 << 12;
 constexpr float CH_RISE = 32.f;                // powers of two by which a maximum may outgrow its reference
 constexpr float CH_WILD = 100.f;               // .. within one tile: 128 weights of 2^100 still have a sum
@@ -480,7 +483,7 @@ attn_chunk_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
       const ChRange range = sight.of(half, t0, t1);
       const int pos = row_place(p, c.sp, c.qt, c.head, half * CH_ROWS + row).pos;
       const int w_lo = __shfl_sync(0xffffffffu, pos, 0), w_hi = __reduce_max_sync(0xffffffffu, pos);
-      const bool turns = range.e - range.b >= CH_TURNS;
+      const bool turns = DH == 128 && range.e - range.b >= CH_TURNS;
       const long long rest = left - (t1 - t0);
       bool asked = false;
       if constexpr (C::QBUFS == 2) {           // the next unit's queries come in while this one's scores are formed

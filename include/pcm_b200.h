@@ -539,7 +539,9 @@ int grpo_rotary_cache(const grpo_kv_cache* cache, const grpo_kv_batch* batch, in
  * over the tokens j of the row's sequence with j <= p and (window = 0 or j > p - window or j < sinks), p the row's position;
  * head h reads key-value head h / (n_heads / n_kv_heads).  A row that sees nothing has out 0 and lse -inf.  Keys and values
  * that a row does not see have no influence on it, NaN and infinities included (such values in the slots of later tokens cost
- * time: the rows that they could reach are formed once more).  A row that sees a score of NaN or +inf is NaN, and so is its lse.
+ * time: the rows that they could reach are formed once more, key by key; so are rows of many-token calls in bf16 whose scores rise by
+ * more than 70, scaled, within 128 keys: a call of such rows only takes some hundred times as long).  A row that sees a score
+ * of NaN or +inf is NaN, and so is its lse.
  * q and out [n_rows][n_heads][head_dim] of the cache's type with row and head strides, on 16-byte boundaries like the cache;
  * lse fp32 [n_rows][n_heads] contiguous, may be NULL.  head_dim 32, 64 or 128.  scale > 0.  out overlaps neither q nor the cache.
  * max_new: no sequence brings more new tokens than this (0: not known); it chooses among kernels and sizes the workspace, and

@@ -554,10 +554,13 @@ static bool attn_sizes_ok(const grpo_kv_cache* c, int64_t n_seq, int64_t n_rows,
   return n_rows * (n_heads / c->n_kv_heads) <= PCM_MAX_VOCAB_CALL;              // rows of a key-value head are counted in 32 bits
 }
 
-// Rows of a key-value head (new tokens times group) up to which a sequence goes to the kernel for few rows.  bf16: two row
-// tiles at head dim 64 (24 rows of 40 sequences over a window of 1024: 31 us, 45 in the kernel for many), one at 128, whose
-// registers hold no more (24 rows of 16 sequences of 8000: 55 us, 44 in the other).  Head dim 32 has the one kernel.
-// fp32: 37 sequences of up to 120 rows took 43 us, 74 to 80 in the kernel for many.
+// Rows of a key-value head (new tokens times group) up to which a sequence goes to the kernel for few rows; one head each below.
+// bf16, two row tiles at head dim 64 (300, 2000 and 8000 tokens of 256, 40 and 16 sequences, 32 rows: 89, 38 and 50 us, 104, 46 and 61
+// in the kernel for many; 48 rows: 149, 57 and 75 against 110, 48 and 63), one at 128, whose registers hold no more (16 rows: 94, 46
+// and 63 us against 124, 55 and 68; 24 rows: 161, 69 and 89 against 124, 55 and 67).  Head dim 32 has the one kernel.
+// fp32: where sequences of few and of many rows meet, a border of 16 takes a launch of either kernel after the other (37 sequences of
+// up to 120 rows: 41 us, 72 with it); batches of one size between 17 and 128 rows would be better off with it (40 sequences of 300
+// tokens, 32 rows of head dim 64: 61 us, 51; 128 rows: 159, 79).
 static int few_rows_of(int dtype, int dh) { return dtype == GRPO_F32 ? 128 : dh == 128 ? 16 : 32; }
 
 // The lines of a call: which kernels take part, with what workers; n_lines and their regions of the workspace.
@@ -607,9 +610,8 @@ extern "C" size_t grpo_paged_attention_workspace_bytes(const grpo_kv_cache* cach
   if (!attn_sizes_ok(cache, n_seq, n_rows, n_heads) || max_new < 0) return 0;
   // as large as any smaller call's: few rows alone, or few and many
   const int group = n_heads / cache->n_kv_heads;
-  CallPlan c = plan_call(cache->dtype, cache->head_dim, n_seq, n_rows, group, max_new);
-  size_t total = c.total;
-  total = layout(n_seq, 2 * sm_count(), cache->dtype == GRPO_F32 ? RF_ROWS : 32, cache->head_dim).total;
+  const CallPlan c = plan_call(cache->dtype, cache->head_dim, n_seq, n_rows, group, max_new);
+  size_t total = layout(n_seq, 2 * sm_count(), cache->dtype == GRPO_F32 ? RF_ROWS : 32, cache->head_dim).total;
   if (c.chunk[c.n - 1]) total += c.at[c.n - 1].total;
   return total;
 }
@@ -672,7 +674,7 @@ extern "C" int grpo_paged_attention(const grpo_kv_cache* cache, const grpo_kv_ba
     else rc = call.chunk[i] ? launch_chunk_bf16(a, dh, s) : launch_rows_bf16(a, dh, s);
   }
   if (rc == PCM_OK) rc = bf16 ? launch_join_as<__nv_bfloat16>(lines, call.n, dh, s) : launch_join_as<float>(lines, call.n, dh, s);
-  prof_end(s, 0.0, 0.0);
+  prof_end(s, 0.0, 0.0);                       // (bytes and products follow from lengths that only the device knows)
   return rc;
 }
 

@@ -8,8 +8,9 @@
 // 128 rows nearly empty, and the products take a fraction of the time of the loads), and keeps its own running maximum, sum
 // and values.  The warps' sums meet at the unit's end.  The weights enter the product with v
 // as a pair of bf16 values, high and low part, so that they are not rounded: the second product hides behind the loads too.
-// A step of 256 sequences of 500 to 8192 tokens, 16/4 heads of 128, takes 257 us (5.9 TB/s), of two of 131072, 32/8 heads, 162 us; one of
-// 300 tokens 12 us, which are launches, dependent reads (lengths, table, keys) and the join.
+// A step of 256 sequences of 500 to 8192 tokens, 16/4 heads of 128, takes 252 us (6.0 TB/s), of two of 131072, 32/8 heads, 158 us, of 256 of
+// 300 tokens, 16 heads of 64, 90 us (3.5 TB/s: units of three tiles); one of 300 tokens
+// 12 us, which are launches, dependent reads (lengths, table, keys) and the join.
 #include <cuda.h>
 
 #include "async_ptx.cuh"

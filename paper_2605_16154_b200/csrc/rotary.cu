@@ -5,8 +5,9 @@
 // turns of t f carry no information and would cost fp32 all of its digits at far positions, so t f is formed and reduced to
 // [-1/2, 1/2] in 64 bits (error below 2^-22 turns at t = 2^31) and only the rest goes through sincospif.  All heads of a row share its
 // angles: a block forms the sines and cosines of its rows once in shared memory, then streams the rows through them, each
-// element read and written once: bound by HBM (119808 rows of 16 heads of 64 in bf16: 78 us, 6.3 TB/s; 98304 new tokens of 16/8 heads
-// into a cache: 129 us, 6.2 TB/s; a step of 64 tokens: 6 us, which are dependent reads of offsets, lengths and table).
+// element read and written once: bound by HBM (119808 rows of 16 heads of 64 in bf16: 80 us, 6.1 TB/s, in fp32 150 us; 98304 new tokens of
+// 16/8 heads into a cache: 130 us, 6.2 TB/s, in fp32 246 us; heads whose turning halves are no multiple of 16 bytes go by the element:
+// 119808 x 16 x 96 in bf16 with 24 turning 721 us, 154 with 48; a step of 64 tokens: 6 us, which are dependent reads of offsets, lengths and table).
 #include <cmath>
 
 #include "paged.cuh"

@@ -38,8 +38,8 @@ constexpr int CH_ROWS = 128, CH_TILE = 128, CH_THREADS = 384;
 constexpr unsigned long long CH_WAIT_NS = 2000000000ull;
 constexpr int CH_TMEM = 512;
 // Tiles of a piece from which on its streams take turns at head dim 128, whose products keep the tensor core as busy as the exponential
-// unit (8 x 1024 tokens, 16/4 heads, the last of 128 x 16 keys: 158 us, 166 without; x 32: 302, 319; x 96: 962, 1014; below 12 tiles
-// the same; two tiles: 5 % more).  At head dim 64 the exponential unit sets the pace and turns cost 6 to 15 % (x 16: 139 us, 122
+// unit (8 x 1024 tokens, 16/4 heads, the last of 128 x 16 keys: 158 us, 166 without; x 32: 302, 319; x 96: 962, 1014; 37 x 16 heads of 256
+// tokens, x 24: 319, 322; below 12 tiles the same; two tiles: 4 % more).  At head dim 64 the exponential unit sets the pace and turns cost 6 to 15 % (x 16: 139 us, 122
 // without; x 32: 259, 225; x 96: 756, 641).
 constexpr int CH_TURNS = 8;
 constexpr int CH_TURN_TRIES = 1 << 12;
